@@ -186,8 +186,8 @@ def _eight(v):
     w = w.view(m, blocks, BLOCK)
     mant, e = torch.frexp(w.abs().amax(2, keepdim=True))  # amax = mant 2^e, mant in [0.5, 1)
     e = torch.clamp_min(torch.where(mant >= 127.5 / 128, e + 1, e) - 7, -126)
-    q = torch.round(torch.ldexp(w, -e))  # to even at a tie, as everywhere
-    return torch.ldexp(q, e).view(m, -1)[:, :n]
+    step = ((e + 127) << 23).view(torch.float32)  # 2^e from its bits: powers computed on the GPU need not be exact
+    return (torch.round(w / step) * step).view(m, -1)[:, :n]  # to even at a tie, as everywhere
 
 
 def _dense_grads(s, x, z):
@@ -327,10 +327,11 @@ def _held8(v):
     n = v.shape[1]
     w = torch.nn.functional.pad(v, (0, -n % BLOCK)).unflatten(1, (-1, BLOCK))
     top = w.abs().amax(2, keepdim=True)
-    e = torch.floor(torch.log2(torch.clamp_min(top, 2.0 ** -200))) - 6
-    e = torch.where(torch.round(top / torch.exp2(e)) > 127, e + 1, e)
-    e = torch.where(torch.round(top / torch.exp2(e - 1)) <= 127, e - 1, e)  # log2 may be one off at a power of two
-    step = torch.exp2(torch.clamp_min(e, -126.0))
+    power = lambda e: ((e + 1023) << 52).view(torch.float64)  # noqa: E731  2^e exactly
+    e = torch.floor(torch.log2(torch.clamp_min(top, 2.0 ** -200))).long() - 6
+    e = torch.where(torch.round(top / power(e)) > 127, e + 1, e)
+    e = torch.where(torch.round(top / power(e - 1)) <= 127, e - 1, e)  # log2 may be one off at a power of two
+    step = power(torch.clamp_min(e, -126))
     return (torch.round(w / step) * step).flatten(1)[:, :n]
 
 
