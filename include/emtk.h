@@ -383,6 +383,143 @@ EMTK_API emtk_status emtk_batcher_stats(emtk_batcher *b, int64_t *batches, int64
 EMTK_API emtk_status emtk_batcher_destroy(emtk_batcher *b);
 
 /* ------------------------------------------------------------------------
+ * Dense layers, gated feed-forward blocks and 8-bit checkpoints.
+ *
+ * Layers for networks that a user trains and serves beside the CNN (a student
+ * of its scores on the patches of emtk_extract_patches, for instance): the
+ * matrix product with bias, activation and residual, the two projections of a
+ * gated block with their activation and product, both with their gradients,
+ * and activations kept in 8 bits between the two passes.  The paper has no
+ * counterpart (its one network is emtk_infer's).
+ *
+ *   - Matrices are row-major: element (i, j) is d[i * ld + j], ld >= columns,
+ *     ld in elements, any ld and any element-aligned address.  Weights are
+ *     [out][in].  m rows (hits, tokens), k inputs, n (or f) outputs, each
+ *     0 .. 2^31 - 1; m = 0 makes the weights' gradients 0 and k = 0 leaves
+ *     the bias.
+ *   - Operands are bf16 or fp16 (one type per call); products are summed in
+ *     fp32 on the tensor cores, and everything up to the stored value is fp32
+ *     but for the products of a backward call with an activation: those take
+ *     dz (dg, du) rounded to the operand type.  Every output is rounded once.
+ *   - Outputs must not overlap inputs or each other, except that y may be the
+ *     residual itself (same address, same ld).
+ *   - A layer handle (emtk_nn) holds the device workspace of its calls.  It
+ *     grows to the largest call it has served (a cudaMalloc, after waiting
+ *     for `stream`): reserve enough in emtk_nn_create to capture calls into a
+ *     graph.  Like a context, a handle is used from one stream at a time.
+ * -------------------------------------------------------------------- */
+typedef struct emtk_nn emtk_nn;
+
+/* Element types.  An argument struct's `type` is BF16 or F16. */
+typedef enum { EMTK_TYPE_BF16 = 0, EMTK_TYPE_F16 = 1, EMTK_TYPE_F32 = 2 } emtk_type;
+
+/* Activations: z, max(z, 0), z Phi(z) (Phi: the normal distribution
+ * function), z / (1 + exp(-z)), 1 / (1 + exp(-z)).  The slope of the second
+ * at 0 is 0. */
+typedef enum {
+    EMTK_ACT_NONE = 0,
+    EMTK_ACT_RELU = 1,
+    EMTK_ACT_GELU = 2,
+    EMTK_ACT_SILU = 3,
+    EMTK_ACT_SIGMOID = 4
+} emtk_act;
+
+/* A matrix argument.  d_scale == NULL: elements of the call's type.
+ * Otherwise an 8-bit checkpoint: d holds int8 codes (ld in bytes) and
+ * d_scale[i * ld_scale + j / 32] the scale of row i's columns 32 (j / 32) ..:
+ *   value(i, j) = code * 2^(scale - 127),
+ * where scale is the least (but at least 1) for which the largest finite
+ * magnitude of the 32 values, divided by 2^(scale - 127), rounds to at most
+ * 127; codes round to nearest, ties to even.  Code -128 stands for a value
+ * that was not finite and reads as NaN.  The values are exact in bf16, so the
+ * products of a backward call take them unrounded; as fp16 they round to
+ * nearest and saturate at +-65504. */
+typedef struct {
+    void *d;
+    int64_t ld;
+    uint8_t *d_scale;
+    int64_t ld_scale;
+} emtk_matrix;
+
+/* Creates a layer handle on CUDA device `device` with `workspace_bytes`
+ * reserved (0: none yet).  wait_timeout_ns (> 0) limits every device-side
+ * wait; debug_stall = 1 (a test knob, else 0) makes the tensor-core kernels
+ * wait for a barrier nothing arrives at, so that the wait runs out and
+ * emtk_nn_check reports EMTK_ERR_TIMEOUT.  EMTK_ERR_UNSUPPORTED on a device
+ * other than compute capability 10.3.  *out is NULL on failure. */
+EMTK_API emtk_status emtk_nn_create(int device, int64_t workspace_bytes, int64_t wait_timeout_ns, int32_t debug_stall,
+                                    emtk_nn **out);
+
+/* Frees the handle (synchronises its device first).  NULL is accepted. */
+EMTK_API emtk_status emtk_nn_destroy(emtk_nn *nn);
+
+/* As emtk_check, for a layer handle. */
+EMTK_API emtk_status emtk_nn_check(emtk_nn *nn, emtk_stream stream);
+
+/* y = act(z) + residual with z = x w^T + bias.
+ *   x [m][k], w [n][k], y [m][n]; bias [n] of the call's type or F32
+ *   (bias_type) or NULL; residual [m][n] or d == NULL; pre [m][n] receives z
+ *   for emtk_dense_backward, in the call's type or as an 8-bit checkpoint, or
+ *   d == NULL. */
+typedef struct {
+    int32_t m, n, k;
+    int32_t act, type, bias_type;
+    emtk_matrix x, w, y, residual, pre;
+    const void *bias;
+} emtk_dense_args;
+EMTK_API emtk_status emtk_dense(emtk_nn *nn, const emtk_dense_args *args, emtk_stream stream);
+
+/* Gradients of emtk_dense from dy [m][n]:
+ *   dz = dy * act'(pre);  dx = dz w [m][k];  dw = dz^T x [n][k], of the
+ *   call's type or F32 (dw_type);  db = sum over rows of dz [n], fp32.
+ * Any of dx, dw, db may be absent (NULL); w is needed for dx, x for dw, pre
+ * for an activation.  x and pre may be 8-bit checkpoints.  The residual's
+ * gradient is dy itself. */
+typedef struct {
+    int32_t m, n, k;
+    int32_t act, type, dw_type;
+    emtk_matrix dy, x, w, pre, dx, dw;
+    float *db;
+} emtk_dense_grad_args;
+EMTK_API emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *args, emtk_stream stream);
+
+/* The first half of a gated feed-forward block, in one kernel:
+ *   h = act(g) * u [m][f] with g = x w_gate^T + bias_gate, u = x w_up^T + bias_up;
+ *   w_gate, w_up [f][k]; both biases or neither.  gate and up receive g and u
+ *   for emtk_gated_backward (the call's type or 8-bit checkpoints), or
+ *   d == NULL for both.  The second half is emtk_dense with a residual. */
+typedef struct {
+    int32_t m, f, k;
+    int32_t act, type, bias_type;
+    emtk_matrix x, w_gate, w_up, h, gate, up;
+    const void *bias_gate, *bias_up;
+} emtk_gated_args;
+EMTK_API emtk_status emtk_gated(emtk_nn *nn, const emtk_gated_args *args, emtk_stream stream);
+
+/* Gradients of emtk_gated from dh [m][f], with the g and u it kept:
+ *   dg = dh * u * act'(g);  du = dh * act(g);
+ *   dx = dg w_gate + du w_up;  dw_gate = dg^T x;  dw_up = du^T x;
+ *   db_gate, db_up = their sums over rows, fp32.
+ * h [m][f] receives act(g) * u once more, so that the forward pass need not
+ * keep it for the second half's gradients.  Every output may be absent;
+ * dw_gate goes with dw_up and db_gate with db_up.  x, gate and up may be
+ * 8-bit checkpoints (gate and up alike). */
+typedef struct {
+    int32_t m, f, k;
+    int32_t act, type, dw_type;
+    emtk_matrix dh, gate, up, x, w_gate, w_up, dx, dw_gate, dw_up, h;
+    float *db_gate, *db_up;
+} emtk_gated_grad_args;
+EMTK_API emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *args, emtk_stream stream);
+
+/* x [m][k] of `type` into the 8-bit checkpoint q, and the values that q
+ * stands for into x. */
+EMTK_API emtk_status emtk_pack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type type, const emtk_matrix *x,
+                                const emtk_matrix *q, emtk_stream stream);
+EMTK_API emtk_status emtk_unpack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type type, const emtk_matrix *q,
+                                  const emtk_matrix *x, emtk_stream stream);
+
+/* ------------------------------------------------------------------------
  * Test hooks: host-side fault injection.  They make the failures a service
  * must survive (an exhausted device, a dispatcher that stops making progress)
  * happen on the host, with no fault on the GPU.  Not for production use.

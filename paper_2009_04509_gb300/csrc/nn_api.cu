@@ -1,0 +1,412 @@
+// C ABI of the dense layers, gated blocks and 8-bit checkpoints
+// (include/emtk.h): argument checks, workspace and the launches of each call.
+#include <nvtx3/nvToolsExt.h>
+
+#include <algorithm>
+#include <new>
+
+#include "emtk_internal.h"
+#include "nn_internal.h"
+
+using namespace emtk;
+
+namespace {
+
+struct DeviceGuard {  // restores the caller's current device
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int dev) {
+        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
+        ok = prev == dev || cudaSetDevice(dev) == cudaSuccess;
+        if (prev == dev) prev = -1;
+    }
+    ~DeviceGuard() {
+        if (prev >= 0) cudaSetDevice(prev);
+    }
+};
+
+struct Range {  // NVTX range on the host thread
+    explicit Range(const char *name) { nvtxRangePushA(name); }
+    ~Range() { nvtxRangePop(); }
+};
+
+emtk_status status_of(cudaError_t e) {
+    if (e == cudaSuccess) return EMTK_OK;
+    return e == cudaErrorMemoryAllocation ? EMTK_ERR_OOM : EMTK_ERR_CUDA;
+}
+
+bool type16(int t) { return t == EMTK_TYPE_BF16 || t == EMTK_TYPE_F16; }
+bool act_known(int a) { return a >= EMTK_ACT_NONE && a <= EMTK_ACT_SIGMOID; }
+bool sizes_ok(int32_t a, int32_t b, int32_t c) { return a >= 0 && b >= 0 && c >= 0; }
+size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
+
+// Collects the first argument error of a call.
+struct Checks {
+    emtk_status st = EMTK_OK;
+    void fail(emtk_status s) {
+        if (st == EMTK_OK) st = s;
+    }
+    void need(bool ok) {
+        if (!ok) fail(EMTK_ERR_ARG);
+    }
+    // A matrix of rows x cols elements of elem bytes; q8: a checkpoint is allowed too.
+    void matrix(const emtk_matrix &m, int64_t rows, int64_t cols, bool required, bool q8, size_t elem = 2) {
+        if (m.d_scale && !q8) return fail(EMTK_ERR_ARG);
+        if (!m.d) {
+            if (m.d_scale || (required && rows > 0 && cols > 0)) fail(EMTK_ERR_ARG);
+            return;
+        }
+        if (m.ld < cols) return fail(EMTK_ERR_ARG);
+        if (m.d_scale) {
+            if (m.ld_scale < (cols + kQ8Block - 1) / kQ8Block) fail(EMTK_ERR_ARG);
+            return;
+        }
+        if (reinterpret_cast<uintptr_t>(m.d) % elem) fail(EMTK_ERR_ALIGN);
+    }
+    void vector(const void *p, size_t elem) {
+        if (reinterpret_cast<uintptr_t>(p) % elem) fail(EMTK_ERR_ALIGN);
+    }
+};
+
+// Workspace of one call, laid out front to back: a first pass adds up the
+// sizes, ensure() makes room, a second pass hands out the addresses.
+struct CallSpace {
+    emtk_nn *nn;
+    size_t used = 0;
+    bool dry = true;
+    void *take(size_t bytes) {
+        void *p = dry ? nullptr : static_cast<uint8_t *>(nn->ws) + used;
+        used += align_up(bytes);
+        return p;
+    }
+    emtk_status ensure(cudaStream_t s) {
+        dry = false;
+        const size_t bytes = used;
+        used = 0;
+        if (bytes <= nn->ws_bytes) return EMTK_OK;
+        cudaError_t e = cudaStreamSynchronize(s);  // earlier calls may still use the old one
+        if (e != cudaSuccess) return status_of(e);
+        e = dev_free(nn->ws);
+        nn->ws = nullptr;
+        nn->ws_bytes = 0;
+        if (e == cudaSuccess) e = dev_alloc(&nn->ws, bytes + bytes / 4);
+        if (e != cudaSuccess) return status_of(e);
+        nn->ws_bytes = bytes + bytes / 4;
+        return EMTK_OK;
+    }
+};
+
+int64_t ld16(int64_t cols) { return (cols + 7) / 8 * 8; }  // rows of 16-byte multiples
+
+MmOperand rows_of(const emtk_matrix &m) { return {m.d, m.ld, false}; }
+MmOperand cols_of(const emtk_matrix &m) { return {m.d, m.ld, true}; }
+
+}  // namespace
+
+extern "C" {
+
+emtk_status emtk_nn_create(int device, int64_t workspace_bytes, int64_t wait_timeout_ns, int32_t debug_stall,
+                           emtk_nn **out) {
+    if (out) *out = nullptr;
+    if (!out || device < 0 || workspace_bytes < 0 || wait_timeout_ns <= 0 || (debug_stall != 0 && debug_stall != 1))
+        return EMTK_ERR_ARG;
+    int ndev = 0;
+    if (cudaGetDeviceCount(&ndev) != cudaSuccess || device >= ndev) return EMTK_ERR_CUDA;
+    DeviceGuard g(device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    cudaDeviceProp prop;
+    if (cudaGetDeviceProperties(&prop, device) != cudaSuccess) return EMTK_ERR_CUDA;
+    if (!(prop.major == 10 && prop.minor == 3)) return EMTK_ERR_UNSUPPORTED;  // built for sm_103a only
+    emtk_nn *nn = new (std::nothrow) emtk_nn;
+    if (!nn) return EMTK_ERR_OOM;
+    nn->device = device;
+    nn->sm_count = prop.multiProcessorCount;
+    nn->timeout_ns = wait_timeout_ns;
+    nn->debug_stall = debug_stall;
+    void *status = nullptr;
+    cudaError_t e = dev_alloc(&status, sizeof(int));
+    nn->status = static_cast<int *>(status);
+    if (e == cudaSuccess) e = cudaMemset(nn->status, 0, sizeof(int));
+    if (e == cudaSuccess && workspace_bytes > 0) {
+        e = dev_alloc(&nn->ws, (size_t)workspace_bytes);
+        if (e == cudaSuccess) nn->ws_bytes = (size_t)workspace_bytes;
+    }
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) {
+        emtk_nn_destroy(nn);
+        return status_of(e);
+    }
+    *out = nn;
+    return EMTK_OK;
+}
+
+emtk_status emtk_nn_destroy(emtk_nn *nn) {
+    if (!nn) return EMTK_OK;
+    DeviceGuard g(nn->device);
+    cudaError_t e = cudaDeviceSynchronize();
+    dev_free(nn->ws);
+    dev_free(nn->status);
+    delete nn;
+    return e == cudaSuccess ? EMTK_OK : EMTK_ERR_CUDA;
+}
+
+emtk_status emtk_nn_check(emtk_nn *nn, emtk_stream stream) {
+    if (!nn) return EMTK_ERR_ARG;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    if (cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess) return EMTK_ERR_CUDA;
+    int status = 0;
+    if (cudaMemcpy(&status, nn->status, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return EMTK_ERR_CUDA;
+    if (status == 0) return EMTK_OK;
+    return cudaMemset(nn->status, 0, sizeof(int)) == cudaSuccess ? EMTK_ERR_TIMEOUT : EMTK_ERR_CUDA;
+}
+
+emtk_status emtk_dense(emtk_nn *nn, const emtk_dense_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_dense_args &a = *p;
+    Checks c;
+    c.need(sizes_ok(a.m, a.n, a.k) && act_known(a.act) && type16(a.type));
+    if (a.bias) c.need(a.bias_type == a.type || a.bias_type == EMTK_TYPE_F32);
+    if (c.st != EMTK_OK) return c.st;
+    c.matrix(a.x, a.m, a.k, true, false);
+    c.matrix(a.w, a.n, a.k, true, false);
+    c.matrix(a.y, a.m, a.n, true, false);
+    c.matrix(a.residual, a.m, a.n, false, false);
+    c.matrix(a.pre, a.m, a.n, false, true);
+    c.vector(a.bias, a.bias_type == EMTK_TYPE_F32 ? 4 : 2);
+    if (c.st != EMTK_OK || a.m == 0 || a.n == 0) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk dense");
+    MmJob j{};
+    j.kind = kMmSum;
+    j.type = (emtk_type)a.type;
+    j.M = a.m;
+    j.N = a.n;
+    j.K = a.k;
+    j.terms = 1;
+    j.a[0] = rows_of(a.x);
+    j.b[0] = rows_of(a.w);
+    j.epi.act = a.act;
+    j.epi.bias[0] = a.bias;
+    j.epi.bias_f32 = a.bias_type == EMTK_TYPE_F32;
+    j.epi.residual = a.residual;
+    j.epi.out = a.y;
+    j.epi.saved[0] = a.pre;
+    return status_of(launch_mm(j, nn, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_dense_grad_args &a = *p;
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    Checks c;
+    c.need(sizes_ok(a.m, a.n, a.k) && act_known(a.act) && type16(a.type));
+    if (a.dw.d) c.need(a.dw_type == a.type || a.dw_type == EMTK_TYPE_F32);
+    if (c.st != EMTK_OK) return c.st;
+    c.matrix(a.dy, a.m, a.n, true, false);
+    c.matrix(a.x, a.m, a.k, a.dw.d != nullptr, true);
+    c.matrix(a.w, a.n, a.k, a.dx.d != nullptr, false);
+    c.matrix(a.pre, a.m, a.n, a.act != EMTK_ACT_NONE, true);
+    c.matrix(a.dx, a.m, a.k, false, false);
+    c.matrix(a.dw, a.n, a.k, false, false, a.dw_type == EMTK_TYPE_F32 ? 4 : 2);
+    c.vector(a.db, 4);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk dense backward");
+    const emtk_type type = (emtk_type)a.type;
+    const bool dx = a.dx.d && a.m > 0 && a.k > 0, dw = a.dw.d && a.n > 0 && a.k > 0;
+    const bool own_dz = a.act != EMTK_ACT_NONE && (dx || dw);
+    const bool x8 = a.x.d_scale && dw;
+    CallSpace ws{nn};
+    emtk_matrix dz = a.dy, x = a.x;
+    float *partial = nullptr;
+    for (int pass = 0; pass < 2; ++pass) {
+        if (own_dz) dz = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.n)), ld16(a.n), nullptr, 0};
+        if (x8) x = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.k)), ld16(a.k), nullptr, 0};
+        if (a.db) partial = static_cast<float *>(ws.take(4 * (size_t)slope_slices(a.m, a.n, nn->sm_count) * a.n));
+        if (pass == 0) {
+            const emtk_status st = ws.ensure(s);
+            if (st != EMTK_OK) return st;
+        }
+    }
+    cudaError_t e = cudaSuccess;
+    if (own_dz || a.db)
+        e = launch_slope(type, a.act, a.m, a.n, a.dy, a.pre, own_dz ? dz.d : nullptr, dz.ld, a.db, partial,
+                         nn->sm_count, s);
+    if (e == cudaSuccess && x8) e = launch_unpack8(type, a.m, a.k, a.x, x, nn->sm_count, s);
+    MmJob j{};
+    j.kind = kMmSum;
+    j.type = type;
+    j.terms = 1;
+    if (e == cudaSuccess && dx) {
+        j.M = a.m;
+        j.N = a.k;
+        j.K = a.n;
+        j.a[0] = rows_of(dz);
+        j.b[0] = cols_of(a.w);
+        j.epi.out = a.dx;
+        e = launch_mm(j, nn, s);
+    }
+    if (e == cudaSuccess && dw) {
+        j.M = a.n;
+        j.N = a.k;
+        j.K = a.m;
+        j.a[0] = cols_of(dz);
+        j.b[0] = cols_of(x);
+        j.epi.out = a.dw;
+        j.epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
+        e = launch_mm(j, nn, s);
+    }
+    return status_of(e);
+}
+
+emtk_status emtk_gated(emtk_nn *nn, const emtk_gated_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_gated_args &a = *p;
+    Checks c;
+    c.need(sizes_ok(a.m, a.f, a.k) && act_known(a.act) && type16(a.type));
+    c.need((a.bias_gate == nullptr) == (a.bias_up == nullptr) && (a.gate.d == nullptr) == (a.up.d == nullptr));
+    if (a.bias_gate) c.need(a.bias_type == a.type || a.bias_type == EMTK_TYPE_F32);
+    if (c.st != EMTK_OK) return c.st;
+    c.matrix(a.x, a.m, a.k, true, false);
+    c.matrix(a.w_gate, a.f, a.k, true, false);
+    c.matrix(a.w_up, a.f, a.k, true, false);
+    c.matrix(a.h, a.m, a.f, true, false);
+    c.matrix(a.gate, a.m, a.f, false, true);
+    c.matrix(a.up, a.m, a.f, false, true);
+    for (const void *b : {a.bias_gate, a.bias_up}) c.vector(b, a.bias_type == EMTK_TYPE_F32 ? 4 : 2);
+    if (c.st != EMTK_OK || a.m == 0 || a.f == 0) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk gated");
+    MmJob j{};
+    j.kind = kMmGated;
+    j.type = (emtk_type)a.type;
+    j.M = a.m;
+    j.N = a.f;
+    j.K = a.k;
+    j.terms = 1;
+    j.a[0] = rows_of(a.x);
+    j.b[0] = rows_of(a.w_gate);
+    j.b[1] = rows_of(a.w_up);
+    j.epi.act = a.act;
+    j.epi.bias[0] = a.bias_gate;
+    j.epi.bias[1] = a.bias_up;
+    j.epi.bias_f32 = a.bias_type == EMTK_TYPE_F32;
+    j.epi.out = a.h;
+    j.epi.saved[0] = a.gate;
+    j.epi.saved[1] = a.up;
+    return status_of(launch_mm(j, nn, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_gated_grad_args &a = *p;
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    Checks c;
+    c.need(sizes_ok(a.m, a.f, a.k) && act_known(a.act) && type16(a.type));
+    c.need((a.dw_gate.d == nullptr) == (a.dw_up.d == nullptr) && (a.db_gate == nullptr) == (a.db_up == nullptr));
+    c.need((a.gate.d_scale == nullptr) == (a.up.d_scale == nullptr));
+    if (a.dw_gate.d) c.need(a.dw_type == a.type || a.dw_type == EMTK_TYPE_F32);
+    if (c.st != EMTK_OK) return c.st;
+    const size_t dw_elem = a.dw_type == EMTK_TYPE_F32 ? 4 : 2;
+    c.matrix(a.dh, a.m, a.f, true, false);
+    c.matrix(a.gate, a.m, a.f, true, true);
+    c.matrix(a.up, a.m, a.f, true, true);
+    c.matrix(a.x, a.m, a.k, a.dw_gate.d != nullptr, true);
+    c.matrix(a.w_gate, a.f, a.k, a.dx.d != nullptr, false);
+    c.matrix(a.w_up, a.f, a.k, a.dx.d != nullptr, false);
+    c.matrix(a.dx, a.m, a.k, false, false);
+    c.matrix(a.dw_gate, a.f, a.k, false, false, dw_elem);
+    c.matrix(a.dw_up, a.f, a.k, false, false, dw_elem);
+    c.matrix(a.h, a.m, a.f, false, false);
+    c.vector(a.db_gate, 4);
+    c.vector(a.db_up, 4);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk gated backward");
+    const emtk_type type = (emtk_type)a.type;
+    const bool dx = a.dx.d && a.m > 0 && a.k > 0, dw = a.dw_gate.d && a.f > 0 && a.k > 0;
+    const bool x8 = a.x.d_scale && dw;
+    CallSpace ws{nn};
+    emtk_matrix dg{}, du{}, x = a.x;
+    float *partial = nullptr;
+    for (int pass = 0; pass < 2; ++pass) {
+        if (dx || dw) {
+            dg = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.f)), ld16(a.f), nullptr, 0};
+            du = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.f)), ld16(a.f), nullptr, 0};
+        }
+        if (x8) x = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.k)), ld16(a.k), nullptr, 0};
+        if (a.db_gate)
+            partial = static_cast<float *>(ws.take(8 * (size_t)slope_slices(a.m, a.f, nn->sm_count) * a.f));
+        if (pass == 0) {
+            const emtk_status st = ws.ensure(s);
+            if (st != EMTK_OK) return st;
+        }
+    }
+    cudaError_t e = cudaSuccess;
+    if (dx || dw || a.db_gate || a.h.d)
+        e = launch_gated_slope(type, a.act, a.m, a.f, a.dh, a.gate, a.up, dg.d, du.d, ld16(a.f), a.h, a.db_gate,
+                               a.db_up, partial, nn->sm_count, s);
+    if (e == cudaSuccess && x8) e = launch_unpack8(type, a.m, a.k, a.x, x, nn->sm_count, s);
+    MmJob j{};
+    j.kind = kMmSum;
+    j.type = type;
+    if (e == cudaSuccess && dx) {
+        j.terms = 2;
+        j.M = a.m;
+        j.N = a.k;
+        j.K = a.f;
+        j.a[0] = rows_of(dg);
+        j.a[1] = rows_of(du);
+        j.b[0] = cols_of(a.w_gate);
+        j.b[1] = cols_of(a.w_up);
+        j.epi.out = a.dx;
+        e = launch_mm(j, nn, s);
+    }
+    j.epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
+    for (int w = 0; w < 2 && e == cudaSuccess && dw; ++w) {
+        j.terms = 1;
+        j.M = a.f;
+        j.N = a.k;
+        j.K = a.m;
+        j.a[0] = cols_of(w ? du : dg);
+        j.b[0] = cols_of(x);
+        j.epi.out = w ? a.dw_up : a.dw_gate;
+        e = launch_mm(j, nn, s);
+    }
+    return status_of(e);
+}
+
+emtk_status emtk_pack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type type, const emtk_matrix *x, const emtk_matrix *q,
+                       emtk_stream stream) {
+    if (!nn || !x || !q || !sizes_ok(m, k, 0) || !type16(type)) return EMTK_ERR_ARG;
+    Checks c;
+    c.matrix(*x, m, k, true, false);
+    c.matrix(*q, m, k, true, true);
+    if (m > 0 && k > 0) c.need(q->d_scale != nullptr);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk pack8");
+    return status_of(launch_pack8(type, m, k, *x, *q, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_unpack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type type, const emtk_matrix *q, const emtk_matrix *x,
+                         emtk_stream stream) {
+    if (!nn || !x || !q || !sizes_ok(m, k, 0) || !type16(type)) return EMTK_ERR_ARG;
+    Checks c;
+    c.matrix(*x, m, k, true, false);
+    c.matrix(*q, m, k, true, true);
+    if (m > 0 && k > 0) c.need(q->d_scale != nullptr);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk unpack8");
+    return status_of(launch_unpack8(type, m, k, *q, *x, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"

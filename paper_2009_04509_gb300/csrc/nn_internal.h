@@ -1,0 +1,75 @@
+// Declarations shared by the dense / gated / checkpoint layers' files
+// (nn_api.cu, nn_mm.cu, nn_pointwise.cu).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/emtk.h"
+
+struct emtk_nn {
+    int device = 0;
+    int sm_count = 0;
+    int64_t timeout_ns = 0;
+    int debug_stall = 0;
+    int *status = nullptr;   // device status word, as a context's
+    void *ws = nullptr;      // workspace of the running call
+    size_t ws_bytes = 0;
+};
+
+namespace emtk {
+
+constexpr int kQ8Block = 32;  // columns that share a checkpoint scale
+
+// Operand of a matrix product: element (i, t) of the contraction t is
+// p[i * ld + t], or p[t * ld + i] if `across` (i runs along memory).
+struct MmOperand {
+    const void *p;
+    int64_t ld;
+    bool across;
+};
+
+// What becomes of the sums.
+//   plain: z = sum + bias[0]; out = act(z) + residual; saved[0] = z
+//   gated: g = sum0 + bias[0], u = sum1 + bias[1]; out = act(g) u;
+//          saved[0] = g, saved[1] = u
+// Absent parts have null pointers.  out is fp32 if out_f32.
+struct MmEpilogue {
+    int act;
+    int bias_f32;
+    int out_f32;
+    const void *bias[2];
+    emtk_matrix residual, out, saved[2];
+};
+
+// out[M][N] from the contraction over K of a[i] and b[i] (rows M and N):
+//   kMmSum:   a[0] b[0]^T (+ a[1] b[1]^T if terms == 2)
+//   kMmGated: sum0 = a[0] b[0]^T and sum1 = a[0] b[1]^T, gated epilogue
+// Both operands' types are `type`; sums are fp32.
+enum MmKind { kMmSum = 0, kMmGated = 1 };
+struct MmJob {
+    MmKind kind;
+    emtk_type type;
+    int M, N, K;
+    int terms;
+    MmOperand a[2], b[2];
+    MmEpilogue epi;
+};
+cudaError_t launch_mm(const MmJob &job, const emtk_nn *nn, cudaStream_t s);
+
+// ---- pointwise passes (nn_pointwise.cu)
+// dz = dy act'(pre) as a 16-bit matrix dz (or none), and its column sums db
+// (or null).  partial: fp32 [slope_slices(m, n, sms)][n] scratch when db is wanted.
+int slope_slices(int m, int n, int sms);
+cudaError_t launch_slope(emtk_type type, int act, int m, int n, const emtk_matrix &dy, const emtk_matrix &pre,
+                         void *dz, int64_t dz_ld, float *db, float *partial, int sms, cudaStream_t s);
+// dg, du, h and the column sums of the gated block; partial: twice as large.
+cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk_matrix &dh, const emtk_matrix &gate,
+                               const emtk_matrix &up, void *dg, void *du, int64_t d_ld, const emtk_matrix &h,
+                               float *db_gate, float *db_up, float *partial, int sms, cudaStream_t s);
+cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
+                         cudaStream_t s);
+cudaError_t launch_unpack8(emtk_type type, int m, int k, const emtk_matrix &q, const emtk_matrix &x, int sms,
+                           cudaStream_t s);
+
+}  // namespace emtk

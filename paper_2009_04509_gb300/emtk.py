@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
+from typing import NamedTuple
 
 import numpy as np
 
@@ -20,6 +22,8 @@ EMTK_FP32, EMTK_TF32, EMTK_BF16, EMTK_FP16, EMTK_FP8 = 0, 1, 2, 3, 4
 EMTK_PATCH_F32, EMTK_PATCH_BF16, EMTK_PATCH_F16 = 0, 1, 2
 PRECISIONS = {"fp32": EMTK_FP32, "tf32": EMTK_TF32, "bf16": EMTK_BF16, "fp16": EMTK_FP16, "fp8": EMTK_FP8}
 PATCH_FORMATS = {"f32": EMTK_PATCH_F32, "bf16": EMTK_PATCH_BF16, "fp16": EMTK_PATCH_F16}
+EMTK_TYPE_BF16, EMTK_TYPE_F16, EMTK_TYPE_F32 = 0, 1, 2
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4}
 KERNELS = ("intervals", "gather", "network", "head", "convert", "hitfind")
 
 EXPORTED = ("emtk_default_options", "emtk_create", "emtk_destroy", "emtk_infer", "emtk_infer_batch",
@@ -27,7 +31,8 @@ EXPORTED = ("emtk_default_options", "emtk_create", "emtk_destroy", "emtk_infer",
             "emtk_status_string", "emtk_extract_patches_static", "emtk_batcher_create", "emtk_batcher_submit",
             "emtk_batcher_wait", "emtk_batcher_stats", "emtk_batcher_destroy", "emtk_get_fp8_scales",
             "emtk_find_hits", "emtk_infer_batch_host", "emtk_debug_fail_alloc", "emtk_debug_alloc_counts",
-            "emtk_debug_batcher_stall")
+            "emtk_debug_batcher_stall", "emtk_nn_create", "emtk_nn_destroy", "emtk_nn_check", "emtk_dense",
+            "emtk_dense_backward", "emtk_gated", "emtk_gated_backward", "emtk_pack8", "emtk_unpack8")
 EMTK_STATIC_SCRATCH_BYTES = 4 << 20
 
 _vp = ctypes.c_void_p
@@ -59,6 +64,25 @@ class emtk_hitfind_request(ctypes.Structure):
     _fields_ = [("d_adc", _vp), ("nwires", ctypes.c_int32), ("nticks", ctypes.c_int32), ("ld", ctypes.c_int64),
                 ("threshold", ctypes.c_float), ("capacity", ctypes.c_int32), ("d_hits", _vp), ("d_info", _vp),
                 ("n_found", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class emtk_matrix(ctypes.Structure):
+    _fields_ = [("d", _vp), ("ld", ctypes.c_int64), ("d_scale", _vp), ("ld_scale", ctypes.c_int64)]
+
+
+def _args_struct(name, ints, matrices, pointers):
+    """An argument struct of the layers: int32 fields, matrices, pointers."""
+    fields = [(f, ctypes.c_int32) for f in ints.split()] + [(f, emtk_matrix) for f in matrices.split()] + \
+        [(f, _vp) for f in pointers.split()]
+    return type(name, (ctypes.Structure,), {"_fields_": fields})
+
+
+emtk_dense_args = _args_struct("emtk_dense_args", "m n k act type bias_type", "x w y residual pre", "bias")
+emtk_dense_grad_args = _args_struct("emtk_dense_grad_args", "m n k act type dw_type", "dy x w pre dx dw", "db")
+emtk_gated_args = _args_struct("emtk_gated_args", "m f k act type bias_type", "x w_gate w_up h gate up",
+                               "bias_gate bias_up")
+emtk_gated_grad_args = _args_struct("emtk_gated_grad_args", "m f k act type dw_type",
+                                    "dh gate up x w_gate w_up dx dw_gate dw_up h", "db_gate db_up")
 
 
 class EmtkError(RuntimeError):
@@ -116,6 +140,17 @@ def load_library(path: str | None = None):
     lib.emtk_debug_batcher_stall.restype = ctypes.c_int
     for name in ("emtk_batcher_create", "emtk_batcher_submit", "emtk_batcher_wait", "emtk_batcher_stats",
                  "emtk_batcher_destroy"):
+        getattr(lib, name).restype = ctypes.c_int
+    lib.emtk_nn_create.argtypes = [ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(_vp)]
+    lib.emtk_nn_destroy.argtypes = [_vp]
+    lib.emtk_nn_check.argtypes = [_vp, _vp]
+    for name in ("emtk_dense", "emtk_dense_backward", "emtk_gated", "emtk_gated_backward"):
+        getattr(lib, name).argtypes = [_vp, ctypes.c_char_p, _vp]  # a packed argument struct
+    for name in ("emtk_pack8", "emtk_unpack8"):
+        getattr(lib, name).argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int, ctypes.c_char_p,
+                                       ctypes.c_char_p, _vp]
+    for name in ("emtk_nn_create", "emtk_nn_destroy", "emtk_nn_check", "emtk_dense", "emtk_dense_backward",
+                 "emtk_gated", "emtk_gated_backward", "emtk_pack8", "emtk_unpack8"):
         getattr(lib, name).restype = ctypes.c_int
     lib.emtk_status_string.argtypes = [ctypes.c_int]
     lib.emtk_status_string.restype = ctypes.c_char_p
@@ -333,6 +368,190 @@ def emtk_batcher_destroy(b) -> None:
     _check(load_library().emtk_batcher_destroy(b), "emtk_batcher_destroy")
     for key in [k for k in _batcher_refs if k[0] == b]:
         del _batcher_refs[key]
+
+
+# ------------------------------------------- dense, gated, 8-bit checkpoints
+class Q8(NamedTuple):
+    """An 8-bit checkpoint of a matrix [m][k] (emtk_matrix in include/emtk.h): int8
+    codes [m][k] and uint8 scales [m][ceil(k / 32)], CUDA tensors with unit column
+    stride.  Where an argument below is a matrix that may be kept in 8 bits, it is
+    either a 16-bit tensor or a Q8."""
+    codes: "object"
+    scales: "object"
+
+
+def emtk_q8_empty(m: int, k: int, device="cuda") -> Q8:
+    """An 8-bit checkpoint's tensors for an [m][k] matrix, contents undefined."""
+    import torch
+    return Q8(torch.empty((m, k), dtype=torch.int8, device=device),
+              torch.empty((m, (k + 31) // 32), dtype=torch.uint8, device=device))
+
+
+# The argument structs of include/emtk.h as bytes: packing one takes a fraction of
+# filling a ctypes.Structure, and a call for one row is short.
+_MATRIX = "QqQq"
+_PACK_MATRIX = struct.Struct("<" + _MATRIX)
+_PACK_DENSE = struct.Struct("<6i" + 5 * _MATRIX + "Q")
+_PACK_DENSE_GRAD = struct.Struct("<6i" + 6 * _MATRIX + "Q")
+_PACK_GATED = struct.Struct("<6i" + 6 * _MATRIX + "2Q")
+_PACK_GATED_GRAD = struct.Struct("<6i" + 10 * _MATRIX + "2Q")
+_ABSENT = (0, 0, 0, 0)
+_TYPES = {}  # torch dtype -> emtk_type
+
+
+def _type_of(t, what: str, f32: bool = False) -> int:
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.bfloat16: EMTK_TYPE_BF16, torch.float16: EMTK_TYPE_F16, torch.float32: EMTK_TYPE_F32})
+    v = _TYPES.get(t.dtype, -1)
+    if v < 0 or (v == EMTK_TYPE_F32 and not f32):
+        raise ValueError(f"{what}: dtype {t.dtype} is not supported")
+    return v
+
+
+def _mat(t, rows: int, cols: int, dtype, what: str) -> tuple:
+    """(d, ld, d_scale, ld_scale) of a [rows][cols] tensor of dtype, or a Q8 where dtype is a
+    (dtype, Q8) pair; absent for None."""
+    if t is None:
+        return _ABSENT
+    if type(dtype) is tuple:
+        if isinstance(t, Q8):
+            import torch
+            d, ld, _, _ = _mat(t.codes, rows, cols, torch.int8, what)
+            s, lds, _, _ = _mat(t.scales, rows, (cols + 31) // 32, torch.uint8, what)
+            return (d, ld, s, lds)
+        dtype = dtype[0]
+    if t.dtype is not dtype:
+        raise ValueError(f"{what}: dtype {t.dtype}, expected {dtype}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(rows, cols)}")
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise ValueError(f"{what}: columns must be contiguous")
+    if ld < cols:
+        if rows > 1:
+            raise ValueError(f"{what}: rows overlap")
+        ld = cols  # one row: its distance to the next says nothing
+    if not t.is_cuda:
+        raise ValueError(f"{what}: not a CUDA tensor")
+    return (t.data_ptr(), ld, 0, 0)
+
+
+def _vec(t, n: int, what: str, dtype=None) -> int:
+    if t is None:
+        return 0
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or not t.is_cuda:
+        raise ValueError(f"{what}: expected a contiguous CUDA vector of {n}")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{what}: dtype {t.dtype}, expected {dtype}")
+    return t.data_ptr()
+
+
+def _act_code(act: str) -> int:
+    if act not in ACTS:
+        raise ValueError(f"act: {act!r} is none of {tuple(ACTS)}")
+    return ACTS[act]
+
+
+def emtk_nn_create(device: int = 0, workspace_bytes: int = 0, wait_timeout_ns: int = 2_000_000_000,
+                   debug_stall: bool = False):
+    """A layer handle (see include/emtk.h), an int."""
+    out = _vp()
+    _check(load_library().emtk_nn_create(int(device), int(workspace_bytes), int(wait_timeout_ns),
+                                         int(bool(debug_stall)), ctypes.byref(out)), "emtk_nn_create")
+    return out.value
+
+
+def emtk_nn_destroy(nn) -> None:
+    _check(load_library().emtk_nn_destroy(nn), "emtk_nn_destroy")
+
+
+def emtk_nn_check(nn, stream=None) -> int:
+    """Returns the status code (does not raise on EMTK_ERR_TIMEOUT)."""
+    return int(load_library().emtk_nn_check(nn, _stream(stream)))
+
+
+def emtk_dense(nn, x, w, y, bias=None, act: str = "none", residual=None, pre=None, stream=None) -> None:
+    """y = act(x w^T + bias) + residual.  x [m][k], w [n][k], y and residual [m][n]: bf16 or fp16 tensors of
+    one dtype, rows any distance apart; bias [n] of that dtype or float32; pre [m][n] (tensor or Q8) receives
+    the activation's input for emtk_dense_backward."""
+    (m, k), n = x.shape, w.shape[0]
+    dt = x.dtype
+    args = _PACK_DENSE.pack(m, n, k, _act_code(act), _type_of(x, "x"),
+                            0 if bias is None else _type_of(bias, "bias", True),
+                            *_mat(x, m, k, dt, "x"), *_mat(w, n, k, dt, "w"), *_mat(y, m, n, dt, "y"),
+                            *_mat(residual, m, n, dt, "residual"), *_mat(pre, m, n, (dt, Q8), "pre"),
+                            _vec(bias, n, "bias"))
+    _check(load_library().emtk_dense(nn, args, _stream(stream)), "emtk_dense")
+
+
+def emtk_dense_backward(nn, dy, x, w, act: str = "none", pre=None, dx=None, dw=None, db=None, stream=None) -> None:
+    """Gradients of emtk_dense from dy [m][n]: dx [m][k], dw [n][k] (x's dtype or float32), db [n] float32,
+    each optional.  x and pre may be Q8; x may be None without dw, w None without dx."""
+    import torch
+    (m, n), dt = dy.shape, dy.dtype
+    like = w if w is not None else dw if dw is not None else x.codes if isinstance(x, Q8) else x
+    k = 0 if like is None else like.shape[1]
+    args = _PACK_DENSE_GRAD.pack(m, n, k, _act_code(act), _type_of(dy, "dy"),
+                                 0 if dw is None else _type_of(dw, "dw", True),
+                                 *_mat(dy, m, n, dt, "dy"), *_mat(x, m, k, (dt, Q8), "x"), *_mat(w, n, k, dt, "w"),
+                                 *_mat(pre, m, n, (dt, Q8), "pre"), *_mat(dx, m, k, dt, "dx"),
+                                 *_mat(dw, n, k, None if dw is None else dw.dtype, "dw"),
+                                 _vec(db, n, "db", torch.float32))
+    _check(load_library().emtk_dense_backward(nn, args, _stream(stream)), "emtk_dense_backward")
+
+
+def emtk_gated(nn, x, w_gate, w_up, h, bias_gate=None, bias_up=None, act: str = "silu", gate=None, up=None,
+               stream=None) -> None:
+    """h = act(x w_gate^T + bias_gate) * (x w_up^T + bias_up): x [m][k], weights [f][k], h [m][f]; gate and up
+    [m][f] (tensors or Q8s) receive the two factors' inputs for emtk_gated_backward."""
+    (m, k), f = x.shape, w_gate.shape[0]
+    dt = x.dtype
+    bias_type = 0 if bias_gate is None else _type_of(bias_gate, "bias_gate", True)
+    if bias_gate is not None and bias_up is not None and bias_gate.dtype is not bias_up.dtype:
+        raise ValueError("bias_up: its dtype must be bias_gate's")
+    args = _PACK_GATED.pack(m, f, k, _act_code(act), _type_of(x, "x"), bias_type,
+                            *_mat(x, m, k, dt, "x"), *_mat(w_gate, f, k, dt, "w_gate"), *_mat(w_up, f, k, dt, "w_up"),
+                            *_mat(h, m, f, dt, "h"), *_mat(gate, m, f, (dt, Q8), "gate"),
+                            *_mat(up, m, f, (dt, Q8), "up"), _vec(bias_gate, f, "bias_gate"),
+                            _vec(bias_up, f, "bias_up"))
+    _check(load_library().emtk_gated(nn, args, _stream(stream)), "emtk_gated")
+
+
+def emtk_gated_backward(nn, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx=None, dw_gate=None, dw_up=None,
+                        db_gate=None, db_up=None, h=None, stream=None) -> None:
+    """Gradients of emtk_gated from dh [m][f] and the gate and up it kept: dx [m][k], dw_gate and dw_up [f][k]
+    (x's dtype or float32), db_gate and db_up [f] float32, and h [m][f] once more; each optional."""
+    import torch
+    (m, f), dt = dh.shape, dh.dtype
+    like = w_gate if w_gate is not None else dw_gate if dw_gate is not None else x.codes if isinstance(x, Q8) else x
+    k = 0 if like is None else like.shape[1]
+    if dw_gate is not None and dw_up is not None and dw_gate.dtype is not dw_up.dtype:
+        raise ValueError("dw_up: its dtype must be dw_gate's")
+    dwt = None if dw_gate is None else dw_gate.dtype
+    args = _PACK_GATED_GRAD.pack(m, f, k, _act_code(act), _type_of(dh, "dh"),
+                                 0 if dw_gate is None else _type_of(dw_gate, "dw_gate", True),
+                                 *_mat(dh, m, f, dt, "dh"), *_mat(gate, m, f, (dt, Q8), "gate"),
+                                 *_mat(up, m, f, (dt, Q8), "up"), *_mat(x, m, k, (dt, Q8), "x"),
+                                 *_mat(w_gate, f, k, dt, "w_gate"), *_mat(w_up, f, k, dt, "w_up"),
+                                 *_mat(dx, m, k, dt, "dx"), *_mat(dw_gate, f, k, dwt, "dw_gate"),
+                                 *_mat(dw_up, f, k, dwt, "dw_up"), *_mat(h, m, f, dt, "h"),
+                                 _vec(db_gate, f, "db_gate", torch.float32), _vec(db_up, f, "db_up", torch.float32))
+    _check(load_library().emtk_gated_backward(nn, args, _stream(stream)), "emtk_gated_backward")
+
+
+def emtk_pack8(nn, x, q: Q8, stream=None) -> None:
+    """Keeps x [m][k] (bf16 or fp16) in the 8-bit checkpoint q."""
+    (m, k), dt = x.shape, x.dtype
+    _check(load_library().emtk_pack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")),
+                                     _PACK_MATRIX.pack(*_mat(q, m, k, (dt, Q8), "q")), _stream(stream)), "emtk_pack8")
+
+
+def emtk_unpack8(nn, q: Q8, x, stream=None) -> None:
+    """The values that the 8-bit checkpoint q stands for, into x [m][k] (bf16 or fp16)."""
+    (m, k), dt = x.shape, x.dtype
+    _check(load_library().emtk_unpack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(q, m, k, (dt, Q8), "q")),
+                                       _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")), _stream(stream)), "emtk_unpack8")
 
 
 # ------------------------------------------------------------- test hooks
