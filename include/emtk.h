@@ -395,7 +395,7 @@ EMTK_API emtk_status emtk_batcher_destroy(emtk_batcher *b);
  *   - Matrices are row-major: element (i, j) is d[i * ld + j], ld >= columns,
  *     ld in elements, any ld and any element-aligned address.  Weights are
  *     [out][in].  m rows (hits, tokens), k inputs, n (or f) outputs, each
- *     0 .. 2^31 - 1; m = 0 makes the weights' gradients 0 and k = 0 leaves
+ *     0 .. 2^30; m = 0 makes the weights' gradients 0 and k = 0 leaves
  *     the bias.
  *   - Operands are bf16 or fp16 (one type per call); products are summed in
  *     fp32 on the tensor cores, and everything up to the stored value is fp32

@@ -1,5 +1,6 @@
 // C ABI of the dense layers, gated blocks and 8-bit checkpoints
 // (include/emtk.h): argument checks, workspace and the launches of each call.
+#include <cuda.h>
 #include <nvtx3/nvToolsExt.h>
 
 #include <algorithm>
@@ -37,7 +38,8 @@ emtk_status status_of(cudaError_t e) {
 
 bool type16(int t) { return t == EMTK_TYPE_BF16 || t == EMTK_TYPE_F16; }
 bool act_known(int a) { return a >= EMTK_ACT_NONE && a <= EMTK_ACT_SIGMOID; }
-bool sizes_ok(int32_t a, int32_t b, int32_t c) { return a >= 0 && b >= 0 && c >= 0; }
+constexpr int32_t kMaxSize = 1 << 30;
+bool sizes_ok(int32_t a, int32_t b, int32_t c) { return std::min({a, b, c}) >= 0 && std::max({a, b, c}) <= kMaxSize; }
 size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
 
 // Collects the first argument error of a call.
@@ -96,7 +98,32 @@ struct CallSpace {
     }
 };
 
+// Operands of a call's products that cannot be read where they lie (a
+// checkpoint, or rows off the 16-byte grid): each gets a copy in the workspace.
+struct Staging {
+    CallSpace &ws;
+    struct Copy {
+        emtk_matrix from, to;
+        int rows, cols;
+    } copies[4];
+    int n = 0;
+    emtk_matrix operator()(const emtk_matrix &m, int rows, int cols);
+    cudaError_t run(emtk_type type, int sms, cudaStream_t s) const {
+        cudaError_t e = cudaSuccess;
+        for (int i = 0; i < n && e == cudaSuccess; ++i)
+            e = launch_copy16(type, copies[i].rows, copies[i].cols, copies[i].from, copies[i].to, sms, s);
+        return e;
+    }
+};
+
 int64_t ld16(int64_t cols) { return (cols + 7) / 8 * 8; }  // rows of 16-byte multiples
+
+emtk_matrix Staging::operator()(const emtk_matrix &m, int rows, int cols) {
+    if (rows == 0 || cols == 0 || (!m.d_scale && mm_operand_ok(m.d, m.ld, rows))) return m;
+    Copy &c = copies[n++];
+    c = {m, {ws.take(2 * (size_t)rows * ld16(cols)), ld16(cols), nullptr, 0}, rows, cols};
+    return c.to;
+}
 
 MmOperand rows_of(const emtk_matrix &m) { return {m.d, m.ld, false}; }
 MmOperand cols_of(const emtk_matrix &m) { return {m.d, m.ld, true}; }
@@ -124,7 +151,12 @@ emtk_status emtk_nn_create(int device, int64_t workspace_bytes, int64_t wait_tim
     nn->timeout_ns = wait_timeout_ns;
     nn->debug_stall = debug_stall;
     void *status = nullptr;
-    cudaError_t e = dev_alloc(&status, sizeof(int));
+    cudaDriverEntryPointQueryResult found;
+    cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &nn->encode, 12000, cudaEnableDefault,
+                                                     &found);
+    if (e == cudaSuccess && (nn->encode == nullptr || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
+    if (e == cudaSuccess) e = init_mm_kernels();
+    if (e == cudaSuccess) e = dev_alloc(&status, sizeof(int));
     nn->status = static_cast<int *>(status);
     if (e == cudaSuccess) e = cudaMemset(nn->status, 0, sizeof(int));
     if (e == cudaSuccess && workspace_bytes > 0) {
@@ -185,15 +217,29 @@ emtk_status emtk_dense(emtk_nn *nn, const emtk_dense_args *p, emtk_stream stream
     j.N = a.n;
     j.K = a.k;
     j.terms = 1;
-    j.a[0] = rows_of(a.x);
-    j.b[0] = rows_of(a.w);
     j.epi.act = a.act;
     j.epi.bias[0] = a.bias;
     j.epi.bias_f32 = a.bias_type == EMTK_TYPE_F32;
     j.epi.residual = a.residual;
     j.epi.out = a.y;
     j.epi.saved[0] = a.pre;
-    return status_of(launch_mm(j, nn, reinterpret_cast<cudaStream_t>(stream)));
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    CallSpace ws{nn};
+    Staging stage{ws};
+    void *partial = nullptr;
+    for (int pass = 0; pass < 2; ++pass) {
+        stage.n = 0;
+        j.a[0] = rows_of(stage(a.x, a.m, a.k));
+        j.b[0] = rows_of(stage(a.w, a.n, a.k));
+        partial = ws.take(mm_workspace(j, nn->sm_count));
+        if (pass == 0) {
+            const emtk_status st = ws.ensure(s);
+            if (st != EMTK_OK) return st;
+        }
+    }
+    cudaError_t e = stage.run(j.type, nn->sm_count, s);
+    if (e == cudaSuccess) e = launch_mm(j, nn, partial, s);
+    return status_of(e);
 }
 
 emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk_stream stream) {
@@ -218,14 +264,41 @@ emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk
     const emtk_type type = (emtk_type)a.type;
     const bool dx = a.dx.d && a.m > 0 && a.k > 0, dw = a.dw.d && a.n > 0 && a.k > 0;
     const bool own_dz = a.act != EMTK_ACT_NONE && (dx || dw);
-    const bool x8 = a.x.d_scale && dw;
     CallSpace ws{nn};
-    emtk_matrix dz = a.dy, x = a.x;
-    float *partial = nullptr;
+    Staging stage{ws};
+    MmJob jx{}, jw{};
+    jx.kind = jw.kind = kMmSum;
+    jx.type = jw.type = type;
+    jx.terms = jw.terms = 1;
+    jx.M = a.m;
+    jx.N = jw.N = a.k;
+    jx.K = jw.M = a.n;
+    jw.K = a.m;
+    jx.epi.out = a.dx;
+    jw.epi.out = a.dw;
+    jw.epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
+    emtk_matrix dz{};
+    float *sums = nullptr;
+    void *partial = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
-        if (own_dz) dz = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.n)), ld16(a.n), nullptr, 0};
-        if (x8) x = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.k)), ld16(a.k), nullptr, 0};
-        if (a.db) partial = static_cast<float *>(ws.take(4 * (size_t)slope_slices(a.m, a.n, nn->sm_count) * a.n));
+        stage.n = 0;
+        if (own_dz)
+            dz = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.n)), ld16(a.n), nullptr, 0};
+        else if (dx || dw)
+            dz = stage(a.dy, a.m, a.n);
+        size_t part = 0;
+        if (dx) {
+            jx.a[0] = rows_of(dz);
+            jx.b[0] = cols_of(stage(a.w, a.n, a.k));
+            part = mm_workspace(jx, nn->sm_count);
+        }
+        if (dw) {
+            jw.a[0] = cols_of(dz);
+            jw.b[0] = cols_of(stage(a.x, a.m, a.k));
+            part = std::max(part, mm_workspace(jw, nn->sm_count));
+        }
+        partial = ws.take(part);
+        if (a.db) sums = static_cast<float *>(ws.take(4 * (size_t)slope_slices(a.m, a.n, nn->sm_count) * a.n));
         if (pass == 0) {
             const emtk_status st = ws.ensure(s);
             if (st != EMTK_OK) return st;
@@ -233,32 +306,11 @@ emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk
     }
     cudaError_t e = cudaSuccess;
     if (own_dz || a.db)
-        e = launch_slope(type, a.act, a.m, a.n, a.dy, a.pre, own_dz ? dz.d : nullptr, dz.ld, a.db, partial,
+        e = launch_slope(type, a.act, a.m, a.n, a.dy, a.pre, own_dz ? dz.d : nullptr, dz.ld, a.db, sums,
                          nn->sm_count, s);
-    if (e == cudaSuccess && x8) e = launch_unpack8(type, a.m, a.k, a.x, x, nn->sm_count, s);
-    MmJob j{};
-    j.kind = kMmSum;
-    j.type = type;
-    j.terms = 1;
-    if (e == cudaSuccess && dx) {
-        j.M = a.m;
-        j.N = a.k;
-        j.K = a.n;
-        j.a[0] = rows_of(dz);
-        j.b[0] = cols_of(a.w);
-        j.epi.out = a.dx;
-        e = launch_mm(j, nn, s);
-    }
-    if (e == cudaSuccess && dw) {
-        j.M = a.n;
-        j.N = a.k;
-        j.K = a.m;
-        j.a[0] = cols_of(dz);
-        j.b[0] = cols_of(x);
-        j.epi.out = a.dw;
-        j.epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
-        e = launch_mm(j, nn, s);
-    }
+    if (e == cudaSuccess) e = stage.run(type, nn->sm_count, s);
+    if (e == cudaSuccess && dx) e = launch_mm(jx, nn, partial, s);
+    if (e == cudaSuccess && dw) e = launch_mm(jw, nn, partial, s);
     return status_of(e);
 }
 
@@ -288,9 +340,6 @@ emtk_status emtk_gated(emtk_nn *nn, const emtk_gated_args *p, emtk_stream stream
     j.N = a.f;
     j.K = a.k;
     j.terms = 1;
-    j.a[0] = rows_of(a.x);
-    j.b[0] = rows_of(a.w_gate);
-    j.b[1] = rows_of(a.w_up);
     j.epi.act = a.act;
     j.epi.bias[0] = a.bias_gate;
     j.epi.bias[1] = a.bias_up;
@@ -298,7 +347,24 @@ emtk_status emtk_gated(emtk_nn *nn, const emtk_gated_args *p, emtk_stream stream
     j.epi.out = a.h;
     j.epi.saved[0] = a.gate;
     j.epi.saved[1] = a.up;
-    return status_of(launch_mm(j, nn, reinterpret_cast<cudaStream_t>(stream)));
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    CallSpace ws{nn};
+    Staging stage{ws};
+    void *partial = nullptr;
+    for (int pass = 0; pass < 2; ++pass) {
+        stage.n = 0;
+        j.a[0] = rows_of(stage(a.x, a.m, a.k));
+        j.b[0] = rows_of(stage(a.w_gate, a.f, a.k));
+        j.b[1] = rows_of(stage(a.w_up, a.f, a.k));
+        partial = ws.take(mm_workspace(j, nn->sm_count));
+        if (pass == 0) {
+            const emtk_status st = ws.ensure(s);
+            if (st != EMTK_OK) return st;
+        }
+    }
+    cudaError_t e = stage.run(j.type, nn->sm_count, s);
+    if (e == cudaSuccess) e = launch_mm(j, nn, partial, s);
+    return status_of(e);
 }
 
 emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk_stream stream) {
@@ -330,18 +396,47 @@ emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk
     Range range("emtk gated backward");
     const emtk_type type = (emtk_type)a.type;
     const bool dx = a.dx.d && a.m > 0 && a.k > 0, dw = a.dw_gate.d && a.f > 0 && a.k > 0;
-    const bool x8 = a.x.d_scale && dw;
     CallSpace ws{nn};
-    emtk_matrix dg{}, du{}, x = a.x;
-    float *partial = nullptr;
+    Staging stage{ws};
+    MmJob jx{}, jw[2]{};
+    jx.kind = jw[0].kind = kMmSum;
+    jx.type = jw[0].type = type;
+    jx.terms = 2;
+    jw[0].terms = 1;
+    jx.M = a.m;
+    jx.N = jw[0].N = a.k;
+    jx.K = jw[0].M = a.f;
+    jw[0].K = a.m;
+    jx.epi.out = a.dx;
+    jw[0].epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
+    jw[1] = jw[0];
+    jw[0].epi.out = a.dw_gate;
+    jw[1].epi.out = a.dw_up;
+    emtk_matrix dg{}, du{};
+    float *sums = nullptr;
+    void *partial = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
+        stage.n = 0;
+        size_t part = 0;
         if (dx || dw) {
             dg = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.f)), ld16(a.f), nullptr, 0};
             du = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.f)), ld16(a.f), nullptr, 0};
         }
-        if (x8) x = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.k)), ld16(a.k), nullptr, 0};
-        if (a.db_gate)
-            partial = static_cast<float *>(ws.take(8 * (size_t)slope_slices(a.m, a.f, nn->sm_count) * a.f));
+        if (dx) {
+            jx.a[0] = rows_of(dg);
+            jx.a[1] = rows_of(du);
+            jx.b[0] = cols_of(stage(a.w_gate, a.f, a.k));
+            jx.b[1] = cols_of(stage(a.w_up, a.f, a.k));
+            part = mm_workspace(jx, nn->sm_count);
+        }
+        if (dw) {
+            jw[0].a[0] = cols_of(dg);
+            jw[1].a[0] = cols_of(du);
+            jw[0].b[0] = jw[1].b[0] = cols_of(stage(a.x, a.m, a.k));
+            part = std::max(part, mm_workspace(jw[0], nn->sm_count));
+        }
+        partial = ws.take(part);
+        if (a.db_gate) sums = static_cast<float *>(ws.take(8 * (size_t)slope_slices(a.m, a.f, nn->sm_count) * a.f));
         if (pass == 0) {
             const emtk_status st = ws.ensure(s);
             if (st != EMTK_OK) return st;
@@ -350,34 +445,10 @@ emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk
     cudaError_t e = cudaSuccess;
     if (dx || dw || a.db_gate || a.h.d)
         e = launch_gated_slope(type, a.act, a.m, a.f, a.dh, a.gate, a.up, dg.d, du.d, ld16(a.f), a.h, a.db_gate,
-                               a.db_up, partial, nn->sm_count, s);
-    if (e == cudaSuccess && x8) e = launch_unpack8(type, a.m, a.k, a.x, x, nn->sm_count, s);
-    MmJob j{};
-    j.kind = kMmSum;
-    j.type = type;
-    if (e == cudaSuccess && dx) {
-        j.terms = 2;
-        j.M = a.m;
-        j.N = a.k;
-        j.K = a.f;
-        j.a[0] = rows_of(dg);
-        j.a[1] = rows_of(du);
-        j.b[0] = cols_of(a.w_gate);
-        j.b[1] = cols_of(a.w_up);
-        j.epi.out = a.dx;
-        e = launch_mm(j, nn, s);
-    }
-    j.epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
-    for (int w = 0; w < 2 && e == cudaSuccess && dw; ++w) {
-        j.terms = 1;
-        j.M = a.f;
-        j.N = a.k;
-        j.K = a.m;
-        j.a[0] = cols_of(w ? du : dg);
-        j.b[0] = cols_of(x);
-        j.epi.out = w ? a.dw_up : a.dw_gate;
-        e = launch_mm(j, nn, s);
-    }
+                               a.db_up, sums, nn->sm_count, s);
+    if (e == cudaSuccess) e = stage.run(type, nn->sm_count, s);
+    if (e == cudaSuccess && dx) e = launch_mm(jx, nn, partial, s);
+    for (int w = 0; w < 2 && e == cudaSuccess && dw; ++w) e = launch_mm(jw[w], nn, partial, s);
     return status_of(e);
 }
 
@@ -406,7 +477,7 @@ emtk_status emtk_unpack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type type, cons
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk unpack8");
-    return status_of(launch_unpack8(type, m, k, *q, *x, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+    return status_of(launch_copy16(type, m, k, *q, *x, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

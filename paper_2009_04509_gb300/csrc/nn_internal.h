@@ -15,6 +15,7 @@ struct emtk_nn {
     int *status = nullptr;   // device status word, as a context's
     void *ws = nullptr;      // workspace of the running call
     size_t ws_bytes = 0;
+    void *encode = nullptr;  // cuTensorMapEncodeTiled
 };
 
 namespace emtk {
@@ -55,7 +56,13 @@ struct MmJob {
     MmOperand a[2], b[2];
     MmEpilogue epi;
 };
-cudaError_t launch_mm(const MmJob &job, const emtk_nn *nn, cudaStream_t s);
+// Whether a matrix of 16-bit elements can be an operand as it lies: TMA wants
+// its address and row distance on 16 bytes.  (Others are copied first.)
+bool mm_operand_ok(const void *p, int64_t ld, int64_t rows);
+// Bytes that `partial` of launch_mm needs (256-byte aligned).
+size_t mm_workspace(const MmJob &job, int sms);
+cudaError_t launch_mm(const MmJob &job, const emtk_nn *nn, void *partial, cudaStream_t s);
+cudaError_t init_mm_kernels();  // once per device
 
 // ---- pointwise passes (nn_pointwise.cu)
 // dz = dy act'(pre) as a 16-bit matrix dz (or none), and its column sums db
@@ -69,7 +76,8 @@ cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk
                                float *db_gate, float *db_up, float *partial, int sms, cudaStream_t s);
 cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
                          cudaStream_t s);
-cudaError_t launch_unpack8(emtk_type type, int m, int k, const emtk_matrix &q, const emtk_matrix &x, int sms,
-                           cudaStream_t s);
+// x = the values of src: a checkpoint, or a 16-bit matrix copied as it is.
+cudaError_t launch_copy16(emtk_type type, int m, int k, const emtk_matrix &src, const emtk_matrix &x, int sms,
+                          cudaStream_t s);
 
 }  // namespace emtk

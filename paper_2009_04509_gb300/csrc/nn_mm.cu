@@ -1,120 +1,673 @@
-// The layers' matrix products, on CUDA cores: a block computes a 64 x 64 tile
-// of the output, 16 steps of the contraction at a time from shared memory, a
-// thread 4 x 4 sums (two sets for the gated block).  Any row distance and
-// alignment.
+// The layers' matrix products on the tcgen05 tensor cores.
+//
+// out[M][N] = sum over the contraction of a and b, in tiles of 256 rows by TN
+// columns, each computed by a pair of CTAs (cta_group::2): every CTA stages 128
+// rows of a and half of the columns' b through shared memory by TMA, one thread
+// of the leader issues the MMAs for both, and each CTA's TMEM holds the sums of
+// its own 128 rows in fp32.  Roles of a CTA's 12 warps: TMA producer, MMA issuer
+// (leader), TMEM owner, and 8 epilogue warps that turn one accumulator into
+// output while the next tile is summed in the other.
+//
+// An operand may lie along the contraction (x, w of the forward pass) or across
+// it (w of dx, both operands of dw): the same 128-byte-swizzled boxes, K-major
+// or MN-major descriptors, so no operand is ever transposed in memory.
+//
+// The gated block's tile holds TN/2 columns of each projection: the pair's first
+// CTA stages w_gate's rows, the second w_up's, so one MMA makes g and u of the
+// same columns side by side in TMEM and the epilogue multiplies them there.
+//
+// Outputs of few tiles and a long contraction are split along it: each part
+// leaves fp32 sums in the workspace and a second kernel adds them in order and
+// applies the epilogue, so results do not depend on timing.
+#include <algorithm>
+
 #include "nn_internal.h"
 #include "nn_math.cuh"
+#include "nn_ptx.cuh"
 
 namespace emtk {
 namespace {
 
-constexpr int kTile = 64, kStep = 16, kThreads = 256;
+constexpr int kTileM = 256;              // rows of a pair's tile
+constexpr int kStep = 64;                // contraction steps of a stage: 128 bytes
+constexpr int kABytes = 128 * kStep * 2;  // a CTA's rows of a stage
+constexpr int kEpiWarps = 8;
+constexpr int kFirstEpiWarp = 4;
+constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
+constexpr int kRowBytes = 80;            // staged row: 64 bytes, padded against bank conflicts
+constexpr int kStageRowsBytes = 32 * kRowBytes;
+constexpr int kBiasBytes = 128 * 4;      // an epilogue warp's columns
 
-template <bool F16>
-__device__ __forceinline__ float element(const MmOperand &o, int64_t i, int64_t t) {
-    const uint16_t *p = static_cast<const uint16_t *>(o.p);
-    return from16<F16>(o.across ? p[t * o.ld + i] : p[i * o.ld + t]);
+template <int TN>
+struct Shape {
+    static constexpr int kBBytes = TN / 2 * kStep * 2;
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = TN == 256 ? 6 : 8;
+    static constexpr int kTmemCols = 2 * TN;
+    // barriers first, then the stages on 1024 bytes
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpiWarps * (kStageRowsBytes + kBiasBytes) + 512;
+};
+
+struct MmParams {
+    CUtensorMap a[2], b[2];
+    MmEpilogue epi;
+    float *partial;  // not null: sums of part p to partial + p * part_elems, rows of part_ld
+    int64_t part_elems, part_ld;
+    int M, N, K;
+    int terms, a_across, b_across;
+    int tiles_m, tiles_n, parts;
+    int chunks;            // of one term
+    int chunks_per_part;
+    int *status;
+    int64_t timeout_ns;
+    int debug_stall;
+};
+
+struct Unit {
+    int m0, n0, part, c0, c1;
+};
+
+// Unit u of the launch: tiles in groups of 8 tile rows, along the rows first, so
+// that the pairs at work share operand panels in L2; a tile's parts are adjacent.
+__device__ __forceinline__ Unit unit_of(const MmParams &p, int u, int cols) {
+    const int t = u / p.parts;
+    Unit r;
+    r.part = u - t * p.parts;
+    const int group = t / (8 * p.tiles_n);
+    const int rows = min(8, p.tiles_m - 8 * group);
+    const int in = t - group * 8 * p.tiles_n;
+    r.m0 = (8 * group + in % rows) * kTileM;
+    r.n0 = in / rows * cols;
+    r.c0 = r.part * p.chunks_per_part;
+    r.c1 = min(r.c0 + p.chunks_per_part, p.chunks * p.terms);
+    return r;
 }
 
-template <bool F16>
-__device__ __forceinline__ float load_bias(const MmEpilogue &e, int which, int n) {
-    if (!e.bias[which]) return 0.f;
-    return e.bias_f32 ? static_cast<const float *>(e.bias[which])[n]
-                      : from16<F16>(static_cast<const uint16_t *>(e.bias[which])[n]);
+__device__ __forceinline__ bool wide_rows(const void *p, int64_t ld, int elem) {
+    return ((reinterpret_cast<uintptr_t>(p) | (uint64_t)(ld * elem)) & 15u) == 0;
 }
 
-template <bool F16, bool GATED>
-__global__ void __launch_bounds__(kThreads) mm_kernel(const MmJob job) {
-    __shared__ float sa[kStep][kTile + 1], sb[GATED ? 2 : 1][kStep][kTile + 1];
-    __shared__ float sz[GATED ? 2 : 1][kTile][kTile + 1];
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    const int64_t i0 = (int64_t)blockIdx.y * kTile, j0 = (int64_t)blockIdx.x * kTile;
-    float acc[GATED ? 2 : 1][4][4] = {};
-    for (int term = 0; term < job.terms; ++term) {
-        for (int t0 = 0; t0 < job.K; t0 += kStep) {
-            __syncthreads();
-            for (int e = threadIdx.x; e < kTile * kStep; e += kThreads) {
-                const int i = e / kStep, t = e % kStep;
-                const bool in = t0 + t < job.K;
-                sa[t][i] = in && i0 + i < job.M ? element<F16>(job.a[term], i0 + i, t0 + t) : 0.f;
-                for (int w = 0; w < (GATED ? 2 : 1); ++w)
-                    sb[w][t][i] = in && j0 + i < job.N ? element<F16>(job.b[GATED ? w : term], j0 + i, t0 + t) : 0.f;
+// Rows r0 .. r0 + 31 (below `rows`), columns c0 .. c0 + 64 / sizeof(T) - 1 (below
+// `cols`) of a matrix, between memory and the warp's staged rows; four lanes move
+// a row where 16-byte pieces fit, a row at a time where they do not.
+template <typename T, bool LOAD>
+__device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int64_t rows, int64_t c0, int64_t cols,
+                                           bool wide, uint8_t *stage, int lane) {
+    constexpr int kPiece = 16 / sizeof(T), kCols = 64 / sizeof(T);
+    const int nr = (int)min((int64_t)32, rows - r0), nc = (int)min((int64_t)kCols, cols - c0);
+    if (wide) {
+        const int c = (lane & 3) * kPiece;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int r = it * 8 + (lane >> 2);
+            if (r >= nr || c >= nc) continue;
+            T *g = base + (r0 + r) * ld + c0 + c;
+            uint8_t *s = stage + r * kRowBytes + (lane & 3) * 16;
+            if (c + kPiece <= nc) {
+                if (LOAD)
+                    *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
+                else
+                    *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(s);
+            } else {
+                for (int i = 0; c + i < nc; ++i) {
+                    if (LOAD)
+                        reinterpret_cast<T *>(s)[i] = g[i];
+                    else
+                        g[i] = reinterpret_cast<const T *>(s)[i];
+                }
             }
-            __syncthreads();
-            for (int t = 0; t < kStep; ++t)
-#pragma unroll
-                for (int w = 0; w < (GATED ? 2 : 1); ++w)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            acc[w][i][j] = fmaf(sa[t][ty + 16 * i], sb[w][t][tx + 16 * j], acc[w][i][j]);
+        }
+    } else if (lane < nc) {
+#pragma unroll 4
+        for (int r = 0; r < nr; ++r) {
+            T *g = base + (r0 + r) * ld + c0 + lane;
+            T *s = reinterpret_cast<T *>(stage + r * kRowBytes) + lane;
+            if (LOAD)
+                *s = *g;
+            else
+                *g = *s;
         }
     }
-    const MmEpilogue &e = job.epi;
+}
+
+// What the epilogue of one warp needs: its 32 rows and its staged rows.
+struct Rows {
+    int64_t r0, rows;  // first row, rows of the matrix
+    uint8_t *stage;
+    int lane;
+};
+
+template <bool F16>
+__device__ __forceinline__ void store16(const emtk_matrix &m, const Rows &w, int64_t c0, int64_t cols,
+                                        const float (&v)[32]) {
+    uint8_t *row = w.stage + w.lane * kRowBytes;
 #pragma unroll
-    for (int w = 0; w < (GATED ? 2 : 1); ++w)
+    for (int i = 0; i < 4; ++i)
+        reinterpret_cast<uint4 *>(row)[i] =
+            make_uint4(pack16<F16>(v[8 * i], v[8 * i + 1]), pack16<F16>(v[8 * i + 2], v[8 * i + 3]),
+                       pack16<F16>(v[8 * i + 4], v[8 * i + 5]), pack16<F16>(v[8 * i + 6], v[8 * i + 7]));
+    __syncwarp();
+    move_block<uint16_t, false>(static_cast<uint16_t *>(m.d), m.ld, w.r0, w.rows, c0, cols, wide_rows(m.d, m.ld, 2),
+                                w.stage, w.lane);
+    __syncwarp();
+}
+
+__device__ __forceinline__ void store32(float *base, int64_t ld, const Rows &w, int64_t c0, int64_t cols,
+                                        const float (&v)[32]) {
+    float4 *row = reinterpret_cast<float4 *>(w.stage + w.lane * kRowBytes);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = 16 * half + 4 * i;
+            row[i] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        }
+        __syncwarp();
+        if (c0 + 16 * half < cols)
+            move_block<float, false>(base, ld, w.r0, w.rows, c0 + 16 * half, cols, wide_rows(base, ld, 4), w.stage,
+                                     w.lane);
+        __syncwarp();
+    }
+}
+
+// A row's 32 columns as one checkpoint block; a lane writes its row's sector.
+__device__ __forceinline__ void store_q8(const emtk_matrix &m, const Rows &w, int64_t c0, int64_t cols,
+                                         const float (&v)[32]) {
+    const int nc = (int)min((int64_t)32, cols - c0);
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, i < nc ? finite_abs(v[i]) : 0.f);
+    const uint32_t b = q8_scale(top);
+    const float inverse = q8_inverse(b);
+    const int64_t r = w.r0 + w.lane;
+    if (r >= w.rows) return;
+    m.d_scale[r * m.ld_scale + c0 / kQ8Block] = (uint8_t)b;
+    uint8_t *p = static_cast<uint8_t *>(m.d) + r * m.ld + c0;
+    if (nc == 32 && wide_rows(m.d, m.ld, 1)) {
+        uint32_t q[8] = {};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) q[i / 4] |= q8_code(v[i], inverse) << (8 * (i % 4));
+        reinterpret_cast<uint4 *>(p)[0] = make_uint4(q[0], q[1], q[2], q[3]);
+        reinterpret_cast<uint4 *>(p)[1] = make_uint4(q[4], q[5], q[6], q[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < nc) p[i] = (uint8_t)q8_code(v[i], inverse);
+    }
+}
+
+template <bool F16>
+__device__ __forceinline__ void store_saved(const emtk_matrix &m, const Rows &w, int64_t c0, int64_t cols,
+                                            const float (&v)[32]) {
+    if (m.d == nullptr) return;
+    if (m.d_scale)
+        store_q8(m, w, c0, cols, v);
+    else
+        store16<F16>(m, w, c0, cols, v);
+}
+
+template <bool F16>
+__device__ __forceinline__ float bias_at(const MmEpilogue &e, int which, int64_t n, int64_t cols) {
+    if (e.bias[which] == nullptr || n >= cols) return 0.f;
+    return e.bias_f32 ? __ldg(static_cast<const float *>(e.bias[which]) + n)
+                      : from16<F16>(__ldg(static_cast<const uint16_t *>(e.bias[which]) + n));
+}
+
+// Sums of a dense tile's 32 columns (z without its bias, which is in `bias`).
+template <bool F16>
+__device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
+                                             const float *bias, float (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] += bias[i];
+    store_saved<F16>(e.saved[0], w, c0, cols, v);
+    if (e.act != EMTK_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = act_f(e.act, v[i]);
+    }
+    if (e.residual.d) {
+        move_block<uint16_t, true>(static_cast<uint16_t *>(e.residual.d), e.residual.ld, w.r0, w.rows, c0, cols,
+                                   wide_rows(e.residual.d, e.residual.ld, 2), w.stage, w.lane);
+        __syncwarp();
+        const uint4 *row = reinterpret_cast<const uint4 *>(w.stage + w.lane * kRowBytes);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 q = row[i];
+            const uint32_t x[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int64_t n = j0 + tx + 16 * j;
-                sz[w][ty + 16 * i][tx + 16 * j] =
-                    n < job.N ? acc[w][i][j] + load_bias<F16>(e, w, (int)n) : 0.f;
+                v[8 * i + 2 * j] += from16<F16>(x[j] & 0xffffu);
+                v[8 * i + 2 * j + 1] += from16<F16>(x[j] >> 16);
             }
-    __syncthreads();
-    // a thread takes 16 columns of a row, half a checkpoint block
-    const int r = threadIdx.x / 4, c0 = (threadIdx.x % 4) * 16;
-    const int64_t i = i0 + r;
-    const bool row_in = i < job.M;
+        }
+        __syncwarp();
+    }
+    if (e.out_f32)
+        store32(static_cast<float *>(e.out.d), e.out.ld, w, c0, cols, v);
+    else
+        store16<F16>(e.out, w, c0, cols, v);
+}
+
+template <bool F16>
+__device__ __forceinline__ void finish_gated(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
+                                             const float *bias_g, const float *bias_u, float (&g)[32],
+                                             float (&u)[32]) {
 #pragma unroll
-    for (int w = 0; w < (GATED ? 2 : 1); ++w) {
-        const emtk_matrix &m = e.saved[w];
-        if (!m.d) continue;
-        float inverse = 0.f;
+    for (int i = 0; i < 32; ++i) {
+        g[i] += bias_g[i];
+        u[i] += bias_u[i];
+    }
+    store_saved<F16>(e.saved[0], w, c0, cols, g);
+    store_saved<F16>(e.saved[1], w, c0, cols, u);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) g[i] = act_f(e.act, g[i]) * u[i];
+    store16<F16>(e.out, w, c0, cols, g);
+}
+
+enum Bar : int { kBarFull = 0, kBarEmpty = 8, kBarAccFull = 16, kBarAccEmpty = 18, kBarDrain = 20, kBarStall = 21, kBars = 22 };
+
+template <bool F16, bool GATED, int TN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    mm_kernel(const __grid_constant__ MmParams p) {
+    using S = Shape<TN>;
+    constexpr int kCols = GATED ? TN / 2 : TN;  // output columns of a tile
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    uint8_t *const base = smem_raw + ((1024u - (raw & 1023u)) & 1023u);
+    const uint32_t stages = smem_u32(base);
+    uint8_t *const tail = base + S::kStages * S::kStageBytes;
+    uint8_t *const epi_rows = tail;
+    float *const epi_bias = reinterpret_cast<float *>(tail + kEpiWarps * kStageRowsBytes);
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(tail + kEpiWarps * (kStageRowsBytes + kBiasBytes));
+    uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(bars + kBars);
+    volatile uint32_t *const abort_flag = tmem_slot + 1;
+    auto bar = [&](int i) { return smem_u32(bars + i); };
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const Guard guard{abort_flag, p.status, p.timeout_ns};
+    const int pair = (int)blockIdx.x / 2, pairs = (int)gridDim.x / 2;
+    const int units = p.tiles_m * p.tiles_n * p.parts;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(bar(kBarFull + s), 1);
+            mbar_init(bar(kBarEmpty + s), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(kBarAccFull + i), 1);
+            mbar_init(bar(kBarAccEmpty + i), 2 * kEpiWarps);
+        }
+        mbar_init(bar(kBarDrain), 1);
+        mbar_init(bar(kBarStall), 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 2) tmem_alloc_pair(smem_u32(tmem_slot), S::kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            // ------------------------------------------------ TMA producer
+            if (p.chunks > 0) {
+                for (int i = 0; i < p.terms; ++i) prefetch_map(&p.a[i]);
+                for (int i = 0; i < (GATED ? 2 : p.terms); ++i) prefetch_map(&p.b[i]);
+            }
+            bool ok = !(p.debug_stall && !wait_bounded(bar(kBarStall), 0u, guard));
+            int it = 0;
+            for (int u = pair; ok && u < units; u += pairs) {
+                const Unit t = unit_of(p, u, kCols);
+                for (int c = t.c0; c < t.c1; ++c, ++it) {
+                    const int s = it % S::kStages, round = it / S::kStages;
+                    if (round > 0 && !wait_bounded(bar(kBarEmpty + s), (uint32_t)(round - 1) & 1u, guard)) {
+                        ok = false;
+                        break;
+                    }
+                    const int term = c / p.chunks, k0 = (c - term * p.chunks) * kStep;
+                    const uint32_t sa = stages + s * S::kStageBytes, sb = sa + kABytes;
+                    const uint32_t full = cluster_addr(bar(kBarFull + s), 0);
+                    if (rank == 0) mbar_expect_tx(bar(kBarFull + s), 2 * S::kStageBytes);
+                    const int ra = t.m0 + 128 * (int)rank;
+                    const CUtensorMap *ma = &p.a[GATED ? 0 : term];
+                    if (p.a_across) {
+                        tma_load_2d_pair(sa, ma, full, ra, k0);
+                        tma_load_2d_pair(sa + 64 * 128, ma, full, ra + 64, k0);
+                    } else {
+                        tma_load_2d_pair(sa, ma, full, k0, ra);
+                    }
+                    const int rb = t.n0 + (GATED ? 0 : TN / 2 * (int)rank);
+                    const CUtensorMap *mb = &p.b[GATED ? (int)rank : term];
+                    if (p.b_across) {
+#pragma unroll
+                        for (int j = 0; j < TN / 128; ++j) tma_load_2d_pair(sb + j * 64 * 128, mb, full, rb + 64 * j, k0);
+                    } else {
+                        tma_load_2d_pair(sb, mb, full, k0, rb);
+                    }
+                }
+            }
+            if (!ok) {  // copies in flight land within microseconds: leave them a millisecond
+                const uint64_t t0 = global_timer_ns();
+                while (global_timer_ns() - t0 < 1000000u) {
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1 && rank == 0) {
+        if (lane == 0) {
+            // ------------------------------------------------ MMA issuer
+            const uint32_t idesc = make_idesc_major(kTileM, TN, F16, p.a_across != 0, p.b_across != 0);
+            const uint64_t da = p.a_across ? sw128_desc_across(stages, 64 * 128) : sw128_desc(stages);
+            const uint64_t db = p.b_across ? sw128_desc_across(stages + kABytes, 64 * 128) : sw128_desc(stages + kABytes);
+            // 16 contraction steps: 32 bytes along a K-major row, 16 rows of an MN-major box
+            const uint64_t step_a = p.a_across ? 2048 >> 4 : 32 >> 4, step_b = p.b_across ? 2048 >> 4 : 32 >> 4;
+            const int last_steps = (p.K - (p.chunks - 1) * kStep + 15) / 16;
+            bool ok = true;
+            int it = 0, tile = 0;
+            for (int u = pair; ok && u < units; u += pairs, ++tile) {
+                const Unit t = unit_of(p, u, kCols);
+                const int ab = tile & 1;
+                if (tile >= 2 && !wait_bounded(bar(kBarAccEmpty + ab), (uint32_t)(tile / 2 - 1) & 1u, guard)) break;
+                tc_fence_after();
+                const uint32_t acc = tmem + (uint32_t)(ab * TN);
+                for (int c = t.c0; c < t.c1; ++c, ++it) {
+                    const int s = it % S::kStages;
+                    if (!wait_bounded(bar(kBarFull + s), (uint32_t)(it / S::kStages) & 1u, guard)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint64_t off = (uint64_t)(s * S::kStageBytes) >> 4;
+                    const int steps = (c + 1) % p.chunks == 0 ? last_steps : kStep / 16;
+                    for (int i = 0; i < steps; ++i)
+                        mma_pair(acc, da + off + i * step_a, db + off + i * step_b, idesc,
+                                 (c > t.c0 || i > 0) ? 1u : 0u);
+                    mma_commit_pair(bar(kBarEmpty + s));
+                }
+                if (ok) mma_commit_pair(bar(kBarAccFull + ab));
+            }
+            // every MMA issued completes before TMEM is released
+            mma_commit_pair(bar(kBarDrain));
+            const uint64_t t0 = global_timer_ns();
+            while (!mbar_try_wait(bar(kBarDrain), 0u) && (int64_t)(global_timer_ns() - t0) < p.timeout_ns) {
+            }
+        }
+        __syncwarp();
+    } else if (warp >= kFirstEpiWarp) {
+        // ---------------------------------------------------- epilogue
+        // Warp e reads TMEM lanes 32 (e % 4) .. (the hardware's rule: a warp's index in
+        // its group of four) and half of the tile's columns.
+        const int e = warp - kFirstEpiWarp;
+        const int q = e & 3, half = e >> 2;
+        constexpr int kMine = kCols / 2;  // output columns of a warp
+        float *const bias = epi_bias + e * (kBiasBytes / 4);
+        Rows w{0, p.M, epi_rows + e * kStageRowsBytes, lane};
+        int tile = 0;
+        for (int u = pair; u < units; u += pairs, ++tile) {
+            const Unit t = unit_of(p, u, kCols);
+            const int ab = tile & 1;
+            w.r0 = t.m0 + 128 * (int64_t)rank + 32 * q;
+            const int64_t n0 = t.n0 + half * kMine;
+            __syncwarp();
+            if (p.partial == nullptr) {
+                for (int j = lane; j < kMine; j += 32) {
+                    bias[j] = bias_at<F16>(p.epi, 0, n0 + j, p.N);
+                    if (GATED) bias[kMine + j] = bias_at<F16>(p.epi, 1, n0 + j, p.N);
+                }
+            }
+            if (!warp_wait(bar(kBarAccFull + ab), (uint32_t)(tile / 2) & 1u, guard, lane)) break;
+            tc_fence_after();
+            const uint32_t acc = tmem + (uint32_t)(ab * TN) + ((uint32_t)(32 * q) << 16);
+            const bool rows_in = w.r0 < p.M;
+#pragma unroll 1
+            for (int j = 0; j < kMine; j += 32) {
+                const int64_t c0 = n0 + j;
+                float v[32], x[GATED ? 32 : 1];
+                const bool in = rows_in && c0 < p.N;
+                if (in && t.c0 < t.c1) {
+                    tmem_ld32(acc + (uint32_t)(half * kMine + j), v);
+                    if constexpr (GATED) tmem_ld32(acc + (uint32_t)(TN / 2 + half * kMine + j), x);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        v[i] = 0.f;
+                        if constexpr (GATED) x[i] = 0.f;
+                    }
+                }
+                if (j + 32 == kMine) {  // this warp has read all of its sums
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(cluster_addr(bar(kBarAccEmpty + ab), 0));
+                }
+                if (!in) continue;
+                if (p.partial != nullptr) {
+                    float *part = p.partial + t.part * p.part_elems;
+                    const int64_t pc = (int64_t)(t.n0 / kCols) * TN + half * kMine + j;
+                    store32(part, p.part_ld, w, pc, p.part_ld, v);
+                    if constexpr (GATED) store32(part, p.part_ld, w, pc + TN / 2, p.part_ld, x);
+                } else if constexpr (GATED) {
+                    finish_gated<F16>(p.epi, w, c0, p.N, bias + j, bias + kMine + j, v, x);
+                } else {
+                    finish_dense<F16>(p.epi, w, c0, p.N, bias + j, v);
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // no arrival or MMA of the pair is outstanding
+    tc_fence_after();
+    if (warp == 2) tmem_free_pair(tmem, S::kTmemCols);
+}
+
+// Adds the parts' sums in order and applies the epilogue: a thread takes 8
+// columns of a row, four threads a checkpoint block.
+template <bool F16, bool GATED, int TN>
+__global__ void __launch_bounds__(256) parts_kernel(const MmEpilogue e, const float *partial, int64_t part_elems,
+                                                    int64_t part_ld, int parts, int M, int N, int groups) {
+    constexpr int kCols = GATED ? TN / 2 : TN;
+    const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;  // groups is a multiple of 4
+    const int64_t r = idx / groups;
+    const int c = (int)(idx - r * groups) * 8;
+    const bool in = r < M && c < N;
+    float v[GATED ? 2 : 1][8] = {};
+    if (in) {
+#pragma unroll
+        for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+            const float *p = partial + r * part_ld + (c / kCols) * TN + c % kCols + h * (TN / 2);
+            for (int i = 0; i < parts; ++i, p += part_elems) {
+                const float4 lo = __ldg(reinterpret_cast<const float4 *>(p));
+                const float4 hi = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+                const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[h][j] += x[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[h][j] += bias_at<F16>(e, h, c + j, N);
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+        const emtk_matrix &m = e.saved[h];
+        if (m.d == nullptr) continue;
         if (m.d_scale) {
             float top = 0.f;
-            for (int c = 0; c < 16; ++c) top = fmaxf(top, finite_abs(sz[w][r][c0 + c]));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, in && c + j < N ? finite_abs(v[h][j]) : 0.f);
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const uint32_t b = q8_scale(top);
-            inverse = q8_inverse(b);
-            if (row_in && (threadIdx.x & 1) == 0 && j0 + c0 < job.N)
-                m.d_scale[i * m.ld_scale + (j0 + c0) / kQ8Block] = (uint8_t)b;
-        }
-        for (int c = 0; c < 16; ++c) {
-            const int64_t j = j0 + c0 + c;
-            if (!row_in || j >= job.N) continue;
-            if (m.d_scale)
-                static_cast<uint8_t *>(m.d)[i * m.ld + j] = (uint8_t)q8_code(sz[w][r][c0 + c], inverse);
-            else
-                static_cast<uint16_t *>(m.d)[i * m.ld + j] = (uint16_t)to16<F16>(sz[w][r][c0 + c]);
+            if (!in) continue;
+            if (c % kQ8Block == 0) m.d_scale[r * m.ld_scale + c / kQ8Block] = (uint8_t)b;
+            for (int j = 0; j < 8; ++j)
+                if (c + j < N)
+                    static_cast<uint8_t *>(m.d)[r * m.ld + c + j] = (uint8_t)q8_code(v[h][j], q8_inverse(b));
+        } else if (in) {
+            for (int j = 0; j < 8; ++j)
+                if (c + j < N) static_cast<uint16_t *>(m.d)[r * m.ld + c + j] = (uint16_t)to16<F16>(v[h][j]);
         }
     }
-    for (int c = 0; c < 16; ++c) {
-        const int64_t j = j0 + c0 + c;
-        if (!row_in || j >= job.N) continue;
-        float v = act_f(e.act, sz[0][r][c0 + c]);
-        if (GATED) v *= sz[GATED ? 1 : 0][r][c0 + c];
-        if (e.residual.d) v += from16<F16>(static_cast<const uint16_t *>(e.residual.d)[i * e.residual.ld + j]);
-        if (e.out_f32)
-            static_cast<float *>(e.out.d)[i * e.out.ld + j] = v;
-        else
-            static_cast<uint16_t *>(e.out.d)[i * e.out.ld + j] = (uint16_t)to16<F16>(v);
+    if (!in) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float y = act_f(e.act, v[0][j]);
+        if (GATED) y *= v[GATED ? 1 : 0][j];
+        if (!GATED && e.residual.d && c + j < N)
+            y += from16<F16>(static_cast<const uint16_t *>(e.residual.d)[r * e.residual.ld + c + j]);
+        v[0][j] = y;
     }
+    if (e.out_f32) {
+        float *o = static_cast<float *>(e.out.d) + r * e.out.ld + c;
+        for (int j = 0; j < 8; ++j)
+            if (c + j < N) o[j] = v[0][j];
+    } else if (c + 8 <= N && wide_rows(e.out.d, e.out.ld, 2)) {
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(e.out.d) + r * e.out.ld + c) =
+            make_uint4(pack16<F16>(v[0][0], v[0][1]), pack16<F16>(v[0][2], v[0][3]), pack16<F16>(v[0][4], v[0][5]),
+                       pack16<F16>(v[0][6], v[0][7]));
+    } else {
+        for (int j = 0; j < 8; ++j)
+            if (c + j < N) static_cast<uint16_t *>(e.out.d)[r * e.out.ld + c + j] = (uint16_t)to16<F16>(v[0][j]);
+    }
+}
+
+// ---------------------------------------------------------------- host
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// rows: the operand's index i (M or N), K its contraction, box_rows of a stage.
+bool encode(EncodeTiled fn, CUtensorMap *map, const MmOperand &o, int rows, int K, int box_rows) {
+    const int64_t lines = o.across ? K : rows;
+    const cuuint64_t dims[2] = {(cuuint64_t)(o.across ? rows : K), (cuuint64_t)lines};
+    const cuuint64_t strides[1] = {(cuuint64_t)(lines > 1 ? 2 * o.ld : (2 * (int64_t)dims[0] + 15) / 16 * 16)};
+    const cuuint32_t box[2] = {64u, (cuuint32_t)(o.across ? kStep : box_rows)};
+    const cuuint32_t one[2] = {1u, 1u};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(o.p), dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Plan {
+    int tn, tiles_m, tiles_n, chunks, parts, chunks_per_part, pairs;
+    int64_t part_elems, part_ld;
+};
+
+// Tile width and split.  A wave is the time the pairs take for one tile each;
+// a 128-wide tile takes 0.6 of a 256-wide one (its a operand is staged for half
+// the products).  Parts of a split contraction keep at least 8 chunks each,
+// and are taken only when the tiles leave more than half of the pairs idle.
+Plan plan_of(const MmJob &j, int sms) {
+    const int pairs = std::max(1, sms / 2);
+    Plan best{};
+    double cost = 0;
+    const int chunks = (int)(((int64_t)j.K + kStep - 1) / kStep), total = chunks * j.terms;
+    for (int tn : {256, 128}) {
+        const int cols = j.kind == kMmGated ? tn / 2 : tn;
+        Plan p{};
+        p.tn = tn;
+        p.tiles_m = (int)(((int64_t)j.M + kTileM - 1) / kTileM);
+        p.tiles_n = (int)(((int64_t)j.N + cols - 1) / cols);
+        p.chunks = chunks;
+        const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+        p.parts = 1;
+        if (tiles * 2 <= pairs && total >= 16)
+            p.parts = (int)std::min<int64_t>(pairs / tiles, total / 8);
+        p.chunks_per_part = std::max(1, (total + p.parts - 1) / p.parts);
+        p.parts = std::max(1, (total + p.chunks_per_part - 1) / p.chunks_per_part);
+        p.part_ld = (int64_t)p.tiles_n * tn;
+        p.part_elems = p.part_ld * p.tiles_m * kTileM;
+        p.pairs = (int)std::min<int64_t>(pairs, tiles * p.parts);
+        const double waves = (double)((tiles * p.parts + pairs - 1) / pairs);
+        const double c = waves * p.chunks_per_part * (tn == 256 ? 1.0 : 0.6);
+        if (best.tn == 0 || c < cost) {
+            best = p;
+            cost = c;
+        }
+    }
+    return best;
+}
+
+template <bool F16, bool GATED, int TN>
+cudaError_t run(const MmParams &p, const Plan &plan, cudaStream_t s) {
+    auto kernel = mm_kernel<F16, GATED, TN>;
+    kernel<<<2 * plan.pairs, kThreads, Shape<TN>::kSmem, s>>>(p);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess || plan.parts == 1) return e;
+    const int groups = (p.N + 31) / 32 * 4;
+    const int64_t threads = (int64_t)p.M * groups;
+    parts_kernel<F16, GATED, TN><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(
+        p.epi, p.partial, p.part_elems, p.part_ld, plan.parts, p.M, p.N, groups);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_mm(const MmJob &job, const emtk_nn *, cudaStream_t s) {
-    if (job.M == 0 || job.N == 0) return cudaSuccess;
-    const dim3 grid((job.N - 1) / kTile + 1, (job.M - 1) / kTile + 1);
-    const bool f16 = job.type == EMTK_TYPE_F16;
-    if (job.kind == kMmGated)
-        f16 ? mm_kernel<true, true><<<grid, kThreads, 0, s>>>(job) : mm_kernel<false, true><<<grid, kThreads, 0, s>>>(job);
-    else
-        f16 ? mm_kernel<true, false><<<grid, kThreads, 0, s>>>(job)
-            : mm_kernel<false, false><<<grid, kThreads, 0, s>>>(job);
-    return cudaGetLastError();
+bool mm_operand_ok(const void *p, int64_t ld, int64_t rows) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (ld * 2) % 16 == 0);
+}
+
+size_t mm_workspace(const MmJob &j, int sms) {
+    if (j.M == 0 || j.N == 0) return 0;
+    const Plan p = plan_of(j, sms);
+    return p.parts > 1 ? (size_t)p.parts * p.part_elems * sizeof(float) : 0;
+}
+
+cudaError_t init_mm_kernels() {
+    cudaError_t e = cudaSuccess;
+#define EMTK_MM_ATTR(F16, GATED, TN)                                                                            \
+    if (e == cudaSuccess)                                                                                       \
+        e = cudaFuncSetAttribute(mm_kernel<F16, GATED, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize,        \
+                                 Shape<TN>::kSmem);
+    EMTK_MM_ATTR(false, false, 256)
+    EMTK_MM_ATTR(false, true, 256)
+    EMTK_MM_ATTR(true, false, 256)
+    EMTK_MM_ATTR(true, true, 256)
+    EMTK_MM_ATTR(false, false, 128)
+    EMTK_MM_ATTR(false, true, 128)
+    EMTK_MM_ATTR(true, false, 128)
+    EMTK_MM_ATTR(true, true, 128)
+#undef EMTK_MM_ATTR
+    return e;
+}
+
+cudaError_t launch_mm(const MmJob &j, const emtk_nn *nn, void *partial, cudaStream_t s) {
+    if (j.M == 0 || j.N == 0) return cudaSuccess;
+    const Plan plan = plan_of(j, nn->sm_count);
+    const bool gated = j.kind == kMmGated, f16 = j.type == EMTK_TYPE_F16;
+    MmParams p;
+    if (j.K > 0) {
+        const auto fn = reinterpret_cast<EncodeTiled>(nn->encode);
+        bool ok = true;
+        for (int i = 0; i < j.terms; ++i) ok = ok && encode(fn, &p.a[i], j.a[i], j.M, j.K, 128);
+        for (int i = 0; i < (gated ? 2 : j.terms); ++i) ok = ok && encode(fn, &p.b[i], j.b[i], j.N, j.K, plan.tn / 2);
+        if (!ok) return cudaErrorInvalidValue;
+    }
+    p.epi = j.epi;
+    p.partial = plan.parts > 1 ? static_cast<float *>(partial) : nullptr;
+    p.part_elems = plan.part_elems;
+    p.part_ld = plan.part_ld;
+    p.M = j.M;
+    p.N = j.N;
+    p.K = j.K;
+    p.terms = j.terms;
+    p.a_across = j.a[0].across;
+    p.b_across = j.b[0].across;
+    p.tiles_m = plan.tiles_m;
+    p.tiles_n = plan.tiles_n;
+    p.parts = plan.parts;
+    p.chunks = plan.chunks;
+    p.chunks_per_part = plan.chunks_per_part;
+    p.status = nn->status;
+    p.timeout_ns = nn->timeout_ns;
+    p.debug_stall = nn->debug_stall;
+    const bool wide = plan.tn == 256;
+    if (f16)
+        return gated ? (wide ? run<true, true, 256>(p, plan, s) : run<true, true, 128>(p, plan, s))
+                     : (wide ? run<true, false, 256>(p, plan, s) : run<true, false, 128>(p, plan, s));
+    return gated ? (wide ? run<false, true, 256>(p, plan, s) : run<false, true, 128>(p, plan, s))
+                 : (wide ? run<false, false, 256>(p, plan, s) : run<false, false, 128>(p, plan, s));
 }
 
 }  // namespace emtk

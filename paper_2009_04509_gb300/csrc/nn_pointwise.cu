@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kThreads) pack8_kernel(Source x, uint8_t *q, i
 }
 
 template <bool F16>
-__global__ void __launch_bounds__(kThreads) unpack8_kernel(Source q, uint16_t *x, int64_t x_ld, int64_t items,
+__global__ void __launch_bounds__(kThreads) copy16_kernel(Source src, uint16_t *x, int64_t x_ld, int64_t items,
                                                            int per_row, int k, int wide) {
     const int lane = threadIdx.x & 31;
     const int64_t warps = (int64_t)gridDim.x * (kThreads / 32);
@@ -257,9 +257,11 @@ __global__ void __launch_bounds__(kThreads) unpack8_kernel(Source q, uint16_t *x
         const int c = (int)(it - r * per_row) * kWarpCols + lane * kVec;
         if (c >= k) continue;
         float v[kVec];
-        load8<F16>(q, r, c, k, v);
+        load8<F16>(src, r, c, k, v);
+        if (src.scale) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = q8_operand<F16>(v[i]);
+            for (int i = 0; i < kVec; ++i) v[i] = q8_operand<F16>(v[i]);
+        }
         store8<F16>(x + r * x_ld, c, k, wide != 0, v);
     }
 }
@@ -331,16 +333,16 @@ cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, con
     return cudaGetLastError();
 }
 
-cudaError_t launch_unpack8(emtk_type type, int m, int k, const emtk_matrix &q, const emtk_matrix &x, int sms,
-                           cudaStream_t s) {
+cudaError_t launch_copy16(emtk_type type, int m, int k, const emtk_matrix &src, const emtk_matrix &x, int sms,
+                          cudaStream_t s) {
     if (m == 0 || k == 0) return cudaSuccess;
     const WarpGrid g = warp_grid(m, k, sms);
     const int wide = aligned(x.d, 2 * x.ld, 16);
     uint16_t *d = static_cast<uint16_t *>(x.d);
     if (type == EMTK_TYPE_F16)
-        unpack8_kernel<true><<<g.blocks, kThreads, 0, s>>>(source_of(q), d, x.ld, g.items, g.per_row, k, wide);
+        copy16_kernel<true><<<g.blocks, kThreads, 0, s>>>(source_of(src), d, x.ld, g.items, g.per_row, k, wide);
     else
-        unpack8_kernel<false><<<g.blocks, kThreads, 0, s>>>(source_of(q), d, x.ld, g.items, g.per_row, k, wide);
+        copy16_kernel<false><<<g.blocks, kThreads, 0, s>>>(source_of(src), d, x.ld, g.items, g.per_row, k, wide);
     return cudaGetLastError();
 }
 
