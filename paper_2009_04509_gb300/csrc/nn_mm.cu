@@ -310,27 +310,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const uint32_t tmem = *tmem_slot;
 
     if (warp == 0) {
-        if (lane == 0) {
-            // ------------------------------------------------ TMA producer
-            if (p.chunks > 0) {
-                for (int i = 0; i < p.terms; ++i) prefetch_map(&p.a[i]);
-                for (int i = 0; i < (GATED ? 2 : p.terms); ++i) prefetch_map(&p.b[i]);
-            }
-            bool ok = !(p.debug_stall && !wait_bounded(bar(kBarStall), 0u, guard));
-            int it = 0;
-            for (int u = pair; ok && u < units; u += pairs) {
-                const Unit t = unit_of(p, u, kCols);
-                for (int c = t.c0; c < t.c1; ++c, ++it) {
-                    const int s = it % S::kStages, round = it / S::kStages;
-                    if (round > 0 && !wait_bounded(bar(kBarEmpty + s), (uint32_t)(round - 1) & 1u, guard)) {
-                        ok = false;
-                        break;
-                    }
-                    const int term = c / p.chunks, k0 = (c - term * p.chunks) * kStep;
+        // ---------------------------------------------------- TMA producer
+        // The warp runs the loop together and one lane issues (here and in the MMA
+        // warp): descriptors and addresses stay in uniform registers.
+        if (p.chunks > 0 && elect_one()) {
+            for (int i = 0; i < p.terms; ++i) prefetch_map(&p.a[i]);
+            for (int i = 0; i < (GATED ? 2 : p.terms); ++i) prefetch_map(&p.b[i]);
+        }
+        __syncwarp();
+        bool ok = !(p.debug_stall && !warp_wait(bar(kBarStall), 0u, guard, lane));
+        int s = 0;
+        uint32_t phase = 1;  // a fresh barrier's previous phase counts as complete
+        for (int u = pair; ok && u < units; u += pairs) {
+            const Unit t = unit_of(p, u, kCols);
+            const int ra = t.m0 + 128 * (int)rank, rb = t.n0 + (GATED ? 0 : TN / 2 * (int)rank);
+            int term = t.c0 / max(1, p.chunks), k0 = (t.c0 - term * p.chunks) * kStep;
+            for (int c = t.c0; c < t.c1; ++c) {
+                if (!warp_wait_all(bar(kBarEmpty + s), phase, guard, lane)) {
+                    ok = false;
+                    break;
+                }
+                if (elect_one()) {
                     const uint32_t sa = stages + s * S::kStageBytes, sb = sa + kABytes;
                     const uint32_t full = cluster_addr(bar(kBarFull + s), 0);
                     if (rank == 0) mbar_expect_tx(bar(kBarFull + s), 2 * S::kStageBytes);
-                    const int ra = t.m0 + 128 * (int)rank;
                     const CUtensorMap *ma = &p.a[GATED ? 0 : term];
                     if (p.a_across) {
                         tma_load_2d_pair(sa, ma, full, ra, k0);
@@ -338,7 +341,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     } else {
                         tma_load_2d_pair(sa, ma, full, k0, ra);
                     }
-                    const int rb = t.n0 + (GATED ? 0 : TN / 2 * (int)rank);
                     const CUtensorMap *mb = &p.b[GATED ? (int)rank : term];
                     if (p.b_across) {
 #pragma unroll
@@ -347,48 +349,65 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         tma_load_2d_pair(sb, mb, full, k0, rb);
                     }
                 }
-            }
-            if (!ok) {  // copies in flight land within microseconds: leave them a millisecond
-                const uint64_t t0 = global_timer_ns();
-                while (global_timer_ns() - t0 < 1000000u) {
+                __syncwarp();
+                k0 += kStep;
+                if (k0 >= p.K) {
+                    k0 = 0;
+                    ++term;
                 }
+                if (++s == S::kStages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+        if (!ok) {  // copies in flight land within microseconds: leave them a millisecond
+            const uint64_t t0 = global_timer_ns();
+            while (global_timer_ns() - t0 < 1000000u) {
             }
         }
         __syncwarp();
     } else if (warp == 1 && rank == 0) {
-        if (lane == 0) {
-            // ------------------------------------------------ MMA issuer
-            const uint32_t idesc = make_idesc_major(kTileM, TN, F16, p.a_across != 0, p.b_across != 0);
-            const uint64_t da = p.a_across ? sw128_desc_across(stages, 64 * 128) : sw128_desc(stages);
-            const uint64_t db = p.b_across ? sw128_desc_across(stages + kABytes, 64 * 128) : sw128_desc(stages + kABytes);
-            // 16 contraction steps: 32 bytes along a K-major row, 16 rows of an MN-major box
-            const uint64_t step_a = p.a_across ? 2048 >> 4 : 32 >> 4, step_b = p.b_across ? 2048 >> 4 : 32 >> 4;
-            const int last_steps = (p.K - (p.chunks - 1) * kStep + 15) / 16;
-            bool ok = true;
-            int it = 0, tile = 0;
-            for (int u = pair; ok && u < units; u += pairs, ++tile) {
-                const Unit t = unit_of(p, u, kCols);
-                const int ab = tile & 1;
-                if (tile >= 2 && !wait_bounded(bar(kBarAccEmpty + ab), (uint32_t)(tile / 2 - 1) & 1u, guard)) break;
+        // ------------------------------------------------------ MMA issuer
+        const uint32_t idesc = make_idesc_major(kTileM, TN, F16, p.a_across != 0, p.b_across != 0);
+        const uint64_t da = p.a_across ? sw128_desc_across(stages, 64 * 128) : sw128_desc(stages);
+        const uint64_t db = p.b_across ? sw128_desc_across(stages + kABytes, 64 * 128) : sw128_desc(stages + kABytes);
+        // 16 contraction steps: 32 bytes along a K-major row, 16 rows of an MN-major box
+        const uint64_t step_a = p.a_across ? 2048 >> 4 : 32 >> 4, step_b = p.b_across ? 2048 >> 4 : 32 >> 4;
+        bool ok = true;
+        int s = 0, tile = 0;
+        uint32_t phase = 0;
+        for (int u = pair; ok && u < units; u += pairs, ++tile) {
+            const Unit t = unit_of(p, u, kCols);
+            const int ab = tile & 1;
+            if (tile >= 2 && !warp_wait_all(bar(kBarAccEmpty + ab), (uint32_t)(tile / 2 - 1) & 1u, guard, lane)) break;
+            tc_fence_after();
+            const uint32_t acc = tmem + (uint32_t)(ab * TN);
+            for (int c = t.c0; c < t.c1; ++c) {
+                if (!warp_wait_all(bar(kBarFull + s), phase, guard, lane)) {
+                    ok = false;
+                    break;
+                }
                 tc_fence_after();
-                const uint32_t acc = tmem + (uint32_t)(ab * TN);
-                for (int c = t.c0; c < t.c1; ++c, ++it) {
-                    const int s = it % S::kStages;
-                    if (!wait_bounded(bar(kBarFull + s), (uint32_t)(it / S::kStages) & 1u, guard)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
+                if (elect_one()) {
                     const uint64_t off = (uint64_t)(s * S::kStageBytes) >> 4;
-                    const int steps = (c + 1) % p.chunks == 0 ? last_steps : kStep / 16;
-                    for (int i = 0; i < steps; ++i)
+#pragma unroll
+                    for (int i = 0; i < kStep / 16; ++i)
                         mma_pair(acc, da + off + i * step_a, db + off + i * step_b, idesc,
-                                 (c > t.c0 || i > 0) ? 1u : 0u);
+                                 (i > 0 || c > t.c0) ? 1u : 0u);
                     mma_commit_pair(bar(kBarEmpty + s));
                 }
-                if (ok) mma_commit_pair(bar(kBarAccFull + ab));
+                __syncwarp();
+                if (++s == S::kStages) {
+                    s = 0;
+                    phase ^= 1;
+                }
             }
-            // every MMA issued completes before TMEM is released
+            if (ok && elect_one()) mma_commit_pair(bar(kBarAccFull + ab));
+            __syncwarp();
+        }
+        // every MMA issued completes before TMEM is released
+        if (elect_one()) {
             mma_commit_pair(bar(kBarDrain));
             const uint64_t t0 = global_timer_ns();
             while (!mbar_try_wait(bar(kBarDrain), 0u) && (int64_t)(global_timer_ns() - t0) < p.timeout_ns) {

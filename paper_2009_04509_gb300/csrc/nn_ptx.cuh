@@ -18,6 +18,21 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// One lane of the converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
+// The whole warp waits for the phase; all lanes take the same path.
+__device__ __forceinline__ bool warp_wait_all(uint32_t bar, uint32_t parity, const Guard &g, int lane) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return warp_wait(bar, parity, g, lane);
+}
 // The address of another CTA's copy of a shared-memory object.
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
     uint32_t r;
