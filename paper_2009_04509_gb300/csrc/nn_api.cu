@@ -102,31 +102,48 @@ struct CallSpace {
 // checkpoint, or rows off the 16-byte grid): each gets a copy in the workspace.
 struct Staging {
     CallSpace &ws;
-    struct Copy {
-        emtk_matrix from, to;
-        int rows, cols;
-    } copies[4];
+    Copy16 copies[kMaxCopies];
     int n = 0;
     emtk_matrix operator()(const emtk_matrix &m, int rows, int cols);
-    cudaError_t run(emtk_type type, int sms, cudaStream_t s) const {
-        cudaError_t e = cudaSuccess;
-        for (int i = 0; i < n && e == cudaSuccess; ++i)
-            e = launch_copy16(type, copies[i].rows, copies[i].cols, copies[i].from, copies[i].to, sms, s);
-        return e;
-    }
 };
 
 int64_t ld16(int64_t cols) { return (cols + 7) / 8 * 8; }  // rows of 16-byte multiples
 
 emtk_matrix Staging::operator()(const emtk_matrix &m, int rows, int cols) {
     if (rows == 0 || cols == 0 || (!m.d_scale && mm_operand_ok(m.d, m.ld, rows))) return m;
-    Copy &c = copies[n++];
+    Copy16 &c = copies[n++];
     c = {m, {ws.take(2 * (size_t)rows * ld16(cols)), ld16(cols), nullptr, 0}, rows, cols};
     return c.to;
 }
 
 MmOperand rows_of(const emtk_matrix &m) { return {m.d, m.ld, false}; }
 MmOperand cols_of(const emtk_matrix &m) { return {m.d, m.ld, true}; }
+
+// The forward pass of a layer: x [M][K] and one or two weights [N][K].
+emtk_status forward(emtk_nn *nn, MmJob &j, const emtk_matrix &x, const emtk_matrix *w, cudaStream_t s) {
+    const int nw = j.kind == kMmGated ? 2 : 1;
+    j.terms = 1;
+    j.a[0] = rows_of(x);
+    for (int i = 0; i < nw; ++i) j.b[i] = rows_of(w[i]);
+    if (few_rows(j)) return status_of(launch_rows(j, s));
+    const MmPlan plan = plan_mm(&j, 1, nn->sm_count);
+    CallSpace ws{nn};
+    Staging stage{ws};
+    void *partial = nullptr;
+    for (int pass = 0; pass < 2; ++pass) {
+        stage.n = 0;
+        j.a[0] = rows_of(stage(x, j.M, j.K));
+        for (int i = 0; i < nw; ++i) j.b[i] = rows_of(stage(w[i], j.N, j.K));
+        partial = ws.take(plan.workspace);
+        if (pass == 0) {
+            const emtk_status st = ws.ensure(s);
+            if (st != EMTK_OK) return st;
+        }
+    }
+    cudaError_t e = launch_copy16(j.type, stage.copies, stage.n, nn->sm_count, s);
+    if (e == cudaSuccess) e = launch_mm(&j, 1, plan, nn, partial, s);
+    return status_of(e);
+}
 
 }  // namespace
 
@@ -216,30 +233,13 @@ emtk_status emtk_dense(emtk_nn *nn, const emtk_dense_args *p, emtk_stream stream
     j.M = a.m;
     j.N = a.n;
     j.K = a.k;
-    j.terms = 1;
     j.epi.act = a.act;
     j.epi.bias[0] = a.bias;
     j.epi.bias_f32 = a.bias_type == EMTK_TYPE_F32;
     j.epi.residual = a.residual;
     j.epi.out = a.y;
     j.epi.saved[0] = a.pre;
-    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    CallSpace ws{nn};
-    Staging stage{ws};
-    void *partial = nullptr;
-    for (int pass = 0; pass < 2; ++pass) {
-        stage.n = 0;
-        j.a[0] = rows_of(stage(a.x, a.m, a.k));
-        j.b[0] = rows_of(stage(a.w, a.n, a.k));
-        partial = ws.take(mm_workspace(j, nn->sm_count));
-        if (pass == 0) {
-            const emtk_status st = ws.ensure(s);
-            if (st != EMTK_OK) return st;
-        }
-    }
-    cudaError_t e = stage.run(j.type, nn->sm_count, s);
-    if (e == cudaSuccess) e = launch_mm(j, nn, partial, s);
-    return status_of(e);
+    return forward(nn, j, a.x, &a.w, reinterpret_cast<cudaStream_t>(stream));
 }
 
 emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk_stream stream) {
@@ -266,17 +266,30 @@ emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk
     const bool own_dz = a.act != EMTK_ACT_NONE && (dx || dw);
     CallSpace ws{nn};
     Staging stage{ws};
-    MmJob jx{}, jw{};
-    jx.kind = jw.kind = kMmSum;
-    jx.type = jw.type = type;
-    jx.terms = jw.terms = 1;
-    jx.M = a.m;
-    jx.N = jw.N = a.k;
-    jx.K = jw.M = a.n;
-    jw.K = a.m;
-    jx.epi.out = a.dx;
-    jw.epi.out = a.dw;
-    jw.epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
+    MmJob jobs[2]{};
+    int n = 0;
+    for (MmJob &j : jobs) {
+        j.kind = kMmSum;
+        j.type = type;
+        j.terms = 1;
+        j.N = a.k;
+    }
+    MmJob &jx = jobs[n], &jw = jobs[n + (dx ? 1 : 0)];
+    if (dx) {
+        jx.M = a.m;
+        jx.K = a.n;
+        jx.epi.out = a.dx;
+        ++n;
+    }
+    if (dw) {
+        jw.M = a.n;
+        jw.K = a.m;
+        jw.epi.out = a.dw;
+        jw.epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
+        ++n;
+    }
+    MmPlan plan{};
+    if (n > 0) plan = plan_mm(jobs, n, nn->sm_count);
     emtk_matrix dz{};
     float *sums = nullptr;
     void *partial = nullptr;
@@ -284,20 +297,17 @@ emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk
         stage.n = 0;
         if (own_dz)
             dz = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.n)), ld16(a.n), nullptr, 0};
-        else if (dx || dw)
+        else if (n > 0)
             dz = stage(a.dy, a.m, a.n);
-        size_t part = 0;
         if (dx) {
             jx.a[0] = rows_of(dz);
             jx.b[0] = cols_of(stage(a.w, a.n, a.k));
-            part = mm_workspace(jx, nn->sm_count);
         }
         if (dw) {
             jw.a[0] = cols_of(dz);
             jw.b[0] = cols_of(stage(a.x, a.m, a.k));
-            part = std::max(part, mm_workspace(jw, nn->sm_count));
         }
-        partial = ws.take(part);
+        partial = ws.take(plan.workspace);
         if (a.db) sums = static_cast<float *>(ws.take(4 * (size_t)slope_slices(a.m, a.n, nn->sm_count) * a.n));
         if (pass == 0) {
             const emtk_status st = ws.ensure(s);
@@ -308,9 +318,8 @@ emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk
     if (own_dz || a.db)
         e = launch_slope(type, a.act, a.m, a.n, a.dy, a.pre, own_dz ? dz.d : nullptr, dz.ld, a.db, sums,
                          nn->sm_count, s);
-    if (e == cudaSuccess) e = stage.run(type, nn->sm_count, s);
-    if (e == cudaSuccess && dx) e = launch_mm(jx, nn, partial, s);
-    if (e == cudaSuccess && dw) e = launch_mm(jw, nn, partial, s);
+    if (e == cudaSuccess) e = launch_copy16(type, stage.copies, stage.n, nn->sm_count, s);
+    if (e == cudaSuccess && n > 0) e = launch_mm(jobs, n, plan, nn, partial, s);
     return status_of(e);
 }
 
@@ -339,7 +348,6 @@ emtk_status emtk_gated(emtk_nn *nn, const emtk_gated_args *p, emtk_stream stream
     j.M = a.m;
     j.N = a.f;
     j.K = a.k;
-    j.terms = 1;
     j.epi.act = a.act;
     j.epi.bias[0] = a.bias_gate;
     j.epi.bias[1] = a.bias_up;
@@ -347,24 +355,8 @@ emtk_status emtk_gated(emtk_nn *nn, const emtk_gated_args *p, emtk_stream stream
     j.epi.out = a.h;
     j.epi.saved[0] = a.gate;
     j.epi.saved[1] = a.up;
-    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    CallSpace ws{nn};
-    Staging stage{ws};
-    void *partial = nullptr;
-    for (int pass = 0; pass < 2; ++pass) {
-        stage.n = 0;
-        j.a[0] = rows_of(stage(a.x, a.m, a.k));
-        j.b[0] = rows_of(stage(a.w_gate, a.f, a.k));
-        j.b[1] = rows_of(stage(a.w_up, a.f, a.k));
-        partial = ws.take(mm_workspace(j, nn->sm_count));
-        if (pass == 0) {
-            const emtk_status st = ws.ensure(s);
-            if (st != EMTK_OK) return st;
-        }
-    }
-    cudaError_t e = stage.run(j.type, nn->sm_count, s);
-    if (e == cudaSuccess) e = launch_mm(j, nn, partial, s);
-    return status_of(e);
+    const emtk_matrix w[2] = {a.w_gate, a.w_up};
+    return forward(nn, j, a.x, w, reinterpret_cast<cudaStream_t>(stream));
 }
 
 emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk_stream stream) {
@@ -398,27 +390,38 @@ emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk
     const bool dx = a.dx.d && a.m > 0 && a.k > 0, dw = a.dw_gate.d && a.f > 0 && a.k > 0;
     CallSpace ws{nn};
     Staging stage{ws};
-    MmJob jx{}, jw[2]{};
-    jx.kind = jw[0].kind = kMmSum;
-    jx.type = jw[0].type = type;
-    jx.terms = 2;
-    jw[0].terms = 1;
-    jx.M = a.m;
-    jx.N = jw[0].N = a.k;
-    jx.K = jw[0].M = a.f;
-    jw[0].K = a.m;
-    jx.epi.out = a.dx;
-    jw[0].epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
-    jw[1] = jw[0];
-    jw[0].epi.out = a.dw_gate;
-    jw[1].epi.out = a.dw_up;
+    MmJob jobs[3]{};
+    int n = 0;
+    for (MmJob &j : jobs) {
+        j.kind = kMmSum;
+        j.type = type;
+        j.terms = 1;
+        j.N = a.k;
+    }
+    MmJob &jx = jobs[0];
+    MmJob *const jw = jobs + (dx ? 1 : 0);  // of w_gate and w_up
+    if (dx) {
+        jx.terms = 2;
+        jx.M = a.m;
+        jx.K = a.f;
+        jx.epi.out = a.dx;
+        ++n;
+    }
+    for (int w = 0; w < 2 && dw; ++w) {
+        jw[w].M = a.f;
+        jw[w].K = a.m;
+        jw[w].epi.out = w ? a.dw_up : a.dw_gate;
+        jw[w].epi.out_f32 = a.dw_type == EMTK_TYPE_F32;
+        ++n;
+    }
+    MmPlan plan{};
+    if (n > 0) plan = plan_mm(jobs, n, nn->sm_count);
     emtk_matrix dg{}, du{};
     float *sums = nullptr;
     void *partial = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
         stage.n = 0;
-        size_t part = 0;
-        if (dx || dw) {
+        if (n > 0) {
             dg = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.f)), ld16(a.f), nullptr, 0};
             du = emtk_matrix{ws.take(2 * (size_t)a.m * ld16(a.f)), ld16(a.f), nullptr, 0};
         }
@@ -427,15 +430,13 @@ emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk
             jx.a[1] = rows_of(du);
             jx.b[0] = cols_of(stage(a.w_gate, a.f, a.k));
             jx.b[1] = cols_of(stage(a.w_up, a.f, a.k));
-            part = mm_workspace(jx, nn->sm_count);
         }
         if (dw) {
             jw[0].a[0] = cols_of(dg);
             jw[1].a[0] = cols_of(du);
             jw[0].b[0] = jw[1].b[0] = cols_of(stage(a.x, a.m, a.k));
-            part = std::max(part, mm_workspace(jw[0], nn->sm_count));
         }
-        partial = ws.take(part);
+        partial = ws.take(plan.workspace);
         if (a.db_gate) sums = static_cast<float *>(ws.take(8 * (size_t)slope_slices(a.m, a.f, nn->sm_count) * a.f));
         if (pass == 0) {
             const emtk_status st = ws.ensure(s);
@@ -443,12 +444,11 @@ emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk
         }
     }
     cudaError_t e = cudaSuccess;
-    if (dx || dw || a.db_gate || a.h.d)
+    if (n > 0 || a.db_gate || a.h.d)
         e = launch_gated_slope(type, a.act, a.m, a.f, a.dh, a.gate, a.up, dg.d, du.d, ld16(a.f), a.h, a.db_gate,
                                a.db_up, sums, nn->sm_count, s);
-    if (e == cudaSuccess) e = stage.run(type, nn->sm_count, s);
-    if (e == cudaSuccess && dx) e = launch_mm(jx, nn, partial, s);
-    for (int w = 0; w < 2 && e == cudaSuccess && dw; ++w) e = launch_mm(jw[w], nn, partial, s);
+    if (e == cudaSuccess) e = launch_copy16(type, stage.copies, stage.n, nn->sm_count, s);
+    if (e == cudaSuccess && n > 0) e = launch_mm(jobs, n, plan, nn, partial, s);
     return status_of(e);
 }
 
@@ -477,7 +477,8 @@ emtk_status emtk_unpack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type type, cons
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk unpack8");
-    return status_of(launch_copy16(type, m, k, *q, *x, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+    const Copy16 copy{*q, *x, m, k};
+    return status_of(launch_copy16(type, &copy, 1, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -59,10 +59,23 @@ struct MmJob {
 // Whether a matrix of 16-bit elements can be an operand as it lies: TMA wants
 // its address and row distance on 16 bytes.  (Others are copied first.)
 bool mm_operand_ok(const void *p, int64_t ld, int64_t rows);
-// Bytes that `partial` of launch_mm needs (256-byte aligned).
-size_t mm_workspace(const MmJob &job, int sms);
-cudaError_t launch_mm(const MmJob &job, const emtk_nn *nn, void *partial, cudaStream_t s);
+// Up to kMaxJobs jobs of one kind and type in one launch (nn_mm.cu); the plan
+// says how they are cut, and how much workspace `partial` it needs.
+constexpr int kMaxJobs = 3;
+struct MmPlan {
+    int tn, pairs, units;
+    struct Cut {
+        int tiles_m, tiles_n, chunks, parts, chunks_per_part, units;
+        int64_t part_ld, part_elems, part_at;
+    } cut[kMaxJobs];
+    size_t workspace;
+};
+MmPlan plan_mm(const MmJob *jobs, int n, int sms);
+cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_nn *nn, void *partial, cudaStream_t s);
 cudaError_t init_mm_kernels();  // once per device
+// The forward pass of 1 to 4 rows (nn_rows.cu), operands anywhere.
+bool few_rows(const MmJob &job);
+cudaError_t launch_rows(const MmJob &job, cudaStream_t s);
 
 // ---- pointwise passes (nn_pointwise.cu)
 // dz = dy act'(pre) as a 16-bit matrix dz (or none), and its column sums db
@@ -76,8 +89,13 @@ cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk
                                float *db_gate, float *db_up, float *partial, int sms, cudaStream_t s);
 cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
                          cudaStream_t s);
-// x = the values of src: a checkpoint, or a 16-bit matrix copied as it is.
-cudaError_t launch_copy16(emtk_type type, int m, int k, const emtk_matrix &src, const emtk_matrix &x, int sms,
-                          cudaStream_t s);
+// to = the values of from (a checkpoint, or a 16-bit matrix as it is), for up
+// to kMaxCopies matrices in one launch.
+constexpr int kMaxCopies = 4;
+struct Copy16 {
+    emtk_matrix from, to;
+    int rows, cols;
+};
+cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, cudaStream_t s);
 
 }  // namespace emtk

@@ -32,54 +32,72 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     return d;
 }
 
+// exp(z) and 1 / v to 2 ulp with flushed subnormals; exp overflows to infinity,
+// whose reciprocal is 0.
+__device__ __forceinline__ float exp_f(float z) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(z * 1.4426950408889634f));
+    return r;
+}
+__device__ __forceinline__ float reciprocal_f(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
 // 1 / (1 + exp(-z)): 0 where exp(-z) overflows (z < -88), the limit.
-__device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float sigmoid_f(float z) { return reciprocal_f(1.f + exp_f(-z)); }
 
-__device__ __forceinline__ float act_f(int act, float z) {
-    switch (act) {
-        case EMTK_ACT_RELU: return z > 0.f ? z : (z == z ? 0.f : z);  // NaN stays
-        case EMTK_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        case EMTK_ACT_SILU: return z * sigmoid_f(z);
-        case EMTK_ACT_SIGMOID: return sigmoid_f(z);
-        default: return z;
-    }
+template <int ACT>
+__device__ __forceinline__ float act_of(float z) {
+    if (ACT == EMTK_ACT_RELU) return z > 0.f ? z : (z == z ? 0.f : z);  // NaN stays
+    if (ACT == EMTK_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if (ACT == EMTK_ACT_SILU) return z * sigmoid_f(z);
+    if (ACT == EMTK_ACT_SIGMOID) return sigmoid_f(z);
+    return z;
 }
 
 // act(z) and act'(z), which share their transcendental.
-__device__ __forceinline__ void act_slope(int act, float z, float &a, float &d) {
+template <int ACT>
+__device__ __forceinline__ void act_slope(float z, float &a, float &d) {
+    a = z;
+    d = 1.f;
+    if (ACT == EMTK_ACT_RELU) {
+        a = act_of<ACT>(z);
+        d = z > 0.f ? 1.f : (z == z ? 0.f : z);
+    } else if (ACT == EMTK_ACT_GELU) {
+        const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+        a = z * p;
+        d = p + z * exp_f(-0.5f * z * z) * 0.39894228040143268f;
+    } else if (ACT == EMTK_ACT_SILU) {
+        const float p = sigmoid_f(z);
+        a = z * p;
+        d = p * (1.f + z * (1.f - p));
+    } else if (ACT == EMTK_ACT_SIGMOID) {
+        const float p = sigmoid_f(z);
+        a = p;
+        d = p * (1.f - p);
+    }
+}
+
+// act of every element, the choice made once.
+template <int N>
+__device__ __forceinline__ void apply_act(int act, float (&v)[N]) {
     switch (act) {
-        case EMTK_ACT_RELU:
-            a = z > 0.f ? z : (z == z ? 0.f : z);
-            d = z > 0.f ? 1.f : (z == z ? 0.f : z);
-            break;
-        case EMTK_ACT_GELU: {
-            const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
-            a = z * p;
-            d = p + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
-            break;
-        }
-        case EMTK_ACT_SILU: {
-            const float p = sigmoid_f(z);
-            a = z * p;
-            d = p * (1.f + z * (1.f - p));
-            break;
-        }
-        case EMTK_ACT_SIGMOID: {
-            const float p = sigmoid_f(z);
-            a = p;
-            d = p * (1.f - p);
-            break;
-        }
-        default: a = z; d = 1.f;
+#define EMTK_ACT_CASE(A)                                      \
+    case A: {                                                 \
+        _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = act_of<A>(v[i]); \
+        break;                                                \
+    }
+        EMTK_ACT_CASE(EMTK_ACT_RELU)
+        EMTK_ACT_CASE(EMTK_ACT_GELU)
+        EMTK_ACT_CASE(EMTK_ACT_SILU)
+        EMTK_ACT_CASE(EMTK_ACT_SIGMOID)
+#undef EMTK_ACT_CASE
+        default: break;
     }
 }
 
 // ---- 8-bit checkpoints (emtk_matrix in include/emtk.h)
-// |v| if finite, else 0: what the block maximum is taken over.
-__device__ __forceinline__ float finite_abs(float v) {
-    const float a = fabsf(v);
-    return a < __int_as_float(0x7f800000) ? a : 0.f;
-}
 // Scale byte of a block whose largest finite magnitude is `top`: with
 // 2^(byte - 127) <= top / 64 < 2^(byte - 126) the quotient is in [64, 128);
 // from 127.5 on (mantissa bits 0x7f0000 and up) it would round to 128, so
@@ -90,13 +108,53 @@ __device__ __forceinline__ uint32_t q8_scale(float top) {
 }
 __device__ __forceinline__ float q8_step(uint32_t b) { return __uint_as_float(b << 23); }         // 2^(b - 127)
 __device__ __forceinline__ float q8_inverse(uint32_t b) { return __uint_as_float((254u - b) << 23); }  // b <= 249
-__device__ __forceinline__ uint32_t q8_code(float v, float inverse) {
-    const uint32_t q = (uint32_t)__float2int_rn(v * inverse) & 0xffu;
-    return fabsf(v) < __int_as_float(0x7f800000) ? q : 0x80u;
+
+// The largest finite magnitude of N values, and whether any is not finite: v * 0
+// is NaN exactly then, and stays NaN in the sum.
+template <int N>
+__device__ __forceinline__ float finite_top(const float (&v)[N], bool &all_finite) {
+    float top = 0.f, zero = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        top = fmaxf(top, fabsf(v[i]));
+        zero = fmaf(v[i], 0.f, zero);
+    }
+    all_finite = zero == 0.f;
+    if (!all_finite) {  // rare
+        top = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(v[i]) < __int_as_float(0x7f800000) ? fabsf(v[i]) : 0.f);
+    }
+    return top;
 }
-__device__ __forceinline__ float q8_value(uint32_t byte, float step) {
-    const int q = (int)(int8_t)byte;
-    return q == -128 ? __int_as_float(0x7fffffff) : (float)q * step;
+// Codes of four values in one word.  Adding 1.5 * 2^23 rounds v / step (at most
+// 127 in magnitude) to a whole number, ties to even, in the low mantissa bits:
+// the quotient by a power of two is exact and the addition rounds once.
+__device__ __forceinline__ uint32_t q8_codes4(const float *v, float inverse, bool all_finite) {
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(fmaf(v[i], inverse, 12582912.f));
+    uint32_t w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+    if (!all_finite) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (!(fabsf(v[i]) < __int_as_float(0x7f800000))) w = (w & ~(0xffu << (8 * i))) | (0x80u << (8 * i));
+    }
+    return w;
+}
+// Values of the four codes of a word.  A byte with its sign bit flipped is code +
+// 128; below the bits of 2^23 it is 2^23 + 128 + code, from which a subtraction and
+// a product by the power of two leave the value, both exact.
+__device__ __forceinline__ void q8_values4(uint32_t w, float step, float *v) {
+    const uint32_t x = w ^ 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = (__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440 + i)) - 8388736.f) * step;
+    if ((x - 0x01010101u) & ~x & 0x80808080u) {  // some byte of x is 0: code -128, rare
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (((x >> (8 * i)) & 0xffu) == 0) v[i] = __int_as_float(0x7fffffff);
+    }
 }
 // The value as an operand of the products: bf16 holds it exactly, fp16 saturates.
 template <bool F16>

@@ -21,6 +21,7 @@
 // applies the epilogue, so results do not depend on timing.
 #include <algorithm>
 
+#include "emtk_internal.h"
 #include "nn_internal.h"
 #include "nn_math.cuh"
 #include "nn_ptx.cuh"
@@ -48,38 +49,49 @@ struct Shape {
     static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpiWarps * (kStageRowsBytes + kBiasBytes) + 512;
 };
 
-struct MmParams {
+struct MmWork {  // one job
     CUtensorMap a[2], b[2];
     MmEpilogue epi;
     float *partial;  // not null: sums of part p to partial + p * part_elems, rows of part_ld
     int64_t part_elems, part_ld;
     int M, N, K;
-    int terms, a_across, b_across;
+    int a_across, b_across;
     int tiles_m, tiles_n, parts;
-    int chunks;            // of one term
+    int chunks, total;     // of one term, of all
     int chunks_per_part;
+    int unit_end;          // units of this job and those before it
+};
+struct MmParams {
+    MmWork job[kMaxJobs];
+    int jobs;
     int *status;
     int64_t timeout_ns;
     int debug_stall;
 };
 
 struct Unit {
-    int m0, n0, part, c0, c1;
+    int job, m0, n0, part, c0, c1;
 };
 
-// Unit u of the launch: tiles in groups of 8 tile rows, along the rows first, so
-// that the pairs at work share operand panels in L2; a tile's parts are adjacent.
+// Unit u of the launch: jobs in order, a job's tiles in groups of 8 tile rows,
+// along the rows first, so that the pairs at work share operand panels in L2; a
+// tile's parts are adjacent.
 __device__ __forceinline__ Unit unit_of(const MmParams &p, int u, int cols) {
-    const int t = u / p.parts;
     Unit r;
-    r.part = u - t * p.parts;
-    const int group = t / (8 * p.tiles_n);
-    const int rows = min(8, p.tiles_m - 8 * group);
-    const int in = t - group * 8 * p.tiles_n;
+    r.job = 0;
+    int begin = 0;
+    while (u >= p.job[r.job].unit_end) begin = p.job[r.job++].unit_end;
+    const MmWork &w = p.job[r.job];
+    u -= begin;
+    const int t = u / w.parts;
+    r.part = u - t * w.parts;
+    const int group = t / (8 * w.tiles_n);
+    const int rows = min(8, w.tiles_m - 8 * group);
+    const int in = t - group * 8 * w.tiles_n;
     r.m0 = (8 * group + in % rows) * kTileM;
     r.n0 = in / rows * cols;
-    r.c0 = r.part * p.chunks_per_part;
-    r.c1 = min(r.c0 + p.chunks_per_part, p.chunks * p.terms);
+    r.c0 = r.part * w.chunks_per_part;
+    r.c1 = min(r.c0 + w.chunks_per_part, w.total);
     return r;
 }
 
@@ -95,7 +107,17 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
                                            bool wide, uint8_t *stage, int lane) {
     constexpr int kPiece = 16 / sizeof(T), kCols = 64 / sizeof(T);
     const int nr = (int)min((int64_t)32, rows - r0), nc = (int)min((int64_t)kCols, cols - c0);
-    if (wide) {
+    if (wide && nr == 32 && nc == kCols) {  // a whole block: four unconditional 16-byte moves a lane
+        T *g = base + (r0 + (lane >> 2)) * ld + c0 + (lane & 3) * kPiece;
+        uint8_t *s = stage + (lane >> 2) * kRowBytes + (lane & 3) * 16;
+#pragma unroll
+        for (int it = 0; it < 4; ++it, g += 8 * ld, s += 8 * kRowBytes) {
+            if (LOAD)
+                *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
+            else
+                *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(s);
+        }
+    } else if (wide) {
         const int c = (lane & 3) * kPiece;
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
@@ -174,25 +196,26 @@ __device__ __forceinline__ void store32(float *base, int64_t ld, const Rows &w, 
 __device__ __forceinline__ void store_q8(const emtk_matrix &m, const Rows &w, int64_t c0, int64_t cols,
                                          const float (&v)[32]) {
     const int nc = (int)min((int64_t)32, cols - c0);
-    float top = 0.f;
+    float x[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, i < nc ? finite_abs(v[i]) : 0.f);
-    const uint32_t b = q8_scale(top);
+    for (int i = 0; i < 32; ++i) x[i] = i < nc ? v[i] : 0.f;
+    bool all_finite;
+    const uint32_t b = q8_scale(finite_top(x, all_finite));
     const float inverse = q8_inverse(b);
     const int64_t r = w.r0 + w.lane;
     if (r >= w.rows) return;
     m.d_scale[r * m.ld_scale + c0 / kQ8Block] = (uint8_t)b;
     uint8_t *p = static_cast<uint8_t *>(m.d) + r * m.ld + c0;
-    if (nc == 32 && wide_rows(m.d, m.ld, 1)) {
-        uint32_t q[8] = {};
+    uint32_t q[8];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) q[i / 4] |= q8_code(v[i], inverse) << (8 * (i % 4));
+    for (int i = 0; i < 8; ++i) q[i] = q8_codes4(x + 4 * i, inverse, all_finite);
+    if (nc == 32 && wide_rows(m.d, m.ld, 1)) {
         reinterpret_cast<uint4 *>(p)[0] = make_uint4(q[0], q[1], q[2], q[3]);
         reinterpret_cast<uint4 *>(p)[1] = make_uint4(q[4], q[5], q[6], q[7]);
     } else {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-            if (i < nc) p[i] = (uint8_t)q8_code(v[i], inverse);
+            if (i < nc) p[i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
     }
 }
 
@@ -213,17 +236,24 @@ __device__ __forceinline__ float bias_at(const MmEpilogue &e, int which, int64_t
                       : from16<F16>(__ldg(static_cast<const uint16_t *>(e.bias[which]) + n));
 }
 
+__device__ __forceinline__ void add_bias(const float *bias, float (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float4 b = reinterpret_cast<const float4 *>(bias)[i];
+        v[4 * i] += b.x;
+        v[4 * i + 1] += b.y;
+        v[4 * i + 2] += b.z;
+        v[4 * i + 3] += b.w;
+    }
+}
+
 // Sums of a dense tile's 32 columns (z without its bias, which is in `bias`).
 template <bool F16>
 __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
                                              const float *bias, float (&v)[32]) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] += bias[i];
+    if (e.bias[0]) add_bias(bias, v);
     store_saved<F16>(e.saved[0], w, c0, cols, v);
-    if (e.act != EMTK_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = act_f(e.act, v[i]);
-    }
+    apply_act(e.act, v);
     if (e.residual.d) {
         move_block<uint16_t, true>(static_cast<uint16_t *>(e.residual.d), e.residual.ld, w.r0, w.rows, c0, cols,
                                    wide_rows(e.residual.d, e.residual.ld, 2), w.stage, w.lane);
@@ -251,15 +281,15 @@ template <bool F16>
 __device__ __forceinline__ void finish_gated(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
                                              const float *bias_g, const float *bias_u, float (&g)[32],
                                              float (&u)[32]) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        g[i] += bias_g[i];
-        u[i] += bias_u[i];
+    if (e.bias[0]) {
+        add_bias(bias_g, g);
+        add_bias(bias_u, u);
     }
     store_saved<F16>(e.saved[0], w, c0, cols, g);
     store_saved<F16>(e.saved[1], w, c0, cols, u);
+    apply_act(e.act, g);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) g[i] = act_f(e.act, g[i]) * u[i];
+    for (int i = 0; i < 32; ++i) g[i] *= u[i];
     store16<F16>(e.out, w, c0, cols, g);
 }
 
@@ -286,7 +316,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const uint32_t rank = cluster_rank();
     const Guard guard{abort_flag, p.status, p.timeout_ns};
     const int pair = (int)blockIdx.x / 2, pairs = (int)gridDim.x / 2;
-    const int units = p.tiles_m * p.tiles_n * p.parts;
+    const int units = p.job[p.jobs - 1].unit_end;
+
+    pdl_trigger();
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) {
@@ -308,23 +340,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    pdl_wait();
 
     if (warp == 0) {
         // ---------------------------------------------------- TMA producer
         // The warp runs the loop together and one lane issues (here and in the MMA
         // warp): descriptors and addresses stay in uniform registers.
-        if (p.chunks > 0 && elect_one()) {
-            for (int i = 0; i < p.terms; ++i) prefetch_map(&p.a[i]);
-            for (int i = 0; i < (GATED ? 2 : p.terms); ++i) prefetch_map(&p.b[i]);
-        }
-        __syncwarp();
         bool ok = !(p.debug_stall && !warp_wait(bar(kBarStall), 0u, guard, lane));
+        const uint32_t full0 = cluster_addr(bar(kBarFull), 0);
         int s = 0;
         uint32_t phase = 1;  // a fresh barrier's previous phase counts as complete
         for (int u = pair; ok && u < units; u += pairs) {
             const Unit t = unit_of(p, u, kCols);
             const int ra = t.m0 + 128 * (int)rank, rb = t.n0 + (GATED ? 0 : TN / 2 * (int)rank);
-            int term = t.c0 / max(1, p.chunks), k0 = (t.c0 - term * p.chunks) * kStep;
+            const MmWork &w = p.job[t.job];
+            int term = t.c0 / max(1, w.chunks), k0 = (t.c0 - term * w.chunks) * kStep;
             for (int c = t.c0; c < t.c1; ++c) {
                 if (!warp_wait_all(bar(kBarEmpty + s), phase, guard, lane)) {
                     ok = false;
@@ -332,17 +362,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 }
                 if (elect_one()) {
                     const uint32_t sa = stages + s * S::kStageBytes, sb = sa + kABytes;
-                    const uint32_t full = cluster_addr(bar(kBarFull + s), 0);
-                    if (rank == 0) mbar_expect_tx(bar(kBarFull + s), 2 * S::kStageBytes);
-                    const CUtensorMap *ma = &p.a[GATED ? 0 : term];
-                    if (p.a_across) {
+                    const uint32_t full = full0 + 8 * s;
+                    if (rank == 0) mbar_expect_tx_relaxed(bar(kBarFull + s), 2 * S::kStageBytes);
+                    const CUtensorMap *ma = &w.a[GATED ? 0 : term];
+                    if (w.a_across) {
                         tma_load_2d_pair(sa, ma, full, ra, k0);
                         tma_load_2d_pair(sa + 64 * 128, ma, full, ra + 64, k0);
                     } else {
                         tma_load_2d_pair(sa, ma, full, k0, ra);
                     }
-                    const CUtensorMap *mb = &p.b[GATED ? (int)rank : term];
-                    if (p.b_across) {
+                    const CUtensorMap *mb = &w.b[GATED ? (int)rank : term];
+                    if (w.b_across) {
 #pragma unroll
                         for (int j = 0; j < TN / 128; ++j) tma_load_2d_pair(sb + j * 64 * 128, mb, full, rb + 64 * j, k0);
                     } else {
@@ -351,7 +381,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 }
                 __syncwarp();
                 k0 += kStep;
-                if (k0 >= p.K) {
+                if (k0 >= w.K) {
                     k0 = 0;
                     ++term;
                 }
@@ -369,16 +399,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         __syncwarp();
     } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------ MMA issuer
-        const uint32_t idesc = make_idesc_major(kTileM, TN, F16, p.a_across != 0, p.b_across != 0);
-        const uint64_t da = p.a_across ? sw128_desc_across(stages, 64 * 128) : sw128_desc(stages);
-        const uint64_t db = p.b_across ? sw128_desc_across(stages + kABytes, 64 * 128) : sw128_desc(stages + kABytes);
-        // 16 contraction steps: 32 bytes along a K-major row, 16 rows of an MN-major box
-        const uint64_t step_a = p.a_across ? 2048 >> 4 : 32 >> 4, step_b = p.b_across ? 2048 >> 4 : 32 >> 4;
         bool ok = true;
         int s = 0, tile = 0;
         uint32_t phase = 0;
         for (int u = pair; ok && u < units; u += pairs, ++tile) {
             const Unit t = unit_of(p, u, kCols);
+            const MmWork &w = p.job[t.job];
+            const uint32_t idesc = make_idesc_major(kTileM, TN, F16, w.a_across != 0, w.b_across != 0);
+            const uint64_t da = w.a_across ? sw128_desc_across(stages, 64 * 128) : sw128_desc(stages);
+            const uint64_t db = w.b_across ? sw128_desc_across(stages + kABytes, 64 * 128) : sw128_desc(stages + kABytes);
+            // 16 contraction steps: 32 bytes along a K-major row, 16 rows of an MN-major box
+            const uint64_t step_a = w.a_across ? 2048 >> 4 : 32 >> 4, step_b = w.b_across ? 2048 >> 4 : 32 >> 4;
             const int ab = tile & 1;
             if (tile >= 2 && !warp_wait_all(bar(kBarAccEmpty + ab), (uint32_t)(tile / 2 - 1) & 1u, guard, lane)) break;
             tc_fence_after();
@@ -422,29 +453,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int q = e & 3, half = e >> 2;
         constexpr int kMine = kCols / 2;  // output columns of a warp
         float *const bias = epi_bias + e * (kBiasBytes / 4);
-        Rows w{0, p.M, epi_rows + e * kStageRowsBytes, lane};
+        Rows w{0, 0, epi_rows + e * kStageRowsBytes, lane};
         int tile = 0;
         for (int u = pair; u < units; u += pairs, ++tile) {
             const Unit t = unit_of(p, u, kCols);
+            const MmWork &job = p.job[t.job];
             const int ab = tile & 1;
+            w.rows = job.M;
             w.r0 = t.m0 + 128 * (int64_t)rank + 32 * q;
             const int64_t n0 = t.n0 + half * kMine;
             __syncwarp();
-            if (p.partial == nullptr) {
+            if (job.partial == nullptr && job.epi.bias[0]) {
                 for (int j = lane; j < kMine; j += 32) {
-                    bias[j] = bias_at<F16>(p.epi, 0, n0 + j, p.N);
-                    if (GATED) bias[kMine + j] = bias_at<F16>(p.epi, 1, n0 + j, p.N);
+                    bias[j] = bias_at<F16>(job.epi, 0, n0 + j, job.N);
+                    if (GATED) bias[kMine + j] = bias_at<F16>(job.epi, 1, n0 + j, job.N);
                 }
             }
             if (!warp_wait(bar(kBarAccFull + ab), (uint32_t)(tile / 2) & 1u, guard, lane)) break;
             tc_fence_after();
             const uint32_t acc = tmem + (uint32_t)(ab * TN) + ((uint32_t)(32 * q) << 16);
-            const bool rows_in = w.r0 < p.M;
+            const bool rows_in = w.r0 < job.M;
 #pragma unroll 1
             for (int j = 0; j < kMine; j += 32) {
                 const int64_t c0 = n0 + j;
                 float v[32], x[GATED ? 32 : 1];
-                const bool in = rows_in && c0 < p.N;
+                const bool in = rows_in && c0 < job.N;
                 if (in && t.c0 < t.c1) {
                     tmem_ld32(acc + (uint32_t)(half * kMine + j), v);
                     if constexpr (GATED) tmem_ld32(acc + (uint32_t)(TN / 2 + half * kMine + j), x);
@@ -461,15 +494,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (lane == 0) mbar_arrive_cluster(cluster_addr(bar(kBarAccEmpty + ab), 0));
                 }
                 if (!in) continue;
-                if (p.partial != nullptr) {
-                    float *part = p.partial + t.part * p.part_elems;
+                if (job.partial != nullptr) {
+                    float *part = job.partial + t.part * job.part_elems;
                     const int64_t pc = (int64_t)(t.n0 / kCols) * TN + half * kMine + j;
-                    store32(part, p.part_ld, w, pc, p.part_ld, v);
-                    if constexpr (GATED) store32(part, p.part_ld, w, pc + TN / 2, p.part_ld, x);
+                    store32(part, job.part_ld, w, pc, job.part_ld, v);
+                    if constexpr (GATED) store32(part, job.part_ld, w, pc + TN / 2, job.part_ld, x);
                 } else if constexpr (GATED) {
-                    finish_gated<F16>(p.epi, w, c0, p.N, bias + j, bias + kMine + j, v, x);
+                    finish_gated<F16>(job.epi, w, c0, job.N, bias + j, bias + kMine + j, v, x);
                 } else {
-                    finish_dense<F16>(p.epi, w, c0, p.N, bias + j, v);
+                    finish_dense<F16>(job.epi, w, c0, job.N, bias + j, v);
                 }
             }
         }
@@ -481,57 +514,75 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     if (warp == 2) tmem_free_pair(tmem, S::kTmemCols);
 }
 
-// Adds the parts' sums in order and applies the epilogue: a thread takes 8
-// columns of a row, four threads a checkpoint block.
+// Adds the parts' sums and applies the epilogue: 2^lanes_log2 neighbouring
+// threads (8 at most) take 8 columns of a row, each every so-manieth part, and
+// join their sums in a fixed tree; four such groups hold a checkpoint block.
 template <bool F16, bool GATED, int TN>
-__global__ void __launch_bounds__(256) parts_kernel(const MmEpilogue e, const float *partial, int64_t part_elems,
-                                                    int64_t part_ld, int parts, int M, int N, int groups) {
+__global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEpilogue e, const float *partial,
+                                                    int64_t part_elems, int64_t part_ld, int parts, int M, int N,
+                                                    int groups, int lanes_log2) {
     constexpr int kCols = GATED ? TN / 2 : TN;
-    const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;  // groups is a multiple of 4
+    const int64_t tid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int lanes = 1 << lanes_log2, mine = threadIdx.x & (lanes - 1);
+    const int64_t idx = tid >> lanes_log2;  // groups is a multiple of 4
     const int64_t r = idx / groups;
     const int c = (int)(idx - r * groups) * 8;
     const bool in = r < M && c < N;
     float v[GATED ? 2 : 1][8] = {};
+    pdl_trigger();
+    pdl_wait();
     if (in) {
 #pragma unroll
         for (int h = 0; h < (GATED ? 2 : 1); ++h) {
-            const float *p = partial + r * part_ld + (c / kCols) * TN + c % kCols + h * (TN / 2);
-            for (int i = 0; i < parts; ++i, p += part_elems) {
-                const float4 lo = __ldg(reinterpret_cast<const float4 *>(p));
-                const float4 hi = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+            const float *p = partial + mine * part_elems + r * part_ld + (c / kCols) * TN + c % kCols + h * (TN / 2);
+#pragma unroll 4
+            for (int i = mine; i < parts; i += lanes, p += lanes * part_elems) {
+                const float4 lo = *reinterpret_cast<const float4 *>(p);
+                const float4 hi = *(reinterpret_cast<const float4 *>(p) + 1);
                 const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[h][j] += x[j];
             }
+        }
+    }
+    for (int d = lanes >> 1; d > 0; d >>= 1)
+#pragma unroll
+        for (int h = 0; h < (GATED ? 2 : 1); ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[h][j] += __shfl_xor_sync(0xffffffffu, v[h][j], d);
+    const bool writes = in && mine == 0;
+#pragma unroll
+    for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+        if (in) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[h][j] += bias_at<F16>(e, h, c + j, N);
         }
-    }
-#pragma unroll
-    for (int h = 0; h < (GATED ? 2 : 1); ++h) {
         const emtk_matrix &m = e.saved[h];
         if (m.d == nullptr) continue;
         if (m.d_scale) {
-            float top = 0.f;
+            float x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, in && c + j < N ? finite_abs(v[h][j]) : 0.f);
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            for (int j = 0; j < 8; ++j) x[j] = in && c + j < N ? v[h][j] : 0.f;
+            bool all_finite;
+            float top = finite_top(x, all_finite);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, lanes));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2 * lanes));
             const uint32_t b = q8_scale(top);
-            if (!in) continue;
+            if (!writes) continue;
             if (c % kQ8Block == 0) m.d_scale[r * m.ld_scale + c / kQ8Block] = (uint8_t)b;
+            const uint32_t q[2] = {q8_codes4(x, q8_inverse(b), all_finite), q8_codes4(x + 4, q8_inverse(b), all_finite)};
             for (int j = 0; j < 8; ++j)
-                if (c + j < N)
-                    static_cast<uint8_t *>(m.d)[r * m.ld + c + j] = (uint8_t)q8_code(v[h][j], q8_inverse(b));
-        } else if (in) {
+                if (c + j < N) static_cast<uint8_t *>(m.d)[r * m.ld + c + j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+        } else if (writes) {
             for (int j = 0; j < 8; ++j)
                 if (c + j < N) static_cast<uint16_t *>(m.d)[r * m.ld + c + j] = (uint16_t)to16<F16>(v[h][j]);
         }
     }
-    if (!in) return;
+    if (!writes) return;
+    apply_act(e.act, v[0]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        float y = act_f(e.act, v[0][j]);
+        float y = v[0][j];
         if (GATED) y *= v[GATED ? 1 : 0][j];
         if (!GATED && e.residual.d && c + j < N)
             y += from16<F16>(static_cast<const uint16_t *>(e.residual.d)[r * e.residual.ld + c + j]);
@@ -568,69 +619,106 @@ bool encode(EncodeTiled fn, CUtensorMap *map, const MmOperand &o, int rows, int 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-struct Plan {
-    int tn, tiles_m, tiles_n, chunks, parts, chunks_per_part, pairs;
-    int64_t part_elems, part_ld;
-};
-
-// Tile width and split.  A wave is the time the pairs take for one tile each;
-// a 128-wide tile takes 0.6 of a 256-wide one (its a operand is staged for half
-// the products).  Parts of a split contraction keep at least 8 chunks each,
-// and are taken only when the tiles leave more than half of the pairs idle.
-Plan plan_of(const MmJob &j, int sms) {
-    const int pairs = std::max(1, sms / 2);
-    Plan best{};
-    double cost = 0;
-    const int chunks = (int)(((int64_t)j.K + kStep - 1) / kStep), total = chunks * j.terms;
-    for (int tn : {256, 128}) {
-        const int cols = j.kind == kMmGated ? tn / 2 : tn;
-        Plan p{};
-        p.tn = tn;
-        p.tiles_m = (int)(((int64_t)j.M + kTileM - 1) / kTileM);
-        p.tiles_n = (int)(((int64_t)j.N + cols - 1) / cols);
-        p.chunks = chunks;
-        const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-        p.parts = 1;
-        if (tiles * 2 <= pairs && total >= 16)
-            p.parts = (int)std::min<int64_t>(pairs / tiles, total / 8);
-        p.chunks_per_part = std::max(1, (total + p.parts - 1) / p.parts);
-        p.parts = std::max(1, (total + p.chunks_per_part - 1) / p.chunks_per_part);
-        p.part_ld = (int64_t)p.tiles_n * tn;
-        p.part_elems = p.part_ld * p.tiles_m * kTileM;
-        p.pairs = (int)std::min<int64_t>(pairs, tiles * p.parts);
-        const double waves = (double)((tiles * p.parts + pairs - 1) / pairs);
-        const double c = waves * p.chunks_per_part * (tn == 256 ? 1.0 : 0.6);
-        if (best.tn == 0 || c < cost) {
-            best = p;
-            cost = c;
-        }
+template <bool F16, bool GATED, int TN>
+cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
+    cudaError_t e = launch_pdl(mm_kernel<F16, GATED, TN>, dim3(2 * plan.pairs), dim3(kThreads), Shape<TN>::kSmem, s, p);
+    for (int i = 0; i < p.jobs && e == cudaSuccess; ++i) {
+        const MmWork &w = p.job[i];
+        if (w.parts == 1) continue;
+        const int groups = (w.N + 31) / 32 * 4;
+        int lanes_log2 = 0;  // up to 8 threads a group, while the parts and the idle threads last
+        while (lanes_log2 < 3 && (2 << lanes_log2) <= w.parts && ((int64_t)w.M * groups << lanes_log2) < 2 * 2048 * plan.pairs)
+            ++lanes_log2;
+        const int64_t threads = (int64_t)w.M * groups << lanes_log2;
+        e = launch_pdl(parts_kernel<F16, GATED, TN>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, w.epi,
+                       static_cast<const float *>(w.partial), w.part_elems, w.part_ld, w.parts, w.M, w.N, groups,
+                       lanes_log2);
     }
-    return best;
+    return e;
 }
 
-template <bool F16, bool GATED, int TN>
-cudaError_t run(const MmParams &p, const Plan &plan, cudaStream_t s) {
-    auto kernel = mm_kernel<F16, GATED, TN>;
-    kernel<<<2 * plan.pairs, kThreads, Shape<TN>::kSmem, s>>>(p);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || plan.parts == 1) return e;
-    const int groups = (p.N + 31) / 32 * 4;
-    const int64_t threads = (int64_t)p.M * groups;
-    parts_kernel<F16, GATED, TN><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(
-        p.epi, p.partial, p.part_elems, p.part_ld, plan.parts, p.M, p.N, groups);
-    return cudaGetLastError();
+// Time of a launch in chunks of a 256-wide tile (0.28 us), for a tile width and
+// a number of parts: the most that any pair is given, plus what joining costs.
+// A 128-wide tile's chunk takes 0.85 of it (half the products, but its a operand
+// is staged all the same); a unit's set-up and epilogue count as 2.
+double cost_of(const MmPlan &p, const MmJob *jobs, int n) {
+    const double chunk = p.tn == 256 ? 1.0 : 0.85;
+    double most = 0, join = 0;
+    int at[kMaxJobs + 1] = {0}, ends = 0;  // pairs where a job's units start over
+    for (int i = 0; i < n; ++i) {
+        ends += p.cut[i].units;
+        at[i + 1] = ends % p.pairs;
+        if (p.cut[i].parts > 1)
+            join += 8 + (double)p.cut[i].parts * (double)p.cut[i].part_elems * 8 / 1.4e6;
+    }
+    for (int k = 0; k <= n; ++k) {
+        double load = 0;
+        int begin = 0;
+        for (int i = 0; i < n; ++i) {
+            const int end = begin + p.cut[i].units;  // units u with u % pairs == at[k]
+            const int count = (end - at[k] + p.pairs - 1) / p.pairs - (begin - at[k] + p.pairs - 1) / p.pairs;
+            load += count * (p.cut[i].chunks_per_part * chunk + 2);
+            begin = end;
+        }
+        most = std::max(most, load);
+    }
+    return most + join;
 }
 
 }  // namespace
 
-bool mm_operand_ok(const void *p, int64_t ld, int64_t rows) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (ld * 2) % 16 == 0);
+MmPlan plan_mm(const MmJob *jobs, int n, int sms) {
+    const int pairs = std::max(1, sms / 2);
+    MmPlan best{};
+    double best_cost = 0;
+    const bool gated = jobs[0].kind == kMmGated;
+    for (const int tn : {256, 128}) {
+        const int cols = gated ? tn / 2 : tn;
+        MmPlan p{};
+        p.tn = tn;
+        int64_t tiles = 0;
+        int longest = 0;
+        for (int i = 0; i < n; ++i) {
+            MmPlan::Cut &c = p.cut[i];
+            c.tiles_m = (int)(((int64_t)jobs[i].M + kTileM - 1) / kTileM);
+            c.tiles_n = (int)(((int64_t)jobs[i].N + cols - 1) / cols);
+            c.chunks = (int)(((int64_t)jobs[i].K + kStep - 1) / kStep);
+            c.part_ld = (int64_t)c.tiles_n * tn;
+            c.part_elems = c.part_ld * jobs[i].M;
+            tiles += (int64_t)c.tiles_m * c.tiles_n;
+            longest = std::max(longest, c.chunks * jobs[i].terms);
+        }
+        // parts of at least 4 chunks, and not many more units than pairs
+        for (int d = 1; d == 1 || (longest / d >= 4 && tiles * d <= 2 * pairs); d += std::max(1, d / 4)) {
+            const int most = std::max(1, (longest + d - 1) / d);
+            p.units = 0;
+            for (int i = 0; i < n; ++i) {
+                MmPlan::Cut &c = p.cut[i];
+                const int total = c.chunks * jobs[i].terms;
+                c.parts = std::max(1, (total + most - 1) / most);
+                c.chunks_per_part = std::max(1, (total + c.parts - 1) / c.parts);
+                c.parts = std::max(1, (total + c.chunks_per_part - 1) / c.chunks_per_part);
+                c.units = c.tiles_m * c.tiles_n * c.parts;
+                p.units += c.units;
+            }
+            p.pairs = std::min(pairs, p.units);
+            const double cost = cost_of(p, jobs, n);
+            if (best.tn == 0 || cost < best_cost) {
+                best = p;
+                best_cost = cost;
+            }
+        }
+    }
+    for (int i = 0; i < n; ++i) {
+        if (best.cut[i].parts == 1) continue;
+        best.cut[i].part_at = (int64_t)(best.workspace / sizeof(float));
+        best.workspace += (size_t)best.cut[i].parts * best.cut[i].part_elems * sizeof(float);
+    }
+    return best;
 }
 
-size_t mm_workspace(const MmJob &j, int sms) {
-    if (j.M == 0 || j.N == 0) return 0;
-    const Plan p = plan_of(j, sms);
-    return p.parts > 1 ? (size_t)p.parts * p.part_elems * sizeof(float) : 0;
+bool mm_operand_ok(const void *p, int64_t ld, int64_t rows) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (ld * 2) % 16 == 0);
 }
 
 cudaError_t init_mm_kernels() {
@@ -651,37 +739,43 @@ cudaError_t init_mm_kernels() {
     return e;
 }
 
-cudaError_t launch_mm(const MmJob &j, const emtk_nn *nn, void *partial, cudaStream_t s) {
-    if (j.M == 0 || j.N == 0) return cudaSuccess;
-    const Plan plan = plan_of(j, nn->sm_count);
-    const bool gated = j.kind == kMmGated, f16 = j.type == EMTK_TYPE_F16;
+cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_nn *nn, void *partial,
+                      cudaStream_t s) {
+    const bool gated = jobs[0].kind == kMmGated, f16 = jobs[0].type == EMTK_TYPE_F16, wide = plan.tn == 256;
+    const auto fn = reinterpret_cast<EncodeTiled>(nn->encode);
     MmParams p;
-    if (j.K > 0) {
-        const auto fn = reinterpret_cast<EncodeTiled>(nn->encode);
-        bool ok = true;
-        for (int i = 0; i < j.terms; ++i) ok = ok && encode(fn, &p.a[i], j.a[i], j.M, j.K, 128);
-        for (int i = 0; i < (gated ? 2 : j.terms); ++i) ok = ok && encode(fn, &p.b[i], j.b[i], j.N, j.K, plan.tn / 2);
-        if (!ok) return cudaErrorInvalidValue;
+    int end = 0;
+    for (int i = 0; i < n; ++i) {
+        const MmJob &j = jobs[i];
+        const MmPlan::Cut &c = plan.cut[i];
+        MmWork &w = p.job[i];
+        if (j.K > 0) {
+            bool ok = true;
+            for (int t = 0; t < j.terms; ++t) ok = ok && encode(fn, &w.a[t], j.a[t], j.M, j.K, 128);
+            for (int t = 0; t < (gated ? 2 : j.terms); ++t) ok = ok && encode(fn, &w.b[t], j.b[t], j.N, j.K, plan.tn / 2);
+            if (!ok) return cudaErrorInvalidValue;
+        }
+        w.epi = j.epi;
+        w.partial = c.parts > 1 ? static_cast<float *>(partial) + c.part_at : nullptr;
+        w.part_elems = c.part_elems;
+        w.part_ld = c.part_ld;
+        w.M = j.M;
+        w.N = j.N;
+        w.K = j.K;
+        w.a_across = j.a[0].across;
+        w.b_across = j.b[0].across;
+        w.tiles_m = c.tiles_m;
+        w.tiles_n = c.tiles_n;
+        w.parts = c.parts;
+        w.chunks = c.chunks;
+        w.total = c.chunks * j.terms;
+        w.chunks_per_part = c.chunks_per_part;
+        w.unit_end = end += c.units;
     }
-    p.epi = j.epi;
-    p.partial = plan.parts > 1 ? static_cast<float *>(partial) : nullptr;
-    p.part_elems = plan.part_elems;
-    p.part_ld = plan.part_ld;
-    p.M = j.M;
-    p.N = j.N;
-    p.K = j.K;
-    p.terms = j.terms;
-    p.a_across = j.a[0].across;
-    p.b_across = j.b[0].across;
-    p.tiles_m = plan.tiles_m;
-    p.tiles_n = plan.tiles_n;
-    p.parts = plan.parts;
-    p.chunks = plan.chunks;
-    p.chunks_per_part = plan.chunks_per_part;
+    p.jobs = n;
     p.status = nn->status;
     p.timeout_ns = nn->timeout_ns;
     p.debug_stall = nn->debug_stall;
-    const bool wide = plan.tn == 256;
     if (f16)
         return gated ? (wide ? run<true, true, 256>(p, plan, s) : run<true, true, 128>(p, plan, s))
                      : (wide ? run<true, false, 256>(p, plan, s) : run<true, false, 128>(p, plan, s));

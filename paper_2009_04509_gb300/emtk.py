@@ -447,6 +447,14 @@ def _vec(t, n: int, what: str, dtype=None) -> int:
     return t.data_ptr()
 
 
+def _current(t, stream) -> int:
+    """The stream argument, or the current stream of t's device."""
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(t.get_device())  # torch.cuda.current_stream() without its object
+    return _stream(stream)
+
+
 def _act_code(act: str) -> int:
     if act not in ACTS:
         raise ValueError(f"act: {act!r} is none of {tuple(ACTS)}")
@@ -482,7 +490,7 @@ def emtk_dense(nn, x, w, y, bias=None, act: str = "none", residual=None, pre=Non
                             *_mat(x, m, k, dt, "x"), *_mat(w, n, k, dt, "w"), *_mat(y, m, n, dt, "y"),
                             *_mat(residual, m, n, dt, "residual"), *_mat(pre, m, n, (dt, Q8), "pre"),
                             _vec(bias, n, "bias"))
-    _check(load_library().emtk_dense(nn, args, _stream(stream)), "emtk_dense")
+    _check(load_library().emtk_dense(nn, args, _current(x, stream)), "emtk_dense")
 
 
 def emtk_dense_backward(nn, dy, x, w, act: str = "none", pre=None, dx=None, dw=None, db=None, stream=None) -> None:
@@ -498,7 +506,7 @@ def emtk_dense_backward(nn, dy, x, w, act: str = "none", pre=None, dx=None, dw=N
                                  *_mat(pre, m, n, (dt, Q8), "pre"), *_mat(dx, m, k, dt, "dx"),
                                  *_mat(dw, n, k, None if dw is None else dw.dtype, "dw"),
                                  _vec(db, n, "db", torch.float32))
-    _check(load_library().emtk_dense_backward(nn, args, _stream(stream)), "emtk_dense_backward")
+    _check(load_library().emtk_dense_backward(nn, args, _current(dy, stream)), "emtk_dense_backward")
 
 
 def emtk_gated(nn, x, w_gate, w_up, h, bias_gate=None, bias_up=None, act: str = "silu", gate=None, up=None,
@@ -515,7 +523,7 @@ def emtk_gated(nn, x, w_gate, w_up, h, bias_gate=None, bias_up=None, act: str = 
                             *_mat(h, m, f, dt, "h"), *_mat(gate, m, f, (dt, Q8), "gate"),
                             *_mat(up, m, f, (dt, Q8), "up"), _vec(bias_gate, f, "bias_gate"),
                             _vec(bias_up, f, "bias_up"))
-    _check(load_library().emtk_gated(nn, args, _stream(stream)), "emtk_gated")
+    _check(load_library().emtk_gated(nn, args, _current(x, stream)), "emtk_gated")
 
 
 def emtk_gated_backward(nn, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx=None, dw_gate=None, dw_up=None,
@@ -537,21 +545,21 @@ def emtk_gated_backward(nn, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx
                                  *_mat(dx, m, k, dt, "dx"), *_mat(dw_gate, f, k, dwt, "dw_gate"),
                                  *_mat(dw_up, f, k, dwt, "dw_up"), *_mat(h, m, f, dt, "h"),
                                  _vec(db_gate, f, "db_gate", torch.float32), _vec(db_up, f, "db_up", torch.float32))
-    _check(load_library().emtk_gated_backward(nn, args, _stream(stream)), "emtk_gated_backward")
+    _check(load_library().emtk_gated_backward(nn, args, _current(dh, stream)), "emtk_gated_backward")
 
 
 def emtk_pack8(nn, x, q: Q8, stream=None) -> None:
     """Keeps x [m][k] (bf16 or fp16) in the 8-bit checkpoint q."""
     (m, k), dt = x.shape, x.dtype
     _check(load_library().emtk_pack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")),
-                                     _PACK_MATRIX.pack(*_mat(q, m, k, (dt, Q8), "q")), _stream(stream)), "emtk_pack8")
+                                     _PACK_MATRIX.pack(*_mat(q, m, k, (dt, Q8), "q")), _current(x, stream)), "emtk_pack8")
 
 
 def emtk_unpack8(nn, q: Q8, x, stream=None) -> None:
     """The values that the 8-bit checkpoint q stands for, into x [m][k] (bf16 or fp16)."""
     (m, k), dt = x.shape, x.dtype
     _check(load_library().emtk_unpack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(q, m, k, (dt, Q8), "q")),
-                                       _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")), _stream(stream)), "emtk_unpack8")
+                                       _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")), _current(x, stream)), "emtk_unpack8")
 
 
 # ------------------------------------------------------------- test hooks
