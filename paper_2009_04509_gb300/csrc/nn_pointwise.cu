@@ -1,7 +1,9 @@
 // Pointwise passes of the dense and gated layers' gradients, and the 8-bit
-// checkpoints.  All of them stream: every element is read once with 16-byte
-// loads (8 columns a thread) where address and row distance allow it, one
-// element at a time where they do not, and what bounds them is HBM.
+// checkpoints.  All of them stream, every element read once, and HBM bounds
+// them.  Where every operand's rows start on 16 bytes (8 for codes) and hold a
+// multiple of 8 columns, a thread takes 8 neighbouring columns with one load and
+// keeps the next ones in flight; elsewhere a warp takes 32 neighbouring columns
+// at a time, one element a lane, which coalesces at any alignment.
 #include <algorithm>
 
 #include "emtk_internal.h"
@@ -11,76 +13,88 @@
 namespace emtk {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kVec = 8;  // columns of a thread
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kVec = 8;                  // columns of a thread
+constexpr int kWarpCols = 32 * kVec;     // columns of a warp's piece of a row
 
-enum Access : int { kAbsent = 0, kWide16, kNarrow16, kWideQ8, kNarrowQ8 };
-
-struct Source {
-    const void *p;
-    const uint8_t *scale;
-    int64_t ld, ld_scale;
-    int access;
+struct Source {  // a 16-bit matrix or a checkpoint
+    const uint8_t *p;
+    const uint8_t *scale;  // not null: checkpoint
+    int64_t row_bytes, ld_scale;
 };
 
-bool aligned(const void *p, int64_t row_bytes, int bytes) {
-    return (reinterpret_cast<uintptr_t>(p) % bytes) == 0 && row_bytes % bytes == 0;
-}
-
 Source source_of(const emtk_matrix &m) {
-    Source s{m.d, m.d_scale, m.ld, m.ld_scale, kAbsent};
-    if (m.d == nullptr) return s;
-    if (m.d_scale)
-        s.access = aligned(m.d, m.ld, kVec) ? kWideQ8 : kNarrowQ8;
-    else
-        s.access = aligned(m.d, 2 * m.ld, 16) ? kWide16 : kNarrow16;
-    return s;
+    return {static_cast<const uint8_t *>(m.d), m.d_scale, m.d_scale ? m.ld : 2 * m.ld, m.ld_scale};
+}
+// Every piece of 8 columns is one aligned load.
+bool wide_source(const Source &s, int cols) {
+    const unsigned bytes = s.scale ? kVec : 2 * kVec;
+    return cols % kVec == 0 && (reinterpret_cast<uintptr_t>(s.p) | (uintptr_t)s.row_bytes) % bytes == 0;
+}
+bool wide_matrix(const void *p, int64_t row_bytes, unsigned bytes) {
+    return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)row_bytes) % bytes == 0;
 }
 
-// Columns c .. c + 7 of row r as fp32; columns from n on read as 0.
-template <bool F16>
-__device__ __forceinline__ void load8(const Source &s, int64_t r, int c, int n, float (&v)[kVec]) {
-    const bool full = c + kVec <= n;
-    if (s.access == kWide16 && full) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(s.p) + r * s.ld + c));
+// Eight neighbouring columns as they lie in memory.
+template <bool Q8>
+struct Piece {
+    uint4 w;
+    __device__ __forceinline__ void load(const uint8_t *p, const uint8_t *) { w = __ldg(reinterpret_cast<const uint4 *>(p)); }
+    template <bool F16>
+    __device__ __forceinline__ void values(float *v) const {
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[2 * i] = from16<F16>(x[i] & 0xffffu);
-            v[2 * i + 1] = from16<F16>(x[i] >> 16);
+            v[2 * i] = F16 ? from16<F16>(x[i] & 0xffffu) : __uint_as_float(x[i] << 16);
+            v[2 * i + 1] = F16 ? from16<F16>(x[i] >> 16) : __uint_as_float(x[i] & 0xffff0000u);
         }
-    } else if (s.access == kWide16 || s.access == kNarrow16) {
-        const uint16_t *p = static_cast<const uint16_t *>(s.p) + r * s.ld + c;
+    }
+};
+template <>
+struct Piece<true> {
+    uint2 w;
+    uint32_t scale;
+    __device__ __forceinline__ void load(const uint8_t *p, const uint8_t *s) {
+        w = __ldg(reinterpret_cast<const uint2 *>(p));
+        scale = __ldg(s);
+    }
+    template <bool F16>
+    __device__ __forceinline__ void values(float *v) const {
+        q8_values4(w.x, q8_step(scale), v);
+        q8_values4(w.y, q8_step(scale), v + 4);
+    }
+};
+
+// Columns c0 + stride i of row r, one element each; those from n on read the last
+// column's (every load is issued, none waits for a branch).
+template <bool F16, bool Q8>
+__device__ __forceinline__ void load_strided(const Source &s, int64_t r, int64_t c0, int stride, int n, float (&v)[kVec]) {
+    const uint8_t *row = s.p + r * s.row_bytes;
+    uint32_t x[kVec], scale[Q8 ? kVec : 1];
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = c + i < n ? from16<F16>(__ldg(p + i)) : 0.f;
-    } else {
-        const uint8_t *p = static_cast<const uint8_t *>(s.p) + r * s.ld + c;
-        const float step = c < n ? q8_step(__ldg(s.scale + r * s.ld_scale + c / kQ8Block)) : 0.f;
-        uint32_t w[2] = {0u, 0u};
-        if (s.access == kWideQ8 && full) {
-            const uint2 q = __ldg(reinterpret_cast<const uint2 *>(p));
-            w[0] = q.x;
-            w[1] = q.y;
+    for (int i = 0; i < kVec; ++i) {
+        const int64_t c = min(c0 + (int64_t)i * stride, (int64_t)n - 1);
+        if (Q8) {
+            x[i] = __ldg(row + c);
+            scale[i] = __ldg(s.scale + r * s.ld_scale + c / kQ8Block);
         } else {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                if (c + i < n) w[i / 4] |= (uint32_t)__ldg(p + i) << (8 * (i % 4));
+            x[i] = __ldg(reinterpret_cast<const uint16_t *>(row) + c);
         }
-        q8_values4(w[0], step, v);
-        q8_values4(w[1], step, v + 4);
+    }
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        if (Q8) {
+            const int q = (int8_t)x[i];
+            v[i] = q == -128 ? __int_as_float(0x7fffffff) : (float)q * q8_step(scale[Q8 ? i : 0]);
+        } else {
+            v[i] = from16<F16>(x[i]);
+        }
     }
 }
 
 template <bool F16>
-__device__ __forceinline__ void store8(uint16_t *row, int c, int n, bool wide, const float (&v)[kVec]) {
-    if (wide && c + kVec <= n) {
-        *reinterpret_cast<uint4 *>(row + c) = make_uint4(pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]),
-                                                         pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (c + i < n) row[c + i] = (uint16_t)to16<F16>(v[i]);
-    }
+__device__ __forceinline__ uint4 pack8x16(const float *v) {
+    return make_uint4(pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7]));
 }
 
 // ------------------------------------------------------------- slopes
@@ -121,79 +135,138 @@ struct SlopeArgs {
     int64_t d_ld;
     uint16_t *h;
     int64_t h_ld;
-    int h_wide;
     float *partial;  // [slices][n], gated: [2][slices][n]; null: no sums
     int m, n, rows, lanes_log2;
 };
 
-template <bool F16, bool GATED, int ACT, bool SUMS>
-__global__ void __launch_bounds__(kThreads) slope_kernel(const __grid_constant__ SlopeArgs a) {
-    const int lanes = 1 << a.lanes_log2;
-    const int at_once = kThreads >> a.lanes_log2;
-    const int c = (int)blockIdx.x * (kVec << a.lanes_log2) + (threadIdx.x & (lanes - 1)) * kVec;
-    const int sub = threadIdx.x >> a.lanes_log2;
-    const int64_t r0 = (int64_t)blockIdx.y * a.rows;
-    const int64_t r1 = min(r0 + a.rows, (int64_t)a.m);
-    float sg[kVec] = {}, su[kVec] = {};
-    pdl_trigger();
-    pdl_wait();
-    if (c < a.n) {
-#pragma unroll 2
-        for (int64_t r = r0 + sub; r < r1; r += at_once) {
-            float d[kVec], g[kVec], dg[kVec];
-            load8<F16>(a.dy, r, c, a.n, d);
-            if (GATED || ACT != EMTK_ACT_NONE) load8<F16>(a.gate, r, c, a.n, g);
-            if (GATED) {
-                float u[kVec], du[kVec], h[kVec];
-                load8<F16>(a.up, r, c, a.n, u);
+template <bool GATED, int ACT>
+__device__ __forceinline__ void slope_of(float d, float g, float u, float &dg, float &du, float &h) {
+    float f = g, s = 1.f;
+    act_slope<ACT>(g, f, s);
+    dg = GATED ? d * u * s : d * s;
+    du = d * f;
+    h = f * u;
+}
+
+// The block's sums of each column, from its threads' (column base + index).
+template <bool GATED>
+__device__ __forceinline__ void block_sums(const SlopeArgs &a, const float (&sg)[kVec], const float (&su)[kVec],
+                                           bool strided) {
+    __shared__ float part[kThreads * kVec];
+    const int cols = kVec << a.lanes_log2, lanes = 1 << a.lanes_log2, at_once = kThreads >> a.lanes_log2;
+    const int64_t col = (int64_t)blockIdx.x * cols + threadIdx.x;
+    float *const row = part + (threadIdx.x >> a.lanes_log2) * cols;
+    const int tl = threadIdx.x & (lanes - 1);
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    float f, s;
-                    act_slope<ACT>(g[i], f, s);
-                    dg[i] = d[i] * u[i] * s;
-                    du[i] = d[i] * f;
-                    h[i] = f * u[i];
-                    if (SUMS) su[i] += du[i];
-                }
-                if (a.du) store8<F16>(a.du + r * a.d_ld, c, a.n, true, du);
-                if (a.h) store8<F16>(a.h + r * a.h_ld, c, a.n, a.h_wide != 0, h);
-            } else {
+    for (int half = 0; half < (GATED ? 2 : 1); ++half) {
+        __syncthreads();
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    float f, s = 1.f;
-                    if (ACT != EMTK_ACT_NONE) act_slope<ACT>(g[i], f, s);
-                    dg[i] = d[i] * s;
-                }
-            }
-            if (SUMS) {
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) sg[i] += dg[i];
-            }
-            if (a.dg) store8<F16>(a.dg + r * a.d_ld, c, a.n, true, dg);
-        }
-    }
-    if constexpr (SUMS) {
-        __shared__ float part[kThreads * kVec];
-        const int cols = kVec << a.lanes_log2;
-        const int col = (int)blockIdx.x * cols + (int)threadIdx.x;
-#pragma unroll
-        for (int half = 0; half < (GATED ? 2 : 1); ++half) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) part[threadIdx.x * kVec + i] = half ? su[i] : sg[i];
-            __syncthreads();
-            if ((int)threadIdx.x < cols && col < a.n) {
-                float sum = 0.f;
-                for (int g = 0; g < at_once; ++g) sum += part[g * cols + threadIdx.x];
-                a.partial[((int64_t)half * gridDim.y + blockIdx.y) * a.n + col] = sum;
-            }
+        for (int i = 0; i < kVec; ++i) row[strided ? i * lanes + tl : tl * kVec + i] = half ? su[i] : sg[i];
+        __syncthreads();
+        if ((int)threadIdx.x < cols && col < a.n) {
+            float sum = 0.f;
+            for (int g = 0; g < at_once; ++g) sum += part[g * cols + threadIdx.x];
+            a.partial[((int64_t)half * gridDim.y + blockIdx.y) * a.n + col] = sum;
         }
     }
 }
 
+// Q8: gate (and up) are checkpoints.  The next row's loads are issued before
+// this row's arithmetic.
+template <bool F16, bool GATED, int ACT, bool Q8, bool SUMS>
+__global__ void __launch_bounds__(kThreads) slope_kernel(const __grid_constant__ SlopeArgs a) {
+    constexpr bool kGate = GATED || ACT != EMTK_ACT_NONE;
+    const int at_once = kThreads >> a.lanes_log2;
+    const int64_t c = (int64_t)blockIdx.x * (kVec << a.lanes_log2) + (threadIdx.x & ((1 << a.lanes_log2) - 1)) * kVec;
+    const int64_t r0 = (int64_t)blockIdx.y * a.rows + (threadIdx.x >> a.lanes_log2);
+    const int64_t r1 = min((int64_t)(blockIdx.y + 1) * a.rows, (int64_t)a.m);
+    float sg[kVec] = {}, su[kVec] = {};
+    pdl_trigger();
+    pdl_wait();
+    if (c < a.n && r0 < r1) {
+        constexpr int kBytes = Q8 ? 1 : 2;
+        const uint8_t *pd = a.dy.p + r0 * a.dy.row_bytes + 2 * c;
+        const uint8_t *pg = kGate ? a.gate.p + r0 * a.gate.row_bytes + kBytes * c : nullptr;
+        const uint8_t *pu = GATED ? a.up.p + r0 * a.up.row_bytes + kBytes * c : nullptr;
+        const uint8_t *gs = kGate && Q8 ? a.gate.scale + r0 * a.gate.ld_scale + c / kQ8Block : nullptr;
+        const uint8_t *us = GATED && Q8 ? a.up.scale + r0 * a.up.ld_scale + c / kQ8Block : nullptr;
+        uint16_t *dg = a.dg + r0 * a.d_ld + c, *du = a.du + r0 * a.d_ld + c, *h = a.h + r0 * a.h_ld + c;
+        const bool has_dg = a.dg != nullptr, has_du = GATED && a.du != nullptr, has_h = GATED && a.h != nullptr;
+        Piece<false> d;
+        Piece<Q8> g, u;
+        auto fetch = [&] {
+            d.load(pd, nullptr);
+            if (kGate) g.load(pg, gs);
+            if (GATED) u.load(pu, us);
+            pd += at_once * a.dy.row_bytes;
+            if (kGate) pg += at_once * a.gate.row_bytes;
+            if (GATED) pu += at_once * a.up.row_bytes;
+            if (kGate && Q8) gs += at_once * a.gate.ld_scale;
+            if (GATED && Q8) us += at_once * a.up.ld_scale;
+        };
+        fetch();
+        for (int64_t r = r0; r < r1; r += at_once) {
+            float dv[kVec], gv[kVec], uv[kVec], x[kVec], y[kVec], z[kVec];
+            const Piece<false> dn = d;
+            const Piece<Q8> gn = g, un = u;
+            if (r + at_once < r1) fetch();
+            dn.template values<F16>(dv);
+            if (kGate) gn.template values<F16>(gv);
+            if (GATED) un.template values<F16>(uv);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                slope_of<GATED, ACT>(dv[i], kGate ? gv[i] : 0.f, GATED ? uv[i] : 0.f, x[i], y[i], z[i]);
+                if (SUMS) {
+                    sg[i] = __fadd_rn(sg[i], x[i]);  // not fused with the product: the sums are of
+                    if (GATED) su[i] = __fadd_rn(su[i], y[i]);  // the same values, stored or not
+                }
+            }
+            if (has_dg) *reinterpret_cast<uint4 *>(dg) = pack8x16<F16>(x);
+            if (has_du) *reinterpret_cast<uint4 *>(du) = pack8x16<F16>(y);
+            if (has_h) *reinterpret_cast<uint4 *>(h) = pack8x16<F16>(z);
+            dg += at_once * a.d_ld;
+            du += at_once * a.d_ld;
+            h += at_once * a.h_ld;
+        }
+    }
+    if constexpr (SUMS) block_sums<GATED>(a, sg, su, false);
+}
+
+// Any alignment, width and mixture of operands.
+template <bool F16, bool GATED, int ACT, bool Q8>
+__global__ void __launch_bounds__(kThreads) slope_any_kernel(const __grid_constant__ SlopeArgs a) {
+    constexpr bool kGate = GATED || ACT != EMTK_ACT_NONE;
+    const int lanes = 1 << a.lanes_log2, at_once = kThreads >> a.lanes_log2;
+    const int64_t c0 = (int64_t)blockIdx.x * (kVec << a.lanes_log2) + (threadIdx.x & (lanes - 1));
+    const int64_t r0 = (int64_t)blockIdx.y * a.rows + (threadIdx.x >> a.lanes_log2);
+    const int64_t r1 = min((int64_t)(blockIdx.y + 1) * a.rows, (int64_t)a.m);
+    float sg[kVec] = {}, su[kVec] = {};
+    pdl_trigger();
+    pdl_wait();
+    for (int64_t r = r0; r < r1; r += at_once) {
+        float d[kVec], g[kVec] = {}, u[kVec] = {};
+        load_strided<F16, false>(a.dy, r, c0, lanes, a.n, d);
+        if (kGate) load_strided<F16, Q8>(a.gate, r, c0, lanes, a.n, g);
+        if (GATED) load_strided<F16, Q8>(a.up, r, c0, lanes, a.n, u);
+        uint16_t *dg = a.dg + r * a.d_ld + c0, *du = a.du + r * a.d_ld + c0, *h = a.h + r * a.h_ld + c0;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            float x, y, z;
+            slope_of<GATED, ACT>(d[i], g[i], u[i], x, y, z);
+            sg[i] = __fadd_rn(sg[i], x);
+            if (GATED) su[i] = __fadd_rn(su[i], y);
+            const bool in = c0 + i * lanes < a.n;
+            if (in && a.dg) dg[i * lanes] = (uint16_t)to16<F16>(x);
+            if (in && GATED && a.du) du[i * lanes] = (uint16_t)to16<F16>(y);
+            if (in && GATED && a.h) h[i * lanes] = (uint16_t)to16<F16>(z);
+        }
+    }
+    if (a.partial) block_sums<GATED>(a, sg, su, true);
+}
+
 // Column sums from the slices' partial sums: a block takes 32 columns, each of
-// its 16 warps every 16th slice, and the warps' sums are added in order.
-constexpr int kSumWarps = 16;
+// its 32 warps every 32nd slice, and the warps' sums are added in order.
+constexpr int kSumWarps = 32;
 __global__ void __launch_bounds__(32 * kSumWarps) slice_sum_kernel(const float *partial, int slices, int n, float *db0,
                                                                    float *db1) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
@@ -216,14 +289,23 @@ __global__ void __launch_bounds__(32 * kSumWarps) slice_sum_kernel(const float *
     (blockIdx.y ? db1 : db0)[c] = sum;
 }
 
-template <bool F16, bool GATED, bool SUMS>
-cudaError_t start_slope(const SlopeArgs &a, int act, dim3 grid, cudaStream_t s) {
-    auto kernel = slope_kernel<F16, GATED, EMTK_ACT_NONE, SUMS>;
-    if (act == EMTK_ACT_RELU) kernel = slope_kernel<F16, GATED, EMTK_ACT_RELU, SUMS>;
-    if (act == EMTK_ACT_GELU) kernel = slope_kernel<F16, GATED, EMTK_ACT_GELU, SUMS>;
-    if (act == EMTK_ACT_SILU) kernel = slope_kernel<F16, GATED, EMTK_ACT_SILU, SUMS>;
-    if (act == EMTK_ACT_SIGMOID) kernel = slope_kernel<F16, GATED, EMTK_ACT_SIGMOID, SUMS>;
-    return launch_pdl(kernel, grid, dim3(kThreads), 0, s, a);
+typedef void (*SlopeKernel)(const SlopeArgs);
+
+template <bool F16, bool GATED, int ACT>
+SlopeKernel slope_for(bool wide, bool q8, bool sums) {
+    if (!wide) return q8 ? slope_any_kernel<F16, GATED, ACT, true> : slope_any_kernel<F16, GATED, ACT, false>;
+    if (q8) return sums ? slope_kernel<F16, GATED, ACT, true, true> : slope_kernel<F16, GATED, ACT, true, false>;
+    return sums ? slope_kernel<F16, GATED, ACT, false, true> : slope_kernel<F16, GATED, ACT, false, false>;
+}
+template <bool F16, bool GATED>
+SlopeKernel slope_for(int act, bool wide, bool q8, bool sums) {
+    switch (act) {
+        case EMTK_ACT_RELU: return slope_for<F16, GATED, EMTK_ACT_RELU>(wide, q8, sums);
+        case EMTK_ACT_GELU: return slope_for<F16, GATED, EMTK_ACT_GELU>(wide, q8, sums);
+        case EMTK_ACT_SILU: return slope_for<F16, GATED, EMTK_ACT_SILU>(wide, q8, sums);
+        case EMTK_ACT_SIGMOID: return slope_for<F16, GATED, EMTK_ACT_SIGMOID>(wide, q8, sums);
+        default: return slope_for<F16, GATED, EMTK_ACT_NONE>(wide, q8, sums);
+    }
 }
 
 template <bool GATED>
@@ -232,63 +314,110 @@ cudaError_t run_slope(emtk_type type, int act, SlopeArgs &a, float *db0, float *
     const SlopeShape h = slope_shape(a.m, a.n, sms, a.partial != nullptr);
     a.rows = h.rows;
     a.lanes_log2 = h.lanes_log2;
-    const dim3 grid((unsigned)h.col_blocks, (unsigned)h.slices);
-    const bool f16 = type == EMTK_TYPE_F16;
-    cudaError_t e = a.partial ? (f16 ? start_slope<true, GATED, true>(a, act, grid, s)
-                                     : start_slope<false, GATED, true>(a, act, grid, s))
-                              : (f16 ? start_slope<true, GATED, false>(a, act, grid, s)
-                                     : start_slope<false, GATED, false>(a, act, grid, s));
-    if (e == cudaSuccess && a.partial)
+    const bool gate = GATED || act != EMTK_ACT_NONE;
+    const bool wide = wide_source(a.dy, a.n) && (!gate || wide_source(a.gate, a.n)) &&
+                      (!GATED || wide_source(a.up, a.n)) && (!a.h || wide_matrix(a.h, 2 * a.h_ld, 16));
+    const bool q8 = gate && a.gate.scale != nullptr, sums = a.partial != nullptr;
+    const SlopeKernel kernel = type == EMTK_TYPE_F16 ? slope_for<true, GATED>(act, wide, q8, sums)
+                                                     : slope_for<false, GATED>(act, wide, q8, sums);
+    cudaError_t e = launch_pdl(kernel, dim3((unsigned)h.col_blocks, (unsigned)h.slices), dim3(kThreads), 0, s, a);
+    if (e == cudaSuccess && sums)
         e = launch_pdl(slice_sum_kernel, dim3((unsigned)((a.n - 1) / 32 + 1), GATED ? 2u : 1u), dim3(32 * kSumWarps), 0,
                        s, static_cast<const float *>(a.partial), h.slices, a.n, db0, db1);
     return e;
 }
 
 // -------------------------------------------------------- checkpoints
-// A warp takes rows, 256 columns of a row at a time (four threads hold a block
-// of 32), up to four such pieces in flight; blocks along y share a row where
-// there are few.
-constexpr int kWarpCols = 32 * kVec;
-constexpr int kPieces = 4;
+// A warp's items are (row, piece of 256 columns), every warps-th one; the step
+// from one to the next is added to row and piece, without a division.  Four
+// items' loads are in flight.
+constexpr int kFlight = 4;
+
+struct Walk {
+    int per_row;
+    int64_t step_rows;
+    int step_pieces;
+};
+
+struct Item {
+    int64_t r;
+    int piece;
+    __device__ __forceinline__ Item(const Walk &w, int64_t first) : r(first / w.per_row), piece((int)(first - r * w.per_row)) {}
+    __device__ __forceinline__ void next(const Walk &w) {
+        r += w.step_rows;
+        piece += w.step_pieces;
+        if (piece >= w.per_row) {
+            piece -= w.per_row;
+            ++r;
+        }
+    }
+};
+
+struct PackArgs {
+    Source x;
+    uint8_t *q, *scale;
+    int64_t q_ld, ld_scale;
+    int m, k;
+    Walk walk;
+};
 
 template <bool F16>
-__global__ void __launch_bounds__(kThreads) pack8_kernel(const Source x, uint8_t *q, int64_t q_ld, uint8_t *scale,
-                                                         int64_t ld_scale, int m, int k, int wide) {
+__global__ void __launch_bounds__(kThreads) pack8_kernel(const __grid_constant__ PackArgs a) {
     const int lane = threadIdx.x & 31;
-    const int step = (int)gridDim.y * kWarpCols;
+    Item it(a.walk, (int64_t)blockIdx.x * kWarps + threadIdx.x / 32);
     pdl_trigger();
     pdl_wait();
-    for (int64_t r = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32; r < m;
-         r += (int64_t)gridDim.x * (kThreads / 32)) {
-        for (int64_t c0 = (int64_t)blockIdx.y * kWarpCols; c0 < k; c0 += (int64_t)kPieces * step) {
-            float v[kPieces][kVec] = {};
+    while (it.r < a.m) {
+        Piece<false> w[kFlight];
+        int64_t r[kFlight];
+        int c[kFlight];
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int64_t c = c0 + (int64_t)i * step + lane * kVec;
-                if (c < k) load8<F16>(x, r, (int)c, k, v[i]);
-            }
+        for (int i = 0; i < kFlight; ++i, it.next(a.walk)) {
+            r[i] = it.r;
+            c[i] = it.piece * kWarpCols + lane * kVec;
+            w[i].w = make_uint4(0u, 0u, 0u, 0u);
+            if (r[i] < a.m && c[i] < a.k) w[i].load(a.x.p + r[i] * a.x.row_bytes + 2 * (int64_t)c[i], nullptr);
+        }
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                if (c0 + (int64_t)i * step >= k) break;  // the whole warp
-                const int64_t c = c0 + (int64_t)i * step + lane * kVec;
-                bool all_finite;
-                float top = finite_top(v[i], all_finite);
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                if (c >= k) continue;
-                const uint32_t b = q8_scale(top);
-                const float inverse = q8_inverse(b);
-                if ((lane & 3) == 0) scale[r * ld_scale + c / kQ8Block] = (uint8_t)b;
-                uint8_t *p = q + r * q_ld + c;
-                const uint2 w = make_uint2(q8_codes4(v[i], inverse, all_finite), q8_codes4(v[i] + 4, inverse, all_finite));
-                if (wide && c + kVec <= k) {
-                    *reinterpret_cast<uint2 *>(p) = w;
-                } else {
+        for (int i = 0; i < kFlight; ++i) {
+            float v[kVec];
+            w[i].template values<F16>(v);
+            bool all_finite;
+            float top = finite_top(v, all_finite);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            if (r[i] >= a.m || c[i] >= a.k) continue;
+            const uint32_t b = q8_scale(top);
+            const float inverse = q8_inverse(b);
+            if ((lane & 3) == 0) a.scale[r[i] * a.ld_scale + c[i] / kQ8Block] = (uint8_t)b;
+            *reinterpret_cast<uint2 *>(a.q + r[i] * a.q_ld + c[i]) =
+                make_uint2(q8_codes4(v, inverse, all_finite), q8_codes4(v + 4, inverse, all_finite));
+        }
+    }
+}
+
+// Any alignment: a block of 32 columns is a warp's lanes.
+template <bool F16>
+__global__ void __launch_bounds__(kThreads) pack8_any_kernel(const __grid_constant__ PackArgs a) {
+    const int lane = threadIdx.x & 31;
+    pdl_trigger();
+    pdl_wait();
+    for (Item it(a.walk, (int64_t)blockIdx.x * kWarps + threadIdx.x / 32); it.r < a.m; it.next(a.walk)) {
+        const int64_t c0 = (int64_t)it.piece * kWarpCols + lane;
+        float v[kVec];
+        load_strided<F16, false>(a.x, it.r, c0, 32, a.k, v);
 #pragma unroll
-                    for (int j = 0; j < kVec; ++j)
-                        if (c + j < k) p[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j % 4)));
-                }
-            }
+        for (int i = 0; i < kVec; ++i) {
+            const int64_t c = c0 + 32 * i;
+            if (c - lane >= a.k) break;  // the whole warp; a last column read again changes no maximum
+            const bool finite = fabsf(v[i]) < __int_as_float(0x7f800000);
+            // magnitudes of floats compare as their bits do
+            const uint32_t top = __reduce_max_sync(0xffffffffu, finite ? __float_as_uint(fabsf(v[i])) : 0u);
+            const uint32_t b = q8_scale(__uint_as_float(top));
+            if (c >= a.k) continue;
+            if (lane == 0) a.scale[it.r * a.ld_scale + c / kQ8Block] = (uint8_t)b;
+            a.q[it.r * a.q_ld + c] =
+                (uint8_t)(finite ? __float_as_uint(fmaf(v[i], q8_inverse(b), 12582912.f)) : 0x80u);
         }
     }
 }
@@ -299,44 +428,72 @@ struct CopyArgs {
         uint16_t *to;
         int64_t to_ld;
         int rows, cols, wide;
+        Walk walk;
     } job[kMaxCopies];
 };
+
+template <bool F16, bool Q8>
+__device__ __forceinline__ void copy_wide(const CopyArgs::One &j, Item it, int lane) {
+    while (it.r < j.rows) {
+        Piece<Q8> w[kFlight];
+        int64_t r[kFlight];
+        int c[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i, it.next(j.walk)) {
+            r[i] = it.r;
+            c[i] = it.piece * kWarpCols + lane * kVec;
+            if (r[i] < j.rows && c[i] < j.cols)
+                w[i].load(j.from.p + r[i] * j.from.row_bytes + (Q8 ? 1 : 2) * (int64_t)c[i],
+                          j.from.scale + r[i] * j.from.ld_scale + c[i] / kQ8Block);
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            if (r[i] >= j.rows || c[i] >= j.cols) continue;
+            float v[kVec];
+            w[i].template values<F16>(v);
+#pragma unroll
+            for (int t = 0; t < kVec; ++t) v[t] = Q8 ? q8_operand<F16>(v[t]) : v[t];
+            *reinterpret_cast<uint4 *>(j.to + r[i] * j.to_ld + c[i]) = pack8x16<F16>(v);
+        }
+    }
+}
+
+template <bool F16, bool Q8>
+__device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it, int lane) {
+    for (; it.r < j.rows; it.next(j.walk)) {
+        const int64_t c0 = (int64_t)it.piece * kWarpCols + lane;
+        float v[kVec];
+        load_strided<F16, Q8>(j.from, it.r, c0, 32, j.cols, v);
+        uint16_t *to = j.to + it.r * j.to_ld + c0;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (c0 + 32 * i < j.cols) to[32 * i] = (uint16_t)to16<F16>(Q8 ? q8_operand<F16>(v[i]) : v[i]);
+    }
+}
 
 template <bool F16>
 __global__ void __launch_bounds__(kThreads) copy16_kernel(const __grid_constant__ CopyArgs a) {
     const CopyArgs::One &j = a.job[blockIdx.z];
     const int lane = threadIdx.x & 31;
-    const int step = (int)gridDim.y * kWarpCols;
+    Item it(j.walk, (int64_t)blockIdx.x * kWarps + threadIdx.x / 32);
     pdl_trigger();
     pdl_wait();
-    for (int64_t r = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32; r < j.rows;
-         r += (int64_t)gridDim.x * (kThreads / 32)) {
-        for (int64_t c0 = (int64_t)blockIdx.y * kWarpCols + lane * kVec; c0 < j.cols; c0 += (int64_t)kPieces * step) {
-            float v[kPieces][kVec];
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                if (c0 + (int64_t)i * step < j.cols) load8<F16>(j.from, r, (int)(c0 + (int64_t)i * step), j.cols, v[i]);
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                if (c0 + (int64_t)i * step >= j.cols) break;
-                if (j.from.scale) {
-#pragma unroll
-                    for (int t = 0; t < kVec; ++t) v[i][t] = q8_operand<F16>(v[i][t]);
-                }
-                store8<F16>(j.to + r * j.to_ld, (int)(c0 + (int64_t)i * step), j.cols, j.wide != 0, v[i]);
-            }
-        }
-    }
+    if (j.wide) return j.from.scale ? copy_wide<F16, true>(j, it, lane) : copy_wide<F16, false>(j, it, lane);
+    if (j.from.scale)
+        copy_any<F16, true>(j, it, lane);
+    else
+        copy_any<F16, false>(j, it, lane);
 }
 
-// Rows over x, eight blocks an SM at most; columns over y where rows alone
-// would leave the SMs short of warps.
-dim3 row_grid(int m, int k, int sms, int jobs) {
-    const int64_t most = (int64_t)8 * sms;
-    const int64_t x = std::min<int64_t>(most, ((int64_t)m + kThreads / 32 - 1) / (kThreads / 32));
-    const int64_t pieces = ((int64_t)k + kWarpCols - 1) / kWarpCols;
-    const int64_t y = std::max<int64_t>(1, std::min<int64_t>(pieces, most / (2 * x)));
-    return dim3((unsigned)x, (unsigned)y, (unsigned)jobs);
+// Blocks of a walk: six an SM at most, all resident at once.
+unsigned walk_blocks(int64_t rows, int64_t cols, int sms) {
+    const int64_t items = rows * ((cols + kWarpCols - 1) / kWarpCols);
+    return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + kWarps - 1) / kWarps, (int64_t)6 * sms));
+}
+Walk walk_of(int64_t cols, unsigned blocks) {
+    const int per_row = (int)((cols + kWarpCols - 1) / kWarpCols);
+    const int64_t warps = (int64_t)blocks * kWarps;
+    return {per_row, warps / per_row, (int)(warps % per_row)};
 }
 
 }  // namespace
@@ -368,7 +525,6 @@ cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk
     a.d_ld = d_ld;
     a.h = static_cast<uint16_t *>(h.d);
     a.h_ld = h.ld;
-    a.h_wide = h.d && aligned(h.d, 2 * h.ld, 16);
     a.partial = db_gate ? partial : nullptr;
     a.m = m;
     a.n = f;
@@ -378,26 +534,29 @@ cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk
 cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
                          cudaStream_t s) {
     if (m == 0 || k == 0) return cudaSuccess;
-    const dim3 grid = row_grid(m, k, sms, 1);
-    const int wide = aligned(q.d, q.ld, kVec);
-    return launch_pdl(type == EMTK_TYPE_F16 ? pack8_kernel<true> : pack8_kernel<false>, grid, dim3(kThreads), 0, s,
-                      source_of(x), static_cast<uint8_t *>(q.d), q.ld, q.d_scale, q.ld_scale, m, k, wide);
+    const unsigned blocks = walk_blocks(m, k, sms);
+    const PackArgs a{source_of(x), static_cast<uint8_t *>(q.d), q.d_scale, q.ld, q.ld_scale, m, k, walk_of(k, blocks)};
+    const bool wide = wide_source(a.x, k) && wide_matrix(q.d, q.ld, kVec), f16 = type == EMTK_TYPE_F16;
+    return launch_pdl(wide ? (f16 ? pack8_kernel<true> : pack8_kernel<false>)
+                           : (f16 ? pack8_any_kernel<true> : pack8_any_kernel<false>),
+                      dim3(blocks), dim3(kThreads), 0, s, a);
 }
 
 cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, cudaStream_t s) {
     CopyArgs a{};
-    int rows = 0, cols = 0, jobs = 0;
+    unsigned jobs = 0, blocks = 0;
+    for (int i = 0; i < n; ++i)
+        if (copies[i].cols > 0) blocks = std::max(blocks, walk_blocks(copies[i].rows, copies[i].cols, sms));
     for (int i = 0; i < n; ++i) {
         const Copy16 &c = copies[i];
         if (c.rows == 0 || c.cols == 0) continue;
-        a.job[jobs++] = {source_of(c.from), static_cast<uint16_t *>(c.to.d), c.to.ld, c.rows, c.cols,
-                         aligned(c.to.d, 2 * c.to.ld, 16)};
-        rows = std::max(rows, c.rows);
-        cols = std::max(cols, c.cols);
+        const Source from = source_of(c.from);
+        a.job[jobs++] = {from, static_cast<uint16_t *>(c.to.d), c.to.ld, c.rows, c.cols,
+                         wide_source(from, c.cols) && wide_matrix(c.to.d, 2 * c.to.ld, 16), walk_of(c.cols, blocks)};
     }
     if (jobs == 0) return cudaSuccess;
-    return launch_pdl(type == EMTK_TYPE_F16 ? copy16_kernel<true> : copy16_kernel<false>,
-                      row_grid(rows, cols, sms, jobs), dim3(kThreads), 0, s, a);
+    return launch_pdl(type == EMTK_TYPE_F16 ? copy16_kernel<true> : copy16_kernel<false>, dim3(blocks, 1, jobs),
+                      dim3(kThreads), 0, s, a);
 }
 
 }  // namespace emtk
