@@ -126,7 +126,8 @@ emtk_status forward(emtk_nn *nn, MmJob &j, const emtk_matrix &x, const emtk_matr
     j.a[0] = rows_of(x);
     for (int i = 0; i < nw; ++i) j.b[i] = rows_of(w[i]);
     if (few_rows(j)) return status_of(launch_rows(j, s));
-    const MmPlan plan = plan_mm(&j, 1, nn->sm_count);
+    const bool thin = skinny(j);
+    const MmPlan plan = thin ? MmPlan{} : plan_mm(&j, 1, nn->sm_count);
     CallSpace ws{nn};
     Staging stage{ws};
     void *partial = nullptr;
@@ -141,7 +142,7 @@ emtk_status forward(emtk_nn *nn, MmJob &j, const emtk_matrix &x, const emtk_matr
         }
     }
     cudaError_t e = launch_copy16(j.type, stage.copies, stage.n, nn->sm_count, s);
-    if (e == cudaSuccess) e = launch_mm(&j, 1, plan, nn, partial, s);
+    if (e == cudaSuccess) e = thin ? launch_skinny(j, nn, s) : launch_mm(&j, 1, plan, nn, partial, s);
     return status_of(e);
 }
 

@@ -2,6 +2,7 @@
 // (nn_api.cu, nn_mm.cu, nn_pointwise.cu).
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -59,11 +60,15 @@ struct MmJob {
 // Whether a matrix of 16-bit elements can be an operand as it lies: TMA wants
 // its address and row distance on 16 bytes.  (Others are copied first.)
 bool mm_operand_ok(const void *p, int64_t ld, int64_t rows);
+// Tensor map of an operand: rows of index i (M or N), K contraction steps, boxes
+// of 128 bytes along memory by box_rows (or 64, where i runs along memory).
+bool encode_operand(const emtk_nn *nn, CUtensorMap *map, const MmOperand &o, int rows, int K, int box_rows);
 // Up to kMaxJobs jobs of one kind and type in one launch (nn_mm.cu); the plan
 // says how they are cut, and how much workspace `partial` it needs.
 constexpr int kMaxJobs = 3;
 struct MmPlan {
     int tn, pairs, units;
+    int order[kMaxJobs];  // of the launch's jobs
     struct Cut {
         int tiles_m, tiles_n, chunks, parts, chunks_per_part, units;
         int64_t part_ld, part_elems, part_at;
@@ -76,6 +81,10 @@ cudaError_t init_mm_kernels();  // once per device
 // The forward pass of 1 to 4 rows (nn_rows.cu), operands anywhere.
 bool few_rows(const MmJob &job);
 cudaError_t launch_rows(const MmJob &job, cudaStream_t s);
+// The forward pass of up to 64 rows (nn_skinny.cu).
+bool skinny(const MmJob &job);
+cudaError_t launch_skinny(const MmJob &job, const emtk_nn *nn, cudaStream_t s);
+cudaError_t init_skinny_kernels();  // once per device
 
 // ---- pointwise passes (nn_pointwise.cu)
 // dz = dy act'(pre) as a 16-bit matrix dz (or none), and its column sums db

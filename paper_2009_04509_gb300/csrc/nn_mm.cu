@@ -140,27 +140,53 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
             }
         }
     } else if (lane < nc) {
-#pragma unroll 4
-        for (int r = 0; r < nr; ++r) {
-            T *g = base + (r0 + r) * ld + c0 + lane;
-            T *s = reinterpret_cast<T *>(stage + r * kRowBytes) + lane;
-            if (LOAD)
-                *s = *g;
-            else
-                *g = *s;
+        T *g = base + r0 * ld + c0 + lane;
+        uint8_t *s = stage + lane * sizeof(T);
+        for (int r = 0; r < nr; r += 8) {  // eight rows' elements in flight
+            T x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r + i < nr) x[i] = LOAD ? g[i * ld] : *reinterpret_cast<const T *>(s + i * kRowBytes);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r + i < nr) {
+                    if (LOAD)
+                        *reinterpret_cast<T *>(s + i * kRowBytes) = x[i];
+                    else
+                        g[i * ld] = x[i];
+                }
+            g += 8 * ld;
+            s += 8 * kRowBytes;
         }
     }
 }
 
-// What the epilogue of one warp needs: its 32 rows and its staged rows.
+// What the epilogue of one warp needs of its tile, in registers: its 32 rows, its
+// staged rows, and of the job what every block of 32 columns uses.
 struct Rows {
     int64_t r0, rows;  // first row, rows of the matrix
     uint8_t *stage;
     int lane;
+    int act;
+    bool has_bias, has_saved, out_f32, out_wide, residual_wide;
+    void *out, *residual;
+    int64_t out_ld, residual_ld;
+    __device__ __forceinline__ void take(const MmEpilogue &e) {
+        act = e.act;
+        has_bias = e.bias[0] != nullptr;
+        has_saved = e.saved[0].d != nullptr;
+        out_f32 = e.out_f32 != 0;
+        out = e.out.d;
+        out_ld = e.out.ld;
+        out_wide = wide_rows(out, out_ld, out_f32 ? 4 : 2);
+        residual = e.residual.d;
+        residual_ld = e.residual.ld;
+        residual_wide = wide_rows(residual, residual_ld, 2);
+    }
 };
 
 template <bool F16>
-__device__ __forceinline__ void store16(const emtk_matrix &m, const Rows &w, int64_t c0, int64_t cols,
+__device__ __forceinline__ void store16(void *base, int64_t ld, bool wide, const Rows &w, int64_t c0, int64_t cols,
                                         const float (&v)[32]) {
     uint8_t *row = w.stage + w.lane * kRowBytes;
 #pragma unroll
@@ -169,12 +195,11 @@ __device__ __forceinline__ void store16(const emtk_matrix &m, const Rows &w, int
             make_uint4(pack16<F16>(v[8 * i], v[8 * i + 1]), pack16<F16>(v[8 * i + 2], v[8 * i + 3]),
                        pack16<F16>(v[8 * i + 4], v[8 * i + 5]), pack16<F16>(v[8 * i + 6], v[8 * i + 7]));
     __syncwarp();
-    move_block<uint16_t, false>(static_cast<uint16_t *>(m.d), m.ld, w.r0, w.rows, c0, cols, wide_rows(m.d, m.ld, 2),
-                                w.stage, w.lane);
+    move_block<uint16_t, false>(static_cast<uint16_t *>(base), ld, w.r0, w.rows, c0, cols, wide, w.stage, w.lane);
     __syncwarp();
 }
 
-__device__ __forceinline__ void store32(float *base, int64_t ld, const Rows &w, int64_t c0, int64_t cols,
+__device__ __forceinline__ void store32(float *base, int64_t ld, bool wide, const Rows &w, int64_t c0, int64_t cols,
                                         const float (&v)[32]) {
     float4 *row = reinterpret_cast<float4 *>(w.stage + w.lane * kRowBytes);
 #pragma unroll
@@ -186,8 +211,7 @@ __device__ __forceinline__ void store32(float *base, int64_t ld, const Rows &w, 
         }
         __syncwarp();
         if (c0 + 16 * half < cols)
-            move_block<float, false>(base, ld, w.r0, w.rows, c0 + 16 * half, cols, wide_rows(base, ld, 4), w.stage,
-                                     w.lane);
+            move_block<float, false>(base, ld, w.r0, w.rows, c0 + 16 * half, cols, wide, w.stage, w.lane);
         __syncwarp();
     }
 }
@@ -222,11 +246,10 @@ __device__ __forceinline__ void store_q8(const emtk_matrix &m, const Rows &w, in
 template <bool F16>
 __device__ __forceinline__ void store_saved(const emtk_matrix &m, const Rows &w, int64_t c0, int64_t cols,
                                             const float (&v)[32]) {
-    if (m.d == nullptr) return;
     if (m.d_scale)
         store_q8(m, w, c0, cols, v);
     else
-        store16<F16>(m, w, c0, cols, v);
+        store16<F16>(m.d, m.ld, wide_rows(m.d, m.ld, 2), w, c0, cols, v);
 }
 
 template <bool F16>
@@ -251,12 +274,12 @@ __device__ __forceinline__ void add_bias(const float *bias, float (&v)[32]) {
 template <bool F16>
 __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
                                              const float *bias, float (&v)[32]) {
-    if (e.bias[0]) add_bias(bias, v);
-    store_saved<F16>(e.saved[0], w, c0, cols, v);
-    apply_act(e.act, v);
-    if (e.residual.d) {
-        move_block<uint16_t, true>(static_cast<uint16_t *>(e.residual.d), e.residual.ld, w.r0, w.rows, c0, cols,
-                                   wide_rows(e.residual.d, e.residual.ld, 2), w.stage, w.lane);
+    if (w.has_bias) add_bias(bias, v);
+    if (w.has_saved) store_saved<F16>(e.saved[0], w, c0, cols, v);
+    apply_act(w.act, v);
+    if (w.residual) {
+        move_block<uint16_t, true>(static_cast<uint16_t *>(w.residual), w.residual_ld, w.r0, w.rows, c0, cols,
+                                   w.residual_wide, w.stage, w.lane);
         __syncwarp();
         const uint4 *row = reinterpret_cast<const uint4 *>(w.stage + w.lane * kRowBytes);
 #pragma unroll
@@ -271,26 +294,28 @@ __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w,
         }
         __syncwarp();
     }
-    if (e.out_f32)
-        store32(static_cast<float *>(e.out.d), e.out.ld, w, c0, cols, v);
+    if (w.out_f32)
+        store32(static_cast<float *>(w.out), w.out_ld, w.out_wide, w, c0, cols, v);
     else
-        store16<F16>(e.out, w, c0, cols, v);
+        store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, v);
 }
 
 template <bool F16>
 __device__ __forceinline__ void finish_gated(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
                                              const float *bias_g, const float *bias_u, float (&g)[32],
                                              float (&u)[32]) {
-    if (e.bias[0]) {
+    if (w.has_bias) {
         add_bias(bias_g, g);
         add_bias(bias_u, u);
     }
-    store_saved<F16>(e.saved[0], w, c0, cols, g);
-    store_saved<F16>(e.saved[1], w, c0, cols, u);
-    apply_act(e.act, g);
+    if (w.has_saved) {
+        store_saved<F16>(e.saved[0], w, c0, cols, g);
+        store_saved<F16>(e.saved[1], w, c0, cols, u);
+    }
+    apply_act(w.act, g);
 #pragma unroll
     for (int i = 0; i < 32; ++i) g[i] *= u[i];
-    store16<F16>(e.out, w, c0, cols, g);
+    store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, g);
 }
 
 enum Bar : int { kBarFull = 0, kBarEmpty = 8, kBarAccFull = 16, kBarAccEmpty = 18, kBarDrain = 20, kBarStall = 21, kBars = 22 };
@@ -354,12 +379,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const Unit t = unit_of(p, u, kCols);
             const int ra = t.m0 + 128 * (int)rank, rb = t.n0 + (GATED ? 0 : TN / 2 * (int)rank);
             const MmWork &w = p.job[t.job];
-            int term = t.c0 / max(1, w.chunks), k0 = (t.c0 - term * w.chunks) * kStep;
+            // Where the pairs share no rows of a, each tile starts at another chunk and wraps
+            // around: in step, all would read the same few address bits of b's rows at a time.
+            int at = t.c0;
+            if (w.tiles_m == 1) at += t.n0 / kCols * 5 % max(1, t.c1 - t.c0);
             for (int c = t.c0; c < t.c1; ++c) {
                 if (!warp_wait_all(bar(kBarEmpty + s), phase, guard, lane)) {
                     ok = false;
                     break;
                 }
+                const int term = at >= w.chunks ? 1 : 0, k0 = (at - term * w.chunks) * kStep;
                 if (elect_one()) {
                     const uint32_t sa = stages + s * S::kStageBytes, sb = sa + kABytes;
                     const uint32_t full = full0 + 8 * s;
@@ -380,11 +409,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                 }
                 __syncwarp();
-                k0 += kStep;
-                if (k0 >= w.K) {
-                    k0 = 0;
-                    ++term;
-                }
+                if (++at == t.c1) at = t.c0;
                 if (++s == S::kStages) {
                     s = 0;
                     phase ^= 1;
@@ -453,31 +478,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int q = e & 3, half = e >> 2;
         constexpr int kMine = kCols / 2;  // output columns of a warp
         float *const bias = epi_bias + e * (kBiasBytes / 4);
-        Rows w{0, 0, epi_rows + e * kStageRowsBytes, lane};
-        int tile = 0;
+        Rows w{};
+        w.stage = epi_rows + e * kStageRowsBytes;
+        w.lane = lane;
+        int tile = 0, taken = -1;
         for (int u = pair; u < units; u += pairs, ++tile) {
             const Unit t = unit_of(p, u, kCols);
             const MmWork &job = p.job[t.job];
             const int ab = tile & 1;
-            w.rows = job.M;
+            if (t.job != taken) {
+                w.take(job.epi);
+                w.rows = job.M;
+                taken = t.job;
+            }
             w.r0 = t.m0 + 128 * (int64_t)rank + 32 * q;
             const int64_t n0 = t.n0 + half * kMine;
             __syncwarp();
-            if (job.partial == nullptr && job.epi.bias[0]) {
+            float *const partial = job.partial;
+            const int N = job.N;
+            if (partial == nullptr && w.has_bias) {
                 for (int j = lane; j < kMine; j += 32) {
-                    bias[j] = bias_at<F16>(job.epi, 0, n0 + j, job.N);
-                    if (GATED) bias[kMine + j] = bias_at<F16>(job.epi, 1, n0 + j, job.N);
+                    bias[j] = bias_at<F16>(job.epi, 0, n0 + j, N);
+                    if (GATED) bias[kMine + j] = bias_at<F16>(job.epi, 1, n0 + j, N);
                 }
             }
             if (!warp_wait(bar(kBarAccFull + ab), (uint32_t)(tile / 2) & 1u, guard, lane)) break;
             tc_fence_after();
             const uint32_t acc = tmem + (uint32_t)(ab * TN) + ((uint32_t)(32 * q) << 16);
-            const bool rows_in = w.r0 < job.M;
+            const bool rows_in = w.r0 < w.rows;
 #pragma unroll 1
             for (int j = 0; j < kMine; j += 32) {
                 const int64_t c0 = n0 + j;
                 float v[32], x[GATED ? 32 : 1];
-                const bool in = rows_in && c0 < job.N;
+                const bool in = rows_in && c0 < N;
                 if (in && t.c0 < t.c1) {
                     tmem_ld32(acc + (uint32_t)(half * kMine + j), v);
                     if constexpr (GATED) tmem_ld32(acc + (uint32_t)(TN / 2 + half * kMine + j), x);
@@ -494,15 +527,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (lane == 0) mbar_arrive_cluster(cluster_addr(bar(kBarAccEmpty + ab), 0));
                 }
                 if (!in) continue;
-                if (job.partial != nullptr) {
-                    float *part = job.partial + t.part * job.part_elems;
+                if (partial != nullptr) {
+                    float *part = partial + t.part * job.part_elems;
                     const int64_t pc = (int64_t)(t.n0 / kCols) * TN + half * kMine + j;
-                    store32(part, job.part_ld, w, pc, job.part_ld, v);
-                    if constexpr (GATED) store32(part, job.part_ld, w, pc + TN / 2, job.part_ld, x);
+                    store32(part, job.part_ld, true, w, pc, job.part_ld, v);
+                    if constexpr (GATED) store32(part, job.part_ld, true, w, pc + TN / 2, job.part_ld, x);
                 } else if constexpr (GATED) {
-                    finish_gated<F16>(job.epi, w, c0, job.N, bias + j, bias + kMine + j, v, x);
+                    finish_gated<F16>(job.epi, w, c0, N, bias + j, bias + kMine + j, v, x);
                 } else {
-                    finish_dense<F16>(job.epi, w, c0, job.N, bias + j, v);
+                    finish_dense<F16>(job.epi, w, c0, N, bias + j, v);
                 }
             }
         }
@@ -607,18 +640,6 @@ typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, 
                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// rows: the operand's index i (M or N), K its contraction, box_rows of a stage.
-bool encode(EncodeTiled fn, CUtensorMap *map, const MmOperand &o, int rows, int K, int box_rows) {
-    const int64_t lines = o.across ? K : rows;
-    const cuuint64_t dims[2] = {(cuuint64_t)(o.across ? rows : K), (cuuint64_t)lines};
-    const cuuint64_t strides[1] = {(cuuint64_t)(lines > 1 ? 2 * o.ld : (2 * (int64_t)dims[0] + 15) / 16 * 16)};
-    const cuuint32_t box[2] = {64u, (cuuint32_t)(o.across ? kStep : box_rows)};
-    const cuuint32_t one[2] = {1u, 1u};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(o.p), dims, strides, box, one,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <bool F16, bool GATED, int TN>
 cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
     cudaError_t e = launch_pdl(mm_kernel<F16, GATED, TN>, dim3(2 * plan.pairs), dim3(kThreads), Shape<TN>::kSmem, s, p);
@@ -641,23 +662,24 @@ cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
 // a number of parts: the most that any pair is given, plus what joining costs.
 // A 128-wide tile's chunk takes 0.85 of it (half the products, but its a operand
 // is staged all the same); a unit's set-up and epilogue count as 2.
-double cost_of(const MmPlan &p, const MmJob *jobs, int n) {
+double cost_of(const MmPlan &p, int n) {
     const double chunk = p.tn == 256 ? 1.0 : 0.85;
     double most = 0, join = 0;
     int at[kMaxJobs + 1] = {0}, ends = 0;  // pairs where a job's units start over
     for (int i = 0; i < n; ++i) {
-        ends += p.cut[i].units;
+        const MmPlan::Cut &c = p.cut[p.order[i]];
+        ends += c.units;
         at[i + 1] = ends % p.pairs;
-        if (p.cut[i].parts > 1)
-            join += 8 + (double)p.cut[i].parts * (double)p.cut[i].part_elems * 8 / 1.4e6;
+        if (c.parts > 1) join += 8 + (double)c.parts * (double)c.part_elems * 8 / 1.4e6;
     }
     for (int k = 0; k <= n; ++k) {
         double load = 0;
         int begin = 0;
         for (int i = 0; i < n; ++i) {
-            const int end = begin + p.cut[i].units;  // units u with u % pairs == at[k]
+            const MmPlan::Cut &c = p.cut[p.order[i]];
+            const int end = begin + c.units;  // units u with u % pairs == at[k]
             const int count = (end - at[k] + p.pairs - 1) / p.pairs - (begin - at[k] + p.pairs - 1) / p.pairs;
-            load += count * (p.cut[i].chunks_per_part * chunk + 2);
+            load += count * (c.chunks_per_part * chunk + 2);
             begin = end;
         }
         most = std::max(most, load);
@@ -688,8 +710,8 @@ MmPlan plan_mm(const MmJob *jobs, int n, int sms) {
             tiles += (int64_t)c.tiles_m * c.tiles_n;
             longest = std::max(longest, c.chunks * jobs[i].terms);
         }
-        // parts of at least 4 chunks, and not many more units than pairs
-        for (int d = 1; d == 1 || (longest / d >= 4 && tiles * d <= 2 * pairs); d += std::max(1, d / 4)) {
+        // parts of at least 4 chunks, as many as pairs at most
+        for (int d = 1; d == 1 || (longest / d >= 4 && d <= pairs); d += std::max(1, d / 4)) {
             const int most = std::max(1, (longest + d - 1) / d);
             p.units = 0;
             for (int i = 0; i < n; ++i) {
@@ -701,8 +723,13 @@ MmPlan plan_mm(const MmJob *jobs, int n, int sms) {
                 c.units = c.tiles_m * c.tiles_n * c.parts;
                 p.units += c.units;
             }
+            // the longest units first
+            for (int i = 0; i < n; ++i) p.order[i] = i;
+            std::stable_sort(p.order, p.order + n, [&](int x, int y) {
+                return p.cut[x].chunks_per_part > p.cut[y].chunks_per_part;
+            });
             p.pairs = std::min(pairs, p.units);
-            const double cost = cost_of(p, jobs, n);
+            const double cost = cost_of(p, n);
             if (best.tn == 0 || cost < best_cost) {
                 best = p;
                 best_cost = cost;
@@ -715,6 +742,18 @@ MmPlan plan_mm(const MmJob *jobs, int n, int sms) {
         best.workspace += (size_t)best.cut[i].parts * best.cut[i].part_elems * sizeof(float);
     }
     return best;
+}
+
+bool encode_operand(const emtk_nn *nn, CUtensorMap *map, const MmOperand &o, int rows, int K, int box_rows) {
+    const int64_t lines = o.across ? K : rows;
+    const cuuint64_t dims[2] = {(cuuint64_t)(o.across ? rows : K), (cuuint64_t)lines};
+    const cuuint64_t strides[1] = {(cuuint64_t)(lines > 1 ? 2 * o.ld : (2 * (int64_t)dims[0] + 15) / 16 * 16)};
+    const cuuint32_t box[2] = {64u, (cuuint32_t)(o.across ? kStep : box_rows)};
+    const cuuint32_t one[2] = {1u, 1u};
+    return reinterpret_cast<EncodeTiled>(nn->encode)(
+               map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(o.p), dims, strides, box, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool mm_operand_ok(const void *p, int64_t ld, int64_t rows) {
@@ -736,23 +775,22 @@ cudaError_t init_mm_kernels() {
     EMTK_MM_ATTR(true, false, 128)
     EMTK_MM_ATTR(true, true, 128)
 #undef EMTK_MM_ATTR
-    return e;
+    return e == cudaSuccess ? init_skinny_kernels() : e;
 }
 
 cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_nn *nn, void *partial,
                       cudaStream_t s) {
     const bool gated = jobs[0].kind == kMmGated, f16 = jobs[0].type == EMTK_TYPE_F16, wide = plan.tn == 256;
-    const auto fn = reinterpret_cast<EncodeTiled>(nn->encode);
     MmParams p;
     int end = 0;
     for (int i = 0; i < n; ++i) {
-        const MmJob &j = jobs[i];
-        const MmPlan::Cut &c = plan.cut[i];
+        const MmJob &j = jobs[plan.order[i]];
+        const MmPlan::Cut &c = plan.cut[plan.order[i]];
         MmWork &w = p.job[i];
         if (j.K > 0) {
             bool ok = true;
-            for (int t = 0; t < j.terms; ++t) ok = ok && encode(fn, &w.a[t], j.a[t], j.M, j.K, 128);
-            for (int t = 0; t < (gated ? 2 : j.terms); ++t) ok = ok && encode(fn, &w.b[t], j.b[t], j.N, j.K, plan.tn / 2);
+            for (int t = 0; t < j.terms; ++t) ok = ok && encode_operand(nn, &w.a[t], j.a[t], j.M, j.K, 128);
+            for (int t = 0; t < (gated ? 2 : j.terms); ++t) ok = ok && encode_operand(nn, &w.b[t], j.b[t], j.N, j.K, plan.tn / 2);
             if (!ok) return cudaErrorInvalidValue;
         }
         w.epi = j.epi;
