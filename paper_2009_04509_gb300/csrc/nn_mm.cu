@@ -270,6 +270,17 @@ __device__ __forceinline__ void add_bias(const float *bias, float (&v)[32]) {
     }
 }
 
+// Gradients: nothing but the sums.  A variant of its own because the other
+// epilogues' code, unrolled over 32 columns and jumped over, cost as much as the
+// stores (20000 x 512 -> 2304, bf16: XX us against 62).
+template <bool F16>
+__device__ __forceinline__ void finish_plain(const Rows &w, int64_t c0, int64_t cols, const float (&v)[32]) {
+    if (w.out_f32)
+        store32(static_cast<float *>(w.out), w.out_ld, w.out_wide, w, c0, cols, v);
+    else
+        store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, v);
+}
+
 // Sums of a dense tile's 32 columns (z without its bias, which is in `bias`).
 template <bool F16>
 __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
@@ -318,12 +329,15 @@ __device__ __forceinline__ void finish_gated(const MmEpilogue &e, const Rows &w,
     store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, g);
 }
 
+enum Kind : int { kPlain, kDense, kGated };
+
 enum Bar : int { kBarFull = 0, kBarEmpty = 8, kBarAccFull = 16, kBarAccEmpty = 18, kBarDrain = 20, kBarStall = 21, kBars = 22 };
 
-template <bool F16, bool GATED, int TN>
+template <bool F16, Kind KIND, int TN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     mm_kernel(const __grid_constant__ MmParams p) {
     using S = Shape<TN>;
+    constexpr bool GATED = KIND == kGated;
     constexpr int kCols = GATED ? TN / 2 : TN;  // output columns of a tile
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -496,7 +510,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             __syncwarp();
             float *const partial = job.partial;
             const int N = job.N;
-            if (partial == nullptr && w.has_bias) {
+            if (KIND != kPlain && partial == nullptr && w.has_bias) {
                 for (int j = lane; j < kMine; j += 32) {
                     bias[j] = bias_at<F16>(job.epi, 0, n0 + j, N);
                     if (GATED) bias[kMine + j] = bias_at<F16>(job.epi, 1, n0 + j, N);
@@ -532,6 +546,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     const int64_t pc = (int64_t)(t.n0 / kCols) * TN + half * kMine + j;
                     store32(part, job.part_ld, true, w, pc, job.part_ld, v);
                     if constexpr (GATED) store32(part, job.part_ld, true, w, pc + TN / 2, job.part_ld, x);
+                } else if constexpr (KIND == kPlain) {
+                    finish_plain<F16>(w, c0, N, v);
                 } else if constexpr (GATED) {
                     finish_gated<F16>(job.epi, w, c0, N, bias + j, bias + kMine + j, v, x);
                 } else {
@@ -550,10 +566,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 // Adds the parts' sums and applies the epilogue: 2^lanes_log2 neighbouring
 // threads (8 at most) take 8 columns of a row, each every so-manieth part, and
 // join their sums in a fixed tree; four such groups hold a checkpoint block.
-template <bool F16, bool GATED, int TN>
+template <bool F16, Kind KIND, int TN>
 __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEpilogue e, const float *partial,
                                                     int64_t part_elems, int64_t part_ld, int parts, int M, int N,
                                                     int groups, int lanes_log2) {
+    constexpr bool GATED = KIND == kGated;
     constexpr int kCols = GATED ? TN / 2 : TN;
     const int64_t tid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int lanes = 1 << lanes_log2, mine = threadIdx.x & (lanes - 1);
@@ -640,9 +657,9 @@ typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, 
                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-template <bool F16, bool GATED, int TN>
+template <bool F16, Kind KIND, int TN>
 cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
-    cudaError_t e = launch_pdl(mm_kernel<F16, GATED, TN>, dim3(2 * plan.pairs), dim3(kThreads), Shape<TN>::kSmem, s, p);
+    cudaError_t e = launch_pdl(mm_kernel<F16, KIND, TN>, dim3(2 * plan.pairs), dim3(kThreads), Shape<TN>::kSmem, s, p);
     for (int i = 0; i < p.jobs && e == cudaSuccess; ++i) {
         const MmWork &w = p.job[i];
         if (w.parts == 1) continue;
@@ -651,7 +668,7 @@ cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
         while (lanes_log2 < 3 && (2 << lanes_log2) <= w.parts && ((int64_t)w.M * groups << lanes_log2) < 2 * 2048 * plan.pairs)
             ++lanes_log2;
         const int64_t threads = (int64_t)w.M * groups << lanes_log2;
-        e = launch_pdl(parts_kernel<F16, GATED, TN>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, w.epi,
+        e = launch_pdl(parts_kernel<F16, KIND, TN>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, w.epi,
                        static_cast<const float *>(w.partial), w.part_elems, w.part_ld, w.parts, w.M, w.N, groups,
                        lanes_log2);
     }
@@ -762,25 +779,38 @@ bool mm_operand_ok(const void *p, int64_t ld, int64_t rows) {
 
 cudaError_t init_mm_kernels() {
     cudaError_t e = cudaSuccess;
-#define EMTK_MM_ATTR(F16, GATED, TN)                                                                            \
-    if (e == cudaSuccess)                                                                                       \
-        e = cudaFuncSetAttribute(mm_kernel<F16, GATED, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize,        \
+#define EMTK_MM_ATTR(F16, KIND, TN)                                                                       \
+    if (e == cudaSuccess)                                                                                 \
+        e = cudaFuncSetAttribute(mm_kernel<F16, KIND, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, \
                                  Shape<TN>::kSmem);
-    EMTK_MM_ATTR(false, false, 256)
-    EMTK_MM_ATTR(false, true, 256)
-    EMTK_MM_ATTR(true, false, 256)
-    EMTK_MM_ATTR(true, true, 256)
-    EMTK_MM_ATTR(false, false, 128)
-    EMTK_MM_ATTR(false, true, 128)
-    EMTK_MM_ATTR(true, false, 128)
-    EMTK_MM_ATTR(true, true, 128)
+#define EMTK_MM_ATTRS(KIND)        \
+    EMTK_MM_ATTR(false, KIND, 256) \
+    EMTK_MM_ATTR(true, KIND, 256)  \
+    EMTK_MM_ATTR(false, KIND, 128) \
+    EMTK_MM_ATTR(true, KIND, 128)
+    EMTK_MM_ATTRS(kPlain)
+    EMTK_MM_ATTRS(kDense)
+    EMTK_MM_ATTRS(kGated)
+#undef EMTK_MM_ATTRS
 #undef EMTK_MM_ATTR
     return e == cudaSuccess ? init_skinny_kernels() : e;
 }
 
+namespace {
+template <bool F16, Kind KIND>
+cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
+    return plan.tn == 256 ? run<F16, KIND, 256>(p, plan, s) : run<F16, KIND, 128>(p, plan, s);
+}
+template <bool F16>
+cudaError_t run(const MmParams &p, const MmPlan &plan, bool gated, bool plain, cudaStream_t s) {
+    if (gated) return run<F16, kGated>(p, plan, s);
+    return plain ? run<F16, kPlain>(p, plan, s) : run<F16, kDense>(p, plan, s);
+}
+}  // namespace
+
 cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_nn *nn, void *partial,
                       cudaStream_t s) {
-    const bool gated = jobs[0].kind == kMmGated, f16 = jobs[0].type == EMTK_TYPE_F16, wide = plan.tn == 256;
+    const bool gated = jobs[0].kind == kMmGated, f16 = jobs[0].type == EMTK_TYPE_F16;
     MmParams p;
     int end = 0;
     for (int i = 0; i < n; ++i) {
@@ -814,11 +844,12 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
     p.status = nn->status;
     p.timeout_ns = nn->timeout_ns;
     p.debug_stall = nn->debug_stall;
-    if (f16)
-        return gated ? (wide ? run<true, true, 256>(p, plan, s) : run<true, true, 128>(p, plan, s))
-                     : (wide ? run<true, false, 256>(p, plan, s) : run<true, false, 128>(p, plan, s));
-    return gated ? (wide ? run<false, true, 256>(p, plan, s) : run<false, true, 128>(p, plan, s))
-                 : (wide ? run<false, false, 256>(p, plan, s) : run<false, false, 128>(p, plan, s));
+    bool plain = !gated;
+    for (int i = 0; i < n; ++i) {
+        const MmEpilogue &e = jobs[i].epi;
+        plain = plain && e.act == EMTK_ACT_NONE && !e.bias[0] && !e.residual.d && !e.saved[0].d;
+    }
+    return f16 ? run<true>(p, plan, gated, plain, s) : run<false>(p, plan, gated, plain, s);
 }
 
 }  // namespace emtk
