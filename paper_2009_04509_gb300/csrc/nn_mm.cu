@@ -35,8 +35,7 @@ constexpr int kABytes = 128 * kStep * 2;  // a CTA's rows of a stage
 constexpr int kEpiWarps = 8;
 constexpr int kFirstEpiWarp = 4;
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
-constexpr int kRowBytes = 80;            // staged row: 64 bytes, padded against bank conflicts
-constexpr int kStageRowsBytes = 32 * kRowBytes;
+constexpr int kStageRowsBytes = 32 * 64;  // an epilogue warp's staged block: 32 rows of 64 bytes
 constexpr int kBiasBytes = 128 * 4;      // an epilogue warp's columns
 
 template <int TN>
@@ -99,6 +98,10 @@ __device__ __forceinline__ bool wide_rows(const void *p, int64_t ld, int elem) {
     return ((reinterpret_cast<uintptr_t>(p) | (uint64_t)(ld * elem)) & 15u) == 0;
 }
 
+// 16-byte piece c of staged row r: the pieces are permuted so that neither a
+// lane to a row nor four lanes to a row meet in a bank.
+__device__ __forceinline__ uint32_t staged(int r, int c) { return (uint32_t)(r * 64 + ((c ^ (r >> 1)) & 3) * 16); }
+
 // Rows r0 .. r0 + 31 (below `rows`), columns c0 .. c0 + 64 / sizeof(T) - 1 (below
 // `cols`) of a matrix, between memory and the warp's staged rows; four lanes move
 // a row where 16-byte pieces fit, a row at a time where they do not.
@@ -109,9 +112,9 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
     const int nr = (int)min((int64_t)32, rows - r0), nc = (int)min((int64_t)kCols, cols - c0);
     if (wide && nr == 32 && nc == kCols) {  // a whole block: four unconditional 16-byte moves a lane
         T *g = base + (r0 + (lane >> 2)) * ld + c0 + (lane & 3) * kPiece;
-        uint8_t *s = stage + (lane >> 2) * kRowBytes + (lane & 3) * 16;
+        uint8_t *s = stage + staged(lane >> 2, lane & 3);  // 8 rows on, the same permutation
 #pragma unroll
-        for (int it = 0; it < 4; ++it, g += 8 * ld, s += 8 * kRowBytes) {
+        for (int it = 0; it < 4; ++it, g += 8 * ld, s += 8 * 64) {
             if (LOAD)
                 *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
             else
@@ -124,7 +127,7 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
             const int r = it * 8 + (lane >> 2);
             if (r >= nr || c >= nc) continue;
             T *g = base + (r0 + r) * ld + c0 + c;
-            uint8_t *s = stage + r * kRowBytes + (lane & 3) * 16;
+            uint8_t *s = stage + staged(r, lane & 3);
             if (c + kPiece <= nc) {
                 if (LOAD)
                     *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
@@ -141,22 +144,21 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
         }
     } else if (lane < nc) {
         T *g = base + r0 * ld + c0 + lane;
-        uint8_t *s = stage + lane * sizeof(T);
-        for (int r = 0; r < nr; r += 8) {  // eight rows' elements in flight
+        const int piece = lane * (int)sizeof(T) / 16, in_piece = lane * (int)sizeof(T) % 16;
+        for (int r = 0; r < nr; r += 8, g += 8 * ld) {  // eight rows' elements in flight
             T x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (r + i < nr) x[i] = LOAD ? g[i * ld] : *reinterpret_cast<const T *>(s + i * kRowBytes);
+                if (r + i < nr)
+                    x[i] = LOAD ? g[i * ld] : *reinterpret_cast<const T *>(stage + staged(r + i, piece) + in_piece);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (r + i < nr) {
                     if (LOAD)
-                        *reinterpret_cast<T *>(s + i * kRowBytes) = x[i];
+                        *reinterpret_cast<T *>(stage + staged(r + i, piece) + in_piece) = x[i];
                     else
                         g[i * ld] = x[i];
                 }
-            g += 8 * ld;
-            s += 8 * kRowBytes;
         }
     }
 }
@@ -188,10 +190,9 @@ struct Rows {
 template <bool F16>
 __device__ __forceinline__ void store16(void *base, int64_t ld, bool wide, const Rows &w, int64_t c0, int64_t cols,
                                         const float (&v)[32]) {
-    uint8_t *row = w.stage + w.lane * kRowBytes;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        reinterpret_cast<uint4 *>(row)[i] =
+        *reinterpret_cast<uint4 *>(w.stage + staged(w.lane, i)) =
             make_uint4(pack16<F16>(v[8 * i], v[8 * i + 1]), pack16<F16>(v[8 * i + 2], v[8 * i + 3]),
                        pack16<F16>(v[8 * i + 4], v[8 * i + 5]), pack16<F16>(v[8 * i + 6], v[8 * i + 7]));
     __syncwarp();
@@ -201,13 +202,12 @@ __device__ __forceinline__ void store16(void *base, int64_t ld, bool wide, const
 
 __device__ __forceinline__ void store32(float *base, int64_t ld, bool wide, const Rows &w, int64_t c0, int64_t cols,
                                         const float (&v)[32]) {
-    float4 *row = reinterpret_cast<float4 *>(w.stage + w.lane * kRowBytes);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int j = 16 * half + 4 * i;
-            row[i] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            *reinterpret_cast<float4 *>(w.stage + staged(w.lane, i)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
         }
         __syncwarp();
         if (c0 + 16 * half < cols)
@@ -292,10 +292,9 @@ __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w,
         move_block<uint16_t, true>(static_cast<uint16_t *>(w.residual), w.residual_ld, w.r0, w.rows, c0, cols,
                                    w.residual_wide, w.stage, w.lane);
         __syncwarp();
-        const uint4 *row = reinterpret_cast<const uint4 *>(w.stage + w.lane * kRowBytes);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint4 q = row[i];
+            const uint4 q = *reinterpret_cast<const uint4 *>(w.stage + staged(w.lane, i));
             const uint32_t x[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

@@ -39,8 +39,11 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// Arrives at a barrier of the cluster after TMEM loads that have completed.  Relaxed:
+// the waiter reads no memory that this thread wrote, and a release would first
+// wait for all of the thread's global stores.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // Arrives expecting bytes; orders nothing (the thread has written nothing that
 // the barrier's waiters read).
