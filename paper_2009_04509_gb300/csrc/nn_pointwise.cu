@@ -1,9 +1,9 @@
 // Pointwise passes of the dense and gated layers' gradients, and the 8-bit
 // checkpoints.  All of them stream, every element read once, and HBM bounds
-// them.  Where every operand's rows start on 16 bytes (8 for codes) and hold a
-// multiple of 8 columns, a thread takes 8 neighbouring columns with one load and
-// keeps the next ones in flight; elsewhere a warp takes 32 neighbouring columns
-// at a time, one element a lane, which coalesces at any alignment.
+// them.  A thread takes 8 neighbouring columns.  Where every operand's rows start
+// on 16 bytes (8 for codes) and hold a multiple of 8 columns, that is one load,
+// with the next ones in flight; elsewhere it is the two aligned words around
+// them, shifted into place, or single elements at the ends of rows and matrices.
 #include <algorithm>
 
 #include "emtk_internal.h"
@@ -65,30 +65,56 @@ struct Piece<true> {
     }
 };
 
-// Columns c0 + stride i of row r, one element each; those from n on read the last
-// column's (every load is issued, none waits for a branch).
+// Columns c .. c + 7 of row r at any alignment; those from n on are 0.  Away from
+// the matrix's first and last bytes, the two aligned words that hold a full piece
+// lie inside the matrix (between its rows, at worst) and are read whole.
 template <bool F16, bool Q8>
-__device__ __forceinline__ void load_strided(const Source &s, int64_t r, int64_t c0, int stride, int n, float (&v)[kVec]) {
-    const uint8_t *row = s.p + r * s.row_bytes;
-    uint32_t x[kVec], scale[Q8 ? kVec : 1];
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        const int64_t c = min(c0 + (int64_t)i * stride, (int64_t)n - 1);
-        if (Q8) {
-            x[i] = __ldg(row + c);
-            scale[i] = __ldg(s.scale + r * s.ld_scale + c / kQ8Block);
+__device__ __forceinline__ void load_any(const Source &s, int64_t r, int64_t c, int rows, int n, float *v) {
+    constexpr int kBytes = Q8 ? 1 : 2, kWord = kVec * kBytes;
+    const uint8_t *p = s.p + r * s.row_bytes + kBytes * c;
+    const int shift = (int)(reinterpret_cast<uintptr_t>(p) % kWord);
+    const uint8_t *const word = p - shift;
+    const uint8_t *const end = s.p + (int64_t)(rows - 1) * s.row_bytes + (int64_t)kBytes * n;
+    const uint32_t scale = Q8 && c < n ? __ldg(s.scale + r * s.ld_scale + c / kQ8Block) : 1u;
+    const bool whole = c + kVec <= n && word >= s.p && word + (shift ? 2 : 1) * kWord <= end;
+    if (Q8) {
+        uint64_t x = 0;
+        if (whole) {
+            x = __ldg(reinterpret_cast<const unsigned long long *>(word));
+            if (shift) {
+                const uint64_t y = __ldg(reinterpret_cast<const unsigned long long *>(word) + 1);
+                x = (x >> (8 * shift)) | (y << (64 - 8 * shift));
+            }
         } else {
-            x[i] = __ldg(reinterpret_cast<const uint16_t *>(row) + c);
-        }
-    }
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        if (Q8) {
-            const int q = (int8_t)x[i];
-            v[i] = q == -128 ? __int_as_float(0x7fffffff) : (float)q * q8_step(scale[Q8 ? i : 0]);
-        } else {
-            v[i] = from16<F16>(x[i]);
+            for (int i = 0; i < kVec; ++i)
+                if (c + i < n) x |= (uint64_t)__ldg(p + i) << (8 * i);
         }
+        q8_values4((uint32_t)x, q8_step(scale), v);
+        q8_values4((uint32_t)(x >> 32), q8_step(scale), v + 4);
+    } else {
+        uint32_t x[8] = {};
+        if (whole) {
+            const uint4 a = __ldg(reinterpret_cast<const uint4 *>(word));
+            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+            if (shift) {
+                const uint4 b = __ldg(reinterpret_cast<const uint4 *>(word) + 1);
+                x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 6; ++i) x[i] = shift & 8 ? x[i + 2] : x[i];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) x[i] = shift & 4 ? x[i + 1] : x[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = shift & 2 ? __funnelshift_r(x[i], x[i + 1], 16) : x[i];
+        } else {
+            const uint16_t *e = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (c + i < n) x[i / 2] |= (uint32_t)__ldg(e + i) << (16 * (i % 2));
+        }
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = from16<F16>((x[i / 2] >> (16 * (i % 2))) & 0xffffu);
     }
 }
 
@@ -97,12 +123,25 @@ __device__ __forceinline__ uint4 pack8x16(const float *v) {
     return make_uint4(pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7]));
 }
 
+// Columns c .. c + 7 (below n) of a row, in one store where it may be.
+template <bool F16>
+__device__ __forceinline__ void store_any(uint16_t *row, int64_t c, int n, bool wide, const float *v) {
+    if (wide && c + kVec <= n) {
+        *reinterpret_cast<uint4 *>(row + c) = pack8x16<F16>(v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (c + i < n) row[c + i] = (uint16_t)to16<F16>(v[i]);
+    }
+}
+
 // ------------------------------------------------------------- slopes
 // A block takes 8 * lanes columns (lanes = 32 .. 4, the fewest that cover
 // narrow matrices) and one slice of the rows, kThreads / lanes rows at a time;
 // a thread adds its rows in order, the block its threads' sums and the second
 // kernel the slices' in fixed orders, so the column sums do not depend on
-// timing.
+// timing.  Up to 512 rows are one slice of 4 lanes' columns, whose sums are the
+// result.
 struct SlopeShape {
     int lanes_log2;  // threads across
     int col_blocks, slices;
@@ -114,13 +153,14 @@ struct SlopeShape {
 SlopeShape slope_shape(int m, int n, int sms, bool sums) {
     SlopeShape h;
     h.lanes_log2 = 5;
-    while (h.lanes_log2 > 2 && (kVec << (h.lanes_log2 - 1)) >= n) --h.lanes_log2;
+    while (h.lanes_log2 > 2 && ((kVec << (h.lanes_log2 - 1)) >= n || (sums && m <= 512))) --h.lanes_log2;
     const int cols = kVec << h.lanes_log2;
     const int at_once = kThreads >> h.lanes_log2;
     h.col_blocks = (int)(((int64_t)n + cols - 1) / cols);
     int64_t slices = std::max<int64_t>(1, (int64_t)(sums ? 8 : 24) * sms / std::max(1, h.col_blocks));
     slices = std::min<int64_t>(slices, std::max<int64_t>(1, ((int64_t)m + 2 * at_once - 1) / (2 * at_once)));
     slices = std::min<int64_t>(slices, 65535);
+    if (sums && m <= 512) slices = 1;
     int64_t rows = ((int64_t)m + slices - 1) / slices;
     rows = (rows + at_once - 1) / at_once * at_once;
     rows = std::max<int64_t>(rows, at_once);
@@ -135,8 +175,8 @@ struct SlopeArgs {
     int64_t d_ld;
     uint16_t *h;
     int64_t h_ld;
-    float *partial;  // [slices][n], gated: [2][slices][n]; null: no sums
-    int m, n, rows, lanes_log2;
+    float *sums[2];  // of dg and du: [slices][n] each; null: none
+    int m, n, rows, lanes_log2, h_wide;
 };
 
 template <bool GATED, int ACT>
@@ -148,10 +188,9 @@ __device__ __forceinline__ void slope_of(float d, float g, float u, float &dg, f
     h = f * u;
 }
 
-// The block's sums of each column, from its threads' (column base + index).
+// The block's sums of each column, from its threads'.
 template <bool GATED>
-__device__ __forceinline__ void block_sums(const SlopeArgs &a, const float (&sg)[kVec], const float (&su)[kVec],
-                                           bool strided) {
+__device__ __forceinline__ void block_sums(const SlopeArgs &a, const float (&sg)[kVec], const float (&su)[kVec]) {
     __shared__ float part[kThreads * kVec];
     const int cols = kVec << a.lanes_log2, lanes = 1 << a.lanes_log2, at_once = kThreads >> a.lanes_log2;
     const int64_t col = (int64_t)blockIdx.x * cols + threadIdx.x;
@@ -161,12 +200,12 @@ __device__ __forceinline__ void block_sums(const SlopeArgs &a, const float (&sg)
     for (int half = 0; half < (GATED ? 2 : 1); ++half) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) row[strided ? i * lanes + tl : tl * kVec + i] = half ? su[i] : sg[i];
+        for (int i = 0; i < kVec; ++i) row[tl * kVec + i] = half ? su[i] : sg[i];
         __syncthreads();
         if ((int)threadIdx.x < cols && col < a.n) {
             float sum = 0.f;
             for (int g = 0; g < at_once; ++g) sum += part[g * cols + threadIdx.x];
-            a.partial[((int64_t)half * gridDim.y + blockIdx.y) * a.n + col] = sum;
+            a.sums[half][(int64_t)blockIdx.y * a.n + col] = sum;
         }
     }
 }
@@ -229,46 +268,45 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const __grid_constant__
             h += at_once * a.h_ld;
         }
     }
-    if constexpr (SUMS) block_sums<GATED>(a, sg, su, false);
+    if constexpr (SUMS) block_sums<GATED>(a, sg, su);
 }
 
-// Any alignment, width and mixture of operands.
+// Any alignment and width.
 template <bool F16, bool GATED, int ACT, bool Q8>
 __global__ void __launch_bounds__(kThreads) slope_any_kernel(const __grid_constant__ SlopeArgs a) {
     constexpr bool kGate = GATED || ACT != EMTK_ACT_NONE;
-    const int lanes = 1 << a.lanes_log2, at_once = kThreads >> a.lanes_log2;
-    const int64_t c0 = (int64_t)blockIdx.x * (kVec << a.lanes_log2) + (threadIdx.x & (lanes - 1));
-    const int64_t r0 = (int64_t)blockIdx.y * a.rows + (threadIdx.x >> a.lanes_log2);
+    const int at_once = kThreads >> a.lanes_log2;
+    const int64_t c = (int64_t)blockIdx.x * (kVec << a.lanes_log2) + (threadIdx.x & ((1 << a.lanes_log2) - 1)) * kVec;
     const int64_t r1 = min((int64_t)(blockIdx.y + 1) * a.rows, (int64_t)a.m);
     float sg[kVec] = {}, su[kVec] = {};
     pdl_trigger();
     pdl_wait();
-    for (int64_t r = r0; r < r1; r += at_once) {
-        float d[kVec], g[kVec] = {}, u[kVec] = {};
-        load_strided<F16, false>(a.dy, r, c0, lanes, a.n, d);
-        if (kGate) load_strided<F16, Q8>(a.gate, r, c0, lanes, a.n, g);
-        if (GATED) load_strided<F16, Q8>(a.up, r, c0, lanes, a.n, u);
-        uint16_t *dg = a.dg + r * a.d_ld + c0, *du = a.du + r * a.d_ld + c0, *h = a.h + r * a.h_ld + c0;
+    if (c < a.n) {
+        for (int64_t r = (int64_t)blockIdx.y * a.rows + (threadIdx.x >> a.lanes_log2); r < r1; r += at_once) {
+            float d[kVec], g[kVec] = {}, u[kVec] = {}, x[kVec], y[kVec], z[kVec];
+            load_any<F16, false>(a.dy, r, c, a.m, a.n, d);
+            if (kGate) load_any<F16, Q8>(a.gate, r, c, a.m, a.n, g);
+            if (GATED) load_any<F16, Q8>(a.up, r, c, a.m, a.n, u);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            float x, y, z;
-            slope_of<GATED, ACT>(d[i], g[i], u[i], x, y, z);
-            sg[i] = __fadd_rn(sg[i], x);
-            if (GATED) su[i] = __fadd_rn(su[i], y);
-            const bool in = c0 + i * lanes < a.n;
-            if (in && a.dg) dg[i * lanes] = (uint16_t)to16<F16>(x);
-            if (in && GATED && a.du) du[i * lanes] = (uint16_t)to16<F16>(y);
-            if (in && GATED && a.h) h[i * lanes] = (uint16_t)to16<F16>(z);
+            for (int i = 0; i < kVec; ++i) {
+                slope_of<GATED, ACT>(d[i], g[i], u[i], x[i], y[i], z[i]);
+                sg[i] = __fadd_rn(sg[i], x[i]);
+                if (GATED) su[i] = __fadd_rn(su[i], y[i]);
+            }
+            // dg and du lie in the workspace, whose rows have room for a last full piece
+            if (a.dg) *reinterpret_cast<uint4 *>(a.dg + r * a.d_ld + c) = pack8x16<F16>(x);
+            if (GATED && a.du) *reinterpret_cast<uint4 *>(a.du + r * a.d_ld + c) = pack8x16<F16>(y);
+            if (GATED && a.h) store_any<F16>(a.h + r * a.h_ld, c, a.n, a.h_wide != 0, z);
         }
     }
-    if (a.partial) block_sums<GATED>(a, sg, su, true);
+    if (a.sums[0]) block_sums<GATED>(a, sg, su);
 }
 
 // Column sums from the slices' partial sums: a block takes 32 columns, each of
 // its 32 warps every 32nd slice, and the warps' sums are added in order.
 constexpr int kSumWarps = 32;
-__global__ void __launch_bounds__(32 * kSumWarps) slice_sum_kernel(const float *partial, int slices, int n, float *db0,
-                                                                   float *db1) {
+__global__ void __launch_bounds__(32 * kSumWarps) slice_sum_kernel(const float *s0, const float *s1, int slices, int n,
+                                                                   float *db0, float *db1) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     __shared__ float part[kSumWarps][32];
@@ -276,7 +314,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) slice_sum_kernel(const float *
     pdl_wait();
     float sum = 0.f;
     if (c < n) {
-        const float *p = partial + (int64_t)blockIdx.y * slices * n + c;
+        const float *p = (blockIdx.y ? s1 : s0) + c;
 #pragma unroll 8
         for (int s = warp; s < slices; s += kSumWarps) sum += p[(int64_t)s * n];
     }
@@ -309,21 +347,27 @@ SlopeKernel slope_for(int act, bool wide, bool q8, bool sums) {
 }
 
 template <bool GATED>
-cudaError_t run_slope(emtk_type type, int act, SlopeArgs &a, float *db0, float *db1, int sms, cudaStream_t s) {
+cudaError_t run_slope(emtk_type type, int act, SlopeArgs &a, float *partial, float *db0, float *db1, int sms,
+                      cudaStream_t s) {
     if (a.n == 0) return cudaSuccess;
-    const SlopeShape h = slope_shape(a.m, a.n, sms, a.partial != nullptr);
+    const bool gate = GATED || act != EMTK_ACT_NONE, sums = db0 != nullptr;
+    const SlopeShape h = slope_shape(a.m, a.n, sms, sums);
     a.rows = h.rows;
     a.lanes_log2 = h.lanes_log2;
-    const bool gate = GATED || act != EMTK_ACT_NONE;
+    a.sums[0] = h.slices == 1 ? db0 : partial;
+    a.sums[1] = h.slices == 1 ? db1 : partial + (int64_t)h.slices * a.n;
+    if (!sums) a.sums[0] = a.sums[1] = nullptr;
+    a.h_wide = a.h && wide_matrix(a.h, 2 * a.h_ld, 16);
     const bool wide = wide_source(a.dy, a.n) && (!gate || wide_source(a.gate, a.n)) &&
-                      (!GATED || wide_source(a.up, a.n)) && (!a.h || wide_matrix(a.h, 2 * a.h_ld, 16));
-    const bool q8 = gate && a.gate.scale != nullptr, sums = a.partial != nullptr;
+                      (!GATED || wide_source(a.up, a.n)) && (!a.h || a.h_wide);
+    const bool q8 = gate && a.gate.scale != nullptr;
     const SlopeKernel kernel = type == EMTK_TYPE_F16 ? slope_for<true, GATED>(act, wide, q8, sums)
                                                      : slope_for<false, GATED>(act, wide, q8, sums);
     cudaError_t e = launch_pdl(kernel, dim3((unsigned)h.col_blocks, (unsigned)h.slices), dim3(kThreads), 0, s, a);
-    if (e == cudaSuccess && sums)
+    if (e == cudaSuccess && sums && h.slices > 1)
         e = launch_pdl(slice_sum_kernel, dim3((unsigned)((a.n - 1) / 32 + 1), GATED ? 2u : 1u), dim3(32 * kSumWarps), 0,
-                       s, static_cast<const float *>(a.partial), h.slices, a.n, db0, db1);
+                       s, static_cast<const float *>(a.sums[0]), static_cast<const float *>(a.sums[1]), h.slices, a.n,
+                       db0, db1);
     return e;
 }
 
@@ -396,29 +440,27 @@ __global__ void __launch_bounds__(kThreads) pack8_kernel(const __grid_constant__
     }
 }
 
-// Any alignment: a block of 32 columns is a warp's lanes.
+// Any alignment.
 template <bool F16>
 __global__ void __launch_bounds__(kThreads) pack8_any_kernel(const __grid_constant__ PackArgs a) {
     const int lane = threadIdx.x & 31;
     pdl_trigger();
     pdl_wait();
     for (Item it(a.walk, (int64_t)blockIdx.x * kWarps + threadIdx.x / 32); it.r < a.m; it.next(a.walk)) {
-        const int64_t c0 = (int64_t)it.piece * kWarpCols + lane;
-        float v[kVec];
-        load_strided<F16, false>(a.x, it.r, c0, 32, a.k, v);
+        const int64_t c = (int64_t)it.piece * kWarpCols + lane * kVec;
+        float v[kVec] = {};
+        if (c < a.k) load_any<F16, false>(a.x, it.r, c, a.m, a.k, v);
+        bool all_finite;
+        float top = finite_top(v, all_finite);
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        if (c >= a.k) continue;
+        const uint32_t b = q8_scale(top);
+        if ((lane & 3) == 0) a.scale[it.r * a.ld_scale + c / kQ8Block] = (uint8_t)b;
+        const uint32_t w[2] = {q8_codes4(v, q8_inverse(b), all_finite), q8_codes4(v + 4, q8_inverse(b), all_finite)};
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            const int64_t c = c0 + 32 * i;
-            if (c - lane >= a.k) break;  // the whole warp; a last column read again changes no maximum
-            const bool finite = fabsf(v[i]) < __int_as_float(0x7f800000);
-            // magnitudes of floats compare as their bits do
-            const uint32_t top = __reduce_max_sync(0xffffffffu, finite ? __float_as_uint(fabsf(v[i])) : 0u);
-            const uint32_t b = q8_scale(__uint_as_float(top));
-            if (c >= a.k) continue;
-            if (lane == 0) a.scale[it.r * a.ld_scale + c / kQ8Block] = (uint8_t)b;
-            a.q[it.r * a.q_ld + c] =
-                (uint8_t)(finite ? __float_as_uint(fmaf(v[i], q8_inverse(b), 12582912.f)) : 0x80u);
-        }
+        for (int i = 0; i < kVec; ++i)
+            if (c + i < a.k) a.q[it.r * a.q_ld + c + i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
     }
 }
 
@@ -427,7 +469,7 @@ struct CopyArgs {
         Source from;
         uint16_t *to;
         int64_t to_ld;
-        int rows, cols, wide;
+        int rows, cols, wide, to_wide;
         Walk walk;
     } job[kMaxCopies];
 };
@@ -460,14 +502,22 @@ __device__ __forceinline__ void copy_wide(const CopyArgs::One &j, Item it, int l
 
 template <bool F16, bool Q8>
 __device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it, int lane) {
-    for (; it.r < j.rows; it.next(j.walk)) {
-        const int64_t c0 = (int64_t)it.piece * kWarpCols + lane;
-        float v[kVec];
-        load_strided<F16, Q8>(j.from, it.r, c0, 32, j.cols, v);
-        uint16_t *to = j.to + it.r * j.to_ld + c0;
+    while (it.r < j.rows) {
+        float v[2][kVec];
+        int64_t r[2], c[2];
 #pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (c0 + 32 * i < j.cols) to[32 * i] = (uint16_t)to16<F16>(Q8 ? q8_operand<F16>(v[i]) : v[i]);
+        for (int i = 0; i < 2; ++i, it.next(j.walk)) {
+            r[i] = it.r;
+            c[i] = (int64_t)it.piece * kWarpCols + lane * kVec;
+            if (r[i] < j.rows && c[i] < j.cols) load_any<F16, Q8>(j.from, r[i], c[i], j.rows, j.cols, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (r[i] >= j.rows || c[i] >= j.cols) continue;
+#pragma unroll
+            for (int t = 0; t < kVec; ++t) v[i][t] = Q8 ? q8_operand<F16>(v[i][t]) : v[i][t];
+            store_any<F16>(j.to + r[i] * j.to_ld, c[i], j.cols, j.to_wide != 0, v[i]);
+        }
     }
 }
 
@@ -507,10 +557,9 @@ cudaError_t launch_slope(emtk_type type, int act, int m, int n, const emtk_matri
     if (act != EMTK_ACT_NONE) a.gate = source_of(pre);
     a.dg = static_cast<uint16_t *>(dz);
     a.d_ld = dz_ld;
-    a.partial = db ? partial : nullptr;
     a.m = m;
     a.n = n;
-    return run_slope<false>(type, act, a, db, nullptr, sms, s);
+    return run_slope<false>(type, act, a, partial, db, nullptr, sms, s);
 }
 
 cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk_matrix &dh, const emtk_matrix &gate,
@@ -525,10 +574,9 @@ cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk
     a.d_ld = d_ld;
     a.h = static_cast<uint16_t *>(h.d);
     a.h_ld = h.ld;
-    a.partial = db_gate ? partial : nullptr;
     a.m = m;
     a.n = f;
-    return run_slope<true>(type, act, a, db_gate, db_up, sms, s);
+    return run_slope<true>(type, act, a, partial, db_gate, db_up, sms, s);
 }
 
 cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
@@ -551,8 +599,9 @@ cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, 
         const Copy16 &c = copies[i];
         if (c.rows == 0 || c.cols == 0) continue;
         const Source from = source_of(c.from);
+        const bool to_wide = wide_matrix(c.to.d, 2 * c.to.ld, 16);
         a.job[jobs++] = {from, static_cast<uint16_t *>(c.to.d), c.to.ld, c.rows, c.cols,
-                         wide_source(from, c.cols) && wide_matrix(c.to.d, 2 * c.to.ld, 16), walk_of(c.cols, blocks)};
+                         to_wide && wide_source(from, c.cols), to_wide, walk_of(c.cols, blocks)};
     }
     if (jobs == 0) return cudaSuccess;
     return launch_pdl(type == EMTK_TYPE_F16 ? copy16_kernel<true> : copy16_kernel<false>, dim3(blocks, 1, jobs),

@@ -410,31 +410,29 @@ def _type_of(t, what: str, f32: bool = False) -> int:
 
 
 def _mat(t, rows: int, cols: int, dtype, what: str) -> tuple:
-    """(d, ld, d_scale, ld_scale) of a [rows][cols] tensor of dtype, or a Q8 where dtype is a
-    (dtype, Q8) pair; absent for None."""
+    """(d, ld, d_scale, ld_scale) of a [rows][cols] CUDA tensor of dtype; absent for None."""
     if t is None:
         return _ABSENT
-    if type(dtype) is tuple:
-        if isinstance(t, Q8):
-            import torch
-            d, ld, _, _ = _mat(t.codes, rows, cols, torch.int8, what)
-            s, lds, _, _ = _mat(t.scales, rows, (cols + 31) // 32, torch.uint8, what)
-            return (d, ld, s, lds)
-        dtype = dtype[0]
-    if t.dtype is not dtype:
-        raise ValueError(f"{what}: dtype {t.dtype}, expected {dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(rows, cols)}")
-    ld, unit = t.stride()
-    if unit != 1 and cols > 1:
-        raise ValueError(f"{what}: columns must be contiguous")
-    if ld < cols:
-        if rows > 1:
-            raise ValueError(f"{what}: rows overlap")
-        ld = cols  # one row: its distance to the next says nothing
-    if not t.is_cuda:
-        raise ValueError(f"{what}: not a CUDA tensor")
-    return (t.data_ptr(), ld, 0, 0)
+    if t.dtype is dtype and t.is_cuda:
+        shape = t.shape
+        if len(shape) == 2 and shape[0] == rows and shape[1] == cols:
+            ld, unit = t.stride()
+            if unit == 1 and ld >= cols:
+                return (t.data_ptr(), ld, 0, 0)
+            if (unit == 1 or cols <= 1) and (ld >= cols or rows <= 1):
+                return (t.data_ptr(), max(ld, cols), 0, 0)  # one row or column: its stride says nothing
+            raise ValueError(f"{what}: strides {t.stride()}: a row's elements must be neighbours and rows apart")
+    raise ValueError(f"{what}: expected a CUDA tensor {(rows, cols)} of {dtype}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+
+
+def _mat8(t, rows: int, cols: int, dtype, what: str) -> tuple:
+    """_mat of a tensor that may be a Q8."""
+    if not isinstance(t, Q8):
+        return _mat(t, rows, cols, dtype, what)
+    import torch
+    d, ld, _, _ = _mat(t.codes, rows, cols, torch.int8, what)
+    s, lds, _, _ = _mat(t.scales, rows, (cols + 31) // 32, torch.uint8, what)
+    return (d, ld, s, lds)
 
 
 def _vec(t, n: int, what: str, dtype=None) -> int:
@@ -488,7 +486,7 @@ def emtk_dense(nn, x, w, y, bias=None, act: str = "none", residual=None, pre=Non
     args = _PACK_DENSE.pack(m, n, k, _act_code(act), _type_of(x, "x"),
                             0 if bias is None else _type_of(bias, "bias", True),
                             *_mat(x, m, k, dt, "x"), *_mat(w, n, k, dt, "w"), *_mat(y, m, n, dt, "y"),
-                            *_mat(residual, m, n, dt, "residual"), *_mat(pre, m, n, (dt, Q8), "pre"),
+                            *_mat(residual, m, n, dt, "residual"), *_mat8(pre, m, n, dt, "pre"),
                             _vec(bias, n, "bias"))
     _check(load_library().emtk_dense(nn, args, _current(x, stream)), "emtk_dense")
 
@@ -502,8 +500,8 @@ def emtk_dense_backward(nn, dy, x, w, act: str = "none", pre=None, dx=None, dw=N
     k = 0 if like is None else like.shape[1]
     args = _PACK_DENSE_GRAD.pack(m, n, k, _act_code(act), _type_of(dy, "dy"),
                                  0 if dw is None else _type_of(dw, "dw", True),
-                                 *_mat(dy, m, n, dt, "dy"), *_mat(x, m, k, (dt, Q8), "x"), *_mat(w, n, k, dt, "w"),
-                                 *_mat(pre, m, n, (dt, Q8), "pre"), *_mat(dx, m, k, dt, "dx"),
+                                 *_mat(dy, m, n, dt, "dy"), *_mat8(x, m, k, dt, "x"), *_mat(w, n, k, dt, "w"),
+                                 *_mat8(pre, m, n, dt, "pre"), *_mat(dx, m, k, dt, "dx"),
                                  *_mat(dw, n, k, None if dw is None else dw.dtype, "dw"),
                                  _vec(db, n, "db", torch.float32))
     _check(load_library().emtk_dense_backward(nn, args, _current(dy, stream)), "emtk_dense_backward")
@@ -520,8 +518,8 @@ def emtk_gated(nn, x, w_gate, w_up, h, bias_gate=None, bias_up=None, act: str = 
         raise ValueError("bias_up: its dtype must be bias_gate's")
     args = _PACK_GATED.pack(m, f, k, _act_code(act), _type_of(x, "x"), bias_type,
                             *_mat(x, m, k, dt, "x"), *_mat(w_gate, f, k, dt, "w_gate"), *_mat(w_up, f, k, dt, "w_up"),
-                            *_mat(h, m, f, dt, "h"), *_mat(gate, m, f, (dt, Q8), "gate"),
-                            *_mat(up, m, f, (dt, Q8), "up"), _vec(bias_gate, f, "bias_gate"),
+                            *_mat(h, m, f, dt, "h"), *_mat8(gate, m, f, dt, "gate"),
+                            *_mat8(up, m, f, dt, "up"), _vec(bias_gate, f, "bias_gate"),
                             _vec(bias_up, f, "bias_up"))
     _check(load_library().emtk_gated(nn, args, _current(x, stream)), "emtk_gated")
 
@@ -539,8 +537,8 @@ def emtk_gated_backward(nn, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx
     dwt = None if dw_gate is None else dw_gate.dtype
     args = _PACK_GATED_GRAD.pack(m, f, k, _act_code(act), _type_of(dh, "dh"),
                                  0 if dw_gate is None else _type_of(dw_gate, "dw_gate", True),
-                                 *_mat(dh, m, f, dt, "dh"), *_mat(gate, m, f, (dt, Q8), "gate"),
-                                 *_mat(up, m, f, (dt, Q8), "up"), *_mat(x, m, k, (dt, Q8), "x"),
+                                 *_mat(dh, m, f, dt, "dh"), *_mat8(gate, m, f, dt, "gate"),
+                                 *_mat8(up, m, f, dt, "up"), *_mat8(x, m, k, dt, "x"),
                                  *_mat(w_gate, f, k, dt, "w_gate"), *_mat(w_up, f, k, dt, "w_up"),
                                  *_mat(dx, m, k, dt, "dx"), *_mat(dw_gate, f, k, dwt, "dw_gate"),
                                  *_mat(dw_up, f, k, dwt, "dw_up"), *_mat(h, m, f, dt, "h"),
@@ -552,13 +550,13 @@ def emtk_pack8(nn, x, q: Q8, stream=None) -> None:
     """Keeps x [m][k] (bf16 or fp16) in the 8-bit checkpoint q."""
     (m, k), dt = x.shape, x.dtype
     _check(load_library().emtk_pack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")),
-                                     _PACK_MATRIX.pack(*_mat(q, m, k, (dt, Q8), "q")), _current(x, stream)), "emtk_pack8")
+                                     _PACK_MATRIX.pack(*_mat8(q, m, k, dt, "q")), _current(x, stream)), "emtk_pack8")
 
 
 def emtk_unpack8(nn, q: Q8, x, stream=None) -> None:
     """The values that the 8-bit checkpoint q stands for, into x [m][k] (bf16 or fp16)."""
     (m, k), dt = x.shape, x.dtype
-    _check(load_library().emtk_unpack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(q, m, k, (dt, Q8), "q")),
+    _check(load_library().emtk_unpack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat8(q, m, k, dt, "q")),
                                        _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")), _current(x, stream)), "emtk_unpack8")
 
 
