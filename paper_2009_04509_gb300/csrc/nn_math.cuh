@@ -47,10 +47,29 @@ __device__ __forceinline__ float reciprocal_f(float v) {
 // 1 / (1 + exp(-z)): 0 where exp(-z) overflows (z < -88), the limit.
 __device__ __forceinline__ float sigmoid_f(float z) { return reciprocal_f(1.f + exp_f(-z)); }
 
+// The normal distribution function and exp(-z^2 / 2), which is both the tail of the
+// one and the derivative's density: 1 - Phi(|z|) = e t (a1 + t (a2 + ..)) / 2 with
+// t = 1 / (1 + p |z| / sqrt 2), formula 7.1.26 of Abramowitz and Stegun (1964),
+// off by at most 7.5e-8, a fifth of an fp32 ulp at 1 and far below 16 bits.
+__device__ __forceinline__ void normal_f(float z, float &phi, float &e) {
+    const float t = reciprocal_f(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
+    e = exp_f(-0.5f * z * z);
+    float s = fmaf(t, 1.061405429f, -1.453152027f);
+    s = fmaf(t, s, 1.421413741f);
+    s = fmaf(t, s, -0.284496736f);
+    s = fmaf(t, s, 0.254829592f);
+    s = 0.5f * t * s * e;
+    phi = z < 0.f ? s : 1.f - s;
+}
+
 template <int ACT>
 __device__ __forceinline__ float act_of(float z) {
     if (ACT == EMTK_ACT_RELU) return z > 0.f ? z : (z == z ? 0.f : z);  // NaN stays
-    if (ACT == EMTK_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if (ACT == EMTK_ACT_GELU) {
+        float phi, e;
+        normal_f(z, phi, e);
+        return z * phi;
+    }
     if (ACT == EMTK_ACT_SILU) return z * sigmoid_f(z);
     if (ACT == EMTK_ACT_SIGMOID) return sigmoid_f(z);
     return z;
@@ -65,9 +84,10 @@ __device__ __forceinline__ void act_slope(float z, float &a, float &d) {
         a = act_of<ACT>(z);
         d = z > 0.f ? 1.f : (z == z ? 0.f : z);
     } else if (ACT == EMTK_ACT_GELU) {
-        const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
-        a = z * p;
-        d = p + z * exp_f(-0.5f * z * z) * 0.39894228040143268f;
+        float phi, e;
+        normal_f(z, phi, e);
+        a = z * phi;
+        d = fmaf(z * 0.39894228f, e, phi);
     } else if (ACT == EMTK_ACT_SILU) {
         const float p = sigmoid_f(z);
         a = z * p;
@@ -142,18 +162,33 @@ __device__ __forceinline__ uint32_t q8_codes4(const float *v, float inverse, boo
     }
     return w;
 }
+// Two sums or products at once.
+__device__ __forceinline__ void add_mul2(float &a, float &b, float add, float mul) {
+    uint64_t v, t;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(t) : "f"(add));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(t));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(t) : "f"(mul));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(t));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
 // Values of the four codes of a word.  A byte with its sign bit flipped is code +
 // 128; below the bits of 2^23 it is 2^23 + 128 + code, from which a subtraction and
-// a product by the power of two leave the value, both exact.
-__device__ __forceinline__ void q8_values4(uint32_t w, float step, float *v) {
+// a product by the power of two leave the value, both exact.  Returns not 0 if some
+// code is -128 (read as a number here).
+__device__ __forceinline__ uint32_t q8_values4_finite(uint32_t w, float step, float *v) {
     const uint32_t x = w ^ 0x80808080u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        v[i] = (__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440 + i)) - 8388736.f) * step;
-    if ((x - 0x01010101u) & ~x & 0x80808080u) {  // some byte of x is 0: code -128, rare
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440 + i));
+    add_mul2(v[0], v[1], -8388736.f, step);
+    add_mul2(v[2], v[3], -8388736.f, step);
+    return (x - 0x01010101u) & ~x & 0x80808080u;  // some byte of x is 0
+}
+__device__ __forceinline__ void q8_values4(uint32_t w, float step, float *v) {
+    if (q8_values4_finite(w, step, v)) {  // rare
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (((x >> (8 * i)) & 0xffu) == 0) v[i] = __int_as_float(0x7fffffff);
+            if (((w >> (8 * i)) & 0xffu) == 0x80u) v[i] = __int_as_float(0x7fffffff);
     }
 }
 // The value as an operand of the products: bf16 holds it exactly, fp16 saturates.

@@ -563,8 +563,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // Adds the parts' sums and applies the epilogue: 2^lanes_log2 neighbouring
-// threads (8 at most) take 8 columns of a row, each every so-manieth part, and
-// join their sums in a fixed tree; four such groups hold a checkpoint block.
+// threads take 8 columns of a row, each every so-manieth part, and join their
+// sums in a fixed tree; four such groups hold a checkpoint block (8 threads each
+// at most, then: the four share a warp).
 template <bool F16, Kind KIND, int TN>
 __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEpilogue e, const float *partial,
                                                     int64_t part_elems, int64_t part_ld, int parts, int M, int N,
@@ -663,8 +664,9 @@ cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
         const MmWork &w = p.job[i];
         if (w.parts == 1) continue;
         const int groups = (w.N + 31) / 32 * 4;
-        int lanes_log2 = 0;  // up to 8 threads a group, while the parts and the idle threads last
-        while (lanes_log2 < 3 && (2 << lanes_log2) <= w.parts && ((int64_t)w.M * groups << lanes_log2) < 2 * 2048 * plan.pairs)
+        int lanes_log2 = 0;  // while the parts and the idle threads last
+        const int most = w.epi.saved[0].d_scale ? 3 : 5;
+        while (lanes_log2 < most && (2 << lanes_log2) <= w.parts && ((int64_t)w.M * groups << lanes_log2) < 2 * 2048 * plan.pairs)
             ++lanes_log2;
         const int64_t threads = (int64_t)w.M * groups << lanes_log2;
         e = launch_pdl(parts_kernel<F16, KIND, TN>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, w.epi,

@@ -188,23 +188,27 @@ __device__ __forceinline__ void slope_of(float d, float g, float u, float &dg, f
     h = f * u;
 }
 
-// The block's sums of each column, from its threads'.
+// The block's sums of each column, from its threads': kThreads / cols threads take
+// a column, each 8 threads' sums, and the first adds theirs.
 template <bool GATED>
 __device__ __forceinline__ void block_sums(const SlopeArgs &a, const float (&sg)[kVec], const float (&su)[kVec]) {
     __shared__ float part[kThreads * kVec];
-    const int cols = kVec << a.lanes_log2, lanes = 1 << a.lanes_log2, at_once = kThreads >> a.lanes_log2;
-    const int64_t col = (int64_t)blockIdx.x * cols + threadIdx.x;
-    float *const row = part + (threadIdx.x >> a.lanes_log2) * cols;
-    const int tl = threadIdx.x & (lanes - 1);
+    const int cols = kVec << a.lanes_log2, share = threadIdx.x / cols, in = threadIdx.x % cols;
+    const int64_t col = (int64_t)blockIdx.x * cols + in;
 #pragma unroll
     for (int half = 0; half < (GATED ? 2 : 1); ++half) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) row[tl * kVec + i] = half ? su[i] : sg[i];
+        for (int i = 0; i < kVec; ++i) part[threadIdx.x * kVec + i] = half ? su[i] : sg[i];
         __syncthreads();
-        if ((int)threadIdx.x < cols && col < a.n) {
-            float sum = 0.f;
-            for (int g = 0; g < at_once; ++g) sum += part[g * cols + threadIdx.x];
+        float sum = 0.f;
+#pragma unroll
+        for (int g = 0; g < kVec; ++g) sum += part[(share * kVec + g) * cols + in];
+        __syncthreads();
+        part[threadIdx.x] = sum;
+        __syncthreads();
+        if (share == 0 && col < a.n) {
+            for (int g = 1; g < kThreads / cols; ++g) sum += part[g * cols + in];
             a.sums[half][(int64_t)blockIdx.y * a.n + col] = sum;
         }
     }

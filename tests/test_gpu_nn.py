@@ -421,6 +421,44 @@ def test_unpack8_saturates_in_fp16(lib, nn):
     assert torch.equal(back, x)  # 64 * 2^10 = 65536 is beyond fp16
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("m,k,n", [(1, 128, 72), (64, 64, 64), (65, 96, 40), (300, 256, 130), (130, 400, 600),
+                                   (1000, 2304, 128), (5000, 128, 300), (9000, 48, 24), (700, 1040, 1030)])
+def test_gradients_from_codes_are_those_from_their_values(lib, nn, dtype, m, k, n):
+    """x as an 8-bit checkpoint whose rows TMA can read, against x as the 16-bit matrix it stands for:
+    the same products of the same values in the same order, so the same bits (with every block's scale
+    different, and zero and NaN blocks)."""
+    g = gen(m + k)
+    t = DT[dtype]
+    x = torch.randn(m, k, generator=g, device="cuda") * torch.exp2(torch.randint(-6, 7, (m, 1), generator=g, device="cuda"))
+    x[m // 3] = 0
+    x = x.to(t)
+    q, values = q8_of(lib, m, k), torch.empty_like(x)
+    lib.emtk_pack8(nn, x, q)
+    lib.emtk_unpack8(nn, q, values)
+    dy, w = (torch.randn(*s, generator=g, device="cuda").to(t) for s in ((m, n), (n, k)))
+    a, b = torch.empty((n, k), dtype=t, device="cuda"), torch.zeros((n, k), dtype=t, device="cuda")
+    c, d = torch.empty_like(x), torch.empty_like(x)
+    lib.emtk_dense_backward(nn, dy, values, w, dx=c, dw=a)
+    lib.emtk_dense_backward(nn, dy, q, w, dx=d, dw=b)
+    assert torch.equal(a, b) and torch.equal(c, d)
+    b.zero_()
+    lib.emtk_dense_backward(nn, dy, values, None, dw=a)
+    lib.emtk_dense_backward(nn, dy, q, None, dw=b)
+    assert torch.equal(a, b)
+    gate, up = (torch.randn(m, n, generator=g, device="cuda").to(t) for _ in "gu")
+    outs = []
+    for xx in (values, q):
+        o = [torch.zeros((n, k), dtype=torch.float32, device="cuda") for _ in "gu"] + [torch.empty_like(x)]
+        lib.emtk_gated_backward(nn, dy, gate, up, xx, w, w, act="silu", dw_gate=o[0], dw_up=o[1], dx=o[2])
+        outs.append(o)
+    assert all(torch.equal(p, r) for p, r in zip(*outs))
+    x[0, 1] = float("nan")
+    lib.emtk_pack8(nn, x, q)
+    lib.emtk_dense_backward(nn, dy, q, None, dw=b)
+    assert torch.isnan(b[:, 1]).all() and torch.equal(torch.isnan(b).any(0).nonzero().flatten().cpu(), torch.tensor([1]))
+
+
 # ------------------------------------------------------------------ odd ends
 @pytest.mark.parametrize("m,k,n", [(0, 8, 8), (4, 0, 40), (4, 8, 0), (0, 0, 0), (300, 0, 300)])
 def test_empty_sizes(lib, nn, m, k, n):
