@@ -376,11 +376,9 @@ cudaError_t run_slope(emtk_type type, int act, SlopeArgs &a, float *partial, flo
 }
 
 // -------------------------------------------------------- checkpoints
-// A warp's items are (row, piece of 256 columns), every warps-th one; the step
-// from one to the next is added to row and piece, without a division.  Four
-// items' loads are in flight.
-constexpr int kFlight = 4;
-
+// Work is dealt out in pieces of a row, every so-manieth one to a thread (aligned
+// rows) or to a warp (256 columns, any); the step from one to the next is added to
+// row and piece, without a division.
 struct Walk {
     int per_row;
     int64_t step_rows;
@@ -401,6 +399,9 @@ struct Item {
     }
 };
 
+constexpr int kPackCols = 16;  // of a thread: two hold a checkpoint block
+constexpr int kBlocks = 5;  // an SM, resident at once
+
 struct PackArgs {
     Source x;
     uint8_t *q, *scale;
@@ -409,37 +410,59 @@ struct PackArgs {
     Walk walk;
 };
 
+// The largest magnitude is found among the 16-bit patterns, whose order is the
+// values' with the sign off, two at a time; one at or above infinity's pattern
+// sends the block to the arithmetic of finite_top.
 template <bool F16>
-__global__ void __launch_bounds__(kThreads) pack8_kernel(const __grid_constant__ PackArgs a) {
-    const int lane = threadIdx.x & 31;
-    Item it(a.walk, (int64_t)blockIdx.x * kWarps + threadIdx.x / 32);
+__global__ void __launch_bounds__(kThreads, kBlocks) pack8_kernel(const __grid_constant__ PackArgs a) {
+    constexpr uint32_t kInfinity = F16 ? 0x7c00u : 0x7f80u;
+    constexpr int kFlight = 2;
+    Item it(a.walk, (int64_t)blockIdx.x * kThreads + threadIdx.x);
     pdl_trigger();
     pdl_wait();
-    while (it.r < a.m) {
-        Piece<false> w[kFlight];
+    while (__any_sync(0xffffffffu, it.r < a.m)) {
+        Piece<false> w[kFlight][2];
         int64_t r[kFlight];
         int c[kFlight];
+        bool in[kFlight];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i, it.next(a.walk)) {
             r[i] = it.r;
-            c[i] = it.piece * kWarpCols + lane * kVec;
-            w[i].w = make_uint4(0u, 0u, 0u, 0u);
-            if (r[i] < a.m && c[i] < a.k) w[i].load(a.x.p + r[i] * a.x.row_bytes + 2 * (int64_t)c[i], nullptr);
+            c[i] = it.piece * kPackCols;
+            in[i] = r[i] < a.m && c[i] < a.k;
+            w[i][0].w = w[i][1].w = make_uint4(0u, 0u, 0u, 0u);
+            if (in[i]) {
+                const uint8_t *p = a.x.p + r[i] * a.x.row_bytes + 2 * (int64_t)c[i];
+                w[i][0].load(p, nullptr);
+                w[i][1].load(p + 16, nullptr);
+            }
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            float v[kVec];
-            w[i].template values<F16>(v);
-            bool all_finite;
-            float top = finite_top(v, all_finite);
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            if (r[i] >= a.m || c[i] >= a.k) continue;
+            uint32_t m = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                for (const uint32_t x : {w[i][h].w.x, w[i][h].w.y, w[i][h].w.z, w[i][h].w.w})
+                    m = __vmaxu2(m, x & 0x7fff7fffu);
+            m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            m = max(m & 0xffffu, m >> 16);
+            float v[kPackCols];
+            w[i][0].template values<F16>(v);
+            w[i][1].template values<F16>(v + 8);
+            float top = from16<F16>(m);
+            const bool all_finite = m < kInfinity;  // of both threads
+            if (!all_finite) {
+                bool mine;
+                top = finite_top(v, mine);
+                top = fmaxf(top, __shfl_xor_sync(3u << (threadIdx.x & 30), top, 1));
+            }
+            if (!in[i]) continue;
             const uint32_t b = q8_scale(top);
             const float inverse = q8_inverse(b);
-            if ((lane & 3) == 0) a.scale[r[i] * a.ld_scale + c[i] / kQ8Block] = (uint8_t)b;
-            *reinterpret_cast<uint2 *>(a.q + r[i] * a.q_ld + c[i]) =
-                make_uint2(q8_codes4(v, inverse, all_finite), q8_codes4(v + 4, inverse, all_finite));
+            if (c[i] % kQ8Block == 0) a.scale[r[i] * a.ld_scale + c[i] / kQ8Block] = (uint8_t)b;
+            *reinterpret_cast<uint4 *>(a.q + r[i] * a.q_ld + c[i]) =
+                make_uint4(q8_codes4(v, inverse, all_finite), q8_codes4(v + 4, inverse, all_finite),
+                           q8_codes4(v + 8, inverse, all_finite), q8_codes4(v + 12, inverse, all_finite));
         }
     }
 }
@@ -478,27 +501,31 @@ struct CopyArgs {
     } job[kMaxCopies];
 };
 
-template <bool F16, bool Q8>
-__device__ __forceinline__ void copy_wide(const CopyArgs::One &j, Item it, int lane) {
+// A checkpoint's values, rows of codes on 8 bytes and of values on 16: 8 columns a
+// thread, so that neighbours' stores meet in whole sectors (16 columns a thread in
+// two stores took 35 us where this takes XX; 20000 x 2304).
+template <bool F16>
+__device__ __forceinline__ void unpack_wide(const CopyArgs::One &j, Item it) {
+    constexpr int kFlight = 4;
     while (it.r < j.rows) {
-        Piece<Q8> w[kFlight];
+        Piece<true> w[kFlight];
         int64_t r[kFlight];
         int c[kFlight];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i, it.next(j.walk)) {
             r[i] = it.r;
-            c[i] = it.piece * kWarpCols + lane * kVec;
-            if (r[i] < j.rows && c[i] < j.cols)
-                w[i].load(j.from.p + r[i] * j.from.row_bytes + (Q8 ? 1 : 2) * (int64_t)c[i],
+            c[i] = it.piece * kVec;
+            if (r[i] < j.rows)
+                w[i].load(j.from.p + r[i] * j.from.row_bytes + c[i],
                           j.from.scale + r[i] * j.from.ld_scale + c[i] / kQ8Block);
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            if (r[i] >= j.rows || c[i] >= j.cols) continue;
+            if (r[i] >= j.rows) continue;
             float v[kVec];
             w[i].template values<F16>(v);
 #pragma unroll
-            for (int t = 0; t < kVec; ++t) v[t] = Q8 ? q8_operand<F16>(v[t]) : v[t];
+            for (int t = 0; t < kVec; ++t) v[t] = q8_operand<F16>(v[t]);
             *reinterpret_cast<uint4 *>(j.to + r[i] * j.to_ld + c[i]) = pack8x16<F16>(v);
         }
     }
@@ -526,28 +553,37 @@ __device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it, int la
 }
 
 template <bool F16>
-__global__ void __launch_bounds__(kThreads) copy16_kernel(const __grid_constant__ CopyArgs a) {
+__global__ void __launch_bounds__(kThreads, kBlocks) copy16_kernel(const __grid_constant__ CopyArgs a) {
     const CopyArgs::One &j = a.job[blockIdx.z];
     const int lane = threadIdx.x & 31;
-    Item it(j.walk, (int64_t)blockIdx.x * kWarps + threadIdx.x / 32);
+    const int64_t thread = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    Item it(j.walk, j.wide ? thread : thread / 32);
     pdl_trigger();
     pdl_wait();
-    if (j.wide) return j.from.scale ? copy_wide<F16, true>(j, it, lane) : copy_wide<F16, false>(j, it, lane);
+    if (j.wide) return unpack_wide<F16>(j, it);
     if (j.from.scale)
         copy_any<F16, true>(j, it, lane);
     else
         copy_any<F16, false>(j, it, lane);
 }
 
-// Blocks of a walk: six an SM at most, all resident at once.
-unsigned walk_blocks(int64_t rows, int64_t cols, int sms) {
-    const int64_t items = rows * ((cols + kWarpCols - 1) / kWarpCols);
-    return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + kWarps - 1) / kWarps, (int64_t)6 * sms));
-}
-Walk walk_of(int64_t cols, unsigned blocks) {
-    const int per_row = (int)((cols + kWarpCols - 1) / kWarpCols);
-    const int64_t warps = (int64_t)blocks * kWarps;
-    return {per_row, warps / per_row, (int)(warps % per_row)};
+// A walk of pieces of `cols` columns over rows of k, by threads or by warps, in
+// blocks that are all resident at once.
+struct WalkPlan {
+    int per_row, workers;  // of a block
+    int64_t items;
+    unsigned blocks(int sms) const {
+        return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + workers - 1) / workers, (int64_t)kBlocks * sms));
+    }
+    Walk walk(unsigned blocks) const {
+        const int64_t all = (int64_t)blocks * workers;
+        return {per_row, all / per_row, (int)(all % per_row)};
+    }
+};
+WalkPlan walk_plan(int64_t rows, int64_t k, int cols, int workers, bool even) {
+    int64_t per_row = (k + cols - 1) / cols;
+    if (even) per_row = (per_row + 1) / 2 * 2;
+    return {(int)per_row, workers, rows * per_row};
 }
 
 }  // namespace
@@ -586,9 +622,12 @@ cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk
 cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
                          cudaStream_t s) {
     if (m == 0 || k == 0) return cudaSuccess;
-    const unsigned blocks = walk_blocks(m, k, sms);
-    const PackArgs a{source_of(x), static_cast<uint8_t *>(q.d), q.d_scale, q.ld, q.ld_scale, m, k, walk_of(k, blocks)};
-    const bool wide = wide_source(a.x, k) && wide_matrix(q.d, q.ld, kVec), f16 = type == EMTK_TYPE_F16;
+    const bool wide = k % kPackCols == 0 && wide_matrix(x.d, 2 * x.ld, 16) && wide_matrix(q.d, q.ld, 16);
+    const bool f16 = type == EMTK_TYPE_F16;
+    // wide: an even number of pieces a row, so that a block's two threads are neighbours
+    const WalkPlan plan = wide ? walk_plan(m, k, kPackCols, kThreads, true) : walk_plan(m, k, kWarpCols, kWarps, false);
+    const unsigned blocks = plan.blocks(sms);
+    const PackArgs a{source_of(x), static_cast<uint8_t *>(q.d), q.d_scale, q.ld, q.ld_scale, m, k, plan.walk(blocks)};
     return launch_pdl(wide ? (f16 ? pack8_kernel<true> : pack8_kernel<false>)
                            : (f16 ? pack8_any_kernel<true> : pack8_any_kernel<false>),
                       dim3(blocks), dim3(kThreads), 0, s, a);
@@ -596,18 +635,21 @@ cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, con
 
 cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, cudaStream_t s) {
     CopyArgs a{};
+    WalkPlan plans[kMaxCopies];
     unsigned jobs = 0, blocks = 0;
-    for (int i = 0; i < n; ++i)
-        if (copies[i].cols > 0) blocks = std::max(blocks, walk_blocks(copies[i].rows, copies[i].cols, sms));
     for (int i = 0; i < n; ++i) {
         const Copy16 &c = copies[i];
         if (c.rows == 0 || c.cols == 0) continue;
         const Source from = source_of(c.from);
         const bool to_wide = wide_matrix(c.to.d, 2 * c.to.ld, 16);
-        a.job[jobs++] = {from, static_cast<uint16_t *>(c.to.d), c.to.ld, c.rows, c.cols,
-                         to_wide && wide_source(from, c.cols), to_wide, walk_of(c.cols, blocks)};
+        const bool wide = from.scale && to_wide && wide_source(from, c.cols);
+        plans[jobs] = wide ? walk_plan(c.rows, c.cols, kVec, kThreads, false)
+                           : walk_plan(c.rows, c.cols, kWarpCols, kWarps, false);
+        blocks = std::max(blocks, plans[jobs].blocks(sms));
+        a.job[jobs++] = {from, static_cast<uint16_t *>(c.to.d), c.to.ld, c.rows, c.cols, wide, to_wide, Walk{}};
     }
     if (jobs == 0) return cudaSuccess;
+    for (unsigned i = 0; i < jobs; ++i) a.job[i].walk = plans[i].walk(blocks);
     return launch_pdl(type == EMTK_TYPE_F16 ? copy16_kernel<true> : copy16_kernel<false>, dim3(blocks, 1, jobs),
                       dim3(kThreads), 0, s, a);
 }
