@@ -35,17 +35,45 @@ constexpr int kABytes = 128 * kStep * 2;  // a CTA's rows of a stage
 constexpr int kEpiWarps = 8;
 constexpr int kFirstEpiWarp = 4;
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
-constexpr int kStageRowsBytes = 32 * 64;  // an epilogue warp's staged block: 32 rows of 64 bytes
-constexpr int kBiasBytes = 128 * 4;      // an epilogue warp's columns
 
-template <int TN>
+// Which epilogue a kernel has: gradients' (nothing but the sums), a dense layer's, a
+// gated block's.  An epilogue warp turns blocks of 32 rows by kBlock columns into
+// output through kStageRow-byte rows of shared memory; the gradients' blocks are
+// twice as wide, which halves the latencies that their stores wait out.
+enum Kind : int { kPlain, kDense, kGated };
+template <Kind KIND>
+struct Epi {
+    static constexpr int kBlock = KIND == kPlain ? 64 : 32;
+    static constexpr int kStageRow = KIND == kPlain ? 128 : 64;
+    static constexpr int kBiasBytes = KIND == kPlain ? 0 : 128 * 4;  // of the warp's columns
+    static constexpr int kWarpBytes = 32 * kStageRow + kBiasBytes;
+};
+
+template <int TN, Kind KIND>
 struct Shape {
     static constexpr int kBBytes = TN / 2 * kStep * 2;
     static constexpr int kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = TN == 256 ? 6 : 8;
     static constexpr int kTmemCols = 2 * TN;
     // barriers first, then the stages on 1024 bytes
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpiWarps * (kStageRowsBytes + kBiasBytes) + 512;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpiWarps * Epi<KIND>::kWarpBytes + 512;
+};
+static_assert(Shape<256, kPlain>::kSmem <= 227 * 1024 && Shape<128, kPlain>::kSmem <= 227 * 1024 &&
+              Shape<256, kGated>::kSmem <= 227 * 1024 && Shape<128, kGated>::kSmem <= 227 * 1024, "shared memory of an SM");
+
+// Division by a fixed d > 0 of 0 <= n < 2^31, as a product: floor(n m / 2^(31 + s)) with
+// 2^(s - 1) < d <= 2^s and m = ceil(2^(31 + s) / d) < 2^32 is exact there.  The integer
+// unit's own division would keep each tile's first MMA waiting.
+struct Divisor {
+    uint32_t mul, shift;
+    Divisor() = default;
+    explicit Divisor(uint32_t d) {
+        uint32_t s = 0;
+        while ((1u << s) < d) ++s;
+        mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
+        shift = 31 + s;
+    }
+    __device__ __forceinline__ int of(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
 };
 
 struct MmWork {  // one job
@@ -59,6 +87,7 @@ struct MmWork {  // one job
     int chunks, total;     // of one term, of all
     int chunks_per_part;
     int unit_end;          // units of this job and those before it
+    Divisor by_parts, by_group, by_last;  // parts; tiles of 8 tile rows; tile rows of the last group
 };
 struct MmParams {
     MmWork job[kMaxJobs];
@@ -82,13 +111,14 @@ __device__ __forceinline__ Unit unit_of(const MmParams &p, int u, int cols) {
     while (u >= p.job[r.job].unit_end) begin = p.job[r.job++].unit_end;
     const MmWork &w = p.job[r.job];
     u -= begin;
-    const int t = u / w.parts;
+    const int t = w.by_parts.of(u);
     r.part = u - t * w.parts;
-    const int group = t / (8 * w.tiles_n);
-    const int rows = min(8, w.tiles_m - 8 * group);
+    const int group = w.by_group.of(t);
     const int in = t - group * 8 * w.tiles_n;
-    r.m0 = (8 * group + in % rows) * kTileM;
-    r.n0 = in / rows * cols;
+    const int rows = min(8, w.tiles_m - 8 * group);
+    const int column = rows == 8 ? in >> 3 : w.by_last.of(in);
+    r.m0 = (8 * group + in - column * rows) * kTileM;
+    r.n0 = column * cols;
     r.c0 = r.part * w.chunks_per_part;
     r.c1 = min(r.c0 + w.chunks_per_part, w.total);
     return r;
@@ -98,36 +128,40 @@ __device__ __forceinline__ bool wide_rows(const void *p, int64_t ld, int elem) {
     return ((reinterpret_cast<uintptr_t>(p) | (uint64_t)(ld * elem)) & 15u) == 0;
 }
 
-// 16-byte piece c of staged row r: the pieces are permuted so that neither a
-// lane to a row nor four lanes to a row meet in a bank.
-__device__ __forceinline__ uint32_t staged(int r, int c) { return (uint32_t)(r * 64 + ((c ^ (r >> 1)) & 3) * 16); }
+// 16-byte piece c of staged row r: the pieces are permuted so that neither a lane to
+// a row nor the lanes of a row meet in a bank.
+template <int ROW>
+__device__ __forceinline__ uint32_t staged(int r, int c) {
+    return (uint32_t)(r * ROW + (ROW == 128 ? (c ^ r) & 7 : (c ^ (r >> 1)) & 3) * 16);
+}
 
-// Rows r0 .. r0 + 31 (below `rows`), columns c0 .. c0 + 64 / sizeof(T) - 1 (below
-// `cols`) of a matrix, between memory and the warp's staged rows; four lanes move
-// a row where 16-byte pieces fit, a row at a time where they do not.
-template <typename T, bool LOAD>
+// Rows r0 .. r0 + 31 (below `rows`), columns c0 .. c0 + ROW / sizeof(T) - 1 (below
+// `cols`) of a matrix, between memory and the warp's staged rows; ROW / 16 lanes
+// move a row where 16-byte pieces fit, a row at a time where they do not.
+template <typename T, bool LOAD, int ROW>
 __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int64_t rows, int64_t c0, int64_t cols,
                                            bool wide, uint8_t *stage, int lane) {
-    constexpr int kPiece = 16 / sizeof(T), kCols = 64 / sizeof(T);
+    constexpr int kPiece = 16 / sizeof(T), kCols = ROW / sizeof(T), kLanes = ROW / 16, kRows = 32 / kLanes;
     const int nr = (int)min((int64_t)32, rows - r0), nc = (int)min((int64_t)kCols, cols - c0);
-    if (wide && nr == 32 && nc == kCols) {  // a whole block: four unconditional 16-byte moves a lane
-        T *g = base + (r0 + (lane >> 2)) * ld + c0 + (lane & 3) * kPiece;
-        uint8_t *s = stage + staged(lane >> 2, lane & 3);  // 8 rows on, the same permutation
+    const int r_first = lane / kLanes, piece = lane % kLanes;
+    if (wide && nr == 32 && nc == kCols) {  // a whole block: unconditional 16-byte moves
+        T *g = base + (r0 + r_first) * ld + c0 + piece * kPiece;
 #pragma unroll
-        for (int it = 0; it < 4; ++it, g += 8 * ld, s += 8 * 64) {
+        for (int it = 0; it < kLanes; ++it, g += kRows * ld) {
+            uint8_t *s = stage + staged<ROW>(r_first + it * kRows, piece);
             if (LOAD)
                 *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
             else
                 *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(s);
         }
     } else if (wide) {
-        const int c = (lane & 3) * kPiece;
+        const int c = piece * kPiece;
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const int r = it * 8 + (lane >> 2);
+        for (int it = 0; it < kLanes; ++it) {
+            const int r = it * kRows + r_first;
             if (r >= nr || c >= nc) continue;
             T *g = base + (r0 + r) * ld + c0 + c;
-            uint8_t *s = stage + staged(r, lane & 3);
+            uint8_t *s = stage + staged<ROW>(r, piece);
             if (c + kPiece <= nc) {
                 if (LOAD)
                     *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
@@ -142,23 +176,26 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
                 }
             }
         }
-    } else if (lane < nc) {
-        T *g = base + r0 * ld + c0 + lane;
-        const int piece = lane * (int)sizeof(T) / 16, in_piece = lane * (int)sizeof(T) % 16;
-        for (int r = 0; r < nr; r += 8, g += 8 * ld) {  // eight rows' elements in flight
-            T x[8];
+    } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (r + i < nr)
-                    x[i] = LOAD ? g[i * ld] : *reinterpret_cast<const T *>(stage + staged(r + i, piece) + in_piece);
+        for (int c = lane; c < kCols; c += 32) {
+            if (c >= nc) continue;
+            T *g = base + r0 * ld + c0 + c;
+            const int at = c * (int)sizeof(T) / 16, in = c * (int)sizeof(T) % 16;
+            for (int r = 0; r < nr; r += 8, g += 8 * ld) {  // eight rows' elements in flight
+                T x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (r + i < nr) {
-                    if (LOAD)
-                        *reinterpret_cast<T *>(stage + staged(r + i, piece) + in_piece) = x[i];
-                    else
-                        g[i * ld] = x[i];
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (r + i < nr) x[i] = LOAD ? g[i * ld] : *reinterpret_cast<const T *>(stage + staged<ROW>(r + i, at) + in);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (r + i < nr) {
+                        if (LOAD)
+                            *reinterpret_cast<T *>(stage + staged<ROW>(r + i, at) + in) = x[i];
+                        else
+                            g[i * ld] = x[i];
+                    }
+            }
         }
     }
 }
@@ -187,31 +224,34 @@ struct Rows {
     }
 };
 
-template <bool F16>
+// A lane's N columns (of its row) in 16 bits.
+template <bool F16, int N>
 __device__ __forceinline__ void store16(void *base, int64_t ld, bool wide, const Rows &w, int64_t c0, int64_t cols,
-                                        const float (&v)[32]) {
+                                        const float (&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<uint4 *>(w.stage + staged(w.lane, i)) =
+    for (int i = 0; i < N / 8; ++i)
+        *reinterpret_cast<uint4 *>(w.stage + staged<2 * N>(w.lane, i)) =
             make_uint4(pack16<F16>(v[8 * i], v[8 * i + 1]), pack16<F16>(v[8 * i + 2], v[8 * i + 3]),
                        pack16<F16>(v[8 * i + 4], v[8 * i + 5]), pack16<F16>(v[8 * i + 6], v[8 * i + 7]));
     __syncwarp();
-    move_block<uint16_t, false>(static_cast<uint16_t *>(base), ld, w.r0, w.rows, c0, cols, wide, w.stage, w.lane);
+    move_block<uint16_t, false, 2 * N>(static_cast<uint16_t *>(base), ld, w.r0, w.rows, c0, cols, wide, w.stage, w.lane);
     __syncwarp();
 }
 
+// A lane's N columns as they are, N / 2 at a time.
+template <int N>
 __device__ __forceinline__ void store32(float *base, int64_t ld, bool wide, const Rows &w, int64_t c0, int64_t cols,
-                                        const float (&v)[32]) {
+                                        const float (&v)[N]) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = 16 * half + 4 * i;
-            *reinterpret_cast<float4 *>(w.stage + staged(w.lane, i)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        for (int i = 0; i < N / 8; ++i) {
+            const int j = N / 2 * half + 4 * i;
+            *reinterpret_cast<float4 *>(w.stage + staged<2 * N>(w.lane, i)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
         }
         __syncwarp();
-        if (c0 + 16 * half < cols)
-            move_block<float, false>(base, ld, w.r0, w.rows, c0 + 16 * half, cols, wide, w.stage, w.lane);
+        if (c0 + N / 2 * half < cols)
+            move_block<float, false, 2 * N>(base, ld, w.r0, w.rows, c0 + N / 2 * half, cols, wide, w.stage, w.lane);
         __syncwarp();
     }
 }
@@ -272,9 +312,9 @@ __device__ __forceinline__ void add_bias(const float *bias, float (&v)[32]) {
 
 // Gradients: nothing but the sums.  A variant of its own because the other
 // epilogues' code, unrolled over 32 columns and jumped over, cost as much as the
-// stores (20000 x 512 -> 2304, bf16: XX us against 62).
-template <bool F16>
-__device__ __forceinline__ void finish_plain(const Rows &w, int64_t c0, int64_t cols, const float (&v)[32]) {
+// stores (20000 x 512 -> 2304, bf16: 41 us against 60 when it was split off).
+template <bool F16, int N>
+__device__ __forceinline__ void finish_plain(const Rows &w, int64_t c0, int64_t cols, const float (&v)[N]) {
     if (w.out_f32)
         store32(static_cast<float *>(w.out), w.out_ld, w.out_wide, w, c0, cols, v);
     else
@@ -289,12 +329,12 @@ __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w,
     if (w.has_saved) store_saved<F16>(e.saved[0], w, c0, cols, v);
     apply_act(w.act, v);
     if (w.residual) {
-        move_block<uint16_t, true>(static_cast<uint16_t *>(w.residual), w.residual_ld, w.r0, w.rows, c0, cols,
+        move_block<uint16_t, true, 64>(static_cast<uint16_t *>(w.residual), w.residual_ld, w.r0, w.rows, c0, cols,
                                    w.residual_wide, w.stage, w.lane);
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(w.stage + staged(w.lane, i));
+            const uint4 q = *reinterpret_cast<const uint4 *>(w.stage + staged<64>(w.lane, i));
             const uint32_t x[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -328,14 +368,13 @@ __device__ __forceinline__ void finish_gated(const MmEpilogue &e, const Rows &w,
     store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, g);
 }
 
-enum Kind : int { kPlain, kDense, kGated };
-
 enum Bar : int { kBarFull = 0, kBarEmpty = 8, kBarAccFull = 16, kBarAccEmpty = 18, kBarDrain = 20, kBarStall = 21, kBars = 22 };
 
 template <bool F16, Kind KIND, int TN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     mm_kernel(const __grid_constant__ MmParams p) {
-    using S = Shape<TN>;
+    using S = Shape<TN, KIND>;
+    using E = Epi<KIND>;
     constexpr bool GATED = KIND == kGated;
     constexpr int kCols = GATED ? TN / 2 : TN;  // output columns of a tile
     extern __shared__ uint8_t smem_raw[];
@@ -343,9 +382,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     uint8_t *const base = smem_raw + ((1024u - (raw & 1023u)) & 1023u);
     const uint32_t stages = smem_u32(base);
     uint8_t *const tail = base + S::kStages * S::kStageBytes;
-    uint8_t *const epi_rows = tail;
-    float *const epi_bias = reinterpret_cast<float *>(tail + kEpiWarps * kStageRowsBytes);
-    uint64_t *const bars = reinterpret_cast<uint64_t *>(tail + kEpiWarps * (kStageRowsBytes + kBiasBytes));
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(tail + kEpiWarps * E::kWarpBytes);
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(bars + kBars);
     volatile uint32_t *const abort_flag = tmem_slot + 1;
     auto bar = [&](int i) { return smem_u32(bars + i); };
@@ -490,9 +527,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int e = warp - kFirstEpiWarp;
         const int q = e & 3, half = e >> 2;
         constexpr int kMine = kCols / 2;  // output columns of a warp
-        float *const bias = epi_bias + e * (kBiasBytes / 4);
+        float *const bias = reinterpret_cast<float *>(tail + e * E::kWarpBytes + 32 * E::kStageRow);
         Rows w{};
-        w.stage = epi_rows + e * kStageRowsBytes;
+        w.stage = tail + e * E::kWarpBytes;
         w.lane = lane;
         int tile = 0, taken = -1;
         for (int u = pair; u < units; u += pairs, ++tile) {
@@ -520,21 +557,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const uint32_t acc = tmem + (uint32_t)(ab * TN) + ((uint32_t)(32 * q) << 16);
             const bool rows_in = w.r0 < w.rows;
 #pragma unroll 1
-            for (int j = 0; j < kMine; j += 32) {
+            for (int j = 0; j < kMine; j += E::kBlock) {
                 const int64_t c0 = n0 + j;
-                float v[32], x[GATED ? 32 : 1];
+                float v[E::kBlock], x[GATED ? 32 : 1];
                 const bool in = rows_in && c0 < N;
                 if (in && t.c0 < t.c1) {
-                    tmem_ld32(acc + (uint32_t)(half * kMine + j), v);
-                    if constexpr (GATED) tmem_ld32(acc + (uint32_t)(TN / 2 + half * kMine + j), x);
+                    tmem_ld(acc + (uint32_t)(half * kMine + j), v);
+                    if constexpr (GATED) tmem_ld(acc + (uint32_t)(TN / 2 + half * kMine + j), x);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
+                    for (int i = 0; i < E::kBlock; ++i) {
                         v[i] = 0.f;
                         if constexpr (GATED) x[i] = 0.f;
                     }
                 }
-                if (j + 32 == kMine) {  // this warp has read all of its sums
+                if (j + E::kBlock == kMine) {  // this warp has read all of its sums
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(cluster_addr(bar(kBarAccEmpty + ab), 0));
@@ -659,7 +696,7 @@ typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, 
 
 template <bool F16, Kind KIND, int TN>
 cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
-    cudaError_t e = launch_pdl(mm_kernel<F16, KIND, TN>, dim3(2 * plan.pairs), dim3(kThreads), Shape<TN>::kSmem, s, p);
+    cudaError_t e = launch_pdl(mm_kernel<F16, KIND, TN>, dim3(2 * plan.pairs), dim3(kThreads), Shape<TN, KIND>::kSmem, s, p);
     for (int i = 0; i < p.jobs && e == cudaSuccess; ++i) {
         const MmWork &w = p.job[i];
         if (w.parts == 1) continue;
@@ -783,7 +820,7 @@ cudaError_t init_mm_kernels() {
 #define EMTK_MM_ATTR(F16, KIND, TN)                                                                       \
     if (e == cudaSuccess)                                                                                 \
         e = cudaFuncSetAttribute(mm_kernel<F16, KIND, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, \
-                                 Shape<TN>::kSmem);
+                                 Shape<TN, KIND>::kSmem);
 #define EMTK_MM_ATTRS(KIND)        \
     EMTK_MM_ATTR(false, KIND, 256) \
     EMTK_MM_ATTR(true, KIND, 256)  \
@@ -840,6 +877,9 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
         w.total = c.chunks * j.terms;
         w.chunks_per_part = c.chunks_per_part;
         w.unit_end = end += c.units;
+        w.by_parts = Divisor((uint32_t)c.parts);
+        w.by_group = Divisor((uint32_t)(8 * c.tiles_n));
+        w.by_last = Divisor((uint32_t)std::max(1, c.tiles_m % 8));
     }
     p.jobs = n;
     p.status = nn->status;

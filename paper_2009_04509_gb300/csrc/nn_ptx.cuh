@@ -91,15 +91,20 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
         : "memory");
 }
 
-// 32 columns of this warp's 32 lanes.
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
-    uint32_t r[32];
+// N columns (a multiple of 16) of this warp's 32 lanes.
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, float (&v)[N]) {
+    uint32_t r[N];
     tmem_ld16<0>(taddr, r);
-    tmem_ld16<16>(taddr + 16, r);
+    if constexpr (N >= 32) tmem_ld16<16>(taddr + 16, r);
+    if constexpr (N >= 64) {
+        tmem_ld16<32>(taddr + 32, r);
+        tmem_ld16<48>(taddr + 48, r);
+    }
     tmem_ld_wait();
     reg_fence(r);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < N; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 // Shared-memory descriptor, MN-major, 128-byte swizzle: 64 elements of the
