@@ -590,6 +590,23 @@ def test_calls_in_a_graph(lib):
     lib.emtk_nn_destroy(h)
 
 
+@pytest.mark.parametrize("m,n", [(300, 200), (20, 200)])
+def test_a_wait_that_runs_out_is_reported(lib, m, n):
+    """A handle whose kernels wait for a barrier nothing arrives at: the wait ends at its limit, the
+    check says so once, and the device goes on working."""
+    h = lib.emtk_nn_create(wait_timeout_ns=50_000_000, debug_stall=True)
+    t = torch.bfloat16
+    x, w, y = (torch.ones(s, dtype=t, device="cuda") for s in ((m, 256), (n, 256), (m, n)))
+    lib.emtk_dense(h, x, w, y)
+    assert lib.emtk_nn_check(h) == lib.EMTK_ERR_TIMEOUT
+    assert lib.emtk_nn_check(h) == lib.EMTK_OK
+    lib.emtk_nn_destroy(h)
+    h = lib.emtk_nn_create()
+    lib.emtk_dense(h, x, w, y)
+    assert lib.emtk_nn_check(h) == lib.EMTK_OK and bool((y == 256).all())
+    lib.emtk_nn_destroy(h)
+
+
 # ------------------------------------------------------------------ refusals
 def test_binding_refuses(lib, nn):
     t = torch.bfloat16
