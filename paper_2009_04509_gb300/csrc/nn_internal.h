@@ -64,15 +64,18 @@ bool mm_operand_ok(const void *p, int64_t ld, int64_t rows);
 // of 128 bytes along memory by box_rows (or 64, where i runs along memory).
 bool encode_operand(const emtk_nn *nn, CUtensorMap *map, const MmOperand &o, int rows, int K, int box_rows);
 // Up to kMaxJobs jobs of one kind and type in one launch (nn_mm.cu); the plan
-// says how they are cut, and how much workspace `partial` it needs.
-constexpr int kMaxJobs = 3;
+// says how they are cut, and how much workspace `partial` it needs.  A piece is a
+// run of a job's tiles whose contraction is cut into equally many parts.
+constexpr int kMaxJobs = 3, kMaxPieces = 2 * kMaxJobs;
 struct MmPlan {
-    int tn, pairs, units;
-    int order[kMaxJobs];  // of the launch's jobs
-    struct Cut {
-        int tiles_m, tiles_n, chunks, parts, chunks_per_part, units;
-        int64_t part_ld, part_elems, part_at;
-    } cut[kMaxJobs];
+    int tn, pairs, units, pieces;
+    struct Job {
+        int tiles_m, tiles_n, chunks, total;
+    } job[kMaxJobs];
+    struct Piece {
+        int job, tile0, tiles, parts, chunks_per_part, units;
+        int64_t part_at;
+    } piece[kMaxPieces];
     size_t workspace;
 };
 MmPlan plan_mm(const MmJob *jobs, int n, int sms);

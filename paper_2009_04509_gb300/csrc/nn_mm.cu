@@ -76,49 +76,57 @@ struct Divisor {
     __device__ __forceinline__ int of(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
 };
 
-struct MmWork {  // one job
+// Where a job's tiles lie: in groups of 8 tile rows, along the rows first, so that
+// the pairs at work share operand panels in L2.
+struct Raster {
+    int tiles_m, tiles_n;
+    Divisor by_group, by_last;  // tiles of 8 tile rows; tile rows of the last group
+    __device__ __forceinline__ void tile(int t, int cols, int &m0, int &n0) const {
+        const int group = by_group.of(t);
+        const int in = t - group * 8 * tiles_n;
+        const int rows = min(8, tiles_m - 8 * group);
+        const int column = rows == 8 ? in >> 3 : by_last.of(in);
+        m0 = (8 * group + in - column * rows) * kTileM;
+        n0 = column * cols;
+    }
+};
+
+struct MmWork {  // one piece of the plan
     CUtensorMap a[2], b[2];
     MmEpilogue epi;
-    float *partial;  // not null: sums of part p to partial + p * part_elems, rows of part_ld
-    int64_t part_elems, part_ld;
+    float *partial;  // not null: [tile of the piece][part][256][TN] fp32 sums
     int M, N, K;
     int a_across, b_across;
-    int tiles_m, tiles_n, parts;
+    Raster raster;
+    int tile0, tiles, parts;
     int chunks, total;     // of one term, of all
     int chunks_per_part;
-    int unit_end;          // units of this job and those before it
-    Divisor by_parts, by_group, by_last;  // parts; tiles of 8 tile rows; tile rows of the last group
+    int unit_end;          // units of this piece and those before it
+    Divisor by_parts;
 };
 struct MmParams {
-    MmWork job[kMaxJobs];
-    int jobs;
+    MmWork piece[kMaxPieces];
+    int pieces;
     int *status;
     int64_t timeout_ns;
     int debug_stall;
 };
 
 struct Unit {
-    int job, m0, n0, part, c0, c1;
+    int piece, tile, m0, n0, part, c0, c1;  // tile: of the piece
 };
 
-// Unit u of the launch: jobs in order, a job's tiles in groups of 8 tile rows,
-// along the rows first, so that the pairs at work share operand panels in L2; a
-// tile's parts are adjacent.
+// Unit u of the launch: pieces in order, a tile's parts adjacent.
 __device__ __forceinline__ Unit unit_of(const MmParams &p, int u, int cols) {
     Unit r;
-    r.job = 0;
+    r.piece = 0;
     int begin = 0;
-    while (u >= p.job[r.job].unit_end) begin = p.job[r.job++].unit_end;
-    const MmWork &w = p.job[r.job];
+    while (u >= p.piece[r.piece].unit_end) begin = p.piece[r.piece++].unit_end;
+    const MmWork &w = p.piece[r.piece];
     u -= begin;
-    const int t = w.by_parts.of(u);
-    r.part = u - t * w.parts;
-    const int group = w.by_group.of(t);
-    const int in = t - group * 8 * w.tiles_n;
-    const int rows = min(8, w.tiles_m - 8 * group);
-    const int column = rows == 8 ? in >> 3 : w.by_last.of(in);
-    r.m0 = (8 * group + in - column * rows) * kTileM;
-    r.n0 = column * cols;
+    r.tile = w.by_parts.of(u);
+    r.part = u - r.tile * w.parts;
+    w.raster.tile(w.tile0 + r.tile, cols, r.m0, r.n0);
     r.c0 = r.part * w.chunks_per_part;
     r.c1 = min(r.c0 + w.chunks_per_part, w.total);
     return r;
@@ -391,7 +399,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const uint32_t rank = cluster_rank();
     const Guard guard{abort_flag, p.status, p.timeout_ns};
     const int pair = (int)blockIdx.x / 2, pairs = (int)gridDim.x / 2;
-    const int units = p.job[p.jobs - 1].unit_end;
+    const int units = p.piece[p.pieces - 1].unit_end;
 
     pdl_trigger();
 
@@ -428,11 +436,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int u = pair; ok && u < units; u += pairs) {
             const Unit t = unit_of(p, u, kCols);
             const int ra = t.m0 + 128 * (int)rank, rb = t.n0 + (GATED ? 0 : TN / 2 * (int)rank);
-            const MmWork &w = p.job[t.job];
+            const MmWork &w = p.piece[t.piece];
             // Where the pairs share no rows of a, each tile starts at another chunk and wraps
             // around: in step, all would read the same few address bits of b's rows at a time.
             int at = t.c0;
-            if (w.tiles_m == 1) at += t.n0 / kCols * 5 % max(1, t.c1 - t.c0);
+            if (w.raster.tiles_m == 1) at += t.n0 / kCols * 5 % max(1, t.c1 - t.c0);
             for (int c = t.c0; c < t.c1; ++c) {
                 if (!warp_wait_all(bar(kBarEmpty + s), phase, guard, lane)) {
                     ok = false;
@@ -479,7 +487,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t phase = 0;
         for (int u = pair; ok && u < units; u += pairs, ++tile) {
             const Unit t = unit_of(p, u, kCols);
-            const MmWork &w = p.job[t.job];
+            const MmWork &w = p.piece[t.piece];
             const uint32_t idesc = make_idesc_major(kTileM, TN, F16, w.a_across != 0, w.b_across != 0);
             const uint64_t da = w.a_across ? sw128_desc_across(stages, 64 * 128) : sw128_desc(stages);
             const uint64_t db = w.b_across ? sw128_desc_across(stages + kABytes, 64 * 128) : sw128_desc(stages + kABytes);
@@ -534,12 +542,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         int tile = 0, taken = -1;
         for (int u = pair; u < units; u += pairs, ++tile) {
             const Unit t = unit_of(p, u, kCols);
-            const MmWork &job = p.job[t.job];
+            const MmWork &job = p.piece[t.piece];
             const int ab = tile & 1;
-            if (t.job != taken) {
+            if (t.piece != taken) {
                 w.take(job.epi);
                 w.rows = job.M;
-                taken = t.job;
+                taken = t.piece;
             }
             w.r0 = t.m0 + 128 * (int64_t)rank + 32 * q;
             const int64_t n0 = t.n0 + half * kMine;
@@ -578,10 +586,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 }
                 if (!in) continue;
                 if (partial != nullptr) {
-                    float *part = partial + t.part * job.part_elems;
-                    const int64_t pc = (int64_t)(t.n0 / kCols) * TN + half * kMine + j;
-                    store32(part, job.part_ld, true, w, pc, job.part_ld, v);
-                    if constexpr (GATED) store32(part, job.part_ld, true, w, pc + TN / 2, job.part_ld, x);
+                    Rows whole = w;  // a tile of the workspace
+                    whole.r0 = 128 * (int64_t)rank + 32 * q;
+                    whole.rows = kTileM;
+                    float *const part = partial + ((int64_t)t.tile * job.parts + t.part) * (kTileM * TN);
+                    store32(part, TN, true, whole, half * kMine + j, TN, v);
+                    if constexpr (GATED) store32(part, TN, true, whole, TN / 2 + half * kMine + j, TN, x);
                 } else if constexpr (KIND == kPlain) {
                     finish_plain<F16>(w, c0, N, v);
                 } else if constexpr (GATED) {
@@ -604,26 +614,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 // sums in a fixed tree; four such groups hold a checkpoint block (8 threads each
 // at most, then: the four share a warp).
 template <bool F16, Kind KIND, int TN>
-__global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEpilogue e, const float *partial,
-                                                    int64_t part_elems, int64_t part_ld, int parts, int M, int N,
-                                                    int groups, int lanes_log2) {
+__global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEpilogue e, const __grid_constant__ Raster raster,
+                                                    const float *partial, int tile0, int tiles, int parts, int M, int N,
+                                                    int lanes_log2) {
     constexpr bool GATED = KIND == kGated;
-    constexpr int kCols = GATED ? TN / 2 : TN;
+    constexpr int kCols = GATED ? TN / 2 : TN, kGroups = kCols / 8;
     const int64_t tid = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     const int lanes = 1 << lanes_log2, mine = threadIdx.x & (lanes - 1);
-    const int64_t idx = tid >> lanes_log2;  // groups is a multiple of 4
-    const int64_t r = idx / groups;
-    const int c = (int)(idx - r * groups) * 8;
-    const bool in = r < M && c < N;
+    const int64_t idx = tid >> lanes_log2;  // a tile's groups are a multiple of four
+    const int tile = (int)(idx / (kTileM * kGroups)), row = (int)(idx / kGroups % kTileM), col = (int)(idx % kGroups) * 8;
+    int m0 = 0, n0 = 0;
+    if (tile < tiles) raster.tile(tile0 + tile, kCols, m0, n0);
+    const int64_t r = m0 + row;
+    const int c = n0 + col;
+    const bool in = tile < tiles && r < M && c < N;
     float v[GATED ? 2 : 1][8] = {};
     pdl_trigger();
     pdl_wait();
     if (in) {
 #pragma unroll
         for (int h = 0; h < (GATED ? 2 : 1); ++h) {
-            const float *p = partial + mine * part_elems + r * part_ld + (c / kCols) * TN + c % kCols + h * (TN / 2);
+            constexpr int kPart = kTileM * TN;
+            const float *p = partial + ((int64_t)tile * parts + mine) * kPart + row * TN + col + h * (TN / 2);
 #pragma unroll 4
-            for (int i = mine; i < parts; i += lanes, p += lanes * part_elems) {
+            for (int i = mine; i < parts; i += lanes, p += lanes * kPart) {
                 const float4 lo = *reinterpret_cast<const float4 *>(p);
                 const float4 hi = *(reinterpret_cast<const float4 *>(p) + 1);
                 const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
@@ -697,17 +711,16 @@ typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, 
 template <bool F16, Kind KIND, int TN>
 cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
     cudaError_t e = launch_pdl(mm_kernel<F16, KIND, TN>, dim3(2 * plan.pairs), dim3(kThreads), Shape<TN, KIND>::kSmem, s, p);
-    for (int i = 0; i < p.jobs && e == cudaSuccess; ++i) {
-        const MmWork &w = p.job[i];
+    for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
+        const MmWork &w = p.piece[i];
         if (w.parts == 1) continue;
-        const int groups = (w.N + 31) / 32 * 4;
+        const int64_t groups = (int64_t)w.tiles * kTileM * (KIND == kGated ? TN / 16 : TN / 8);
         int lanes_log2 = 0;  // while the parts and the idle threads last
         const int most = w.epi.saved[0].d_scale ? 3 : 5;
-        while (lanes_log2 < most && (2 << lanes_log2) <= w.parts && ((int64_t)w.M * groups << lanes_log2) < 2 * 2048 * plan.pairs)
+        while (lanes_log2 < most && (2 << lanes_log2) <= w.parts && (groups << lanes_log2) < 2 * 2048 * plan.pairs)
             ++lanes_log2;
-        const int64_t threads = (int64_t)w.M * groups << lanes_log2;
-        e = launch_pdl(parts_kernel<F16, KIND, TN>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, w.epi,
-                       static_cast<const float *>(w.partial), w.part_elems, w.part_ld, w.parts, w.M, w.N, groups,
+        e = launch_pdl(parts_kernel<F16, KIND, TN>, dim3((unsigned)(((groups << lanes_log2) + 255) / 256)), dim3(256), 0,
+                       s, w.epi, w.raster, static_cast<const float *>(w.partial), w.tile0, w.tiles, w.parts, w.M, w.N,
                        lanes_log2);
     }
     return e;
@@ -717,21 +730,21 @@ cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
 // a number of parts: the most that any pair is given, plus what joining costs.
 // A 128-wide tile's chunk takes 0.85 of it (half the products, but its a operand
 // is staged all the same); a unit's set-up and epilogue count as 2.
-double cost_of(const MmPlan &p, int n) {
+double cost_of(const MmPlan &p) {
     const double chunk = p.tn == 256 ? 1.0 : 0.85;
     double most = 0, join = 0;
-    int at[kMaxJobs + 1] = {0}, ends = 0;  // pairs where a job's units start over
-    for (int i = 0; i < n; ++i) {
-        const MmPlan::Cut &c = p.cut[p.order[i]];
+    int at[kMaxPieces + 1] = {0}, ends = 0;  // pairs where a piece's units start over
+    for (int i = 0; i < p.pieces; ++i) {
+        const MmPlan::Piece &c = p.piece[i];
         ends += c.units;
         at[i + 1] = ends % p.pairs;
-        if (c.parts > 1) join += 8 + (double)c.parts * (double)c.part_elems * 8 / 1.4e6;
+        if (c.parts > 1) join += 8 + (double)c.units * (kTileM * 8) * p.tn / 1.4e6;
     }
-    for (int k = 0; k <= n; ++k) {
+    for (int k = 0; k <= p.pieces; ++k) {
         double load = 0;
         int begin = 0;
-        for (int i = 0; i < n; ++i) {
-            const MmPlan::Cut &c = p.cut[p.order[i]];
+        for (int i = 0; i < p.pieces; ++i) {
+            const MmPlan::Piece &c = p.piece[i];
             const int end = begin + c.units;  // units u with u % pairs == at[k]
             const int count = (end - at[k] + p.pairs - 1) / p.pairs - (begin - at[k] + p.pairs - 1) / p.pairs;
             load += count * (c.chunks_per_part * chunk + 2);
@@ -742,8 +755,33 @@ double cost_of(const MmPlan &p, int n) {
     return most + join;
 }
 
+// Adds tiles [tile0, tile0 + tiles) of a job, their contraction in parts of at most
+// `most` chunks.
+void add_piece(MmPlan &p, int job, int tile0, int tiles, int most) {
+    if (tiles == 0) return;
+    MmPlan::Piece &c = p.piece[p.pieces++];
+    const int total = p.job[job].total;
+    c = {job, tile0, tiles, std::max(1, (total + most - 1) / most), 0, 0, 0};
+    c.chunks_per_part = std::max(1, (total + c.parts - 1) / c.parts);
+    c.parts = std::max(1, (total + c.chunks_per_part - 1) / c.chunks_per_part);
+    c.units = tiles * c.parts;
+    p.units += c.units;
+}
+
+// The longest units first; the plan's cost.
+double finish_plan(MmPlan &p, int pairs) {
+    std::stable_sort(p.piece, p.piece + p.pieces, [](const MmPlan::Piece &x, const MmPlan::Piece &y) {
+        return x.chunks_per_part > y.chunks_per_part;
+    });
+    p.pairs = std::min(pairs, p.units);
+    return cost_of(p);
+}
+
 }  // namespace
 
+// Tries both tile widths and, for each, the jobs' contractions cut into parts of one
+// length (few tiles, long sums) and, where the tiles fill the pairs at least once,
+// the tiles of the last, partly filled round cut alone.
 MmPlan plan_mm(const MmJob *jobs, int n, int sms) {
     const int pairs = std::max(1, sms / 2);
     MmPlan best{};
@@ -751,50 +789,55 @@ MmPlan plan_mm(const MmJob *jobs, int n, int sms) {
     const bool gated = jobs[0].kind == kMmGated;
     for (const int tn : {256, 128}) {
         const int cols = gated ? tn / 2 : tn;
-        MmPlan p{};
-        p.tn = tn;
+        MmPlan base{};
+        base.tn = tn;
         int64_t tiles = 0;
-        int longest = 0;
+        int longest = 0, long_job = 0;
         for (int i = 0; i < n; ++i) {
-            MmPlan::Cut &c = p.cut[i];
+            MmPlan::Job &c = base.job[i];
             c.tiles_m = (int)(((int64_t)jobs[i].M + kTileM - 1) / kTileM);
             c.tiles_n = (int)(((int64_t)jobs[i].N + cols - 1) / cols);
             c.chunks = (int)(((int64_t)jobs[i].K + kStep - 1) / kStep);
-            c.part_ld = (int64_t)c.tiles_n * tn;
-            c.part_elems = c.part_ld * jobs[i].M;
+            c.total = c.chunks * jobs[i].terms;
             tiles += (int64_t)c.tiles_m * c.tiles_n;
-            longest = std::max(longest, c.chunks * jobs[i].terms);
-        }
-        // parts of at least 4 chunks, as many as pairs at most
-        for (int d = 1; d == 1 || (longest / d >= 4 && d <= pairs); d += std::max(1, d / 4)) {
-            const int most = std::max(1, (longest + d - 1) / d);
-            p.units = 0;
-            for (int i = 0; i < n; ++i) {
-                MmPlan::Cut &c = p.cut[i];
-                const int total = c.chunks * jobs[i].terms;
-                c.parts = std::max(1, (total + most - 1) / most);
-                c.chunks_per_part = std::max(1, (total + c.parts - 1) / c.parts);
-                c.parts = std::max(1, (total + c.chunks_per_part - 1) / c.chunks_per_part);
-                c.units = c.tiles_m * c.tiles_n * c.parts;
-                p.units += c.units;
+            if (c.total > longest) {
+                longest = c.total;
+                long_job = i;
             }
-            // the longest units first
-            for (int i = 0; i < n; ++i) p.order[i] = i;
-            std::stable_sort(p.order, p.order + n, [&](int x, int y) {
-                return p.cut[x].chunks_per_part > p.cut[y].chunks_per_part;
-            });
-            p.pairs = std::min(pairs, p.units);
-            const double cost = cost_of(p, n);
+        }
+        auto consider = [&](MmPlan &p) {
+            const double cost = finish_plan(p, pairs);
             if (best.tn == 0 || cost < best_cost) {
                 best = p;
                 best_cost = cost;
             }
+        };
+        // parts of at least 4 chunks, as many as pairs at most
+        for (int d = 1; d == 1 || (longest / d >= 4 && d <= pairs); d += std::max(1, d / 4)) {
+            MmPlan p = base;
+            for (int i = 0; i < n; ++i)
+                add_piece(p, i, 0, p.job[i].tiles_m * p.job[i].tiles_n, std::max(1, (longest + d - 1) / d));
+            consider(p);
+        }
+        // the last round's tiles, of the job with the longest units
+        const int of_long = base.job[long_job].tiles_m * base.job[long_job].tiles_n;
+        const int rest = (int)(tiles % pairs);
+        if (tiles <= pairs || tiles > 40 * pairs || rest == 0 || rest > of_long) continue;
+        for (int d = 2; longest / d >= 4 && d <= pairs; d += std::max(1, d / 2)) {
+            MmPlan p = base;
+            for (int i = 0; i < n; ++i) {
+                const int all = p.job[i].tiles_m * p.job[i].tiles_n, cut = i == long_job ? rest : 0;
+                add_piece(p, i, 0, all - cut, std::max(1, p.job[i].total));
+                add_piece(p, i, all - cut, cut, (longest + d - 1) / d);
+            }
+            consider(p);
         }
     }
-    for (int i = 0; i < n; ++i) {
-        if (best.cut[i].parts == 1) continue;
-        best.cut[i].part_at = (int64_t)(best.workspace / sizeof(float));
-        best.workspace += (size_t)best.cut[i].parts * best.cut[i].part_elems * sizeof(float);
+    for (int i = 0; i < best.pieces; ++i) {
+        MmPlan::Piece &c = best.piece[i];
+        if (c.parts == 1) continue;
+        c.part_at = (int64_t)(best.workspace / sizeof(float));
+        best.workspace += (size_t)c.units * kTileM * best.tn * sizeof(float);
     }
     return best;
 }
@@ -851,37 +894,35 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
     const bool gated = jobs[0].kind == kMmGated, f16 = jobs[0].type == EMTK_TYPE_F16;
     MmParams p;
     int end = 0;
-    for (int i = 0; i < n; ++i) {
-        const MmJob &j = jobs[plan.order[i]];
-        const MmPlan::Cut &c = plan.cut[plan.order[i]];
-        MmWork &w = p.job[i];
+    for (int i = 0; i < plan.pieces; ++i) {
+        const MmPlan::Piece &c = plan.piece[i];
+        const MmPlan::Job &t = plan.job[c.job];
+        const MmJob &j = jobs[c.job];
+        MmWork &w = p.piece[i];
         if (j.K > 0) {
             bool ok = true;
-            for (int t = 0; t < j.terms; ++t) ok = ok && encode_operand(nn, &w.a[t], j.a[t], j.M, j.K, 128);
-            for (int t = 0; t < (gated ? 2 : j.terms); ++t) ok = ok && encode_operand(nn, &w.b[t], j.b[t], j.N, j.K, plan.tn / 2);
+            for (int k = 0; k < j.terms; ++k) ok = ok && encode_operand(nn, &w.a[k], j.a[k], j.M, j.K, 128);
+            for (int k = 0; k < (gated ? 2 : j.terms); ++k) ok = ok && encode_operand(nn, &w.b[k], j.b[k], j.N, j.K, plan.tn / 2);
             if (!ok) return cudaErrorInvalidValue;
         }
         w.epi = j.epi;
         w.partial = c.parts > 1 ? static_cast<float *>(partial) + c.part_at : nullptr;
-        w.part_elems = c.part_elems;
-        w.part_ld = c.part_ld;
         w.M = j.M;
         w.N = j.N;
         w.K = j.K;
         w.a_across = j.a[0].across;
         w.b_across = j.b[0].across;
-        w.tiles_m = c.tiles_m;
-        w.tiles_n = c.tiles_n;
+        w.raster = {t.tiles_m, t.tiles_n, Divisor((uint32_t)(8 * t.tiles_n)), Divisor((uint32_t)std::max(1, t.tiles_m % 8))};
+        w.tile0 = c.tile0;
+        w.tiles = c.tiles;
         w.parts = c.parts;
-        w.chunks = c.chunks;
-        w.total = c.chunks * j.terms;
+        w.chunks = t.chunks;
+        w.total = t.total;
         w.chunks_per_part = c.chunks_per_part;
         w.unit_end = end += c.units;
         w.by_parts = Divisor((uint32_t)c.parts);
-        w.by_group = Divisor((uint32_t)(8 * c.tiles_n));
-        w.by_last = Divisor((uint32_t)std::max(1, c.tiles_m % 8));
     }
-    p.jobs = n;
+    p.pieces = plan.pieces;
     p.status = nn->status;
     p.timeout_ns = nn->timeout_ns;
     p.debug_stall = nn->debug_stall;
