@@ -65,58 +65,68 @@ struct Piece<true> {
     }
 };
 
-// Columns c .. c + 7 of row r at any alignment; those from n on are 0.  Away from
+// Columns c .. c + 7 of a row at any alignment; those from n on are 0.  Away from
 // the matrix's first and last bytes, the two aligned words that hold a full piece
 // lie inside the matrix (between its rows, at worst) and are read whole.
-template <bool F16, bool Q8>
-__device__ __forceinline__ void load_any(const Source &s, int64_t r, int64_t c, int rows, int n, float *v) {
-    constexpr int kBytes = Q8 ? 1 : 2, kWord = kVec * kBytes;
-    const uint8_t *p = s.p + r * s.row_bytes + kBytes * c;
-    const int shift = (int)(reinterpret_cast<uintptr_t>(p) % kWord);
-    const uint8_t *const word = p - shift;
-    const uint8_t *const end = s.p + (int64_t)(rows - 1) * s.row_bytes + (int64_t)kBytes * n;
-    const uint32_t scale = Q8 && c < n ? __ldg(s.scale + r * s.ld_scale + c / kQ8Block) : 1u;
-    const bool whole = c + kVec <= n && word >= s.p && word + (shift ? 2 : 1) * kWord <= end;
-    if (Q8) {
-        uint64_t x = 0;
-        if (whole) {
-            x = __ldg(reinterpret_cast<const unsigned long long *>(word));
-            if (shift) {
-                const uint64_t y = __ldg(reinterpret_cast<const unsigned long long *>(word) + 1);
-                x = (x >> (8 * shift)) | (y << (64 - 8 * shift));
-            }
+template <bool Q8>
+struct AnyPiece {
+    static constexpr int kBytes = Q8 ? 1 : 2, kWord = kVec * kBytes, kWords = kWord / 4;
+    uint32_t x[2 * kWords];
+    uint32_t scale;
+    int shift;  // bytes to drop
+    __device__ __forceinline__ void load(const Source &s, int64_t r, int64_t c, int rows, int n) {
+        const uint8_t *p = s.p + r * s.row_bytes + kBytes * c;
+        shift = (int)(reinterpret_cast<uintptr_t>(p) % kWord);
+        const uint8_t *const word = p - shift;
+        const uint8_t *const end = s.p + (int64_t)(rows - 1) * s.row_bytes + (int64_t)kBytes * n;
+        if (Q8) scale = c < n ? __ldg(s.scale + r * s.ld_scale + c / kQ8Block) : 1u;
+#pragma unroll
+        for (int i = 0; i < 2 * kWords; ++i) x[i] = 0u;
+        if (c + kVec <= n && word >= s.p && word + (shift ? 2 : 1) * kWord <= end) {
+            fetch(word, x);
+            if (shift) fetch(word + kWord, x + kWords);
         } else {
+            shift = 0;
 #pragma unroll
             for (int i = 0; i < kVec; ++i)
-                if (c + i < n) x |= (uint64_t)__ldg(p + i) << (8 * i);
+                if (c + i < n)
+                    x[i * kBytes / 4] |= (Q8 ? (uint32_t)__ldg(p + i) : (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p) + i))
+                                         << (8 * kBytes * i % 32);
         }
-        q8_values4((uint32_t)x, q8_step(scale), v);
-        q8_values4((uint32_t)(x >> 32), q8_step(scale), v + 4);
-    } else {
-        uint32_t x[8] = {};
-        if (whole) {
-            const uint4 a = __ldg(reinterpret_cast<const uint4 *>(word));
-            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-            if (shift) {
-                const uint4 b = __ldg(reinterpret_cast<const uint4 *>(word) + 1);
-                x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-            }
-#pragma unroll
-            for (int i = 0; i < 6; ++i) x[i] = shift & 8 ? x[i + 2] : x[i];
-#pragma unroll
-            for (int i = 0; i < 5; ++i) x[i] = shift & 4 ? x[i + 1] : x[i];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = shift & 2 ? __funnelshift_r(x[i], x[i + 1], 16) : x[i];
-        } else {
-            const uint16_t *e = reinterpret_cast<const uint16_t *>(p);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                if (c + i < n) x[i / 2] |= (uint32_t)__ldg(e + i) << (16 * (i % 2));
-        }
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = from16<F16>((x[i / 2] >> (16 * (i % 2))) & 0xffffu);
     }
-}
+    template <bool F16>
+    __device__ __forceinline__ void values(float *v) const {
+        if constexpr (Q8) {
+            const uint64_t lo = x[0] | (uint64_t)x[1] << 32, hi = x[2] | (uint64_t)x[3] << 32;
+            const uint64_t w = shift ? (lo >> (8 * shift)) | (hi << (64 - 8 * shift)) : lo;
+            q8_values4((uint32_t)w, q8_step(scale), v);
+            q8_values4((uint32_t)(w >> 32), q8_step(scale), v + 4);
+        } else {
+            uint32_t y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = x[i];
+#pragma unroll
+            for (int i = 0; i < 6; ++i) y[i] = shift & 8 ? y[i + 2] : y[i];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) y[i] = shift & 4 ? y[i + 1] : y[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = shift & 2 ? __funnelshift_r(y[i], y[i + 1], 16) : y[i];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] = from16<F16>((y[i / 2] >> (16 * (i % 2))) & 0xffffu);
+        }
+    }
+
+private:
+    static __device__ __forceinline__ void fetch(const uint8_t *p, uint32_t *to) {
+        if constexpr (Q8) {
+            const uint2 w = __ldg(reinterpret_cast<const uint2 *>(p));
+            to[0] = w.x, to[1] = w.y;
+        } else {
+            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(p));
+            to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
+        }
+    }
+};
 
 template <bool F16>
 __device__ __forceinline__ uint4 pack8x16(const float *v) {
@@ -149,15 +159,16 @@ struct SlopeShape {
 };
 
 // Blocks for every SM: with sums few enough that the slices' partial sums stay
-// small against the rows, without them enough to even out the end.
-SlopeShape slope_shape(int m, int n, int sms, bool sums) {
+// small against the rows (the any-alignment kernel, two blocks an SM at a time:
+// two rounds of them), without them enough to even out the end.
+SlopeShape slope_shape(int m, int n, int sms, bool sums, bool wide) {
     SlopeShape h;
     h.lanes_log2 = 5;
     while (h.lanes_log2 > 2 && ((kVec << (h.lanes_log2 - 1)) >= n || (sums && m <= 512))) --h.lanes_log2;
     const int cols = kVec << h.lanes_log2;
     const int at_once = kThreads >> h.lanes_log2;
     h.col_blocks = (int)(((int64_t)n + cols - 1) / cols);
-    int64_t slices = std::max<int64_t>(1, (int64_t)(sums ? 8 : 24) * sms / std::max(1, h.col_blocks));
+    int64_t slices = std::max<int64_t>(1, (int64_t)(!wide ? 4 : sums ? 8 : 24) * sms / std::max(1, h.col_blocks));
     slices = std::min<int64_t>(slices, std::max<int64_t>(1, ((int64_t)m + 2 * at_once - 1) / (2 * at_once)));
     slices = std::min<int64_t>(slices, 65535);
     if (sums && m <= 512) slices = 1;
@@ -286,11 +297,21 @@ __global__ void __launch_bounds__(kThreads) slope_any_kernel(const __grid_consta
     pdl_trigger();
     pdl_wait();
     if (c < a.n) {
-        for (int64_t r = (int64_t)blockIdx.y * a.rows + (threadIdx.x >> a.lanes_log2); r < r1; r += at_once) {
+        AnyPiece<false> d_next;
+        AnyPiece<Q8> g_next, u_next;
+        auto fetch = [&](int64_t r) {
+            d_next.load(a.dy, r, c, a.m, a.n);
+            if (kGate) g_next.load(a.gate, r, c, a.m, a.n);
+            if (GATED) u_next.load(a.up, r, c, a.m, a.n);
+        };
+        int64_t r = (int64_t)blockIdx.y * a.rows + (threadIdx.x >> a.lanes_log2);
+        if (r < r1) fetch(r);
+        for (; r < r1; r += at_once) {
             float d[kVec], g[kVec] = {}, u[kVec] = {}, x[kVec], y[kVec], z[kVec];
-            load_any<F16, false>(a.dy, r, c, a.m, a.n, d);
-            if (kGate) load_any<F16, Q8>(a.gate, r, c, a.m, a.n, g);
-            if (GATED) load_any<F16, Q8>(a.up, r, c, a.m, a.n, u);
+            d_next.template values<F16>(d);
+            if (kGate) g_next.template values<F16>(g);
+            if (GATED) u_next.template values<F16>(u);
+            if (r + at_once < r1) fetch(r + at_once);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
                 slope_of<GATED, ACT>(d[i], g[i], u[i], x[i], y[i], z[i]);
@@ -355,15 +376,15 @@ cudaError_t run_slope(emtk_type type, int act, SlopeArgs &a, float *partial, flo
                       cudaStream_t s) {
     if (a.n == 0) return cudaSuccess;
     const bool gate = GATED || act != EMTK_ACT_NONE, sums = db0 != nullptr;
-    const SlopeShape h = slope_shape(a.m, a.n, sms, sums);
+    a.h_wide = a.h && wide_matrix(a.h, 2 * a.h_ld, 16);
+    const bool wide = wide_source(a.dy, a.n) && (!gate || wide_source(a.gate, a.n)) &&
+                      (!GATED || wide_source(a.up, a.n)) && (!a.h || a.h_wide);
+    const SlopeShape h = slope_shape(a.m, a.n, sms, sums, wide);
     a.rows = h.rows;
     a.lanes_log2 = h.lanes_log2;
     a.sums[0] = h.slices == 1 ? db0 : partial;
     a.sums[1] = h.slices == 1 ? db1 : partial + (int64_t)h.slices * a.n;
     if (!sums) a.sums[0] = a.sums[1] = nullptr;
-    a.h_wide = a.h && wide_matrix(a.h, 2 * a.h_ld, 16);
-    const bool wide = wide_source(a.dy, a.n) && (!gate || wide_source(a.gate, a.n)) &&
-                      (!GATED || wide_source(a.up, a.n)) && (!a.h || a.h_wide);
     const bool q8 = gate && a.gate.scale != nullptr;
     const SlopeKernel kernel = type == EMTK_TYPE_F16 ? slope_for<true, GATED>(act, wide, q8, sums)
                                                      : slope_for<false, GATED>(act, wide, q8, sums);
@@ -476,7 +497,11 @@ __global__ void __launch_bounds__(kThreads) pack8_any_kernel(const __grid_consta
     for (Item it(a.walk, (int64_t)blockIdx.x * kWarps + threadIdx.x / 32); it.r < a.m; it.next(a.walk)) {
         const int64_t c = (int64_t)it.piece * kWarpCols + lane * kVec;
         float v[kVec] = {};
-        if (c < a.k) load_any<F16, false>(a.x, it.r, c, a.m, a.k, v);
+        if (c < a.k) {
+            AnyPiece<false> piece;
+            piece.load(a.x, it.r, c, a.m, a.k);
+            piece.template values<F16>(v);
+        }
         bool all_finite;
         float top = finite_top(v, all_finite);
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -503,7 +528,7 @@ struct CopyArgs {
 
 // A checkpoint's values, rows of codes on 8 bytes and of values on 16: 8 columns a
 // thread, so that neighbours' stores meet in whole sectors (16 columns a thread in
-// two stores took 35 us where this takes XX; 20000 x 2304).
+// two stores took 35 us where this takes 22; 20000 x 2304).
 template <bool F16>
 __device__ __forceinline__ void unpack_wide(const CopyArgs::One &j, Item it) {
     constexpr int kFlight = 4;
@@ -534,20 +559,23 @@ __device__ __forceinline__ void unpack_wide(const CopyArgs::One &j, Item it) {
 template <bool F16, bool Q8>
 __device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it, int lane) {
     while (it.r < j.rows) {
-        float v[2][kVec];
-        int64_t r[2], c[2];
+        constexpr int kFlight = 2;
+        AnyPiece<Q8> w[kFlight];
+        int64_t r[kFlight], c[kFlight];
 #pragma unroll
-        for (int i = 0; i < 2; ++i, it.next(j.walk)) {
+        for (int i = 0; i < kFlight; ++i, it.next(j.walk)) {
             r[i] = it.r;
             c[i] = (int64_t)it.piece * kWarpCols + lane * kVec;
-            if (r[i] < j.rows && c[i] < j.cols) load_any<F16, Q8>(j.from, r[i], c[i], j.rows, j.cols, v[i]);
+            if (r[i] < j.rows && c[i] < j.cols) w[i].load(j.from, r[i], c[i], j.rows, j.cols);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kFlight; ++i) {
             if (r[i] >= j.rows || c[i] >= j.cols) continue;
+            float v[kVec];
+            w[i].template values<F16>(v);
 #pragma unroll
-            for (int t = 0; t < kVec; ++t) v[i][t] = Q8 ? q8_operand<F16>(v[i][t]) : v[i][t];
-            store_any<F16>(j.to + r[i] * j.to_ld, c[i], j.cols, j.to_wide != 0, v[i]);
+            for (int t = 0; t < kVec; ++t) v[t] = Q8 ? q8_operand<F16>(v[t]) : v[t];
+            store_any<F16>(j.to + r[i] * j.to_ld, c[i], j.cols, j.to_wide != 0, v);
         }
     }
 }
@@ -588,7 +616,9 @@ WalkPlan walk_plan(int64_t rows, int64_t k, int cols, int workers, bool even) {
 
 }  // namespace
 
-int slope_slices(int m, int n, int sms) { return n > 0 ? slope_shape(m, n, sms, true).slices : 1; }
+int slope_slices(int m, int n, int sms) {
+    return n > 0 ? std::max(slope_shape(m, n, sms, true, true).slices, slope_shape(m, n, sms, true, false).slices) : 1;
+}
 
 cudaError_t launch_slope(emtk_type type, int act, int m, int n, const emtk_matrix &dy, const emtk_matrix &pre,
                          void *dz, int64_t dz_ld, float *db, float *partial, int sms, cudaStream_t s) {

@@ -435,21 +435,27 @@ def _mat8(t, rows: int, cols: int, dtype, what: str) -> tuple:
     return (d, ld, s, lds)
 
 
-def _vec(t, n: int, what: str, dtype=None) -> int:
+def _vec(t, n: int, what: str, f32: bool = False) -> int:
     if t is None:
         return 0
     if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or not t.is_cuda:
         raise ValueError(f"{what}: expected a contiguous CUDA vector of {n}")
-    if dtype is not None and t.dtype is not dtype:
-        raise ValueError(f"{what}: dtype {t.dtype}, expected {dtype}")
+    if f32 and _type_of(t, what, True) != EMTK_TYPE_F32:
+        raise ValueError(f"{what}: dtype {t.dtype}, expected float32")
     return t.data_ptr()
+
+
+_raw_stream = None
 
 
 def _current(t, stream) -> int:
     """The stream argument, or the current stream of t's device."""
+    global _raw_stream
     if stream is None:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(t.get_device())  # torch.cuda.current_stream() without its object
+        if _raw_stream is None:
+            import torch
+            _raw_stream = torch._C._cuda_getCurrentRawStream  # torch.cuda.current_stream() without its object
+        return _raw_stream(t.get_device())
     return _stream(stream)
 
 
@@ -494,7 +500,6 @@ def emtk_dense(nn, x, w, y, bias=None, act: str = "none", residual=None, pre=Non
 def emtk_dense_backward(nn, dy, x, w, act: str = "none", pre=None, dx=None, dw=None, db=None, stream=None) -> None:
     """Gradients of emtk_dense from dy [m][n]: dx [m][k], dw [n][k] (x's dtype or float32), db [n] float32,
     each optional.  x and pre may be Q8; x may be None without dw, w None without dx."""
-    import torch
     (m, n), dt = dy.shape, dy.dtype
     like = w if w is not None else dw if dw is not None else x.codes if isinstance(x, Q8) else x
     k = 0 if like is None else like.shape[1]
@@ -503,7 +508,7 @@ def emtk_dense_backward(nn, dy, x, w, act: str = "none", pre=None, dx=None, dw=N
                                  *_mat(dy, m, n, dt, "dy"), *_mat8(x, m, k, dt, "x"), *_mat(w, n, k, dt, "w"),
                                  *_mat8(pre, m, n, dt, "pre"), *_mat(dx, m, k, dt, "dx"),
                                  *_mat(dw, n, k, None if dw is None else dw.dtype, "dw"),
-                                 _vec(db, n, "db", torch.float32))
+                                 _vec(db, n, "db", True))
     _check(load_library().emtk_dense_backward(nn, args, _current(dy, stream)), "emtk_dense_backward")
 
 
@@ -528,7 +533,6 @@ def emtk_gated_backward(nn, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx
                         db_gate=None, db_up=None, h=None, stream=None) -> None:
     """Gradients of emtk_gated from dh [m][f] and the gate and up it kept: dx [m][k], dw_gate and dw_up [f][k]
     (x's dtype or float32), db_gate and db_up [f] float32, and h [m][f] once more; each optional."""
-    import torch
     (m, f), dt = dh.shape, dh.dtype
     like = w_gate if w_gate is not None else dw_gate if dw_gate is not None else x.codes if isinstance(x, Q8) else x
     k = 0 if like is None else like.shape[1]
@@ -542,7 +546,7 @@ def emtk_gated_backward(nn, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx
                                  *_mat(w_gate, f, k, dt, "w_gate"), *_mat(w_up, f, k, dt, "w_up"),
                                  *_mat(dx, m, k, dt, "dx"), *_mat(dw_gate, f, k, dwt, "dw_gate"),
                                  *_mat(dw_up, f, k, dwt, "dw_up"), *_mat(h, m, f, dt, "h"),
-                                 _vec(db_gate, f, "db_gate", torch.float32), _vec(db_up, f, "db_up", torch.float32))
+                                 _vec(db_gate, f, "db_gate", True), _vec(db_up, f, "db_up", True))
     _check(load_library().emtk_gated_backward(nn, args, _current(dh, stream)), "emtk_gated_backward")
 
 
