@@ -102,21 +102,25 @@ struct AnyPiece {
             q8_values4((uint32_t)w, q8_step(scale), v);
             q8_values4((uint32_t)(w >> 32), q8_step(scale), v + 4);
         } else {
-            uint32_t y[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = x[i];
-#pragma unroll
-            for (int i = 0; i < 6; ++i) y[i] = shift & 8 ? y[i + 2] : y[i];
-#pragma unroll
-            for (int i = 0; i < 5; ++i) y[i] = shift & 4 ? y[i + 1] : y[i];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = shift & 2 ? __funnelshift_r(y[i], y[i + 1], 16) : y[i];
+            uint32_t y[4];
+            const int half = 8 * (shift & 3);
+            switch (shift >> 2) {  // one case to a row
+                case 0: words<0>(y, half); break;
+                case 1: words<1>(y, half); break;
+                case 2: words<2>(y, half); break;
+                default: words<3>(y, half);
+            }
 #pragma unroll
             for (int i = 0; i < kVec; ++i) v[i] = from16<F16>((y[i / 2] >> (16 * (i % 2))) & 0xffffu);
         }
     }
 
 private:
+    template <int FIRST>
+    __device__ __forceinline__ void words(uint32_t (&y)[4], int bits) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = __funnelshift_r(x[FIRST + i], x[FIRST + i + 1], bits);
+    }
     static __device__ __forceinline__ void fetch(const uint8_t *p, uint32_t *to) {
         if constexpr (Q8) {
             const uint2 w = __ldg(reinterpret_cast<const uint2 *>(p));
@@ -150,7 +154,7 @@ __device__ __forceinline__ void store_any(uint16_t *row, int64_t c, int n, bool 
 // narrow matrices) and one slice of the rows, kThreads / lanes rows at a time;
 // a thread adds its rows in order, the block its threads' sums and the second
 // kernel the slices' in fixed orders, so the column sums do not depend on
-// timing.  Up to 512 rows are one slice of 4 lanes' columns, whose sums are the
+// timing.  Up to 512 rows are one slice of 2 lanes' columns, whose sums are the
 // result.
 struct SlopeShape {
     int lanes_log2;  // threads across
@@ -164,14 +168,15 @@ struct SlopeShape {
 SlopeShape slope_shape(int m, int n, int sms, bool sums, bool wide) {
     SlopeShape h;
     h.lanes_log2 = 5;
-    while (h.lanes_log2 > 2 && ((kVec << (h.lanes_log2 - 1)) >= n || (sums && m <= 512))) --h.lanes_log2;
+    const bool one_slice = sums && m <= 512;
+    while (h.lanes_log2 > (one_slice ? 1 : 2) && ((kVec << (h.lanes_log2 - 1)) >= n || one_slice)) --h.lanes_log2;
     const int cols = kVec << h.lanes_log2;
     const int at_once = kThreads >> h.lanes_log2;
     h.col_blocks = (int)(((int64_t)n + cols - 1) / cols);
     int64_t slices = std::max<int64_t>(1, (int64_t)(!wide ? 4 : sums ? 8 : 24) * sms / std::max(1, h.col_blocks));
     slices = std::min<int64_t>(slices, std::max<int64_t>(1, ((int64_t)m + 2 * at_once - 1) / (2 * at_once)));
     slices = std::min<int64_t>(slices, 65535);
-    if (sums && m <= 512) slices = 1;
+    if (one_slice) slices = 1;
     int64_t rows = ((int64_t)m + slices - 1) / slices;
     rows = (rows + at_once - 1) / at_once * at_once;
     rows = std::max<int64_t>(rows, at_once);
@@ -397,9 +402,9 @@ cudaError_t run_slope(emtk_type type, int act, SlopeArgs &a, float *partial, flo
 }
 
 // -------------------------------------------------------- checkpoints
-// Work is dealt out in pieces of a row, every so-manieth one to a thread (aligned
-// rows) or to a warp (256 columns, any); the step from one to the next is added to
-// row and piece, without a division.
+// Work is dealt out in pieces of a row, every so-manieth one to a thread (or to a
+// warp, 256 columns); the step from one to the next is added to row and piece,
+// without a division.
 struct Walk {
     int per_row;
     int64_t step_rows;
@@ -557,7 +562,7 @@ __device__ __forceinline__ void unpack_wide(const CopyArgs::One &j, Item it) {
 }
 
 template <bool F16, bool Q8>
-__device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it, int lane) {
+__device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it) {
     while (it.r < j.rows) {
         constexpr int kFlight = 2;
         AnyPiece<Q8> w[kFlight];
@@ -565,12 +570,12 @@ __device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it, int la
 #pragma unroll
         for (int i = 0; i < kFlight; ++i, it.next(j.walk)) {
             r[i] = it.r;
-            c[i] = (int64_t)it.piece * kWarpCols + lane * kVec;
-            if (r[i] < j.rows && c[i] < j.cols) w[i].load(j.from, r[i], c[i], j.rows, j.cols);
+            c[i] = (int64_t)it.piece * kVec;
+            if (r[i] < j.rows) w[i].load(j.from, r[i], c[i], j.rows, j.cols);
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            if (r[i] >= j.rows || c[i] >= j.cols) continue;
+            if (r[i] >= j.rows) continue;
             float v[kVec];
             w[i].template values<F16>(v);
 #pragma unroll
@@ -583,16 +588,14 @@ __device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it, int la
 template <bool F16>
 __global__ void __launch_bounds__(kThreads, kBlocks) copy16_kernel(const __grid_constant__ CopyArgs a) {
     const CopyArgs::One &j = a.job[blockIdx.z];
-    const int lane = threadIdx.x & 31;
-    const int64_t thread = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    Item it(j.walk, j.wide ? thread : thread / 32);
+    const Item it(j.walk, (int64_t)blockIdx.x * kThreads + threadIdx.x);
     pdl_trigger();
     pdl_wait();
     if (j.wide) return unpack_wide<F16>(j, it);
     if (j.from.scale)
-        copy_any<F16, true>(j, it, lane);
+        copy_any<F16, true>(j, it);
     else
-        copy_any<F16, false>(j, it, lane);
+        copy_any<F16, false>(j, it);
 }
 
 // A walk of pieces of `cols` columns over rows of k, by threads or by warps, in
@@ -673,8 +676,7 @@ cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, 
         const Source from = source_of(c.from);
         const bool to_wide = wide_matrix(c.to.d, 2 * c.to.ld, 16);
         const bool wide = from.scale && to_wide && wide_source(from, c.cols);
-        plans[jobs] = wide ? walk_plan(c.rows, c.cols, kVec, kThreads, false)
-                           : walk_plan(c.rows, c.cols, kWarpCols, kWarps, false);
+        plans[jobs] = walk_plan(c.rows, c.cols, kVec, kThreads, false);
         blocks = std::max(blocks, plans[jobs].blocks(sms));
         a.job[jobs++] = {from, static_cast<uint16_t *>(c.to.d), c.to.ld, c.rows, c.cols, wide, to_wide, Walk{}};
     }
