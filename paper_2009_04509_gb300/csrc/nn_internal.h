@@ -65,15 +65,16 @@ bool mm_operand_ok(const void *p, int64_t ld, int64_t rows);
 bool encode_operand(const emtk_nn *nn, CUtensorMap *map, const MmOperand &o, int rows, int K, int box_rows);
 // Up to kMaxJobs jobs of one kind and type in one launch (nn_mm.cu); the plan
 // says how they are cut, and how much workspace `partial` it needs.  A piece is a
-// run of a job's tiles whose contraction is cut into equally many parts.
-constexpr int kMaxJobs = 3, kMaxPieces = 2 * kMaxJobs;
+// run of a job's tiles whose contraction is cut into equally many parts, dealt in
+// turn to pair_count of the launch's CTA pairs from pair_lo on.
+constexpr int kMaxJobs = 3, kMaxPieces = 8;
 struct MmPlan {
     int tn, pairs, units, pieces;
     struct Job {
         int tiles_m, tiles_n, chunks, total;
     } job[kMaxJobs];
     struct Piece {
-        int job, tile0, tiles, parts, chunks_per_part, units;
+        int job, tile0, tiles, parts, chunks_per_part, units, pair_lo, pair_count;
         int64_t part_at;
     } piece[kMaxPieces];
     size_t workspace;

@@ -101,7 +101,7 @@ struct MmWork {  // one piece of the plan
     int tile0, tiles, parts;
     int chunks, total;     // of one term, of all
     int chunks_per_part;
-    int unit_end;          // units of this piece and those before it
+    int units, pair_lo, pair_count;  // unit u is pair pair_lo + u % pair_count's
     Divisor by_parts;
 };
 struct MmParams {
@@ -116,14 +116,29 @@ struct Unit {
     int piece, tile, m0, n0, part, c0, c1;  // tile: of the piece
 };
 
-// Unit u of the launch: pieces in order, a tile's parts adjacent.
-__device__ __forceinline__ Unit unit_of(const MmParams &p, int u, int cols) {
+// A pair's way through its units: the pieces in order.
+struct Cursor {
+    int piece = -1, u = 0;
+    __device__ __forceinline__ bool advance(const MmParams &p, int pair) {
+        if (piece >= 0) {
+            u += p.piece[piece].pair_count;
+            if (u < p.piece[piece].units) return true;
+        }
+        while (++piece < p.pieces) {
+            const MmWork &w = p.piece[piece];
+            u = pair - w.pair_lo;
+            if (u >= 0 && u < w.pair_count && u < w.units) return true;
+        }
+        return false;
+    }
+};
+
+// The cursor's unit: a tile's parts are adjacent.
+__device__ __forceinline__ Unit unit_of(const MmParams &p, const Cursor &at, int cols) {
     Unit r;
-    r.piece = 0;
-    int begin = 0;
-    while (u >= p.piece[r.piece].unit_end) begin = p.piece[r.piece++].unit_end;
+    r.piece = at.piece;
+    const int u = at.u;
     const MmWork &w = p.piece[r.piece];
-    u -= begin;
     r.tile = w.by_parts.of(u);
     r.part = u - r.tile * w.parts;
     w.raster.tile(w.tile0 + r.tile, cols, r.m0, r.n0);
@@ -398,8 +413,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     const Guard guard{abort_flag, p.status, p.timeout_ns};
-    const int pair = (int)blockIdx.x / 2, pairs = (int)gridDim.x / 2;
-    const int units = p.piece[p.pieces - 1].unit_end;
+    const int pair = (int)blockIdx.x / 2;
+    Cursor cursor;
 
     pdl_trigger();
 
@@ -433,8 +448,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t full0 = cluster_addr(bar(kBarFull), 0);
         int s = 0;
         uint32_t phase = 1;  // a fresh barrier's previous phase counts as complete
-        for (int u = pair; ok && u < units; u += pairs) {
-            const Unit t = unit_of(p, u, kCols);
+        while (ok && cursor.advance(p, pair)) {
+            const Unit t = unit_of(p, cursor, kCols);
             const int ra = t.m0 + 128 * (int)rank, rb = t.n0 + (GATED ? 0 : TN / 2 * (int)rank);
             const MmWork &w = p.piece[t.piece];
             // Where the pairs share no rows of a, each tile starts at another chunk and wraps
@@ -485,8 +500,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         bool ok = true;
         int s = 0, tile = 0;
         uint32_t phase = 0;
-        for (int u = pair; ok && u < units; u += pairs, ++tile) {
-            const Unit t = unit_of(p, u, kCols);
+        for (; ok && cursor.advance(p, pair); ++tile) {
+            const Unit t = unit_of(p, cursor, kCols);
             const MmWork &w = p.piece[t.piece];
             const uint32_t idesc = make_idesc_major(kTileM, TN, F16, w.a_across != 0, w.b_across != 0);
             const uint64_t da = w.a_across ? sw128_desc_across(stages, 64 * 128) : sw128_desc(stages);
@@ -540,8 +555,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         w.stage = tail + e * E::kWarpBytes;
         w.lane = lane;
         int tile = 0, taken = -1;
-        for (int u = pair; u < units; u += pairs, ++tile) {
-            const Unit t = unit_of(p, u, kCols);
+        for (; cursor.advance(p, pair); ++tile) {
+            const Unit t = unit_of(p, cursor, kCols);
             const MmWork &job = p.piece[t.piece];
             const int ab = tile & 1;
             if (t.piece != taken) {
@@ -730,25 +745,24 @@ cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
 // a number of parts: the most that any pair is given, plus what joining costs.
 // A 128-wide tile's chunk takes 0.85 of it (half the products, but its a operand
 // is staged all the same); a unit's set-up and epilogue count as 2.
+double unit_cost(const MmPlan &p, const MmPlan::Piece &c) { return c.chunks_per_part * (p.tn == 256 ? 1.0 : 0.85) + 2; }
+
 double cost_of(const MmPlan &p) {
-    const double chunk = p.tn == 256 ? 1.0 : 0.85;
+    int at[3 * kMaxPieces + 1] = {0}, ats = 1;  // pairs where the number of some piece's units changes
     double most = 0, join = 0;
-    int at[kMaxPieces + 1] = {0}, ends = 0;  // pairs where a piece's units start over
     for (int i = 0; i < p.pieces; ++i) {
         const MmPlan::Piece &c = p.piece[i];
-        ends += c.units;
-        at[i + 1] = ends % p.pairs;
+        for (const int a : {c.pair_lo, c.pair_lo + c.pair_count, c.pair_lo + c.units % c.pair_count})
+            if (a > 0 && a < p.pairs) at[ats++] = a;
         if (c.parts > 1) join += 8 + (double)c.units * (kTileM * 8) * p.tn / 1.4e6;
     }
-    for (int k = 0; k <= p.pieces; ++k) {
+    for (int k = 0; k < ats; ++k) {
         double load = 0;
-        int begin = 0;
         for (int i = 0; i < p.pieces; ++i) {
             const MmPlan::Piece &c = p.piece[i];
-            const int end = begin + c.units;  // units u with u % pairs == at[k]
-            const int count = (end - at[k] + p.pairs - 1) / p.pairs - (begin - at[k] + p.pairs - 1) / p.pairs;
-            load += count * (c.chunks_per_part * chunk + 2);
-            begin = end;
+            const int first = at[k] - c.pair_lo;
+            if (first >= 0 && first < c.pair_count && first < c.units)
+                load += ((c.units - first - 1) / c.pair_count + 1) * unit_cost(p, c);
         }
         most = std::max(most, load);
     }
@@ -761,19 +775,52 @@ void add_piece(MmPlan &p, int job, int tile0, int tiles, int most) {
     if (tiles == 0) return;
     MmPlan::Piece &c = p.piece[p.pieces++];
     const int total = p.job[job].total;
-    c = {job, tile0, tiles, std::max(1, (total + most - 1) / most), 0, 0, 0};
+    c = {};
+    c.job = job;
+    c.tile0 = tile0;
+    c.tiles = tiles;
+    c.parts = std::max(1, (total + most - 1) / most);
     c.chunks_per_part = std::max(1, (total + c.parts - 1) / c.parts);
     c.parts = std::max(1, (total + c.chunks_per_part - 1) / c.chunks_per_part);
     c.units = tiles * c.parts;
     p.units += c.units;
 }
 
-// The longest units first; the plan's cost.
+// Deals the units out, the longest first, and returns the plan's cost.  Where a
+// piece's last round leaves some pairs without one of its units, the next piece
+// gives those pairs as many of its shorter units first as take the same time.
 double finish_plan(MmPlan &p, int pairs) {
     std::stable_sort(p.piece, p.piece + p.pieces, [](const MmPlan::Piece &x, const MmPlan::Piece &y) {
         return x.chunks_per_part > y.chunks_per_part;
     });
     p.pairs = std::min(pairs, p.units);
+    MmPlan::Piece sorted[kMaxPieces];
+    const int n = p.pieces;
+    std::copy(p.piece, p.piece + n, sorted);
+    p.pieces = 0;
+    int longer = 0;  // pairs that have one of the last piece's units more than the others
+    double cost = 0;
+    for (int i = 0; i < n; ++i) {
+        MmPlan::Piece c = sorted[i];
+        const double mine = unit_cost(p, c);
+        if (longer > 0 && p.pieces + (n - i) < kMaxPieces) {
+            MmPlan::Piece even = c;
+            even.pair_lo = longer;
+            even.pair_count = p.pairs - longer;
+            even.tiles = std::min(c.tiles, (int)(cost / mine + 0.5) * even.pair_count / c.parts);
+            even.units = even.tiles * c.parts;
+            if (even.tiles > 0) p.piece[p.pieces++] = even;
+            c.tile0 += even.tiles;
+            c.tiles -= even.tiles;
+            c.units -= even.units;
+        }
+        if (c.tiles == 0) continue;
+        c.pair_lo = 0;
+        c.pair_count = p.pairs;
+        p.piece[p.pieces++] = c;
+        longer = c.units % p.pairs;
+        cost = mine;
+    }
     return cost_of(p);
 }
 
@@ -893,7 +940,6 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
                       cudaStream_t s) {
     const bool gated = jobs[0].kind == kMmGated, f16 = jobs[0].type == EMTK_TYPE_F16;
     MmParams p;
-    int end = 0;
     for (int i = 0; i < plan.pieces; ++i) {
         const MmPlan::Piece &c = plan.piece[i];
         const MmPlan::Job &t = plan.job[c.job];
@@ -919,7 +965,9 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
         w.chunks = t.chunks;
         w.total = t.total;
         w.chunks_per_part = c.chunks_per_part;
-        w.unit_end = end += c.units;
+        w.units = c.units;
+        w.pair_lo = c.pair_lo;
+        w.pair_count = c.pair_count;
         w.by_parts = Divisor((uint32_t)c.parts);
     }
     p.pieces = plan.pieces;
