@@ -33,6 +33,7 @@ struct Range {  // NVTX range on the host thread
 
 emtk_status status_of(cudaError_t e) {
     if (e == cudaSuccess) return EMTK_OK;
+    cudaGetLastError();  // reported here; not left for a later launch to find
     return e == cudaErrorMemoryAllocation ? EMTK_ERR_OOM : EMTK_ERR_CUDA;
 }
 

@@ -8,6 +8,12 @@
 
 #include "../../include/emtk.h"
 
+#ifdef __CUDACC__
+#define EMTK_HOST_DEVICE __host__ __device__ __forceinline__
+#else
+#define EMTK_HOST_DEVICE inline
+#endif
+
 struct emtk_nn {
     int device = 0;
     int sm_count = 0;
@@ -63,6 +69,23 @@ bool mm_operand_ok(const void *p, int64_t ld, int64_t rows);
 // Tensor map of an operand: rows of index i (M or N), K contraction steps, boxes
 // of 128 bytes along memory by box_rows (or 64, where i runs along memory).
 bool encode_operand(const emtk_nn *nn, CUtensorMap *map, const MmOperand &o, int rows, int K, int box_rows);
+constexpr int kMmTileRows = 256, kMmStep = 64;  // rows of a tile, contraction steps of a chunk
+
+// Division by a fixed d > 0 of 0 <= n < 2^31, as a product: floor(n m / 2^(31 + s)) with
+// 2^(s - 1) < d <= 2^s and m = ceil(2^(31 + s) / d) < 2^32 is exact there.  The integer
+// unit's own division would keep each tile's first MMA waiting.
+struct Divisor {
+    uint32_t mul, shift;
+    Divisor() = default;
+    explicit Divisor(uint32_t d) {
+        uint32_t s = 0;
+        while ((1u << s) < d) ++s;
+        mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
+        shift = 31 + s;
+    }
+    EMTK_HOST_DEVICE int of(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
+};
+
 // Up to kMaxJobs jobs of one kind and type in one launch (nn_mm.cu); the plan
 // says how they are cut, and how much workspace `partial` it needs.  A piece is a
 // run of a job's tiles whose contraction is cut into equally many parts, dealt in
