@@ -329,17 +329,22 @@ __device__ __forceinline__ void finish_plain(const Rows &w, int64_t c0, int64_t 
         store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, v);
 }
 
+// The residual's block into the warp's staged rows.
+__device__ __forceinline__ void stage_residual(const Rows &w, int64_t c0, int64_t cols) {
+    move_block<uint16_t, true, 64>(static_cast<uint16_t *>(w.residual), w.residual_ld, w.r0, w.rows, c0, cols,
+                                   w.residual_wide, w.stage, w.lane);
+    __syncwarp();
+}
+
 // Sums of a dense tile's 32 columns (z without its bias, which is in `bias`).
 template <bool F16>
 __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
-                                             const float *bias, float (&v)[32]) {
+                                             const float *bias, bool staged_residual, float (&v)[32]) {
     if (w.has_bias) add_bias(bias, v);
     if (w.has_saved) store_saved<F16>(e.saved[0], w, c0, cols, v);
     apply_act(w.act, v);
     if (w.residual) {
-        move_block<uint16_t, true, 64>(static_cast<uint16_t *>(w.residual), w.residual_ld, w.r0, w.rows, c0, cols,
-                                   w.residual_wide, w.stage, w.lane);
-        __syncwarp();
+        if (!staged_residual) stage_residual(w, c0, cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint4 q = *reinterpret_cast<const uint4 *>(w.stage + staged<64>(w.lane, i));
@@ -560,6 +565,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (GATED) bias[kMine + j] = bias_at<F16>(job.epi, 1, n0 + j, N);
                 }
             }
+            // the first block's residual comes while the tile is summed (a z to be kept needs
+            // the staged rows first)
+            const bool early = KIND == kDense && partial == nullptr && w.residual && !w.has_saved && w.r0 < w.rows && n0 < N;
+            if (early) stage_residual(w, n0, N);
             if (!warp_wait(bar(kBarAccFull + ab), (uint32_t)(tile / 2) & 1u, guard, lane)) break;
             tc_fence_after();
             const uint32_t acc = tmem + (uint32_t)(ab * TN) + ((uint32_t)(32 * q) << 16);
@@ -597,7 +606,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 } else if constexpr (GATED) {
                     finish_gated<F16>(job.epi, w, c0, N, bias + j, bias + kMine + j, v, x);
                 } else {
-                    finish_dense<F16>(job.epi, w, c0, N, bias + j, v);
+                    finish_dense<F16>(job.epi, w, c0, N, bias + j, j == 0 && early, v);
                 }
             }
         }
