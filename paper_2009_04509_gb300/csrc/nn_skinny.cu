@@ -9,6 +9,11 @@
 // up to 8 CTAs splits the contraction: each leaves its fp32 sums in shared
 // memory, and every CTA adds the cluster's sums for its share of the rows, in
 // rank order, over distributed shared memory; no second kernel, no workspace.
+//
+// HBM bounds it.  4096 -> 2 x 10240 gated, bf16 (168 MB of weights): 31 us for 8 rows,
+// 32 for 16, 38 for 64 (5.4, 5.2 and 4.5 TB/s); 4096 -> 10240 dense: 18 us for 8 rows.
+// With all CTAs starting at the same chunk 16 rows took 56 us.  What is left to the
+// copy's 6.8 TB/s is the ramp and, from 32 rows on, the epilogue.
 #include <algorithm>
 
 #include "emtk_internal.h"
