@@ -70,34 +70,39 @@ struct Piece<true> {
     }
 };
 
-// Columns c .. c + 7 of a row at any alignment; those from n on are 0.  Away from
-// the matrix's first and last bytes, the two aligned words that hold a full piece
-// lie inside the matrix (between its rows, at worst) and are read whole.
+// Columns c .. c + 7 of a row at any alignment; those from n on are 0.  A full piece
+// of any row but the first and the last lies in two aligned words of the matrix
+// (between its rows, at worst), which are read whole; others go by elements.
 template <bool Q8>
 struct AnyPiece {
     static constexpr int kBytes = Q8 ? 1 : 2, kWord = kVec * kBytes, kWords = kWord / 4;
     uint32_t x[2 * kWords];
     uint32_t scale;
     int shift;  // bytes to drop
-    __device__ __forceinline__ void load(const Source &s, int64_t r, int64_t c, int rows, int n) {
-        const uint8_t *p = s.p + r * s.row_bytes + kBytes * c;
-        shift = (int)(reinterpret_cast<uintptr_t>(p) % kWord);
-        const uint8_t *const word = p - shift;
-        const uint8_t *const end = s.p + (int64_t)(rows - 1) * s.row_bytes + (int64_t)kBytes * n;
-        if (Q8) scale = c < n ? __ldg(s.scale + r * s.ld_scale + c / kQ8Block) : 1u;
-#pragma unroll
-        for (int i = 0; i < 2 * kWords; ++i) x[i] = 0u;
-        if (c + kVec <= n && word >= s.p && word + (shift ? 2 : 1) * kWord <= end) {
-            fetch(word, x);
-            if (shift) fetch(word + kWord, x + kWords);
+    // p: the first element; valid: columns up to n, at least 1
+    __device__ __forceinline__ void load(const uint8_t *p, const uint8_t *s, bool inside, int valid) {
+        if (Q8) scale = __ldg(s);
+        shift = 0;
+        if (inside) {
+            shift = (int)(reinterpret_cast<uintptr_t>(p) % kWord);
+            fetch(p - shift, x);
+            fetch(p - shift + kWord, x + kWords);
         } else {
-            shift = 0;
+#pragma unroll
+            for (int i = 0; i < 2 * kWords; ++i) x[i] = 0u;
 #pragma unroll
             for (int i = 0; i < kVec; ++i)
-                if (c + i < n)
+                if (i < valid)
                     x[i * kBytes / 4] |= (Q8 ? (uint32_t)__ldg(p + i) : (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p) + i))
                                          << (8 * kBytes * i % 32);
         }
+    }
+    __device__ __forceinline__ void load(const Source &s, int64_t r, int64_t c, int rows, int n) {
+        load(s.p + r * s.row_bytes + kBytes * c, Q8 ? s.scale + r * s.ld_scale + c / kQ8Block : nullptr,
+             inside_of(r, c, rows, n), (int)min((int64_t)kVec, n - c));
+    }
+    static __device__ __forceinline__ bool inside_of(int64_t r, int64_t c, int rows, int n) {
+        return r > 0 && r < rows - 1 && c + kVec <= n;
     }
     template <bool F16>
     __device__ __forceinline__ void values(float *v) const {
@@ -168,7 +173,7 @@ struct SlopeShape {
 };
 
 // Blocks for every SM: with sums few enough that the slices' partial sums stay
-// small against the rows (the any-alignment kernel, two blocks an SM at a time:
+// small against the rows (the any-alignment kernel, three blocks an SM at a time:
 // two rounds of them), without them enough to even out the end.
 SlopeShape slope_shape(int m, int n, int sms, bool sums, bool wide) {
     SlopeShape h;
@@ -178,7 +183,7 @@ SlopeShape slope_shape(int m, int n, int sms, bool sums, bool wide) {
     const int cols = kVec << h.lanes_log2;
     const int at_once = kThreads >> h.lanes_log2;
     h.col_blocks = (int)(((int64_t)n + cols - 1) / cols);
-    int64_t slices = std::max<int64_t>(1, (int64_t)(!wide ? 4 : sums ? 8 : 24) * sms / std::max(1, h.col_blocks));
+    int64_t slices = std::max<int64_t>(1, (int64_t)(!wide ? 6 : sums ? 8 : 24) * sms / std::max(1, h.col_blocks));
     slices = std::min<int64_t>(slices, std::max<int64_t>(1, ((int64_t)m + 2 * at_once - 1) / (2 * at_once)));
     slices = std::min<int64_t>(slices, 65535);
     if (one_slice) slices = 1;
@@ -296,9 +301,11 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const __grid_constant__
     if constexpr (SUMS) block_sums<GATED>(a, sg, su);
 }
 
-// Any alignment and width.
+// Any alignment and width; three blocks an SM (two or four were slower at most of
+// 2048 x 5461, 8192 x 2731 and 20000 x 515).
+constexpr int kAnyBlocks = 3;
 template <bool F16, bool GATED, int ACT, bool Q8>
-__global__ void __launch_bounds__(kThreads) slope_any_kernel(const __grid_constant__ SlopeArgs a) {
+__global__ void __launch_bounds__(kThreads, kAnyBlocks) slope_any_kernel(const __grid_constant__ SlopeArgs a) {
     constexpr bool kGate = GATED || ACT != EMTK_ACT_NONE;
     const int at_once = kThreads >> a.lanes_log2;
     const int64_t c = (int64_t)blockIdx.x * (kVec << a.lanes_log2) + (threadIdx.x & ((1 << a.lanes_log2) - 1)) * kVec;
@@ -307,21 +314,30 @@ __global__ void __launch_bounds__(kThreads) slope_any_kernel(const __grid_consta
     pdl_trigger();
     pdl_wait();
     if (c < a.n) {
-        AnyPiece<false> d_next;
-        AnyPiece<Q8> g_next, u_next;
-        auto fetch = [&](int64_t r) {
-            d_next.load(a.dy, r, c, a.m, a.n);
-            if (kGate) g_next.load(a.gate, r, c, a.m, a.n);
-            if (GATED) u_next.load(a.up, r, c, a.m, a.n);
-        };
-        int64_t r = (int64_t)blockIdx.y * a.rows + (threadIdx.x >> a.lanes_log2);
-        if (r < r1) fetch(r);
-        for (; r < r1; r += at_once) {
+        constexpr int kBytes = Q8 ? 1 : 2;
+        const int64_t r0 = (int64_t)blockIdx.y * a.rows + (threadIdx.x >> a.lanes_log2);
+        const int valid = (int)min((int64_t)kVec, a.n - c);
+        const uint8_t *dp = a.dy.p + r0 * a.dy.row_bytes + 2 * c;
+        const uint8_t *gp = kGate ? a.gate.p + r0 * a.gate.row_bytes + kBytes * c : nullptr;
+        const uint8_t *up = GATED ? a.up.p + r0 * a.up.row_bytes + kBytes * c : nullptr;
+        const uint8_t *gs = kGate && Q8 ? a.gate.scale + r0 * a.gate.ld_scale + c / kQ8Block : nullptr;
+        const uint8_t *us = GATED && Q8 ? a.up.scale + r0 * a.up.ld_scale + c / kQ8Block : nullptr;
+        for (int64_t r = r0; r < r1; r += at_once) {
             float d[kVec], g[kVec] = {}, u[kVec] = {}, x[kVec], y[kVec], z[kVec];
-            d_next.template values<F16>(d);
-            if (kGate) g_next.template values<F16>(g);
-            if (GATED) u_next.template values<F16>(u);
-            if (r + at_once < r1) fetch(r + at_once);
+            AnyPiece<false> pd;
+            AnyPiece<Q8> pg, pu;
+            const bool inside = AnyPiece<false>::inside_of(r, c, a.m, a.n);
+            pd.load(dp, nullptr, inside, valid);
+            if (kGate) pg.load(gp, gs, inside, valid);
+            if (GATED) pu.load(up, us, inside, valid);
+            dp += at_once * a.dy.row_bytes;
+            if (kGate) gp += at_once * a.gate.row_bytes;
+            if (GATED) up += at_once * a.up.row_bytes;
+            if (kGate && Q8) gs += at_once * a.gate.ld_scale;
+            if (GATED && Q8) us += at_once * a.up.ld_scale;
+            pd.template values<F16>(d);
+            if (kGate) pg.template values<F16>(g);
+            if (GATED) pu.template values<F16>(u);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
                 slope_of<GATED, ACT>(d[i], g[i], u[i], x[i], y[i], z[i]);
