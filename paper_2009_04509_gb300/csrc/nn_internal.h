@@ -107,7 +107,7 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
 cudaError_t init_mm_kernels();  // once per device
 // The forward pass of 1 to 4 rows (nn_rows.cu), operands anywhere.
 bool few_rows(const MmJob &job);
-cudaError_t launch_rows(const MmJob &job, cudaStream_t s);
+cudaError_t launch_rows(const MmJob &job, int sms, cudaStream_t s);
 // The forward pass of up to 64 rows (nn_skinny.cu).
 bool skinny(const MmJob &job);
 cudaError_t launch_skinny(const MmJob &job, const emtk_nn *nn, cudaStream_t s);

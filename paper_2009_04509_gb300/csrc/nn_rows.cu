@@ -7,8 +7,10 @@
 // from L1.  The warps of a group hold different pieces and add their sums in
 // shared memory, in order.  A tile of the tensor-core kernel would be 97% zero
 // rows and needs a second kernel to join its split contraction.  Four rows a warp
-// and no unrolling measured best (4096 -> 10240 gated, one row, bf16: 26.3 us, 6.4
-// TB/s; two or eight rows 31.6, unrolled twice 27.5): 40 registers, six blocks an SM.
+// and no unrolling measured best (4096 -> 2 x 10240 gated, one row, bf16: 25.4 us, 6.6
+// TB/s, with blocks of 8 warps 26.0; two or eight weight rows a warp 31.6, unrolled
+// twice 27.5).  HBM bounds it from 50 MB of weights on; 4096 -> 4096 takes 7.3 us, of
+// which 5 are its bytes.
 #include <algorithm>
 
 #include "emtk_internal.h"
@@ -18,7 +20,7 @@
 namespace emtk {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMostWarps = 8;  // of a block
 constexpr int kHeld = 4;  // weight rows of a warp
 
 struct RowsParams {
@@ -49,11 +51,11 @@ __device__ __forceinline__ void unpack(const uint4 &q, float (&v)[8]) {
 
 // ROWS: rows of x.  WIDE: every row of x and w starts on 16 bytes.
 template <bool F16, bool GATED, int ROWS, bool WIDE>
-__global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ RowsParams p) {
+__global__ void __launch_bounds__(32 * kMostWarps) rows_kernel(const __grid_constant__ RowsParams p) {
     constexpr int kOut = GATED ? kHeld / 2 : kHeld;  // output columns of a group
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     const int split = 1 << p.split_log2, part = warp & (split - 1);
-    const int64_t n0 = ((int64_t)blockIdx.x * (kWarps >> p.split_log2) + (warp >> p.split_log2)) * kOut;
+    const int64_t n0 = ((int64_t)blockIdx.x * (blockDim.x >> (5 + p.split_log2)) + (warp >> p.split_log2)) * kOut;
     const uint16_t *w[kHeld];
 #pragma unroll
     for (int r = 0; r < kHeld; ++r) {
@@ -106,7 +108,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ 
         for (int i = 0; i < ROWS; ++i)
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) acc[r][i] += __shfl_xor_sync(0xffffffffu, acc[r][i], d);
-    __shared__ float sums[kWarps][kHeld * ROWS];
+    __shared__ float sums[kMostWarps][kHeld * ROWS];
     if (lane == 0) {
 #pragma unroll
         for (int r = 0; r < kHeld; ++r)
@@ -139,18 +141,18 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ 
 }
 
 template <bool F16, bool GATED, int ROWS>
-cudaError_t run(const RowsParams &p, unsigned blocks, bool wide, cudaStream_t s) {
-    if (wide) return launch_pdl(rows_kernel<F16, GATED, ROWS, true>, dim3(blocks), dim3(kThreads), 0, s, p);
-    return launch_pdl(rows_kernel<F16, GATED, ROWS, false>, dim3(blocks), dim3(kThreads), 0, s, p);
+cudaError_t run(const RowsParams &p, unsigned warps, unsigned blocks, bool wide, cudaStream_t s) {
+    if (wide) return launch_pdl(rows_kernel<F16, GATED, ROWS, true>, dim3(blocks), dim3(32 * warps), 0, s, p);
+    return launch_pdl(rows_kernel<F16, GATED, ROWS, false>, dim3(blocks), dim3(32 * warps), 0, s, p);
 }
 
 template <bool F16, bool GATED>
-cudaError_t run(const RowsParams &p, int rows, unsigned blocks, bool wide, cudaStream_t s) {
+cudaError_t run(const RowsParams &p, int rows, unsigned warps, unsigned blocks, bool wide, cudaStream_t s) {
     switch (rows) {
-        case 1: return run<F16, GATED, 1>(p, blocks, wide, s);
-        case 2: return run<F16, GATED, 2>(p, blocks, wide, s);
-        case 3: return run<F16, GATED, 3>(p, blocks, wide, s);
-        default: return run<F16, GATED, 4>(p, blocks, wide, s);
+        case 1: return run<F16, GATED, 1>(p, warps, blocks, wide, s);
+        case 2: return run<F16, GATED, 2>(p, warps, blocks, wide, s);
+        case 3: return run<F16, GATED, 3>(p, warps, blocks, wide, s);
+        default: return run<F16, GATED, 4>(p, warps, blocks, wide, s);
     }
 }
 
@@ -166,14 +168,14 @@ bool wide_operands(const MmJob &j) {
 }  // namespace
 
 // Up to 2 rows; of 3 and 4 only where TMA cannot read the weights as they lie and
-// nn_skinny.cu would have to copy them first.  4096 -> 10240 gated, wide rows: 1 row
-// 27.3 us here (6.1 TB/s), 2 rows 32.3, 4 rows 52.2; nn_skinny.cu 32.9 for 8.
+// nn_skinny.cu would have to copy them first.  4096 -> 2 x 10240 gated, wide
+// rows, bf16: 1 row 25.4 us here, 2 rows 29.0, 4 rows 52; nn_skinny.cu 31 for 3 to 8.
 // Checkpoints are left to the kernels that hold 32 columns of a row together.
 bool few_rows(const MmJob &j) {
     return j.M <= 4 && (j.M <= 2 || !wide_operands(j)) && !j.epi.saved[0].d_scale && !j.epi.saved[1].d_scale;
 }
 
-cudaError_t launch_rows(const MmJob &j, cudaStream_t s) {
+cudaError_t launch_rows(const MmJob &j, int sms, cudaStream_t s) {
     const bool gated = j.kind == kMmGated;
     RowsParams p{};
     p.x = static_cast<const uint16_t *>(j.a[0].p);
@@ -186,14 +188,21 @@ cudaError_t launch_rows(const MmJob &j, cudaStream_t s) {
     p.epi = j.epi;
     p.N = j.N;
     p.K = j.K;
-    // as many warps to a group as have a step of 256 each
-    while (p.split_log2 < 3 && (256 << (p.split_log2 + 1)) <= j.K) ++p.split_log2;
+    // Warps of a group: one for every four steps of 256 (a longer way leaves the end of
+    // the launch uneven), and more down to a step each while an SM has fewer than 16.
+    // One row, bf16: 8192 -> 2 x 8192 with 8 warps 39.6 us, 4 40.6, 2 44.7; 4096 -> 4096
+    // with 4 warps 7.3 us, 8 7.6, 2 8.8; 1024 -> 2 x 4096 with 2 4.7 us, 4 5.0.
     const int out = gated ? kHeld / 2 : kHeld;
-    const int64_t per_block = (int64_t)(kWarps >> p.split_log2) * out;
+    const int64_t groups = ((int64_t)j.N + out - 1) / out;
+    while (p.split_log2 < 3 && (1024 << (p.split_log2 + 1)) <= j.K) ++p.split_log2;
+    while ((1 << p.split_log2) < kMostWarps && (256 << (p.split_log2 + 1)) <= j.K && (groups << p.split_log2) < (int64_t)16 * sms)
+        ++p.split_log2;
+    const unsigned warps = std::max(4u, 1u << p.split_log2);
+    const int64_t per_block = (int64_t)(warps >> p.split_log2) * out;
     const unsigned blocks = (unsigned)((j.N + per_block - 1) / per_block);
     if (j.type == EMTK_TYPE_F16)
-        return gated ? run<true, true>(p, j.M, blocks, wide, s) : run<true, false>(p, j.M, blocks, wide, s);
-    return gated ? run<false, true>(p, j.M, blocks, wide, s) : run<false, false>(p, j.M, blocks, wide, s);
+        return gated ? run<true, true>(p, j.M, warps, blocks, wide, s) : run<true, false>(p, j.M, warps, blocks, wide, s);
+    return gated ? run<false, true>(p, j.M, warps, blocks, wide, s) : run<false, false>(p, j.M, warps, blocks, wide, s);
 }
 
 }  // namespace emtk
