@@ -127,7 +127,7 @@ emtk_status forward(emtk_nn *nn, MmJob &j, const emtk_matrix &x, const emtk_matr
     j.a[0] = rows_of(x);
     for (int i = 0; i < nw; ++i) j.b[i] = rows_of(w[i]);
     if (few_rows(j)) return status_of(launch_rows(j, nn->sm_count, s));
-    const bool thin = skinny(j);
+    const bool thin = skinny(j, nn->sm_count);
     const MmPlan plan = thin ? MmPlan{} : plan_mm(&j, 1, nn->sm_count);
     CallSpace ws{nn};
     Staging stage{ws};

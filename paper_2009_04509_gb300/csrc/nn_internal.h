@@ -108,8 +108,8 @@ cudaError_t init_mm_kernels();  // once per device
 // The forward pass of 1 to 4 rows (nn_rows.cu), operands anywhere.
 bool few_rows(const MmJob &job);
 cudaError_t launch_rows(const MmJob &job, int sms, cudaStream_t s);
-// The forward pass of up to 64 rows (nn_skinny.cu).
-bool skinny(const MmJob &job);
+// The forward pass of up to 128 rows (nn_skinny.cu).
+bool skinny(const MmJob &job, int sms);
 cudaError_t launch_skinny(const MmJob &job, const emtk_nn *nn, cudaStream_t s);
 cudaError_t init_skinny_kernels();  // once per device
 

@@ -166,11 +166,12 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
     constexpr int kPiece = 16 / sizeof(T), kCols = ROW / sizeof(T), kLanes = ROW / 16, kRows = 32 / kLanes;
     const int nr = (int)min((int64_t)32, rows - r0), nc = (int)min((int64_t)kCols, cols - c0);
     const int r_first = lane / kLanes, piece = lane % kLanes;
-    if (wide && nr == 32 && nc == kCols) {  // a whole block: unconditional 16-byte moves
+    if (wide && nc == kCols) {  // whole rows: 16-byte moves
         T *g = base + (r0 + r_first) * ld + c0 + piece * kPiece;
 #pragma unroll
         for (int it = 0; it < kLanes; ++it, g += kRows * ld) {
             uint8_t *s = stage + staged<ROW>(r_first + it * kRows, piece);
+            if (r_first + it * kRows >= nr) continue;
             if (LOAD)
                 *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
             else

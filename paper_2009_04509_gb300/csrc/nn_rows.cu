@@ -169,7 +169,8 @@ bool wide_operands(const MmJob &j) {
 
 // Up to 2 rows; of 3 and 4 only where TMA cannot read the weights as they lie and
 // nn_skinny.cu would have to copy them first.  4096 -> 2 x 10240 gated, wide
-// rows, bf16: 1 row 25.4 us here, 2 rows 29.0, 4 rows 52; nn_skinny.cu 31 for 3 to 8.
+// rows, bf16: 1 row 25.4 us here, 2 rows 29.0, 4 rows 52; nn_skinny.cu 29.4 for 3 to 8
+// (4096 -> 4096 dense: 7.3, 7.4, 13 and 9.5).
 // Checkpoints are left to the kernels that hold 32 columns of a row together.
 bool few_rows(const MmJob &j) {
     return j.M <= 4 && (j.M <= 2 || !wide_operands(j)) && !j.epi.saved[0].d_scale && !j.epi.saved[1].d_scale;

@@ -1,8 +1,8 @@
-// The layers' forward pass for up to 64 rows, on the tcgen05 tensor cores.
+// The layers' forward pass for up to 128 rows, on the tcgen05 tensor cores.
 //
 // The time is that of reading the weights once.  So the weights take the MMA's
 // 128 rows (of the gated block 64 rows of each projection) and the rows of x its
-// 16, 32 or 64 columns: every byte staged by TMA but x's is a weight, where a
+// 16 to 128 columns: every byte staged by TMA but x's is a weight, where a
 // tile of nn_mm.cu would stage 256 mostly empty rows of x.  Two CTAs of about
 // 105 KB share an SM, so that one's set-up and epilogue run beside the other's
 // stream.  Where the output tiles are fewer than the CTAs that fit, a cluster of
@@ -10,10 +10,12 @@
 // memory, and every CTA adds the cluster's sums for its share of the rows, in
 // rank order, over distributed shared memory; no second kernel, no workspace.
 //
-// HBM bounds it.  4096 -> 2 x 10240 gated, bf16 (168 MB of weights): 31 us for 8 rows,
-// 32 for 16, 38 for 64 (5.4, 5.2 and 4.5 TB/s); 4096 -> 10240 dense: 18 us for 8 rows.
-// With all CTAs starting at the same chunk 16 rows took 56 us.  What is left to the
-// copy's 6.8 TB/s is the ramp and, from 32 rows on, the epilogue.
+// HBM bounds it.  4096 -> 2 x 10240 gated, bf16 (168 MB of weights): 29.4 us for 3 to 8
+// rows, 29.6 for 16, 33 for 64, 39 for 128 (5.7, 5.7, 5.0 and 4.3 TB/s); 4096 -> 4096
+// dense: 9.5 us for 8 rows.  With all CTAs starting at the same chunk 16 rows took 56
+// us, and with a thread finishing one column, its cluster's sums one after another, 64
+// rows took 38.  What is left to the copy's 6.8 TB/s is the ramp and, from 32 rows on,
+// the epilogue and x's tiles.
 #include <algorithm>
 
 #include "emtk_internal.h"
@@ -24,7 +26,7 @@
 namespace emtk {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 256;
 constexpr int kStep = 64;                    // contraction steps of a chunk: 128 bytes
 constexpr int kWeightRows = 128;
 constexpr int kWBytes = kWeightRows * kStep * 2;
@@ -33,13 +35,12 @@ constexpr int kMostParts = 8;                // portable cluster size
 template <int NT>  // columns of the MMA: rows of x
 struct Shape {
     static constexpr int kChunk = kWBytes + NT * kStep * 2;
-    static constexpr int kSlots = NT == 16 ? 6 : NT == 32 ? 5 : 4;
+    static constexpr int kSlots = NT == 16 ? 6 : NT == 32 ? 5 : NT == 64 ? 4 : 3;
     static constexpr int kTmemCols = NT < 32 ? 32 : NT;
     static constexpr int kSmem = 1024 + kSlots * kChunk + 256;
+    static_assert(kSmem <= 113 * 1024, "two CTAs an SM");
+    static_assert(NT * kWeightRows * 4 <= kSlots * kChunk, "the sums take the slots' place");
 };
-static_assert(Shape<16>::kSmem <= 113 * 1024 && Shape<32>::kSmem <= 113 * 1024 && Shape<64>::kSmem <= 113 * 1024,
-              "two CTAs an SM");
-static_assert(64 * kWeightRows * 4 <= 4 * Shape<64>::kChunk, "the sums take the slots' place");
 
 struct SkinnyParams {
     CUtensorMap w[2], x;
@@ -50,10 +51,33 @@ struct SkinnyParams {
     int debug_stall;
 };
 
-__device__ __forceinline__ float load_cluster(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
+}
+// Up to four neighbouring 16-bit elements, one access where the matrix allows.
+__device__ __forceinline__ void store4(void *base, int64_t at, int n, bool wide, uint32_t lo, uint32_t hi) {
+    uint16_t *p = static_cast<uint16_t *>(base) + at;
+    if (wide && n >= 4) {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(lo, hi);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = (uint16_t)((i < 2 ? lo : hi) >> (16 * (i % 2)));
+    }
+}
+__device__ __forceinline__ uint2 load4(const void *base, int64_t at, int n, bool wide) {
+    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+    if (wide && n >= 4) return *reinterpret_cast<const uint2 *>(p);
+    uint32_t x[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) x[i / 2] |= (uint32_t)p[i] << (16 * (i % 2));
+    return make_uint2(x[0], x[1]);
+}
+__device__ __forceinline__ bool wide4(const void *p, int64_t row_bytes, unsigned bytes) {
+    return ((reinterpret_cast<uintptr_t>(p) | (uint64_t)row_bytes) & (bytes - 1)) == 0;
 }
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
     asm volatile(
@@ -181,7 +205,7 @@ __global__ void __launch_bounds__(kThreads) skinny_kernel(const __grid_constant_
     float *const sums = reinterpret_cast<float *>(base);
     const bool ok = warp_wait(bar(kBarAcc), 0u, guard, lane);
     tc_fence_after();
-    if (ok) {
+    if (ok && warp < 4) {
         const uint32_t acc = tmem + ((uint32_t)(32 * warp) << 16);
         float *const mine = sums + 32 * warp + lane;
 #pragma unroll
@@ -196,71 +220,72 @@ __global__ void __launch_bounds__(kThreads) skinny_kernel(const __grid_constant_
     }
     tc_fence_before();
     cluster_sync();
-    // Rows rank, rank + parts, ..: a thread's output column stays its own.
+    // This CTA's rows of x are rank, rank + parts, ..; a thread keeps four columns, and
+    // has the whole cluster's sums of them in flight at once.
+    constexpr int kLanes = kOut / 4, kSums = GATED ? 2 : 1;
     const MmEpilogue &e = p.epi;
-    const int col = threadIdx.x % kOut, first = rank + p.parts * (threadIdx.x / kOut);
-    const int n = n0 + col;
-    const bool in = n < p.N;
-    float bias[GATED ? 2 : 1] = {};
+    const int col = threadIdx.x % kLanes * 4, n = n0 + col, valid = min(4, p.N - n);
+    const bool out_wide = wide4(e.out.d, 2 * e.out.ld, 8), res_wide = wide4(e.residual.d, 2 * e.residual.ld, 8);
+    float bias[kSums][4] = {};
 #pragma unroll
-    for (int h = 0; h < (GATED ? 2 : 1); ++h)
-        if (e.bias[h] && in)
-            bias[h] = e.bias_f32 ? __ldg(static_cast<const float *>(e.bias[h]) + n)
-                                 : from16<F16>(__ldg(static_cast<const uint16_t *>(e.bias[h]) + n));
-    // four rows at a time: their remote loads and stores are independent
-    constexpr int kRows = 4, kSums = GATED ? 2 : 1;
-    const int step = p.parts * (kThreads / kOut);
-    for (int t0 = first; t0 < p.M; t0 += kRows * step) {
-        float z[kRows][kSums], y[kRows];
-        uint16_t res[kRows];
+    for (int h = 0; h < kSums; ++h)
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int t = min(t0 + i * step, p.M - 1);
-            res[i] = !GATED && e.residual.d && in
-                         ? static_cast<const uint16_t *>(e.residual.d)[t * e.residual.ld + n] : (uint16_t)0;
-        }
-        for (int r = 0; r < p.parts; ++r) {
-            const uint32_t from = cluster_addr(smem_u32(sums + col), r);
+        for (int i = 0; i < 4; ++i)
+            if (e.bias[h] && i < valid)
+                bias[h][i] = e.bias_f32 ? __ldg(static_cast<const float *>(e.bias[h]) + n + i)
+                                        : from16<F16>(__ldg(static_cast<const uint16_t *>(e.bias[h]) + n + i));
+    const uint32_t from = smem_u32(sums + col);
+    for (int t = rank + p.parts * (threadIdx.x / kLanes); t < p.M; t += p.parts * (kThreads / kLanes)) {
+        uint2 res = make_uint2(0u, 0u);
+        if (!GATED && e.residual.d) res = load4(e.residual.d, t * e.residual.ld + n, valid, res_wide);
+        float z[kSums][4];
 #pragma unroll
-            for (int i = 0; i < kRows; ++i)
+        for (int h = 0; h < kSums; ++h) {
+            float4 part[kMostParts];
 #pragma unroll
-                for (int h = 0; h < kSums; ++h) {
-                    const float v = load_cluster(from + 4 * ((t0 + i * step) % NT * kWeightRows + h * kOut));
-                    z[i][h] = r == 0 ? v : z[i][h] + v;
-                }
+            for (int r = 0; r < kMostParts; ++r)
+                if (r < p.parts) part[r] = load_cluster(cluster_addr(from + 4 * (t * kWeightRows + h * kOut), r));
+            z[h][0] = part[0].x, z[h][1] = part[0].y, z[h][2] = part[0].z, z[h][3] = part[0].w;
+#pragma unroll
+            for (int r = 1; r < kMostParts; ++r)
+                if (r < p.parts) z[h][0] += part[r].x, z[h][1] += part[r].y, z[h][2] += part[r].z, z[h][3] += part[r].w;
         }
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int t = t0 + i * step;
-            if (t >= p.M) break;  // the whole warp
+        for (int h = 0; h < kSums; ++h) {
 #pragma unroll
-            for (int h = 0; h < kSums; ++h) {
-                const float v = z[i][h] += bias[h];
-                const emtk_matrix &m = e.saved[h];
-                if (m.d == nullptr) continue;
-                if (m.d_scale) {  // a warp's lanes are one block of 32 columns
-                    const bool finite = fabsf(v) < __int_as_float(0x7f800000);
-                    const uint32_t top = __reduce_max_sync(0xffffffffu, in && finite ? __float_as_uint(fabsf(v)) : 0u);
-                    const uint32_t b = q8_scale(__uint_as_float(top));
-                    if (in && lane == 0) m.d_scale[t * m.ld_scale + n / kQ8Block] = (uint8_t)b;
-                    if (in)
-                        static_cast<uint8_t *>(m.d)[t * m.ld + n] =
-                            (uint8_t)(finite ? __float_as_uint(fmaf(v, q8_inverse(b), 12582912.f)) : 0x80u);
-                } else if (in) {
-                    static_cast<uint16_t *>(m.d)[t * m.ld + n] = (uint16_t)to16<F16>(v);
+            for (int i = 0; i < 4; ++i) z[h][i] = i < valid ? z[h][i] + bias[h][i] : 0.f;
+            const emtk_matrix &m = e.saved[h];
+            if (m.d == nullptr) continue;
+            if (m.d_scale) {  // eight neighbouring threads are a block of 32 columns
+                const uint32_t group = 0xffu << (lane & 24);
+                bool all_finite;
+                float top = finite_top(z[h], all_finite);
+#pragma unroll
+                for (int d = 1; d < 8; d <<= 1) top = fmaxf(top, __shfl_xor_sync(group, top, d));
+                const uint32_t b = q8_scale(top);
+                if (valid > 0 && (lane & 7) == 0) m.d_scale[t * m.ld_scale + n / kQ8Block] = (uint8_t)b;
+                const uint32_t codes = q8_codes4(z[h], q8_inverse(b), all_finite);
+                uint8_t *const to = static_cast<uint8_t *>(m.d) + t * m.ld + n;
+                if (valid == 4 && wide4(m.d, m.ld, 4)) {
+                    *reinterpret_cast<uint32_t *>(to) = codes;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < valid) to[i] = (uint8_t)(codes >> (8 * i));
                 }
+            } else {
+                store4(m.d, t * m.ld + n, valid, wide4(m.d, 2 * m.ld, 8), pack16<F16>(z[h][0], z[h][1]),
+                       pack16<F16>(z[h][2], z[h][3]));
             }
         }
+        apply_act(e.act, z[0]);
+        const uint32_t x[2] = {res.x, res.y};
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) y[i] = z[i][0];
-        apply_act(e.act, y);
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int t = t0 + i * step;
-            if (GATED) y[i] *= z[i][kSums - 1];
-            if (!GATED && e.residual.d) y[i] += from16<F16>(res[i]);
-            if (in && t < p.M) static_cast<uint16_t *>(e.out.d)[t * e.out.ld + n] = (uint16_t)to16<F16>(y[i]);
+        for (int i = 0; i < 4; ++i) {
+            if (GATED) z[0][i] *= z[kSums - 1][i];
+            if (!GATED && e.residual.d) z[0][i] += from16<F16>((x[i / 2] >> (16 * (i % 2))) & 0xffffu);
         }
+        store4(e.out.d, t * e.out.ld + n, valid, out_wide, pack16<F16>(z[0][0], z[0][1]), pack16<F16>(z[0][2], z[0][3]));
     }
     cluster_sync();  // the cluster's sums have been read
     tc_fence_after();
@@ -290,7 +315,8 @@ template <bool F16, bool GATED>
 cudaError_t run(const SkinnyParams &p, int nt, unsigned ctas, cudaStream_t s) {
     if (nt == 16) return run<F16, GATED, 16>(p, ctas, s);
     if (nt == 32) return run<F16, GATED, 32>(p, ctas, s);
-    return run<F16, GATED, 64>(p, ctas, s);
+    if (nt == 64) return run<F16, GATED, 64>(p, ctas, s);
+    return run<F16, GATED, 128>(p, ctas, s);
 }
 
 int tiles_of(const MmJob &j) {
@@ -298,13 +324,28 @@ int tiles_of(const MmJob &j) {
     return (int)(((int64_t)j.N + out - 1) / out);
 }
 int chunks_of(const MmJob &j) { return (int)(((int64_t)j.K + kStep - 1) / kStep); }
+// Two CTAs an SM, each with at least 4 chunks.
+int parts_of(const MmJob &j, int sms) {
+    return std::max(1, std::min({kMostParts, 2 * sms / std::max(1, tiles_of(j)), chunks_of(j) / 4}));
+}
 
 }  // namespace
 
-// A cluster splits the contraction 8 ways at most, so a few columns with a very
-// long contraction are left to nn_mm.cu, which splits it over all SMs.
-bool skinny(const MmJob &j) {
-    return j.M <= 64 && j.K > 0 && (tiles_of(j) * kMostParts >= 76 || chunks_of(j) <= 512);
+// Up to 128 rows, where this is the faster kernel.  A cluster splits the contraction 8
+// ways at most, so a few columns with a long contraction are left to nn_mm.cu, which
+// splits it over all SMs (16384 -> 128, 8 rows, bf16: 9.1 us here, 7.5 there; -> 1024: 11.0
+// and 14.1).  From 25 rows on the epilogue counts against a short contraction (256 ->
+// 8192, 48 rows: 6.1 and 5.4; 1024 -> 4096: 6.5 and 7.8) and a second round of CTAs
+// shows (1024 -> 40960, 48 rows: 26.0 and 23.0); beyond 64 it takes a longer one still
+// (1024 -> 4096, 96 rows: 8.2 and 7.5; 4096 -> 4096: 12.8 and 15.0).
+bool skinny(const MmJob &j, int sms) {
+    if (j.M > 128 || j.K == 0) return false;
+    const int tiles = tiles_of(j), chunks = chunks_of(j), parts = parts_of(j, sms);
+    const bool short_way = (chunks + parts - 1) / parts <= 16, one_round = tiles <= 2 * sms;
+    const int64_t ctas = (int64_t)tiles * parts;
+    if (j.M <= 24) return short_way || 4 * ctas >= sms;
+    if (j.M <= 64) return chunks >= 8 && one_round && (short_way || 4 * ctas >= sms);
+    return chunks >= 32 && one_round && (short_way || 2 * ctas >= sms);
 }
 
 cudaError_t init_skinny_kernels() {
@@ -321,6 +362,7 @@ cudaError_t init_skinny_kernels() {
     EMTK_SKINNY_ATTRS(16)
     EMTK_SKINNY_ATTRS(32)
     EMTK_SKINNY_ATTRS(64)
+    EMTK_SKINNY_ATTRS(128)
 #undef EMTK_SKINNY_ATTRS
 #undef EMTK_SKINNY_ATTR
     return e;
@@ -328,7 +370,7 @@ cudaError_t init_skinny_kernels() {
 
 cudaError_t launch_skinny(const MmJob &j, const emtk_nn *nn, cudaStream_t s) {
     const bool gated = j.kind == kMmGated;
-    const int nt = j.M <= 16 ? 16 : j.M <= 32 ? 32 : 64, tiles = tiles_of(j);
+    const int nt = j.M <= 16 ? 16 : j.M <= 32 ? 32 : j.M <= 64 ? 64 : 128, tiles = tiles_of(j);
     SkinnyParams p;
     for (int i = 0; i < (gated ? 2 : 1); ++i)
         if (!encode_operand(nn, &p.w[i], j.b[i], j.N, j.K, gated ? 64 : 128)) return cudaErrorInvalidValue;
@@ -338,8 +380,7 @@ cudaError_t launch_skinny(const MmJob &j, const emtk_nn *nn, cudaStream_t s) {
     p.N = j.N;
     p.K = j.K;
     p.chunks = chunks_of(j);
-    // two CTAs an SM, each with at least 4 chunks
-    p.parts = std::max(1, std::min({kMostParts, 2 * nn->sm_count / tiles, p.chunks / 4}));
+    p.parts = parts_of(j, nn->sm_count);
     p.chunks_per_part = (p.chunks + p.parts - 1) / p.parts;
     p.parts = (p.chunks + p.chunks_per_part - 1) / p.chunks_per_part;
     p.status = nn->status;

@@ -145,7 +145,7 @@ def q8_values(q, cols):
 SHAPES = [(1, 1, 1), (1, 4096, 72), (2, 7, 5), (3, 777, 130), (5, 64, 512), (8, 2048, 96), (9, 200, 48), (16, 1000, 33),
           (17, 129, 65), (33, 72, 257), (64, 512, 128), (100, 2304, 40), (127, 2305, 131), (128, 128, 128),
           (129, 65, 257), (255, 64, 31), (300, 1000, 333), (513, 40, 1030), (1693, 48, 640), (20, 30011, 24),
-          (256, 9292, 128), (2500, 700, 3000), (5000, 1032, 1100)]
+          (256, 9292, 128), (24, 600, 1000), (47, 1000, 1200), (70, 2500, 700), (120, 2304, 515), (128, 2112, 4100), (2500, 700, 3000), (5000, 1032, 1100)]
 
 
 def dense_inputs(m, k, n, dtype, pad, shift, seed, bias, residual):
