@@ -279,7 +279,11 @@ __device__ __forceinline__ void store32(float *base, int64_t ld, bool wide, cons
     }
 }
 
-// A row's 32 columns as one checkpoint block; a lane writes its row's sector.
+// A row's 32 columns as one checkpoint block.  Rows of codes on 16 bytes: a lane writes
+// its row's sector.  Others go through the staged rows so that a store of the warp falls
+// into few sectors: 8 lanes to a row by words, or all 32 by bytes.  (By bytes from its own
+// row's lane, 32 sectors a store, 1981 x 648 -> 2 x 3032 took 138 us where this takes
+// QQQ.)
 __device__ __forceinline__ void store_q8(const emtk_matrix &m, const Rows &w, int64_t c0, int64_t cols,
                                          const float (&v)[32]) {
     const int nc = (int)min((int64_t)32, cols - c0);
@@ -290,20 +294,35 @@ __device__ __forceinline__ void store_q8(const emtk_matrix &m, const Rows &w, in
     const uint32_t b = q8_scale(finite_top(x, all_finite));
     const float inverse = q8_inverse(b);
     const int64_t r = w.r0 + w.lane;
-    if (r >= w.rows) return;
-    m.d_scale[r * m.ld_scale + c0 / kQ8Block] = (uint8_t)b;
-    uint8_t *p = static_cast<uint8_t *>(m.d) + r * m.ld + c0;
+    if (r < w.rows) m.d_scale[r * m.ld_scale + c0 / kQ8Block] = (uint8_t)b;
+    uint8_t *const base = static_cast<uint8_t *>(m.d) + w.r0 * m.ld + c0;
     uint32_t q[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[i] = q8_codes4(x + 4 * i, inverse, all_finite);
-    if (nc == 32 && wide_rows(m.d, m.ld, 1)) {
-        reinterpret_cast<uint4 *>(p)[0] = make_uint4(q[0], q[1], q[2], q[3]);
-        reinterpret_cast<uint4 *>(p)[1] = make_uint4(q[4], q[5], q[6], q[7]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < nc) p[i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
+    const uint32_t low = (uint32_t)(reinterpret_cast<uintptr_t>(m.d) | (uintptr_t)m.ld);
+    if (nc == 32 && (low & 15u) == 0) {
+        uint4 *p = reinterpret_cast<uint4 *>(base + w.lane * m.ld);
+        if (r >= w.rows) return;
+        p[0] = make_uint4(q[0], q[1], q[2], q[3]);
+        p[1] = make_uint4(q[4], q[5], q[6], q[7]);
+        return;
     }
+    constexpr int kRow = 36;  // bytes of a staged row: a word off 32, so that lanes meet in no bank
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t *>(w.stage + w.lane * kRow + 4 * i) = q[i];
+    __syncwarp();
+    const int nr = (int)min((int64_t)32, w.rows - w.r0);
+    if (nc % 4 == 0 && (low & 3u) == 0) {
+        const int first = w.lane / 8, c = w.lane % 8 * 4;
+#pragma unroll
+        for (int i = first; i < 32; i += 4)
+            if (i < nr && c < nc)
+                *reinterpret_cast<uint32_t *>(base + i * m.ld + c) = *reinterpret_cast<const uint32_t *>(w.stage + i * kRow + c);
+    } else if (w.lane < nc) {
+#pragma unroll 8
+        for (int i = 0; i < nr; ++i) base[i * m.ld + w.lane] = w.stage[i * kRow + w.lane];
+    }
+    __syncwarp();
 }
 
 template <bool F16>
@@ -633,6 +652,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     if (warp == 2) tmem_free_pair(tmem, S::kTmemCols);
 }
 
+// Eight columns of a row, of which the first n exist.
+template <bool F16>
+__device__ __forceinline__ void store8(uint16_t *p, int n, const float (&v)[8]) {
+    if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]),
+                                                   pack16<F16>(v[6], v[7]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) p[j] = (uint16_t)to16<F16>(v[j]);
+    }
+}
+
 // Adds the parts' sums and applies the epilogue: 2^lanes_log2 neighbouring
 // threads take 8 columns of a row, each every so-manieth part, and join their
 // sums in a fixed tree; four such groups hold a checkpoint block (8 threads each
@@ -696,11 +728,15 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEp
             if (!writes) continue;
             if (c % kQ8Block == 0) m.d_scale[r * m.ld_scale + c / kQ8Block] = (uint8_t)b;
             const uint32_t q[2] = {q8_codes4(x, q8_inverse(b), all_finite), q8_codes4(x + 4, q8_inverse(b), all_finite)};
-            for (int j = 0; j < 8; ++j)
-                if (c + j < N) static_cast<uint8_t *>(m.d)[r * m.ld + c + j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+            uint8_t *const codes = static_cast<uint8_t *>(m.d) + r * m.ld + c;
+            if (c + 8 <= N && (reinterpret_cast<uintptr_t>(codes) & 7u) == 0) {
+                *reinterpret_cast<uint2 *>(codes) = make_uint2(q[0], q[1]);
+            } else {
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < N) codes[j] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+            }
         } else if (writes) {
-            for (int j = 0; j < 8; ++j)
-                if (c + j < N) static_cast<uint16_t *>(m.d)[r * m.ld + c + j] = (uint16_t)to16<F16>(v[h][j]);
+            store8<F16>(static_cast<uint16_t *>(m.d) + r * m.ld + c, N - c, v[h]);
         }
     }
     if (!writes) return;
@@ -717,13 +753,8 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEp
         float *o = static_cast<float *>(e.out.d) + r * e.out.ld + c;
         for (int j = 0; j < 8; ++j)
             if (c + j < N) o[j] = v[0][j];
-    } else if (c + 8 <= N && wide_rows(e.out.d, e.out.ld, 2)) {
-        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(e.out.d) + r * e.out.ld + c) =
-            make_uint4(pack16<F16>(v[0][0], v[0][1]), pack16<F16>(v[0][2], v[0][3]), pack16<F16>(v[0][4], v[0][5]),
-                       pack16<F16>(v[0][6], v[0][7]));
     } else {
-        for (int j = 0; j < 8; ++j)
-            if (c + j < N) static_cast<uint16_t *>(e.out.d)[r * e.out.ld + c + j] = (uint16_t)to16<F16>(v[0][j]);
+        store8<F16>(static_cast<uint16_t *>(e.out.d) + r * e.out.ld + c, N - c, v[0]);
     }
 }
 
