@@ -157,12 +157,12 @@ __device__ __forceinline__ uint32_t staged(int r, int c) {
     return (uint32_t)(r * ROW + (ROW == 128 ? (c ^ r) & 7 : (c ^ (r >> 1)) & 3) * 16);
 }
 
-// Rows r0 .. r0 + 31 (below `rows`), columns c0 .. c0 + ROW / sizeof(T) - 1 (below
-// `cols`) of a matrix, between memory and the warp's staged rows; ROW / 16 lanes
-// move a row where 16-byte pieces fit, a row at a time where they do not.
-template <typename T, bool LOAD, int ROW>
-__device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int64_t rows, int64_t c0, int64_t cols,
-                                           bool wide, uint8_t *stage, int lane) {
+// Stores rows r0 .. r0 + 31 (below `rows`), columns c0 .. c0 + ROW / sizeof(T) - 1 (below
+// `cols`) of a matrix from the warp's staged rows; ROW / 16 lanes move a row where
+// 16-byte pieces fit, a row at a time where they do not.
+template <typename T, int ROW>
+__device__ __forceinline__ void store_block(T *base, int64_t ld, int64_t r0, int64_t rows, int64_t c0, int64_t cols,
+                                            bool wide, const uint8_t *stage, int lane) {
     constexpr int kPiece = 16 / sizeof(T), kCols = ROW / sizeof(T), kLanes = ROW / 16, kRows = 32 / kLanes;
     const int nr = (int)min((int64_t)32, rows - r0), nc = (int)min((int64_t)kCols, cols - c0);
     const int r_first = lane / kLanes, piece = lane % kLanes;
@@ -170,12 +170,8 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
         T *g = base + (r0 + r_first) * ld + c0 + piece * kPiece;
 #pragma unroll
         for (int it = 0; it < kLanes; ++it, g += kRows * ld) {
-            uint8_t *s = stage + staged<ROW>(r_first + it * kRows, piece);
             if (r_first + it * kRows >= nr) continue;
-            if (LOAD)
-                *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
-            else
-                *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(s);
+            *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(stage + staged<ROW>(r_first + it * kRows, piece));
         }
     } else if (wide) {
         const int c = piece * kPiece;
@@ -184,19 +180,11 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
             const int r = it * kRows + r_first;
             if (r >= nr || c >= nc) continue;
             T *g = base + (r0 + r) * ld + c0 + c;
-            uint8_t *s = stage + staged<ROW>(r, piece);
+            const uint8_t *s = stage + staged<ROW>(r, piece);
             if (c + kPiece <= nc) {
-                if (LOAD)
-                    *reinterpret_cast<uint4 *>(s) = *reinterpret_cast<const uint4 *>(g);
-                else
-                    *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(s);
+                *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(s);
             } else {
-                for (int i = 0; c + i < nc; ++i) {
-                    if (LOAD)
-                        reinterpret_cast<T *>(s)[i] = g[i];
-                    else
-                        g[i] = reinterpret_cast<const T *>(s)[i];
-                }
+                for (int i = 0; c + i < nc; ++i) g[i] = reinterpret_cast<const T *>(s)[i];
             }
         }
     } else {
@@ -205,19 +193,14 @@ __device__ __forceinline__ void move_block(T *base, int64_t ld, int64_t r0, int6
             if (c >= nc) continue;
             T *g = base + r0 * ld + c0 + c;
             const int at = c * (int)sizeof(T) / 16, in = c * (int)sizeof(T) % 16;
-            for (int r = 0; r < nr; r += 8, g += 8 * ld) {  // eight rows' elements in flight
+            for (int r = 0; r < nr; r += 8, g += 8 * ld) {
                 T x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (r + i < nr) x[i] = LOAD ? g[i * ld] : *reinterpret_cast<const T *>(stage + staged<ROW>(r + i, at) + in);
+                    if (r + i < nr) x[i] = *reinterpret_cast<const T *>(stage + staged<ROW>(r + i, at) + in);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (r + i < nr) {
-                        if (LOAD)
-                            *reinterpret_cast<T *>(stage + staged<ROW>(r + i, at) + in) = x[i];
-                        else
-                            g[i * ld] = x[i];
-                    }
+                    if (r + i < nr) g[i * ld] = x[i];
             }
         }
     }
@@ -257,7 +240,7 @@ __device__ __forceinline__ void store16(void *base, int64_t ld, bool wide, const
             make_uint4(pack16<F16>(v[8 * i], v[8 * i + 1]), pack16<F16>(v[8 * i + 2], v[8 * i + 3]),
                        pack16<F16>(v[8 * i + 4], v[8 * i + 5]), pack16<F16>(v[8 * i + 6], v[8 * i + 7]));
     __syncwarp();
-    move_block<uint16_t, false, 2 * N>(static_cast<uint16_t *>(base), ld, w.r0, w.rows, c0, cols, wide, w.stage, w.lane);
+    store_block<uint16_t, 2 * N>(static_cast<uint16_t *>(base), ld, w.r0, w.rows, c0, cols, wide, w.stage, w.lane);
     __syncwarp();
 }
 
@@ -274,7 +257,7 @@ __device__ __forceinline__ void store32(float *base, int64_t ld, bool wide, cons
         }
         __syncwarp();
         if (c0 + N / 2 * half < cols)
-            move_block<float, false, 2 * N>(base, ld, w.r0, w.rows, c0 + N / 2 * half, cols, wide, w.stage, w.lane);
+            store_block<float, 2 * N>(base, ld, w.r0, w.rows, c0 + N / 2 * half, cols, wide, w.stage, w.lane);
         __syncwarp();
     }
 }
@@ -283,7 +266,7 @@ __device__ __forceinline__ void store32(float *base, int64_t ld, bool wide, cons
 // its row's sector.  Others go through the staged rows so that a store of the warp falls
 // into few sectors: 8 lanes to a row by words, or all 32 by bytes.  (By bytes from its own
 // row's lane, 32 sectors a store, 1981 x 648 -> 2 x 3032 took 138 us where this takes
-// QQQ.)
+// 30.)
 __device__ __forceinline__ void store_q8(const emtk_matrix &m, const Rows &w, int64_t c0, int64_t cols,
                                          const float (&v)[32]) {
     const int nc = (int)min((int64_t)32, cols - c0);
@@ -363,22 +346,43 @@ __device__ __forceinline__ void finish_plain(const Rows &w, int64_t c0, int64_t 
         store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, v);
 }
 
-// The residual's block into the warp's staged rows.
-__device__ __forceinline__ void stage_residual(const Rows &w, int64_t c0, int64_t cols) {
-    move_block<uint16_t, true, 64>(static_cast<uint16_t *>(w.residual), w.residual_ld, w.r0, w.rows, c0, cols,
-                                   w.residual_wide, w.stage, w.lane);
-    __syncwarp();
+// The residual's block on its way into the warp's staged rows: whole rows of 16-byte
+// pieces asynchronously, without registers that the wait would hold, others by elements.
+__device__ __forceinline__ void fetch_residual(const Rows &w, int64_t c0, int64_t cols) {
+    const int nr = (int)min((int64_t)32, w.rows - w.r0), nc = (int)min((int64_t)32, cols - c0);
+    const uint16_t *const base = static_cast<const uint16_t *>(w.residual) + w.r0 * w.residual_ld + c0;
+    if (w.residual_wide && nc == 32) {
+        const int first = w.lane / 4, piece = w.lane % 4;
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+            if (first + 8 * it < nr)
+                copy_async_16(smem_u32(w.stage + staged<64>(first + 8 * it, piece)),
+                              base + (first + 8 * it) * w.residual_ld + 8 * piece);
+    } else if (w.lane < nc) {
+        const uint16_t *g = base + w.lane;
+        for (int r = 0; r < nr; r += 8, g += 8 * w.residual_ld) {  // eight rows' elements in flight
+            uint16_t x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r + i < nr) x[i] = g[i * w.residual_ld];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r + i < nr) *reinterpret_cast<uint16_t *>(w.stage + staged<64>(r + i, w.lane / 8) + w.lane % 8 * 2) = x[i];
+        }
+    }
 }
 
 // Sums of a dense tile's 32 columns (z without its bias, which is in `bias`).
 template <bool F16>
 __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
-                                             const float *bias, bool staged_residual, float (&v)[32]) {
+                                             const float *bias, bool fetched, float (&v)[32]) {
     if (w.has_bias) add_bias(bias, v);
     if (w.has_saved) store_saved<F16>(e.saved[0], w, c0, cols, v);
     apply_act(w.act, v);
     if (w.residual) {
-        if (!staged_residual) stage_residual(w, c0, cols);
+        if (!fetched) fetch_residual(w, c0, cols);
+        copy_async_wait();
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint4 q = *reinterpret_cast<const uint4 *>(w.stage + staged<64>(w.lane, i));
@@ -599,10 +603,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (GATED) bias[kMine + j] = bias_at<F16>(job.epi, 1, n0 + j, N);
                 }
             }
-            // the first block's residual comes while the tile is summed (a z to be kept needs
-            // the staged rows first)
-            const bool early = KIND == kDense && partial == nullptr && w.residual && !w.has_saved && w.r0 < w.rows && n0 < N;
-            if (early) stage_residual(w, n0, N);
+            // the residual of a block comes while the one before is finished, the first one's
+            // while the tile is summed (a z to be kept needs the staged rows first)
+            const bool early = KIND == kDense && partial == nullptr && w.residual && !w.has_saved && w.r0 < w.rows;
+            if (early && n0 < N) fetch_residual(w, n0, N);
             if (!warp_wait(bar(kBarAccFull + ab), (uint32_t)(tile / 2) & 1u, guard, lane)) break;
             tc_fence_after();
             const uint32_t acc = tmem + (uint32_t)(ab * TN) + ((uint32_t)(32 * q) << 16);
@@ -640,7 +644,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 } else if constexpr (GATED) {
                     finish_gated<F16>(job.epi, w, c0, N, bias + j, bias + kMine + j, v, x);
                 } else {
-                    finish_dense<F16>(job.epi, w, c0, N, bias + j, j == 0 && early, v);
+                    finish_dense<F16>(job.epi, w, c0, N, bias + j, early, v);
+                    if (early && j + E::kBlock < kMine && c0 + E::kBlock < N) fetch_residual(w, c0 + E::kBlock, N);
                 }
             }
         }

@@ -455,6 +455,7 @@ struct PackArgs {
     int64_t q_ld, ld_scale;
     int m, k;
     Walk walk;
+    int lanes_log2;  // of pack8_any_kernel
 };
 
 // The largest magnitude is found among the 16-bit patterns, whose order is the
@@ -514,16 +515,39 @@ __global__ void __launch_bounds__(kThreads, kBlocks) pack8_kernel(const __grid_c
     }
 }
 
-// Any alignment.
+// Eight bytes a lane, neighbours in a row of n bytes at p, whatever its alignment: each
+// lane stores the 8 aligned bytes that start in its own, the row's ends go by bytes.
+// Groups of `lanes` lanes hold a row each and call this together.
+__device__ __forceinline__ void store_codes(uint8_t *p, int n, const uint32_t (&w)[2], int lanes, int lane) {
+    const int head = (int)(-reinterpret_cast<uintptr_t>(p) & 7u);
+    const uint64_t own = w[0] | (uint64_t)w[1] << 32;
+    const uint64_t next = __shfl_down_sync(0xffffffffu, own, 1, lanes);
+    if (8 * lane + head + 8 <= n) {
+        const uint64_t x = head ? (own >> (8 * head)) | (next << (64 - 8 * head)) : own;
+        *reinterpret_cast<uint2 *>(p + 8 * lane + head) = make_uint2((uint32_t)x, (uint32_t)(x >> 32));
+    }
+    const int tail = head + max(n - head, 0) / 8 * 8;
+    for (int e0 = 0; e0 < 16; e0 += lanes) {  // every lane of the warp goes around as often: they exchange
+        const int e = e0 + lane;
+        const int c = e < 8 ? e : tail + e - 8;
+        const uint64_t x = __shfl_sync(0xffffffffu, own, (c >> 3) & (lanes - 1), lanes);
+        if (e < 16 && c < (e < 8 ? min(head, n) : n)) p[c] = (uint8_t)(x >> (8 * (c & 7)));
+    }
+}
+
+// Any alignment: 2^lanes_log2 lanes (4 .. 32, the fewest that cover narrow rows) take a
+// piece of a row.
 template <bool F16>
-__global__ void __launch_bounds__(kThreads) pack8_any_kernel(const __grid_constant__ PackArgs a) {
-    const int lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(kThreads, kBlocks) pack8_any_kernel(const __grid_constant__ PackArgs a) {
+    const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
+    Item it(a.walk, ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> a.lanes_log2);
     pdl_trigger();
     pdl_wait();
-    for (Item it(a.walk, (int64_t)blockIdx.x * kWarps + threadIdx.x / 32); it.r < a.m; it.next(a.walk)) {
-        const int64_t c = (int64_t)it.piece * kWarpCols + lane * kVec;
+    for (; __any_sync(0xffffffffu, it.r < a.m); it.next(a.walk)) {
+        const int64_t first = (int64_t)it.piece * (kVec * lanes), c = first + lane * kVec;
+        const bool in = it.r < a.m && c < a.k;
         float v[kVec] = {};
-        if (c < a.k) {
+        if (in) {
             AnyPiece<false> piece;
             piece.load(a.x, it.r, c, a.m, a.k);
             piece.template values<F16>(v);
@@ -532,13 +556,10 @@ __global__ void __launch_bounds__(kThreads) pack8_any_kernel(const __grid_consta
         float top = finite_top(v, all_finite);
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        if (c >= a.k) continue;
         const uint32_t b = q8_scale(top);
-        if ((lane & 3) == 0) a.scale[it.r * a.ld_scale + c / kQ8Block] = (uint8_t)b;
+        if (in && (lane & 3) == 0) a.scale[it.r * a.ld_scale + c / kQ8Block] = (uint8_t)b;
         const uint32_t w[2] = {q8_codes4(v, q8_inverse(b), all_finite), q8_codes4(v + 4, q8_inverse(b), all_finite)};
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (c + i < a.k) a.q[it.r * a.q_ld + c + i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+        store_codes(a.q + it.r * a.q_ld + first, it.r < a.m ? (int)min(a.k - first, (int64_t)kVec * lanes) : 0, w, lanes, lane);
     }
 }
 
@@ -547,7 +568,7 @@ struct CopyArgs {
         Source from;
         uint16_t *to;
         int64_t to_ld;
-        int rows, cols, wide, to_wide;
+        int rows, cols, wide, odd;  // odd: the target's rows are not on 16 bytes
         Walk walk;
     } job[kMaxCopies];
 };
@@ -601,7 +622,47 @@ __device__ __forceinline__ void copy_any(const CopyArgs::One &j, Item it) {
             w[i].template values<F16>(v);
 #pragma unroll
             for (int t = 0; t < kVec; ++t) v[t] = Q8 ? q8_operand<F16>(v[t]) : v[t];
-            store_any<F16>(j.to + r[i] * j.to_ld, c[i], j.cols, j.to_wide != 0, v);
+            store_any<F16>(j.to + r[i] * j.to_ld, c[i], j.cols, true, v);
+        }
+    }
+}
+
+// A checkpoint's values into rows on any element: a thread takes the 8 columns whose
+// values lie on 16 bytes there (8 piece - offset of the row ..), so that its store is one
+// and only the rows' ends go by elements.  Two blocks of 32 columns may meet in them.
+template <bool F16>
+__device__ __forceinline__ void unpack_odd(const CopyArgs::One &j, Item it) {
+    for (; it.r < j.rows; it.next(j.walk)) {
+        uint16_t *const to = j.to + it.r * j.to_ld;
+        const int64_t c = (int64_t)it.piece * kVec - (int64_t)((reinterpret_cast<uintptr_t>(to) >> 1) & 7u);
+        const int lo = (int)max((int64_t)0, -c), hi = (int)min((int64_t)kVec, j.cols - c);
+        if (lo >= hi) continue;
+        const uint8_t *const p = j.from.p + it.r * j.from.row_bytes + c, *const s = j.from.scale + it.r * j.from.ld_scale;
+        const bool whole = lo == 0 && hi == kVec;
+        const int left = kQ8Block - (int)((c + lo) % kQ8Block) + lo;  // columns before the second block
+        const float step0 = q8_step(__ldg(s + (c + lo) / kQ8Block)), step1 = q8_step(__ldg(s + (c + hi - 1) / kQ8Block));
+        uint64_t w = 0;
+        if (whole && it.r > 0 && it.r < j.rows - 1) {  // two aligned words, both within the matrix
+            const int shift = 8 * (int)(reinterpret_cast<uintptr_t>(p) & 7u);
+            const uint64_t *const at = reinterpret_cast<const uint64_t *>(p - shift / 8);
+            const uint64_t x = __ldg(at), y = shift ? __ldg(at + 1) : 0u;
+            w = shift ? (x >> shift) | (y << (64 - shift)) : x;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (i >= lo && i < hi) w |= (uint64_t)__ldg(p + i) << (8 * i);
+        }
+        float v[kVec];
+        q8_values4((uint32_t)w, 1.f, v);
+        q8_values4((uint32_t)(w >> 32), 1.f, v + 4);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = q8_operand<F16>(v[i] * (i < left ? step0 : step1));
+        if (whole) {
+            *reinterpret_cast<uint4 *>(to + c) = pack8x16<F16>(v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (i >= lo && i < hi) to[c + i] = (uint16_t)to16<F16>(v[i]);
         }
     }
 }
@@ -613,6 +674,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) copy16_kernel(const __grid_
     pdl_trigger();
     pdl_wait();
     if (j.wide) return unpack_wide<F16>(j, it);
+    if (j.odd) return unpack_odd<F16>(j, it);
     if (j.from.scale)
         copy_any<F16, true>(j, it);
     else
@@ -679,9 +741,12 @@ cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, con
     const bool wide = k % kPackCols == 0 && wide_matrix(x.d, 2 * x.ld, 16) && wide_matrix(q.d, q.ld, 16);
     const bool f16 = type == EMTK_TYPE_F16;
     // wide: an even number of pieces a row, so that a block's two threads are neighbours
-    const WalkPlan plan = wide ? walk_plan(m, k, kPackCols, kThreads, true) : walk_plan(m, k, kWarpCols, kWarps, false);
+    int lanes_log2 = 5;
+    while (lanes_log2 > 2 && (kVec << (lanes_log2 - 1)) >= k) --lanes_log2;
+    const WalkPlan plan = wide ? walk_plan(m, k, kPackCols, kThreads, true)
+                               : walk_plan(m, k, kVec << lanes_log2, kThreads >> lanes_log2, false);
     const unsigned blocks = plan.blocks(sms);
-    const PackArgs a{source_of(x), static_cast<uint8_t *>(q.d), q.d_scale, q.ld, q.ld_scale, m, k, plan.walk(blocks)};
+    const PackArgs a{source_of(x), static_cast<uint8_t *>(q.d), q.d_scale, q.ld, q.ld_scale, m, k, plan.walk(blocks), lanes_log2};
     return launch_pdl(wide ? (f16 ? pack8_kernel<true> : pack8_kernel<false>)
                            : (f16 ? pack8_any_kernel<true> : pack8_any_kernel<false>),
                       dim3(blocks), dim3(kThreads), 0, s, a);
@@ -695,11 +760,11 @@ cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, 
         const Copy16 &c = copies[i];
         if (c.rows == 0 || c.cols == 0) continue;
         const Source from = source_of(c.from);
-        const bool to_wide = wide_matrix(c.to.d, 2 * c.to.ld, 16);
-        const bool wide = from.scale && to_wide && wide_source(from, c.cols);
-        plans[jobs] = walk_plan(c.rows, c.cols, kVec, kThreads, false);
+        const bool odd = !wide_matrix(c.to.d, 2 * c.to.ld, 16);  // a caller's values: the workspace's rows never are
+        const bool wide = from.scale && !odd && wide_source(from, c.cols);
+        plans[jobs] = walk_plan(c.rows, (int64_t)c.cols + (odd ? kVec - 1 : 0), kVec, kThreads, false);
         blocks = std::max(blocks, plans[jobs].blocks(sms));
-        a.job[jobs++] = {from, static_cast<uint16_t *>(c.to.d), c.to.ld, c.rows, c.cols, wide, to_wide, Walk{}};
+        a.job[jobs++] = {from, static_cast<uint16_t *>(c.to.d), c.to.ld, c.rows, c.cols, wide, odd, Walk{}};
     }
     if (jobs == 0) return cudaSuccess;
     for (unsigned i = 0; i < jobs; ++i) a.job[i].walk = plans[i].walk(blocks);

@@ -1,6 +1,6 @@
 // Inline PTX of the CTA-pair matrix products (nn_mm.cu) beyond tc_ptx.cuh:
 // tcgen05 with cta_group::2, 2-d TMA loads that signal the pair's leader,
-// cluster barriers and remote arrivals, and descriptors of operands that run
+// asynchronous copies, cluster barriers and remote arrivals, and descriptors of operands that run
 // along memory (MN-major).  Each wraps one documented PTX instruction or
 // encoding.
 #pragma once
@@ -33,6 +33,12 @@ __device__ __forceinline__ bool warp_wait_all(uint32_t bar, uint32_t parity, con
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     return warp_wait(bar, parity, g, lane);
 }
+// 16 bytes from global into shared memory without a register in between, and the wait
+// for all that this thread has started.
+__device__ __forceinline__ void copy_async_16(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // The address of another CTA's copy of a shared-memory object.
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
     uint32_t r;
