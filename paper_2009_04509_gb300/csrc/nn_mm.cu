@@ -51,10 +51,17 @@ constexpr int kFirstEpiWarp = 4;
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
 
 // Which epilogue a kernel has: gradients' (nothing but the sums), a dense layer's, a
-// gated block's.  An epilogue warp turns blocks of 32 rows by kBlock columns into
-// output through kStageRow-byte rows of shared memory; the gradients' blocks are
-// twice as wide, which halves the latencies that their stores wait out.
-enum Kind : int { kPlain, kDense, kGated };
+// gated block's, and those that keep z or g and u as well.  Each is a variant of its
+// own: unrolled over a block's columns, the others' code, jumped over, costs as much as
+// the stores, in instruction fetches or spilled registers (bf16, 20000 x 512 -> 2304
+// with the dense layer's code as well: 60 us instead of 41; 8192 x 64 -> 4096 with a
+// residual, with the kept z's: 42 instead of 37).  An epilogue warp turns blocks of 32
+// rows by kBlock columns into output through kStageRow-byte rows of shared memory; the
+// gradients' blocks are twice as wide, which halves the latencies that their stores
+// wait out.
+enum Kind : int { kPlain, kDense, kGated, kDenseKept, kGatedKept };
+constexpr bool is_gated(Kind k) { return k == kGated || k == kGatedKept; }
+constexpr bool keeps(Kind k) { return k == kDenseKept || k == kGatedKept; }
 template <Kind KIND>
 struct Epi {
     static constexpr int kBlock = KIND == kPlain ? 64 : 32;
@@ -146,8 +153,9 @@ __device__ __forceinline__ Unit unit_of(const MmParams &p, const Cursor &at, int
     return r;
 }
 
-__device__ __forceinline__ bool wide_rows(const void *p, int64_t ld, int elem) {
-    return ((reinterpret_cast<uintptr_t>(p) | (uint64_t)(ld * elem)) & 15u) == 0;
+// The rows' alignment: 0 on 16 bytes, a multiple of 4 on words.
+__device__ __forceinline__ uint32_t row_bits(const void *p, int64_t ld, int elem) {
+    return (uint32_t)(reinterpret_cast<uintptr_t>(p) | (uint64_t)(ld * elem)) & 15u;
 }
 
 // 16-byte piece c of staged row r: the pieces are permuted so that neither a lane to
@@ -157,52 +165,50 @@ __device__ __forceinline__ uint32_t staged(int r, int c) {
     return (uint32_t)(r * ROW + (ROW == 128 ? (c ^ r) & 7 : (c ^ (r >> 1)) & 3) * 16);
 }
 
+// nr staged rows of nc elements to `to`, neighbours in memory by neighbouring lanes.
+template <typename T, int ROW>
+__device__ __forceinline__ void store_elements(T *to, int64_t ld, int nr, int nc, const uint8_t *stage, int lane) {
+    constexpr int kCols = ROW / (int)sizeof(T), kAcross = kCols < 32 ? kCols : 32, kDown = 32 / kAcross;
+    const int first = lane / kAcross;
+#pragma unroll
+    for (int c = lane % kAcross; c < kCols; c += kAcross) {
+        if (c >= nc) continue;
+        const int at = c * (int)sizeof(T) / 16, in = c * (int)sizeof(T) % 16;
+        T *g = to + first * ld + c;
+        for (int r = first; r < nr; r += 4 * kDown, g += 4 * kDown * ld) {
+            T x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r + i * kDown < nr) x[i] = *reinterpret_cast<const T *>(stage + staged<ROW>(r + i * kDown, at) + in);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (r + i * kDown < nr) g[i * kDown * ld] = x[i];
+        }
+    }
+}
+
 // Stores rows r0 .. r0 + 31 (below `rows`), columns c0 .. c0 + ROW / sizeof(T) - 1 (below
-// `cols`) of a matrix from the warp's staged rows; ROW / 16 lanes move a row where
-// 16-byte pieces fit, a row at a time where they do not.
+// `cols`) of a matrix from the warp's staged rows: 16-byte pieces, ROW / 16 lanes to a
+// row, where they fit; else words or elements (8192 x 64 -> n, bf16: 15 us at n = 4096,
+// 21 at 4090, 30 at 4095).  low: row_bits of the matrix.
 template <typename T, int ROW>
 __device__ __forceinline__ void store_block(T *base, int64_t ld, int64_t r0, int64_t rows, int64_t c0, int64_t cols,
-                                            bool wide, const uint8_t *stage, int lane) {
+                                            uint32_t low, const uint8_t *stage, int lane) {
     constexpr int kPiece = 16 / sizeof(T), kCols = ROW / sizeof(T), kLanes = ROW / 16, kRows = 32 / kLanes;
     const int nr = (int)min((int64_t)32, rows - r0), nc = (int)min((int64_t)kCols, cols - c0);
-    const int r_first = lane / kLanes, piece = lane % kLanes;
-    if (wide && nc == kCols) {  // whole rows: 16-byte moves
-        T *g = base + (r0 + r_first) * ld + c0 + piece * kPiece;
+    T *const to = base + r0 * ld + c0;
+    if (low == 0 && nc == kCols) {
+        const int r_first = lane / kLanes, piece = lane % kLanes;
+        T *g = to + r_first * ld + piece * kPiece;
 #pragma unroll
         for (int it = 0; it < kLanes; ++it, g += kRows * ld) {
             if (r_first + it * kRows >= nr) continue;
             *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(stage + staged<ROW>(r_first + it * kRows, piece));
         }
-    } else if (wide) {
-        const int c = piece * kPiece;
-#pragma unroll
-        for (int it = 0; it < kLanes; ++it) {
-            const int r = it * kRows + r_first;
-            if (r >= nr || c >= nc) continue;
-            T *g = base + (r0 + r) * ld + c0 + c;
-            const uint8_t *s = stage + staged<ROW>(r, piece);
-            if (c + kPiece <= nc) {
-                *reinterpret_cast<uint4 *>(g) = *reinterpret_cast<const uint4 *>(s);
-            } else {
-                for (int i = 0; c + i < nc; ++i) g[i] = reinterpret_cast<const T *>(s)[i];
-            }
-        }
+    } else if (sizeof(T) == 2 && (low & 3u) == 0 && nc % 2 == 0) {
+        store_elements<uint32_t, ROW>(reinterpret_cast<uint32_t *>(to), ld / 2, nr, nc / 2, stage, lane);
     } else {
-#pragma unroll
-        for (int c = lane; c < kCols; c += 32) {
-            if (c >= nc) continue;
-            T *g = base + r0 * ld + c0 + c;
-            const int at = c * (int)sizeof(T) / 16, in = c * (int)sizeof(T) % 16;
-            for (int r = 0; r < nr; r += 8, g += 8 * ld) {
-                T x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (r + i < nr) x[i] = *reinterpret_cast<const T *>(stage + staged<ROW>(r + i, at) + in);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (r + i < nr) g[i * ld] = x[i];
-            }
-        }
+        store_elements<T, ROW>(to, ld, nr, nc, stage, lane);
     }
 }
 
@@ -213,26 +219,26 @@ struct Rows {
     uint8_t *stage;
     int lane;
     int act;
-    bool has_bias, has_saved, out_f32, out_wide, residual_wide;
+    bool has_bias, out_f32;
+    uint32_t out_low, residual_low;  // row_bits
     void *out, *residual;
     int64_t out_ld, residual_ld;
     __device__ __forceinline__ void take(const MmEpilogue &e) {
         act = e.act;
         has_bias = e.bias[0] != nullptr;
-        has_saved = e.saved[0].d != nullptr;
         out_f32 = e.out_f32 != 0;
         out = e.out.d;
         out_ld = e.out.ld;
-        out_wide = wide_rows(out, out_ld, out_f32 ? 4 : 2);
+        out_low = row_bits(out, out_ld, out_f32 ? 4 : 2);
         residual = e.residual.d;
         residual_ld = e.residual.ld;
-        residual_wide = wide_rows(residual, residual_ld, 2);
+        residual_low = row_bits(residual, residual_ld, 2);
     }
 };
 
 // A lane's N columns (of its row) in 16 bits.
 template <bool F16, int N>
-__device__ __forceinline__ void store16(void *base, int64_t ld, bool wide, const Rows &w, int64_t c0, int64_t cols,
+__device__ __forceinline__ void store16(void *base, int64_t ld, uint32_t low, const Rows &w, int64_t c0, int64_t cols,
                                         const float (&v)[N]) {
 #pragma unroll
     for (int i = 0; i < N / 8; ++i)
@@ -240,13 +246,13 @@ __device__ __forceinline__ void store16(void *base, int64_t ld, bool wide, const
             make_uint4(pack16<F16>(v[8 * i], v[8 * i + 1]), pack16<F16>(v[8 * i + 2], v[8 * i + 3]),
                        pack16<F16>(v[8 * i + 4], v[8 * i + 5]), pack16<F16>(v[8 * i + 6], v[8 * i + 7]));
     __syncwarp();
-    store_block<uint16_t, 2 * N>(static_cast<uint16_t *>(base), ld, w.r0, w.rows, c0, cols, wide, w.stage, w.lane);
+    store_block<uint16_t, 2 * N>(static_cast<uint16_t *>(base), ld, w.r0, w.rows, c0, cols, low, w.stage, w.lane);
     __syncwarp();
 }
 
 // A lane's N columns as they are, N / 2 at a time.
 template <int N>
-__device__ __forceinline__ void store32(float *base, int64_t ld, bool wide, const Rows &w, int64_t c0, int64_t cols,
+__device__ __forceinline__ void store32(float *base, int64_t ld, uint32_t low, const Rows &w, int64_t c0, int64_t cols,
                                         const float (&v)[N]) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -257,7 +263,7 @@ __device__ __forceinline__ void store32(float *base, int64_t ld, bool wide, cons
         }
         __syncwarp();
         if (c0 + N / 2 * half < cols)
-            store_block<float, 2 * N>(base, ld, w.r0, w.rows, c0 + N / 2 * half, cols, wide, w.stage, w.lane);
+            store_block<float, 2 * N>(base, ld, w.r0, w.rows, c0 + N / 2 * half, cols, low, w.stage, w.lane);
         __syncwarp();
     }
 }
@@ -314,7 +320,7 @@ __device__ __forceinline__ void store_saved(const emtk_matrix &m, const Rows &w,
     if (m.d_scale)
         store_q8(m, w, c0, cols, v);
     else
-        store16<F16>(m.d, m.ld, wide_rows(m.d, m.ld, 2), w, c0, cols, v);
+        store16<F16>(m.d, m.ld, row_bits(m.d, m.ld, 2), w, c0, cols, v);
 }
 
 template <bool F16>
@@ -335,29 +341,34 @@ __device__ __forceinline__ void add_bias(const float *bias, float (&v)[32]) {
     }
 }
 
-// Gradients: nothing but the sums.  A variant of its own because the other
-// epilogues' code, unrolled over 32 columns and jumped over, cost as much as the
-// stores (20000 x 512 -> 2304, bf16: 41 us against 60 when it was split off).
+// Gradients: nothing but the sums.
 template <bool F16, int N>
 __device__ __forceinline__ void finish_plain(const Rows &w, int64_t c0, int64_t cols, const float (&v)[N]) {
     if (w.out_f32)
-        store32(static_cast<float *>(w.out), w.out_ld, w.out_wide, w, c0, cols, v);
+        store32(static_cast<float *>(w.out), w.out_ld, w.out_low, w, c0, cols, v);
     else
-        store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, v);
+        store16<F16>(w.out, w.out_ld, w.out_low, w, c0, cols, v);
 }
 
-// The residual's block on its way into the warp's staged rows: whole rows of 16-byte
-// pieces asynchronously, without registers that the wait would hold, others by elements.
+// The residual's block on its way into the warp's staged rows: 16-byte pieces
+// or words asynchronously, without registers that the wait would hold, else elements.
 __device__ __forceinline__ void fetch_residual(const Rows &w, int64_t c0, int64_t cols) {
     const int nr = (int)min((int64_t)32, w.rows - w.r0), nc = (int)min((int64_t)32, cols - c0);
     const uint16_t *const base = static_cast<const uint16_t *>(w.residual) + w.r0 * w.residual_ld + c0;
-    if (w.residual_wide && nc == 32) {
+    if (w.residual_low == 0 && nc == 32) {
         const int first = w.lane / 4, piece = w.lane % 4;
 #pragma unroll
         for (int it = 0; it < 4; ++it)
             if (first + 8 * it < nr)
                 copy_async_16(smem_u32(w.stage + staged<64>(first + 8 * it, piece)),
                               base + (first + 8 * it) * w.residual_ld + 8 * piece);
+    } else if ((w.residual_low & 3u) == 0 && nc % 2 == 0) {
+        const int first = w.lane / 16, c = w.lane % 16;
+#pragma unroll
+        for (int it = 0; it < 16; ++it)
+            if (first + 2 * it < nr && 2 * c < nc)
+                copy_async_4(smem_u32(w.stage + staged<64>(first + 2 * it, c / 4) + c % 4 * 4),
+                             base + (first + 2 * it) * w.residual_ld + 2 * c);
     } else if (w.lane < nc) {
         const uint16_t *g = base + w.lane;
         for (int r = 0; r < nr; r += 8, g += 8 * w.residual_ld) {  // eight rows' elements in flight
@@ -373,11 +384,11 @@ __device__ __forceinline__ void fetch_residual(const Rows &w, int64_t c0, int64_
 }
 
 // Sums of a dense tile's 32 columns (z without its bias, which is in `bias`).
-template <bool F16>
+template <bool F16, bool KEEP>
 __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
                                              const float *bias, bool fetched, float (&v)[32]) {
     if (w.has_bias) add_bias(bias, v);
-    if (w.has_saved) store_saved<F16>(e.saved[0], w, c0, cols, v);
+    if constexpr (KEEP) store_saved<F16>(e.saved[0], w, c0, cols, v);
     apply_act(w.act, v);
     if (w.residual) {
         if (!fetched) fetch_residual(w, c0, cols);
@@ -395,13 +406,10 @@ __device__ __forceinline__ void finish_dense(const MmEpilogue &e, const Rows &w,
         }
         __syncwarp();
     }
-    if (w.out_f32)
-        store32(static_cast<float *>(w.out), w.out_ld, w.out_wide, w, c0, cols, v);
-    else
-        store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, v);
+    store16<F16>(w.out, w.out_ld, w.out_low, w, c0, cols, v);
 }
 
-template <bool F16>
+template <bool F16, bool KEEP>
 __device__ __forceinline__ void finish_gated(const MmEpilogue &e, const Rows &w, int64_t c0, int64_t cols,
                                              const float *bias_g, const float *bias_u, float (&g)[32],
                                              float (&u)[32]) {
@@ -409,14 +417,14 @@ __device__ __forceinline__ void finish_gated(const MmEpilogue &e, const Rows &w,
         add_bias(bias_g, g);
         add_bias(bias_u, u);
     }
-    if (w.has_saved) {
+    if constexpr (KEEP) {
         store_saved<F16>(e.saved[0], w, c0, cols, g);
         store_saved<F16>(e.saved[1], w, c0, cols, u);
     }
     apply_act(w.act, g);
 #pragma unroll
     for (int i = 0; i < 32; ++i) g[i] *= u[i];
-    store16<F16>(w.out, w.out_ld, w.out_wide, w, c0, cols, g);
+    store16<F16>(w.out, w.out_ld, w.out_low, w, c0, cols, g);
 }
 
 enum Bar : int { kBarFull = 0, kBarEmpty = 8, kBarAccFull = 16, kBarAccEmpty = 18, kBarDrain = 20, kBarStall = 21, kBars = 22 };
@@ -426,7 +434,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     mm_kernel(const __grid_constant__ MmParams p) {
     using S = Shape<TN, KIND>;
     using E = Epi<KIND>;
-    constexpr bool GATED = KIND == kGated;
+    constexpr bool GATED = is_gated(KIND);
     constexpr int kCols = GATED ? TN / 2 : TN;  // output columns of a tile
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -605,7 +613,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
             // the residual of a block comes while the one before is finished, the first one's
             // while the tile is summed (a z to be kept needs the staged rows first)
-            const bool early = KIND == kDense && partial == nullptr && w.residual && !w.has_saved && w.r0 < w.rows;
+            const bool early = KIND == kDense && partial == nullptr && w.residual && w.r0 < w.rows;
             if (early && n0 < N) fetch_residual(w, n0, N);
             if (!warp_wait(bar(kBarAccFull + ab), (uint32_t)(tile / 2) & 1u, guard, lane)) break;
             tc_fence_after();
@@ -637,14 +645,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     whole.r0 = 128 * (int64_t)rank + 32 * q;
                     whole.rows = kTileM;
                     float *const part = partial + ((int64_t)t.tile * job.parts + t.part) * (kTileM * TN);
-                    store32(part, TN, true, whole, half * kMine + j, TN, v);
-                    if constexpr (GATED) store32(part, TN, true, whole, TN / 2 + half * kMine + j, TN, x);
+                    store32(part, TN, 0u, whole, half * kMine + j, TN, v);
+                    if constexpr (GATED) store32(part, TN, 0u, whole, TN / 2 + half * kMine + j, TN, x);
                 } else if constexpr (KIND == kPlain) {
                     finish_plain<F16>(w, c0, N, v);
                 } else if constexpr (GATED) {
-                    finish_gated<F16>(job.epi, w, c0, N, bias + j, bias + kMine + j, v, x);
+                    finish_gated<F16, keeps(KIND)>(job.epi, w, c0, N, bias + j, bias + kMine + j, v, x);
                 } else {
-                    finish_dense<F16>(job.epi, w, c0, N, bias + j, early, v);
+                    finish_dense<F16, keeps(KIND)>(job.epi, w, c0, N, bias + j, early, v);
                     if (early && j + E::kBlock < kMine && c0 + E::kBlock < N) fetch_residual(w, c0 + E::kBlock, N);
                 }
             }
@@ -770,16 +778,17 @@ typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, 
 
 template <bool F16, Kind KIND, int TN>
 cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
+    constexpr Kind kJoin = is_gated(KIND) ? kGated : KIND == kPlain ? kPlain : kDense;  // it keeps what there is to keep
     cudaError_t e = launch_pdl(mm_kernel<F16, KIND, TN>, dim3(2 * plan.pairs), dim3(kThreads), Shape<TN, KIND>::kSmem, s, p);
     for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
         const MmWork &w = p.piece[i];
         if (w.parts == 1) continue;
-        const int64_t groups = (int64_t)w.tiles * kTileM * (KIND == kGated ? TN / 16 : TN / 8);
+        const int64_t groups = (int64_t)w.tiles * kTileM * (is_gated(KIND) ? TN / 16 : TN / 8);
         int lanes_log2 = 0;  // while the parts and the idle threads last
         const int most = w.epi.saved[0].d_scale ? 3 : 5;
         while (lanes_log2 < most && (2 << lanes_log2) <= w.parts && (groups << lanes_log2) < 2 * 2048 * plan.pairs)
             ++lanes_log2;
-        e = launch_pdl(parts_kernel<F16, KIND, TN>, dim3((unsigned)(((groups << lanes_log2) + 255) / 256)), dim3(256), 0,
+        e = launch_pdl(parts_kernel<F16, kJoin, TN>, dim3((unsigned)(((groups << lanes_log2) + 255) / 256)), dim3(256), 0,
                        s, w.epi, w.raster, static_cast<const float *>(w.partial), w.tile0, w.tiles, w.parts, w.M, w.N,
                        lanes_log2);
     }
@@ -818,6 +827,8 @@ cudaError_t init_mm_kernels() {
     EMTK_MM_ATTRS(kPlain)
     EMTK_MM_ATTRS(kDense)
     EMTK_MM_ATTRS(kGated)
+    EMTK_MM_ATTRS(kDenseKept)
+    EMTK_MM_ATTRS(kGatedKept)
 #undef EMTK_MM_ATTRS
 #undef EMTK_MM_ATTR
     return e == cudaSuccess ? init_skinny_kernels() : e;
@@ -829,9 +840,14 @@ cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
     return plan.tn == 256 ? run<F16, KIND, 256>(p, plan, s) : run<F16, KIND, 128>(p, plan, s);
 }
 template <bool F16>
-cudaError_t run(const MmParams &p, const MmPlan &plan, bool gated, bool plain, cudaStream_t s) {
-    if (gated) return run<F16, kGated>(p, plan, s);
-    return plain ? run<F16, kPlain>(p, plan, s) : run<F16, kDense>(p, plan, s);
+cudaError_t run(const MmParams &p, const MmPlan &plan, Kind kind, cudaStream_t s) {
+    switch (kind) {
+        case kPlain: return run<F16, kPlain>(p, plan, s);
+        case kDense: return run<F16, kDense>(p, plan, s);
+        case kGated: return run<F16, kGated>(p, plan, s);
+        case kDenseKept: return run<F16, kDenseKept>(p, plan, s);
+        default: return run<F16, kGatedKept>(p, plan, s);
+    }
 }
 }  // namespace
 
@@ -873,12 +889,14 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
     p.status = nn->status;
     p.timeout_ns = nn->timeout_ns;
     p.debug_stall = nn->debug_stall;
-    bool plain = !gated;
+    bool plain = !gated, kept = false;
     for (int i = 0; i < n; ++i) {
         const MmEpilogue &e = jobs[i].epi;
-        plain = plain && e.act == EMTK_ACT_NONE && !e.bias[0] && !e.residual.d && !e.saved[0].d;
+        kept = kept || e.saved[0].d;
+        plain = plain && e.act == EMTK_ACT_NONE && !e.bias[0] && !e.residual.d && !kept;
     }
-    return f16 ? run<true>(p, plan, gated, plain, s) : run<false>(p, plan, gated, plain, s);
+    const Kind kind = plain ? kPlain : gated ? (kept ? kGatedKept : kGated) : (kept ? kDenseKept : kDense);
+    return f16 ? run<true>(p, plan, kind, s) : run<false>(p, plan, kind, s);
 }
 
 }  // namespace emtk

@@ -33,10 +33,13 @@ __device__ __forceinline__ bool warp_wait_all(uint32_t bar, uint32_t parity, con
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     return warp_wait(bar, parity, g, lane);
 }
-// 16 bytes from global into shared memory without a register in between, and the wait
-// for all that this thread has started.
+// 16 or 4 bytes from global into shared memory without a register in between, and the
+// wait for all that this thread has started.
 __device__ __forceinline__ void copy_async_16(uint32_t to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async_4(uint32_t to, const void *from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // The address of another CTA's copy of a shared-memory object.

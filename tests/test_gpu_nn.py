@@ -669,3 +669,64 @@ def test_numpy_definition_of_the_scale_byte(lib, nn):
     assert (np.rint(v / 2.0 ** (s - 127)) <= 127).all()
     lower = s - 1
     assert ((np.rint(v / 2.0 ** (lower - 127)) > 127) | (s == 1)).all()
+
+
+# ------------------------------------------------- row distances of what is written
+# (m, k, n): tiles of 256 rows, last rows and columns partial; a contraction that is split.
+@pytest.mark.parametrize("m,k,n", [(300, 96, 152), (257, 200, 340), (700, 64, 95), (256, 9292, 72), (260, 5000, 131)])
+@pytest.mark.parametrize("pad", [0, 2, 4, 7])
+def test_row_distances(lib, nn, m, k, n, pad):
+    """y, a residual, z and g, u kept in 16 and in 8 bits with rows on 16, 8, 4, 2 bytes and (codes) on any
+    byte: the values, and that nothing between the rows is touched.  A call's sums are in the same order
+    whatever the distance, so its results are compared with the same call's on aligned rows bit by bit; those
+    are tested against 64 bits above."""
+    dt = torch.bfloat16
+    g = gen(m + n + pad)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dt)  # noqa: E731
+    x, w, w2, b, c = r(m, k), r(n, k) / 8, r(n, k) / 8, r(n), r(m, n)
+    wide = -(-n // 16) * 16 + 16 - n  # aligned rows
+
+    def run(pad, kept):
+        y, h = (Buf(m, n, dt, pad) for _ in "yh")
+        res = Buf(m, n, dt, pad, 0, c)
+        new = (lambda: q8_of(lib, m, n, pad)) if kept == 8 else (lambda: Buf(m, n, dt, pad))
+        z, gate, up = new(), new(), new()
+        t = (lambda q: q) if kept == 8 else (lambda q: q.t)
+        lib.emtk_dense(nn, x, w, y.t, bias=b, act="gelu", residual=res.t, pre=t(z))
+        alone = Buf(m, n, dt, pad), Buf(m, n, dt, pad)
+        lib.emtk_dense(nn, x, w, alone[0].t, bias=b, act="gelu", residual=res.t)
+        lib.emtk_gated(nn, x, w, w2, h.t, act="silu", gate=t(gate), up=t(up))
+        lib.emtk_gated(nn, x, w, w2, alone[1].t, act="silu")
+        assert all(v.surroundings_untouched() for v in (y, h, *alone))
+        for q in (z, gate, up):
+            if kept == 8:
+                assert bool((q.codes._base[:, n:] == 77).all()) and bool((q.scales._base[:, (n + 31) // 32:] == 99).all())
+            else:
+                assert q.surroundings_untouched()
+        return [v.t for v in (y, h, *alone)] + [v for q in (z, gate, up) for v in ((q.codes, q.scales) if kept == 8 else (q.t,))]
+
+    for kept in (16, 8):
+        for got, want in zip(run(pad, kept), run(wide, kept)):
+            assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("m,k", [(1, 40), (33, 24), (50, 70), (40, 100), (21, 200), (600, 85), (1500, 264), (300, 1000),
+                                 (70, 2305), (5000, 33)])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 0), (1, 1), (6, 2), (3, 5)])
+def test_pack8_and_back_at_any_distance(lib, nn, m, k, pad, shift):
+    """Rows of values and of codes at every alignment, narrow rows that share a warp included."""
+    g = gen(m * k + pad)
+    x = torch.randn(m, k, generator=g, device="cuda") * torch.exp(2 * torch.randn(m, k, generator=g, device="cuda"))
+    x = Buf(m, k, torch.bfloat16, pad, shift, x)
+    nb = (k + 31) // 32
+    whole = torch.full((m * (k + pad) + shift + 16,), 77, dtype=torch.int8, device="cuda")
+    codes = whole[shift:shift + m * (k + pad)].view(m, k + pad)
+    q = lib.Q8(codes[:, :k], torch.full((m, nb), 99, dtype=torch.uint8, device="cuda"))
+    lib.emtk_pack8(nn, x.t, q)
+    want = held8(x.t.double())
+    assert torch.equal(q8_values(q, k), want)
+    assert bool((codes[:, k:] == 77).all()) and bool((whole[:shift] == 77).all()) and bool((whole[-16:] == 77).all())
+    for p, s in ((pad, shift), (0, 0), (1, 3)):
+        back = Buf(m, k, torch.bfloat16, p, s)
+        lib.emtk_unpack8(nn, q, back.t)
+        assert torch.equal(back.t.double(), want) and back.surroundings_untouched()
