@@ -455,6 +455,7 @@ struct PackArgs {
     int64_t q_ld, ld_scale;
     int m, k;
     Walk walk;
+    int whole;       // of pack8_kernel: codes on 16 bytes, k a multiple of 16
     int lanes_log2;  // of pack8_any_kernel
 };
 
@@ -482,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) pack8_kernel(const __grid_c
             if (in[i]) {
                 const uint8_t *p = a.x.p + r[i] * a.x.row_bytes + 2 * (int64_t)c[i];
                 w[i][0].load(p, nullptr);
-                w[i][1].load(p + 16, nullptr);
+                if (c[i] + kVec < a.k) w[i][1].load(p + 16, nullptr);
             }
         }
 #pragma unroll
@@ -508,9 +509,15 @@ __global__ void __launch_bounds__(kThreads, kBlocks) pack8_kernel(const __grid_c
             const uint32_t b = q8_scale(top);
             const float inverse = q8_inverse(b);
             if (c[i] % kQ8Block == 0) a.scale[r[i] * a.ld_scale + c[i] / kQ8Block] = (uint8_t)b;
-            *reinterpret_cast<uint4 *>(a.q + r[i] * a.q_ld + c[i]) =
-                make_uint4(q8_codes4(v, inverse, all_finite), q8_codes4(v + 4, inverse, all_finite),
-                           q8_codes4(v + 8, inverse, all_finite), q8_codes4(v + 12, inverse, all_finite));
+            uint8_t *const to = a.q + r[i] * a.q_ld + c[i];
+            const uint2 lo = make_uint2(q8_codes4(v, inverse, all_finite), q8_codes4(v + 4, inverse, all_finite));
+            const uint2 hi = make_uint2(q8_codes4(v + 8, inverse, all_finite), q8_codes4(v + 12, inverse, all_finite));
+            if (a.whole) {
+                *reinterpret_cast<uint4 *>(to) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            } else {
+                *reinterpret_cast<uint2 *>(to) = lo;
+                if (c[i] + kVec < a.k) *reinterpret_cast<uint2 *>(to + kVec) = hi;
+            }
         }
     }
 }
@@ -543,23 +550,32 @@ __global__ void __launch_bounds__(kThreads, kBlocks) pack8_any_kernel(const __gr
     Item it(a.walk, ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> a.lanes_log2);
     pdl_trigger();
     pdl_wait();
-    for (; __any_sync(0xffffffffu, it.r < a.m); it.next(a.walk)) {
-        const int64_t first = (int64_t)it.piece * (kVec * lanes), c = first + lane * kVec;
-        const bool in = it.r < a.m && c < a.k;
-        float v[kVec] = {};
-        if (in) {
-            AnyPiece<false> piece;
-            piece.load(a.x, it.r, c, a.m, a.k);
-            piece.template values<F16>(v);
+    while (__any_sync(0xffffffffu, it.r < a.m)) {
+        constexpr int kFlight = 2;
+        AnyPiece<false> piece[kFlight];
+        int64_t r[kFlight], first[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i, it.next(a.walk)) {
+            r[i] = it.r;
+            first[i] = (int64_t)it.piece * (kVec * lanes);
+            if (r[i] < a.m && first[i] + lane * kVec < a.k) piece[i].load(a.x, r[i], first[i] + lane * kVec, a.m, a.k);
         }
-        bool all_finite;
-        float top = finite_top(v, all_finite);
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const uint32_t b = q8_scale(top);
-        if (in && (lane & 3) == 0) a.scale[it.r * a.ld_scale + c / kQ8Block] = (uint8_t)b;
-        const uint32_t w[2] = {q8_codes4(v, q8_inverse(b), all_finite), q8_codes4(v + 4, q8_inverse(b), all_finite)};
-        store_codes(a.q + it.r * a.q_ld + first, it.r < a.m ? (int)min(a.k - first, (int64_t)kVec * lanes) : 0, w, lanes, lane);
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const int64_t c = first[i] + lane * kVec;
+            const bool in = r[i] < a.m && c < a.k;
+            float v[kVec] = {};
+            if (in) piece[i].template values<F16>(v);
+            bool all_finite;
+            float top = finite_top(v, all_finite);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const uint32_t b = q8_scale(top);
+            if (in && (lane & 3) == 0) a.scale[r[i] * a.ld_scale + c / kQ8Block] = (uint8_t)b;
+            const uint32_t w[2] = {q8_codes4(v, q8_inverse(b), all_finite), q8_codes4(v + 4, q8_inverse(b), all_finite)};
+            store_codes(a.q + r[i] * a.q_ld + first[i], r[i] < a.m ? (int)min(a.k - first[i], (int64_t)kVec * lanes) : 0, w,
+                        lanes, lane);
+        }
     }
 }
 
@@ -738,7 +754,8 @@ cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk
 cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
                          cudaStream_t s) {
     if (m == 0 || k == 0) return cudaSuccess;
-    const bool wide = k % kPackCols == 0 && wide_matrix(x.d, 2 * x.ld, 16) && wide_matrix(q.d, q.ld, 16);
+    const bool wide = k % kVec == 0 && wide_matrix(x.d, 2 * x.ld, 16) && wide_matrix(q.d, q.ld, 8);
+    const bool whole = k % kPackCols == 0 && wide_matrix(q.d, q.ld, 16);
     const bool f16 = type == EMTK_TYPE_F16;
     // wide: an even number of pieces a row, so that a block's two threads are neighbours
     int lanes_log2 = 5;
@@ -746,7 +763,7 @@ cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, con
     const WalkPlan plan = wide ? walk_plan(m, k, kPackCols, kThreads, true)
                                : walk_plan(m, k, kVec << lanes_log2, kThreads >> lanes_log2, false);
     const unsigned blocks = plan.blocks(sms);
-    const PackArgs a{source_of(x), static_cast<uint8_t *>(q.d), q.d_scale, q.ld, q.ld_scale, m, k, plan.walk(blocks), lanes_log2};
+    const PackArgs a{source_of(x), static_cast<uint8_t *>(q.d), q.d_scale, q.ld, q.ld_scale, m, k, plan.walk(blocks), whole, lanes_log2};
     return launch_pdl(wide ? (f16 ? pack8_kernel<true> : pack8_kernel<false>)
                            : (f16 ? pack8_any_kernel<true> : pack8_any_kernel<false>),
                       dim3(blocks), dim3(kThreads), 0, s, a);
