@@ -7,8 +7,9 @@
 // Measured, bf16: the gated slopes of 8192 x 10240 from 8-bit g and u, 104 us (6.5 TB/s
 // of the bytes they need); a dense layer's of 20000 x 512 with column sums, 15 us;
 // pack8 of 20000 x 2304, 21 us (6.7 TB/s); unpack8 of the same, 22 us (6.3 TB/s).  At
-// odd alignment the gated slopes of 2048 x 5461 take 34 us (3.3 TB/s): 115 registers
-// leave two blocks an SM, too few to cover the loads.
+// odd alignment the gated slopes of 2048 x 5461 take 25 us (4.5 TB/s; 80 registers, three
+// blocks an SM), pack8 and unpack8 of 8192 x 4095 44 and 31 us against 14 and 15 of 8192 x
+// 4096: there instructions bound them, the shifting of words and the rows' ends.
 #include <algorithm>
 
 #include "emtk_internal.h"
@@ -18,9 +19,8 @@
 namespace emtk {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kVec = 8;                  // columns of a thread
-constexpr int kWarpCols = 32 * kVec;     // columns of a warp's piece of a row
+constexpr int kThreads = 256;
+constexpr int kVec = 8;  // columns of a thread
 
 struct Source {  // a 16-bit matrix or a checkpoint
     const uint8_t *p;
@@ -424,7 +424,7 @@ cudaError_t run_slope(emtk_type type, int act, SlopeArgs &a, float *partial, flo
 
 // -------------------------------------------------------- checkpoints
 // Work is dealt out in pieces of a row, every so-manieth one to a thread (or to a
-// warp, 256 columns); the step from one to the next is added to row and piece,
+// group of lanes); the step from one to the next is added to row and piece,
 // without a division.
 struct Walk {
     int per_row;
