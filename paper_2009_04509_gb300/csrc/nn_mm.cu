@@ -614,7 +614,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             // the residual of a block comes while the one before is finished, the first one's
             // while the tile is summed (a z to be kept needs the staged rows first)
             const bool early = KIND == kDense && partial == nullptr && w.residual && w.r0 < w.rows;
-            if (early && n0 < N) fetch_residual(w, n0, N);
+            if (early && n0 < N) {
+                fetch_residual(w, n0, N);
+                if (w.r0 + lane < w.rows) {  // the other blocks of the lane's row: into L2 meanwhile
+                    const uint16_t *g = static_cast<const uint16_t *>(w.residual) + (w.r0 + lane) * w.residual_ld + n0;
+#pragma unroll
+                    for (int j = E::kBlock; j < kMine; j += 64) prefetch_l2(g + min((int64_t)j, N - 1 - n0));
+                    prefetch_l2(g + min((int64_t)kMine, N - n0) - 1);
+                }
+            }
             if (!warp_wait(bar(kBarAccFull + ab), (uint32_t)(tile / 2) & 1u, guard, lane)) break;
             tc_fence_after();
             const uint32_t acc = tmem + (uint32_t)(ab * TN) + ((uint32_t)(32 * q) << 16);

@@ -41,6 +41,7 @@ __device__ __forceinline__ void copy_async_16(uint32_t to, const void *from) {
 __device__ __forceinline__ void copy_async_4(uint32_t to, const void *from) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // The address of another CTA's copy of a shared-memory object.
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
