@@ -54,8 +54,8 @@ constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
 // gated block's, and those that keep z or g and u as well.  Each is a variant of its
 // own: unrolled over a block's columns, the others' code, jumped over, costs as much as
 // the stores, in instruction fetches or spilled registers (bf16, 20000 x 512 -> 2304
-// with the dense layer's code as well: 60 us instead of 41; 8192 x 64 -> 4096 with a
-// residual, with the kept z's: 42 instead of 37).  An epilogue warp turns blocks of 32
+// with the dense layer's code as well: 60 us, 41 when split off; 8192 x 64 -> 4096
+// with a residual, with the kept z's: 42, 37 when split off).  An epilogue warp turns blocks of 32
 // rows by kBlock columns into output through kStageRow-byte rows of shared memory; the
 // gradients' blocks are twice as wide, which halves the latencies that their stores
 // wait out.
@@ -665,6 +665,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 }
             }
         }
+        if (KIND == kDense) copy_async_wait();  // a wait that gave up left a residual's copies in flight
     }
     tc_fence_before();
     __syncthreads();
