@@ -525,6 +525,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 }
             }
         }
+        // The last commits' arrivals at this CTA's stages (at unused ones the wait is none).
+        for (int i = 0; ok && i < S::kStages; ++i) {
+            ok = warp_wait_all(bar(kBarEmpty + s), phase, guard, lane);
+            if (++s == S::kStages) {
+                s = 0;
+                phase ^= 1;
+            }
+        }
         if (!ok) {  // copies in flight land within microseconds: leave them a millisecond
             const uint64_t t0 = global_timer_ns();
             while (global_timer_ns() - t0 < 1000000u) {
@@ -571,13 +579,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (ok && elect_one()) mma_commit_pair(bar(kBarAccFull + ab));
             __syncwarp();
         }
-        // every MMA issued completes before TMEM is released
-        if (elect_one()) {
-            mma_commit_pair(bar(kBarDrain));
-            const uint64_t t0 = global_timer_ns();
-            while (!mbar_try_wait(bar(kBarDrain), 0u) && (int64_t)(global_timer_ns() - t0) < p.timeout_ns) {
-            }
-        }
+        if (elect_one()) mma_commit_pair(bar(kBarDrain));
         __syncwarp();
     } else if (warp >= kFirstEpiWarp) {
         // ---------------------------------------------------- epilogue
@@ -669,6 +671,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
+    // Every MMA issued is complete, and both CTAs have seen the arrival that says so:
+    // neither may leave, nor release TMEM, while one is on its way to its shared memory.
+    // (The accumulators' arrivals are seen by the epilogues, the stages' by the producers.)
+    if (warp == 1) {
+        const uint64_t t0 = global_timer_ns();
+        while (!__all_sync(0xffffffffu, mbar_try_wait(bar(kBarDrain), 0u)) &&
+               __any_sync(0xffffffffu, (int64_t)(global_timer_ns() - t0) < p.timeout_ns)) {
+        }
+        __syncwarp();
+    }
     cluster_sync();  // no arrival or MMA of the pair is outstanding
     tc_fence_after();
     if (warp == 2) tmem_free_pair(tmem, S::kTmemCols);
