@@ -486,8 +486,9 @@ EMTK_API emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args
 /* The first half of a gated feed-forward block, in one kernel:
  *   h = act(g) * u [m][f] with g = x w_gate^T + bias_gate, u = x w_up^T + bias_up;
  *   w_gate, w_up [f][k]; both biases or neither.  gate and up receive g and u
- *   for emtk_gated_backward (the call's type or 8-bit checkpoints), or
- *   d == NULL for both.  The second half is emtk_dense with a residual. */
+ *   (each in the call's type or as an 8-bit checkpoint; emtk_gated_backward
+ *   takes them where they are alike), or d == NULL for both.  The second half
+ *   is emtk_dense with a residual. */
 typedef struct {
     int32_t m, f, k;
     int32_t act, type, bias_type;

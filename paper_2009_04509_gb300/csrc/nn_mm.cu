@@ -805,8 +805,8 @@ cudaError_t run(const MmParams &p, const MmPlan &plan, cudaStream_t s) {
         const MmWork &w = p.piece[i];
         if (w.parts == 1) continue;
         const int64_t groups = (int64_t)w.tiles * kTileM * (is_gated(KIND) ? TN / 16 : TN / 8);
-        int lanes_log2 = 0;  // while the parts and the idle threads last
-        const int most = w.epi.saved[0].d_scale ? 3 : 5;
+        int lanes_log2 = 0;  // while the parts and the idle threads last, and a checkpoint's block fits a warp
+        const int most = w.epi.saved[0].d_scale || w.epi.saved[1].d_scale ? 3 : 5;
         while (lanes_log2 < most && (2 << lanes_log2) <= w.parts && (groups << lanes_log2) < 2 * 2048 * plan.pairs)
             ++lanes_log2;
         e = launch_pdl(parts_kernel<F16, kJoin, TN>, dim3((unsigned)(((groups << lanes_log2) + 255) / 256)), dim3(256), 0,

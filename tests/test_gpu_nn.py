@@ -730,3 +730,24 @@ def test_pack8_and_back_at_any_distance(lib, nn, m, k, pad, shift):
         back = Buf(m, k, torch.bfloat16, p, s)
         lib.emtk_unpack8(nn, q, back.t)
         assert torch.equal(back.t.double(), want) and back.surroundings_untouched()
+
+
+@pytest.mark.parametrize("eight", ["gate", "up"])
+@pytest.mark.parametrize("m,k,f", [(256, 9292, 128), (256, 9292, 72), (64, 16384, 64), (40, 100, 72), (8, 512, 40), (300, 96, 152)])
+def test_gate_and_up_kept_in_unlike_kinds(lib, nn, m, k, f, eight):
+    """One of g and u kept in 16 bits, the other in 8, where the contraction is split over many parts (the
+    first three) and where it is not: each within the bounds of its own kind."""
+    dt = torch.bfloat16
+    g = gen(m + f)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dt)  # noqa: E731
+    x, wg, wu = r(m, k), r(f, k) / 16, r(f, k) / 16
+    h, kept16, kept8 = torch.empty((m, f), dtype=dt, device="cuda"), torch.empty((m, f), dtype=dt, device="cuda"), q8_of(lib, m, f)
+    gate, up = (kept8, kept16) if eight == "gate" else (kept16, kept8)
+    lib.emtk_gated(nn, x, wg, wu, h, act="silu", gate=gate, up=up)
+    for w, kept in ((wg, gate), (wu, up)):
+        z, e = x.double() @ w.double().t(), (k + 2) * E * (x.double().abs() @ w.double().abs().t())
+        if kept is kept16:
+            close(kept, z, stored(e, z, "bf16"), "kept in 16 bits")
+        else:
+            top = torch.nn.functional.pad(z.abs() + e, (0, -f % 32)).view(m, -1, 32).amax(2).repeat_interleave(32, 1)[:, :f]
+            close(q8_values(kept, f), z, e + top / 127.5 + 2.0 ** -126, "kept in 8 bits")
