@@ -405,8 +405,13 @@ EMTK_API emtk_status emtk_batcher_destroy(emtk_batcher *b);
  *     residual itself (same address, same ld).
  *   - A layer handle (emtk_nn) holds the device workspace of its calls.  It
  *     grows to the largest call it has served (a cudaMalloc, after waiting
- *     for `stream`): reserve enough in emtk_nn_create to capture calls into a
- *     graph.  Like a context, a handle is used from one stream at a time.
+ *     for `stream`).  A call that is captured into a graph must find the
+ *     workspace large enough, or is refused with EMTK_ERR_CUDA and the
+ *     capture goes on without it: reserve enough in emtk_nn_create, or make
+ *     the same calls once before.  A workspace that a graph holds is kept
+ *     when a later call outgrows it, so the graph stays good until
+ *     emtk_nn_destroy; replaying it counts as a call.  Like a context, a
+ *     handle is used from one stream at a time.
  * -------------------------------------------------------------------- */
 typedef struct emtk_nn emtk_nn;
 
@@ -450,7 +455,8 @@ typedef struct {
 EMTK_API emtk_status emtk_nn_create(int device, int64_t workspace_bytes, int64_t wait_timeout_ns, int32_t debug_stall,
                                     emtk_nn **out);
 
-/* Frees the handle (synchronises its device first).  NULL is accepted. */
+/* Frees the handle (synchronises its device first); graphs that hold its
+ * calls must not be replayed any more.  NULL is accepted. */
 EMTK_API emtk_status emtk_nn_destroy(emtk_nn *nn);
 
 /* As emtk_check, for a layer handle. */

@@ -72,7 +72,9 @@ struct Checks {
 };
 
 // Workspace of one call, laid out front to back: a first pass adds up the
-// sizes, ensure() makes room, a second pass hands out the addresses.
+// sizes, ensure() makes room, a second pass hands out the addresses.  A workspace
+// whose address a captured call holds is kept when it is outgrown: the graph may
+// be replayed at any time.
 struct CallSpace {
     emtk_nn *nn;
     size_t used = 0;
@@ -86,10 +88,26 @@ struct CallSpace {
         dry = false;
         const size_t bytes = used;
         used = 0;
-        if (bytes <= nn->ws_bytes) return EMTK_OK;
-        cudaError_t e = cudaStreamSynchronize(s);  // earlier calls may still use the old one
+        if (bytes == 0) return EMTK_OK;
+        cudaStreamCaptureStatus capture;
+        cudaError_t e = cudaStreamIsCapturing(s, &capture);
         if (e != cudaSuccess) return status_of(e);
-        e = dev_free(nn->ws);
+        const bool capturing = capture != cudaStreamCaptureStatusNone;
+        if (bytes <= nn->ws_bytes) {
+            nn->captured = nn->captured || capturing;
+            return EMTK_OK;
+        }
+        if (capturing) return EMTK_ERR_CUDA;  // refused before it would spoil the capture
+        if (nn->captured) {
+            emtk_nn::Outgrown *const kept = new (std::nothrow) emtk_nn::Outgrown{nn->ws, nn->outgrown};
+            if (!kept) return EMTK_ERR_OOM;
+            nn->outgrown = kept;
+            nn->captured = false;
+        } else {
+            e = cudaStreamSynchronize(s);  // earlier calls may still use the old one
+            if (e != cudaSuccess) return status_of(e);
+            e = dev_free(nn->ws);
+        }
         nn->ws = nullptr;
         nn->ws_bytes = 0;
         if (e == cudaSuccess) e = dev_alloc(&nn->ws, bytes + bytes / 4);
@@ -196,6 +214,11 @@ emtk_status emtk_nn_destroy(emtk_nn *nn) {
     DeviceGuard g(nn->device);
     cudaError_t e = cudaDeviceSynchronize();
     dev_free(nn->ws);
+    while (emtk_nn::Outgrown *const o = nn->outgrown) {
+        dev_free(o->ws);
+        nn->outgrown = o->next;
+        delete o;
+    }
     dev_free(nn->status);
     delete nn;
     return e == cudaSuccess ? EMTK_OK : EMTK_ERR_CUDA;

@@ -22,6 +22,11 @@ struct emtk_nn {
     int *status = nullptr;   // device status word, as a context's
     void *ws = nullptr;      // workspace of the running call
     size_t ws_bytes = 0;
+    bool captured = false;   // a graph holds the workspace's address
+    struct Outgrown {        // workspaces that graphs hold, kept until the handle goes
+        void *ws;
+        Outgrown *next;
+    } *outgrown = nullptr;
     void *encode = nullptr;  // cuTensorMapEncodeTiled
 };
 

@@ -751,3 +751,43 @@ def test_gate_and_up_kept_in_unlike_kinds(lib, nn, m, k, f, eight):
         else:
             top = torch.nn.functional.pad(z.abs() + e, (0, -f % 32)).view(m, -1, 32).amax(2).repeat_interleave(32, 1)[:, :f]
             close(q8_values(kept, f), z, e + top / 127.5 + 2.0 ** -126, "kept in 8 bits")
+
+
+def test_a_graph_outlives_a_larger_call(lib):
+    """A call captured into a graph, then a larger one that the workspace has to grow for: the workspace that
+    the graph holds is kept (seen in the library's count of allocations before the graph runs again), the
+    graph gives its results, and all of it goes with the handle."""
+    before = lib.emtk_debug_alloc_counts()
+    h = lib.emtk_nn_create()
+    t = torch.bfloat16
+    g = gen(8)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(t)  # noqa: E731
+    dy, x, w, z = r(200, 72), r(200, 96), r(72, 96), r(200, 72)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    step = lambda: lib.emtk_dense_backward(h, dy, x, w, act="gelu", pre=z, dx=dx, dw=dw)  # noqa: E731
+    large = [r(*s) for s in ((3000, 520), (3000, 264), (520, 264), (3000, 520))]
+    out = [torch.empty_like(large[1]), torch.empty_like(large[2])]
+    grow = lambda: lib.emtk_dense_backward(h, *large[:3], act="gelu", pre=large[3], dx=out[0], dw=out[1])  # noqa: E731
+    step()
+    want = dx.clone(), dw.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+        with pytest.raises(lib.EmtkError):  # too large for the workspace, and it cannot grow now
+            grow()
+    held = lib.emtk_debug_alloc_counts()[0]
+    grow()
+    assert lib.emtk_debug_alloc_counts()[0] == held + 1
+    grown = [v.clone() for v in out]
+    for _ in range(3):
+        dx.zero_(), dw.zero_()
+        graph.replay()
+        assert torch.equal(dx, want[0]) and torch.equal(dw, want[1])
+        grow()
+        assert all(torch.equal(a, b) for a, b in zip(out, grown))
+    assert lib.emtk_nn_check(h) == lib.EMTK_OK
+    torch.cuda.synchronize()
+    del graph
+    lib.emtk_nn_destroy(h)
+    assert lib.emtk_debug_alloc_counts() == before
