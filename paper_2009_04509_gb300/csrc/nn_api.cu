@@ -110,9 +110,12 @@ struct CallSpace {
         }
         nn->ws = nullptr;
         nn->ws_bytes = 0;
-        if (e == cudaSuccess) e = dev_alloc(&nn->ws, bytes + bytes / 4);
+        size_t device_free = 0, device_total = 0;
+        if (e == cudaSuccess) e = cudaMemGetInfo(&device_free, &device_total);
+        const size_t size = workspace_size(bytes, device_free);
+        if (e == cudaSuccess) e = dev_alloc(&nn->ws, size);
         if (e != cudaSuccess) return status_of(e);
-        nn->ws_bytes = bytes + bytes / 4;
+        nn->ws_bytes = size;
         return EMTK_OK;
     }
 };

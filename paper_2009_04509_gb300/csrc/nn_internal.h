@@ -34,6 +34,13 @@ namespace emtk {
 
 constexpr int kQ8Block = 32;  // columns that share a checkpoint scale
 
+// Size of a workspace that has to hold `need` bytes: a quarter more, so that slowly
+// growing calls seldom wait, unless the device has little left beside it.
+inline size_t workspace_size(size_t need, size_t device_free) {
+    const size_t ample = need + need / 4;
+    return ample <= device_free - device_free / 16 ? ample : need;
+}
+
 // Operand of a matrix product: element (i, t) of the contraction t is
 // p[i * ld + t], or p[t * ld + i] if `across` (i runs along memory).
 struct MmOperand {
