@@ -791,3 +791,31 @@ def test_a_graph_outlives_a_larger_call(lib):
     del graph
     lib.emtk_nn_destroy(h)
     assert lib.emtk_debug_alloc_counts() == before
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_gelu_in_its_tail(lib, nn, dtype):
+    """z Phi(z) and its slope for z in [-12, 0], relative to the value (the slope: to the sum of its two terms):
+    the exponent z^2 / 2, up to 72 and on to 104 in powers of two, is rounded twice (2^-23 of it: 1.2e-5 of the
+    value), the rest of the arithmetic is some ten fp32 roundings: together below 2^-16, and the one to 16 bits.
+    z itself is exact: one product, with 1, few rows and many columns, and the reverse."""
+    dt = DT[dtype]
+    z = torch.linspace(-12, 0, 4803, dtype=torch.float64, device="cuda").to(dt).unique()
+    n = z.numel()
+    z64 = z.double()
+    phi, e = torch.special.erfc(-z64 * math.sqrt(0.5)) / 2, torch.exp(-z64 * z64 / 2) / math.sqrt(2 * math.pi)
+    bound = lambda v, mag: 2.0 ** -16 * mag + U[dtype] * v.abs() + max(TINY[dtype], 2.0 ** -133)  # noqa: E731
+    want = z64 * phi
+    one = torch.ones((1, 1), dtype=dt, device="cuda")
+    for rows in (1, 3, 40, 200):
+        y, ones = torch.empty((rows, n), dtype=dt, device="cuda"), torch.ones((rows, 1), dtype=dt, device="cuda")
+        lib.emtk_dense(nn, ones, z.view(n, 1), y, act="gelu")
+        close(y, want.expand(rows, n), bound(want, want.abs()), f"{rows} rows")
+        lib.emtk_gated(nn, ones, z.view(n, 1), torch.ones((n, 1), dtype=dt, device="cuda"), y, act="gelu")
+        close(y, want.expand(rows, n), bound(want, want.abs()), f"{rows} rows, gated")
+    y = torch.empty((n, 1), dtype=dt, device="cuda")
+    lib.emtk_dense(nn, z.view(n, 1), one, y, act="gelu")
+    close(y[:, 0], want, bound(want, want.abs()), "a column")
+    want = phi + z64 * e
+    lib.emtk_dense_backward(nn, torch.ones((n, 1), dtype=dt, device="cuda"), None, one, act="gelu", pre=z.view(n, 1), dx=y)
+    close(y[:, 0], want, bound(want, phi + z64.abs() * e), "slope")
