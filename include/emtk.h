@@ -400,7 +400,10 @@ EMTK_API emtk_status emtk_batcher_destroy(emtk_batcher *b);
  *   - Operands are bf16 or fp16 (one type per call); products are summed in
  *     fp32 on the tensor cores, and everything up to the stored value is fp32
  *     but for the products of a backward call with an activation: those take
- *     dz (dg, du) rounded to the operand type.  Every output is rounded once.
+ *     dz (dg, du) rounded to the operand type.  In fp16 that is off by 2^-11
+ *     of the value and at most 2^-19 of the call's largest dz (dg or du),
+ *     whatever that is: beyond 65504 or below 2^-6 all are stored by a power
+ *     of two, which the sums undo.  Every output is rounded once.
  *   - Outputs must not overlap inputs or each other, except that y may be the
  *     residual itself (same address, same ld).
  *   - A layer handle (emtk_nn) holds the device workspace of its calls.  It

@@ -168,6 +168,14 @@ emtk_status forward(emtk_nn *nn, MmJob &j, const emtk_matrix &x, const emtk_matr
     return status_of(e);
 }
 
+// The status of a backward call.  Where a launch failed, the products have not reset the
+// slopes' range.
+emtk_status finished(cudaError_t e, SlopeRange *range, cudaStream_t s) {
+    const emtk_status st = status_of(e);
+    if (st != EMTK_OK && range) status_of(cudaMemsetAsync(range, 0, sizeof(SlopeRange), s));
+    return st;
+}
+
 }  // namespace
 
 extern "C" {
@@ -196,9 +204,10 @@ emtk_status emtk_nn_create(int device, int64_t workspace_bytes, int64_t wait_tim
                                                      &found);
     if (e == cudaSuccess && (nn->encode == nullptr || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
     if (e == cudaSuccess) e = init_mm_kernels();
-    if (e == cudaSuccess) e = dev_alloc(&status, sizeof(int));
+    if (e == cudaSuccess) e = dev_alloc(&status, sizeof(int) + sizeof(SlopeRange));
     nn->status = static_cast<int *>(status);
-    if (e == cudaSuccess) e = cudaMemset(nn->status, 0, sizeof(int));
+    nn->range = reinterpret_cast<SlopeRange *>(nn->status + 1);
+    if (e == cudaSuccess) e = cudaMemset(nn->status, 0, sizeof(int) + sizeof(SlopeRange));
     if (e == cudaSuccess && workspace_bytes > 0) {
         e = dev_alloc(&nn->ws, (size_t)workspace_bytes);
         if (e == cudaSuccess) nn->ws_bytes = (size_t)workspace_bytes;
@@ -342,13 +351,16 @@ emtk_status emtk_dense_backward(emtk_nn *nn, const emtk_dense_grad_args *p, emtk
             if (st != EMTK_OK) return st;
         }
     }
+    // (ReLU's dz is dy or 0 and rounds nothing.)
+    SlopeRange *const kept_in = own_dz && type == EMTK_TYPE_F16 && a.act != EMTK_ACT_RELU ? nn->range : nullptr;
+    for (MmJob &j : jobs) j.epi.range = kept_in;
     cudaError_t e = cudaSuccess;
     if (own_dz || a.db)
-        e = launch_slope(type, a.act, a.m, a.n, a.dy, a.pre, own_dz ? dz.d : nullptr, dz.ld, a.db, sums,
+        e = launch_slope(type, a.act, a.m, a.n, a.dy, a.pre, own_dz ? dz.d : nullptr, dz.ld, a.db, sums, kept_in,
                          nn->sm_count, s);
     if (e == cudaSuccess) e = launch_copy16(type, stage.copies, stage.n, nn->sm_count, s);
     if (e == cudaSuccess && n > 0) e = launch_mm(jobs, n, plan, nn, partial, s);
-    return status_of(e);
+    return finished(e, kept_in, s);
 }
 
 emtk_status emtk_gated(emtk_nn *nn, const emtk_gated_args *p, emtk_stream stream) {
@@ -471,13 +483,15 @@ emtk_status emtk_gated_backward(emtk_nn *nn, const emtk_gated_grad_args *p, emtk
             if (st != EMTK_OK) return st;
         }
     }
+    SlopeRange *const kept_in = n > 0 && type == EMTK_TYPE_F16 ? nn->range : nullptr;
+    for (MmJob &j : jobs) j.epi.range = kept_in;
     cudaError_t e = cudaSuccess;
     if (n > 0 || a.db_gate || a.h.d)
         e = launch_gated_slope(type, a.act, a.m, a.f, a.dh, a.gate, a.up, dg.d, du.d, ld16(a.f), a.h, a.db_gate,
-                               a.db_up, sums, nn->sm_count, s);
+                               a.db_up, sums, kept_in, nn->sm_count, s);
     if (e == cudaSuccess) e = launch_copy16(type, stage.copies, stage.n, nn->sm_count, s);
     if (e == cudaSuccess && n > 0) e = launch_mm(jobs, n, plan, nn, partial, s);
-    return status_of(e);
+    return finished(e, kept_in, s);
 }
 
 emtk_status emtk_pack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type type, const emtk_matrix *x, const emtk_matrix *q,

@@ -14,12 +14,17 @@
 #define EMTK_HOST_DEVICE inline
 #endif
 
+namespace emtk {
+struct SlopeRange;
+}
+
 struct emtk_nn {
     int device = 0;
     int sm_count = 0;
     int64_t timeout_ns = 0;
     int debug_stall = 0;
     int *status = nullptr;   // device status word, as a context's
+    emtk::SlopeRange *range = nullptr;  // beside it: of the running backward call's slopes
     void *ws = nullptr;      // workspace of the running call
     size_t ws_bytes = 0;
     bool captured = false;   // a graph holds the workspace's address
@@ -49,17 +54,27 @@ struct MmOperand {
     bool across;
 };
 
+// Slopes dz (dg and du) in fp16: their largest finite magnitudes (zero between calls:
+// the products, which come last, reset them), and the inverse of the power of two by
+// which they are stored (nn_math.cuh), which the products' sums take.
+struct SlopeRange {
+    uint32_t peak[2];
+    float unscale;
+};
+
 // What becomes of the sums.
 //   plain: z = sum + bias[0]; out = act(z) + residual; saved[0] = z
 //   gated: g = sum0 + bias[0], u = sum1 + bias[1]; out = act(g) u;
 //          saved[0] = g, saved[1] = u
-// Absent parts have null pointers.  out is fp32 if out_f32.
+// Absent parts have null pointers.  out is fp32 if out_f32.  range (of a gradient: no other
+// parts): the sums are of scaled slopes.
 struct MmEpilogue {
     int act;
     int bias_f32;
     int out_f32;
     const void *bias[2];
     emtk_matrix residual, out, saved[2];
+    const SlopeRange *range;
 };
 
 // out[M][N] from the contraction over K of a[i] and b[i] (rows M and N):
@@ -128,13 +143,14 @@ cudaError_t init_skinny_kernels();  // once per device
 // ---- pointwise passes (nn_pointwise.cu)
 // dz = dy act'(pre) as a 16-bit matrix dz (or none), and its column sums db
 // (or null).  partial: fp32 [slope_slices(m, n, sms)][n] scratch when db is wanted.
+// range (fp16, or null): dz is stored by a power of two that keeps it in fp16's range.
 int slope_slices(int m, int n, int sms);
 cudaError_t launch_slope(emtk_type type, int act, int m, int n, const emtk_matrix &dy, const emtk_matrix &pre,
-                         void *dz, int64_t dz_ld, float *db, float *partial, int sms, cudaStream_t s);
+                         void *dz, int64_t dz_ld, float *db, float *partial, SlopeRange *range, int sms, cudaStream_t s);
 // dg, du, h and the column sums of the gated block; partial: twice as large.
 cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk_matrix &dh, const emtk_matrix &gate,
                                const emtk_matrix &up, void *dg, void *du, int64_t d_ld, const emtk_matrix &h,
-                               float *db_gate, float *db_up, float *partial, int sms, cudaStream_t s);
+                               float *db_gate, float *db_up, float *partial, SlopeRange *range, int sms, cudaStream_t s);
 cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
                          cudaStream_t s);
 // to = the values of from (a checkpoint, or a 16-bit matrix as it is), for up

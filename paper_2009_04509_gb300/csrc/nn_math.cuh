@@ -123,6 +123,20 @@ __device__ __forceinline__ void apply_act(int act, float (&v)[N]) {
     }
 }
 
+// ---- slopes held in fp16 for the products of a backward call
+// Power of two by which they are stored, from the bits of the largest finite |dz| (or
+// |dg| and |du|): 1 where fp16 holds that to full precision with room below it (an
+// element is off by 2^-25 beside its rounding: 2^-19 of the largest or less), or it is 0.
+// Else the larger is brought to 2^14 .. 2^15, as far as the power and its inverse are
+// normal numbers.
+__device__ __forceinline__ float slope_scale(uint32_t peak0, uint32_t peak1) {
+    const uint32_t low = __float_as_uint(0.015625f), high = __float_as_uint(65504.f);
+    if ((peak0 == 0u || (peak0 >= low && peak0 <= high)) && (peak1 == 0u || (peak1 >= low && peak1 <= high))) return 1.f;
+    return __uint_as_float(min(127u + 14u + 127u - (max(peak0, peak1) >> 23), 127u + 112u) << 23);
+}
+// 1 / slope_scale.
+__device__ __forceinline__ float slope_unscale(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }
+
 // ---- 8-bit checkpoints (emtk_matrix in include/emtk.h)
 // Scale byte of a block whose largest finite magnitude is `top`: with
 // 2^(byte - 127) <= top / 64 < 2^(byte - 126) the quotient is in [64, 128);

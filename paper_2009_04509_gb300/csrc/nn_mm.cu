@@ -114,6 +114,7 @@ struct MmParams {
     MmWork piece[kMaxPieces];
     int pieces;
     int *status;
+    SlopeRange *range;  // to be reset, or null
     int64_t timeout_ns;
     int debug_stall;
 };
@@ -220,6 +221,7 @@ struct Rows {
     int lane;
     int act;
     bool has_bias, out_f32;
+    float unscale;  // of fp16 slopes' sums, else 1
     uint32_t out_low, residual_low;  // row_bits
     void *out, *residual;
     int64_t out_ld, residual_ld;
@@ -227,6 +229,7 @@ struct Rows {
         act = e.act;
         has_bias = e.bias[0] != nullptr;
         out_f32 = e.out_f32 != 0;
+        unscale = e.range ? e.range->unscale : 1.f;
         out = e.out.d;
         out_ld = e.out.ld;
         out_low = row_bits(out, out_ld, out_f32 ? 4 : 2);
@@ -343,7 +346,11 @@ __device__ __forceinline__ void add_bias(const float *bias, float (&v)[32]) {
 
 // Gradients: nothing but the sums.
 template <bool F16, int N>
-__device__ __forceinline__ void finish_plain(const Rows &w, int64_t c0, int64_t cols, const float (&v)[N]) {
+__device__ __forceinline__ void finish_plain(const Rows &w, int64_t c0, int64_t cols, float (&v)[N]) {
+    if (F16 && w.unscale != 1.f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] *= w.unscale;
+    }
     if (w.out_f32)
         store32(static_cast<float *>(w.out), w.out_ld, w.out_low, w, c0, cols, v);
     else
@@ -475,6 +482,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     pdl_wait();
+    if (KIND == kPlain && F16 && p.range && blockIdx.x == 0 && threadIdx.x < 2) p.range->peak[threadIdx.x] = 0u;
 
     if (warp == 0) {
         // ---------------------------------------------------- TMA producer
@@ -741,6 +749,11 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEp
         for (int h = 0; h < (GATED ? 2 : 1); ++h)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[h][j] += __shfl_xor_sync(0xffffffffu, v[h][j], d);
+    if (KIND == kPlain && F16 && e.range) {
+        const float unscale = e.range->unscale;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[0][j] *= unscale;
+    }
     const bool writes = in && mine == 0;
 #pragma unroll
     for (int h = 0; h < (GATED ? 2 : 1); ++h) {
@@ -908,6 +921,7 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
     }
     p.pieces = plan.pieces;
     p.status = nn->status;
+    p.range = jobs[0].epi.range ? nn->range : nullptr;
     p.timeout_ns = nn->timeout_ns;
     p.debug_stall = nn->debug_stall;
     bool plain = !gated, kept = false;

@@ -819,3 +819,133 @@ def test_gelu_in_its_tail(lib, nn, dtype):
     want = phi + z64 * e
     lib.emtk_dense_backward(nn, torch.ones((n, 1), dtype=dt, device="cuda"), None, one, act="gelu", pre=z.view(n, 1), dx=y)
     close(y[:, 0], want, bound(want, phi + z64.abs() * e), "slope")
+
+
+# --------------------------------------------- slopes beyond fp16's range
+def stored_slopes(v, err, peak):
+    """Error of dz, dg or du as the products take them in fp16: 2^-11 of the value and 2^-19 of the call's largest."""
+    return err + U["fp16"] * (v.abs() + err) + 2.0 ** -19 * peak
+
+
+@pytest.mark.parametrize("shape", [(33, 40, 72), (300, 264, 520), (257, 129, 65), (3000, 40, 24), (600, 85, 701)])
+@pytest.mark.parametrize("size", [2.0 ** -23, 2.0 ** -12, 1.0, 2.0 ** 8, 2.0 ** 13])
+def test_fp16_gated_slopes_of_any_size(lib, nn, shape, size):
+    """dg = dh u act'(g) and du = dh act(g) where fp16 would lose them, below its least or beyond its largest
+    number, and the gradients are ordinary ones: dh and u of `size` / 2 .. `size`, x and the weights so that
+    dx and the fp32 dw fit.  The call before and the call after are not affected."""
+    m, k, f = shape
+    g = gen(m + k)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    dt = torch.float16
+    signs = lambda *s: torch.sign(r(*s)) * (0.5 + 0.5 * torch.rand(*s, generator=g, device="cuda"))  # noqa: E731
+    small = min(1.0, 2.0 ** -6 / size)  # of x and the weights
+    dh, up, gate = (signs(m, f) * size).to(dt), (signs(m, f) * size).to(dt), r(m, f).to(dt)
+    x, wg, wu = (r(*s).mul_(small).to(dt) for s in ((m, k), (f, k), (f, k)))
+    new = lambda: [torch.empty((m, k), dtype=dt, device="cuda")] + \
+        [torch.empty(s, device="cuda") for s in ((f, k), (f, k), (f,), (f,))]  # noqa: E731
+    call = lambda d, u, o: lib.emtk_gated_backward(nn, d, gate, u, x, wg, wu, act="silu", dx=o[0], dw_gate=o[1], dw_up=o[2],
+                                                   db_gate=o[3], db_up=o[4])  # noqa: E731
+    plain = r(m, f).to(dt), r(m, f).to(dt)
+    before, out, after = new(), new(), new()
+    call(*plain, before)
+    call(dh, up, out)
+    call(*plain, after)
+    assert all(torch.equal(a, b) for a, b in zip(before, after))
+    d, u64, g64 = dh.double(), up.double(), gate.double()
+    a, s = act64("silu", g64), slope64("silu", g64)
+    ea, es = act_err(g64, a, 0 * g64), act_err(g64, s, 0 * g64)
+    dg, du = d * u64 * s, d * a
+    eg, eu = (d * u64).abs() * es + 2 * E * dg.abs(), d.abs() * ea + E * du.abs()
+    peak = torch.maximum(dg.abs().max(), du.abs().max())
+    rg, ru = stored_slopes(dg, eg, peak), stored_slopes(du, eu, peak)
+    wg64, wu64, x64 = wg.double(), wu.double(), x.double()
+    want = dg @ wg64 + du @ wu64
+    mag = (dg.abs() + rg) @ wg64.abs() + (du.abs() + ru) @ wu64.abs()
+    close(out[0], want, stored(rg @ wg64.abs() + ru @ wu64.abs() + (2 * f + 1) * E * mag, want, "fp16"), "dx")
+    for name, got, v, e, rounded, db in (("gate", out[1], dg, eg, rg, out[3]), ("up", out[2], du, eu, ru, out[4])):
+        want = v.t() @ x64
+        err = rounded.t() @ x64.abs() + (m + 1) * E * ((v.abs() + rounded).t() @ x64.abs())
+        close(got, want, err + E * want.abs(), "dw_" + name)
+        close(db, v.sum(0), e.sum(0) + m * E * (v.abs() + e).sum(0), "db_" + name)
+
+
+@pytest.mark.parametrize("shape", [(33, 40, 72), (300, 264, 520), (257, 129, 65), (3000, 40, 24), (5000, 33, 8)])
+@pytest.mark.parametrize("size", [2.0 ** -22, 2.0 ** -14, 2.0 ** -6, 60000.0])
+@pytest.mark.parametrize("act", ["gelu", "sigmoid"])
+def test_fp16_dense_slopes_of_any_size(lib, nn, shape, size, act):
+    """dz = dy act'(z) likewise: gelu's slope, 1.13 at its largest, takes 60000 beyond fp16."""
+    m, k, n = shape
+    g = gen(m + k)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    dt = torch.float16
+    dy = (torch.sign(r(m, n)) * (0.9 + 0.1 * torch.rand(m, n, generator=g, device="cuda")) * size).to(dt)
+    z = (1.4 + 0.2 * r(m, n)).to(dt)
+    small = min(1.0, 2.0 ** -6 / size)
+    x, w = r(m, k).mul_(small).to(dt), r(n, k).mul_(small).to(dt)
+    dx, dw = torch.empty((m, k), dtype=dt, device="cuda"), torch.empty((n, k), device="cuda")
+    lib.emtk_dense_backward(nn, dy, x, w, act=act, pre=z, dx=dx, dw=dw)
+    s, d = slope64(act, z.double()), dy.double()
+    dz, e = d * s, d.abs() * act_err(z.double(), s, 0 * s)
+    rounded = stored_slopes(dz, e, dz.abs().max())
+    x64, w64 = x.double(), w.double()
+    want = dz @ w64
+    err = rounded @ w64.abs() + (n + 1) * E * ((dz.abs() + rounded) @ w64.abs())
+    close(dx, want, stored(err, want, "fp16"), "dx")
+    want = dz.t() @ x64
+    close(dw, want, rounded.t() @ x64.abs() + (m + 1) * E * ((dz.abs() + rounded).t() @ x64.abs()) + E * want.abs(), "dw")
+
+
+def test_fp16_slopes_from_checkpoints_in_a_graph(lib):
+    """Sizes that only the device knows: a captured call on ordinary values is replayed with u in 8 bits near
+    10^10, with dh near the least number, with an infinity in one row, and on the ordinary values again."""
+    h = lib.emtk_nn_create(workspace_bytes=64 << 20)
+    m, k, f = 200, 96, 72
+    dt = torch.float16
+    g = gen(6)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    dh, gate, x, w = r(m, f).to(dt), r(m, f), r(m, k).to(dt), (r(f, k) / 8).to(dt)
+    gq, uq = lib.emtk_q8_empty(m, f), lib.emtk_q8_empty(m, f)
+    u = r(m, f)
+    lib.emtk_pack8(h, gate.to(dt), gq)
+    lib.emtk_pack8(h, u.to(dt), uq)
+    dx, dwg, dwu = torch.empty((m, k), dtype=dt, device="cuda"), torch.empty((f, k), device="cuda"), torch.empty((f, k), device="cuda")
+    step = lambda: lib.emtk_gated_backward(h, dh, gq, uq, x, w, w, act="silu", dx=dx, dw_gate=dwg, dw_up=dwu)  # noqa: E731
+    step()
+    ordinary = [v.clone() for v in (dx, dwg, dwu)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+
+    def check():
+        g64, u64, d = q8_values(gq, f), q8_values(uq, f), dh.double()
+        a, s = act64("silu", g64), slope64("silu", g64)
+        dg, du = d * u64 * s, d * a
+        eg, eu = (d * u64).abs() * act_err(g64, s, 0 * s) + 2 * E * dg.abs(), d.abs() * act_err(g64, a, 0 * a) + E * du.abs()
+        peak = torch.maximum(dg.abs().max(), du.abs().max())
+        x64 = x.double()
+        for got, v, e in ((dwg, dg, eg), (dwu, du, eu)):
+            rounded = stored_slopes(v, e, peak)
+            want = v.t() @ x64
+            close(got, want, rounded.t() @ x64.abs() + (m + 2) * E * ((v.abs() + rounded).t() @ x64.abs()), "dw")
+
+    kept = dh.clone()
+    lib.emtk_pack8(h, (u * 1e10).to(torch.bfloat16), uq)
+    graph.replay()
+    check()
+    lib.emtk_pack8(h, u.to(dt), uq)
+    dh.copy_(kept * 2.0 ** -17)
+    graph.replay()
+    check()
+    dh.copy_(kept)
+    dh[17, 3] = float("inf")
+    graph.replay()
+    rest = torch.arange(m, device="cuda") != 17
+    assert not bool(torch.isfinite(dx[17]).all()) and torch.equal(dx[rest], ordinary[0][rest])
+    dh.copy_(kept)
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip((dx, dwg, dwu), ordinary))
+    assert lib.emtk_nn_check(h) == lib.EMTK_OK
+    torch.cuda.synchronize()
+    del graph
+    lib.emtk_nn_destroy(h)
