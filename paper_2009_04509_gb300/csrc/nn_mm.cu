@@ -101,7 +101,7 @@ struct MmWork {  // one piece of the plan
     CUtensorMap a[2], b[2];
     MmEpilogue epi;
     float *partial;  // not null: [tile of the piece][part][256][TN] fp32 sums
-    int M, N, K;
+    int M, N;
     int a_across, b_across;
     Raster raster;
     int tile0, tiles, parts;
@@ -904,7 +904,6 @@ cudaError_t launch_mm(const MmJob *jobs, int n, const MmPlan &plan, const emtk_n
         w.partial = c.parts > 1 ? static_cast<float *>(partial) + c.part_at : nullptr;
         w.M = j.M;
         w.N = j.N;
-        w.K = j.K;
         w.a_across = j.a[0].across;
         w.b_across = j.b[0].across;
         w.raster = {t.tiles_m, t.tiles_n, Divisor((uint32_t)(8 * t.tiles_n)), Divisor((uint32_t)std::max(1, t.tiles_m % 8))};

@@ -45,7 +45,7 @@ struct Shape {
 struct SkinnyParams {
     CUtensorMap w[2], x;
     MmEpilogue epi;
-    int M, N, K, parts, chunks_per_part, chunks;
+    int M, N, parts, chunks_per_part, chunks;
     int *status;
     int64_t timeout_ns;
     int debug_stall;
@@ -378,7 +378,6 @@ cudaError_t launch_skinny(const MmJob &j, const emtk_nn *nn, cudaStream_t s) {
     p.epi = j.epi;
     p.M = j.M;
     p.N = j.N;
-    p.K = j.K;
     p.chunks = chunks_of(j);
     p.parts = parts_of(j, nn->sm_count);
     p.chunks_per_part = (p.chunks + p.parts - 1) / p.parts;

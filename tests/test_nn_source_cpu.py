@@ -27,3 +27,29 @@ def test_no_cta_of_a_pair_leaves_before_its_arrivals():
     assert "rank" not in filled and "rank" not in tail  # both CTAs run these
     # the accumulators' last phases: the epilogue waits for every tile's
     assert committed <= waited(filled) | waited(tail) | (waited(epilogue) & {"kBarAccFull"})
+
+
+def _sources():
+    return {n: open(os.path.join(CSRC, n)).read() for n in sorted(os.listdir(CSRC)) if n.startswith("nn_")}
+
+
+def test_every_device_function_of_the_layers_is_called():
+    text = "\n".join(_sources().values())
+    names = set(re.findall(r"__(?:device|global)__[^;{}=]*?\b([a-z]\w*)\s*\(", re.sub(r"__launch_bounds__\([^)]*\)|__cluster_dims__\([^)]*\)", "", text)))
+    assert len(names) > 60
+    assert [n for n in sorted(names) if len(re.findall(rf"\b{n}\b", text)) < 2] == []
+
+
+def test_every_field_of_a_kernels_parameters_is_read():
+    """A field of a structure that is passed to a kernel by value is read somewhere, not only set."""
+    src = _sources()
+    for name, struct in (("nn_mm.cu", "MmWork"), ("nn_mm.cu", "MmParams"), ("nn_skinny.cu", "SkinnyParams"),
+                         ("nn_rows.cu", "RowsParams"), ("nn_pointwise.cu", "SlopeArgs"), ("nn_pointwise.cu", "PackArgs")):
+        text = re.sub(r"//[^\n]*|\bj\.\w+", "", src[name])  # j: the job, whose fields have the same names
+        body = re.search(rf"struct {struct} {{(.*?)\n}};", text, re.S).group(1)
+        fields = re.findall(r"\*?\b(\w+)(?:\[\w+\])*\s*[,;]", body)
+        assert len(fields) > 4, struct
+        for f in fields:
+            uses = len(re.findall(rf"(?:\.|->){f}\b", text))
+            sets = len(re.findall(rf"(?:\.|->){f}(?:\[\w+\])*\s*=[^=]", text))
+            assert uses > sets, f"{struct}.{f}"
