@@ -409,11 +409,11 @@ def _type_of(t, what: str, f32: bool = False) -> int:
     return v
 
 
-def _mat(t, rows: int, cols: int, dtype, what: str) -> tuple:
-    """(d, ld, d_scale, ld_scale) of a [rows][cols] CUDA tensor of dtype; absent for None."""
+def _mat(on, t, rows: int, cols: int, dtype, what: str) -> tuple:
+    """(d, ld, d_scale, ld_scale) of a [rows][cols] tensor of dtype on CUDA device `on`; absent for None."""
     if t is None:
         return _ABSENT
-    if t.dtype is dtype and t.is_cuda:
+    if t.dtype is dtype and t.get_device() == on:
         shape = t.shape
         if len(shape) == 2 and shape[0] == rows and shape[1] == cols:
             ld, unit = t.stride()
@@ -422,24 +422,24 @@ def _mat(t, rows: int, cols: int, dtype, what: str) -> tuple:
             if (unit == 1 or cols <= 1) and (ld >= cols or rows <= 1):
                 return (t.data_ptr(), max(ld, cols), 0, 0)  # one row or column: its stride says nothing
             raise ValueError(f"{what}: strides {t.stride()}: a row's elements must be neighbours and rows apart")
-    raise ValueError(f"{what}: expected a CUDA tensor {(rows, cols)} of {dtype}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    raise ValueError(f"{what}: expected a tensor {(rows, cols)} of {dtype} on CUDA device {on}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
-def _mat8(t, rows: int, cols: int, dtype, what: str) -> tuple:
+def _mat8(on, t, rows: int, cols: int, dtype, what: str) -> tuple:
     """_mat of a tensor that may be a Q8."""
     if not isinstance(t, Q8):
-        return _mat(t, rows, cols, dtype, what)
+        return _mat(on, t, rows, cols, dtype, what)
     import torch
-    d, ld, _, _ = _mat(t.codes, rows, cols, torch.int8, what)
-    s, lds, _, _ = _mat(t.scales, rows, (cols + 31) // 32, torch.uint8, what)
+    d, ld, _, _ = _mat(on, t.codes, rows, cols, torch.int8, what)
+    s, lds, _, _ = _mat(on, t.scales, rows, (cols + 31) // 32, torch.uint8, what)
     return (d, ld, s, lds)
 
 
-def _vec(t, n: int, what: str, f32: bool = False) -> int:
+def _vec(on, t, n: int, what: str, f32: bool = False) -> int:
     if t is None:
         return 0
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or not t.is_cuda:
-        raise ValueError(f"{what}: expected a contiguous CUDA vector of {n}")
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.get_device() != on:
+        raise ValueError(f"{what}: expected a contiguous vector of {n} on CUDA device {on}, got {tuple(t.shape)} on {t.device}")
     if f32 and _type_of(t, what, True) != EMTK_TYPE_F32:
         raise ValueError(f"{what}: dtype {t.dtype}, expected float32")
     return t.data_ptr()
@@ -459,6 +459,19 @@ def _current(t, stream) -> int:
     return _stream(stream)
 
 
+_nn_devices = {}  # layer handle -> its device
+
+
+def _device_of(nn, t) -> int:
+    """The device that a call's tensors must be on: the handle's (of a handle made elsewhere, t's)."""
+    device = _nn_devices.get(nn)
+    if device is None:
+        device = t.get_device()
+        if device < 0:
+            raise ValueError(f"expected CUDA tensors, got one on {t.device}")
+    return device
+
+
 def _act_code(act: str) -> int:
     if act not in ACTS:
         raise ValueError(f"act: {act!r} is none of {tuple(ACTS)}")
@@ -467,14 +480,16 @@ def _act_code(act: str) -> int:
 
 def emtk_nn_create(device: int = 0, workspace_bytes: int = 0, wait_timeout_ns: int = 2_000_000_000,
                    debug_stall: bool = False):
-    """A layer handle (see include/emtk.h), an int."""
+    """A layer handle (see include/emtk.h), an int.  The tensors of its calls are on ``device``."""
     out = _vp()
     _check(load_library().emtk_nn_create(int(device), int(workspace_bytes), int(wait_timeout_ns),
                                          int(bool(debug_stall)), ctypes.byref(out)), "emtk_nn_create")
+    _nn_devices[out.value] = int(device)
     return out.value
 
 
 def emtk_nn_destroy(nn) -> None:
+    _nn_devices.pop(nn, None)
     _check(load_library().emtk_nn_destroy(nn), "emtk_nn_destroy")
 
 
@@ -489,11 +504,12 @@ def emtk_dense(nn, x, w, y, bias=None, act: str = "none", residual=None, pre=Non
     the activation's input for emtk_dense_backward."""
     (m, k), n = x.shape, w.shape[0]
     dt = x.dtype
+    on = _device_of(nn, x)
     args = _PACK_DENSE.pack(m, n, k, _act_code(act), _type_of(x, "x"),
                             0 if bias is None else _type_of(bias, "bias", True),
-                            *_mat(x, m, k, dt, "x"), *_mat(w, n, k, dt, "w"), *_mat(y, m, n, dt, "y"),
-                            *_mat(residual, m, n, dt, "residual"), *_mat8(pre, m, n, dt, "pre"),
-                            _vec(bias, n, "bias"))
+                            *_mat(on, x, m, k, dt, "x"), *_mat(on, w, n, k, dt, "w"), *_mat(on, y, m, n, dt, "y"),
+                            *_mat(on, residual, m, n, dt, "residual"), *_mat8(on, pre, m, n, dt, "pre"),
+                            _vec(on, bias, n, "bias"))
     _check(load_library().emtk_dense(nn, args, _current(x, stream)), "emtk_dense")
 
 
@@ -501,14 +517,15 @@ def emtk_dense_backward(nn, dy, x, w, act: str = "none", pre=None, dx=None, dw=N
     """Gradients of emtk_dense from dy [m][n]: dx [m][k], dw [n][k] (x's dtype or float32), db [n] float32,
     each optional.  x and pre may be Q8; x may be None without dw, w None without dx."""
     (m, n), dt = dy.shape, dy.dtype
+    on = _device_of(nn, dy)
     like = w if w is not None else dw if dw is not None else x.codes if isinstance(x, Q8) else x
     k = 0 if like is None else like.shape[1]
     args = _PACK_DENSE_GRAD.pack(m, n, k, _act_code(act), _type_of(dy, "dy"),
                                  0 if dw is None else _type_of(dw, "dw", True),
-                                 *_mat(dy, m, n, dt, "dy"), *_mat8(x, m, k, dt, "x"), *_mat(w, n, k, dt, "w"),
-                                 *_mat8(pre, m, n, dt, "pre"), *_mat(dx, m, k, dt, "dx"),
-                                 *_mat(dw, n, k, None if dw is None else dw.dtype, "dw"),
-                                 _vec(db, n, "db", True))
+                                 *_mat(on, dy, m, n, dt, "dy"), *_mat8(on, x, m, k, dt, "x"), *_mat(on, w, n, k, dt, "w"),
+                                 *_mat8(on, pre, m, n, dt, "pre"), *_mat(on, dx, m, k, dt, "dx"),
+                                 *_mat(on, dw, n, k, None if dw is None else dw.dtype, "dw"),
+                                 _vec(on, db, n, "db", True))
     _check(load_library().emtk_dense_backward(nn, args, _current(dy, stream)), "emtk_dense_backward")
 
 
@@ -518,14 +535,15 @@ def emtk_gated(nn, x, w_gate, w_up, h, bias_gate=None, bias_up=None, act: str = 
     [m][f] (tensors or Q8s) receive the two factors' inputs for emtk_gated_backward."""
     (m, k), f = x.shape, w_gate.shape[0]
     dt = x.dtype
+    on = _device_of(nn, x)
     bias_type = 0 if bias_gate is None else _type_of(bias_gate, "bias_gate", True)
     if bias_gate is not None and bias_up is not None and bias_gate.dtype is not bias_up.dtype:
         raise ValueError("bias_up: its dtype must be bias_gate's")
     args = _PACK_GATED.pack(m, f, k, _act_code(act), _type_of(x, "x"), bias_type,
-                            *_mat(x, m, k, dt, "x"), *_mat(w_gate, f, k, dt, "w_gate"), *_mat(w_up, f, k, dt, "w_up"),
-                            *_mat(h, m, f, dt, "h"), *_mat8(gate, m, f, dt, "gate"),
-                            *_mat8(up, m, f, dt, "up"), _vec(bias_gate, f, "bias_gate"),
-                            _vec(bias_up, f, "bias_up"))
+                            *_mat(on, x, m, k, dt, "x"), *_mat(on, w_gate, f, k, dt, "w_gate"), *_mat(on, w_up, f, k, dt, "w_up"),
+                            *_mat(on, h, m, f, dt, "h"), *_mat8(on, gate, m, f, dt, "gate"),
+                            *_mat8(on, up, m, f, dt, "up"), _vec(on, bias_gate, f, "bias_gate"),
+                            _vec(on, bias_up, f, "bias_up"))
     _check(load_library().emtk_gated(nn, args, _current(x, stream)), "emtk_gated")
 
 
@@ -534,6 +552,7 @@ def emtk_gated_backward(nn, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx
     """Gradients of emtk_gated from dh [m][f] and the gate and up it kept: dx [m][k], dw_gate and dw_up [f][k]
     (x's dtype or float32), db_gate and db_up [f] float32, and h [m][f] once more; each optional."""
     (m, f), dt = dh.shape, dh.dtype
+    on = _device_of(nn, dh)
     like = w_gate if w_gate is not None else dw_gate if dw_gate is not None else x.codes if isinstance(x, Q8) else x
     k = 0 if like is None else like.shape[1]
     if dw_gate is not None and dw_up is not None and dw_gate.dtype is not dw_up.dtype:
@@ -541,27 +560,29 @@ def emtk_gated_backward(nn, dh, gate, up, x, w_gate, w_up, act: str = "silu", dx
     dwt = None if dw_gate is None else dw_gate.dtype
     args = _PACK_GATED_GRAD.pack(m, f, k, _act_code(act), _type_of(dh, "dh"),
                                  0 if dw_gate is None else _type_of(dw_gate, "dw_gate", True),
-                                 *_mat(dh, m, f, dt, "dh"), *_mat8(gate, m, f, dt, "gate"),
-                                 *_mat8(up, m, f, dt, "up"), *_mat8(x, m, k, dt, "x"),
-                                 *_mat(w_gate, f, k, dt, "w_gate"), *_mat(w_up, f, k, dt, "w_up"),
-                                 *_mat(dx, m, k, dt, "dx"), *_mat(dw_gate, f, k, dwt, "dw_gate"),
-                                 *_mat(dw_up, f, k, dwt, "dw_up"), *_mat(h, m, f, dt, "h"),
-                                 _vec(db_gate, f, "db_gate", True), _vec(db_up, f, "db_up", True))
+                                 *_mat(on, dh, m, f, dt, "dh"), *_mat8(on, gate, m, f, dt, "gate"),
+                                 *_mat8(on, up, m, f, dt, "up"), *_mat8(on, x, m, k, dt, "x"),
+                                 *_mat(on, w_gate, f, k, dt, "w_gate"), *_mat(on, w_up, f, k, dt, "w_up"),
+                                 *_mat(on, dx, m, k, dt, "dx"), *_mat(on, dw_gate, f, k, dwt, "dw_gate"),
+                                 *_mat(on, dw_up, f, k, dwt, "dw_up"), *_mat(on, h, m, f, dt, "h"),
+                                 _vec(on, db_gate, f, "db_gate", True), _vec(on, db_up, f, "db_up", True))
     _check(load_library().emtk_gated_backward(nn, args, _current(dh, stream)), "emtk_gated_backward")
 
 
 def emtk_pack8(nn, x, q: Q8, stream=None) -> None:
     """Keeps x [m][k] (bf16 or fp16) in the 8-bit checkpoint q."""
     (m, k), dt = x.shape, x.dtype
-    _check(load_library().emtk_pack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")),
-                                     _PACK_MATRIX.pack(*_mat8(q, m, k, dt, "q")), _current(x, stream)), "emtk_pack8")
+    on = _device_of(nn, x)
+    _check(load_library().emtk_pack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(on, x, m, k, dt, "x")),
+                                     _PACK_MATRIX.pack(*_mat8(on, q, m, k, dt, "q")), _current(x, stream)), "emtk_pack8")
 
 
 def emtk_unpack8(nn, q: Q8, x, stream=None) -> None:
     """The values that the 8-bit checkpoint q stands for, into x [m][k] (bf16 or fp16)."""
     (m, k), dt = x.shape, x.dtype
-    _check(load_library().emtk_unpack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat8(q, m, k, dt, "q")),
-                                       _PACK_MATRIX.pack(*_mat(x, m, k, dt, "x")), _current(x, stream)), "emtk_unpack8")
+    on = _device_of(nn, x)
+    _check(load_library().emtk_unpack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat8(on, q, m, k, dt, "q")),
+                                       _PACK_MATRIX.pack(*_mat(on, x, m, k, dt, "x")), _current(x, stream)), "emtk_unpack8")
 
 
 # ------------------------------------------------------------- test hooks

@@ -86,3 +86,71 @@ def test_binding_checks_shapes_before_the_library():
     for change in (dict(w=torch.zeros(6, 9, dtype=torch.bfloat16)), dict(act="tanh"), dict(x=x.float()), {}):
         with pytest.raises(ValueError):  # the last: tensors of the host
             emtk.emtk_dense(1, **dict(dict(x=x, w=w, y=y), **change))
+
+
+def test_binding_refuses_tensors_of_another_device(monkeypatch):
+    """A tensor of another GPU than the handle's is refused before the library sees its address, each argument
+    alone; all on the handle's are passed on.  Stand-ins for the tensors and the library: no GPU is needed."""
+    torch = pytest.importorskip("torch")
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                if name == "emtk_nn_create":
+                    args[-1]._obj.value = 4096 + args[0]
+                calls.append(name)
+                return 0
+            return call
+
+    class Tensor:
+        is_cuda = True
+
+        def __init__(self, *shape, dtype=torch.bfloat16, device=1):
+            self.shape, self.dtype, self.device_index, self.device = shape, dtype, device, f"cuda:{device}"
+
+        def get_device(self):
+            return self.device_index
+
+        def dim(self):
+            return len(self.shape)
+
+        def stride(self, i=None):
+            s = (self.shape[-1], 1) if len(self.shape) == 2 else (1,)
+            return s if i is None else s[i]
+
+        def data_ptr(self):
+            return 1 << 20
+
+    monkeypatch.setattr(emtk, "load_library", lambda path=None: Library())
+    m, k, n, f32 = 4, 8, 6, torch.float32
+    T = Tensor
+
+    def q8(rows, cols, device=1):
+        return emtk.Q8(T(rows, cols, dtype=torch.int8, device=device), T(rows, 1, dtype=torch.uint8, device=device))
+
+    nn = emtk.emtk_nn_create(1)
+    every = [
+        (emtk.emtk_dense, dict(x=T(m, k), w=T(n, k), y=T(m, n), bias=T(n), residual=T(m, n), pre=T(m, n))),
+        (emtk.emtk_dense, dict(x=T(m, k), w=T(n, k), y=T(m, n), pre=q8(m, n))),
+        (emtk.emtk_dense_backward, dict(dy=T(m, n), x=T(m, k), w=T(n, k), pre=T(m, n), dx=T(m, k), dw=T(n, k), db=T(n, dtype=f32))),
+        (emtk.emtk_gated, dict(x=T(m, k), w_gate=T(n, k), w_up=T(n, k), h=T(m, n), bias_gate=T(n), bias_up=T(n), gate=q8(m, n), up=q8(m, n))),
+        (emtk.emtk_gated_backward, dict(dh=T(m, n), gate=T(m, n), up=T(m, n), x=q8(m, k), w_gate=T(n, k), w_up=T(n, k), dx=T(m, k),
+                                        dw_gate=T(n, k), dw_up=T(n, k), db_gate=T(n, dtype=f32), db_up=T(n, dtype=f32), h=T(m, n))),
+        (emtk.emtk_pack8, dict(x=T(m, k), q=q8(m, k))),
+        (emtk.emtk_unpack8, dict(q=q8(m, k), x=T(m, k))),
+    ]
+    for call, args in every:
+        calls.clear()
+        call(nn, **args, stream=0)
+        assert calls == [call.__name__]
+        for name, t in args.items():
+            parts = [t] if not isinstance(t, emtk.Q8) else list(t)
+            for i, part in enumerate(parts):
+                other = T(*part.shape, dtype=part.dtype, device=0)
+                moved = other if not isinstance(t, emtk.Q8) else emtk.Q8(*(other if j == i else p for j, p in enumerate(parts)))
+                calls.clear()
+                with pytest.raises(ValueError):
+                    call(nn, **dict(args, **{name: moved}), stream=0)
+                assert calls == [], (call.__name__, name)
+    emtk.emtk_nn_destroy(nn)
