@@ -24,8 +24,8 @@
 // What bounds it.  A chunk of 64 steps of a 256-wide tile is 512 cycles of the
 // tensor pipe and takes 519 (bf16, measured in the loop); its 32 KB a CTA from L2
 // come just as fast, so a 128-wide tile's chunk, 24 KB, is bound by L2 (420 cycles
-// against 256 of the pipe).  16384 x 4096 -> 4096 with residual, bf16: 297 us, 1.85
-// PFLOP/s, tensor pipe 89% active.  8192 x 4096 -> 2 x 10240 gated: 693 us, 1.98
+// against 256 of the pipe).  16384 x 4096 -> 4096 with residual, bf16: 293 us, 1.88
+// PFLOP/s, tensor pipe 88% active (342 in a row, at the power limit).  8192 x 4096 -> 2 x 10240 gated: 693 us, 1.98
 // PFLOP/s.  20000 x 512 -> 2304 (dx) with 512 x 20000 x 2304 (dw): 60 us, 1.57
 // PFLOP/s; there the epilogue's 92 MB of stores take about as long as the MMAs.
 // A few tiles: 4 us for one, then about 0.2 us a chunk.

@@ -9,8 +9,8 @@
 // rows and needs a second kernel to join its split contraction.  Four rows a warp
 // and no unrolling measured best (4096 -> 2 x 10240 gated, one row, bf16: 25.4 us, 6.6
 // TB/s, with blocks of 8 warps 26.0; two or eight weight rows a warp 31.6, unrolled
-// twice 27.5).  HBM bounds it from 50 MB of weights on; 4096 -> 4096 takes 7.3 us, of
-// which 5 are its bytes.
+// twice 27.5).  HBM bounds it from 50 MB of weights on; 4096 -> 4096 takes 7.4 us with
+// the weights from HBM, of which 5 are their bytes (5.8 from L2).
 #include <algorithm>
 
 #include "emtk_internal.h"
@@ -168,9 +168,12 @@ bool wide_operands(const MmJob &j) {
 }  // namespace
 
 // Up to 2 rows; of 3 and 4 only where TMA cannot read the weights as they lie and
-// nn_skinny.cu would have to copy them first.  4096 -> 2 x 10240 gated, wide
-// rows, bf16: 1 row 25.4 us here, 2 rows 29.0, 4 rows 52; nn_skinny.cu 29.4 for 3 to 8
-// (4096 -> 4096 dense: 7.3, 7.4, 13 and 9.5).
+// nn_skinny.cu would have to copy them first.  bf16, weights from HBM, 1, 2, 3, 4 rows:
+//                                  here                nn_skinny.cu
+//   4096 -> 2 x 10240 gated, wide  25.3 28.7 31.9 34.9 29.9 31.2 30.6 30.2
+//     rows of 4097 elements        70   88   64   97   88 for each
+//   4096 -> 4096 dense, wide       7.4  7.4  9.9  11.6 9.5 for each
+//     rows of 4097 elements        25   32   18   21   17.6 for each: the copy stays in L2
 // Checkpoints are left to the kernels that hold 32 columns of a row together.
 bool few_rows(const MmJob &j) {
     return j.M <= 4 && (j.M <= 2 || !wide_operands(j)) && !j.epi.saved[0].d_scale && !j.epi.saved[1].d_scale;
@@ -191,8 +194,8 @@ cudaError_t launch_rows(const MmJob &j, int sms, cudaStream_t s) {
     p.K = j.K;
     // Warps of a group: one for every four steps of 256 (a longer way leaves the end of
     // the launch uneven), and more down to a step each while an SM has fewer than 16.
-    // One row, bf16: 8192 -> 2 x 8192 with 8 warps 39.6 us, 4 40.6, 2 44.7; 4096 -> 4096
-    // with 4 warps 7.3 us, 8 7.6, 2 8.8; 1024 -> 2 x 4096 with 2 4.7 us, 4 5.0.
+    // One row, bf16, the same weights each time: 8192 -> 2 x 8192 with 8 warps 39.6 us, 4
+    // 40.6, 2 44.7; 4096 -> 4096 with 4 warps 7.3 us in a row, 8 7.6, 2 8.8; 1024 -> 2 x 4096 with 2 4.7 us, 4 5.0.
     const int out = gated ? kHeld / 2 : kHeld;
     const int64_t groups = ((int64_t)j.N + out - 1) / out;
     while (p.split_log2 < 3 && (1024 << (p.split_log2 + 1)) <= j.K) ++p.split_log2;

@@ -10,9 +10,9 @@
 // memory, and every CTA adds the cluster's sums for its share of the rows, in
 // rank order, over distributed shared memory; no second kernel, no workspace.
 //
-// HBM bounds it.  4096 -> 2 x 10240 gated, bf16 (168 MB of weights): 29.4 us for 3 to 8
-// rows, 29.6 for 16, 33 for 64, 39 for 128 (5.7, 5.7, 5.0 and 4.3 TB/s); 4096 -> 4096
-// dense: 9.5 us for 8 rows.  With all CTAs starting at the same chunk 16 rows took 56
+// HBM bounds it.  4096 -> 2 x 10240 gated, bf16 (168 MB of weights, none of them in L2):
+// 30.4 us for 3 rows, 31.3 for 8, 32.5 for 16, 33.8 for 64, 38.7 for 128 (5.5, 5.4, 5.2,
+// 5.0 and 4.3 TB/s); 4096 -> 4096 dense: 9.8 us for 8 rows.  With all CTAs starting at the same chunk 16 rows took 56
 // us, and with a thread finishing one column, its cluster's sums one after another, 64
 // rows took 38.  What is left to the copy's 6.8 TB/s is the ramp and, from 32 rows on,
 // the epilogue and x's tiles.
