@@ -56,7 +56,8 @@ struct MmOperand {
 
 // Slopes dz (dg and du) in fp16: their largest finite magnitudes (zero between calls:
 // the products, which come last, reset them), and the inverse of the power of two by
-// which they are stored (nn_math.cuh), which the products' sums take.
+// which they are stored (nn_math.cuh), which the products' sums take.  Kernels in a row
+// write and read the one line that this is in, so they read it from L2.
 struct SlopeRange {
     uint32_t peak[2];
     float unscale;

@@ -229,7 +229,7 @@ struct Rows {
         act = e.act;
         has_bias = e.bias[0] != nullptr;
         out_f32 = e.out_f32 != 0;
-        unscale = e.range ? e.range->unscale : 1.f;
+        unscale = e.range ? __ldcg(&e.range->unscale) : 1.f;
         out = e.out.d;
         out_ld = e.out.ld;
         out_low = row_bits(out, out_ld, out_f32 ? 4 : 2);
@@ -750,7 +750,7 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ MmEp
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[h][j] += __shfl_xor_sync(0xffffffffu, v[h][j], d);
     if (KIND == kPlain && F16 && e.range) {
-        const float unscale = e.range->unscale;
+        const float unscale = __ldcg(&e.range->unscale);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[0][j] *= unscale;
     }

@@ -254,7 +254,7 @@ struct Ranged {
     // false: there is nothing to do again
     __device__ __forceinline__ bool start(const SlopeArgs &a) {
         if (!F16 || !a.again) return true;
-        scale = slope_scale(a.range->peak[0], a.range->peak[1]);
+        scale = slope_scale(__ldcg(a.range->peak), __ldcg(a.range->peak + 1));
         if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.range->unscale = slope_unscale(scale);
         return scale != 1.f;
     }
