@@ -188,7 +188,7 @@ def prepare(case, seed):
             s["dlast"] = _matrix(g, seqs, n, torch.float32, 0, 0.1) if case["state"] else None
             s["df"], s["dx"], s["do"] = like(), like(), like() if gated else None
             s["dstate"] = torch.empty((seqs, n), dtype=torch.float32, device="cuda")
-            s["states"] = torch.empty((m // 256 + seqs, n), dtype=torch.float32, device="cuda")
+            s["states"] = torch.empty((m // 128 + seqs, n), dtype=torch.float32, device="cuda")
     return s
 
 
