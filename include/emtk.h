@@ -530,6 +530,171 @@ EMTK_API emtk_status emtk_unpack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type t
                                   const emtk_matrix *x, emtk_stream stream);
 
 /* ------------------------------------------------------------------------
+ * Around a network's products: residual norms, dropout, a gated recurrence
+ * along sequences and log probabilities.
+ *
+ * What a deeper or sequential network has beside its dense layers and gated
+ * blocks: the norms before and after a block with its gate, dropout and
+ * residual sum, a recurrence that carries a state along the ticks of a wire or
+ * the tokens of a text, and the loss or the answer at its end.  Matrices,
+ * types, handles, streams, workspaces and refusals are as for the layers
+ * above; a matrix here is never an 8-bit checkpoint.  Arithmetic, sums and
+ * states are fp32 and every output is rounded once.  Outputs must not overlap
+ * inputs or each other, except where an entry says so.
+ * -------------------------------------------------------------------- */
+
+/* Dropout's random numbers: element (i, j) of a matrix has 16 bits of the
+ * counter-based generator Philox4x32-10 (Salmon et al. 2011), key (seed's
+ * lower and upper word), counter (j / 8, i, lower and upper word of offset +
+ * *d_offset): the word (j % 8) / 2 of its four, its lower half where j is even.
+ * The element becomes 0 where those are below t = round(65536 p) (to even at a
+ * tie), and is multiplied by 65536 / (65536 - t) elsewhere.  No mask is stored: a
+ * backward pass is given the same numbers.  0 <= p < 1, t at most 65535; p = 0
+ * drops nothing.  d_offset, 8-byte aligned, lets a captured call take other
+ * numbers at each replay; NULL adds nothing. */
+typedef struct {
+    uint64_t seed, offset;
+    const uint64_t *d_offset;
+    float p;
+    int32_t reserved;
+} emtk_drop;
+
+/* y = x under dropout; its backward pass is the same call from dy to dx.  y may
+ * be x itself (same address, same ld). */
+EMTK_API emtk_status emtk_dropout(emtk_nn *nn, int32_t m, int32_t n, emtk_type type, const emtk_matrix *x,
+                                  const emtk_matrix *y, const emtk_drop *drop, emtk_stream stream);
+
+/* Norms over a row of n values:
+ *   RMS:   x / sqrt(mean(x^2) + eps) * weight + bias
+ *   LAYER: (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight + bias
+ * weight and bias [n] of the call's type or F32 (param_type), or NULL for 1 and
+ * 0.  eps >= 0. */
+typedef enum { EMTK_NORM_NONE = 0, EMTK_NORM_RMS = 1, EMTK_NORM_LAYER = 2 } emtk_norm_kind;
+typedef struct {
+    int32_t kind, param_type;
+    float eps;
+    int32_t reserved;
+    const void *weight, *bias;
+} emtk_norm;
+
+/* The seam between two blocks of a network, in one pass:
+ *   y = scale * residual + gate * dropout(post(block)),   h = pre(y)
+ * with the norm `post` after the block before and `pre` before the next one.
+ * All [m][n], n <= 16384, but gate's rows: row i takes its row i / gate_every
+ * (gate_every = m: one row for all; it has one at least).  Absent parts have d == NULL: no residual, no block (then
+ * no post, gate or drop either), a gate of 1, y not written; h is given where
+ * pre is a norm, and only there.  drop may have p = 0.  h is of the unrounded
+ * y.  y may be the residual itself (same address, same ld). */
+typedef struct {
+    int32_t m, n, type, gate_every;
+    float scale;
+    int32_t reserved;
+    emtk_norm post, pre;
+    emtk_drop drop;
+    emtk_matrix residual, block, gate, y, h;
+} emtk_residual_norm_args;
+EMTK_API emtk_status emtk_residual_norm(emtk_nn *nn, const emtk_residual_norm_args *args, emtk_stream stream);
+
+/* Its gradients from dy (of y's other uses, or absent) and dh (given where pre
+ * is a norm), with the y that it wrote and the block's output:
+ *   t = dy + pre'(y)^T dh;  d_residual = scale t;
+ *   d_gate[g] = sum over its rows of t * dropout(post(block)), fp32 [..][n];
+ *   d_block = post'(block)^T (dropout's factors * gate * t);
+ *   dw_pre, db_pre, dw_post, db_post [n], fp32: of the norms' weights and biases.
+ * Every output may be absent.  y is needed for pre, block for d_block, d_gate,
+ * dw_post and db_post; m = 0 makes the sums 0.  d_residual may be dy itself (same
+ * address, same ld). */
+typedef struct {
+    int32_t m, n, type, gate_every;
+    float scale;
+    int32_t reserved;
+    emtk_norm post, pre;
+    emtk_drop drop;
+    emtk_matrix dy, dh, y, block, gate, d_residual, d_block, d_gate;
+    float *dw_pre, *db_pre, *dw_post, *db_post;
+} emtk_residual_norm_grad_args;
+EMTK_API emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residual_norm_grad_args *args,
+                                                 emtk_stream stream);
+
+/* Log probabilities of logits [m][v] (BF16, F16 or F32) at a temperature > 0:
+ * with l_j = z_j / temperature - ln sum_k exp(z_k / temperature) of a row,
+ *   logprob [m] = l of the row's token; 0 where the token is negative (none is
+ *                 given), NaN where it is v or more;
+ *   entropy [m] = -sum_j exp(l_j) l_j;
+ *   lse [m]     = ln sum_k exp(z_k / temperature), for the backward call;
+ *   top_logprob, top_index [m][top]: the `top` largest, 0 <= top <= 32 and
+ *                 top <= v, descending, the lowest index first among equals.
+ * All fp32, contiguous, each or NULL (tokens and logprob go together, top's two
+ * as well).  A logit of -infinity has probability 0.  A row of nothing else
+ * (or v = 0) has lse and every l -infinity and entropy 0; a row with NaN or
+ * +infinity has NaN logprob, entropy and top_logprob, and NaN counts as the
+ * least logit. */
+typedef struct {
+    int32_t m, v, type, top;
+    float temperature;
+    int32_t reserved;
+    emtk_matrix logits;
+    const int32_t *tokens;
+    float *logprob, *entropy, *lse, *top_logprob;
+    int32_t *top_index;
+} emtk_logprobs_args;
+EMTK_API emtk_status emtk_logprobs(emtk_nn *nn, const emtk_logprobs_args *args, emtk_stream stream);
+
+/* The gradient of logits from d_logprob [m] and d_entropy [m] (each or NULL),
+ * with the lse, and for d_entropy the entropy, that emtk_logprobs wrote:
+ *   d_logits_j = (d_logprob (1[j is the token] - p_j) - d_entropy p_j (l_j + entropy)) / temperature
+ * with p = exp(l); 0 where p_j = 0 and j is no token.  A token outside 0 .. v - 1
+ * gets no d_logprob.  d_logits, of the logits' type, may be the logits themselves
+ * (same address, same ld). */
+typedef struct {
+    int32_t m, v, type, reserved0;
+    float temperature;
+    int32_t reserved;
+    emtk_matrix logits, d_logits;
+    const int32_t *tokens;
+    const float *lse, *entropy, *d_logprob, *d_entropy;
+} emtk_logprobs_grad_args;
+EMTK_API emtk_status emtk_logprobs_backward(emtk_nn *nn, const emtk_logprobs_grad_args *args, emtk_stream stream);
+
+/* A gated linear recurrence along sequences, each column by itself: from the
+ * state h_0 of a sequence, over its rows t = 1 ..,
+ *   a_t = 1 / (1 + exp(-f_t));  h_t = a_t h_(t-1) + (1 - a_t) x_t;  y_t = act(o_t) h_t
+ * (y = h without o; act is NONE then).  f, x, o, y [rows][n]; the rows of the
+ * `seqs` sequences lie one after another: sequence s has rows offsets[s] ..
+ * offsets[s + 1] - 1 (device int32 [seqs + 1], rising; clamped to 0 .. rows, rows
+ * outside every sequence are left as they were), or, with offsets NULL,
+ * rows / seqs rows each (a whole number).  state [seqs][n], fp32: h_0, or NULL
+ * for 0; last [seqs][n]: the state after the last row (of an empty sequence: h_0),
+ * or NULL; it may be `state` itself.  states
+ * [rows / EMTK_RECURRENCE_STEP + seqs][n], fp32, or NULL, receives what the
+ * backward call needs.  The state is fp32 and kept so that forget gates near 1
+ * lose nothing: h_t = h_(t-1) + b_t (x_t - h_(t-1)) with b_t = 1 / (1 + exp(f_t)). */
+#define EMTK_RECURRENCE_STEP 128
+typedef struct {
+    int32_t rows, n, seqs, act, type, reserved;
+    emtk_matrix f, x, o, y;
+    const int32_t *offsets;
+    const float *state;
+    float *last, *states;
+} emtk_recurrence_args;
+EMTK_API emtk_status emtk_recurrence(emtk_nn *nn, const emtk_recurrence_args *args, emtk_stream stream);
+
+/* Its gradients from dy [rows][n] and d_last [seqs][n] (or NULL for 0), with the
+ * states that it wrote and the same f, x, o, offsets: from the last row of a
+ * sequence,
+ *   g_t = act(o_t) dy_t + a_(t+1) g_(t+1), d_last in the place of the latter at the end;
+ *   dx = (1 - a) g;  df = g (h_(t-1) - x) a (1 - a);  d_o = dy h act'(o);  d_state = a_1 g_1.
+ * Every output may be absent (d_o with o alone). */
+typedef struct {
+    int32_t rows, n, seqs, act, type, reserved;
+    emtk_matrix dy, f, x, o, df, dx, d_o;
+    const int32_t *offsets;
+    const float *states, *d_last;
+    float *d_state;
+} emtk_recurrence_grad_args;
+EMTK_API emtk_status emtk_recurrence_backward(emtk_nn *nn, const emtk_recurrence_grad_args *args, emtk_stream stream);
+
+/* ------------------------------------------------------------------------
  * Test hooks: host-side fault injection.  They make the failures a service
  * must survive (an exhausted device, a dispatcher that stops making progress)
  * happen on the host, with no fault on the GPU.  Not for production use.

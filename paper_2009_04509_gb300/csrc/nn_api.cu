@@ -1,9 +1,10 @@
-// C ABI of the dense layers, gated blocks and 8-bit checkpoints
-// (include/emtk.h): argument checks, workspace and the launches of each call.
+// C ABI of the layers and of what stands around them (include/emtk.h): argument
+// checks, workspace and the launches of each call.
 #include <cuda.h>
 #include <nvtx3/nvToolsExt.h>
 
 #include <algorithm>
+#include <cmath>
 #include <new>
 
 #include "emtk_internal.h"
@@ -65,6 +66,22 @@ struct Checks {
             return;
         }
         if (reinterpret_cast<uintptr_t>(m.d) % elem) fail(EMTK_ERR_ALIGN);
+    }
+    // Two matrices share no element, or all of them (the same address and ld).
+    void whole_or_apart(const emtk_matrix &a, const emtk_matrix &b, bool may_be_same) {
+        if (a.d && a.d == b.d && (a.ld != b.ld || !may_be_same)) fail(EMTK_ERR_ARG);
+    }
+    void norm(const emtk_norm &n, int type) {
+        need(n.kind >= EMTK_NORM_NONE && n.kind <= EMTK_NORM_LAYER);
+        if (n.kind == EMTK_NORM_NONE) return need(!n.weight && !n.bias);
+        need(n.eps >= 0.f && n.eps < INFINITY);
+        if (!n.weight && !n.bias) return;
+        need(n.param_type == type || n.param_type == EMTK_TYPE_F32);
+        for (const void *p : {n.weight, n.bias}) vector(p, n.param_type == EMTK_TYPE_F32 ? 4 : 2);
+    }
+    void drop(const emtk_drop &d) {
+        need(d.p >= 0.f && d.p < 1.f);
+        vector(d.d_offset, 8);
     }
     void vector(const void *p, size_t elem) {
         if (reinterpret_cast<uintptr_t>(p) % elem) fail(EMTK_ERR_ALIGN);
@@ -168,6 +185,8 @@ emtk_status forward(emtk_nn *nn, MmJob &j, const emtk_matrix &x, const emtk_matr
     return status_of(e);
 }
 
+int64_t gate_rows(int32_t m, int32_t every) { return std::max<int64_t>(1, ((int64_t)m + every - 1) / every); }
+
 // The status of a backward call.  Where a launch failed, the products have not reset the
 // slopes' range.
 emtk_status finished(cudaError_t e, SlopeRange *range, cudaStream_t s) {
@@ -204,6 +223,7 @@ emtk_status emtk_nn_create(int device, int64_t workspace_bytes, int64_t wait_tim
                                                      &found);
     if (e == cudaSuccess && (nn->encode == nullptr || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
     if (e == cudaSuccess) e = init_mm_kernels();
+    if (e == cudaSuccess) e = init_norm_kernels();
     if (e == cudaSuccess) e = dev_alloc(&status, sizeof(int) + sizeof(SlopeRange));
     nn->status = static_cast<int *>(status);
     nn->range = reinterpret_cast<SlopeRange *>(nn->status + 1);
@@ -521,6 +541,194 @@ emtk_status emtk_unpack8(emtk_nn *nn, int32_t m, int32_t k, emtk_type type, cons
     Range range("emtk unpack8");
     const Copy16 copy{*q, *x, m, k};
     return status_of(launch_copy16(type, &copy, 1, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_dropout(emtk_nn *nn, int32_t m, int32_t n, emtk_type type, const emtk_matrix *x, const emtk_matrix *y,
+                         const emtk_drop *drop, emtk_stream stream) {
+    if (!nn || !x || !y || !drop || !sizes_ok(m, n, 0) || !type16(type)) return EMTK_ERR_ARG;
+    Checks c;
+    c.matrix(*x, m, n, true, false);
+    c.matrix(*y, m, n, true, false);
+    c.whole_or_apart(*x, *y, true);
+    c.drop(*drop);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk dropout");
+    return status_of(launch_dropout(type, m, n, *x, *y, *drop, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_residual_norm(emtk_nn *nn, const emtk_residual_norm_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_residual_norm_args &a = *p;
+    Checks c;
+    c.need(sizes_ok(a.m, a.n, 0) && a.n <= kMaxNormWidth && type16(a.type));
+    c.need(!a.gate.d || a.gate_every > 0);
+    if (c.st != EMTK_OK) return c.st;
+    c.norm(a.post, a.type);
+    c.norm(a.pre, a.type);
+    c.drop(a.drop);
+    if (a.m > 0 && a.n > 0) {  // what has no elements may have no address
+        c.need(a.block.d || (a.post.kind == EMTK_NORM_NONE && !a.gate.d && a.drop.p == 0.f));
+        c.need((a.residual.d || a.block.d) && (a.y.d || a.h.d) && (a.h.d != nullptr) == (a.pre.kind != EMTK_NORM_NONE));
+    }
+    c.matrix(a.residual, a.m, a.n, false, false);
+    c.matrix(a.block, a.m, a.n, false, false);
+    if (c.st == EMTK_OK && a.gate.d) c.matrix(a.gate, gate_rows(a.m, a.gate_every), a.n, false, false);
+    c.matrix(a.y, a.m, a.n, false, false);
+    c.matrix(a.h, a.m, a.n, false, false);
+    c.whole_or_apart(a.y, a.residual, true);
+    for (const emtk_matrix *in : {&a.block, &a.gate}) c.whole_or_apart(a.y, *in, false);
+    for (const emtk_matrix *in : {&a.block, &a.gate, &a.residual, &a.y}) c.whole_or_apart(a.h, *in, false);
+    if (c.st != EMTK_OK || a.m == 0 || a.n == 0) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk residual norm");
+    return status_of(launch_residual_norm(a, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residual_norm_grad_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    emtk_residual_norm_grad_args a = *p;
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    Checks c;
+    c.need(sizes_ok(a.m, a.n, 0) && a.n <= kMaxNormWidth && type16(a.type));
+    if (!a.gate.d && !a.d_gate.d) a.gate_every = std::max(1, a.m);
+    c.need(a.gate_every > 0);
+    if (c.st != EMTK_OK) return c.st;
+    const bool pre = a.pre.kind != EMTK_NORM_NONE, post = a.post.kind != EMTK_NORM_NONE;
+    const int64_t gates = gate_rows(a.m, a.gate_every);
+    c.norm(a.post, a.type);
+    c.norm(a.pre, a.type);
+    c.drop(a.drop);
+    if (a.m > 0 && a.n > 0) {
+        c.need((a.dh.d != nullptr) == pre && (a.dy.d || a.dh.d));
+        c.need(a.block.d || (!post && !a.gate.d && a.drop.p == 0.f));
+    }
+    c.need(pre || (!a.dw_pre && !a.db_pre));
+    c.need(post || (!a.dw_post && !a.db_post));
+    c.matrix(a.dy, a.m, a.n, false, false);
+    c.matrix(a.dh, a.m, a.n, pre, false);
+    c.matrix(a.y, a.m, a.n, pre, false);
+    c.matrix(a.block, a.m, a.n, a.d_block.d || a.d_gate.d || a.dw_post || a.db_post, false);
+    c.matrix(a.gate, gates, a.n, false, false);
+    c.matrix(a.d_residual, a.m, a.n, false, false);
+    c.matrix(a.d_block, a.m, a.n, false, false);
+    c.matrix(a.d_gate, gates, a.n, false, false, 4);
+    for (const void *v : {a.dw_pre, a.db_pre, a.dw_post, a.db_post}) c.vector(v, 4);
+    c.whole_or_apart(a.d_residual, a.dy, true);
+    c.whole_or_apart(a.d_block, a.d_residual, false);
+    for (const emtk_matrix *in : {&a.dh, &a.y, &a.block, &a.gate}) c.whole_or_apart(a.d_residual, *in, false);
+    for (const emtk_matrix *in : {&a.dy, &a.dh, &a.y, &a.block, &a.gate}) c.whole_or_apart(a.d_block, *in, false);
+    if (c.st != EMTK_OK || a.n == 0) return c.st;
+    if (!a.d_block.d && !a.d_gate.d && !a.dw_post && !a.db_post) a.block.d = nullptr;  // nothing needs it
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk residual norm backward");
+    CallSpace ws{nn};
+    void *space = nullptr;
+    for (int pass = 0; pass < 2; ++pass) {
+        space = ws.take(residual_norm_workspace(a, nn->sm_count));
+        if (pass == 0) {
+            const emtk_status st = ws.ensure(s);
+            if (st != EMTK_OK) return st;
+        }
+    }
+    return status_of(launch_residual_norm_grad(a, space, nn->sm_count, s));
+}
+
+emtk_status emtk_logprobs(emtk_nn *nn, const emtk_logprobs_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_logprobs_args &a = *p;
+    Checks c;
+    c.need(sizes_ok(a.m, a.v, 0) && (type16(a.type) || a.type == EMTK_TYPE_F32));
+    c.need(a.top >= 0 && a.top <= std::min(32, a.v) && a.temperature > 0.f && a.temperature < INFINITY &&
+           1.f / a.temperature < INFINITY);
+    c.need((a.tokens == nullptr) == (a.logprob == nullptr));
+    c.need((a.top > 0) == (a.top_logprob != nullptr) && (a.top > 0) == (a.top_index != nullptr));
+    if (c.st != EMTK_OK) return c.st;
+    c.matrix(a.logits, a.m, a.v, true, false, a.type == EMTK_TYPE_F32 ? 4 : 2);
+    for (const void *v : {(const void *)a.tokens, (const void *)a.logprob, (const void *)a.entropy, (const void *)a.lse,
+                          (const void *)a.top_logprob, (const void *)a.top_index})
+        c.vector(v, 4);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk logprobs");
+    return status_of(launch_logprobs(a, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_logprobs_backward(emtk_nn *nn, const emtk_logprobs_grad_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_logprobs_grad_args &a = *p;
+    const size_t elem = a.type == EMTK_TYPE_F32 ? 4 : 2;
+    Checks c;
+    c.need(sizes_ok(a.m, a.v, 0) && (type16(a.type) || a.type == EMTK_TYPE_F32));
+    c.need(a.temperature > 0.f && a.temperature < INFINITY && 1.f / a.temperature < INFINITY);
+    c.need(a.m == 0 || a.lse);
+    c.need(!a.d_logprob || a.tokens);
+    c.need(!a.d_entropy || a.entropy);
+    if (c.st != EMTK_OK) return c.st;
+    c.matrix(a.logits, a.m, a.v, true, false, elem);
+    c.matrix(a.d_logits, a.m, a.v, true, false, elem);
+    c.whole_or_apart(a.d_logits, a.logits, true);
+    for (const void *v : {(const void *)a.tokens, (const void *)a.lse, (const void *)a.entropy, (const void *)a.d_logprob,
+                          (const void *)a.d_entropy})
+        c.vector(v, 4);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk logprobs backward");
+    return status_of(launch_logprobs_grad(a, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_recurrence(emtk_nn *nn, const emtk_recurrence_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_recurrence_args &a = *p;
+    Checks c;
+    c.need(sizes_ok(a.rows, a.n, a.seqs) && act_known(a.act) && type16(a.type));
+    if (c.st != EMTK_OK) return c.st;
+    c.need(a.offsets || (a.seqs > 0 ? a.rows % a.seqs == 0 : a.rows == 0));
+    const bool some = a.rows > 0 && a.n > 0;  // what has no elements may have no address
+    c.need(!some || a.o.d || a.act == EMTK_ACT_NONE);
+    c.matrix(a.f, a.rows, a.n, true, false);
+    c.matrix(a.x, a.rows, a.n, true, false);
+    c.matrix(a.o, a.rows, a.n, false, false);
+    c.matrix(a.y, a.rows, a.n, true, false);
+    for (const emtk_matrix *in : {&a.f, &a.x, &a.o}) c.whole_or_apart(a.y, *in, false);
+    for (const void *v : {(const void *)a.offsets, (const void *)a.state, (const void *)a.last, (const void *)a.states})
+        c.vector(v, 4);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk recurrence");
+    return status_of(launch_recurrence(a, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+emtk_status emtk_recurrence_backward(emtk_nn *nn, const emtk_recurrence_grad_args *p, emtk_stream stream) {
+    if (!nn || !p) return EMTK_ERR_ARG;
+    const emtk_recurrence_grad_args &a = *p;
+    Checks c;
+    c.need(sizes_ok(a.rows, a.n, a.seqs) && act_known(a.act) && type16(a.type));
+    if (c.st != EMTK_OK) return c.st;
+    c.need(a.offsets || (a.seqs > 0 ? a.rows % a.seqs == 0 : a.rows == 0));
+    const bool some = a.rows > 0 && a.n > 0;
+    c.need(!some || a.o.d || (a.act == EMTK_ACT_NONE && !a.d_o.d));
+    c.need(!some || a.states || a.seqs == 0);
+    const emtk_matrix *const in[] = {&a.dy, &a.f, &a.x, &a.o}, *const out[] = {&a.df, &a.dx, &a.d_o};
+    for (const emtk_matrix *i : in) c.matrix(*i, a.rows, a.n, i != &a.o, false);
+    for (const emtk_matrix *o : out) c.matrix(*o, a.rows, a.n, false, false);
+    for (const emtk_matrix *o : out)
+        for (const emtk_matrix *i : in) c.whole_or_apart(*o, *i, false);
+    c.whole_or_apart(a.df, a.dx, false);
+    for (const emtk_matrix *o : {&a.df, &a.dx}) c.whole_or_apart(a.d_o, *o, false);
+    for (const void *v : {(const void *)a.offsets, (const void *)a.states, (const void *)a.d_last, (const void *)a.d_state})
+        c.vector(v, 4);
+    if (c.st != EMTK_OK) return c.st;
+    DeviceGuard g(nn->device);
+    if (!g.ok) return EMTK_ERR_CUDA;
+    Range range("emtk recurrence backward");
+    return status_of(launch_recurrence_grad(a, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

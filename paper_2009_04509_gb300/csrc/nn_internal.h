@@ -38,6 +38,7 @@ struct emtk_nn {
 namespace emtk {
 
 constexpr int kQ8Block = 32;  // columns that share a checkpoint scale
+constexpr int kMaxNormWidth = 16384;  // of residual norms: a row is held in a block's registers
 
 // Size of a workspace that has to hold `need` bytes: a quarter more, so that slowly
 // growing calls seldom wait, unless the device has little left beside it.
@@ -162,5 +163,17 @@ struct Copy16 {
     int rows, cols;
 };
 cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, cudaStream_t s);
+
+// ---- around the products: argument structs as they came, checked
+cudaError_t launch_dropout(emtk_type type, int m, int n, const emtk_matrix &x, const emtk_matrix &y, const emtk_drop &drop,
+                           int sms, cudaStream_t s);  // nn_dropout.cu
+cudaError_t init_norm_kernels();  // once per device
+cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, cudaStream_t s);  // nn_norm.cu
+size_t residual_norm_workspace(const emtk_residual_norm_grad_args &p, int sms);
+cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, int sms, cudaStream_t s);
+cudaError_t launch_logprobs(const emtk_logprobs_args &p, int sms, cudaStream_t s);  // nn_logprob.cu
+cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, int sms, cudaStream_t s);
+cudaError_t launch_recurrence(const emtk_recurrence_args &p, int sms, cudaStream_t s);  // nn_recur.cu
+cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, int sms, cudaStream_t s);
 
 }  // namespace emtk

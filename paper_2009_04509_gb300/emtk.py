@@ -23,6 +23,8 @@ EMTK_PATCH_F32, EMTK_PATCH_BF16, EMTK_PATCH_F16 = 0, 1, 2
 PRECISIONS = {"fp32": EMTK_FP32, "tf32": EMTK_TF32, "bf16": EMTK_BF16, "fp16": EMTK_FP16, "fp8": EMTK_FP8}
 PATCH_FORMATS = {"f32": EMTK_PATCH_F32, "bf16": EMTK_PATCH_BF16, "fp16": EMTK_PATCH_F16}
 EMTK_TYPE_BF16, EMTK_TYPE_F16, EMTK_TYPE_F32 = 0, 1, 2
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+EMTK_RECURRENCE_STEP = 128
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4}
 KERNELS = ("intervals", "gather", "network", "head", "convert", "hitfind")
 
@@ -32,7 +34,9 @@ EXPORTED = ("emtk_default_options", "emtk_create", "emtk_destroy", "emtk_infer",
             "emtk_batcher_wait", "emtk_batcher_stats", "emtk_batcher_destroy", "emtk_get_fp8_scales",
             "emtk_find_hits", "emtk_infer_batch_host", "emtk_debug_fail_alloc", "emtk_debug_alloc_counts",
             "emtk_debug_batcher_stall", "emtk_nn_create", "emtk_nn_destroy", "emtk_nn_check", "emtk_dense",
-            "emtk_dense_backward", "emtk_gated", "emtk_gated_backward", "emtk_pack8", "emtk_unpack8")
+            "emtk_dense_backward", "emtk_gated", "emtk_gated_backward", "emtk_pack8", "emtk_unpack8", "emtk_dropout", "emtk_residual_norm",
+            "emtk_residual_norm_backward", "emtk_logprobs", "emtk_logprobs_backward", "emtk_recurrence",
+            "emtk_recurrence_backward")
 EMTK_STATIC_SCRATCH_BYTES = 4 << 20
 
 _vp = ctypes.c_void_p
@@ -70,10 +74,20 @@ class emtk_matrix(ctypes.Structure):
     _fields_ = [("d", _vp), ("ld", ctypes.c_int64), ("d_scale", _vp), ("ld_scale", ctypes.c_int64)]
 
 
-def _args_struct(name, ints, matrices, pointers):
-    """An argument struct of the layers: int32 fields, matrices, pointers."""
-    fields = [(f, ctypes.c_int32) for f in ints.split()] + [(f, emtk_matrix) for f in matrices.split()] + \
-        [(f, _vp) for f in pointers.split()]
+class emtk_drop(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("d_offset", _vp), ("p", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class emtk_norm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("param_type", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("weight", _vp), ("bias", _vp)]
+
+
+def _args_struct(name, ints, matrices, pointers, floats="", parts=()):
+    """An argument struct of the layers: int32 fields (those in `floats` fp32), other structs, matrices, pointers."""
+    fields = [(f, ctypes.c_float if f in floats.split() else ctypes.c_int32) for f in ints.split()] + list(parts) + \
+        [(f, emtk_matrix) for f in matrices.split()] + [(f, _vp) for f in pointers.split()]
     return type(name, (ctypes.Structure,), {"_fields_": fields})
 
 
@@ -83,6 +97,20 @@ emtk_gated_args = _args_struct("emtk_gated_args", "m f k act type bias_type", "x
                                "bias_gate bias_up")
 emtk_gated_grad_args = _args_struct("emtk_gated_grad_args", "m f k act type dw_type",
                                     "dh gate up x w_gate w_up dx dw_gate dw_up h", "db_gate db_up")
+_SEAM_PARTS = (("post", emtk_norm), ("pre", emtk_norm), ("drop", emtk_drop))
+emtk_residual_norm_args = _args_struct("emtk_residual_norm_args", "m n type gate_every scale reserved",
+                                       "residual block gate y h", "", "scale", _SEAM_PARTS)
+emtk_residual_norm_grad_args = _args_struct("emtk_residual_norm_grad_args", "m n type gate_every scale reserved",
+                                            "dy dh y block gate d_residual d_block d_gate",
+                                            "dw_pre db_pre dw_post db_post", "scale", _SEAM_PARTS)
+emtk_logprobs_args = _args_struct("emtk_logprobs_args", "m v type top temperature reserved", "logits",
+                                  "tokens logprob entropy lse top_logprob top_index", "temperature")
+emtk_logprobs_grad_args = _args_struct("emtk_logprobs_grad_args", "m v type reserved0 temperature reserved",
+                                       "logits d_logits", "tokens lse entropy d_logprob d_entropy", "temperature")
+emtk_recurrence_args = _args_struct("emtk_recurrence_args", "rows n seqs act type reserved", "f x o y",
+                                    "offsets state last states")
+emtk_recurrence_grad_args = _args_struct("emtk_recurrence_grad_args", "rows n seqs act type reserved",
+                                         "dy f x o df dx d_o", "offsets states d_last d_state")
 
 
 class EmtkError(RuntimeError):
@@ -144,13 +172,17 @@ def load_library(path: str | None = None):
     lib.emtk_nn_create.argtypes = [ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(_vp)]
     lib.emtk_nn_destroy.argtypes = [_vp]
     lib.emtk_nn_check.argtypes = [_vp, _vp]
-    for name in ("emtk_dense", "emtk_dense_backward", "emtk_gated", "emtk_gated_backward"):
+    packed = ("emtk_dense", "emtk_dense_backward", "emtk_gated", "emtk_gated_backward", "emtk_residual_norm",
+              "emtk_residual_norm_backward", "emtk_logprobs", "emtk_logprobs_backward", "emtk_recurrence",
+              "emtk_recurrence_backward")
+    for name in packed:
         getattr(lib, name).argtypes = [_vp, ctypes.c_char_p, _vp]  # a packed argument struct
     for name in ("emtk_pack8", "emtk_unpack8"):
         getattr(lib, name).argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int, ctypes.c_char_p,
                                        ctypes.c_char_p, _vp]
-    for name in ("emtk_nn_create", "emtk_nn_destroy", "emtk_nn_check", "emtk_dense", "emtk_dense_backward",
-                 "emtk_gated", "emtk_gated_backward", "emtk_pack8", "emtk_unpack8"):
+    lib.emtk_dropout.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int, ctypes.c_char_p, ctypes.c_char_p,
+                                 ctypes.c_char_p, _vp]
+    for name in packed + ("emtk_nn_create", "emtk_nn_destroy", "emtk_nn_check", "emtk_pack8", "emtk_unpack8", "emtk_dropout"):
         getattr(lib, name).restype = ctypes.c_int
     lib.emtk_status_string.argtypes = [ctypes.c_int]
     lib.emtk_status_string.restype = ctypes.c_char_p
@@ -583,6 +615,205 @@ def emtk_unpack8(nn, q: Q8, x, stream=None) -> None:
     on = _device_of(nn, x)
     _check(load_library().emtk_unpack8(nn, m, k, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat8(on, q, m, k, dt, "q")),
                                        _PACK_MATRIX.pack(*_mat(on, x, m, k, dt, "x")), _current(x, stream)), "emtk_unpack8")
+
+
+# ------------------- residual norms, dropout, log probabilities, recurrence
+class Drop(NamedTuple):
+    """Dropout (emtk_drop in include/emtk.h): the share dropped, and what the random numbers are made of.  The
+    backward pass takes the same one.  ``offset_tensor``: a CUDA tensor of one int64 that is added to ``offset``
+    on the device, so that a captured call takes other numbers at each replay."""
+    p: float
+    seed: int
+    offset: int = 0
+    offset_tensor: "object" = None
+
+
+class Norm(NamedTuple):
+    """A norm over a row (emtk_norm in include/emtk.h): "rms" or "layer", its weight and bias (vectors of the
+    call's dtype or float32, or None for 1 and 0) and the eps beside the variance."""
+    kind: str
+    weight: "object" = None
+    bias: "object" = None
+    eps: float = 1e-6
+
+
+_NORM, _DROP = "iif4xQQ", "QQQf4x"
+_PACK_DROP = struct.Struct("<" + _DROP)
+_PACK_SEAM = struct.Struct("<4if4x" + 2 * _NORM + _DROP + 5 * _MATRIX)
+_PACK_SEAM_GRAD = struct.Struct("<4if4x" + 2 * _NORM + _DROP + 8 * _MATRIX + "4Q")
+_PACK_LOGPROBS = struct.Struct("<4if4x" + _MATRIX + "6Q")
+_PACK_LOGPROBS_GRAD = struct.Struct("<3i4xf4x" + 2 * _MATRIX + "5Q")
+_PACK_RECURRENCE = struct.Struct("<5i4x" + 4 * _MATRIX + "4Q")
+_PACK_RECURRENCE_GRAD = struct.Struct("<5i4x" + 7 * _MATRIX + "4Q")
+_NO_NORM = (0, 0, 0.0, 0, 0)
+_NO_DROP = (0, 0, 0, 0.0)
+_WORD = (1 << 64) - 1
+
+
+def _drop(on, d) -> tuple:
+    """The fields of emtk_drop; absent for None."""
+    if d is None:
+        return _NO_DROP
+    p, seed, offset, t = d
+    if t is not None:
+        import torch
+        if t.dtype is not torch.int64 or t.numel() != 1 or t.get_device() != on:
+            raise ValueError(f"offset_tensor: expected one int64 on CUDA device {on}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+        t = t.data_ptr()
+    return (seed & _WORD, offset & _WORD, t or 0, p)
+
+
+def _norm(on, v, n: int, dtype, what: str) -> tuple:
+    """The fields of emtk_norm; absent for None."""
+    if v is None:
+        return _NO_NORM
+    kind, weight, bias, eps = v
+    if kind not in NORMS:
+        raise ValueError(f"{what}: {kind!r} is none of {tuple(NORMS)}")
+    one = weight if weight is not None else bias
+    if weight is not None and bias is not None and weight.dtype is not bias.dtype:
+        raise ValueError(f"{what}: its bias' dtype must be its weight's")
+    return (NORMS[kind], 0 if one is None else _type_of(one, what, True), eps, _vec(on, weight, n, what), _vec(on, bias, n, what))
+
+
+def _whole(on, t, shape: tuple, dtype, what: str) -> int:
+    """A contiguous tensor of a shape and dtype on CUDA device `on`; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.get_device() != on:
+        raise ValueError(f"{what}: expected a contiguous tensor {shape} of {dtype} on CUDA device {on}, got {tuple(t.shape)} of "
+                         f"{t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _gate(on, gate, m: int, n: int, every, dtype, what: str) -> tuple:
+    """(matrix, rows to a gate row) of a gate: [n], one row for all, or [ceil(m / every)][n]."""
+    every = max(1, m) if every is None else int(every)
+    if gate is None:
+        return _ABSENT, every
+    if gate.dim() == 1:
+        gate = gate[None]
+    if every <= 0:
+        raise ValueError(f"gate_every: {every} is not positive")
+    return _mat(on, gate, max(1, -(-m // every)), n, dtype, what), every
+
+
+def emtk_dropout(nn, x, y, drop: Drop, stream=None) -> None:
+    """y = x under dropout, [m][n] of bf16 or fp16; dx from dy is the same call.  y may be x."""
+    (m, n), dt = x.shape, x.dtype
+    on = _device_of(nn, x)
+    _check(load_library().emtk_dropout(nn, m, n, _type_of(x, "x"), _PACK_MATRIX.pack(*_mat(on, x, m, n, dt, "x")),
+                                       _PACK_MATRIX.pack(*_mat(on, y, m, n, dt, "y")), _PACK_DROP.pack(*_drop(on, drop)),
+                                       _current(x, stream)), "emtk_dropout")
+
+
+def emtk_residual_norm(nn, residual=None, block=None, y=None, h=None, post: Norm = None, pre: Norm = None, gate=None,
+                       gate_every: int = None, scale: float = 1.0, drop: Drop = None, stream=None) -> None:
+    """y = scale * residual + gate * dropout(post(block)) and h = pre(y), [m][n] of bf16 or fp16, n <= 16384, each part
+    optional.  gate: [n], or [ceil(m / gate_every)][n] with row i taking row i // gate_every.  y may be residual."""
+    like = block if block is not None else residual
+    if like is None:
+        raise ValueError("residual, block: one must be given")
+    (m, n), dt = like.shape, like.dtype
+    on = _device_of(nn, like)
+    g, every = _gate(on, gate, m, n, gate_every, dt, "gate")
+    args = _PACK_SEAM.pack(m, n, _type_of(like, "block" if like is block else "residual"), every, scale, *_norm(on, post, n, dt, "post"),
+                           *_norm(on, pre, n, dt, "pre"), *_drop(on, drop), *_mat(on, residual, m, n, dt, "residual"),
+                           *_mat(on, block, m, n, dt, "block"), *g, *_mat(on, y, m, n, dt, "y"), *_mat(on, h, m, n, dt, "h"))
+    _check(load_library().emtk_residual_norm(nn, args, _current(like, stream)), "emtk_residual_norm")
+
+
+def emtk_residual_norm_backward(nn, dy=None, dh=None, y=None, block=None, d_residual=None, d_block=None, post: Norm = None,
+                                pre: Norm = None, gate=None, gate_every: int = None, scale: float = 1.0, drop: Drop = None,
+                                d_gate=None, dw_pre=None, db_pre=None, dw_post=None, db_post=None, stream=None) -> None:
+    """Gradients of emtk_residual_norm from dy (of y's other uses) and dh, with the y that it wrote: d_residual and
+    d_block [m][n], d_gate (gate's shape), dw_pre, db_pre, dw_post, db_post [n] float32; each optional.  d_residual may
+    be dy."""
+    like = dh if dh is not None else dy
+    if like is None:
+        raise ValueError("dy, dh: one must be given")
+    (m, n), dt = like.shape, like.dtype
+    on = _device_of(nn, like)
+    import torch
+    g, every = _gate(on, gate, m, n, gate_every, dt, "gate")
+    dg, _ = _gate(on, d_gate, m, n, gate_every, torch.float32, "d_gate")
+    args = _PACK_SEAM_GRAD.pack(m, n, _type_of(like, "dh" if like is dh else "dy"), every, scale, *_norm(on, post, n, dt, "post"),
+                                *_norm(on, pre, n, dt, "pre"), *_drop(on, drop), *_mat(on, dy, m, n, dt, "dy"),
+                                *_mat(on, dh, m, n, dt, "dh"), *_mat(on, y, m, n, dt, "y"), *_mat(on, block, m, n, dt, "block"), *g,
+                                *_mat(on, d_residual, m, n, dt, "d_residual"), *_mat(on, d_block, m, n, dt, "d_block"), *dg,
+                                *(_vec(on, t, n, what, True) for t, what in ((dw_pre, "dw_pre"), (db_pre, "db_pre"),
+                                                                            (dw_post, "dw_post"), (db_post, "db_post"))))
+    _check(load_library().emtk_residual_norm_backward(nn, args, _current(like, stream)), "emtk_residual_norm_backward")
+
+
+def emtk_logprobs(nn, logits, tokens=None, logprob=None, entropy=None, lse=None, top_logprob=None, top_index=None,
+                  temperature: float = 1.0, stream=None) -> None:
+    """Of logits [m][v] (bf16, fp16 or float32), float32 and contiguous, each optional: logprob [m] of tokens [m] (int32;
+    negative: none), entropy [m], lse [m] for the backward call, top_logprob [m][top] and top_index [m][top] (int32) of
+    the largest `top` <= 32."""
+    import torch
+    (m, v), on = logits.shape, _device_of(nn, logits)
+    f32, i32 = torch.float32, torch.int32
+    some = top_logprob if top_logprob is not None else top_index
+    top = 0 if some is None else some.shape[1]
+    args = _PACK_LOGPROBS.pack(m, v, _type_of(logits, "logits", True), top, temperature, *_mat(on, logits, m, v, logits.dtype, "logits"),
+                               _whole(on, tokens, (m,), i32, "tokens"), _whole(on, logprob, (m,), f32, "logprob"),
+                               _whole(on, entropy, (m,), f32, "entropy"), _whole(on, lse, (m,), f32, "lse"),
+                               _whole(on, top_logprob, (m, top), f32, "top_logprob"), _whole(on, top_index, (m, top), i32, "top_index"))
+    _check(load_library().emtk_logprobs(nn, args, _current(logits, stream)), "emtk_logprobs")
+
+
+def emtk_logprobs_backward(nn, logits, lse, d_logits, tokens=None, d_logprob=None, entropy=None, d_entropy=None,
+                           temperature: float = 1.0, stream=None) -> None:
+    """The gradient of logits, of their dtype, from d_logprob [m] (with the tokens) and d_entropy [m] (with the entropy
+    that emtk_logprobs wrote), each optional, and its lse.  d_logits may be logits."""
+    import torch
+    (m, v), dt, on = logits.shape, logits.dtype, _device_of(nn, logits)
+    f32 = torch.float32
+    args = _PACK_LOGPROBS_GRAD.pack(m, v, _type_of(logits, "logits", True), temperature, *_mat(on, logits, m, v, dt, "logits"),
+                                    *_mat(on, d_logits, m, v, dt, "d_logits"), _whole(on, tokens, (m,), torch.int32, "tokens"),
+                                    _whole(on, lse, (m,), f32, "lse"), _whole(on, entropy, (m,), f32, "entropy"),
+                                    _whole(on, d_logprob, (m,), f32, "d_logprob"), _whole(on, d_entropy, (m,), f32, "d_entropy"))
+    _check(load_library().emtk_logprobs_backward(nn, args, _current(logits, stream)), "emtk_logprobs_backward")
+
+
+def emtk_recurrence_states(rows: int, n: int, seqs: int, device="cuda"):
+    """The tensor in which emtk_recurrence keeps what its backward call needs, contents undefined."""
+    import torch
+    return torch.empty((rows // EMTK_RECURRENCE_STEP + seqs, n), dtype=torch.float32, device=device)
+
+
+def emtk_recurrence(nn, f, x, y, o=None, act: str = "none", seqs: int = 1, offsets=None, state=None, last=None, states=None,
+                    stream=None) -> None:
+    """h_t = h_(t-1) + (x_t - h_(t-1)) / (1 + exp(f_t)) along each sequence and y = act(o) h (y = h without o), [rows][n]
+    of bf16 or fp16.  Sequences lie one after another: offsets [seqs + 1] (int32) says where, or each has rows / seqs
+    rows.  state and last [seqs][n] float32: the states before and after (last may be state); states
+    (emtk_recurrence_states) is for the backward call."""
+    import torch
+    (rows, n), dt, on = f.shape, f.dtype, _device_of(nn, f)
+    f32, seqs = torch.float32, int(seqs)
+    args = _PACK_RECURRENCE.pack(rows, n, seqs, _act_code(act), _type_of(f, "f"), *_mat(on, f, rows, n, dt, "f"),
+                                 *_mat(on, x, rows, n, dt, "x"), *_mat(on, o, rows, n, dt, "o"), *_mat(on, y, rows, n, dt, "y"),
+                                 _whole(on, offsets, (seqs + 1,), torch.int32, "offsets"), _whole(on, state, (seqs, n), f32, "state"),
+                                 _whole(on, last, (seqs, n), f32, "last"),
+                                 _whole(on, states, (rows // EMTK_RECURRENCE_STEP + seqs, n), f32, "states"))
+    _check(load_library().emtk_recurrence(nn, args, _current(f, stream)), "emtk_recurrence")
+
+
+def emtk_recurrence_backward(nn, dy, f, x, states, df=None, dx=None, o=None, act: str = "none", seqs: int = 1, offsets=None,
+                             d_last=None, d_o=None, d_state=None, stream=None) -> None:
+    """Gradients of emtk_recurrence from dy and d_last [seqs][n] float32 (None: 0), with the states that it kept: df, dx,
+    d_o [rows][n] and d_state [seqs][n] float32, each optional."""
+    import torch
+    (rows, n), dt, on = f.shape, f.dtype, _device_of(nn, f)
+    f32, seqs = torch.float32, int(seqs)
+    args = _PACK_RECURRENCE_GRAD.pack(rows, n, seqs, _act_code(act), _type_of(f, "f"), *_mat(on, dy, rows, n, dt, "dy"),
+                                      *_mat(on, f, rows, n, dt, "f"), *_mat(on, x, rows, n, dt, "x"), *_mat(on, o, rows, n, dt, "o"),
+                                      *_mat(on, df, rows, n, dt, "df"), *_mat(on, dx, rows, n, dt, "dx"),
+                                      *_mat(on, d_o, rows, n, dt, "d_o"), _whole(on, offsets, (seqs + 1,), torch.int32, "offsets"),
+                                      _whole(on, states, (rows // EMTK_RECURRENCE_STEP + seqs, n), f32, "states"),
+                                      _whole(on, d_last, (seqs, n), f32, "d_last"), _whole(on, d_state, (seqs, n), f32, "d_state"))
+    _check(load_library().emtk_recurrence_backward(nn, args, _current(f, stream)), "emtk_recurrence_backward")
 
 
 # ------------------------------------------------------------- test hooks
