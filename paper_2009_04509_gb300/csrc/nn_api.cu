@@ -137,6 +137,15 @@ struct CallSpace {
     }
 };
 
+// The workspace of a call that needs one piece.
+emtk_status one_space(emtk_nn *nn, size_t bytes, cudaStream_t s, void **space) {
+    CallSpace ws{nn};
+    ws.take(bytes);
+    const emtk_status st = ws.ensure(s);
+    if (st == EMTK_OK) *space = ws.take(bytes);
+    return st;
+}
+
 // Operands of a call's products that cannot be read where they lie (a
 // checkpoint, or rows off the 16-byte grid): each gets a copy in the workspace.
 struct Staging {
@@ -224,6 +233,7 @@ emtk_status emtk_nn_create(int device, int64_t workspace_bytes, int64_t wait_tim
     if (e == cudaSuccess && (nn->encode == nullptr || found != cudaDriverEntryPointSuccess)) e = cudaErrorNotSupported;
     if (e == cudaSuccess) e = init_mm_kernels();
     if (e == cudaSuccess) e = init_norm_kernels();
+    if (e == cudaSuccess) e = init_recur_kernels();
     if (e == cudaSuccess) e = dev_alloc(&status, sizeof(int) + sizeof(SlopeRange));
     nn->status = static_cast<int *>(status);
     nn->range = reinterpret_cast<SlopeRange *>(nn->status + 1);
@@ -625,16 +635,9 @@ emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residual_norm_gr
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk residual norm backward");
-    CallSpace ws{nn};
     void *space = nullptr;
-    for (int pass = 0; pass < 2; ++pass) {
-        space = ws.take(residual_norm_workspace(a, nn->sm_count));
-        if (pass == 0) {
-            const emtk_status st = ws.ensure(s);
-            if (st != EMTK_OK) return st;
-        }
-    }
-    return status_of(launch_residual_norm_grad(a, space, nn->sm_count, s));
+    const emtk_status st = one_space(nn, residual_norm_workspace(a, nn->sm_count), s, &space);
+    return st != EMTK_OK ? st : status_of(launch_residual_norm_grad(a, space, nn->sm_count, s));
 }
 
 emtk_status emtk_logprobs(emtk_nn *nn, const emtk_logprobs_args *p, emtk_stream stream) {
@@ -702,7 +705,10 @@ emtk_status emtk_recurrence(emtk_nn *nn, const emtk_recurrence_args *p, emtk_str
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk recurrence");
-    return status_of(launch_recurrence(a, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+    void *space = nullptr;
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const emtk_status st = one_space(nn, recurrence_workspace(a.rows, a.n, a.seqs, a.offsets == nullptr, true, nn->sm_count), s, &space);
+    return st != EMTK_OK ? st : status_of(launch_recurrence(a, space, nn, s));
 }
 
 emtk_status emtk_recurrence_backward(emtk_nn *nn, const emtk_recurrence_grad_args *p, emtk_stream stream) {
@@ -728,7 +734,10 @@ emtk_status emtk_recurrence_backward(emtk_nn *nn, const emtk_recurrence_grad_arg
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk recurrence backward");
-    return status_of(launch_recurrence_grad(a, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+    void *space = nullptr;
+    const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const emtk_status st = one_space(nn, recurrence_workspace(a.rows, a.n, a.seqs, a.offsets == nullptr, false, nn->sm_count), s, &space);
+    return st != EMTK_OK ? st : status_of(launch_recurrence_grad(a, space, nn, s));
 }
 
 }  // extern "C"

@@ -98,6 +98,9 @@ bool mm_operand_ok(const void *p, int64_t ld, int64_t rows);
 // Tensor map of an operand: rows of index i (M or N), K contraction steps, boxes
 // of 128 bytes along memory by box_rows (or 64, where i runs along memory).
 bool encode_operand(const emtk_nn *nn, CUtensorMap *map, const MmOperand &o, int rows, int K, int box_rows);
+// Tensor map of a matrix of 16-bit elements: boxes of box_cols (64 bytes to 256 columns) by
+// box_rows as they lie, unswizzled.
+bool encode_rows(const emtk_nn *nn, CUtensorMap *map, const emtk_matrix &m, int rows, int cols, int box_cols, int box_rows);
 constexpr int kMmTileRows = 256, kMmStep = 64;  // rows of a tile, contraction steps of a chunk
 
 // Division by a fixed d > 0 of 0 <= n < 2^31, as a product: floor(n m / 2^(31 + s)) with
@@ -173,7 +176,9 @@ size_t residual_norm_workspace(const emtk_residual_norm_grad_args &p, int sms);
 cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, int sms, cudaStream_t s);
 cudaError_t launch_logprobs(const emtk_logprobs_args &p, int sms, cudaStream_t s);  // nn_logprob.cu
 cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, int sms, cudaStream_t s);
-cudaError_t launch_recurrence(const emtk_recurrence_args &p, int sms, cudaStream_t s);  // nn_recur.cu
-cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, int sms, cudaStream_t s);
+cudaError_t init_recur_kernels();  // once per device
+size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, bool forward, int sms);  // uniform: without offsets
+cudaError_t launch_recurrence(const emtk_recurrence_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s);  // nn_recur.cu
+cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s);
 
 }  // namespace emtk

@@ -439,7 +439,7 @@ cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
     while (cluster < kMostCluster && (int64_t)a.m * cluster < 2 * sms && pieces >= 2 * cluster * kThreads * kFlight) cluster *= 2;
     if (cluster == 1)
         return launch_pdl(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)a.m), dim3(kThreads), 0, s, a, cluster);
-    return launch_cluster(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)(a.m * cluster)), dim3(kThreads), cluster, s, a, cluster);
+    return launch_cluster(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)(a.m * cluster)), dim3(kThreads), 0, cluster, s, a, cluster);
 }
 template <int TYPE>
 cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {

@@ -843,6 +843,15 @@ bool encode_operand(const emtk_nn *nn, CUtensorMap *map, const MmOperand &o, int
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_rows(const emtk_nn *nn, CUtensorMap *map, const emtk_matrix &m, int rows, int cols, int box_cols, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? 2 * m.ld : (2 * (int64_t)cols + 15) / 16 * 16)};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1u, 1u};
+    return reinterpret_cast<EncodeTiled>(nn->encode)(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, m.d, dims, strides, box, one,
+                                                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                                                     CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool mm_operand_ok(const void *p, int64_t ld, int64_t rows) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (ld * 2) % 16 == 0);
 }

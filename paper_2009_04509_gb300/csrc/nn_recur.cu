@@ -3,18 +3,24 @@
 //   b = 1 / (1 + exp(f));  h_t = h_(t-1) + b_t (x_t - h_(t-1));  y = act(o) h
 //
 // A run of steps maps the state before it to the one after it, linearly: h becomes H + A h,
-// with H the state that the run makes of 0 and A = prod(1 - b).  A factor is held as q:
+// with H the state that the run makes of 0 and A = prod(1 - b).  A run's factor is held as q:
 // itself where it is below a half, else as its complement with the sign changed, A - 1, so
 // that neither what is kept for long nor what is nearly forgotten loses its low bits: at
-// f = 8 a rounding of 1 - b in fp32 alone is 10^-4 of the state it settles to.
+// f = 8 a rounding of 1 - b in fp32 alone is 10^-4 of the state it settles to.  A step's is
+// held as -b and used as h + b (x - h), off by 2^-24 of the state before it at most.
 //
 // A block takes 32 columns and goes along a sequence in tiles of 128 steps: each half
-// warp a run of 8 steps, two columns to a lane.  The runs' (q, H) meet in shared memory, each
-// half warp joins those before its own and goes over its 8 steps once more, from
-// registers: everything is read once and written once.  Where columns and sequences are
-// too few for the SMs, a cluster of blocks takes neighbouring tiles of a sequence and
-// exchanges its tiles' (q, H) through shared memory.  Orders are fixed: the same call gives
-// the same bits.
+// warp a run of 16 steps, two columns to a lane.  The runs' (q, H) meet in shared memory, each
+// half warp joins those before its own and goes over its steps once more, from shared
+// memory, where TMA brought the tile: everything is read once and written once.
+//
+// Where equal sequences and their columns are too few for the SMs, or lengths are unlike,
+// tiles are made independent in three kernels: the first leaves each tile's (q, H), the second
+// goes along those (a 128th of the data) to each tile's state, the third makes each
+// tile's outputs.  f and x are read twice then; HBM or L2 is kept busy whatever the
+// sequences are.  (Clusters of blocks that exchange their tiles' (q, H) round by round were
+// slower: a round waits 1.4 us for the exchange, as long as a tile takes.)  Orders are fixed:
+// the same call gives the same bits.
 //
 // Backwards, g_t = u_t + (1 - b_(t+1)) g_(t+1) with u = act(o) dy: passing p = (1 - b) g down,
 // a run makes p of R + A p, with the same A.  A tile's states come from the one
@@ -31,10 +37,14 @@
 namespace emtk {
 namespace {
 
-constexpr int kCols = 32, kRuns = 16, kLen = 8, kTile = kRuns * kLen, kThreads = 16 * kRuns;
-constexpr int kMostCluster = 8;
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr int kLanes = 16, kCols = 2 * kLanes;  // two columns a lane
+constexpr int kRuns = 8, kLen = 16, kTile = kRuns * kLen, kThreads = kLanes * kRuns;
 constexpr int kShort = 8;  // steps up to which a thread takes a whole sequence
 static_assert(kTile == EMTK_RECURRENCE_STEP, "states are kept once a tile");
+
+// Where what is kept of a sequence's tile lies: tiles of different sequences, in order and with gaps.
+__device__ __forceinline__ int64_t place_of(int r0, int tile, int seq) { return (int64_t)(r0 / kTile) + tile + seq; }
 
 struct Plane {  // a 16-bit matrix
     uint8_t *p;
@@ -54,69 +64,147 @@ struct Sequences {
             r1 = r0 + length;
         }
     }
+    // The sequence whose tiles' places include this one, if any's do: the last that begins
+    // at it or before.  All lanes of a warp look together.
+    __device__ __forceinline__ int at_place(int place) const {
+        int low = 0, high = seqs;  // it is in low .. high - 1
+        const int lane = threadIdx.x & 31;
+        while (high - low > 1) {
+            const int step = (high - low + 31) / 32, s = low + lane * step;
+            int r0 = 0, r1;
+            if (s < high) rows_of(s, r0, r1);
+            const uint32_t before = __ballot_sync(0xffffffffu, s < high && (lane == 0 || place_of(r0, 0, s) <= place));
+            low += (31 - __clz(before)) * step;
+            high = min(low + step, high);
+        }
+        return low;
+    }
 };
 
+struct Waits {  // of the kernels' bounded waits
+    int *status;
+    int64_t timeout_ns;
+};
+constexpr int kMostIn = 4;  // matrices of a tile: f, x, o and dy, in this order
+struct Tiles {
+    CUtensorMap in[kMostIn], out[3];  // out: y, or df, dx, d_o; of what is there
+    Waits waits;
+};
+
+// `starts`: what comes into each tile (its state, or backwards its p), at place_of; null
+// where a block goes along a whole sequence.
 struct RecurArgs {
     Plane f, x, o, y;
     Sequences at;
-    const float *state;
+    const float *state, *starts;
     float *last, *states;
     int col_tiles, words;  // words: every row starts on 4 bytes
 };
 struct RecurGradArgs {
-    Plane dy, f, x, o, df, dx, d_o;
+    Plane f, x, o, dy, df, dx, d_o;
     Sequences at;
-    const float *states, *d_last;
+    const float *states, *d_last, *starts;
     float *d_state;
     int col_tiles, words;
 };
 
+// ---- two columns at a time: one instruction for the two products or sums
+__device__ __forceinline__ uint64_t bits_of(float2 v) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 pair_of(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ float2 operator+(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 operator*(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)), "l"(bits_of(c)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float exp2_f(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 operator-(float2 a, float2 b) { return fma2(b, both(-1.f), a); }
+__device__ __forceinline__ float2 operator-(float2 a) { return make_float2(-a.x, -a.y); }
+
+template <bool F16>
+__device__ __forceinline__ float2 values_of(uint32_t w) {
+    return make_float2(from16<F16>(F16 ? w & 0xffffu : w), F16 ? from16<F16>(w >> 16) : __uint_as_float(w & 0xffff0000u));
+}
+template <int ACT>
+__device__ __forceinline__ float2 act2(float2 z) {
+    return make_float2(act_of<ACT>(z.x), act_of<ACT>(z.y));
+}
+
 // Two neighbouring columns, of which `valid` exist.
-__device__ __forceinline__ uint32_t load_pair(const Plane &a, int64_t r, int c, int valid, bool words) {
-    const uint16_t *const p = reinterpret_cast<const uint16_t *>(a.p + r * a.row_bytes) + c;
+__device__ __forceinline__ uint32_t load_pair(const uint8_t *p, int valid, bool words) {
     if (words && valid == 2) return __ldg(reinterpret_cast<const uint32_t *>(p));
+    const uint16_t *const h = reinterpret_cast<const uint16_t *>(p);
     uint32_t v = 0;
-    if (valid > 0) v = __ldg(p);
-    if (valid > 1) v |= (uint32_t)__ldg(p + 1) << 16;
+    if (valid > 0) v = __ldg(h);
+    if (valid > 1) v |= (uint32_t)__ldg(h + 1) << 16;
     return v;
 }
-__device__ __forceinline__ void store_pair(const Plane &a, int64_t r, int c, int valid, bool words, uint32_t v) {
-    uint16_t *const p = reinterpret_cast<uint16_t *>(a.p + r * a.row_bytes) + c;
+__device__ __forceinline__ void store_pair(uint8_t *p, int valid, bool words, uint32_t v) {
+    uint16_t *const h = reinterpret_cast<uint16_t *>(p);
     if (words && valid == 2) {
         *reinterpret_cast<uint32_t *>(p) = v;
         return;
     }
-    if (valid > 0) p[0] = (uint16_t)v;
-    if (valid > 1) p[1] = (uint16_t)(v >> 16);
+    if (valid > 0) h[0] = (uint16_t)v;
+    if (valid > 1) h[1] = (uint16_t)(v >> 16);
 }
-template <bool F16>
-__device__ __forceinline__ float half_of(uint32_t w, int which) {
-    return which ? (F16 ? from16<F16>(w >> 16) : __uint_as_float(w & 0xffff0000u)) : from16<F16>(F16 ? w & 0xffffu : w);
-}
+__device__ __forceinline__ uint8_t *place(const Plane &a, int64_t row, int col) { return a.p + row * a.row_bytes + 2 * (int64_t)col; }
+
 // fp32 states [..][n]
-__device__ __forceinline__ void load_state(const float *p, int64_t row, int n, int c, int valid, float (&v)[2]) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) v[j] = p && j < valid ? p[row * n + c + j] : 0.f;
+__device__ __forceinline__ float2 load_state(const float *p, int64_t row, int n, int c, int valid) {
+    p += row * n + c;
+    return make_float2(valid > 0 ? p[0] : 0.f, valid > 1 ? p[1] : 0.f);
 }
-__device__ __forceinline__ void store_state(float *p, int64_t row, int n, int c, int valid, const float (&v)[2]) {
-    if (!p) return;
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-        if (j < valid) p[row * n + c + j] = v[j];
+__device__ __forceinline__ void store_state(float *p, int64_t row, int n, int c, int valid, float2 v) {
+    p += row * n + c;
+    if (valid > 0) p[0] = v.x;
+    if (valid > 1) p[1] = v.y;
 }
 
-// Factors held as q (above); -0 is the complement 0.
-__device__ __forceinline__ bool is_complement(float q) { return __float_as_int(q) < 0; }
-// a step's: of exp(f), beyond 80 of which 1 - a is 0 already
-__device__ __forceinline__ float factor_of(float f) {
-    const float e = exp_f(f > 80.f ? 80.f : f), b = reciprocal_f(1.f + e);
-    return e > 1.f ? -b : e * b;
+// ---- a step's factor, as m = a - 1 = -1 / (1 + exp(f))
+template <bool F16>
+__device__ __forceinline__ float2 minus_rest(uint32_t w) {
+    const float2 z = values_of<F16>(w) * both(kLog2E);
+    const float2 d = fma2(make_float2(exp2_f(z.x), exp2_f(z.y)), both(-1.f), both(-1.f));  // -infinity: keeps all
+    return make_float2(reciprocal_f(d.x), reciprocal_f(d.y));
 }
-__device__ __forceinline__ float times(float q, float v) { return fmaf(q, v, is_complement(q) ? v : 0.f); }  // a v
-__device__ __forceinline__ float complement(float q) { return is_complement(q) ? -q : 1.f - q; }            // 1 - a
-// a h + (1 - a) x
-__device__ __forceinline__ float step(float q, float h, float x) { return fmaf(q, h - x, is_complement(q) ? h : x); }
-// of a run, from its product and its complement
+constexpr uint32_t kKeepAll16 = 0x7c007c00u, kKeepAll = 0x7f807f80u;  // f of a step that is not there: infinity
+__device__ __forceinline__ float2 step(float2 m, float2 h, float2 x) { return fma2(m, h - x, h); }  // a h + (1 - a) x
+__device__ __forceinline__ float2 kept(float2 m, float2 v) { return fma2(m, v, v); }                // a v
+// a (1 - a): a = exp(f) (1 - a), right to its last bits where it is small too; beyond 80 it is 1
+__device__ __forceinline__ float slope_of(float f, float m) {
+    const float b = -m;
+    return exp2_f((f > 80.f ? 80.f : f) * kLog2E) * b * b;
+}
+
+// ---- a run's factor, held as q (above); -0 is the complement 0
+__device__ __forceinline__ bool is_complement(float q) { return __float_as_int(q) < 0; }
+__device__ __forceinline__ float times(float q, float v) { return fmaf(q, v, is_complement(q) ? v : 0.f); }
+__device__ __forceinline__ float2 times(float2 q, float2 v) {
+    return fma2(q, v, make_float2(is_complement(q.x) ? v.x : 0.f, is_complement(q.y) ? v.y : 0.f));
+}
 __device__ __forceinline__ float factor_of(float product, float complement) { return complement < 0.5f ? -complement : product; }
 __device__ __forceinline__ float product_of(float p, float q) {  // of two runs
     if (!is_complement(p) || !is_complement(q)) return is_complement(p) ? times(p, q) : times(q, p);
@@ -124,233 +212,438 @@ __device__ __forceinline__ float product_of(float p, float q) {  // of two runs
     return c < 0.5f ? -c : 1.f - c;
 }
 
-// Runs of two columns: (q0, H0, q1, H1).
-__device__ __forceinline__ void then(float (&state)[2], const float4 &run) {
-    state[0] = run.y + times(run.x, state[0]);
-    state[1] = run.w + times(run.z, state[1]);
+// Runs of two columns: (q0, q1, H0, H1).
+__device__ __forceinline__ float2 then(float2 state, const float4 &run) {
+    return make_float2(run.z, run.w) + times(make_float2(run.x, run.y), state);
 }
-__device__ __forceinline__ void join(float4 &a, const float4 &b) {  // a, then b
-    a.y = b.y + times(b.x, a.y);
-    a.w = b.w + times(b.z, a.w);
-    a.x = product_of(a.x, b.x);
-    a.z = product_of(a.z, b.z);
+__device__ __forceinline__ float4 join(const float4 &a, const float4 &b) {  // a, then b
+    const float2 h = then(make_float2(a.z, a.w), b);
+    return make_float4(product_of(a.x, b.x), product_of(a.y, b.y), h.x, h.y);
 }
 
-// The cluster's tiles of this round: each block's run is written to every block.
-__device__ __forceinline__ void share(float4 (*slots)[16], const float4 &run, int rank, int cluster, int lane) {
-    const uint32_t mine = smem_u32(&slots[rank][lane]);
-    for (int other = 0; other < cluster; ++other) {
-        const uint32_t to = cluster_addr(mine, other);
-        store_cluster(to, __float_as_uint(run.x));
-        store_cluster(to + 4, __float_as_uint(run.y));
-        store_cluster(to + 8, __float_as_uint(run.z));
-        store_cluster(to + 12, __float_as_uint(run.w));
-    }
+// ---- a tile in shared memory: kTile rows of 32 columns to a matrix
+constexpr int kPlane = kTile * kLanes;  // words
+// The words of a thread's run: word i is its step i.
+__device__ __forceinline__ uint32_t *run_of(uint32_t *plane, int run, int lane) { return plane + run * kLen * kLanes + lane; }
+
+// Rows row .. row + kTile - 1 into `plane`, those from `end` on as `fill`, by all threads.
+__device__ __forceinline__ void fill_plane(uint32_t *plane, const Plane &a, int64_t row, int64_t end, int col, int valid, bool words,
+                                           uint32_t fill) {
+    const int lane = threadIdx.x % kLanes;
+    int r = threadIdx.x / kLanes;
+    const uint8_t *p = place(a, row + r, col);
+#pragma unroll 8
+    for (int i = 0; i < kLen; ++i, r += kRuns, p += kRuns * a.row_bytes)
+        plane[r * kLanes + lane] = row + r < end ? load_pair(p, valid, words) : fill;
+}
+__device__ __forceinline__ void empty_plane(const uint32_t *plane, const Plane &a, int64_t row, int64_t end, int col, int valid, bool words) {
+    const int lane = threadIdx.x % kLanes;
+    int r = threadIdx.x / kLanes;
+    uint8_t *p = place(a, row + r, col);
+#pragma unroll 8
+    for (int i = 0; i < kLen; ++i, r += kRuns, p += kRuns * a.row_bytes)
+        if (row + r < end) store_pair(p, valid, words, plane[r * kLanes + lane]);
 }
 
-// A half warp's run from state 0, and its steps' factors; steps from `count` on change nothing.
+// The steps of a thread's run that the sequence does not have, in each of N planes.
+template <int N>
+__device__ __forceinline__ void mask_run(uint32_t *planes, int run, int lane, int count, uint32_t keep_all) {
+    for (int i = count; i < kLen; ++i)
+#pragma unroll
+        for (int k = 0; k < N; ++k) run_of(planes + k * kPlane, run, lane)[i * kLanes] = k == 0 ? keep_all : 0u;
+}
+
+// A half warp's run from state 0, and its steps' factors.
 template <bool F16>
-__device__ __forceinline__ float4 local_run(const uint32_t (&wf)[kLen], const uint32_t (&wx)[kLen], int count,
-                                            float (&q)[kLen][2]) {
-    float h[2] = {0.f, 0.f}, product[2] = {1.f, 1.f}, rest[2] = {0.f, 0.f};
+__device__ __forceinline__ float4 local_run(const uint32_t *f, const uint32_t *x, float2 (&m)[kLen]) {
+    float2 h = both(0.f), product = both(1.f), rest = both(0.f);
 #pragma unroll
-    for (int i = 0; i < kLen; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            q[i][j] = i < count ? factor_of(half_of<F16>(wf[i], j)) : -0.f;
-            h[j] = step(q[i][j], h[j], half_of<F16>(wx[i], j));
-            rest[j] = step(q[i][j], rest[j], 1.f);
-            product[j] = times(q[i][j], product[j]);
-        }
-    return make_float4(factor_of(product[0], rest[0]), h[0], factor_of(product[1], rest[1]), h[1]);
+    for (int i = 0; i < kLen; ++i) {
+        m[i] = minus_rest<F16>(f[i * kLanes]);
+        h = step(m[i], h, values_of<F16>(x[i * kLanes]));
+        rest = step(m[i], rest, both(1.f));
+        product = kept(m[i], product);
+    }
+    return make_float4(factor_of(product.x, rest.x), factor_of(product.y, rest.y), h.x, h.y);
 }
 
+// The same from its end, for p.
 template <bool F16, int ACT>
-__global__ void __launch_bounds__(kThreads) recur_kernel(const __grid_constant__ RecurArgs a, int cluster) {
-    __shared__ float4 runs[2][kRuns][16];
-    __shared__ float4 tiles[2][kMostCluster][16];
-    const int run = threadIdx.x / 16, lane = threadIdx.x % 16;
-    const int rank = cluster > 1 ? (int)cluster_rank() : 0;
-    const int unit = blockIdx.x / cluster, s = unit / a.col_tiles;
-    const int col = (unit - s * a.col_tiles) * kCols + 2 * lane, n = a.at.n;
-    const int valid = min(max(n - col, 0), 2);
+__device__ __forceinline__ float2 local_back(const float2 (&m)[kLen], const uint32_t *d, const uint32_t *o, bool gated) {
+    float2 p = both(0.f);
+#pragma unroll
+    for (int i = kLen - 1; i >= 0; --i) {
+        const float2 dy = values_of<F16>(d[i * kLanes]);
+        p = kept(m[i], gated ? fma2(dy, act2<ACT>(values_of<F16>(o[i * kLanes])), p) : p + dy);
+    }
+    return p;
+}
+
+// Where a block works: a sequence's columns, all of its tiles or the one at a place.
+struct Unit {
+    int run, lane, seq, col0, col, valid;
+    int r0, r1, tile, tiles;  // the sequence's rows; the tiles to do, from `tile` on (or from its end)
+    __device__ __forceinline__ Unit(const Sequences &at, int col_tiles, bool one_tile)
+        : run(threadIdx.x / kLanes), lane(threadIdx.x % kLanes) {
+        const int unit = blockIdx.x / col_tiles;
+        col0 = ((int)blockIdx.x - unit * col_tiles) * kCols;
+        col = col0 + 2 * lane;
+        valid = min(max(at.n - col, 0), 2);
+        seq = one_tile ? at.at_place(unit) : unit;
+        at.rows_of(seq, r0, r1);
+        tiles = (r1 - r0 + kTile - 1) / kTile;
+        tile = 0;
+        if (one_tile) {
+            tile = unit - (int)place_of(r0, 0, seq);
+            tiles = tile >= 0 && tile < tiles ? 1 : 0;
+        }
+    }
+};
+
+// Tiles on their way: two stages of planes, filled by TMA a tile ahead, one barrier each.
+// A stage's results take its inputs' places and leave by TMA too, where rows are whole
+// pieces of 16 bytes (at 31 columns a store wrote the 32nd, the caller's padding); it is
+// filled again once they are read, in the middle of the next tile.
+struct Pipe {
+    uint32_t *stages;  // [2][planes][kPlane]
+    uint64_t *full;    // [2]
+    int planes;
+    Guard guard;
+    bool ok = true;
+
+    __device__ __forceinline__ void start() {
+        if (threadIdx.x == 0) {
+            mbar_init(smem_u32(full), 1);
+            mbar_init(smem_u32(full + 1), 1);
+            *guard.abort = 0;
+            fence_mbar_init();
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ uint32_t *stage(int s) const { return stages + s * planes * kPlane; }
+    // One thread: the tile of rows row .. into stage s.
+    __device__ __forceinline__ void load(const Tiles &t, const bool (&has)[kMostIn], int s, int col, int row) const {
+        const uint32_t bar = smem_u32(full + s);
+        int bytes = 0;
+#pragma unroll
+        for (int k = 0; k < kMostIn; ++k) bytes += has[k] ? 4 * kPlane : 0;
+        mbar_expect_tx(bar, bytes);
+#pragma unroll
+        for (int k = 0; k < kMostIn; ++k)
+            if (has[k]) tma_load_2d(smem_u32(stage(s) + k * kPlane), &t.in[k], bar, col, row);
+    }
+    __device__ __forceinline__ void wait(int s, uint32_t parity) {
+        if (ok) ok = wait_bounded(smem_u32(full + s), parity, guard);
+    }
+};
+
+// Results in flight have been read when a block leaves; copies in flight after a wait
+// that gave up land within microseconds: they are left a millisecond.
+__device__ __forceinline__ void pipe_end(const Pipe &pipe) {
+    if (threadIdx.x == 0) bulk_wait_read();
+    if (pipe.ok) return;
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 1000000u) {
+    }
+}
+
+// The tiles of a sequence one after another, or (a.starts) a tile.
+template <bool F16, int ACT, bool TMA>
+__global__ void __launch_bounds__(kThreads, 4) recur_kernel(const __grid_constant__ RecurArgs a, const __grid_constant__ Tiles maps) {
+    extern __shared__ __align__(128) uint32_t planes[];
+    __shared__ float4 runs[2][kRuns][kLanes];
+    __shared__ uint64_t full[2];
+    __shared__ uint32_t abort_flag;
+    const int n = a.at.n;
     const bool words = a.words != 0, gated = a.o.p != nullptr;
-    if (cluster > 1) cluster_arrive();
+    constexpr uint32_t kFill = F16 ? kKeepAll16 : kKeepAll;
+    Pipe pipe{planes, full, 3, {&abort_flag, maps.waits.status, maps.waits.timeout_ns}};
+    if (TMA) pipe.start();
+    pdl_trigger();
+    pdl_wait();
+    const Unit u(a.at, a.col_tiles, a.starts != nullptr);
+    const bool has[kMostIn] = {true, true, gated, false};
+    auto fetch = [&](int i, int s) {  // the i-th tile
+        if (TMA && threadIdx.x == 0 && i < u.tiles) pipe.load(maps, has, s, u.col0, u.r0 + (u.tile + i) * kTile);
+    };
+    fetch(0, 0);
+    fetch(1, 1);
+    float2 carry = both(0.f);
+    if (a.starts) {
+        if (u.tiles > 0) carry = load_state(a.starts, place_of(u.r0, u.tile, u.seq), n, u.col, u.valid);
+    } else if (a.state) {
+        carry = load_state(a.state, u.seq, n, u.col, u.valid);
+    }
+    int turn = 0, parity = 0;
+    for (int i = 0; i < u.tiles; ++i) {
+        const int64_t row = (int64_t)u.r0 + (int64_t)(u.tile + i) * kTile;
+        const int count = (int)max(min((int64_t)kLen, u.r1 - row - u.run * kLen), (int64_t)0);  // steps of this run
+        uint32_t *const stage = TMA ? pipe.stage(turn) : planes;
+        if (TMA) {
+            pipe.wait(turn, parity);
+        } else {
+            __syncthreads();  // the results of the tile before have left
+            fill_plane(stage, a.f, row, u.r1, u.col, u.valid, words, kFill);
+            fill_plane(stage + kPlane, a.x, row, u.r1, u.col, u.valid, words, 0u);
+            if (gated) fill_plane(stage + 2 * kPlane, a.o, row, u.r1, u.col, u.valid, words, 0u);
+            __syncthreads();
+        }
+        if (count < kLen) mask_run<3>(stage, u.run, u.lane, count, kFill);
+        const uint32_t *const f = run_of(stage, u.run, u.lane), *const o = run_of(stage + 2 * kPlane, u.run, u.lane);
+        uint32_t *const x = run_of(stage + kPlane, u.run, u.lane);
+        float2 m[kLen], h;
+        runs[turn][u.run][u.lane] = local_run<F16>(f, x, m);
+        __syncthreads();
+        if (TMA && i > 0) {  // the other stage's results have been read: its next tile
+            if (threadIdx.x == 0) bulk_wait_read();
+            fetch(i + 1, turn ^ 1);
+        }
+        if (a.states && u.run == 0) store_state(a.states, place_of(u.r0, u.tile + i, u.seq), n, u.col, u.valid, carry);
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) {
+            if (r == u.run) h = carry;
+            carry = then(carry, runs[turn][r][u.lane]);
+        }
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) {
+            h = step(m[j], h, values_of<F16>(x[j * kLanes]));
+            const float2 y = gated ? h * act2<ACT>(values_of<F16>(o[j * kLanes])) : h;
+            x[j * kLanes] = pack16<F16>(y.x, y.y);
+        }
+        if (TMA) bulk_fence();
+        __syncthreads();
+        if (TMA && n % 8 == 0 && row + kTile <= u.r1) {
+            if (threadIdx.x == 0) bulk_store(&maps.out[0], smem_u32(stage + kPlane), u.col0, (int)row);
+        } else {
+            empty_plane(stage + kPlane, a.y, row, u.r1, u.col, u.valid, words);
+        }
+        parity ^= turn;
+        turn ^= 1;
+    }
+    if (a.last && !a.starts && u.run == 0) store_state(a.last, u.seq, n, u.col, u.valid, carry);
+    if (TMA) pipe_end(pipe);
+}
+
+// Backwards: the tiles of a sequence from its last, or (a.starts) a tile.
+template <bool F16, int ACT, bool TMA>
+__global__ void __launch_bounds__(kThreads, 3) recur_grad_kernel(const __grid_constant__ RecurGradArgs a,
+                                                                 const __grid_constant__ Tiles maps) {
+    extern __shared__ __align__(128) uint32_t planes[];
+    __shared__ float4 runs[2][kRuns][kLanes];  // q and H of the runs
+    __shared__ float2 back[2][kRuns][kLanes];  // R
+    __shared__ uint64_t full[2];
+    __shared__ uint32_t abort_flag;
+    const int n = a.at.n;
+    const bool words = a.words != 0, gated = a.o.p != nullptr;
+    constexpr uint32_t kFill = F16 ? kKeepAll16 : kKeepAll;
+    Pipe pipe{planes, full, 4, {&abort_flag, maps.waits.status, maps.waits.timeout_ns}};
+    if (TMA) pipe.start();
+    pdl_trigger();
+    pdl_wait();
+    const Unit u(a.at, a.col_tiles, a.starts != nullptr);
+    const bool has[kMostIn] = {true, true, gated, true};
+    auto fetch = [&](int i, int s) {
+        if (TMA && threadIdx.x == 0 && i < u.tiles) pipe.load(maps, has, s, u.col0, u.r0 + (u.tile + u.tiles - 1 - i) * kTile);
+    };
+    fetch(0, 0);
+    fetch(1, 1);
+    float2 carry = both(0.f);
+    if (a.starts) {
+        if (u.tiles > 0) carry = load_state(a.starts, place_of(u.r0, u.tile, u.seq), n, u.col, u.valid);
+    } else if (a.d_last) {
+        carry = load_state(a.d_last, u.seq, n, u.col, u.valid);
+    }
+    int turn = 0, parity = 0;
+    for (int i = 0; i < u.tiles; ++i) {
+        const int tile = u.tile + u.tiles - 1 - i;
+        const int64_t row = (int64_t)u.r0 + (int64_t)tile * kTile;
+        const int count = (int)max(min((int64_t)kLen, u.r1 - row - u.run * kLen), (int64_t)0);
+        uint32_t *const stage = TMA ? pipe.stage(turn) : planes;
+        float2 h = load_state(a.states, place_of(u.r0, tile, u.seq), n, u.col, u.valid);
+        if (TMA) {
+            pipe.wait(turn, parity);
+        } else {
+            __syncthreads();  // the results of the tile before have left
+            fill_plane(stage, a.f, row, u.r1, u.col, u.valid, words, kFill);
+            fill_plane(stage + kPlane, a.x, row, u.r1, u.col, u.valid, words, 0u);
+            if (gated) fill_plane(stage + 2 * kPlane, a.o, row, u.r1, u.col, u.valid, words, 0u);
+            fill_plane(stage + 3 * kPlane, a.dy, row, u.r1, u.col, u.valid, words, 0u);
+            __syncthreads();
+        }
+        if (count < kLen) mask_run<4>(stage, u.run, u.lane, count, kFill);
+        uint32_t *const f = run_of(stage, u.run, u.lane), *const x = run_of(stage + kPlane, u.run, u.lane),
+                 *const o = run_of(stage + 2 * kPlane, u.run, u.lane);
+        const uint32_t *const d = run_of(stage + 3 * kPlane, u.run, u.lane);
+        float2 m[kLen], p;
+        runs[turn][u.run][u.lane] = local_run<F16>(f, x, m);
+        back[turn][u.run][u.lane] = local_back<F16, ACT>(m, d, o, gated);
+        __syncthreads();
+        if (TMA && i > 0) {
+            if (threadIdx.x == 0) bulk_wait_read();
+            fetch(i + 1, turn ^ 1);
+        }
+#pragma unroll
+        for (int r = kRuns - 1; r >= 0; --r) {
+            if (r == u.run) p = carry;
+            const float4 c = runs[turn][r][u.lane];
+            carry = back[turn][r][u.lane] + times(make_float2(c.x, c.y), carry);
+        }
+        for (int r = 0; r < u.run; ++r) h = then(h, runs[turn][r][u.lane]);
+        float2 before[kLen + 1];  // the state before each step, and after the last
+        before[0] = h;
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) before[j + 1] = step(m[j], before[j], values_of<F16>(x[j * kLanes]));
+#pragma unroll
+        for (int j = kLen - 1; j >= 0; --j) {
+            const float2 dy = values_of<F16>(d[j * kLanes]), xj = values_of<F16>(x[j * kLanes]);
+            float2 g = p + dy;
+            if (gated) {
+                const float2 oj = values_of<F16>(o[j * kLanes]);
+                float2 act, slope;
+                act_slope<ACT>(oj.x, act.x, slope.x);
+                act_slope<ACT>(oj.y, act.y, slope.y);
+                g = fma2(dy, act, p);
+                const float2 d_o = dy * slope * before[j + 1];
+                o[j * kLanes] = pack16<F16>(d_o.x, d_o.y);
+            }
+            const float2 fj = values_of<F16>(f[j * kLanes]), slope_f = make_float2(slope_of(fj.x, m[j].x), slope_of(fj.y, m[j].y));
+            const float2 dx = -m[j] * g, df = g * (before[j] - xj) * slope_f;
+            f[j * kLanes] = pack16<F16>(df.x, df.y);
+            x[j * kLanes] = pack16<F16>(dx.x, dx.y);
+            p = kept(m[j], g);
+        }
+        if (TMA) bulk_fence();
+        __syncthreads();
+        const Plane *const out[3] = {&a.df, &a.dx, &a.d_o};
+        if (TMA && n % 8 == 0 && row + kTile <= u.r1) {
+            if (threadIdx.x == 0) {
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (out[k]->p) bulk_store(&maps.out[k], smem_u32(stage + k * kPlane), u.col0, (int)row);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                if (out[k]->p) empty_plane(stage + k * kPlane, *out[k], row, u.r1, u.col, u.valid, words);
+        }
+        parity ^= turn;
+        turn ^= 1;
+    }
+    if (a.d_state && !a.starts && u.run == 0) store_state(a.d_state, u.seq, n, u.col, u.valid, carry);
+    if (TMA) pipe_end(pipe);
+}
+
+// ---- independent tiles
+// What a tile makes of what comes into it: [place][n] of q and of H (or backwards of R).
+struct Sum {
+    float *factor, *made;
+};
+// BACK: R from f, o and dy; else H from f and x.
+template <bool F16, int ACT, bool BACK, bool TMA>
+__global__ void __launch_bounds__(kThreads) tile_sum_kernel(const __grid_constant__ RecurGradArgs a, const __grid_constant__ Tiles maps,
+                                                            const Sum sum) {
+    __shared__ __align__(128) uint32_t planes[(BACK ? kMostIn : 2) * kPlane];
+    __shared__ float4 runs[kRuns][kLanes];
+    __shared__ uint64_t full[2];
+    __shared__ uint32_t abort_flag;
+    const bool words = a.words != 0, gated = BACK && a.o.p != nullptr;
+    constexpr uint32_t kFill = F16 ? kKeepAll16 : kKeepAll;
+    constexpr int kX = BACK ? 3 : 1;  // the plane of x or dy
+    Pipe pipe{planes, full, 0, {&abort_flag, maps.waits.status, maps.waits.timeout_ns}};
+    if (TMA) pipe.start();
+    pdl_trigger();
+    pdl_wait();
+    const Unit u(a.at, a.col_tiles, true);
+    if (u.tiles == 0) return;
+    const int64_t row = (int64_t)u.r0 + (int64_t)u.tile * kTile;
+    if (TMA) {
+        const bool has[kMostIn] = {true, !BACK, gated, BACK};
+        if (threadIdx.x == 0) pipe.load(maps, has, 0, u.col0, (int)row);
+        pipe.wait(0, 0);
+    } else {
+        fill_plane(planes, a.f, row, u.r1, u.col, u.valid, words, kFill);
+        fill_plane(planes + kX * kPlane, BACK ? a.dy : a.x, row, u.r1, u.col, u.valid, words, 0u);
+        if (gated) fill_plane(planes + 2 * kPlane, a.o, row, u.r1, u.col, u.valid, words, 0u);
+        __syncthreads();
+    }
+    const int count = (int)max(min((int64_t)kLen, u.r1 - row - u.run * kLen), (int64_t)0);
+    if (count < kLen) mask_run<BACK ? 4 : 2>(planes, u.run, u.lane, count, kFill);
+    float2 m[kLen];
+    const uint32_t *const x = run_of(planes + kX * kPlane, u.run, u.lane);
+    float4 mine = local_run<F16>(run_of(planes, u.run, u.lane), x, m);
+    if (BACK) {
+        const float2 p = local_back<F16, ACT>(m, x, run_of(planes + 2 * kPlane, u.run, u.lane), gated);
+        mine.z = p.x;
+        mine.w = p.y;
+    }
+    runs[u.run][u.lane] = mine;
+    __syncthreads();
+    if (u.run == 0) {
+        float4 all = runs[BACK ? kRuns - 1 : 0][u.lane];
+#pragma unroll
+        for (int r = 1; r < kRuns; ++r) all = join(all, runs[BACK ? kRuns - 1 - r : r][u.lane]);
+        const int64_t place = place_of(u.r0, u.tile, u.seq);
+        store_state(sum.factor, place, a.at.n, u.col, u.valid, make_float2(all.x, all.y));
+        store_state(sum.made, place, a.at.n, u.col, u.valid, make_float2(all.z, all.w));
+    }
+    if (TMA) pipe_end(pipe);
+}
+
+// Along a sequence's tiles, a column to a lane: what comes into each (starts) and what comes
+// out in the end.  Each warp takes a few neighbouring tiles in registers and joins them, the
+// warps meet in shared memory, and each goes along its own from what those before it make.
+constexpr int kScanWarps = 32, kScanTiles = 8;
+template <bool BACK>
+__global__ void __launch_bounds__(32 * kScanWarps) tile_scan_kernel(const __grid_constant__ Sequences at, const Sum sum, const float *begin,
+                                                                    float *starts, float *end, int col_tiles) {
+    __shared__ float2 shares[2][kScanWarps][32];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    const int seq = blockIdx.x / col_tiles, n = at.n, col = ((int)blockIdx.x - seq * col_tiles) * 32 + lane;
     pdl_trigger();
     pdl_wait();
     int r0, r1;
-    a.at.rows_of(s, r0, r1);
-    float carry[2];
-    load_state(a.state, s, n, col, valid, carry);
-    if (cluster > 1) cluster_wait();
-    const int all = (r1 - r0 + kTile - 1) / kTile;
+    at.rows_of(seq, r0, r1);
+    const int tiles = (r1 - r0 + kTile - 1) / kTile;
+    const bool in = col < n;
+    // (`end` may be `begin`: it is written after every thread's last barrier, or by the one that reads it)
+    float carry = begin && in ? begin[(int64_t)seq * n + col] : 0.f;
     int turn = 0;
-    for (int first = 0; first < all; first += cluster, turn ^= 1) {
-        const int tile = first + rank;
-        const int64_t row = (int64_t)r0 + (int64_t)tile * kTile + run * kLen;
-        const int count = (int)min((int64_t)kLen, r1 - row);  // of this run; none if negative
-        uint32_t wf[kLen], wx[kLen], wo[kLen];
+    for (int t0 = 0; t0 < tiles; t0 += kScanWarps * kScanTiles, turn ^= 1) {
+        // tile t of the order that is gone along
+        auto index = [&](int t) { return place_of(r0, BACK ? tiles - 1 - t : t, seq) * n + col; };
+        const int first = t0 + warp * kScanTiles;
+        float q[kScanTiles], made[kScanTiles];
 #pragma unroll
-        for (int i = 0; i < kLen; ++i) {
-            wf[i] = wx[i] = wo[i] = 0u;
-            if (i >= count) continue;
-            wf[i] = load_pair(a.f, row + i, col, valid, words);
-            wx[i] = load_pair(a.x, row + i, col, valid, words);
-            if (gated) wo[i] = load_pair(a.o, row + i, col, valid, words);
+        for (int i = 0; i < kScanTiles; ++i) {
+            q[i] = -0.f;  // keeps all, makes nothing
+            made[i] = 0.f;
+            if (in && first + i < tiles) {
+                q[i] = sum.factor[index(first + i)];
+                made[i] = sum.made[index(first + i)];
+            }
         }
-        float q[kLen][2], h[2];
-        runs[turn][run][lane] = local_run<F16>(wf, wx, count, q);
+        float factor = -0.f, all = 0.f;
+#pragma unroll
+        for (int i = 0; i < kScanTiles; ++i) {
+            all = made[i] + times(q[i], all);
+            factor = product_of(factor, q[i]);
+        }
+        shares[turn][warp][lane] = make_float2(factor, all);
         __syncthreads();
-        if (cluster > 1) {
-            if (run == 0) {
-                float4 sum = runs[turn][0][lane];
-#pragma unroll
-                for (int r = 1; r < kRuns; ++r) join(sum, runs[turn][r][lane]);
-                share(tiles[turn], sum, rank, cluster, lane);
-            }
-            __syncwarp();
-            cluster_sync();
-            for (int other = 0; other < cluster; ++other) {
-                if (other == rank) h[0] = carry[0], h[1] = carry[1];
-                then(carry, tiles[turn][other][lane]);
-            }
-            if (run == 0 && tile < all) store_state(a.states, (int64_t)r0 / kTile + tile + s, n, col, valid, h);
-            for (int r = 0; r < run; ++r) then(h, runs[turn][r][lane]);
-        } else {
-            if (run == 0) store_state(a.states, (int64_t)r0 / kTile + tile + s, n, col, valid, carry);
-#pragma unroll
-            for (int r = 0; r < kRuns; ++r) {
-                if (r == run) h[0] = carry[0], h[1] = carry[1];
-                then(carry, runs[turn][r][lane]);
-            }
+        float v = carry;
+#pragma unroll 8
+        for (int w = 0; w < kScanWarps; ++w) {
+            if (w == warp) v = carry;
+            const float2 share = shares[turn][w][lane];
+            carry = share.y + times(share.x, carry);
         }
 #pragma unroll
-        for (int i = 0; i < kLen; ++i) {
-            if (i >= count) continue;
-            float y[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                h[j] = step(q[i][j], h[j], half_of<F16>(wx[i], j));
-                y[j] = gated ? h[j] * act_of<ACT>(half_of<F16>(wo[i], j)) : h[j];
-            }
-            store_pair(a.y, row + i, col, valid, words, pack16<F16>(y[0], y[1]));
+        for (int i = 0; i < kScanTiles; ++i) {
+            if (in && first + i < tiles) starts[index(first + i)] = v;
+            v = made[i] + times(q[i], v);
         }
     }
-    if (rank == 0 && run == 0) store_state(a.last, s, n, col, valid, carry);
-}
-
-template <bool F16, int ACT>
-__global__ void __launch_bounds__(kThreads) recur_grad_kernel(const __grid_constant__ RecurGradArgs a, int cluster) {
-    __shared__ float4 runs[2][kRuns][16];  // q and H of the runs
-    __shared__ float2 back[2][kRuns][16];  // R
-    __shared__ float4 tiles[2][kMostCluster][16];  // q and R of the tiles
-    const int run = threadIdx.x / 16, lane = threadIdx.x % 16;
-    const int rank = cluster > 1 ? (int)cluster_rank() : 0;
-    const int unit = blockIdx.x / cluster, s = unit / a.col_tiles;
-    const int col = (unit - s * a.col_tiles) * kCols + 2 * lane, n = a.at.n;
-    const int valid = min(max(n - col, 0), 2);
-    const bool words = a.words != 0, gated = a.o.p != nullptr;
-    if (cluster > 1) cluster_arrive();
-    pdl_trigger();
-    pdl_wait();
-    int r0, r1;
-    a.at.rows_of(s, r0, r1);
-    float carry[2];
-    load_state(a.d_last, s, n, col, valid, carry);
-    if (cluster > 1) cluster_wait();
-    const int all = (r1 - r0 + kTile - 1) / kTile;
-    int turn = 0;
-    for (int first = 0; first < all; first += cluster, turn ^= 1) {
-        const int tile = all - 1 - (first + rank);  // negative: nothing is left for this block
-        const int64_t row = (int64_t)r0 + (int64_t)tile * kTile + run * kLen;
-        const int count = tile < 0 ? 0 : (int)min((int64_t)kLen, r1 - row);
-        uint32_t wf[kLen], wx[kLen], wo[kLen], wd[kLen];
-#pragma unroll
-        for (int i = 0; i < kLen; ++i) {
-            wf[i] = wx[i] = wo[i] = wd[i] = 0u;
-            if (i >= count) continue;
-            wf[i] = load_pair(a.f, row + i, col, valid, words);
-            wx[i] = load_pair(a.x, row + i, col, valid, words);
-            wd[i] = load_pair(a.dy, row + i, col, valid, words);
-            if (gated) wo[i] = load_pair(a.o, row + i, col, valid, words);
-        }
-        float h[2] = {0.f, 0.f};
-        if (tile >= 0) load_state(a.states, (int64_t)r0 / kTile + tile + s, n, col, valid, h);
-        float q[kLen][2], p[2] = {0.f, 0.f};
-        runs[turn][run][lane] = local_run<F16>(wf, wx, count, q);
-#pragma unroll
-        for (int i = kLen - 1; i >= 0; --i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float dy = half_of<F16>(wd[i], j);
-                const float g = p[j] + (gated ? dy * act_of<ACT>(half_of<F16>(wo[i], j)) : dy);
-                p[j] = times(q[i][j], g);
-            }
-        back[turn][run][lane] = make_float2(p[0], p[1]);
-        __syncthreads();
-        auto down = [&](float (&v)[2], int r) {  // p past the run r
-            const float4 c = runs[turn][r][lane];
-            const float2 d = back[turn][r][lane];
-            v[0] = d.x + times(c.x, v[0]);
-            v[1] = d.y + times(c.z, v[1]);
-        };
-        if (cluster > 1) {
-            if (run == 0) {
-                float4 sum = runs[turn][kRuns - 1][lane];
-                sum.y = back[turn][kRuns - 1][lane].x;
-                sum.w = back[turn][kRuns - 1][lane].y;
-#pragma unroll
-                for (int r = kRuns - 2; r >= 0; --r) {
-                    const float4 c = runs[turn][r][lane];
-                    const float2 d = back[turn][r][lane];
-                    join(sum, make_float4(c.x, d.x, c.z, d.y));
-                }
-                share(tiles[turn], sum, rank, cluster, lane);
-            }
-            __syncwarp();
-            cluster_sync();
-            for (int other = 0; other < cluster; ++other) {
-                if (other == rank) p[0] = carry[0], p[1] = carry[1];
-                then(carry, tiles[turn][other][lane]);
-            }
-            for (int r = kRuns - 1; r > run; --r) down(p, r);
-        } else {
-#pragma unroll
-            for (int r = kRuns - 1; r >= 0; --r) {
-                if (r == run) p[0] = carry[0], p[1] = carry[1];
-                down(carry, r);
-            }
-        }
-        for (int r = 0; r < run; ++r) then(h, runs[turn][r][lane]);
-        float before[kLen][2];  // the state before each step
-#pragma unroll
-        for (int i = 0; i < kLen; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                before[i][j] = h[j];
-                h[j] = step(q[i][j], h[j], half_of<F16>(wx[i], j));
-            }
-#pragma unroll
-        for (int i = kLen - 1; i >= 0; --i) {
-            if (i >= count) continue;
-            float df[2], dx[2], d_o[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float dy = half_of<F16>(wd[i], j), x = half_of<F16>(wx[i], j);
-                float act = 1.f, slope = 0.f;
-                if (gated) act_slope<ACT>(half_of<F16>(wo[i], j), act, slope);
-                const float g = fmaf(dy, act, p[j]), size = fabsf(q[i][j]);  // a or 1 - a, the smaller
-                dx[j] = complement(q[i][j]) * g;
-                df[j] = g * (before[i][j] - x) * fmaf(-size, size, size);
-                d_o[j] = dy * slope * step(q[i][j], before[i][j], x);
-                p[j] = times(q[i][j], g);
-            }
-            if (a.df.p) store_pair(a.df, row + i, col, valid, words, pack16<F16>(df[0], df[1]));
-            if (a.dx.p) store_pair(a.dx, row + i, col, valid, words, pack16<F16>(dx[0], dx[1]));
-            if (a.d_o.p) store_pair(a.d_o, row + i, col, valid, words, pack16<F16>(d_o[0], d_o[1]));
-        }
-    }
-    if (rank == 0 && run == 0) store_state(a.d_state, s, n, col, valid, carry);
+    if (end && in && warp == 0) end[(int64_t)seq * n + col] = carry;
 }
 
 // Sequences of up to kShort steps, all of one length: two columns of one to a thread.
@@ -365,23 +658,18 @@ __global__ void __launch_bounds__(256) recur_short_kernel(const __grid_constant_
     pdl_wait();
     if (s >= a.at.seqs) return;
     const int64_t r0 = s * a.at.length;
-    float h[2];
-    load_state(a.state, s, n, col, valid, h);
-    store_state(a.states, r0 / kTile + s, n, col, valid, h);
+    float2 h = a.state ? load_state(a.state, s, n, col, valid) : both(0.f);
+    if (a.states) store_state(a.states, r0 / kTile + s, n, col, valid, h);
 #pragma unroll
     for (int i = 0; i < kShort; ++i) {
         if (i >= a.at.length) break;
-        const uint32_t f = load_pair(a.f, r0 + i, col, valid, words), x = load_pair(a.x, r0 + i, col, valid, words);
-        const uint32_t o = gated ? load_pair(a.o, r0 + i, col, valid, words) : 0u;
-        float y[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            h[j] = step(factor_of(half_of<F16>(f, j)), h[j], half_of<F16>(x, j));
-            y[j] = gated ? h[j] * act_of<ACT>(half_of<F16>(o, j)) : h[j];
-        }
-        store_pair(a.y, r0 + i, col, valid, words, pack16<F16>(y[0], y[1]));
+        const uint32_t f = load_pair(place(a.f, r0 + i, col), valid, words), x = load_pair(place(a.x, r0 + i, col), valid, words);
+        const uint32_t o = gated ? load_pair(place(a.o, r0 + i, col), valid, words) : 0u;
+        h = step(minus_rest<F16>(f), h, values_of<F16>(x));
+        const float2 y = gated ? h * act2<ACT>(values_of<F16>(o)) : h;
+        store_pair(place(a.y, r0 + i, col), valid, words, pack16<F16>(y.x, y.y));
     }
-    store_state(a.last, s, n, col, valid, h);
+    if (a.last) store_state(a.last, s, n, col, valid, h);
 }
 
 // ---------------------------------------------------------------- host
@@ -389,55 +677,134 @@ bool on_words(const emtk_matrix &m, int rows) {
     return !m.d || (reinterpret_cast<uintptr_t>(m.d) % 4 == 0 && (rows <= 1 || m.ld % 2 == 0));
 }
 
-// Blocks of a unit (32 columns of a sequence): as many as its tiles occupy, until there
-// are three for each SM.
-int cluster_of(int64_t units, int rows, int seqs, int sms) {
-    const int64_t tiles = ((int64_t)rows + (int64_t)seqs * kTile - 1) / ((int64_t)seqs * kTile);
-    int c = 1;
-    while (c < kMostCluster && units * c < 3 * sms && 2 * c <= tiles) c *= 2;
-    return c;
+// Whether blocks go along whole sequences: all of one length, and three units (32 columns
+// of one) to every two SMs.  20000 rows of 2048 columns, forward and backward: 256 units 107 and
+// 187 us, as independent tiles 103 and 212; 64 units 281 and 535, independent 95 and 202;
+// 1024 units (of 1250 rows) 59 and 134, independent as with 64.
+bool along(int seqs, int col_tiles, int sms) { return 2 * (int64_t)seqs * col_tiles >= 3 * sms; }
+int64_t places(int rows, int seqs) { return (int64_t)rows / kTile + seqs; }
+
+// Workspace of independent tiles: (q, H) and, where they are not kept anyway, the starts.
+Sum sums_in(void *workspace, int64_t places, int n) {
+    float *const p = static_cast<float *>(workspace);
+    return {p, p + places * n};
 }
+
+constexpr size_t shared_bytes(int planes, bool tma, bool along) { return (size_t)(tma && along ? 2 : 1) * planes * kPlane * 4; }
+
+bool grid_ok(int64_t blocks) { return blocks <= INT32_MAX; }
 
 template <typename Kernel, typename Args>
-cudaError_t run_tiles(Kernel kernel, const Args &a, int sms, cudaStream_t s) {
-    const int64_t units = (int64_t)a.at.seqs * a.col_tiles;
-    const int cluster = cluster_of(units, a.at.rows, a.at.seqs, sms);
-    if (units * cluster > INT32_MAX) return cudaErrorInvalidValue;
-    const dim3 grid((unsigned)(units * cluster)), block(kThreads);
-    return cluster == 1 ? launch_pdl(kernel, grid, block, 0, s, a, cluster) : launch_cluster(kernel, grid, block, cluster, s, a, cluster);
+cudaError_t run_tiles(Kernel kernel, int planes, bool tma, const Args &a, const Tiles &maps, cudaStream_t s) {
+    const bool whole = a.starts == nullptr;
+    const int64_t blocks = (whole ? a.at.seqs : places(a.at.rows, a.at.seqs)) * a.col_tiles;
+    if (!grid_ok(blocks)) return cudaErrorInvalidValue;
+    return launch_pdl(kernel, dim3((unsigned)blocks), dim3(kThreads), shared_bytes(planes, tma, whole), s, a, maps);
+}
+
+// Each tile's start, by the first two kernels.
+template <bool F16, int ACT, bool BACK>
+cudaError_t run_starts(const RecurGradArgs &a, const Tiles *maps, void *workspace, const float *begin, float *starts, float *end,
+                       cudaStream_t s) {
+    const int64_t all = places(a.at.rows, a.at.seqs), blocks = all * a.col_tiles;
+    if (!grid_ok(blocks)) return cudaErrorInvalidValue;
+    const Sum sum = sums_in(workspace, all, a.at.n);
+    const dim3 grid((unsigned)blocks), block(kThreads);
+    const cudaError_t e = maps ? launch_pdl(tile_sum_kernel<F16, ACT, BACK, true>, grid, block, 0, s, a, *maps, sum)
+                               : launch_pdl(tile_sum_kernel<F16, ACT, BACK, false>, grid, block, 0, s, a, Tiles{}, sum);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(tile_scan_kernel<BACK>, dim3((unsigned)(a.at.seqs * (int64_t)a.col_tiles)), dim3(32 * kScanWarps), 0, s, a.at, sum,
+                      begin, starts, end, a.col_tiles);
 }
 
 template <bool F16, int ACT>
-cudaError_t run(const RecurArgs &a, int sms, cudaStream_t s) {
+cudaError_t run(RecurArgs a, const Tiles *maps, void *workspace, int sms, cudaStream_t s) {
     if (!a.at.offsets && a.at.length <= kShort) {
         const int64_t blocks = ((int64_t)a.at.seqs * ((a.at.n + 1) / 2) + 255) / 256;
-        if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+        if (!grid_ok(blocks)) return cudaErrorInvalidValue;
         return launch_pdl(recur_short_kernel<F16, ACT>, dim3((unsigned)blocks), dim3(256), 0, s, a);
     }
-    return run_tiles(recur_kernel<F16, ACT>, a, sms, s);
+    if (a.at.offsets || !along(a.at.seqs, a.col_tiles, sms)) {
+        RecurGradArgs g{};
+        g.f = a.f;
+        g.x = a.x;
+        g.at = a.at;
+        g.col_tiles = a.col_tiles;
+        g.words = a.words;
+        float *const starts = a.states ? a.states : sums_in(workspace, places(a.at.rows, a.at.seqs), a.at.n).made + places(a.at.rows, a.at.seqs) * a.at.n;
+        const cudaError_t e = run_starts<F16, EMTK_ACT_NONE, false>(g, maps, workspace, a.state, starts, a.last, s);
+        if (e != cudaSuccess) return e;
+        a.starts = starts;
+        a.states = nullptr;
+    }
+    return maps ? run_tiles(recur_kernel<F16, ACT, true>, 3, true, a, *maps, s) : run_tiles(recur_kernel<F16, ACT, false>, 3, false, a, Tiles{}, s);
 }
 template <bool F16, int ACT>
-cudaError_t run(const RecurGradArgs &a, int sms, cudaStream_t s) {
-    return run_tiles(recur_grad_kernel<F16, ACT>, a, sms, s);
+cudaError_t run(RecurGradArgs a, const Tiles *maps, void *workspace, int sms, cudaStream_t s) {
+    if (a.at.offsets || !along(a.at.seqs, a.col_tiles, sms)) {
+        float *const starts = sums_in(workspace, places(a.at.rows, a.at.seqs), a.at.n).made + places(a.at.rows, a.at.seqs) * a.at.n;
+        const cudaError_t e = run_starts<F16, ACT, true>(a, maps, workspace, a.d_last, starts, a.d_state, s);
+        if (e != cudaSuccess) return e;
+        a.starts = starts;
+    }
+    return maps ? run_tiles(recur_grad_kernel<F16, ACT, true>, 4, true, a, *maps, s)
+                : run_tiles(recur_grad_kernel<F16, ACT, false>, 4, false, a, Tiles{}, s);
 }
 template <bool F16, typename Args>
-cudaError_t run(const Args &a, int act, int sms, cudaStream_t s) {
+cudaError_t run(const Args &a, const Tiles *maps, void *workspace, int act, int sms, cudaStream_t s) {
     switch (act) {
-        case EMTK_ACT_RELU: return run<F16, EMTK_ACT_RELU>(a, sms, s);
-        case EMTK_ACT_GELU: return run<F16, EMTK_ACT_GELU>(a, sms, s);
-        case EMTK_ACT_SILU: return run<F16, EMTK_ACT_SILU>(a, sms, s);
-        case EMTK_ACT_SIGMOID: return run<F16, EMTK_ACT_SIGMOID>(a, sms, s);
-        default: return run<F16, EMTK_ACT_NONE>(a, sms, s);
+        case EMTK_ACT_RELU: return run<F16, EMTK_ACT_RELU>(a, maps, workspace, sms, s);
+        case EMTK_ACT_GELU: return run<F16, EMTK_ACT_GELU>(a, maps, workspace, sms, s);
+        case EMTK_ACT_SILU: return run<F16, EMTK_ACT_SILU>(a, maps, workspace, sms, s);
+        case EMTK_ACT_SIGMOID: return run<F16, EMTK_ACT_SIGMOID>(a, maps, workspace, sms, s);
+        default: return run<F16, EMTK_ACT_NONE>(a, maps, workspace, sms, s);
     }
 }
-template <typename Args>
-cudaError_t run(const Args &a, int type, int act, int sms, cudaStream_t s) {
-    return type == EMTK_TYPE_F16 ? run<true>(a, act, sms, s) : run<false>(a, act, sms, s);
+
+// Tensor maps of the matrices that are there; false if one lies off TMA's 16-byte grid.
+template <int IN, int OUT>
+bool make_maps(const emtk_nn *nn, Tiles &t, const emtk_matrix *const (&in)[IN], const emtk_matrix *const (&out)[OUT], int rows, int n) {
+    t.waits = {nn->status, nn->timeout_ns};
+    for (const emtk_matrix *m : in)
+        if (m->d && !mm_operand_ok(m->d, m->ld, rows)) return false;
+    for (const emtk_matrix *m : out)
+        if (m->d && !mm_operand_ok(m->d, m->ld, rows)) return false;
+    for (int i = 0; i < IN; ++i)
+        if (in[i]->d && !encode_rows(nn, &t.in[i], *in[i], rows, n, kCols, kTile)) return false;
+    for (int i = 0; i < OUT; ++i)
+        if (out[i]->d && !encode_rows(nn, &t.out[i], *out[i], rows, n, kCols, kTile)) return false;
+    return rows > 0;
+}
+
+template <bool F16, int ACT>
+cudaError_t init_kernels() {
+    cudaError_t e = cudaFuncSetAttribute(recur_kernel<F16, ACT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes(3, true, true));
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(recur_grad_kernel<F16, ACT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes(4, true, true));
+    return e;
+}
+template <bool F16>
+cudaError_t init_kernels() {
+    for (const cudaError_t e : {init_kernels<F16, EMTK_ACT_NONE>(), init_kernels<F16, EMTK_ACT_RELU>(), init_kernels<F16, EMTK_ACT_GELU>(),
+                                init_kernels<F16, EMTK_ACT_SILU>(), init_kernels<F16, EMTK_ACT_SIGMOID>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
 }
 
 }  // namespace
 
-cudaError_t launch_recurrence(const emtk_recurrence_args &p, int sms, cudaStream_t s) {
+cudaError_t init_recur_kernels() {
+    const cudaError_t e = init_kernels<false>();
+    return e == cudaSuccess ? init_kernels<true>() : e;
+}
+
+size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, bool forward, int sms) {
+    if (n == 0 || seqs == 0 || (uniform && forward && rows / seqs <= kShort)) return 0;
+    const bool whole = uniform && along(seqs, (n + kCols - 1) / kCols, sms);
+    return whole ? 0 : 3 * sizeof(float) * places(rows, seqs) * n;
+}
+
+cudaError_t launch_recurrence(const emtk_recurrence_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s) {
     if (p.n == 0 || p.seqs == 0) return cudaSuccess;
     RecurArgs a{};
     a.f = plane_of(p.f);
@@ -450,16 +817,20 @@ cudaError_t launch_recurrence(const emtk_recurrence_args &p, int sms, cudaStream
     a.states = p.states;
     a.col_tiles = (p.n + kCols - 1) / kCols;
     a.words = on_words(p.f, p.rows) && on_words(p.x, p.rows) && on_words(p.o, p.rows) && on_words(p.y, p.rows);
-    return run(a, p.type, p.act, sms, s);
+    Tiles maps;
+    const emtk_matrix *const in[] = {&p.f, &p.x, &p.o}, *const out[] = {&p.y};
+    const bool tma = (p.offsets || a.at.length > kShort) && make_maps(nn, maps, in, out, p.rows, p.n);
+    return p.type == EMTK_TYPE_F16 ? run<true>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s)
+                                   : run<false>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s);
 }
 
-cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, int sms, cudaStream_t s) {
+cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s) {
     if (p.n == 0 || p.seqs == 0) return cudaSuccess;
     RecurGradArgs a{};
-    a.dy = plane_of(p.dy);
     a.f = plane_of(p.f);
     a.x = plane_of(p.x);
     a.o = plane_of(p.o);
+    a.dy = plane_of(p.dy);
     a.df = plane_of(p.df);
     a.dx = plane_of(p.dx);
     a.d_o = plane_of(p.d_o);
@@ -470,7 +841,11 @@ cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, int sms, 
     a.col_tiles = (p.n + kCols - 1) / kCols;
     a.words = on_words(p.dy, p.rows) && on_words(p.f, p.rows) && on_words(p.x, p.rows) && on_words(p.o, p.rows) &&
               on_words(p.df, p.rows) && on_words(p.dx, p.rows) && on_words(p.d_o, p.rows);
-    return run(a, p.type, p.act, sms, s);
+    Tiles maps;
+    const emtk_matrix *const in[] = {&p.f, &p.x, &p.o, &p.dy}, *const out[] = {&p.df, &p.dx, &p.d_o};
+    const bool tma = make_maps(nn, maps, in, out, p.rows, p.n);
+    return p.type == EMTK_TYPE_F16 ? run<true>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s)
+                                   : run<false>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s);
 }
 
 }  // namespace emtk

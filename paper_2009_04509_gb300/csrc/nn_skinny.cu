@@ -79,13 +79,6 @@ __device__ __forceinline__ uint2 load4(const void *base, int64_t at, int n, bool
 __device__ __forceinline__ bool wide4(const void *p, int64_t row_bytes, unsigned bytes) {
     return ((reinterpret_cast<uintptr_t>(p) | (uint64_t)row_bytes) & (bytes - 1)) == 0;
 }
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
-            dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1)
-        : "memory");
-}
 
 enum Bar : int { kBarFull = 0, kBarEmpty = 6, kBarAcc = 12, kBarDrain = 13, kBarStall = 14, kBars = 15 };
 

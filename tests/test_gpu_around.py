@@ -572,8 +572,8 @@ def recur64(f, x, o, dy, at, h0, dlast, act):
         h[who[t]] = a[row] * h[who[t]] + b[row] * x[row]
         states[row] = h[who[t]]
     gate = act64(act, o) if o is not None else torch.ones_like(f)
-    g, mag = dlast.clone(), dlast.abs()
-    out = dict(y=states * gate, last=h, states=states, before=before, dx=torch.zeros_like(f), df=torch.zeros_like(f), mag=torch.zeros_like(f))
+    g, mag, err = dlast.clone(), dlast.abs(), torch.zeros_like(dlast)
+    out = dict(y=states * gate, last=h, states=states, before=before, dx=torch.zeros_like(f), df=torch.zeros_like(f), mag=torch.zeros_like(f), err=torch.zeros_like(f))
     for t in reversed(range(steps)):
         row = [at[i] + t for i in who[t]]
         g[who[t]] += gate[row] * dy[row]
@@ -581,9 +581,11 @@ def recur64(f, x, o, dy, at, h0, dlast, act):
         out["dx"][row] = b[row] * g[who[t]]
         out["df"][row] = g[who[t]] * (before[row] - x[row]) * a[row] * b[row]
         out["mag"][row] = mag[who[t]]
+        out["err"][row] = err[who[t]]
         g[who[t]] *= a[row]
+        err[who[t]] = a[row] * err[who[t]] + (8 + 4 * f[row].abs()) * E * b[row] * mag[who[t]]
         mag[who[t]] *= a[row]
-    out.update(dstate=g, dstate_mag=mag, do=dy * states * slope64(act, o) if o is not None else None)
+    out.update(dstate=g, dstate_mag=mag, dstate_err=err, do=dy * states * slope64(act, o) if o is not None else None)
     return out
 
 
@@ -601,7 +603,9 @@ def recur_case(i):
 @pytest.mark.parametrize("i", range(48))
 def test_recurrence(lib, nn, i, dtype):
     """Both passes.  An error of b of a few E (and |f| E, of the exponential) moves the state by so much of max |x - h|;
-    the roundings of a step stay for as long as the state does, at most min(T, 1 / b) steps."""
+    the roundings of a step stay for as long as the state does, at most min(T, 1 / b) steps.  A step passes g - b g on,
+    off by b's error: (8 + 4 |f|) E b |g|, which later factors shrink as they do g (`err`); where a = 1 - b is small that
+    is more than so much of a g."""
     c = recur_case(i)
     lead, tail = (c["lead"], c["tail"]) if c["offsets"] else (0, 0)
     at = np.cumsum([lead] + c["lengths"]).tolist()
@@ -637,11 +641,11 @@ def test_recurrence(lib, nn, i, dtype):
     near(y.t[inside], want["y"][inside], dtype, (k * top * (abs(gate) + 1) + ka * want["states"].abs() * (1 + abs(gate)))[inside] if o else k * top, "y")
     kd = k + (ka if o else 0.0)
     mag = want["mag"] + (0 if not o else dy.t.double().abs())  # an activation's own error is of 1 + its value
-    near(dx.t[inside], want["dx"][inside], dtype, (2 * kd * mag * b)[inside] if o else (2 * k * want["mag"] * b)[inside], "dx")
+    near(dx.t[inside], want["dx"][inside], dtype, (2 * kd * mag * b)[inside] + (want["err"] * b)[inside], "dx")
     ab = torch.sigmoid(f64) * b
     size = (want["before"] - x64).abs() * mag * ab
-    near(df.t[inside], want["df"][inside], dtype, (4 * kd * size + 2 * k * top * mag * ab)[inside], "df")
-    near(dstate, want["dstate"], "f32", 4 * (k + 16 * E) * (want["dstate_mag"] + want["dstate"].abs()) + (16 * E * 4 if o else 0.0), "d_state")
+    near(df.t[inside], want["df"][inside], dtype, (4 * kd * size + (2 * k * top * mag + want["err"] * (want["before"] - x64).abs()) * ab)[inside], "df")
+    near(dstate, want["dstate"], "f32", 4 * (k + 16 * E) * (want["dstate_mag"] + want["dstate"].abs()) + want["dstate_err"] + (16 * E * 4 if o else 0.0), "d_state")
     if o:
         s = slope64(act, z)
         near(do.t[inside], want["do"][inside], dtype,
