@@ -637,7 +637,7 @@ emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residual_norm_gr
     Range range("emtk residual norm backward");
     void *space = nullptr;
     const emtk_status st = one_space(nn, residual_norm_workspace(a, nn->sm_count), s, &space);
-    return st != EMTK_OK ? st : status_of(launch_residual_norm_grad(a, space, nn->sm_count, s));
+    return st != EMTK_OK ? st : status_of(launch_residual_norm_grad(a, space, nn, s));
 }
 
 emtk_status emtk_logprobs(emtk_nn *nn, const emtk_logprobs_args *p, emtk_stream stream) {

@@ -43,9 +43,8 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            float v[kPiece];
+            Eight v = w[i].template values<F16>();
             uint32_t q[4];
-            w[i].template values<F16>(v);
             dropped(a.drop, offset, (uint32_t)r[i], (uint32_t)(c[i] / kPiece + lane), v);
             words8<F16>(v, q);
             store_run<ANY>(r[i] >= 0 ? a.y.row(r[i]) + c[i] : nullptr, r[i] >= 0 ? min(a.n - c[i], kPiece << a.lanes_log2) : 0, q,

@@ -14,7 +14,7 @@
 
 #include "emtk_internal.h"
 #include "nn_internal.h"
-#include "nn_math.cuh"
+#include "nn_pair.cuh"
 #include "nn_ptx.cuh"
 
 namespace emtk {
@@ -23,16 +23,10 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostTop = 32, kMostCluster = 8;
 constexpr int kFlight = 4;  // pieces of a thread in flight
-constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 constexpr float kFar = -1e4f;  // an exponent whose power is 0, in the place of -infinity where that would meet a 0
 
 __device__ __forceinline__ float minus_infinity() { return __int_as_float(0xff800000); }
-__device__ __forceinline__ float exp2_f(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 
 // Elements of each type: TYPE is an emtk_type.
 template <int TYPE>

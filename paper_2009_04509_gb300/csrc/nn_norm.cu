@@ -10,14 +10,15 @@
 //
 // Gradients.  With x^ = (x - mean) / std and q = w d of an output's gradient d, a norm's
 // input has the gradient (q - mean(q) - x^ mean(q x^)) / std (mean(q) not for RMS).  A block
-// of threads takes a slice of the rows, one after another, and adds the columns' sums (the
-// parameters' and the gate's gradients) in shared memory, where each column is one
-// thread's; a second kernel adds the slices in order, so results do not depend on timing.
+// of threads takes a slice of the rows, one after another, which bulk copies bring to shared
+// memory ahead, and adds the columns' sums (the parameters' and the gate's gradients) in shared
+// memory too, where each column is one thread's; a second kernel adds the slices in order, so results do not depend on timing.
 #include <algorithm>
 
 #include "emtk_internal.h"
 #include "nn_internal.h"
 #include "nn_pieces.cuh"
+#include "nn_ptx.cuh"
 
 namespace emtk {
 namespace {
@@ -42,75 +43,115 @@ struct SeamArgs {
     int m, n, gate_every;
 };
 
-// The sums of K values over the block's threads, in every thread.  `turn` alternates
-// between two buffers, so that one barrier a call is enough.
+// The sums of K (1, 2 or 4) values over the block's threads, in every thread.  In a warp
+// each exchange halves the values that a lane still holds, and then the lanes; the warps'
+// sums are read back with one value to a lane and added the same way: a sum costs a third
+// of the shuffles that one tree for each value would.  `turn` alternates between two
+// buffers, so that one barrier a call is enough.
+struct Reduction {
+    float (*buffer)[4 * kMaxWarps];  // [2]
+    int warps, turn;
+};
 template <int K>
-__device__ __forceinline__ void block_sum(float (&v)[K], float (*buffer)[4][kMaxWarps], int &turn, int warps) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1)
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], d);
-    if (warps == 1) return;
+__device__ __forceinline__ void block_sum(float (&v)[K], Reduction &b) {
     const int lane = threadIdx.x & 31;
-    if (lane == 0) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) buffer[turn][k][threadIdx.x / 32] = v[k];
+    float x = v[0];
+    if constexpr (K == 4) {  // lane & 3 keeps its value
+        const bool upper = (lane & 2) != 0;
+        const float k0 = upper ? v[2] : v[0], k1 = upper ? v[3] : v[1];
+        const float s0 = upper ? v[0] : v[2], s1 = upper ? v[1] : v[3];
+        const float a = k0 + __shfl_xor_sync(0xffffffffu, s0, 2), c = k1 + __shfl_xor_sync(0xffffffffu, s1, 2);
+        const bool odd = (lane & 1) != 0;
+        x = (odd ? c : a) + __shfl_xor_sync(0xffffffffu, odd ? a : c, 1);
+    } else if constexpr (K == 2) {
+        const bool odd = (lane & 1) != 0;
+        x = (odd ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 1);
     }
-    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = lane < warps ? buffer[turn][k][lane] : 0.f;
+    for (int d = K; d < 32; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
+    if (b.warps > 1) {
+        float *const buffer = b.buffer[b.turn];
+        if (lane < K) buffer[threadIdx.x / 32 * K + lane] = x;
+        __syncthreads();
+        x = 0.f;
+        for (int i = lane; i < b.warps * K; i += 32) x += buffer[i];
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1)
+        for (int d = K; d < 32; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
+        b.turn ^= 1;
+    }
 #pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], d);
-    turn ^= 1;
+    for (int k = 0; k < K; ++k) v[k] = K == 1 ? x : __shfl_sync(0xffffffffu, x, k);
 }
 
-// x becomes norm(x) w + c; columns from n on stay out of the sums.
+__device__ __forceinline__ float sum_of(const Eight &e) {
+    const float2 a = (e.v[0] + e.v[1]) + (e.v[2] + e.v[3]);
+    return a.x + a.y;
+}
+__device__ __forceinline__ float dot(const Eight &a, const Eight &b) {
+    float2 s = a.v[0] * b.v[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) s = fma2(a.v[i], b.v[i], s);
+    return s.x + s.y;
+}
+// e - mean, in the columns that are there.
+__device__ __forceinline__ void centre(Eight &e, float mean, int c, int n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.v[i] = e.v[i] - both(mean);
+    if (c + kPiece > n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.v[i] = make_float2(c + 2 * i < n ? e.v[i].x : 0.f, c + 2 * i + 1 < n ? e.v[i].y : 0.f);
+    }
+}
+
+// x becomes norm(x) weight + bias.
 template <bool F16, int C>
-__device__ __forceinline__ void normalise(const NormArgs &a, float (&x)[C][kPiece], int n, float inverse_n,
-                                          float (*buffer)[4][kMaxWarps], int &turn, int warps) {
-    float mean = 0.f;
+__device__ __forceinline__ void normalise(const NormArgs &a, Eight (&x)[C], int n, float inverse_n, Reduction &b) {
     if (a.kind == EMTK_NORM_LAYER) {
         float sum[1] = {0.f};
 #pragma unroll
-        for (int k = 0; k < C; ++k)
+        for (int k = 0; k < C; ++k) sum[0] += sum_of(x[k]);
+        block_sum(sum, b);
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) sum[0] += x[k][i];
-        block_sum(sum, buffer, turn, warps);
-        mean = sum[0] * inverse_n;
+        for (int k = 0; k < C; ++k) centre(x[k], sum[0] * inverse_n, (k * blockDim.x + threadIdx.x) * kPiece, n);
     }
     float square[1] = {0.f};
 #pragma unroll
-    for (int k = 0; k < C; ++k) {
-        const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) {
-            x[k][i] = c + i < n ? x[k][i] - mean : 0.f;
-            square[0] = fmaf(x[k][i], x[k][i], square[0]);
-        }
-    }
-    block_sum(square, buffer, turn, warps);
+    for (int k = 0; k < C; ++k) square[0] += dot(x[k], x[k]);
+    block_sum(square, b);
     const float r = rsqrtf(fmaf(square[0], inverse_n, a.eps));
 #pragma unroll
     for (int k = 0; k < C; ++k) {
         const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-        if (c >= n) continue;
-        float w[kPiece], b[kPiece];
-        param8<F16>(a.weight, c, n, 1.f, w);
-        param8<F16>(a.bias, c, n, 0.f, b);
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) x[k][i] = fmaf(x[k][i] * r, w[i], b[i]);
+        for (int i = 0; i < 4; ++i) x[k].v[i] = x[k].v[i] * both(r);
+        if (a.weight.p && c < n) {
+            const Eight w = param8<F16>(a.weight, c, n);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[k].v[i] = x[k].v[i] * w.v[i];
+        }
+        if (a.bias.p && c < n) {
+            const Eight w = param8<F16>(a.bias, c, n);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[k].v[i] = x[k].v[i] + w.v[i];
+        }
     }
+}
+
+// The run of a row that a warp stores together: from column `run` on.
+template <bool F16, bool ANY>
+__device__ __forceinline__ void store_piece(const Rows16 &to, int64_t row, int n, const Eight &e, int k) {
+    uint32_t w[4];
+    words8<F16>(e, w);
+    const int run = (k * blockDim.x + (threadIdx.x & ~31)) * kPiece;
+    store_run<ANY>(to.row(row) + run, max(0, min(n - run, 32 * kPiece)), w, 32, threadIdx.x & 31);
 }
 
 // A row to a block of threads, C pieces to a thread.
 template <bool F16, bool ANY, int C, int THREADS>
 __global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_constant__ SeamArgs a) {
-    __shared__ float buffer[2][4][kMaxWarps];
-    int turn = 0;
+    __shared__ float buffer[2][4 * kMaxWarps];
+    Reduction reduction{buffer, (int)blockDim.x / 32, 0};
     const int64_t row = blockIdx.x;
-    const int warps = blockDim.x / 32, lane = threadIdx.x & 31;
     Piece16<ANY> residual[C], block[C];
     pdl_trigger();
     pdl_wait();
@@ -122,42 +163,29 @@ __global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_con
         if (a.block.p && c < a.n) block[k].load(a.block, row, c, a.m, a.n);
         if (a.residual.p && c < a.n) residual[k].load(a.residual, row, c, a.m, a.n);
     }
-    float v[C][kPiece];
+    Eight v[C];
 #pragma unroll
-    for (int k = 0; k < C; ++k) block[k].template values<F16>(v[k]);
-    if (a.post.kind != EMTK_NORM_NONE) normalise<F16>(a.post, v, a.n, a.inverse_n, buffer, turn, warps);
+    for (int k = 0; k < C; ++k) v[k] = block[k].template values<F16>();
+    if (a.post.kind != EMTK_NORM_NONE) normalise<F16>(a.post, v, a.n, a.inverse_n, reduction);
     const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0u;
-    const Param gate{a.gate.p ? a.gate.row(row / a.gate_every) : nullptr, 0};
 #pragma unroll
     for (int k = 0; k < C; ++k) {
         const int first = k * blockDim.x + threadIdx.x, c = first * kPiece;
         if (a.drop.below) dropped(a.drop, offset, (uint32_t)row, (uint32_t)first, v[k]);
-        float g[kPiece], r[kPiece];
-        if (c < a.n) {
-            param8<F16>(gate, c, a.n, 1.f, g);
-        } else {
+        if (a.gate.p && c < a.n) {
+            const Eight g = param8<F16>({a.gate.row(row / a.gate_every), 0}, c, a.n);
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) g[i] = 0.f;
+            for (int i = 0; i < 4; ++i) v[k].v[i] = v[k].v[i] * g.v[i];
         }
-        residual[k].template values<F16>(r);
+        const Eight r = residual[k].template values<F16>();
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) v[k][i] = fmaf(v[k][i], g[i], a.scale * r[i]);
-        if (a.y.p) {
-            uint32_t w[4];
-            words8<F16>(v[k], w);
-            const int run = c - kPiece * lane;
-            store_run<ANY>(a.y.row(row) + run, max(0, min(a.n - run, 32 * kPiece)), w, 32, lane);
-        }
+        for (int i = 0; i < 4; ++i) v[k].v[i] = fma2(r.v[i], both(a.scale), v[k].v[i]);
+        if (a.y.p) store_piece<F16, ANY>(a.y, row, a.n, v[k], k);
     }
     if (a.pre.kind == EMTK_NORM_NONE) return;
-    normalise<F16>(a.pre, v, a.n, a.inverse_n, buffer, turn, warps);
+    normalise<F16>(a.pre, v, a.n, a.inverse_n, reduction);
 #pragma unroll
-    for (int k = 0; k < C; ++k) {
-        uint32_t w[4];
-        words8<F16>(v[k], w);
-        const int run = (k * blockDim.x + (threadIdx.x & ~31)) * kPiece;
-        store_run<ANY>(a.h.row(row) + run, max(0, min(a.n - run, 32 * kPiece)), w, 32, lane);
-    }
+    for (int k = 0; k < C; ++k) store_piece<F16, ANY>(a.h, row, a.n, v[k], k);
 }
 
 // ---------------------------------------------------------------- gradients
@@ -171,8 +199,11 @@ struct Slices {
     int rows;  // of a part
 };
 
+enum Input : int { kInY, kInDh, kInBlock, kInDy, kInputs };
+
 struct SeamGradArgs {
-    Rows16 dy, dh, y, block, gate, d_residual, d_block;
+    Rows16 in[kInputs];  // y, dh, block, dy
+    Rows16 gate, d_residual, d_block;
     NormArgs post, pre;
     Drop drop;
     float scale, inverse_n;
@@ -184,6 +215,7 @@ struct SeamGradArgs {
     float *spill;           // not null: the running sums, in place of shared memory, [slices][sums][columns]
     int sums;               // wanted
     int at[kSums];          // place of each among them
+    int stages, row_bytes;  // rows in shared memory, and the room for one of a matrix
 };
 
 template <int C>
@@ -192,13 +224,13 @@ struct Columns {  // a thread's running sums: [sum][piece][half][thread] of four
     __device__ __forceinline__ float4 *of(int sum, int k, int half) const {
         return base + ((sum * C + k) * 2 + half) * (int)blockDim.x + threadIdx.x;
     }
-    __device__ __forceinline__ void add(int sum, int k, const float (&v)[kPiece]) const {
+    __device__ __forceinline__ void add(int sum, int k, const Eight &e) const {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             float4 *const p = of(sum, k, half);
-            float4 s = *p;
-            s.x += v[4 * half], s.y += v[4 * half + 1], s.z += v[4 * half + 2], s.w += v[4 * half + 3];
-            *p = s;
+            const float4 s = *p;
+            const float2 a = make_float2(s.x, s.y) + e.v[2 * half], b = make_float2(s.z, s.w) + e.v[2 * half + 1];
+            *p = make_float4(a.x, a.y, b.x, b.y);
         }
     }
     // Writes columns c .. of a sum to `to` and starts it again.
@@ -215,14 +247,106 @@ struct Columns {  // a thread's running sums: [sum][piece][half][thread] of four
     }
 };
 
-template <bool F16, bool ANY, int C, int THREADS>
-__global__ void __launch_bounds__(THREADS) residual_norm_grad_kernel(const __grid_constant__ SeamGradArgs a) {
-    extern __shared__ float4 columns_smem[];
-    __shared__ float buffer[2][4][kMaxWarps];
-    int turn = 0;
-    const int warps = blockDim.x / 32, lane = threadIdx.x & 31;
+// Rows on their way into shared memory: a stage has room for one row of each matrix, as it
+// lies in its aligned 16-byte pieces, copied a row or two ahead by one thread.  Rows whose
+// outer pieces would reach beyond the matrix are copied by elements when their turn comes.
+struct RowPipe {
+    uint8_t *stages;
+    uint64_t *full;
+    Guard guard;
+    uint32_t phases = 0;  // of each stage
+    bool ok = true;
+
+    __device__ __forceinline__ uint8_t *place(const SeamGradArgs &a, int s, int input) const {
+        return stages + (s * kInputs + input) * a.row_bytes;
+    }
+    static __device__ __forceinline__ int head_of(const Rows16 &x, int64_t row) {
+        return (int)(reinterpret_cast<uintptr_t>(x.row(row)) % 16);
+    }
+    static __device__ __forceinline__ int bytes_of(const SeamGradArgs &a, int input, int64_t row) {  // of its aligned pieces
+        return (head_of(a.in[input], row) + 2 * a.n + 15) / 16 * 16;
+    }
+    static __device__ __forceinline__ bool by_hand(const SeamGradArgs &a, int64_t row) {
+        if (row >= kPiece && row < a.m - kPiece) return false;  // the 14 bytes around are of rows between
+#pragma unroll
+        for (int i = 0; i < kInputs; ++i) {
+            if (!a.in[i].p) continue;
+            const int64_t first = row * a.in[i].row_bytes - head_of(a.in[i], row), last = (a.m - 1) * a.in[i].row_bytes + 2 * a.n;
+            if (first < 0 || first + bytes_of(a, i, row) > last) return true;
+        }
+        return false;
+    }
+    // One thread starts the copies of a row.
+    __device__ __forceinline__ void fetch(const SeamGradArgs &a, int64_t row, int s) const {
+        if (by_hand(a, row)) return;
+        const uint32_t bar = smem_u32(full + s);
+        int bytes[kInputs], all = 0;
+#pragma unroll
+        for (int i = 0; i < kInputs; ++i) {
+            bytes[i] = a.in[i].p ? bytes_of(a, i, row) : 0;
+            all += bytes[i];
+        }
+        mbar_expect_tx(bar, (uint32_t)all);
+#pragma unroll
+        for (int i = 0; i < kInputs; ++i)
+            if (bytes[i])
+                bulk_load(smem_u32(place(a, s, i)), reinterpret_cast<const uint8_t *>(a.in[i].row(row)) - head_of(a.in[i], row), bytes[i], bar);
+    }
+    // All threads: the row is in stage s.
+    __device__ __forceinline__ void wait(const SeamGradArgs &a, int64_t row, int s) {
+        if (by_hand(a, row)) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kInputs; ++i) {
+                if (!a.in[i].p) continue;
+                uint16_t *const to = reinterpret_cast<uint16_t *>(place(a, s, i) + head_of(a.in[i], row));
+                for (int c = threadIdx.x; c < a.n; c += blockDim.x) to[c] = a.in[i].row(row)[c];
+            }
+            bulk_fence();
+            __syncthreads();
+            return;
+        }
+        if (ok) ok = wait_bounded(smem_u32(full + s), (phases >> s) & 1u, guard);
+        phases ^= 1u << s;
+    }
+    // A piece of the row, columns from n on 0.
+    __device__ __forceinline__ void piece(const SeamGradArgs &a, int64_t row, int s, int input, int c, uint32_t (&w)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = 0u;
+        if (!a.in[input].p || c >= a.n) return;
+        const uint4 *const p = reinterpret_cast<const uint4 *>(place(a, s, input)) + c / kPiece;
+        const int halves = head_of(a.in[input], row) / 2;
+        const uint4 lo = p[0];
+        if (halves) {
+            const uint4 hi = p[1];
+            const uint32_t x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            shift_words(x, halves, w);
+        } else {
+            w[0] = lo.x, w[1] = lo.y, w[2] = lo.z, w[3] = lo.w;
+        }
+        if (c + kPiece > a.n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] &= (c + 2 * i < a.n ? 0xffffu : 0u) | (c + 2 * i + 1 < a.n ? 0xffff0000u : 0u);
+        }
+    }
+};
+
+template <bool F16, int C>
+__global__ void __launch_bounds__(1024) residual_norm_grad_kernel(const __grid_constant__ SeamGradArgs a, int *status, int64_t timeout_ns) {
+    extern __shared__ __align__(128) uint8_t shared[];
+    __shared__ float buffer[2][4 * kMaxWarps];
+    __shared__ uint64_t full[2];
+    __shared__ uint32_t abort_flag;
+    Reduction reduction{buffer, (int)blockDim.x / 32, 0};
     const int slice = blockIdx.x;
-    Columns<C> sums{columns_smem};
+    RowPipe pipe{shared, full, {&abort_flag, status, timeout_ns}};
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(full), 1);
+        mbar_init(smem_u32(full + 1), 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    Columns<C> sums{reinterpret_cast<float4 *>(shared + a.stages * kInputs * a.row_bytes)};
     pdl_trigger();
     pdl_wait();
     if (a.spill) sums.base = reinterpret_cast<float4 *>(a.spill) + (int64_t)slice * a.sums * C * 2 * blockDim.x;
@@ -237,153 +361,178 @@ __global__ void __launch_bounds__(THREADS) residual_norm_grad_kernel(const __gri
         r0 = min((int64_t)slice * a.slices.groups_each * a.gate_every, (int64_t)a.m);
         r1 = min(r0 + (int64_t)a.slices.groups_each * a.gate_every, (int64_t)a.m);
     }
-    const bool pre = a.pre.kind != EMTK_NORM_NONE, has_block = a.block.p != nullptr;
+    const bool pre = a.pre.kind != EMTK_NORM_NONE, post = a.post.kind != EMTK_NORM_NONE, has_block = a.in[kInBlock].p != nullptr;
     const bool pre_mean = a.pre.kind == EMTK_NORM_LAYER, post_mean = a.post.kind == EMTK_NORM_LAYER;
+    const bool gate_sum = a.partial[kSumGate] || a.gate_out;
     const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0u;
-    Piece16<ANY> py[C], ph[C], pb[C], pd[C];
-    auto fetch = [&](int64_t row) {
-#pragma unroll
-        for (int k = 0; k < C; ++k) {
-            const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-            py[k].clear();
-            ph[k].clear();
-            pb[k].clear();
-            pd[k].clear();
-            if (c >= a.n) continue;
-            if (pre) py[k].load(a.y, row, c, a.m, a.n);
-            if (pre) ph[k].load(a.dh, row, c, a.m, a.n);
-            if (has_block) pb[k].load(a.block, row, c, a.m, a.n);
-            if (a.dy.p) pd[k].load(a.dy, row, c, a.m, a.n);
-        }
-    };
-    if (r0 < r1) fetch(r0);
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 0; i < a.stages && r0 + i < r1; ++i) pipe.fetch(a, r0 + i, i);
+    int s = 0;
+    int64_t group = r0 / a.gate_every, group_end = (group + 1) * a.gate_every;
     for (int64_t row = r0; row < r1; ++row) {
-        float y[C][kPiece], d[C][kPiece], b[C][kPiece], t[C][kPiece];  // y, b: centred; d: dh
-#pragma unroll
-        for (int k = 0; k < C; ++k) {
-            py[k].template values<F16>(y[k]);
-            ph[k].template values<F16>(d[k]);
-            pb[k].template values<F16>(b[k]);
-            pd[k].template values<F16>(t[k]);
-        }
-        if (C == 1 && row + 1 < r1) fetch(row + 1);
-        float mean_y = 0.f, mean_b = 0.f;
-        if (pre_mean || post_mean) {
-            float s[2] = {};
-#pragma unroll
-            for (int k = 0; k < C; ++k)
-#pragma unroll
-                for (int i = 0; i < kPiece; ++i) s[0] += y[k][i], s[1] += b[k][i];
-            block_sum(s, buffer, turn, warps);
-            if (pre_mean) mean_y = s[0] * a.inverse_n;
-            if (post_mean) mean_b = s[1] * a.inverse_n;
-        }
-        float s[4] = {};  // squares of y and b, q, q y
+        pipe.wait(a, row, s);
+        Eight y[C], d[C], b[C], t[C];  // y, b: centred; d: dh, then q; t: of dy on
 #pragma unroll
         for (int k = 0; k < C; ++k) {
             const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-            float w[kPiece];
-            if (c < a.n) {
-                param8<F16>(a.pre.weight, c, a.n, 1.f, w);
-            } else {
+            uint32_t w[4];
+            pipe.piece(a, row, s, kInY, c, w);
+            y[k] = values8<F16>(w);
+            pipe.piece(a, row, s, kInDh, c, w);
+            d[k] = values8<F16>(w);
+            pipe.piece(a, row, s, kInBlock, c, w);
+            b[k] = values8<F16>(w);
+            pipe.piece(a, row, s, kInDy, c, w);
+            t[k] = values8<F16>(w);
+        }
+        if (pre_mean || post_mean) {
+            float v[2] = {};
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) w[i] = 0.f;
+            for (int k = 0; k < C; ++k) {
+                v[0] += sum_of(y[k]);
+                v[1] += sum_of(b[k]);
             }
+            block_sum(v, reduction);
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) {
-                y[k][i] = c + i < a.n ? y[k][i] - mean_y : 0.f;
-                b[k][i] = c + i < a.n ? b[k][i] - mean_b : 0.f;
-                const float q = d[k][i] * w[i];
-                s[0] = fmaf(y[k][i], y[k][i], s[0]);
-                s[1] = fmaf(b[k][i], b[k][i], s[1]);
-                s[2] += q;
-                s[3] = fmaf(q, y[k][i], s[3]);
+            for (int k = 0; k < C; ++k) {
+                const int c = (k * blockDim.x + threadIdx.x) * kPiece;
+                if (pre_mean) centre(y[k], v[0] * a.inverse_n, c, a.n);
+                if (post_mean) centre(b[k], v[1] * a.inverse_n, c, a.n);
             }
         }
-        block_sum(s, buffer, turn, warps);
-        const float ry = pre ? rsqrtf(fmaf(s[0], a.inverse_n, a.pre.eps)) : 0.f;
-        const float rb = a.post.kind != EMTK_NORM_NONE ? rsqrtf(fmaf(s[1], a.inverse_n, a.post.eps)) : 1.f;
-        const float q_mean = pre_mean ? s[2] * a.inverse_n : 0.f, qy = s[3] * a.inverse_n * ry * ry;
-        const Param gate{a.gate.p ? a.gate.row(row / a.gate_every) : nullptr, 0};
+        if (a.partial[kSumPreB]) {
+#pragma unroll
+            for (int k = 0; k < C; ++k) sums.add(a.at[kSumPreB], k, d[k]);
+        }
+        float ry = 0.f, rb = 1.f;
+        if (pre || post) {
+            float v[4] = {};  // squares of y and b, q, q y
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                const int c = (k * blockDim.x + threadIdx.x) * kPiece;
+                v[0] += dot(y[k], y[k]);
+                v[1] += dot(b[k], b[k]);
+                Eight q = d[k];
+                if (a.pre.weight.p && c < a.n) {
+                    const Eight w = param8<F16>(a.pre.weight, c, a.n);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) q.v[i] = q.v[i] * w.v[i];
+                }
+                v[2] += sum_of(q);
+                v[3] += dot(q, y[k]);
+            }
+            block_sum(v, reduction);
+            if (pre) ry = rsqrtf(fmaf(v[0], a.inverse_n, a.pre.eps));
+            if (post) rb = rsqrtf(fmaf(v[1], a.inverse_n, a.post.eps));
+            if (pre) {
+                const float q_mean = pre_mean ? v[2] * a.inverse_n : 0.f, qy = v[3] * a.inverse_n * ry * ry;
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    const int c = (k * blockDim.x + threadIdx.x) * kPiece;
+                    if (a.partial[kSumPreW]) {
+                        Eight x;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x.v[i] = d[k].v[i] * (y[k].v[i] * both(ry));
+                        sums.add(a.at[kSumPreW], k, x);
+                    }
+                    if (a.pre.weight.p && c < a.n) {
+                        const Eight w = param8<F16>(a.pre.weight, c, a.n);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) d[k].v[i] = d[k].v[i] * w.v[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        t[k].v[i] = fma2(d[k].v[i] - fma2(y[k].v[i], both(qy), both(q_mean)), both(ry), t[k].v[i]);
+                }
+            }
+        }
+        // every thread has taken the row from its stage: the sums' barrier, or where there was none, one more
+        if (!(reduction.warps > 1 && (pre || post))) __syncthreads();
+        if (threadIdx.x == 0 && row + a.stages < r1) pipe.fetch(a, row + a.stages, s);
+        if (++s == a.stages) s = 0;
+        if (row >= group_end) {
+            ++group;
+            group_end += a.gate_every;
+        }
         float u[2] = {};  // the sums for the block's norm
 #pragma unroll
         for (int k = 0; k < C; ++k) {
             const int first = k * blockDim.x + threadIdx.x, c = first * kPiece;
-            const bool in = c < a.n;
-            float w[kPiece], x[kPiece];
-            if (pre && in) {
-                param8<F16>(a.pre.weight, c, a.n, 1.f, w);
-#pragma unroll
-                for (int i = 0; i < kPiece; ++i) {
-                    t[k][i] = fmaf(ry, d[k][i] * w[i] - q_mean - y[k][i] * qy, t[k][i]);
-                    x[i] = d[k][i] * y[k][i] * ry;
-                }
-                if (a.partial[kSumPreW]) sums.add(a.at[kSumPreW], k, x);
-                if (a.partial[kSumPreB]) sums.add(a.at[kSumPreB], k, d[k]);
-            }
             if (a.d_residual.p) {
-                uint32_t q[4];
+                Eight x;
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) x[i] = t[k][i] * a.scale;
-                words8<F16>(x, q);
-                const int run = c - kPiece * lane;
-                store_run<ANY>(a.d_residual.row(row) + run, max(0, min(a.n - run, 32 * kPiece)), q, 32, lane);
+                for (int i = 0; i < 4; ++i) x.v[i] = t[k].v[i] * both(a.scale);
+                store_piece<F16, true>(a.d_residual, row, a.n, x, k);
             }
-            if (!has_block || !in) continue;
+            if (!has_block) continue;
             if (a.drop.below) dropped(a.drop, offset, (uint32_t)row, (uint32_t)first, t[k]);
-            float g[kPiece];
-            param8<F16>(a.post.weight, c, a.n, 1.f, w);
+            if (c + kPiece > a.n) centre(t[k], 0.f, c, a.n);
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) b[k][i] *= rb;  // now normalised
-            if (a.partial[kSumGate] || a.gate_out) {
-                param8<F16>(a.post.bias, c, a.n, 0.f, g);
+            for (int i = 0; i < 4; ++i) b[k].v[i] = b[k].v[i] * both(rb);  // now normalised
+            Eight w;
+            w.fill(1.f);
+            if (a.post.weight.p && c < a.n) w = param8<F16>(a.post.weight, c, a.n);
+            if (gate_sum) {
+                Eight x;
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) x[i] = t[k][i] * fmaf(b[k][i], w[i], g[i]);
+                for (int i = 0; i < 4; ++i) x.v[i] = b[k].v[i] * w.v[i];
+                if (a.post.bias.p && c < a.n) {
+                    const Eight bias = param8<F16>(a.post.bias, c, a.n);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x.v[i] = x.v[i] + bias.v[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x.v[i] = x.v[i] * t[k].v[i];
                 sums.add(a.at[kSumGate], k, x);
             }
-            param8<F16>(gate, c, a.n, 1.f, g);
+            if (a.gate.p && c < a.n) {
+                const Eight g = param8<F16>({a.gate.row(group), 0}, c, a.n);
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) t[k][i] *= g[i];
+                for (int i = 0; i < 4; ++i) t[k].v[i] = t[k].v[i] * g.v[i];
+            }
             if (a.partial[kSumPostW]) {
+                Eight x;
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) x[i] = t[k][i] * b[k][i];
+                for (int i = 0; i < 4; ++i) x.v[i] = t[k].v[i] * b[k].v[i];
                 sums.add(a.at[kSumPostW], k, x);
             }
             if (a.partial[kSumPostB]) sums.add(a.at[kSumPostB], k, t[k]);
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) {
-                t[k][i] *= w[i];
-                u[0] += c + i < a.n ? t[k][i] : 0.f;
-                u[1] = fmaf(c + i < a.n ? t[k][i] : 0.f, b[k][i], u[1]);
-            }
+            for (int i = 0; i < 4; ++i) t[k].v[i] = t[k].v[i] * w.v[i];
+            u[0] += sum_of(t[k]);
+            u[1] += dot(t[k], b[k]);
         }
         if (a.d_block.p) {
-            if (a.post.kind != EMTK_NORM_NONE) block_sum(u, buffer, turn, warps);
-            const float t_mean = post_mean ? u[0] * a.inverse_n : 0.f;
-            const float tb = a.post.kind != EMTK_NORM_NONE ? u[1] * a.inverse_n : 0.f;
+            float mean = 0.f, along = 0.f;
+            if (post) {
+                block_sum(u, reduction);
+                mean = post_mean ? u[0] * a.inverse_n : 0.f;
+                along = u[1] * a.inverse_n;
+            }
 #pragma unroll
             for (int k = 0; k < C; ++k) {
-                float x[kPiece];
-                uint32_t q[4];
 #pragma unroll
-                for (int i = 0; i < kPiece; ++i) x[i] = rb * (t[k][i] - t_mean - b[k][i] * tb);
-                words8<F16>(x, q);
-                const int run = (k * blockDim.x + (threadIdx.x & ~31)) * kPiece;
-                store_run<ANY>(a.d_block.row(row) + run, max(0, min(a.n - run, 32 * kPiece)), q, 32, lane);
+                for (int i = 0; i < 4; ++i) t[k].v[i] = (t[k].v[i] - fma2(b[k].v[i], both(along), both(mean))) * both(rb);
+                store_piece<F16, true>(a.d_block, row, a.n, t[k], k);
             }
         }
-        if (a.gate_out && ((row + 1) % a.gate_every == 0 || row + 1 == r1)) {
+        if (a.gate_out && (row + 1 == group_end || row + 1 == r1)) {
 #pragma unroll
             for (int k = 0; k < C; ++k)
-                sums.flush(a.at[kSumGate], k, a.gate_out + row / a.gate_every * a.gate_ld, (k * blockDim.x + threadIdx.x) * kPiece, a.n);
+                sums.flush(a.at[kSumGate], k, a.gate_out + group * a.gate_ld, (k * blockDim.x + threadIdx.x) * kPiece, a.n);
         }
-        if (C > 1 && row + 1 < r1) fetch(row + 1);
     }
 #pragma unroll
     for (int k = 0; k < C; ++k)
         for (int i = 0; i < kSums; ++i)
             if (a.partial[i])
                 sums.flush(a.at[i], k, a.partial[i] + (int64_t)slice * a.n, (k * blockDim.x + threadIdx.x) * kPiece, a.n);
+    if (!pipe.ok) {  // copies in flight land within microseconds: leave them a millisecond
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 1000000u) {
+        }
+    }
 }
 
 // Adds slices' sums: a block takes 32 columns of one result, each of its warps every
@@ -440,32 +589,38 @@ cudaError_t run(const SeamArgs &a, cudaStream_t s) {
     return launch_pdl(kernel, dim3((unsigned)a.m), dim3((unsigned)h.threads), 0, s, a);
 }
 
-constexpr int kMostShared = 220 * 1024;  // of running sums in shared memory
+constexpr int kMostShared = 222 * 1024;  // of a block, beside what it has fixed
 
 struct GradPlan {
     Shape shape;
     Slices slices;
-    size_t columns;   // bytes of a slice's running sums
-    size_t shared;    // of them in shared memory, else 0
-    int sums;
+    size_t columns;  // bytes of a slice's running sums
+    size_t shared;   // of a block: rows, and the sums if there is room
+    bool spilled;
+    int sums, stages, row_bytes;
 };
 GradPlan grad_plan(int m, int n, int gate_every, int sums, int sms) {
     GradPlan p;
     p.shape = shape_of(n, 1024);
     p.sums = sums;
     p.columns = (size_t)sums * p.shape.pieces * p.shape.threads * kPiece * 4;
-    p.shared = p.columns <= kMostShared ? p.columns : 0;
+    // a row as it lies: up to 14 bytes before it, whole pieces, and the one after the last
+    p.row_bytes = (2 * n + 14 + 15) / 16 * 16 + 16;
+    const size_t stage = (size_t)kInputs * p.row_bytes;
+    p.spilled = stage + p.columns > kMostShared;
+    const size_t sums_bytes = p.spilled ? 0 : p.columns;
+    p.stages = 2 * stage + sums_bytes <= kMostShared ? 2 : 1;
+    p.shared = p.stages * stage + sums_bytes;
     const int warps = p.shape.threads / 32;
-    int each = std::max(1, 32 / warps);  // blocks of an SM
-    if (p.shared) each = std::max(1, std::min(each, (int)(kMostShared / p.shared)));
+    const int each = std::max(1, std::min(32 / warps, (int)(kMostShared / (p.shared + 2048))));  // blocks of an SM
     // two rows at least to a slice, and no more slices than are resident at once
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>((int64_t)sms * each, ((int64_t)m + 1) / 2));
     const int64_t groups = std::max<int64_t>(1, ((int64_t)m + gate_every - 1) / gate_every);
     Slices &l = p.slices;
     if (groups < want) {
-        const int64_t parts = want / groups;
-        l.rows = (int)((std::min<int64_t>(gate_every, std::max(1, m)) + parts - 1) / parts);
-        l.parts = (int)((std::min<int64_t>(gate_every, std::max(1, m)) + l.rows - 1) / l.rows);
+        const int64_t parts = want / groups, rows = std::min<int64_t>(gate_every, std::max(1, m));
+        l.rows = (int)((rows + parts - 1) / parts);
+        l.parts = (int)((rows + l.rows - 1) / l.rows);
         l.groups_each = 1;
         l.count = (int)(groups * l.parts);
     } else {
@@ -477,38 +632,19 @@ GradPlan grad_plan(int m, int n, int gate_every, int sums, int sms) {
     return p;
 }
 
-template <bool F16, bool ANY, int C, int THREADS>
-cudaError_t run_grad(const SeamGradArgs &a, const GradPlan &p, cudaStream_t s) {
-    return launch_pdl(residual_norm_grad_kernel<F16, ANY, C, THREADS>, dim3((unsigned)p.slices.count),
-                      dim3((unsigned)p.shape.threads), p.shared, s, a);
-}
-template <bool F16, bool ANY>
-cudaError_t run_grad(const SeamGradArgs &a, const GradPlan &p, cudaStream_t s) {
-    if (p.shape.pieces == 2) return run_grad<F16, ANY, 2, 1024>(a, p, s);
-    return p.shape.threads <= 256   ? run_grad<F16, ANY, 1, 256>(a, p, s)
-           : p.shape.threads <= 512 ? run_grad<F16, ANY, 1, 512>(a, p, s)
-                                    : run_grad<F16, ANY, 1, 1024>(a, p, s);
+template <bool F16>
+cudaError_t run_grad(const SeamGradArgs &a, const GradPlan &p, const emtk_nn *nn, cudaStream_t s) {
+    return launch_pdl(p.shape.pieces == 1 ? residual_norm_grad_kernel<F16, 1> : residual_norm_grad_kernel<F16, 2>,
+                      dim3((unsigned)p.slices.count), dim3((unsigned)p.shape.threads), p.shared, s, a, nn->status, nn->timeout_ns);
 }
 
 }  // namespace
 
 cudaError_t init_norm_kernels() {
     cudaError_t e = cudaSuccess;
-#define EMTK_NORM_ATTR(F16, ANY, C, THREADS)                                             \
-    if (e == cudaSuccess)                                                                \
-        e = cudaFuncSetAttribute(residual_norm_grad_kernel<F16, ANY, C, THREADS>,        \
-                                 cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
-#define EMTK_NORM_ATTRS(F16, ANY)      \
-    EMTK_NORM_ATTR(F16, ANY, 1, 256)   \
-    EMTK_NORM_ATTR(F16, ANY, 1, 512)   \
-    EMTK_NORM_ATTR(F16, ANY, 1, 1024)  \
-    EMTK_NORM_ATTR(F16, ANY, 2, 1024)
-    EMTK_NORM_ATTRS(false, false)
-    EMTK_NORM_ATTRS(false, true)
-    EMTK_NORM_ATTRS(true, false)
-    EMTK_NORM_ATTRS(true, true)
-#undef EMTK_NORM_ATTRS
-#undef EMTK_NORM_ATTR
+    for (void (*kernel)(const SeamGradArgs, int *, int64_t) : {residual_norm_grad_kernel<false, 1>, residual_norm_grad_kernel<false, 2>,
+                                                               residual_norm_grad_kernel<true, 1>, residual_norm_grad_kernel<true, 2>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     return e;
 }
 
@@ -538,17 +674,16 @@ static int norm_sums(const emtk_residual_norm_grad_args &p) {
 }
 size_t residual_norm_workspace(const emtk_residual_norm_grad_args &p, int sms) {
     const GradPlan g = grad_plan(p.m, p.n, p.gate_every, norm_sums(p), sms);
-    const size_t spill = g.shared == g.columns ? 0 : g.columns * g.slices.count;
-    return spill + (size_t)g.sums * g.slices.count * p.n * 4;
+    return (g.spilled ? g.columns * g.slices.count : 0) + (size_t)g.sums * g.slices.count * p.n * 4;
 }
 
-cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, int sms, cudaStream_t s) {
-    const GradPlan g = grad_plan(p.m, p.n, p.gate_every, norm_sums(p), sms);
+cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s) {
+    const GradPlan g = grad_plan(p.m, p.n, p.gate_every, norm_sums(p), nn->sm_count);
     SeamGradArgs a{};
-    a.dy = rows16_of(p.dy);
-    a.dh = rows16_of(p.dh);
-    a.y = rows16_of(p.y);
-    a.block = rows16_of(p.block);
+    a.in[kInY] = rows16_of(p.y);
+    a.in[kInDh] = rows16_of(p.dh);
+    a.in[kInBlock] = rows16_of(p.block);
+    a.in[kInDy] = rows16_of(p.dy);
     a.gate = rows16_of(p.gate);
     a.d_residual = rows16_of(p.d_residual);
     a.d_block = rows16_of(p.d_block);
@@ -563,7 +698,9 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
     a.slices = g.slices;
     a.sums = g.sums;
     float *at = static_cast<float *>(workspace);
-    if (g.shared != g.columns) {
+    a.stages = g.stages;
+    a.row_bytes = g.row_bytes;
+    if (g.spilled) {
         a.spill = at;
         at += g.columns / 4 * g.slices.count;
     }
@@ -592,13 +729,7 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
     j.slices = g.slices.count;
     j.parts = g.slices.parts;
     j.n = p.n;
-    const bool any = !(on_grid(p.dy, p.m) && on_grid(p.dh, p.m) && on_grid(p.y, p.m) && on_grid(p.block, p.m) &&
-                       on_grid(p.d_residual, p.m) && on_grid(p.d_block, p.m));
-    cudaError_t e;
-    if (p.type == EMTK_TYPE_F16)
-        e = any ? run_grad<true, true>(a, g, s) : run_grad<true, false>(a, g, s);
-    else
-        e = any ? run_grad<false, true>(a, g, s) : run_grad<false, false>(a, g, s);
+    cudaError_t e = p.type == EMTK_TYPE_F16 ? run_grad<true>(a, g, nn, s) : run_grad<false>(a, g, nn, s);
     const int gates = j.gate_to ? std::max(1, g.slices.count / g.slices.parts) : 0;
     if (e == cudaSuccess && j.results + gates > 0)
         e = launch_pdl(residual_norm_join_kernel, dim3((unsigned)((p.n + 31) / 32), (unsigned)(j.results + gates)),

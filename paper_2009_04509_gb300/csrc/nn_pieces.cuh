@@ -6,7 +6,7 @@
 // which hold neighbours' bytes too; those are dropped, whatever their state.
 #pragma once
 
-#include "nn_math.cuh"
+#include "nn_pair.cuh"
 
 namespace emtk {
 namespace {
@@ -24,18 +24,24 @@ inline bool on_grid(const emtk_matrix &m, int64_t rows, size_t elem = 2) {
     return !m.d || (reinterpret_cast<uintptr_t>(m.d) % 16 == 0 && (rows <= 1 || m.ld * elem % 16 == 0));
 }
 
-template <bool F16>
-__device__ __forceinline__ void values8(const uint32_t *w, float (&v)[kPiece]) {
+struct Eight {  // a piece's values
+    float2 v[4];
+    __device__ __forceinline__ void fill(float x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = F16 ? from16<F16>(w[i] & 0xffffu) : __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = F16 ? from16<F16>(w[i] >> 16) : __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < 4; ++i) v[i] = both(x);
     }
+};
+template <bool F16>
+__device__ __forceinline__ Eight values8(const uint32_t *w) {
+    Eight e;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.v[i] = values_of<F16>(w[i]);
+    return e;
 }
 template <bool F16>
-__device__ __forceinline__ void words8(const float (&v)[kPiece], uint32_t (&w)[4]) {
+__device__ __forceinline__ void words8(const Eight &e, uint32_t (&w)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack16<F16>(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) w[i] = pack16<F16>(e.v[i].x, e.v[i].y);
 }
 
 // Four words out of eight, from half word `halves` on; one case to a row.
@@ -87,14 +93,13 @@ struct Piece16 {
         for (int i = 0; i < 4; ++i) x[i] = 0u;
     }
     template <bool F16>
-    __device__ __forceinline__ void values(float (&v)[kPiece]) const {
+    __device__ __forceinline__ Eight values() const {
         if (ANY && halves) {
             uint32_t y[4];
             shift_words(x, halves, y);
-            values8<F16>(y, v);
-        } else {
-            values8<F16>(x, v);
+            return values8<F16>(y);
         }
+        return values8<F16>(x);
     }
 };
 
@@ -151,31 +156,34 @@ struct Param {
     const void *p;
     int f32;
 };
+// Columns c .. of one that is there; those from n on are 0.
 template <bool F16>
-__device__ __forceinline__ void param8(const Param &a, int c, int n, float fill, float (&v)[kPiece]) {
-    if (a.p == nullptr) {
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) v[i] = fill;
-    } else if (a.f32) {
+__device__ __forceinline__ Eight param8(const Param &a, int c, int n) {
+    Eight e;
+    if (a.f32) {
         const float *const p = static_cast<const float *>(a.p) + c;
         if (c + kPiece <= n && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
             const float4 lo = __ldg(reinterpret_cast<const float4 *>(p)), hi = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-            v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+            e.v[0] = make_float2(lo.x, lo.y), e.v[1] = make_float2(lo.z, lo.w);
+            e.v[2] = make_float2(hi.x, hi.y), e.v[3] = make_float2(hi.z, hi.w);
         } else {
 #pragma unroll
-            for (int i = 0; i < kPiece; ++i) v[i] = c + i < n ? __ldg(p + i) : fill;
+            for (int i = 0; i < 4; ++i)
+                e.v[i] = make_float2(c + 2 * i < n ? __ldg(p + 2 * i) : 0.f, c + 2 * i + 1 < n ? __ldg(p + 2 * i + 1) : 0.f);
         }
-    } else {
-        const uint16_t *const p = static_cast<const uint16_t *>(a.p) + c;
-        if (c + kPiece <= n && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(p));
-            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-            values8<F16>(x, v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i) v[i] = c + i < n ? from16<F16>(__ldg(p + i)) : fill;
-        }
+        return e;
     }
+    const uint16_t *const p = static_cast<const uint16_t *>(a.p) + c;
+    uint32_t w[4] = {};
+    if (c + kPiece <= n && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4 *>(p));
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i)
+            if (c + i < n) w[i / 2] |= (uint32_t)__ldg(p + i) << (16 * (i % 2));
+    }
+    return values8<F16>(w);
 }
 
 // ---- dropout
@@ -200,7 +208,7 @@ inline Drop drop_of(const emtk_drop &d) {
 __device__ __forceinline__ uint64_t drop_offset(const Drop &d) { return d.offset + (d.d_offset ? *d.d_offset : 0u); }
 
 // The piece's elements under dropout: row r, columns 8 g ..
-__device__ __forceinline__ void dropped(const Drop &d, uint64_t offset, uint32_t r, uint32_t g, float (&v)[kPiece]) {
+__device__ __forceinline__ void dropped(const Drop &d, uint64_t offset, uint32_t r, uint32_t g, Eight &e) {
     uint32_t x[4] = {g, r, (uint32_t)offset, (uint32_t)(offset >> 32)};
     uint32_t k0 = (uint32_t)d.seed, k1 = (uint32_t)(d.seed >> 32);
 #pragma unroll
@@ -216,8 +224,8 @@ __device__ __forceinline__ void dropped(const Drop &d, uint64_t offset, uint32_t
     const uint32_t high = d.below << 16;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        v[2 * i] = (x[i] << 16) >= high ? v[2 * i] * d.factor : 0.f;
-        v[2 * i + 1] = x[i] >= high ? v[2 * i + 1] * d.factor : 0.f;
+        const float2 v = e.v[i] * both(d.factor);
+        e.v[i] = make_float2((x[i] << 16) >= high ? v.x : 0.f, x[i] >= high ? v.y : 0.f);
     }
 }
 

@@ -31,13 +31,12 @@
 
 #include "emtk_internal.h"
 #include "nn_internal.h"
-#include "nn_math.cuh"
+#include "nn_pair.cuh"
 #include "nn_ptx.cuh"
 
 namespace emtk {
 namespace {
 
-constexpr float kLog2E = 1.4426950408889634f;
 constexpr int kLanes = 16, kCols = 2 * kLanes;  // two columns a lane
 constexpr int kRuns = 8, kLen = 16, kTile = kRuns * kLen, kThreads = kLanes * kRuns;
 constexpr int kShort = 8;  // steps up to which a thread takes a whole sequence
@@ -108,45 +107,6 @@ struct RecurGradArgs {
     int col_tiles, words;
 };
 
-// ---- two columns at a time: one instruction for the two products or sums
-__device__ __forceinline__ uint64_t bits_of(float2 v) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
-    return r;
-}
-__device__ __forceinline__ float2 pair_of(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ float2 operator+(float2 a, float2 b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)));
-    return pair_of(r);
-}
-__device__ __forceinline__ float2 operator*(float2 a, float2 b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)));
-    return pair_of(r);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits_of(a)), "l"(bits_of(b)), "l"(bits_of(c)));
-    return pair_of(r);
-}
-__device__ __forceinline__ float exp2_f(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-__device__ __forceinline__ float2 operator-(float2 a, float2 b) { return fma2(b, both(-1.f), a); }
-__device__ __forceinline__ float2 operator-(float2 a) { return make_float2(-a.x, -a.y); }
-
-template <bool F16>
-__device__ __forceinline__ float2 values_of(uint32_t w) {
-    return make_float2(from16<F16>(F16 ? w & 0xffffu : w), F16 ? from16<F16>(w >> 16) : __uint_as_float(w & 0xffff0000u));
-}
 template <int ACT>
 __device__ __forceinline__ float2 act2(float2 z) {
     return make_float2(act_of<ACT>(z.x), act_of<ACT>(z.y));
