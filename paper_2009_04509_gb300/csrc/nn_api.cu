@@ -594,7 +594,7 @@ emtk_status emtk_residual_norm(emtk_nn *nn, const emtk_residual_norm_args *p, em
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk residual norm");
-    return status_of(launch_residual_norm(a, reinterpret_cast<cudaStream_t>(stream)));
+    return status_of(launch_residual_norm(a, nn, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residual_norm_grad_args *p, emtk_stream stream) {

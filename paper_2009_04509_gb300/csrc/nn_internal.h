@@ -171,7 +171,7 @@ cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, 
 cudaError_t launch_dropout(emtk_type type, int m, int n, const emtk_matrix &x, const emtk_matrix &y, const emtk_drop &drop,
                            int sms, cudaStream_t s);  // nn_dropout.cu
 cudaError_t init_norm_kernels();  // once per device
-cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, cudaStream_t s);  // nn_norm.cu
+cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, const emtk_nn *nn, cudaStream_t s);  // nn_norm.cu
 size_t residual_norm_workspace(const emtk_residual_norm_grad_args &p, int sms);
 cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s);
 cudaError_t launch_logprobs(const emtk_logprobs_args &p, int sms, cudaStream_t s);  // nn_logprob.cu

@@ -3,16 +3,18 @@
 //   v = D post(b);  y = s r + g v;  h = pre(y)
 //   post(b) = (b - mean) / sqrt(mean((b - mean)^2) + eps) w + c   (mean 0 for RMS)
 //
-// A row is held in the registers of one block of threads, eight neighbouring columns to a
+// A row is held in the registers of a group of threads, eight neighbouring columns to a
 // piece, so each matrix is read once and every output written once; variances are of the
-// centred values.  HBM bounds the forward pass (8 bytes a value in 16 bits) and the
-// backward pass (12), the call a single row.
+// centred values.  HBM bounds the forward pass (8 bytes a value in 16 bits), the call a
+// single row.
 //
 // Gradients.  With x^ = (x - mean) / std and q = w d of an output's gradient d, a norm's
-// input has the gradient (q - mean(q) - x^ mean(q x^)) / std (mean(q) not for RMS).  A block
-// of threads takes a slice of the rows, one after another, which bulk copies bring to shared
-// memory ahead, and adds the columns' sums (the parameters' and the gate's gradients) in shared
-// memory too, where each column is one thread's; a second kernel adds the slices in order, so results do not depend on timing.
+// input has the gradient (q - mean(q) - x^ mean(q x^)) / std (mean(q) not for RMS).  One kernel
+// goes along rows and writes the inputs' gradients (12 bytes a value) and a few numbers of each
+// row, from which another, along columns, adds the parameters' and the gate's (up to 8 bytes a
+// value again; in one kernel, each thread adding its columns row by row, the four barriers
+// of a row and its sums in shared memory took three times as long).  Sums of slices of
+// rows are joined in order, so results do not depend on timing.
 #include <algorithm>
 
 #include "emtk_internal.h"
@@ -23,7 +25,7 @@
 namespace emtk {
 namespace {
 
-constexpr int kMaxWarps = 32;
+constexpr int kMaxWarps = 32, kMostGroups = 8, kGroupThreads = 128;
 
 struct NormArgs {
     int kind;
@@ -35,26 +37,27 @@ NormArgs norm_args(const emtk_norm &n) {
     return {n.kind, n.eps, {n.weight, f32}, {n.bias, f32}};
 }
 
-struct SeamArgs {
-    Rows16 residual, block, gate, y, h;
-    NormArgs post, pre;
-    Drop drop;
-    float scale, inverse_n;
-    int m, n, gate_every;
-};
-
-// The sums of K (1, 2 or 4) values over the block's threads, in every thread.  In a warp
+// The sums of K (1, 2 or 4) values over a group's threads, in every thread.  In a warp
 // each exchange halves the values that a lane still holds, and then the lanes; the warps'
 // sums are read back with one value to a lane and added the same way: a sum costs a third
 // of the shuffles that one tree for each value would.  `turn` alternates between two
 // buffers, so that one barrier a call is enough.
+// A group: the threads of a row, blockDim.x of them, blockDim.y groups to a block (one,
+// where a row has more than kGroupThreads).
 struct Reduction {
-    float (*buffer)[4 * kMaxWarps];  // [2]
-    int warps, turn;
+    float *buffer;  // [2][4 * kMaxWarps] of the block, from the group's place on
+    int tid, warps, turn;
+    bool grouped;
+    __device__ __forceinline__ void sync() const {
+        if (grouped)
+            asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.y + 1), "r"(32 * warps) : "memory");
+        else
+            __syncthreads();
+    }
 };
 template <int K>
-__device__ __forceinline__ void block_sum(float (&v)[K], Reduction &b) {
-    const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void row_sum(float (&v)[K], Reduction &b) {
+    const int lane = b.tid & 31;
     float x = v[0];
     if constexpr (K == 4) {  // lane & 3 keeps its value
         const bool upper = (lane & 2) != 0;
@@ -70,9 +73,9 @@ __device__ __forceinline__ void block_sum(float (&v)[K], Reduction &b) {
 #pragma unroll
     for (int d = K; d < 32; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
     if (b.warps > 1) {
-        float *const buffer = b.buffer[b.turn];
-        if (lane < K) buffer[threadIdx.x / 32 * K + lane] = x;
-        __syncthreads();
+        float *const buffer = b.buffer + b.turn * 4 * kMaxWarps;
+        if (lane < K) buffer[b.tid / 32 * K + lane] = x;
+        b.sync();
         x = 0.f;
         for (int i = lane; i < b.warps * K; i += 32) x += buffer[i];
 #pragma unroll
@@ -102,290 +105,352 @@ __device__ __forceinline__ void centre(Eight &e, float mean, int c, int n) {
         for (int i = 0; i < 4; ++i) e.v[i] = make_float2(c + 2 * i < n ? e.v[i].x : 0.f, c + 2 * i + 1 < n ? e.v[i].y : 0.f);
     }
 }
+__device__ __forceinline__ Eight operator*(const Eight &a, const Eight &b) {
+    Eight r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = a.v[i] * b.v[i];
+    return r;
+}
+__device__ __forceinline__ Eight operator*(const Eight &a, float b) {
+    Eight r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = a.v[i] * both(b);
+    return r;
+}
+__device__ __forceinline__ Eight operator+(const Eight &a, const Eight &b) {
+    Eight r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = a.v[i] + b.v[i];
+    return r;
+}
+
+constexpr int kMostInputs = 4, kMostStages = 2;
+struct Inputs {
+    Rows16 in[kMostInputs];
+    int m, n;
+    int row_bytes, stages;  // of kBulk: room for one row in shared memory, rows on their way
+};
+// Room for a row: up to 14 bytes before it, whole pieces, and the one after the last.
+int bulk_row_bytes(int n) { return (2 * n + 14 + 15) / 16 * 16 + 16; }
+
+struct Waits {  // of the kernels' bounded waits
+    int *status;
+    int64_t timeout_ns;
+};
+
+// How a group of threads has its row.
+//   kDirect   one of a block's, two pieces a thread, on the 16-byte grid and of whole pieces
+//   kSmall    several to a block, a piece a thread, likewise
+//   kSmallAny several to a block, a piece a thread, anywhere
+//   kBulk     a block goes from row to row, two pieces a thread, anywhere: a row of each matrix is
+//             copied to shared memory, a row or two ahead, in the aligned 16-byte pieces
+//             that it lies in, and shifted into place from there: many rows are on their
+//             way without a register.  Rows whose outer pieces would reach beyond the
+//             matrix are copied by elements.
+// A thread's pieces are tid and tid + threads; but for the last of a thread, they are whole.
+enum Kind : int { kDirect, kSmall, kSmallAny, kBulk };
+
+template <bool F16, Kind KIND, int COUNT>  // COUNT: matrices
+struct RowIo {
+    static constexpr int C = KIND == kDirect || KIND == kBulk ? 2 : 1;
+    static constexpr bool ODD = KIND == kSmallAny || KIND == kBulk;
+    const Inputs &a;
+    int64_t row;
+    int tid, threads;
+    bool last;  // the last piece is this thread's, or beyond the row
+    // kBulk
+    uint8_t *stages;
+    uint64_t *full;
+    Guard guard;
+    uint32_t phases = 0;
+    int stage = 0;
+    bool ok = true;
+
+    __device__ __forceinline__ RowIo(const Inputs &inputs, uint8_t *shared, uint64_t *bars, uint32_t *abort_flag, const Waits &w)
+        : a(inputs), stages(shared), full(bars), guard{abort_flag, w.status, w.timeout_ns} {
+        tid = threadIdx.x;
+        threads = blockDim.x;
+        row = KIND == kSmall || KIND == kSmallAny ? (int64_t)blockIdx.x * blockDim.y + threadIdx.y : (int64_t)blockIdx.x;
+        last = column(C - 1) + kPiece > a.n;
+        if (KIND == kBulk) {
+            if (tid == 0) {
+                for (int i = 0; i < kMostStages; ++i) mbar_init(smem_u32(full + i), 1);
+                *abort_flag = 0;
+                fence_mbar_init();
+            }
+            __syncthreads();
+        }
+    }
+    __device__ __forceinline__ int column(int k) const { return (k * threads + tid) * kPiece; }
+
+    // ---- kBulk: rows on their way
+    __device__ __forceinline__ int head(int i, int64_t r) const { return (int)(reinterpret_cast<uintptr_t>(a.in[i].row(r)) % 16); }
+    __device__ __forceinline__ int bytes(int i, int64_t r) const { return (head(i, r) + 2 * a.n + 15) / 16 * 16; }
+    __device__ __forceinline__ uint8_t *place(int s, int i) const { return stages + (s * COUNT + i) * a.row_bytes; }
+    __device__ __forceinline__ bool by_elements(int64_t r) const {
+        if (r >= kPiece && r < a.m - kPiece) return false;  // the 14 bytes around are of rows between
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            if (!a.in[i].p) continue;
+            const int64_t first = r * a.in[i].row_bytes - head(i, r), end = (a.m - 1) * a.in[i].row_bytes + 2 * (int64_t)a.n;
+            if (first < 0 || first + bytes(i, r) > end) return true;
+        }
+        return false;
+    }
+    __device__ __forceinline__ void fetch(int64_t r, int s) const {  // one thread
+        if (r >= a.m || by_elements(r)) return;
+        const uint32_t bar = smem_u32(full + s);
+        uint32_t all = 0;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) all += a.in[i].p ? (uint32_t)bytes(i, r) : 0u;
+        mbar_expect_tx(bar, all);
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+            if (a.in[i].p)
+                bulk_load(smem_u32(place(s, i)), reinterpret_cast<const uint8_t *>(a.in[i].row(r)) - head(i, r), bytes(i, r), bar);
+    }
+    __device__ __forceinline__ void begin() const {
+        if (KIND == kBulk && tid == 0)
+            for (int i = 0; i < a.stages; ++i) fetch(row + (int64_t)i * gridDim.x, i);
+    }
+    // The row's arrival; all threads.
+    __device__ __forceinline__ void wait() {
+        if (KIND != kBulk) return;
+        if (by_elements(row)) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                if (!a.in[i].p) continue;
+                uint16_t *const to = reinterpret_cast<uint16_t *>(place(stage, i) + head(i, row));
+                for (int c = tid; c < a.n; c += threads) to[c] = a.in[i].row(row)[c];
+            }
+            bulk_fence();
+            __syncthreads();
+        } else {
+            if (ok) ok = wait_bounded(smem_u32(full + stage), (phases >> stage) & 1u, guard);
+            phases ^= 1u << stage;
+        }
+    }
+    // Every thread has taken its pieces, and met the others since: the stage may be filled again.
+    __device__ __forceinline__ void release() {
+        if (KIND != kBulk) return;
+        if (tid == 0) fetch(row + (int64_t)a.stages * gridDim.x, stage);
+        if (++stage == a.stages) stage = 0;
+    }
+    __device__ __forceinline__ bool next() {  // to the block's next row
+        if (KIND != kBulk) return false;
+        row += gridDim.x;
+        return row < a.m;
+    }
+    __device__ __forceinline__ void end() const {
+        if (KIND != kBulk || ok) return;
+        const uint64_t t0 = global_timer_ns();  // copies in flight land within microseconds: leave them a millisecond
+        while (global_timer_ns() - t0 < 1000000u) {
+        }
+    }
+
+    // A matrix' pieces, columns from n on 0.
+    __device__ __forceinline__ void load(int which, uint32_t (&w)[C][4]) const {
+#pragma unroll
+        for (int k = 0; k < C; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[k][i] = 0u;
+        if (!a.in[which].p) return;
+        if constexpr (KIND == kBulk) {
+            const uint4 *const base = reinterpret_cast<const uint4 *>(place(stage, which));
+            const int halves = head(which, row) / 2, most = (a.n - 1) / kPiece;
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                const uint4 *const p = base + min(k * threads + tid, most);
+                const uint4 lo = p[0];
+                if (halves) {
+                    const uint4 hi = p[1];
+                    const uint32_t x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                    shift_words(x, halves, w[k]);
+                } else {
+                    w[k][0] = lo.x, w[k][1] = lo.y, w[k][2] = lo.z, w[k][3] = lo.w;
+                }
+            }
+            if (last) {
+                const int left = a.n - column(C - 1);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[C - 1][i] &= (2 * i < left ? 0xffffu : 0u) | (2 * i + 1 < left ? 0xffff0000u : 0u);
+            }
+        } else if constexpr (KIND == kSmallAny) {
+            if (tid * kPiece >= a.n) return;
+            Piece16<true> x;
+            x.load(a.in[which], row, tid * kPiece, a.m, a.n);
+            if (x.halves) {
+                shift_words(x.x, x.halves, w[0]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[0][i] = x.x[i];
+            }
+        } else {
+            const uint4 *const p = reinterpret_cast<const uint4 *>(a.in[which].row(row)) + tid;
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                if (k == C - 1 && last) continue;
+                const uint4 x = p[k * threads];
+                w[k][0] = x.x, w[k][1] = x.y, w[k][2] = x.z, w[k][3] = x.w;
+            }
+        }
+    }
+    // A vector's columns of piece k; 0 from n on.
+    __device__ __forceinline__ Eight param(const Param &p, int k) const {
+        if (KIND == kDirect && k < C - 1) return param8<F16>(p, column(k), 1 << 30);
+        return param8<F16>(p, column(k), a.n);
+    }
+    __device__ __forceinline__ void store(const Rows16 &to, int k, const Eight &e) const {
+        uint32_t w[4];
+        words8<F16>(e, w);
+        if constexpr (ODD) {
+            const int run = (k * threads + (tid & ~31)) * kPiece;
+            store_run<true>(to.row(row) + run, max(0, min(a.n - run, 32 * kPiece)), w, 32, tid & 31);
+        } else if (k < C - 1 || !last) {
+            reinterpret_cast<uint4 *>(to.row(row))[k * threads + tid] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+};
 
 // x becomes norm(x) weight + bias.
-template <bool F16, int C>
-__device__ __forceinline__ void normalise(const NormArgs &a, Eight (&x)[C], int n, float inverse_n, Reduction &b) {
+template <bool F16, typename Io>
+__device__ __forceinline__ void normalise(const NormArgs &a, Eight (&x)[Io::C], const Io &io, float inverse_n, Reduction &b) {
     if (a.kind == EMTK_NORM_LAYER) {
-        float sum[1] = {0.f};
+        float sum[1] = {sum_of(x[0])};
+        if (Io::C > 1) sum[0] += sum_of(x[Io::C - 1]);
+        row_sum(sum, b);
 #pragma unroll
-        for (int k = 0; k < C; ++k) sum[0] += sum_of(x[k]);
-        block_sum(sum, b);
-#pragma unroll
-        for (int k = 0; k < C; ++k) centre(x[k], sum[0] * inverse_n, (k * blockDim.x + threadIdx.x) * kPiece, n);
+        for (int k = 0; k < Io::C; ++k) centre(x[k], sum[0] * inverse_n, k < Io::C - 1 ? 0 : io.column(k), io.a.n);
     }
-    float square[1] = {0.f};
-#pragma unroll
-    for (int k = 0; k < C; ++k) square[0] += dot(x[k], x[k]);
-    block_sum(square, b);
+    float square[1] = {dot(x[0], x[0])};
+    if (Io::C > 1) square[0] += dot(x[Io::C - 1], x[Io::C - 1]);
+    row_sum(square, b);
     const float r = rsqrtf(fmaf(square[0], inverse_n, a.eps));
 #pragma unroll
-    for (int k = 0; k < C; ++k) {
-        const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[k].v[i] = x[k].v[i] * both(r);
-        if (a.weight.p && c < n) {
-            const Eight w = param8<F16>(a.weight, c, n);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[k].v[i] = x[k].v[i] * w.v[i];
-        }
-        if (a.bias.p && c < n) {
-            const Eight w = param8<F16>(a.bias, c, n);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[k].v[i] = x[k].v[i] + w.v[i];
-        }
+    for (int k = 0; k < Io::C; ++k) {
+        x[k] = x[k] * r;
+        if (a.weight.p) x[k] = x[k] * io.param(a.weight, k);
+        if (a.bias.p) x[k] = x[k] + io.param(a.bias, k);
     }
 }
 
-// The run of a row that a warp stores together: from column `run` on.
-template <bool F16, bool ANY>
-__device__ __forceinline__ void store_piece(const Rows16 &to, int64_t row, int n, const Eight &e, int k) {
-    uint32_t w[4];
-    words8<F16>(e, w);
-    const int run = (k * blockDim.x + (threadIdx.x & ~31)) * kPiece;
-    store_run<ANY>(to.row(row) + run, max(0, min(n - run, 32 * kPiece)), w, 32, threadIdx.x & 31);
-}
+enum SeamInput : int { kInResidual, kInBlock };
+struct SeamArgs {
+    Inputs in;
+    Rows16 gate, y, h;
+    NormArgs post, pre;
+    Drop drop;
+    float scale, inverse_n;
+    int gate_every;
+};
 
-// A row to a block of threads, C pieces to a thread.
-template <bool F16, bool ANY, int C, int THREADS>
-__global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_constant__ SeamArgs a) {
-    __shared__ float buffer[2][4 * kMaxWarps];
-    Reduction reduction{buffer, (int)blockDim.x / 32, 0};
-    const int64_t row = blockIdx.x;
-    Piece16<ANY> residual[C], block[C];
+template <bool F16, Kind KIND, int THREADS>
+__global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_constant__ SeamArgs a, const Waits waits) {
+    extern __shared__ __align__(128) uint8_t rows[];
+    __shared__ float buffer[2 * 4 * kMaxWarps];
+    __shared__ uint64_t full[kMostStages];
+    __shared__ uint32_t abort_flag;
+    using Io = RowIo<F16, KIND, 2>;
+    constexpr int C = Io::C;
+    Io io(a.in, rows, full, &abort_flag, waits);
+    constexpr bool kGrouped = KIND == kSmall || KIND == kSmallAny;
+    Reduction reduction{buffer + (kGrouped ? threadIdx.y * (io.threads / 32) * 4 : 0), io.tid, io.threads / 32, 0, kGrouped};
     pdl_trigger();
     pdl_wait();
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-        const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-        residual[k].clear();
-        block[k].clear();
-        if (a.block.p && c < a.n) block[k].load(a.block, row, c, a.m, a.n);
-        if (a.residual.p && c < a.n) residual[k].load(a.residual, row, c, a.m, a.n);
-    }
-    Eight v[C];
-#pragma unroll
-    for (int k = 0; k < C; ++k) v[k] = block[k].template values<F16>();
-    if (a.post.kind != EMTK_NORM_NONE) normalise<F16>(a.post, v, a.n, a.inverse_n, reduction);
+    if (io.row >= a.in.m) return;
+    io.begin();
     const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0u;
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-        const int first = k * blockDim.x + threadIdx.x, c = first * kPiece;
-        if (a.drop.below) dropped(a.drop, offset, (uint32_t)row, (uint32_t)first, v[k]);
-        if (a.gate.p && c < a.n) {
-            const Eight g = param8<F16>({a.gate.row(row / a.gate_every), 0}, c, a.n);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[k].v[i] = v[k].v[i] * g.v[i];
+    do {
+        io.wait();
+        uint32_t wb[C][4], wr[C][4];
+        io.load(kInBlock, wb);
+        io.load(kInResidual, wr);
+        if (KIND == kBulk) {
+            __syncthreads();
+            io.release();
         }
-        const Eight r = residual[k].template values<F16>();
+        Eight v[C];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[k].v[i] = fma2(r.v[i], both(a.scale), v[k].v[i]);
-        if (a.y.p) store_piece<F16, ANY>(a.y, row, a.n, v[k], k);
-    }
-    if (a.pre.kind == EMTK_NORM_NONE) return;
-    normalise<F16>(a.pre, v, a.n, a.inverse_n, reduction);
+        for (int k = 0; k < C; ++k) v[k] = values8<F16>(wb[k]);
+        if (a.post.kind != EMTK_NORM_NONE) normalise<F16>(a.post, v, io, a.inverse_n, reduction);
+        const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0};
 #pragma unroll
-    for (int k = 0; k < C; ++k) store_piece<F16, ANY>(a.h, row, a.n, v[k], k);
+        for (int k = 0; k < C; ++k) {
+            if (a.drop.below) dropped(a.drop, offset, (uint32_t)io.row, (uint32_t)(k * io.threads + io.tid), v[k]);
+            if (a.gate.p) v[k] = v[k] * io.param(gate, k);
+            const Eight r = values8<F16>(wr[k]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[k].v[i] = fma2(r.v[i], both(a.scale), v[k].v[i]);
+            if (a.y.p) io.store(a.y, k, v[k]);
+        }
+        if (a.pre.kind != EMTK_NORM_NONE) {
+            normalise<F16>(a.pre, v, io, a.inverse_n, reduction);
+#pragma unroll
+            for (int k = 0; k < C; ++k) io.store(a.h, k, v[k]);
+        }
+    } while (io.next());
+    io.end();
 }
 
 // ---------------------------------------------------------------- gradients
-// Column sums of a slice: dw_pre, db_pre, dw_post, db_post, d_gate.
-enum Sum : int { kSumPreW, kSumPreB, kSumPostW, kSumPostB, kSumGate, kSums };
+enum GradInput : int { kInY, kInDh, kInOut, kInDy };  // kInOut: the block's output
 
-// Slices of rows: `parts` of a gate row's rows each, or, with parts = 1, `groups_each`
-// whole gate rows.
-struct Slices {
-    int count, parts, groups_each;
-    int rows;  // of a part
+// What the columns' kernel needs of a row: of y and of the block's output the mean and
+// 1 / std, and of q = weight * dh the mean and, over std, the mean of q y^.
+struct RowStats {
+    float mean_y, ry, q_mean, qy, mean_b, rb, unused[2];
 };
 
-enum Input : int { kInY, kInDh, kInBlock, kInDy, kInputs };
-
 struct SeamGradArgs {
-    Rows16 in[kInputs];  // y, dh, block, dy
+    Inputs in;  // y, dh, block, dy
     Rows16 gate, d_residual, d_block;
     NormArgs post, pre;
     Drop drop;
     float scale, inverse_n;
-    int m, n, gate_every;
-    Slices slices;
-    float *partial[kSums];  // [slices][n] sums, or the result itself; null: not wanted
-    float *gate_out;        // of whole gate rows: d_gate
-    int64_t gate_ld;
-    float *spill;           // not null: the running sums, in place of shared memory, [slices][sums][columns]
-    int sums;               // wanted
-    int at[kSums];          // place of each among them
-    int stages, row_bytes;  // rows in shared memory, and the room for one of a matrix
+    int gate_every;
+    RowStats *stats;  // null: no sums are wanted
 };
 
-template <int C>
-struct Columns {  // a thread's running sums: [sum][piece][half][thread] of four
-    float4 *base;
-    __device__ __forceinline__ float4 *of(int sum, int k, int half) const {
-        return base + ((sum * C + k) * 2 + half) * (int)blockDim.x + threadIdx.x;
-    }
-    __device__ __forceinline__ void add(int sum, int k, const Eight &e) const {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float4 *const p = of(sum, k, half);
-            const float4 s = *p;
-            const float2 a = make_float2(s.x, s.y) + e.v[2 * half], b = make_float2(s.z, s.w) + e.v[2 * half + 1];
-            *p = make_float4(a.x, a.y, b.x, b.y);
-        }
-    }
-    // Writes columns c .. of a sum to `to` and starts it again.
-    __device__ __forceinline__ void flush(int sum, int k, float *to, int c, int n) const {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float4 *const p = of(sum, k, half);
-            const float v[4] = {p->x, p->y, p->z, p->w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (c + 4 * half + i < n) to[c + 4 * half + i] = v[i];
-            *p = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-    }
-};
-
-// Rows on their way into shared memory: a stage has room for one row of each matrix, as it
-// lies in its aligned 16-byte pieces, copied a row or two ahead by one thread.  Rows whose
-// outer pieces would reach beyond the matrix are copied by elements when their turn comes.
-struct RowPipe {
-    uint8_t *stages;
-    uint64_t *full;
-    Guard guard;
-    uint32_t phases = 0;  // of each stage
-    bool ok = true;
-
-    __device__ __forceinline__ uint8_t *place(const SeamGradArgs &a, int s, int input) const {
-        return stages + (s * kInputs + input) * a.row_bytes;
-    }
-    static __device__ __forceinline__ int head_of(const Rows16 &x, int64_t row) {
-        return (int)(reinterpret_cast<uintptr_t>(x.row(row)) % 16);
-    }
-    static __device__ __forceinline__ int bytes_of(const SeamGradArgs &a, int input, int64_t row) {  // of its aligned pieces
-        return (head_of(a.in[input], row) + 2 * a.n + 15) / 16 * 16;
-    }
-    static __device__ __forceinline__ bool by_hand(const SeamGradArgs &a, int64_t row) {
-        if (row >= kPiece && row < a.m - kPiece) return false;  // the 14 bytes around are of rows between
-#pragma unroll
-        for (int i = 0; i < kInputs; ++i) {
-            if (!a.in[i].p) continue;
-            const int64_t first = row * a.in[i].row_bytes - head_of(a.in[i], row), last = (a.m - 1) * a.in[i].row_bytes + 2 * a.n;
-            if (first < 0 || first + bytes_of(a, i, row) > last) return true;
-        }
-        return false;
-    }
-    // One thread starts the copies of a row.
-    __device__ __forceinline__ void fetch(const SeamGradArgs &a, int64_t row, int s) const {
-        if (by_hand(a, row)) return;
-        const uint32_t bar = smem_u32(full + s);
-        int bytes[kInputs], all = 0;
-#pragma unroll
-        for (int i = 0; i < kInputs; ++i) {
-            bytes[i] = a.in[i].p ? bytes_of(a, i, row) : 0;
-            all += bytes[i];
-        }
-        mbar_expect_tx(bar, (uint32_t)all);
-#pragma unroll
-        for (int i = 0; i < kInputs; ++i)
-            if (bytes[i])
-                bulk_load(smem_u32(place(a, s, i)), reinterpret_cast<const uint8_t *>(a.in[i].row(row)) - head_of(a.in[i], row), bytes[i], bar);
-    }
-    // All threads: the row is in stage s.
-    __device__ __forceinline__ void wait(const SeamGradArgs &a, int64_t row, int s) {
-        if (by_hand(a, row)) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kInputs; ++i) {
-                if (!a.in[i].p) continue;
-                uint16_t *const to = reinterpret_cast<uint16_t *>(place(a, s, i) + head_of(a.in[i], row));
-                for (int c = threadIdx.x; c < a.n; c += blockDim.x) to[c] = a.in[i].row(row)[c];
-            }
-            bulk_fence();
-            __syncthreads();
-            return;
-        }
-        if (ok) ok = wait_bounded(smem_u32(full + s), (phases >> s) & 1u, guard);
-        phases ^= 1u << s;
-    }
-    // A piece of the row, columns from n on 0.
-    __device__ __forceinline__ void piece(const SeamGradArgs &a, int64_t row, int s, int input, int c, uint32_t (&w)[4]) const {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = 0u;
-        if (!a.in[input].p || c >= a.n) return;
-        const uint4 *const p = reinterpret_cast<const uint4 *>(place(a, s, input)) + c / kPiece;
-        const int halves = head_of(a.in[input], row) / 2;
-        const uint4 lo = p[0];
-        if (halves) {
-            const uint4 hi = p[1];
-            const uint32_t x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            shift_words(x, halves, w);
-        } else {
-            w[0] = lo.x, w[1] = lo.y, w[2] = lo.z, w[3] = lo.w;
-        }
-        if (c + kPiece > a.n) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] &= (c + 2 * i < a.n ? 0xffffu : 0u) | (c + 2 * i + 1 < a.n ? 0xffff0000u : 0u);
-        }
-    }
-};
-
-template <bool F16, int C>
-__global__ void __launch_bounds__(1024) residual_norm_grad_kernel(const __grid_constant__ SeamGradArgs a, int *status, int64_t timeout_ns) {
-    extern __shared__ __align__(128) uint8_t shared[];
-    __shared__ float buffer[2][4 * kMaxWarps];
-    __shared__ uint64_t full[2];
+template <bool F16, Kind KIND, int THREADS, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS) residual_norm_grad_kernel(const __grid_constant__ SeamGradArgs a, const Waits waits) {
+    extern __shared__ __align__(128) uint8_t rows[];
+    __shared__ float buffer[2 * 4 * kMaxWarps];
+    __shared__ uint64_t full[kMostStages];
     __shared__ uint32_t abort_flag;
-    Reduction reduction{buffer, (int)blockDim.x / 32, 0};
-    const int slice = blockIdx.x;
-    RowPipe pipe{shared, full, {&abort_flag, status, timeout_ns}};
-    if (threadIdx.x == 0) {
-        mbar_init(smem_u32(full), 1);
-        mbar_init(smem_u32(full + 1), 1);
-        abort_flag = 0;
-        fence_mbar_init();
-    }
-    Columns<C> sums{reinterpret_cast<float4 *>(shared + a.stages * kInputs * a.row_bytes)};
+    using Io = RowIo<F16, KIND, 4>;
+    constexpr int C = Io::C;
+    Io io(a.in, rows, full, &abort_flag, waits);
+    constexpr bool kGrouped = KIND == kSmall || KIND == kSmallAny;
+    Reduction reduction{buffer + (kGrouped ? threadIdx.y * (io.threads / 32) * 4 : 0), io.tid, io.threads / 32, 0, kGrouped};
+    const bool pre = a.pre.kind != EMTK_NORM_NONE, post = a.post.kind != EMTK_NORM_NONE;
+    const bool pre_mean = a.pre.kind == EMTK_NORM_LAYER, post_mean = a.post.kind == EMTK_NORM_LAYER;
+    const int n = a.in.n;
     pdl_trigger();
     pdl_wait();
-    if (a.spill) sums.base = reinterpret_cast<float4 *>(a.spill) + (int64_t)slice * a.sums * C * 2 * blockDim.x;
-    for (int i = 0; i < a.sums * C * 2; ++i) sums.base[i * blockDim.x + threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
-    int64_t r0, r1;  // the slice's rows
-    if (a.slices.parts > 1) {
-        const int64_t begin = (int64_t)(slice / a.slices.parts) * a.gate_every, at = (int64_t)(slice % a.slices.parts) * a.slices.rows;
-        const int64_t end = min(begin + a.gate_every, (int64_t)a.m);
-        r0 = min(begin + at, end);
-        r1 = min(begin + at + a.slices.rows, end);
-    } else {
-        r0 = min((int64_t)slice * a.slices.groups_each * a.gate_every, (int64_t)a.m);
-        r1 = min(r0 + (int64_t)a.slices.groups_each * a.gate_every, (int64_t)a.m);
-    }
-    const bool pre = a.pre.kind != EMTK_NORM_NONE, post = a.post.kind != EMTK_NORM_NONE, has_block = a.in[kInBlock].p != nullptr;
-    const bool pre_mean = a.pre.kind == EMTK_NORM_LAYER, post_mean = a.post.kind == EMTK_NORM_LAYER;
-    const bool gate_sum = a.partial[kSumGate] || a.gate_out;
+    if (io.row >= a.in.m) return;
+    io.begin();
     const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0u;
-    __syncthreads();
-    if (threadIdx.x == 0)
-        for (int i = 0; i < a.stages && r0 + i < r1; ++i) pipe.fetch(a, r0 + i, i);
-    int s = 0;
-    int64_t group = r0 / a.gate_every, group_end = (group + 1) * a.gate_every;
-    for (int64_t row = r0; row < r1; ++row) {
-        pipe.wait(a, row, s);
-        Eight y[C], d[C], b[C], t[C];  // y, b: centred; d: dh, then q; t: of dy on
+    do {
+        io.wait();
+        uint32_t w[C][4], wt[C][4];
+        Eight y[C], q[C], b[C];
+        io.load(kInY, w);
 #pragma unroll
-        for (int k = 0; k < C; ++k) {
-            const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-            uint32_t w[4];
-            pipe.piece(a, row, s, kInY, c, w);
-            y[k] = values8<F16>(w);
-            pipe.piece(a, row, s, kInDh, c, w);
-            d[k] = values8<F16>(w);
-            pipe.piece(a, row, s, kInBlock, c, w);
-            b[k] = values8<F16>(w);
-            pipe.piece(a, row, s, kInDy, c, w);
-            t[k] = values8<F16>(w);
+        for (int k = 0; k < C; ++k) y[k] = values8<F16>(w[k]);
+        io.load(kInDh, w);
+#pragma unroll
+        for (int k = 0; k < C; ++k) q[k] = values8<F16>(w[k]);
+        io.load(kInOut, w);
+#pragma unroll
+        for (int k = 0; k < C; ++k) b[k] = values8<F16>(w[k]);
+        io.load(kInDy, wt);
+        if (KIND == kBulk) {
+            __syncthreads();
+            io.release();
         }
+        RowStats stats{};
+        stats.rb = 1.f;
         if (pre_mean || post_mean) {
             float v[2] = {};
 #pragma unroll
@@ -393,146 +458,207 @@ __global__ void __launch_bounds__(1024) residual_norm_grad_kernel(const __grid_c
                 v[0] += sum_of(y[k]);
                 v[1] += sum_of(b[k]);
             }
-            block_sum(v, reduction);
+            row_sum(v, reduction);
+            stats.mean_y = pre_mean ? v[0] * a.inverse_n : 0.f;
+            stats.mean_b = post_mean ? v[1] * a.inverse_n : 0.f;
 #pragma unroll
             for (int k = 0; k < C; ++k) {
-                const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-                if (pre_mean) centre(y[k], v[0] * a.inverse_n, c, a.n);
-                if (post_mean) centre(b[k], v[1] * a.inverse_n, c, a.n);
+                if (pre_mean) centre(y[k], stats.mean_y, k < C - 1 ? 0 : io.column(k), n);
+                if (post_mean) centre(b[k], stats.mean_b, k < C - 1 ? 0 : io.column(k), n);
             }
         }
-        if (a.partial[kSumPreB]) {
+        if (a.pre.weight.p) {
 #pragma unroll
-            for (int k = 0; k < C; ++k) sums.add(a.at[kSumPreB], k, d[k]);
+            for (int k = 0; k < C; ++k) q[k] = q[k] * io.param(a.pre.weight, k);
         }
-        float ry = 0.f, rb = 1.f;
         if (pre || post) {
             float v[4] = {};  // squares of y and b, q, q y
 #pragma unroll
             for (int k = 0; k < C; ++k) {
-                const int c = (k * blockDim.x + threadIdx.x) * kPiece;
                 v[0] += dot(y[k], y[k]);
                 v[1] += dot(b[k], b[k]);
-                Eight q = d[k];
-                if (a.pre.weight.p && c < a.n) {
-                    const Eight w = param8<F16>(a.pre.weight, c, a.n);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) q.v[i] = q.v[i] * w.v[i];
-                }
-                v[2] += sum_of(q);
-                v[3] += dot(q, y[k]);
+                v[2] += sum_of(q[k]);
+                v[3] += dot(q[k], y[k]);
             }
-            block_sum(v, reduction);
-            if (pre) ry = rsqrtf(fmaf(v[0], a.inverse_n, a.pre.eps));
-            if (post) rb = rsqrtf(fmaf(v[1], a.inverse_n, a.post.eps));
-            if (pre) {
-                const float q_mean = pre_mean ? v[2] * a.inverse_n : 0.f, qy = v[3] * a.inverse_n * ry * ry;
-#pragma unroll
-                for (int k = 0; k < C; ++k) {
-                    const int c = (k * blockDim.x + threadIdx.x) * kPiece;
-                    if (a.partial[kSumPreW]) {
-                        Eight x;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x.v[i] = d[k].v[i] * (y[k].v[i] * both(ry));
-                        sums.add(a.at[kSumPreW], k, x);
-                    }
-                    if (a.pre.weight.p && c < a.n) {
-                        const Eight w = param8<F16>(a.pre.weight, c, a.n);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) d[k].v[i] = d[k].v[i] * w.v[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        t[k].v[i] = fma2(d[k].v[i] - fma2(y[k].v[i], both(qy), both(q_mean)), both(ry), t[k].v[i]);
-                }
-            }
+            row_sum(v, reduction);
+            if (pre) stats.ry = rsqrtf(fmaf(v[0], a.inverse_n, a.pre.eps));
+            if (post) stats.rb = rsqrtf(fmaf(v[1], a.inverse_n, a.post.eps));
+            stats.q_mean = pre_mean ? v[2] * a.inverse_n : 0.f;
+            stats.qy = v[3] * a.inverse_n * stats.ry * stats.ry;
         }
-        // every thread has taken the row from its stage: the sums' barrier, or where there was none, one more
-        if (!(reduction.warps > 1 && (pre || post))) __syncthreads();
-        if (threadIdx.x == 0 && row + a.stages < r1) pipe.fetch(a, row + a.stages, s);
-        if (++s == a.stages) s = 0;
-        if (row >= group_end) {
-            ++group;
-            group_end += a.gate_every;
-        }
+        if (a.stats && io.tid == 0) a.stats[io.row] = stats;
+        const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0};
         float u[2] = {};  // the sums for the block's norm
 #pragma unroll
         for (int k = 0; k < C; ++k) {
-            const int first = k * blockDim.x + threadIdx.x, c = first * kPiece;
-            if (a.d_residual.p) {
-                Eight x;
+            Eight t = values8<F16>(wt[k]);
+            if (pre) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x.v[i] = t[k].v[i] * both(a.scale);
-                store_piece<F16, true>(a.d_residual, row, a.n, x, k);
+                for (int i = 0; i < 4; ++i)
+                    t.v[i] = fma2(q[k].v[i] - fma2(y[k].v[i], both(stats.qy), both(stats.q_mean)), both(stats.ry), t.v[i]);
             }
-            if (!has_block) continue;
-            if (a.drop.below) dropped(a.drop, offset, (uint32_t)row, (uint32_t)first, t[k]);
-            if (c + kPiece > a.n) centre(t[k], 0.f, c, a.n);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) b[k].v[i] = b[k].v[i] * both(rb);  // now normalised
-            Eight w;
-            w.fill(1.f);
-            if (a.post.weight.p && c < a.n) w = param8<F16>(a.post.weight, c, a.n);
-            if (gate_sum) {
-                Eight x;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x.v[i] = b[k].v[i] * w.v[i];
-                if (a.post.bias.p && c < a.n) {
-                    const Eight bias = param8<F16>(a.post.bias, c, a.n);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x.v[i] = x.v[i] + bias.v[i];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x.v[i] = x.v[i] * t[k].v[i];
-                sums.add(a.at[kSumGate], k, x);
-            }
-            if (a.gate.p && c < a.n) {
-                const Eight g = param8<F16>({a.gate.row(group), 0}, c, a.n);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t[k].v[i] = t[k].v[i] * g.v[i];
-            }
-            if (a.partial[kSumPostW]) {
-                Eight x;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x.v[i] = t[k].v[i] * b[k].v[i];
-                sums.add(a.at[kSumPostW], k, x);
-            }
-            if (a.partial[kSumPostB]) sums.add(a.at[kSumPostB], k, t[k]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t[k].v[i] = t[k].v[i] * w.v[i];
-            u[0] += sum_of(t[k]);
-            u[1] += dot(t[k], b[k]);
+            if (a.d_residual.p) io.store(a.d_residual, k, t * a.scale);
+            if (!a.d_block.p) continue;
+            if (a.drop.below) dropped(a.drop, offset, (uint32_t)io.row, (uint32_t)(k * io.threads + io.tid), t);
+            if (k == C - 1 && io.last) centre(t, 0.f, io.column(k), n);
+            if (a.gate.p) t = t * io.param(gate, k);
+            if (a.post.weight.p) t = t * io.param(a.post.weight, k);
+            q[k] = t;
+            b[k] = b[k] * stats.rb;  // now normalised
+            u[0] += sum_of(t);
+            u[1] += dot(t, b[k]);
         }
         if (a.d_block.p) {
             float mean = 0.f, along = 0.f;
             if (post) {
-                block_sum(u, reduction);
+                row_sum(u, reduction);
                 mean = post_mean ? u[0] * a.inverse_n : 0.f;
                 along = u[1] * a.inverse_n;
             }
 #pragma unroll
             for (int k = 0; k < C; ++k) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) t[k].v[i] = (t[k].v[i] - fma2(b[k].v[i], both(along), both(mean))) * both(rb);
-                store_piece<F16, true>(a.d_block, row, a.n, t[k], k);
+                for (int i = 0; i < 4; ++i) q[k].v[i] = (q[k].v[i] - fma2(b[k].v[i], both(along), both(mean))) * both(stats.rb);
+                io.store(a.d_block, k, q[k]);
             }
         }
-        if (a.gate_out && (row + 1 == group_end || row + 1 == r1)) {
-#pragma unroll
-            for (int k = 0; k < C; ++k)
-                sums.flush(a.at[kSumGate], k, a.gate_out + group * a.gate_ld, (k * blockDim.x + threadIdx.x) * kPiece, a.n);
+    } while (io.next());
+    io.end();
+}
+
+// ---- column sums: dw_pre, db_pre, dw_post, db_post, d_gate
+enum Sum : int { kSumPreW, kSumPreB, kSumPostW, kSumPostB, kSumGate, kSums };
+
+// Slices of rows: `parts` of a gate row's rows each, or, with parts = 1, `groups_each`
+// whole gate rows.
+struct Slices {
+    int count, parts, groups_each;
+    int rows;  // of a part
+    __device__ __forceinline__ void range(int slice, int gate_every, int m, int64_t &r0, int64_t &r1) const {
+        if (parts > 1) {
+            const int64_t begin = (int64_t)(slice / parts) * gate_every, at = (int64_t)(slice % parts) * rows;
+            const int64_t end = min(begin + gate_every, (int64_t)m);
+            r0 = min(begin + at, end);
+            r1 = min(begin + at + rows, end);
+        } else {
+            r0 = min((int64_t)slice * groups_each * gate_every, (int64_t)m);
+            r1 = min(r0 + (int64_t)groups_each * gate_every, (int64_t)m);
         }
     }
+};
+
+struct SumArgs {
+    SeamGradArgs g;
+    Slices slices;
+    float *partial[kSums];  // [slices][n] sums, or the result itself; null: not wanted
+    float *gate_out;        // of whole gate rows: d_gate
+    int64_t gate_ld;
+};
+
+constexpr int kSumThreads = 128, kSumRows = kSumThreads / 32;
+
+// The sums of the block's rows of threads for a run of columns, in order, to `to`.
+__device__ __forceinline__ void flush_sum(Eight &e, float (*shared)[32 * kPiece], float *to, int c0, int n) {
+    __syncthreads();
+    float *const mine = shared[threadIdx.x / 32] + threadIdx.x % 32;  // value i of a lane: 32 i on, so that lanes meet in no bank
 #pragma unroll
-    for (int k = 0; k < C; ++k)
-        for (int i = 0; i < kSums; ++i)
-            if (a.partial[i])
-                sums.flush(a.at[i], k, a.partial[i] + (int64_t)slice * a.n, (k * blockDim.x + threadIdx.x) * kPiece, a.n);
-    if (!pipe.ok) {  // copies in flight land within microseconds: leave them a millisecond
-        const uint64_t t0 = global_timer_ns();
-        while (global_timer_ns() - t0 < 1000000u) {
-        }
+    for (int i = 0; i < 4; ++i) {
+        mine[64 * i] = e.v[i].x;
+        mine[64 * i + 32] = e.v[i].y;
     }
+    __syncthreads();
+#pragma unroll
+    for (int c = threadIdx.x; c < 32 * kPiece; c += kSumThreads) {
+        const int at = c % kPiece * 32 + c / kPiece;
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < kSumRows; ++r) sum += shared[r][at];
+        if (c0 + c < n) to[c0 + c] = sum;
+    }
+    e.fill(0.f);
+}
+
+// A block takes 256 columns and a slice's rows, a warp every fourth of them, a piece to a
+// lane.  BLOCK: sums over the block's output (all inputs are read); else of the norm after
+// it alone (y and dh).
+template <bool F16, bool ANY, bool BLOCK>
+__global__ void __launch_bounds__(kSumThreads, BLOCK ? 3 : 5) residual_norm_sum_kernel(const __grid_constant__ SumArgs a) {
+    __shared__ float shared[kSumRows][32 * kPiece];
+    const SeamGradArgs &g = a.g;
+    const int n = g.in.n, m = g.in.m, slice = blockIdx.y;
+    const int c0 = blockIdx.x * 32 * kPiece, c = c0 + threadIdx.x % 32 * kPiece;
+    const bool in = c < n, pre = g.pre.kind != EMTK_NORM_NONE;
+    pdl_trigger();
+    pdl_wait();
+    int64_t r0, r1;
+    a.slices.range(slice, g.gate_every, m, r0, r1);
+    Eight sum[BLOCK ? kSums : 2], weight, post_weight, post_bias;
+#pragma unroll
+    for (Eight &e : sum) e.fill(0.f);
+    weight.fill(1.f);
+    post_weight.fill(1.f);
+    post_bias.fill(0.f);
+    if (in && g.pre.weight.p) weight = param8<F16>(g.pre.weight, c, n);
+    if (BLOCK && in && g.post.weight.p) post_weight = param8<F16>(g.post.weight, c, n);
+    if (BLOCK && in && g.post.bias.p) post_bias = param8<F16>(g.post.bias, c, n);
+    const uint64_t offset = BLOCK && g.drop.below ? drop_offset(g.drop) : 0u;
+    // where whole gate rows are summed, one after another
+    for (int64_t begin = r0; begin < r1;) {
+        const int64_t group = begin / g.gate_every, end = a.gate_out ? min((group + 1) * g.gate_every, r1) : r1;
+        Piece16<ANY> wy, wd, wb, wt;
+        auto fetch = [&](int64_t row) {
+            if (pre) wy.load(g.in.in[kInY], row, c, m, n);
+            if (pre) wd.load(g.in.in[kInDh], row, c, m, n);
+            if (BLOCK) wb.load(g.in.in[kInOut], row, c, m, n);
+            if (BLOCK && g.in.in[kInDy].p) wt.load(g.in.in[kInDy], row, c, m, n);
+        };
+        wy.clear();
+        wd.clear();
+        wb.clear();
+        wt.clear();
+        int64_t row = begin + threadIdx.x / 32;
+        if (in && row < end) fetch(row);
+        for (; row < end; row += kSumRows) {
+            Eight y = wy.template values<F16>(), d = wd.template values<F16>();
+            Eight b = wb.template values<F16>(), t = wt.template values<F16>();
+            const float4 s = __ldg(reinterpret_cast<const float4 *>(g.stats + row));
+            const float2 s2 = __ldg(reinterpret_cast<const float2 *>(g.stats + row) + 2);
+            if (in && row + kSumRows < end) fetch(row + kSumRows);
+            const float mean_y = s.x, ry = s.y, q_mean = s.z, qy = s.w, mean_b = s2.x, rb = s2.y;
+            if (pre) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    y.v[i] = y.v[i] - both(mean_y);
+                    sum[kSumPreW].v[i] = fma2(d.v[i], y.v[i] * both(ry), sum[kSumPreW].v[i]);
+                    sum[kSumPreB].v[i] = sum[kSumPreB].v[i] + d.v[i];
+                    if (BLOCK) t.v[i] = fma2(d.v[i] * weight.v[i] - fma2(y.v[i], both(qy), both(q_mean)), both(ry), t.v[i]);
+                }
+            }
+            if constexpr (BLOCK) {
+                if (g.drop.below) dropped(g.drop, offset, (uint32_t)row, (uint32_t)(c / kPiece), t);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    b.v[i] = (b.v[i] - both(mean_b)) * both(rb);
+                    sum[kSumGate].v[i] = fma2(t.v[i], fma2(b.v[i], post_weight.v[i], post_bias.v[i]), sum[kSumGate].v[i]);
+                }
+                if (g.gate.p && in) {
+                    const Eight gate = param8<F16>({g.gate.row(row / g.gate_every), 0}, c, n);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t.v[i] = t.v[i] * gate.v[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum[kSumPostW].v[i] = fma2(t.v[i], b.v[i], sum[kSumPostW].v[i]);
+                    sum[kSumPostB].v[i] = sum[kSumPostB].v[i] + t.v[i];
+                }
+            }
+        }
+        if (BLOCK && a.gate_out) flush_sum(sum[BLOCK ? kSumGate : 0], shared, a.gate_out + group * a.gate_ld, c0, n);
+        begin = end;
+    }
+#pragma unroll
+    for (int i = 0; i < (BLOCK ? kSums : 2); ++i)
+        if (a.partial[i]) flush_sum(sum[i], shared, a.partial[i] + (int64_t)slice * n, c0, n);
 }
 
 // Adds slices' sums: a block takes 32 columns of one result, each of its warps every
@@ -571,52 +697,75 @@ __global__ void __launch_bounds__(32 * kMaxWarps) residual_norm_join_kernel(cons
 }
 
 // ---------------------------------------------------------------- host
-// Pieces of a thread and threads of a block.
+// How rows are had, threads of a row, rows of a block.
 struct Shape {
-    int pieces, threads;
+    Kind kind;
+    int threads, groups;
 };
-Shape shape_of(int n, int most_threads) {
-    const int all = (n + kPiece - 1) / kPiece, c = all > most_threads ? 2 : 1;
-    return {c, std::max(1, ((all + c - 1) / c + 31) / 32) * 32};
+Shape shape_of(int n, bool on_grid, bool bulk) {
+    const int all = (n + kPiece - 1) / kPiece;
+    if (all <= kGroupThreads) {
+        const int threads = (all + 31) / 32 * 32;
+        return {on_grid && n % kPiece == 0 ? kSmall : kSmallAny, threads, std::min(kMostGroups, 256 / threads)};
+    }
+    return {!bulk && on_grid && n % kPiece == 0 ? kDirect : kBulk, ((all + 1) / 2 + 31) / 32 * 32, 1};
 }
 
-template <bool F16, bool ANY>
-cudaError_t run(const SeamArgs &a, cudaStream_t s) {
-    const Shape h = shape_of(a.n, 256);
-    void (*kernel)(const SeamArgs) = h.pieces == 1      ? residual_norm_kernel<F16, ANY, 1, 256>
-                                     : h.threads <= 256 ? residual_norm_kernel<F16, ANY, 2, 256>
-                                                        : residual_norm_kernel<F16, ANY, 2, 1024>;
-    return launch_pdl(kernel, dim3((unsigned)a.m), dim3((unsigned)h.threads), 0, s, a);
+// Blocks of an SM at once, as far as registers and shared memory go.
+int blocks_of(const Shape &h, size_t shared, int registers) {
+    return (int)std::max<size_t>(1, std::min<size_t>((size_t)65536 / (registers * h.threads), (size_t)222 * 1024 / (shared + 2560)));
 }
 
-constexpr int kMostShared = 222 * 1024;  // of a block, beside what it has fixed
+template <typename Args>
+cudaError_t run_rows(void (*kernel)(const Args, const Waits), const Shape &h, int inputs, int registers, Args &a, const emtk_nn *nn, cudaStream_t s) {
+    int64_t blocks = ((int64_t)a.in.m + h.groups - 1) / h.groups;
+    size_t shared = 0;
+    if (h.kind == kBulk) {
+        const size_t row = (size_t)inputs * a.in.row_bytes;
+        a.in.stages = 2 * row <= 222 * 1024 ? 2 : 1;
+        shared = a.in.stages * row;
+        blocks = std::min<int64_t>(blocks, (int64_t)nn->sm_count * blocks_of(h, shared, registers));
+    }
+    return launch_pdl(kernel, dim3((unsigned)blocks), dim3((unsigned)h.threads, (unsigned)h.groups), shared, s, a, Waits{nn->status, nn->timeout_ns});
+}
 
-struct GradPlan {
-    Shape shape;
-    Slices slices;
-    size_t columns;  // bytes of a slice's running sums
-    size_t shared;   // of a block: rows, and the sums if there is room
-    bool spilled;
-    int sums, stages, row_bytes;
-};
-GradPlan grad_plan(int m, int n, int gate_every, int sums, int sms) {
-    GradPlan p;
-    p.shape = shape_of(n, 1024);
-    p.sums = sums;
-    p.columns = (size_t)sums * p.shape.pieces * p.shape.threads * kPiece * 4;
-    // a row as it lies: up to 14 bytes before it, whole pieces, and the one after the last
-    p.row_bytes = (2 * n + 14 + 15) / 16 * 16 + 16;
-    const size_t stage = (size_t)kInputs * p.row_bytes;
-    p.spilled = stage + p.columns > kMostShared;
-    const size_t sums_bytes = p.spilled ? 0 : p.columns;
-    p.stages = 2 * stage + sums_bytes <= kMostShared ? 2 : 1;
-    p.shared = p.stages * stage + sums_bytes;
-    const int warps = p.shape.threads / 32;
-    const int each = std::max(1, std::min(32 / warps, (int)(kMostShared / (p.shared + 2048))));  // blocks of an SM
-    // two rows at least to a slice, and no more slices than are resident at once
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((int64_t)sms * each, ((int64_t)m + 1) / 2));
+template <bool F16>
+cudaError_t run(SeamArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) {
+    switch (h.kind) {
+        case kSmall: return run_rows(residual_norm_kernel<F16, kSmall, 256>, h, 2, 64, a, nn, s);
+        case kSmallAny: return run_rows(residual_norm_kernel<F16, kSmallAny, 256>, h, 2, 64, a, nn, s);
+        case kDirect:
+            return run_rows(h.threads <= 256   ? residual_norm_kernel<F16, kDirect, 256>
+                            : h.threads <= 512 ? residual_norm_kernel<F16, kDirect, 512>
+                                               : residual_norm_kernel<F16, kDirect, 1024>, h, 2, 64, a, nn, s);
+        default:
+            return run_rows(h.threads <= 512 ? residual_norm_kernel<F16, kBulk, 512> : residual_norm_kernel<F16, kBulk, 1024>, h, 2, 64, a, nn, s);
+    }
+}
+template <bool F16>
+cudaError_t run(SeamGradArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) {
+    switch (h.kind) {
+        case kSmall: return run_rows(residual_norm_grad_kernel<F16, kSmall, 256, 3>, h, 4, 80, a, nn, s);
+        case kSmallAny: return run_rows(residual_norm_grad_kernel<F16, kSmallAny, 256, 3>, h, 4, 80, a, nn, s);
+        default:
+            if (h.threads <= 256) return run_rows(residual_norm_grad_kernel<F16, kBulk, 256, 3>, h, 4, 80, a, nn, s);
+            if (h.threads <= 384) return run_rows(residual_norm_grad_kernel<F16, kBulk, 384, 2>, h, 4, 80, a, nn, s);
+            if (h.threads <= 512) return run_rows(residual_norm_grad_kernel<F16, kBulk, 512, 1>, h, 4, 128, a, nn, s);
+            return run_rows(residual_norm_grad_kernel<F16, kBulk, 1024, 1>, h, 4, 64, a, nn, s);
+    }
+}
+template <typename Args>
+cudaError_t run(Args &a, int type, const Shape &h, const emtk_nn *nn, cudaStream_t s) {
+    return type == EMTK_TYPE_F16 ? run<true>(a, h, nn, s) : run<false>(a, h, nn, s);
+}
+
+// How the columns' kernel cuts the rows: blocks for two rounds of every SM, of 16 rows at
+// least.
+Slices slices_of(int m, int n, int gate_every, int sms) {
+    const int64_t columns = ((int64_t)n + 32 * kPiece - 1) / (32 * kPiece);
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((4 * (int64_t)sms + columns - 1) / columns, ((int64_t)m + 15) / 16));
     const int64_t groups = std::max<int64_t>(1, ((int64_t)m + gate_every - 1) / gate_every);
-    Slices &l = p.slices;
+    Slices l;
     if (groups < want) {
         const int64_t parts = want / groups, rows = std::min<int64_t>(gate_every, std::max(1, m));
         l.rows = (int)((rows + parts - 1) / parts);
@@ -629,29 +778,30 @@ GradPlan grad_plan(int m, int n, int gate_every, int sums, int sms) {
         l.rows = 0;
         l.count = (int)((groups + l.groups_each - 1) / l.groups_each);
     }
-    return p;
-}
-
-template <bool F16>
-cudaError_t run_grad(const SeamGradArgs &a, const GradPlan &p, const emtk_nn *nn, cudaStream_t s) {
-    return launch_pdl(p.shape.pieces == 1 ? residual_norm_grad_kernel<F16, 1> : residual_norm_grad_kernel<F16, 2>,
-                      dim3((unsigned)p.slices.count), dim3((unsigned)p.shape.threads), p.shared, s, a, nn->status, nn->timeout_ns);
+    return l;
 }
 
 }  // namespace
 
-cudaError_t init_norm_kernels() {
+template <bool F16>
+static cudaError_t init_kernels() {
     cudaError_t e = cudaSuccess;
-    for (void (*kernel)(const SeamGradArgs, int *, int64_t) : {residual_norm_grad_kernel<false, 1>, residual_norm_grad_kernel<false, 2>,
-                                                               residual_norm_grad_kernel<true, 1>, residual_norm_grad_kernel<true, 2>})
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    for (void (*kernel)(const SeamArgs, const Waits) : {residual_norm_kernel<F16, kBulk, 512>, residual_norm_kernel<F16, kBulk, 1024>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024);
+    for (void (*kernel)(const SeamGradArgs, const Waits) :
+         {residual_norm_grad_kernel<F16, kBulk, 256, 3>, residual_norm_grad_kernel<F16, kBulk, 384, 2>,
+          residual_norm_grad_kernel<F16, kBulk, 512, 1>, residual_norm_grad_kernel<F16, kBulk, 1024, 1>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024);
     return e;
 }
+cudaError_t init_norm_kernels() {
+    const cudaError_t e = init_kernels<false>();
+    return e == cudaSuccess ? init_kernels<true>() : e;
+}
 
-cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, cudaStream_t s) {
+cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, const emtk_nn *nn, cudaStream_t s) {
     SeamArgs a{};
-    a.residual = rows16_of(p.residual);
-    a.block = rows16_of(p.block);
+    a.in = {{rows16_of(p.residual), rows16_of(p.block)}, p.m, p.n, bulk_row_bytes(p.n), 1};
     a.gate = rows16_of(p.gate);
     a.y = rows16_of(p.y);
     a.h = rows16_of(p.h);
@@ -660,12 +810,9 @@ cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, cudaStream_t 
     if (p.block.d) a.drop = drop_of(p.drop);
     a.scale = p.scale;
     a.inverse_n = 1.f / (float)p.n;
-    a.m = p.m;
-    a.n = p.n;
     a.gate_every = p.gate_every;
-    const bool any = !(on_grid(p.residual, p.m) && on_grid(p.block, p.m) && on_grid(p.y, p.m) && on_grid(p.h, p.m));
-    if (p.type == EMTK_TYPE_F16) return any ? run<true, true>(a, s) : run<true, false>(a, s);
-    return any ? run<false, true>(a, s) : run<false, false>(a, s);
+    const bool whole = on_grid(p.residual, p.m) && on_grid(p.block, p.m) && on_grid(p.y, p.m) && on_grid(p.h, p.m);
+    return run(a, p.type, shape_of(p.n, whole, false), nn, s);
 }
 
 // The sums that a call wants, and the workspace that they take.
@@ -673,17 +820,13 @@ static int norm_sums(const emtk_residual_norm_grad_args &p) {
     return (p.dw_pre ? 1 : 0) + (p.db_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.db_post ? 1 : 0) + (p.d_gate.d ? 1 : 0);
 }
 size_t residual_norm_workspace(const emtk_residual_norm_grad_args &p, int sms) {
-    const GradPlan g = grad_plan(p.m, p.n, p.gate_every, norm_sums(p), sms);
-    return (g.spilled ? g.columns * g.slices.count : 0) + (size_t)g.sums * g.slices.count * p.n * 4;
+    const int sums = norm_sums(p);
+    return sums ? (size_t)p.m * sizeof(RowStats) + (size_t)sums * slices_of(p.m, p.n, p.gate_every, sms).count * p.n * sizeof(float) : 0;
 }
 
 cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s) {
-    const GradPlan g = grad_plan(p.m, p.n, p.gate_every, norm_sums(p), nn->sm_count);
     SeamGradArgs a{};
-    a.in[kInY] = rows16_of(p.y);
-    a.in[kInDh] = rows16_of(p.dh);
-    a.in[kInBlock] = rows16_of(p.block);
-    a.in[kInDy] = rows16_of(p.dy);
+    a.in = {{rows16_of(p.y), rows16_of(p.dh), rows16_of(p.block), rows16_of(p.dy)}, p.m, p.n, bulk_row_bytes(p.n), 1};
     a.gate = rows16_of(p.gate);
     a.d_residual = rows16_of(p.d_residual);
     a.d_block = rows16_of(p.d_block);
@@ -692,45 +835,52 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
     if (p.block.d) a.drop = drop_of(p.drop);
     a.scale = p.scale;
     a.inverse_n = 1.f / (float)p.n;
-    a.m = p.m;
-    a.n = p.n;
     a.gate_every = p.gate_every;
-    a.slices = g.slices;
-    a.sums = g.sums;
-    float *at = static_cast<float *>(workspace);
-    a.stages = g.stages;
-    a.row_bytes = g.row_bytes;
-    if (g.spilled) {
-        a.spill = at;
-        at += g.columns / 4 * g.slices.count;
-    }
+    const int sums = norm_sums(p);
+    if (sums) a.stats = static_cast<RowStats *>(workspace);
+    const bool odd = !(on_grid(p.dy, p.m) && on_grid(p.dh, p.m) && on_grid(p.y, p.m) && on_grid(p.block, p.m));
+    const bool whole = !odd && on_grid(p.d_residual, p.m) && on_grid(p.d_block, p.m);
+    cudaError_t e = p.m > 0 ? run(a, p.type, shape_of(p.n, whole, true), nn, s) : cudaSuccess;
+    if (e != cudaSuccess || !sums) return e;
+
+    const Slices slices = slices_of(p.m, p.n, p.gate_every, nn->sm_count);
+    SumArgs t{};
+    t.g = a;
+    t.slices = slices;
+    float *at = reinterpret_cast<float *>(a.stats + p.m);
     float *const out[kSums] = {p.dw_pre, p.db_pre, p.dw_post, p.db_post, static_cast<float *>(p.d_gate.d)};
     JoinArgs j{};
-    int place = 0;
     for (int i = 0; i < kSums; ++i) {
         if (!out[i]) continue;
-        a.at[i] = place++;
-        if (i == kSumGate && g.slices.parts == 1 && p.m > 0) {
-            a.gate_out = out[i];
-            a.gate_ld = p.d_gate.ld;
+        if (i == kSumGate && slices.parts == 1 && p.m > 0) {
+            t.gate_out = out[i];
+            t.gate_ld = p.d_gate.ld;
             continue;
         }
-        a.partial[i] = at;
-        at += (size_t)g.slices.count * p.n;
+        t.partial[i] = at;
+        at += (size_t)slices.count * p.n;
         if (i == kSumGate) {
-            j.gate_from = a.partial[i];
+            j.gate_from = t.partial[i];
             j.gate_to = out[i];
             j.gate_ld = p.d_gate.ld;
         } else {
-            j.from[j.results] = a.partial[i];
+            j.from[j.results] = t.partial[i];
             j.to[j.results++] = out[i];
         }
     }
-    j.slices = g.slices.count;
-    j.parts = g.slices.parts;
+    j.slices = slices.count;
+    j.parts = slices.parts;
     j.n = p.n;
-    cudaError_t e = p.type == EMTK_TYPE_F16 ? run_grad<true>(a, g, nn, s) : run_grad<false>(a, g, nn, s);
-    const int gates = j.gate_to ? std::max(1, g.slices.count / g.slices.parts) : 0;
+    const bool block = p.dw_post || p.db_post || p.d_gate.d, f16 = p.type == EMTK_TYPE_F16;
+    void (*kernel)(const SumArgs);
+    if (block)
+        kernel = odd ? (f16 ? residual_norm_sum_kernel<true, true, true> : residual_norm_sum_kernel<false, true, true>)
+                     : (f16 ? residual_norm_sum_kernel<true, false, true> : residual_norm_sum_kernel<false, false, true>);
+    else
+        kernel = odd ? (f16 ? residual_norm_sum_kernel<true, true, false> : residual_norm_sum_kernel<false, true, false>)
+                     : (f16 ? residual_norm_sum_kernel<true, false, false> : residual_norm_sum_kernel<false, false, false>);
+    e = launch_pdl(kernel, dim3((unsigned)((p.n + 32 * kPiece - 1) / (32 * kPiece)), (unsigned)slices.count), dim3(kSumThreads), 0, s, t);
+    const int gates = j.gate_to ? std::max(1, slices.count / slices.parts) : 0;
     if (e == cudaSuccess && j.results + gates > 0)
         e = launch_pdl(residual_norm_join_kernel, dim3((unsigned)((p.n + 31) / 32), (unsigned)(j.results + gates)),
                        dim3(32 * kMaxWarps), 0, s, j);
