@@ -555,6 +555,7 @@ struct SumArgs {
     int64_t gate_ld;
 };
 
+constexpr int kSumBlocks = 3, kSumBlocksPre = 5;  // of an SM at once
 constexpr int kSumThreads = 128, kSumRows = kSumThreads / 32;
 
 // The sums of the block's rows of threads for a run of columns, in order, to `to`.
@@ -582,7 +583,7 @@ __device__ __forceinline__ void flush_sum(Eight &e, float (*shared)[32 * kPiece]
 // lane.  BLOCK: sums over the block's output (all inputs are read); else of the norm after
 // it alone (y and dh).
 template <bool F16, bool ANY, bool BLOCK>
-__global__ void __launch_bounds__(kSumThreads, BLOCK ? 3 : 5) residual_norm_sum_kernel(const __grid_constant__ SumArgs a) {
+__global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPre) residual_norm_sum_kernel(const __grid_constant__ SumArgs a) {
     __shared__ float shared[kSumRows][32 * kPiece];
     const SeamGradArgs &g = a.g;
     const int n = g.in.n, m = g.in.m, slice = blockIdx.y;
@@ -759,11 +760,11 @@ cudaError_t run(Args &a, int type, const Shape &h, const emtk_nn *nn, cudaStream
     return type == EMTK_TYPE_F16 ? run<true>(a, h, nn, s) : run<false>(a, h, nn, s);
 }
 
-// How the columns' kernel cuts the rows: blocks for two rounds of every SM, of 16 rows at
-// least.
-Slices slices_of(int m, int n, int gate_every, int sms) {
+// How the columns' kernel cuts the rows: as many blocks as run at once (a second round of
+// few blocks costs as much as the first), of 16 rows at least.
+Slices slices_of(int m, int n, int gate_every, bool block, int sms) {
     const int64_t columns = ((int64_t)n + 32 * kPiece - 1) / (32 * kPiece);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((4 * (int64_t)sms + columns - 1) / columns, ((int64_t)m + 15) / 16));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((block ? kSumBlocks : kSumBlocksPre) * (int64_t)sms / columns, ((int64_t)m + 15) / 16));
     const int64_t groups = std::max<int64_t>(1, ((int64_t)m + gate_every - 1) / gate_every);
     Slices l;
     if (groups < want) {
@@ -819,9 +820,10 @@ cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, const emtk_nn
 static int norm_sums(const emtk_residual_norm_grad_args &p) {
     return (p.dw_pre ? 1 : 0) + (p.db_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.db_post ? 1 : 0) + (p.d_gate.d ? 1 : 0);
 }
+static bool block_sums(const emtk_residual_norm_grad_args &p) { return p.dw_post || p.db_post || p.d_gate.d; }
 size_t residual_norm_workspace(const emtk_residual_norm_grad_args &p, int sms) {
     const int sums = norm_sums(p);
-    return sums ? (size_t)p.m * sizeof(RowStats) + (size_t)sums * slices_of(p.m, p.n, p.gate_every, sms).count * p.n * sizeof(float) : 0;
+    return sums ? (size_t)p.m * sizeof(RowStats) + (size_t)sums * slices_of(p.m, p.n, p.gate_every, block_sums(p), sms).count * p.n * sizeof(float) : 0;
 }
 
 cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s) {
@@ -843,7 +845,7 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
     cudaError_t e = p.m > 0 ? run(a, p.type, shape_of(p.n, whole, true), nn, s) : cudaSuccess;
     if (e != cudaSuccess || !sums) return e;
 
-    const Slices slices = slices_of(p.m, p.n, p.gate_every, nn->sm_count);
+    const Slices slices = slices_of(p.m, p.n, p.gate_every, block_sums(p), nn->sm_count);
     SumArgs t{};
     t.g = a;
     t.slices = slices;
@@ -871,7 +873,7 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
     j.slices = slices.count;
     j.parts = slices.parts;
     j.n = p.n;
-    const bool block = p.dw_post || p.db_post || p.d_gate.d, f16 = p.type == EMTK_TYPE_F16;
+    const bool block = block_sums(p), f16 = p.type == EMTK_TYPE_F16;
     void (*kernel)(const SumArgs);
     if (block)
         kernel = odd ? (f16 ? residual_norm_sum_kernel<true, true, true> : residual_norm_sum_kernel<false, true, true>)
