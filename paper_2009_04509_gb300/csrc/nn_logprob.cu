@@ -7,6 +7,15 @@
 // Two runs' triples join the same way.  HBM bounds large calls (one read of the logits;
 // the gradient one read and one write), the call small ones.
 //
+// The K largest come from a second look at a small part of the row.  On the way each thread
+// notes the largest of its pieces (16 bytes; the lowest column among equals).  Of the
+// pieces' maxima, any K that are at hand bound the K-th from below, and every one of the
+// row's K largest lies in a piece whose maximum is at or above that bound: only the strips
+// of threads that hold such pieces are read again, and what is at or above the bound, a
+// few dozen as a rule, is ranked by comparing all with all.  (Each warp keeping a sorted list
+// in its lanes took up to five times the whole pass: an insertion is a dozen dependent
+// exchanges.)
+//
 // A row goes to a few lanes, to a block of threads, or, where rows are few and long, to a
 // cluster of blocks that join through shared memory.  Rows start anywhere: their aligned
 // 16-byte pieces are loaded whole, the up to 14 elements around them singly.
@@ -107,55 +116,17 @@ struct Sums {
     }
 };
 
-// Order of logits, and the lowest index first among equals; NaN is the least.  Never 0.
-__device__ __forceinline__ uint64_t key_of(float z, int column) {
+// Order of logits; NaN is the least.  Never 0.
+__device__ __forceinline__ uint32_t order_of(float z) {
     const uint32_t b = __float_as_uint(z + 0.f);  // -0 and 0 are equal
-    const uint32_t u = z != z ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-    return ((uint64_t)u << 32) | (uint32_t)~column;
+    return z != z ? 1u : b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float value_of(uint64_t key) {
-    const uint32_t u = (uint32_t)(key >> 32);
-    if (u == 0u) return __int_as_float(0x7fffffff);
-    return __uint_as_float((u & 0x80000000u) ? u & 0x7fffffffu : ~u);
+__device__ __forceinline__ float value_of(uint32_t order) {
+    return order == 1u ? __int_as_float(0x7fffffff) : __uint_as_float((order & 0x80000000u) ? order & 0x7fffffffu : ~order);
 }
-__device__ __forceinline__ uint64_t warp_max(uint64_t key) {
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(key >> 32));
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(key >> 32) == hi ? (uint32_t)key : 0u);
-    return ((uint64_t)hi << 32) | lo;
-}
-
-// A warp's largest keys, descending over its lanes; 0: none yet.
-struct TopList {
-    uint64_t mine, least;  // this lane's, and the one at `top`, which all know
-    float bar;             // value of `least`; NaN while there is none
-    __device__ __forceinline__ void clear() { mine = least = 0u, bar = __int_as_float(0x7fffffff); }
-    __device__ __forceinline__ void insert(uint64_t key, int top, int lane) {
-        const int at = __popc(__ballot_sync(0xffffffffu, mine > key));
-        const uint64_t up = __shfl_up_sync(0xffffffffu, mine, 1);
-        mine = lane < at ? mine : lane == at ? key : up;
-        least = __shfl_sync(0xffffffffu, mine, top - 1);
-        bar = least ? value_of(least) : __int_as_float(0x7fffffff);
-    }
-    // N values of each lane, the first `valid` of them from `column` on.
-    template <int N>
-    __device__ __forceinline__ void push(const float (&z)[N], int valid, int column, int top, int lane) {
-        bool some = false;
-#pragma unroll
-        for (int i = 0; i < N; ++i) some = some || (i < valid && !(z[i] < bar));
-        if (!__any_sync(0xffffffffu, some)) return;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint64_t key = i < valid ? key_of(z[i], column + i) : 0u;
-            uint32_t mask = __ballot_sync(0xffffffffu, key > least);
-            while (mask) {
-                const int from = __ffs(mask) - 1;
-                insert(__shfl_sync(0xffffffffu, key, from), top, lane);
-                mask &= mask - 1;
-                mask &= __ballot_sync(0xffffffffu, key > least);
-            }
-        }
-    }
-};
+// The lowest place first among equals; 0: nothing.
+__device__ __forceinline__ uint64_t key_of(uint32_t order, int place) { return ((uint64_t)order << 32) | (uint32_t)~place; }
+__device__ __forceinline__ int place_of(uint64_t key) { return (int)~(uint32_t)key; }
 
 struct LogprobArgs {
     const uint8_t *z;
@@ -168,53 +139,153 @@ struct LogprobArgs {
     int lanes_log2;      // of a row, in lanes_kernel
 };
 
-// The row's logits that thread `t` of `threads` takes, part `part` of `parts` of the row.
-// All threads of a warp run this together.
-template <int TYPE, bool TOP>
-__device__ __forceinline__ void take_row(const LogprobArgs &a, const uint8_t *row, bool in, int t, int threads, int part,
-                                         int parts, Sums &sums, TopList &list) {
+// A thread's strip of a row, thread t of `threads` at part `part` of `parts` of it: every
+// threads-th piece of the part, and the elements around the pieces, the head (unit 0; pieces
+// are units 1 ..) for the first thread and the tail (the last unit) for the last.
+template <int TYPE>
+struct Strip {
     using E = Elem<TYPE>;
-    const typename E::T *const p = reinterpret_cast<const typename E::T *>(row);
-    const Split s = split_row<TYPE>(row, in ? a.v : 0);
-    const int lane = threadIdx.x & 31;
-    // a part's pieces; the elements around them go with the first
-    const int each = (s.pieces + parts - 1) / parts, begin = part * each, end = min(begin + each, s.pieces);
-    const int singles = part == 0 ? s.head + s.tail : 0;
-    for (int e = t; TOP ? __any_sync(0xffffffffu, e < singles) : e < singles; e += threads) {
-        const int column = e < s.head ? e : s.pieces * E::kPer + e;
-        float z[1] = {0.f};
-        if (e < singles) {
-            z[0] = E::value(p[column]);
-            sums.raise(z[0], a.k);
-            sums.add(z[0], a.k);
-        }
-        if (TOP) list.push(z, e < singles ? 1 : 0, column, a.top, lane);
+    const typename E::T *p;
+    Split split;
+    int t, threads, first, end;  // first piece, end of the part's pieces
+    bool ends;                   // the part has the row's ends
+    __device__ __forceinline__ Strip(const uint8_t *row, int v, int t, int threads, int part, int parts)
+        : p(reinterpret_cast<const typename E::T *>(row)), split(split_row<TYPE>(row, v)), t(t), threads(threads) {
+        const int each = (split.pieces + parts - 1) / parts;
+        first = part * each + t;
+        end = min((part + 1) * each, split.pieces);
+        ends = part == 0;
     }
-    const uint4 *const q = reinterpret_cast<const uint4 *>(p + s.head);
-    for (int at = begin + t; TOP ? __any_sync(0xffffffffu, at < end) : at < end; at += kFlight * threads) {
+    __device__ __forceinline__ int column(int unit) const { return unit == 0 ? 0 : split.head + (unit - 1) * E::kPer; }
+    __device__ __forceinline__ int units() const { return split.pieces + 2; }
+    // A unit's values, and how many there are.
+    __device__ __forceinline__ int values(int unit, float (&z)[E::kPer]) const {
+        if (unit > 0 && unit <= split.pieces) {
+            E::values(__ldg(reinterpret_cast<const uint4 *>(p + split.head) + unit - 1), z);
+            return E::kPer;
+        }
+        const int n = unit == 0 ? split.head : split.tail;
+#pragma unroll
+        for (int i = 0; i < E::kPer; ++i) z[i] = i < n ? E::value(p[column(unit) + i]) : minus_infinity();
+        return n;
+    }
+};
+
+// The largest of a strip's units, by its largest value.
+struct Best {
+    uint32_t order = 0u;
+    int unit = 0;
+    __device__ __forceinline__ void offer(uint32_t o, int u) {
+        if (o > order) order = o, unit = u;
+    }
+    __device__ __forceinline__ uint64_t key() const { return order ? key_of(order, unit) : 0u; }
+};
+
+template <int N>
+__device__ __forceinline__ float largest(const float (&z)[N]) {
+    float top = z[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, z[i]);
+    return top;
+}
+
+template <int TYPE, bool TOP>
+__device__ __forceinline__ void take_strip(const Strip<TYPE> &s, float k, Sums &sums, Best &best) {
+    using E = Elem<TYPE>;
+    auto take = [&](const float (&z)[E::kPer], int n, int unit) {
+        const float top = largest(z);
+        sums.raise(top, k);
+#pragma unroll
+        for (int i = 0; i < E::kPer; ++i)
+            if (i < n) sums.add(z[i], k);
+        if (TOP) best.offer(order_of(top), unit);
+    };
+    float z[E::kPer];
+    if (s.ends && s.t == 0 && s.split.head > 0) {
+        const int n = s.values(0, z);
+        take(z, n, 0);
+    }
+    const uint4 *const q = reinterpret_cast<const uint4 *>(s.p + s.split.head);
+    for (int at = s.first; at < s.end; at += kFlight * s.threads) {
         uint4 w[kFlight];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i)
-            if (at + i * threads < end) w[i] = __ldg(q + at + i * threads);
+            if (at + i * s.threads < s.end) w[i] = __ldg(q + at + i * s.threads);
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            const bool has = at + i * threads < end;
-            float z[E::kPer];
-            if (has) {
-                E::values(w[i], z);
-                float top = z[0];
-#pragma unroll
-                for (int j = 1; j < E::kPer; ++j) top = fmaxf(top, z[j]);
-                sums.raise(top, a.k);
-#pragma unroll
-                for (int j = 0; j < E::kPer; ++j) sums.add(z[j], a.k);
-            } else {
-#pragma unroll
-                for (int j = 0; j < E::kPer; ++j) z[j] = 0.f;
-            }
-            if (TOP) list.push(z, has ? E::kPer : 0, s.head + (at + i * threads) * E::kPer, a.top, lane);
+            if (at + i * s.threads >= s.end) continue;
+            E::values(w[i], z);
+            take(z, E::kPer, at + i * s.threads + 1);
         }
     }
+    if (s.ends && s.t == s.threads - 1 && s.split.tail > 0) {
+        const int n = s.values(s.units() - 1, z);
+        take(z, n, s.units() - 1);
+    }
+}
+
+// ---- the largest: candidates in shared memory
+struct Found {
+    uint64_t *keys;
+    int *count;
+    int room;
+    __device__ __forceinline__ void add(uint64_t key) const {
+        const int at = atomicAdd(count, 1);  // in any order: they are ranked
+        if (at < room) keys[at] = key;
+    }
+};
+// A unit's elements at or above the bound, if the unit is.
+template <int TYPE>
+__device__ __forceinline__ void offer_unit(const Strip<TYPE> &s, int unit, uint64_t bound, const Found &found) {
+    float z[Elem<TYPE>::kPer];
+    const int n = s.values(unit, z);
+    if (n == 0 || key_of(order_of(largest(z)), unit) < bound) return;
+#pragma unroll
+    for (int i = 0; i < Elem<TYPE>::kPer; ++i) {
+        const uint32_t o = order_of(z[i]);
+        if (i < n && o >= (uint32_t)(bound >> 32)) found.add(key_of(o, s.column(unit) + i));
+    }
+}
+// The strip of thread t again, by itself or (lanes = 32) by a warp.
+template <int TYPE>
+__device__ __forceinline__ void offer_strip(const Strip<TYPE> &s, int t, int lane, int lanes, uint64_t bound, const Found &found) {
+    if (s.ends && t == 0 && lane == 0 && s.split.head > 0) offer_unit(s, 0, bound, found);
+    for (int at = s.first - s.t + t + lane * s.threads; at < s.end; at += lanes * s.threads) offer_unit(s, at + 1, bound, found);
+    if (s.ends && t == s.threads - 1 && lane == 0 && s.split.tail > 0) offer_unit(s, s.units() - 1, bound, found);
+}
+// Where there was no room for all: the strip's largest element below `limit`.
+template <int TYPE>
+__device__ __forceinline__ uint64_t next_below(const Strip<TYPE> &s, uint64_t limit) {
+    uint64_t best = 0u;
+    auto look = [&](int unit) {
+        float z[Elem<TYPE>::kPer];
+        const int n = s.values(unit, z);
+        for (int i = 0; i < n; ++i) {
+            const uint64_t key = key_of(order_of(z[i]), s.column(unit) + i);
+            if (key < limit && key > best) best = key;
+        }
+    };
+    if (s.ends && s.t == 0) look(0);
+    for (int at = s.first; at < s.end; at += s.threads) look(at + 1);
+    if (s.ends && s.t == s.threads - 1) look(s.units() - 1);
+    return best;
+}
+__device__ __forceinline__ uint64_t warp_max(uint64_t key) {
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(key >> 32));
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(key >> 32) == hi ? (uint32_t)key : 0u);
+    return ((uint64_t)hi << 32) | lo;
+}
+// How many of n keys are larger.
+__device__ __forceinline__ int rank_of(uint64_t key, const uint64_t *keys, int n) {
+    int rank = 0;
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) rank += keys[i] > key ? 1 : 0;
+    return rank;
+}
+// The key of a rank among the warp's; 0 if there is none.
+__device__ __forceinline__ uint64_t ranked(uint64_t key, int rank, int which) {
+    const uint32_t has = __ballot_sync(0xffffffffu, key != 0u && rank == which);
+    return has ? __shfl_sync(0xffffffffu, key, __ffs(has) - 1) : 0u;
 }
 
 // l of a logit, from the row's sums.
@@ -231,10 +302,9 @@ __device__ __forceinline__ void finish_row(const LogprobArgs &a, int64_t row, co
     if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - x.w * kLn2 / x.s;
     if (a.lse) a.lse[row] = empty ? minus_infinity() : fmaf(x.m, a.inverse_t, log_s);
 }
-__device__ __forceinline__ void finish_top(const LogprobArgs &a, int64_t row, const Sums &x, uint64_t key, int lane) {
-    if (lane >= a.top) return;
-    a.top_logprob[row * a.top + lane] = logprob_of(value_of(key), x, logf(x.s), a.inverse_t);
-    a.top_index[row * a.top + lane] = (int)~(uint32_t)key;
+__device__ __forceinline__ void finish_top(const LogprobArgs &a, int64_t row, const Sums &x, uint64_t key, int rank) {
+    a.top_logprob[row * a.top + rank] = logprob_of(value_of((uint32_t)(key >> 32)), x, logf(x.s), a.inverse_t);
+    a.top_index[row * a.top + rank] = place_of(key);
 }
 template <int TYPE>
 __device__ __forceinline__ float token_logit(const LogprobArgs &a, const uint8_t *row, int token) {
@@ -242,22 +312,26 @@ __device__ __forceinline__ float token_logit(const LogprobArgs &a, const uint8_t
     return token >= 0 && token < a.v ? E::value(reinterpret_cast<const typename E::T *>(row)[token]) : 0.f;
 }
 
+// Room for a warp's candidates: where fewer lanes than K have a piece, all elements are.
+constexpr int kWarpRoom = 32 * 8 + 16;
 // Short rows: 2^lanes_log2 lanes to a row (a warp where the largest are wanted).
 template <int TYPE, bool TOP>
 __global__ void __launch_bounds__(kThreads) logprob_lanes_kernel(const __grid_constant__ LogprobArgs a) {
+    __shared__ uint64_t keys[TOP ? kWarps : 1][kWarpRoom];
+    __shared__ int counts[kWarps];
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
     const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> a.lanes_log2;
     const bool in = row < a.m;
     const uint8_t *const p = a.z + row * a.row_bytes;
     Sums sums;
-    TopList list;
+    Best best;
     sums.clear();
-    list.clear();
     pdl_trigger();
     pdl_wait();
     const int token = in && a.tokens ? a.tokens[row] : -1;
     const float z = in ? token_logit<TYPE>(a, p, token) : 0.f;
-    take_row<TYPE, TOP>(a, p, in, lane, lanes, 0, 1, sums, list);
+    const Strip<TYPE> strip(p, in ? a.v : 0, lane, lanes, 0, 1);
+    take_strip<TYPE, TOP>(strip, a.k, sums, best);
     for (int d = lanes >> 1; d > 0; d >>= 1) {
         Sums o;
         o.m = __shfl_xor_sync(0xffffffffu, sums.m, d);
@@ -267,47 +341,63 @@ __global__ void __launch_bounds__(kThreads) logprob_lanes_kernel(const __grid_co
     }
     if (!in) return;
     if (lane == 0) finish_row(a, row, sums, token, z);
-    if (TOP) finish_top(a, row, sums, list.mine, lane);
+    if constexpr (TOP) {
+        const int warp = threadIdx.x / 32;
+        const Found found{keys[warp], counts + warp, kWarpRoom};
+        if (lane == 0) counts[warp] = 0;
+        keys[warp][lane] = best.key();
+        __syncwarp();
+        const uint64_t bound = ranked(best.key(), rank_of(best.key(), keys[warp], 32), a.top - 1);
+        __syncwarp();
+        if (best.key() && best.key() >= bound) offer_strip(strip, lane, 0, 1, bound, found);
+        __syncwarp();
+        const int n = counts[warp];
+        if (n <= kWarpRoom) {
+            for (int i = lane; i < n; i += 32) {
+                const uint64_t key = keys[warp][i];
+                const int rank = rank_of(key, keys[warp], n);
+                if (rank < a.top) finish_top(a, row, sums, key, rank);
+            }
+        } else {
+            uint64_t limit = ~0ull;
+            for (int i = 0; i < a.top; ++i) {
+                limit = warp_max(next_below(strip, limit));
+                if (lane == 0) finish_top(a, row, sums, limit, i);
+            }
+        }
+    }
 }
 
-// What a block leaves for the join: its sums and its largest keys.
+// What a block leaves for the join: its sums and its largest keys, in order.
 struct Joined {
     Sums sums;
     uint64_t key[kMostTop];
 };
-
-// The largest `top` of up to 32 descending lists, key i in lane i: each round takes the
-// largest head.
-__device__ __forceinline__ uint64_t merge_lists(const uint64_t *mine, int top, int lane) {
-    uint64_t out = 0u, head = mine ? mine[0] : 0u;
-    int at = 0;
-    for (int i = 0; i < top; ++i) {
-        const uint64_t best = warp_max(head);
-        if (lane == i) out = best;
-        if (best && head == best) head = ++at < top ? mine[at] : 0u;  // keys are unlike: they hold the column
-    }
-    return out;
-}
+constexpr int kBlockRoom = 512;  // for candidates
 
 // A row to a block, or, in a cluster, to its blocks.
 template <int TYPE, bool TOP>
 __global__ void __launch_bounds__(kThreads) logprob_block_kernel(const __grid_constant__ LogprobArgs a, int cluster) {
-    __shared__ Joined warps[kWarps];
+    __shared__ Sums warps[kWarps];
     __shared__ Joined blocks[kMostCluster];
+    __shared__ Joined all;
+    __shared__ uint64_t keys[TOP ? kBlockRoom : 1];
+    __shared__ uint64_t bounds[kWarps][2];
+    __shared__ int count;
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     const int rank = cluster > 1 ? (int)cluster_rank() : 0;
     const int64_t row = blockIdx.x / (unsigned)cluster;
     const uint8_t *const p = a.z + row * a.row_bytes;
     Sums sums;
-    TopList list;
+    Best best;
     sums.clear();
-    list.clear();
     if (cluster > 1) cluster_arrive();  // it has started
     pdl_trigger();
     pdl_wait();
     const int token = a.tokens ? a.tokens[row] : -1;
     const float z = threadIdx.x == 0 ? token_logit<TYPE>(a, p, token) : 0.f;
-    take_row<TYPE, TOP>(a, p, true, threadIdx.x, kThreads, rank, cluster, sums, list);
+    const Strip<TYPE> strip(p, a.v, threadIdx.x, kThreads, rank, cluster);
+    take_strip<TYPE, TOP>(strip, a.k, sums, best);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
         Sums o;
@@ -316,35 +406,88 @@ __global__ void __launch_bounds__(kThreads) logprob_block_kernel(const __grid_co
         o.w = __shfl_xor_sync(0xffffffffu, sums.w, d);
         sums.join(o, a.k);
     }
-    if (lane == 0) warps[warp].sums = sums;
-    if (TOP && lane < a.top) warps[warp].key[lane] = list.mine;
+    if (lane == 0) warps[warp] = sums;
+    if constexpr (TOP) {
+        // K pieces at or above it: an eighth of them of every warp, or all of one
+        keys[threadIdx.x] = best.key();
+        if (threadIdx.x == 0) count = 0;
+        __syncwarp();
+        const int mine = rank_of(best.key(), keys + 32 * warp, 32);
+        const uint64_t few = ranked(best.key(), mine, (a.top + kWarps - 1) / kWarps - 1), many = ranked(best.key(), mine, a.top - 1);
+        if (lane == 0) bounds[warp][0] = few, bounds[warp][1] = many;
+    }
     __syncwarp();
     if (cluster > 1) cluster_wait();
     __syncthreads();
-    uint64_t key = 0u;
-    if (warp == 0) {
-        sums = warps[0].sums;
+    if (threadIdx.x == 0) {
+        sums = warps[0];
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) sums.join(warps[w].sums, a.k);
-        if (TOP) key = merge_lists(lane < kWarps ? warps[lane].key : nullptr, a.top, lane);
+        for (int w = 1; w < kWarps; ++w) sums.join(warps[w], a.k);
+        all.sums = sums;
     }
+    if constexpr (TOP) {
+        uint64_t few = bounds[0][0], bound = bounds[0][1];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+            few = min(few, bounds[w][0]);
+            bound = max(bound, bounds[w][1]);
+        }
+        bound = max(bound, few);
+        const Found found{keys, &count, kBlockRoom};
+        const uint32_t again = __ballot_sync(0xffffffffu, best.key() && best.key() >= bound);
+        int width = 4;  // lanes of a strip: a piece each, if it is short
+        while (width < 32 && width * kThreads < strip.end - strip.first + (int)threadIdx.x) width *= 2;
+        for (int i = lane / width; i < __popc(again); i += 32 / width)
+            offer_strip(strip, 32 * warp + (int)__fns(again, 0, i + 1), lane % width, width, bound, found);
+        __syncthreads();
+        const int n = count;
+        if (n <= kBlockRoom) {
+            for (int i = threadIdx.x; i < n; i += kThreads) {
+                const uint64_t key = keys[i];
+                const int at = rank_of(key, keys, n);
+                if (at < a.top) all.key[at] = key;
+            }
+        } else {  // many at or above every bound: one after another
+            uint64_t limit = ~0ull;
+            for (int i = 0; i < a.top; ++i) {
+                const uint64_t best_of = warp_max(next_below(strip, limit));
+                if (lane == 0) bounds[warp][i & 1] = best_of;
+                __syncthreads();
+                limit = bounds[0][i & 1];
+                for (int w = 1; w < kWarps; ++w) limit = max(limit, bounds[w][i & 1]);
+                if (threadIdx.x == 0) all.key[i] = limit;
+            }
+        }
+    }
+    __syncthreads();
     if (cluster > 1) {
         if (warp == 0) {
             const uint32_t to = cluster_addr(smem_u32(&blocks[rank]), 0);
-            if (lane < 3) store_cluster(to + 4 * lane, __float_as_uint(lane == 0 ? sums.m : lane == 1 ? sums.s : sums.w));
-            if (TOP && lane < a.top) store_cluster(to + (uint32_t)offsetof(Joined, key) + 8 * lane, key);
+            const Sums &x = all.sums;
+            if (lane < 3) store_cluster(to + 4 * lane, __float_as_uint(lane == 0 ? x.m : lane == 1 ? x.s : x.w));
+            if (TOP && lane < a.top) store_cluster(to + (uint32_t)offsetof(Joined, key) + 8 * lane, all.key[lane]);
         }
         __syncwarp();
         cluster_sync();
         if (rank != 0) return;
-        if (warp == 0) {
+        if (threadIdx.x == 0) {
             sums = blocks[0].sums;
             for (int b = 1; b < cluster; ++b) sums.join(blocks[b].sums, a.k);
-            if (TOP) key = merge_lists(lane < cluster ? blocks[lane].key : nullptr, a.top, lane);
+            all.sums = sums;
         }
+        if constexpr (TOP) {
+            const int n = cluster * a.top;
+            const int b = threadIdx.x / a.top;
+            uint64_t key = 0u;
+            if ((int)threadIdx.x < n) key = keys[threadIdx.x] = blocks[b].key[threadIdx.x - b * a.top];
+            __syncthreads();
+            const int at = (int)threadIdx.x < n ? rank_of(key, keys, n) : n;
+            if (at < a.top) all.key[at] = key;
+        }
+        __syncthreads();
     }
-    if (threadIdx.x == 0) finish_row(a, row, sums, token, z);
-    if (TOP && warp == 0) finish_top(a, row, sums, key, lane);
+    if (threadIdx.x == 0) finish_row(a, row, all.sums, token, z);
+    if (TOP && (int)threadIdx.x < a.top) finish_top(a, row, all.sums, all.key[threadIdx.x], threadIdx.x);
 }
 
 // ---------------------------------------------------------------- gradient

@@ -429,12 +429,19 @@ _PACK_GATED = struct.Struct("<6i" + 6 * _MATRIX + "2Q")
 _PACK_GATED_GRAD = struct.Struct("<6i" + 10 * _MATRIX + "2Q")
 _ABSENT = (0, 0, 0, 0)
 _TYPES = {}  # torch dtype -> emtk_type
+_F32 = _I32 = None  # torch's float32 and int32, once torch is here
+
+
+def _load_types() -> None:
+    global _F32, _I32
+    import torch
+    _TYPES.update({torch.bfloat16: EMTK_TYPE_BF16, torch.float16: EMTK_TYPE_F16, torch.float32: EMTK_TYPE_F32})
+    _F32, _I32 = torch.float32, torch.int32
 
 
 def _type_of(t, what: str, f32: bool = False) -> int:
     if not _TYPES:
-        import torch
-        _TYPES.update({torch.bfloat16: EMTK_TYPE_BF16, torch.float16: EMTK_TYPE_F16, torch.float32: EMTK_TYPE_F32})
+        _load_types()
     v = _TYPES.get(t.dtype, -1)
     if v < 0 or (v == EMTK_TYPE_F32 and not f32):
         raise ValueError(f"{what}: dtype {t.dtype} is not supported")
@@ -445,15 +452,13 @@ def _mat(on, t, rows: int, cols: int, dtype, what: str) -> tuple:
     """(d, ld, d_scale, ld_scale) of a [rows][cols] tensor of dtype on CUDA device `on`; absent for None."""
     if t is None:
         return _ABSENT
-    if t.dtype is dtype and t.get_device() == on:
-        shape = t.shape
-        if len(shape) == 2 and shape[0] == rows and shape[1] == cols:
-            ld, unit = t.stride()
-            if unit == 1 and ld >= cols:
-                return (t.data_ptr(), ld, 0, 0)
-            if (unit == 1 or cols <= 1) and (ld >= cols or rows <= 1):
-                return (t.data_ptr(), max(ld, cols), 0, 0)  # one row or column: its stride says nothing
-            raise ValueError(f"{what}: strides {t.stride()}: a row's elements must be neighbours and rows apart")
+    if t.dtype is dtype and t.shape == (rows, cols) and t.get_device() == on:
+        ld, unit = t.stride()
+        if unit == 1 and ld >= cols:
+            return (t.data_ptr(), ld, 0, 0)
+        if (unit == 1 or cols <= 1) and (ld >= cols or rows <= 1):
+            return (t.data_ptr(), max(ld, cols), 0, 0)  # one row or column: its stride says nothing
+        raise ValueError(f"{what}: strides {t.stride()}: a row's elements must be neighbours and rows apart")
     raise ValueError(f"{what}: expected a tensor {(rows, cols)} of {dtype} on CUDA device {on}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
@@ -470,7 +475,7 @@ def _mat8(on, t, rows: int, cols: int, dtype, what: str) -> tuple:
 def _vec(on, t, n: int, what: str, f32: bool = False) -> int:
     if t is None:
         return 0
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.get_device() != on:
+    if t.shape != (n,) or t.get_device() != on or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous vector of {n} on CUDA device {on}, got {tuple(t.shape)} on {t.device}")
     if f32 and _type_of(t, what, True) != EMTK_TYPE_F32:
         raise ValueError(f"{what}: dtype {t.dtype}, expected float32")
@@ -663,24 +668,28 @@ def _drop(on, d) -> tuple:
     return (seed & _WORD, offset & _WORD, t or 0, p)
 
 
-def _norm(on, v, n: int, dtype, what: str) -> tuple:
+def _norm(on, v, n: int, what: str) -> tuple:
     """The fields of emtk_norm; absent for None."""
     if v is None:
         return _NO_NORM
     kind, weight, bias, eps = v
-    if kind not in NORMS:
-        raise ValueError(f"{what}: {kind!r} is none of {tuple(NORMS)}")
-    one = weight if weight is not None else bias
-    if weight is not None and bias is not None and weight.dtype is not bias.dtype:
+    code = NORMS.get(kind, 0)
+    if not code:
+        raise ValueError(f"{what}: {kind!r} is none of {tuple(NORMS)[1:]}")
+    if bias is None:
+        if weight is None:
+            return (code, 0, eps, 0, 0)
+        return (code, _type_of(weight, what, True), eps, _vec(on, weight, n, what), 0)
+    if weight is not None and weight.dtype is not bias.dtype:
         raise ValueError(f"{what}: its bias' dtype must be its weight's")
-    return (NORMS[kind], 0 if one is None else _type_of(one, what, True), eps, _vec(on, weight, n, what), _vec(on, bias, n, what))
+    return (code, _type_of(bias, what, True), eps, _vec(on, weight, n, what), _vec(on, bias, n, what))
 
 
 def _whole(on, t, shape: tuple, dtype, what: str) -> int:
     """A contiguous tensor of a shape and dtype on CUDA device `on`; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.get_device() != on:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != on or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous tensor {shape} of {dtype} on CUDA device {on}, got {tuple(t.shape)} of "
                          f"{t.dtype} on {t.device}")
     return t.data_ptr()
@@ -717,8 +726,8 @@ def emtk_residual_norm(nn, residual=None, block=None, y=None, h=None, post: Norm
     (m, n), dt = like.shape, like.dtype
     on = _device_of(nn, like)
     g, every = _gate(on, gate, m, n, gate_every, dt, "gate")
-    args = _PACK_SEAM.pack(m, n, _type_of(like, "block" if like is block else "residual"), every, scale, *_norm(on, post, n, dt, "post"),
-                           *_norm(on, pre, n, dt, "pre"), *_drop(on, drop), *_mat(on, residual, m, n, dt, "residual"),
+    args = _PACK_SEAM.pack(m, n, _type_of(like, "block" if like is block else "residual"), every, scale, *_norm(on, post, n, "post"),
+                           *_norm(on, pre, n, "pre"), *_drop(on, drop), *_mat(on, residual, m, n, dt, "residual"),
                            *_mat(on, block, m, n, dt, "block"), *g, *_mat(on, y, m, n, dt, "y"), *_mat(on, h, m, n, dt, "h"))
     _check(load_library().emtk_residual_norm(nn, args, _current(like, stream)), "emtk_residual_norm")
 
@@ -733,16 +742,15 @@ def emtk_residual_norm_backward(nn, dy=None, dh=None, y=None, block=None, d_resi
     if like is None:
         raise ValueError("dy, dh: one must be given")
     (m, n), dt = like.shape, like.dtype
-    on = _device_of(nn, like)
-    import torch
+    on, code = _device_of(nn, like), _type_of(like, "dh" if like is dh else "dy")
     g, every = _gate(on, gate, m, n, gate_every, dt, "gate")
-    dg, _ = _gate(on, d_gate, m, n, gate_every, torch.float32, "d_gate")
-    args = _PACK_SEAM_GRAD.pack(m, n, _type_of(like, "dh" if like is dh else "dy"), every, scale, *_norm(on, post, n, dt, "post"),
-                                *_norm(on, pre, n, dt, "pre"), *_drop(on, drop), *_mat(on, dy, m, n, dt, "dy"),
+    dg, _ = _gate(on, d_gate, m, n, gate_every, _F32, "d_gate")
+    args = _PACK_SEAM_GRAD.pack(m, n, code, every, scale, *_norm(on, post, n, "post"),
+                                *_norm(on, pre, n, "pre"), *_drop(on, drop), *_mat(on, dy, m, n, dt, "dy"),
                                 *_mat(on, dh, m, n, dt, "dh"), *_mat(on, y, m, n, dt, "y"), *_mat(on, block, m, n, dt, "block"), *g,
                                 *_mat(on, d_residual, m, n, dt, "d_residual"), *_mat(on, d_block, m, n, dt, "d_block"), *dg,
-                                *(_vec(on, t, n, what, True) for t, what in ((dw_pre, "dw_pre"), (db_pre, "db_pre"),
-                                                                            (dw_post, "dw_post"), (db_post, "db_post"))))
+                                _vec(on, dw_pre, n, "dw_pre", True), _vec(on, db_pre, n, "db_pre", True),
+                                _vec(on, dw_post, n, "dw_post", True), _vec(on, db_post, n, "db_post", True))
     _check(load_library().emtk_residual_norm_backward(nn, args, _current(like, stream)), "emtk_residual_norm_backward")
 
 
@@ -751,15 +759,13 @@ def emtk_logprobs(nn, logits, tokens=None, logprob=None, entropy=None, lse=None,
     """Of logits [m][v] (bf16, fp16 or float32), float32 and contiguous, each optional: logprob [m] of tokens [m] (int32;
     negative: none), entropy [m], lse [m] for the backward call, top_logprob [m][top] and top_index [m][top] (int32) of
     the largest `top` <= 32."""
-    import torch
-    (m, v), on = logits.shape, _device_of(nn, logits)
-    f32, i32 = torch.float32, torch.int32
+    (m, v), on, code = logits.shape, _device_of(nn, logits), _type_of(logits, "logits", True)
     some = top_logprob if top_logprob is not None else top_index
     top = 0 if some is None else some.shape[1]
-    args = _PACK_LOGPROBS.pack(m, v, _type_of(logits, "logits", True), top, temperature, *_mat(on, logits, m, v, logits.dtype, "logits"),
-                               _whole(on, tokens, (m,), i32, "tokens"), _whole(on, logprob, (m,), f32, "logprob"),
-                               _whole(on, entropy, (m,), f32, "entropy"), _whole(on, lse, (m,), f32, "lse"),
-                               _whole(on, top_logprob, (m, top), f32, "top_logprob"), _whole(on, top_index, (m, top), i32, "top_index"))
+    args = _PACK_LOGPROBS.pack(m, v, code, top, temperature, *_mat(on, logits, m, v, logits.dtype, "logits"),
+                               _whole(on, tokens, (m,), _I32, "tokens"), _whole(on, logprob, (m,), _F32, "logprob"),
+                               _whole(on, entropy, (m,), _F32, "entropy"), _whole(on, lse, (m,), _F32, "lse"),
+                               _whole(on, top_logprob, (m, top), _F32, "top_logprob"), _whole(on, top_index, (m, top), _I32, "top_index"))
     _check(load_library().emtk_logprobs(nn, args, _current(logits, stream)), "emtk_logprobs")
 
 
@@ -767,13 +773,11 @@ def emtk_logprobs_backward(nn, logits, lse, d_logits, tokens=None, d_logprob=Non
                            temperature: float = 1.0, stream=None) -> None:
     """The gradient of logits, of their dtype, from d_logprob [m] (with the tokens) and d_entropy [m] (with the entropy
     that emtk_logprobs wrote), each optional, and its lse.  d_logits may be logits."""
-    import torch
-    (m, v), dt, on = logits.shape, logits.dtype, _device_of(nn, logits)
-    f32 = torch.float32
-    args = _PACK_LOGPROBS_GRAD.pack(m, v, _type_of(logits, "logits", True), temperature, *_mat(on, logits, m, v, dt, "logits"),
-                                    *_mat(on, d_logits, m, v, dt, "d_logits"), _whole(on, tokens, (m,), torch.int32, "tokens"),
-                                    _whole(on, lse, (m,), f32, "lse"), _whole(on, entropy, (m,), f32, "entropy"),
-                                    _whole(on, d_logprob, (m,), f32, "d_logprob"), _whole(on, d_entropy, (m,), f32, "d_entropy"))
+    (m, v), dt, on, code = logits.shape, logits.dtype, _device_of(nn, logits), _type_of(logits, "logits", True)
+    args = _PACK_LOGPROBS_GRAD.pack(m, v, code, temperature, *_mat(on, logits, m, v, dt, "logits"),
+                                    *_mat(on, d_logits, m, v, dt, "d_logits"), _whole(on, tokens, (m,), _I32, "tokens"),
+                                    _whole(on, lse, (m,), _F32, "lse"), _whole(on, entropy, (m,), _F32, "entropy"),
+                                    _whole(on, d_logprob, (m,), _F32, "d_logprob"), _whole(on, d_entropy, (m,), _F32, "d_entropy"))
     _check(load_library().emtk_logprobs_backward(nn, args, _current(logits, stream)), "emtk_logprobs_backward")
 
 
@@ -789,14 +793,12 @@ def emtk_recurrence(nn, f, x, y, o=None, act: str = "none", seqs: int = 1, offse
     of bf16 or fp16.  Sequences lie one after another: offsets [seqs + 1] (int32) says where, or each has rows / seqs
     rows.  state and last [seqs][n] float32: the states before and after (last may be state); states
     (emtk_recurrence_states) is for the backward call."""
-    import torch
-    (rows, n), dt, on = f.shape, f.dtype, _device_of(nn, f)
-    f32, seqs = torch.float32, int(seqs)
-    args = _PACK_RECURRENCE.pack(rows, n, seqs, _act_code(act), _type_of(f, "f"), *_mat(on, f, rows, n, dt, "f"),
+    (rows, n), dt, on, code, seqs = f.shape, f.dtype, _device_of(nn, f), _type_of(f, "f"), int(seqs)
+    args = _PACK_RECURRENCE.pack(rows, n, seqs, _act_code(act), code, *_mat(on, f, rows, n, dt, "f"),
                                  *_mat(on, x, rows, n, dt, "x"), *_mat(on, o, rows, n, dt, "o"), *_mat(on, y, rows, n, dt, "y"),
-                                 _whole(on, offsets, (seqs + 1,), torch.int32, "offsets"), _whole(on, state, (seqs, n), f32, "state"),
-                                 _whole(on, last, (seqs, n), f32, "last"),
-                                 _whole(on, states, (rows // EMTK_RECURRENCE_STEP + seqs, n), f32, "states"))
+                                 _whole(on, offsets, (seqs + 1,), _I32, "offsets"), _whole(on, state, (seqs, n), _F32, "state"),
+                                 _whole(on, last, (seqs, n), _F32, "last"),
+                                 _whole(on, states, (rows // EMTK_RECURRENCE_STEP + seqs, n), _F32, "states"))
     _check(load_library().emtk_recurrence(nn, args, _current(f, stream)), "emtk_recurrence")
 
 
@@ -804,15 +806,13 @@ def emtk_recurrence_backward(nn, dy, f, x, states, df=None, dx=None, o=None, act
                              d_last=None, d_o=None, d_state=None, stream=None) -> None:
     """Gradients of emtk_recurrence from dy and d_last [seqs][n] float32 (None: 0), with the states that it kept: df, dx,
     d_o [rows][n] and d_state [seqs][n] float32, each optional."""
-    import torch
-    (rows, n), dt, on = f.shape, f.dtype, _device_of(nn, f)
-    f32, seqs = torch.float32, int(seqs)
-    args = _PACK_RECURRENCE_GRAD.pack(rows, n, seqs, _act_code(act), _type_of(f, "f"), *_mat(on, dy, rows, n, dt, "dy"),
+    (rows, n), dt, on, code, seqs = f.shape, f.dtype, _device_of(nn, f), _type_of(f, "f"), int(seqs)
+    args = _PACK_RECURRENCE_GRAD.pack(rows, n, seqs, _act_code(act), code, *_mat(on, dy, rows, n, dt, "dy"),
                                       *_mat(on, f, rows, n, dt, "f"), *_mat(on, x, rows, n, dt, "x"), *_mat(on, o, rows, n, dt, "o"),
                                       *_mat(on, df, rows, n, dt, "df"), *_mat(on, dx, rows, n, dt, "dx"),
-                                      *_mat(on, d_o, rows, n, dt, "d_o"), _whole(on, offsets, (seqs + 1,), torch.int32, "offsets"),
-                                      _whole(on, states, (rows // EMTK_RECURRENCE_STEP + seqs, n), f32, "states"),
-                                      _whole(on, d_last, (seqs, n), f32, "d_last"), _whole(on, d_state, (seqs, n), f32, "d_state"))
+                                      *_mat(on, d_o, rows, n, dt, "d_o"), _whole(on, offsets, (seqs + 1,), _I32, "offsets"),
+                                      _whole(on, states, (rows // EMTK_RECURRENCE_STEP + seqs, n), _F32, "states"),
+                                      _whole(on, d_last, (seqs, n), _F32, "d_last"), _whole(on, d_state, (seqs, n), _F32, "d_state"))
     _check(load_library().emtk_recurrence_backward(nn, args, _current(f, stream)), "emtk_recurrence_backward")
 
 
