@@ -18,28 +18,35 @@ struct DropoutArgs {
     Rows16 x, y;
     Drop drop;
     int m, n, lanes_log2;
-    int runs;         // of a row
-    int64_t all;      // runs of the matrix
+    int runs;                        // of a row
+    int64_t step_rows;               // from a worker's run to its next, without a division
+    int step_runs;
 };
 
 template <bool F16, bool ANY>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant__ DropoutArgs a) {
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int64_t workers = (int64_t)gridDim.x * (kThreads >> a.lanes_log2);
-    int64_t run = (int64_t)blockIdx.x * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+    const int64_t first = (int64_t)blockIdx.x * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+    int64_t row = first / a.runs;
+    int run = (int)(first - row * a.runs);
     pdl_trigger();
     pdl_wait();
     const uint64_t offset = drop_offset(a.drop);
-    for (; __any_sync(0xffffffffu, run < a.all); run += kFlight * workers) {
+    while (__any_sync(0xffffffffu, row < a.m)) {
         Piece16<ANY> w[kFlight];
         int r[kFlight], c[kFlight];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            const int64_t at = run + i * workers;
-            r[i] = at < a.all ? (int)(at / a.runs) : -1;
-            c[i] = (int)(at - (int64_t)r[i] * a.runs) * (kPiece << a.lanes_log2);
+            r[i] = row < a.m ? (int)row : -1;
+            c[i] = run * (kPiece << a.lanes_log2);
             w[i].clear();
             if (r[i] >= 0 && c[i] + kPiece * lane < a.n) w[i].load(a.x, r[i], c[i] + kPiece * lane, a.m, a.n);
+            row += a.step_rows;
+            run += a.step_runs;
+            if (run >= a.runs) {
+                run -= a.runs;
+                ++row;
+            }
         }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
@@ -68,9 +75,10 @@ cudaError_t launch_dropout(emtk_type type, int m, int n, const emtk_matrix &x, c
     while (a.lanes_log2 > 2 && (kPiece << (a.lanes_log2 - 1)) >= n) --a.lanes_log2;
     const int64_t cols = kPiece << a.lanes_log2;
     a.runs = (int)((n + cols - 1) / cols);
-    a.all = (int64_t)m * a.runs;
-    const int64_t per_block = kThreads >> a.lanes_log2;
-    const unsigned blocks = (unsigned)std::min<int64_t>((a.all + per_block - 1) / per_block, 8ll * sms);
+    const int64_t all = (int64_t)m * a.runs, per_block = kThreads >> a.lanes_log2;
+    const unsigned blocks = (unsigned)std::min<int64_t>((all + per_block - 1) / per_block, 8ll * sms);
+    a.step_rows = blocks * per_block / a.runs;
+    a.step_runs = (int)(blocks * per_block % a.runs);
     const bool any = !on_grid(x, m) || !on_grid(y, m), f16 = type == EMTK_TYPE_F16;
     return launch_pdl(any ? (f16 ? dropout_kernel<true, true> : dropout_kernel<false, true>)
                           : (f16 ? dropout_kernel<true, false> : dropout_kernel<false, false>),

@@ -51,6 +51,18 @@ struct Elem {
             v[2 * i + 1] = TYPE == EMTK_TYPE_F16 ? from16<true>(w[i] >> 16) : __uint_as_float(w[i] & 0xffff0000u);
         }
     }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        uint32_t r;
+        if (TYPE == EMTK_TYPE_F16)
+            asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else
+            asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ float largest(const uint4 &q) {  // NaN only if all are
+        const float2 v = values_of<TYPE == EMTK_TYPE_F16>(larger(larger(q.x, q.y), larger(q.z, q.w)));
+        return fmaxf(v.x, v.y);
+    }
     static __device__ __forceinline__ uint16_t stored(float v) { return (uint16_t)to16<TYPE == EMTK_TYPE_F16>(v); }
     static __device__ __forceinline__ uint4 stored(const float *v) {
         constexpr bool F16 = TYPE == EMTK_TYPE_F16;
@@ -64,6 +76,9 @@ struct Elem<EMTK_TYPE_F32> {
     static __device__ __forceinline__ float value(float x) { return x; }
     static __device__ __forceinline__ void values(const uint4 &q, float *v) {
         v[0] = __uint_as_float(q.x), v[1] = __uint_as_float(q.y), v[2] = __uint_as_float(q.z), v[3] = __uint_as_float(q.w);
+    }
+    static __device__ __forceinline__ float largest(const uint4 &q) {
+        return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
     }
     static __device__ __forceinline__ float stored(float v) { return v; }
     static __device__ __forceinline__ uint4 stored(const float *v) {
@@ -101,12 +116,6 @@ struct Sums {
         s *= f;
         m = to;
     }
-    __device__ __forceinline__ void add(float z, float k) {
-        const float base = m == minus_infinity() ? 0.f : m;
-        const float d = (z - base) * k, e = exp2_f(d);
-        s += e;
-        w = fmaf(e, fmaxf(d, kFar), w);
-    }
     __device__ __forceinline__ void join(Sums o, float k) {
         const float top = fmaxf(m, o.m);
         raise(top, k);
@@ -114,6 +123,33 @@ struct Sums {
         s += o.s;
         w += o.w;
     }
+};
+// A thread's: even and odd elements' sums apart, so that one instruction adds two.
+struct Sums2 {
+    float m;
+    float2 s, w;
+    __device__ __forceinline__ void clear() { m = minus_infinity(), s = w = both(0.f); }
+    __device__ __forceinline__ void raise(float to, float k) {
+        if (!(to > m)) return;
+        const float d = m == minus_infinity() ? 0.f : fmaxf((m - to) * k, kFar);
+        const float f = exp2_f(d);
+        w = fma2(both(d), s, w) * both(f);
+        s = s * both(f);
+        m = to;
+    }
+    // N values, none above the maximum, absent ones -infinity.
+    template <int N>
+    __device__ __forceinline__ void add(const float (&z)[N], float k) {
+        const float base = m == minus_infinity() ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const float2 d = (make_float2(z[i], z[i + 1]) - both(base)) * both(k);
+            const float2 e = make_float2(exp2_f(d.x), exp2_f(d.y));
+            s = s + e;
+            w = fma2(e, make_float2(fmaxf(d.x, kFar), fmaxf(d.y, kFar)), w);  // of -infinity: 0
+        }
+    }
+    __device__ __forceinline__ Sums all() const { return {m, s.x + s.y, w.x + w.y}; }
 };
 
 // Order of logits; NaN is the least.  Never 0.
@@ -190,20 +226,19 @@ __device__ __forceinline__ float largest(const float (&z)[N]) {
 }
 
 template <int TYPE, bool TOP>
-__device__ __forceinline__ void take_strip(const Strip<TYPE> &s, float k, Sums &sums, Best &best) {
+__device__ __forceinline__ Sums take_strip(const Strip<TYPE> &s, float k, Best &best) {
     using E = Elem<TYPE>;
-    auto take = [&](const float (&z)[E::kPer], int n, int unit) {
-        const float top = largest(z);
+    Sums2 sums;
+    sums.clear();
+    auto take = [&](const float (&z)[E::kPer], float top, int unit) {
         sums.raise(top, k);
-#pragma unroll
-        for (int i = 0; i < E::kPer; ++i)
-            if (i < n) sums.add(z[i], k);
+        sums.add(z, k);
         if (TOP) best.offer(order_of(top), unit);
     };
     float z[E::kPer];
     if (s.ends && s.t == 0 && s.split.head > 0) {
-        const int n = s.values(0, z);
-        take(z, n, 0);
+        s.values(0, z);
+        take(z, largest(z), 0);
     }
     const uint4 *const q = reinterpret_cast<const uint4 *>(s.p + s.split.head);
     for (int at = s.first; at < s.end; at += kFlight * s.threads) {
@@ -215,13 +250,14 @@ __device__ __forceinline__ void take_strip(const Strip<TYPE> &s, float k, Sums &
         for (int i = 0; i < kFlight; ++i) {
             if (at + i * s.threads >= s.end) continue;
             E::values(w[i], z);
-            take(z, E::kPer, at + i * s.threads + 1);
+            take(z, E::largest(w[i]), at + i * s.threads + 1);
         }
     }
     if (s.ends && s.t == s.threads - 1 && s.split.tail > 0) {
-        const int n = s.values(s.units() - 1, z);
-        take(z, n, s.units() - 1);
+        s.values(s.units() - 1, z);
+        take(z, largest(z), s.units() - 1);
     }
+    return sums.all();
 }
 
 // ---- the largest: candidates in shared memory
@@ -323,15 +359,13 @@ __global__ void __launch_bounds__(kThreads) logprob_lanes_kernel(const __grid_co
     const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> a.lanes_log2;
     const bool in = row < a.m;
     const uint8_t *const p = a.z + row * a.row_bytes;
-    Sums sums;
     Best best;
-    sums.clear();
     pdl_trigger();
     pdl_wait();
     const int token = in && a.tokens ? a.tokens[row] : -1;
     const float z = in ? token_logit<TYPE>(a, p, token) : 0.f;
     const Strip<TYPE> strip(p, in ? a.v : 0, lane, lanes, 0, 1);
-    take_strip<TYPE, TOP>(strip, a.k, sums, best);
+    Sums sums = take_strip<TYPE, TOP>(strip, a.k, best);
     for (int d = lanes >> 1; d > 0; d >>= 1) {
         Sums o;
         o.m = __shfl_xor_sync(0xffffffffu, sums.m, d);
@@ -388,16 +422,14 @@ __global__ void __launch_bounds__(kThreads) logprob_block_kernel(const __grid_co
     const int rank = cluster > 1 ? (int)cluster_rank() : 0;
     const int64_t row = blockIdx.x / (unsigned)cluster;
     const uint8_t *const p = a.z + row * a.row_bytes;
-    Sums sums;
     Best best;
-    sums.clear();
     if (cluster > 1) cluster_arrive();  // it has started
     pdl_trigger();
     pdl_wait();
     const int token = a.tokens ? a.tokens[row] : -1;
     const float z = threadIdx.x == 0 ? token_logit<TYPE>(a, p, token) : 0.f;
     const Strip<TYPE> strip(p, a.v, threadIdx.x, kThreads, rank, cluster);
-    take_strip<TYPE, TOP>(strip, a.k, sums, best);
+    Sums sums = take_strip<TYPE, TOP>(strip, a.k, best);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
         Sums o;
