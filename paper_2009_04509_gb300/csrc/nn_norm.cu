@@ -46,7 +46,7 @@ NormArgs norm_args(const emtk_norm &n) {
 // where a row has more than kGroupThreads).
 struct Reduction {
     float *buffer;  // [2][4 * kMaxWarps] of the block, from the group's place on
-    int tid, warps, turn;
+    int tid, warps, turn, width;  // width: lanes of a row, if it has less than a warp
     bool grouped;
     __device__ __forceinline__ void sync() const {
         if (grouped)
@@ -71,7 +71,8 @@ __device__ __forceinline__ void row_sum(float (&v)[K], Reduction &b) {
         x = (odd ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 1);
     }
 #pragma unroll
-    for (int d = K; d < 32; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
+    for (int d = K; d < 32; d *= 2)
+        if (d < b.width) x += __shfl_xor_sync(0xffffffffu, x, d);
     if (b.warps > 1) {
         float *const buffer = b.buffer + b.turn * 4 * kMaxWarps;
         if (lane < K) buffer[b.tid / 32 * K + lane] = x;
@@ -83,7 +84,7 @@ __device__ __forceinline__ void row_sum(float (&v)[K], Reduction &b) {
         b.turn ^= 1;
     }
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = K == 1 ? x : __shfl_sync(0xffffffffu, x, k);
+    for (int k = 0; k < K; ++k) v[k] = K == 1 ? x : __shfl_sync(0xffffffffu, x, k, b.width);
 }
 
 __device__ __forceinline__ float sum_of(const Eight &e) {
@@ -140,24 +141,27 @@ struct Waits {  // of the kernels' bounded waits
 
 // How a group of threads has its row.
 //   kDirect   one of a block's, two pieces a thread, on the 16-byte grid and of whole pieces
-//   kSmall    several to a block, a piece a thread, likewise
-//   kSmallAny several to a block, a piece a thread, anywhere
+//   kDirectAny the same, anywhere
+//   kSmall    several to a block (and to a warp, where they are short), a piece a thread, on the
+//             grid and of whole pieces
+//   kSmallAny the same, anywhere
 //   kBulk     a block goes from row to row, two pieces a thread, anywhere: a row of each matrix is
 //             copied to shared memory, a row or two ahead, in the aligned 16-byte pieces
 //             that it lies in, and shifted into place from there: many rows are on their
 //             way without a register.  Rows whose outer pieces would reach beyond the
 //             matrix are copied by elements.
 // A thread's pieces are tid and tid + threads; but for the last of a thread, they are whole.
-enum Kind : int { kDirect, kSmall, kSmallAny, kBulk };
+enum Kind : int { kDirect, kDirectAny, kSmall, kSmallAny, kBulk };
 
 template <bool F16, Kind KIND, int COUNT>  // COUNT: matrices
 struct RowIo {
-    static constexpr int C = KIND == kDirect || KIND == kBulk ? 2 : 1;
-    static constexpr bool ODD = KIND == kSmallAny || KIND == kBulk;
+    static constexpr int C = KIND == kSmall || KIND == kSmallAny ? 1 : 2;
+    static constexpr bool ODD = KIND != kDirect && KIND != kSmall;
     const Inputs &a;
     int64_t row;
     int tid, threads;
     bool last;  // the last piece is this thread's, or beyond the row
+    bool live;  // false: a row that is not there, in a warp of rows that are
     // kBulk
     uint8_t *stages;
     uint64_t *full;
@@ -172,6 +176,8 @@ struct RowIo {
         threads = blockDim.x;
         row = KIND == kSmall || KIND == kSmallAny ? (int64_t)blockIdx.x * blockDim.y + threadIdx.y : (int64_t)blockIdx.x;
         last = column(C - 1) + kPiece > a.n;
+        live = row < a.m;
+        if (C == 1 && threads < 32) row = min(row, (int64_t)a.m - 1);  // its warp's exchanges need all lanes
         if (KIND == kBulk) {
             if (tid == 0) {
                 for (int i = 0; i < kMostStages; ++i) mbar_init(smem_u32(full + i), 1);
@@ -276,15 +282,21 @@ struct RowIo {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[C - 1][i] &= (2 * i < left ? 0xffffu : 0u) | (2 * i + 1 < left ? 0xffff0000u : 0u);
             }
-        } else if constexpr (KIND == kSmallAny) {
-            if (tid * kPiece >= a.n) return;
-            Piece16<true> x;
-            x.load(a.in[which], row, tid * kPiece, a.m, a.n);
-            if (x.halves) {
-                shift_words(x.x, x.halves, w[0]);
-            } else {
+        } else if constexpr (ODD) {
+            Piece16<true> x[C];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[0][i] = x.x[i];
+            for (int k = 0; k < C; ++k) {
+                x[k].clear();
+                if (column(k) < a.n) x[k].load(a.in[which], row, column(k), a.m, a.n);
+            }
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                if (x[k].halves) {
+                    shift_words(x[k].x, x[k].halves, w[k]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[k][i] = x[k].x[i];
+                }
             }
         } else {
             const uint4 *const p = reinterpret_cast<const uint4 *>(a.in[which].row(row)) + tid;
@@ -304,10 +316,13 @@ struct RowIo {
     __device__ __forceinline__ void store(const Rows16 &to, int k, const Eight &e) const {
         uint32_t w[4];
         words8<F16>(e, w);
-        if constexpr (ODD) {
+        if constexpr (C == 1 && ODD) {
+            const int lanes = min(32, threads), run = tid / lanes * lanes * kPiece;
+            store_run<true>(to.row(row) + run, live ? max(0, min(a.n - run, lanes * kPiece)) : 0, w, lanes, tid & (lanes - 1));
+        } else if constexpr (ODD) {
             const int run = (k * threads + (tid & ~31)) * kPiece;
             store_run<true>(to.row(row) + run, max(0, min(a.n - run, 32 * kPiece)), w, 32, tid & 31);
-        } else if (k < C - 1 || !last) {
+        } else if ((k < C - 1 || !last) && live) {
             reinterpret_cast<uint4 *>(to.row(row))[k * threads + tid] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
@@ -355,10 +370,11 @@ __global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_con
     constexpr int C = Io::C;
     Io io(a.in, rows, full, &abort_flag, waits);
     constexpr bool kGrouped = KIND == kSmall || KIND == kSmallAny;
-    Reduction reduction{buffer + (kGrouped ? threadIdx.y * (io.threads / 32) * 4 : 0), io.tid, io.threads / 32, 0, kGrouped};
+    Reduction reduction{buffer + (kGrouped ? threadIdx.y * (io.threads / 32) * 4 : 0), io.tid, io.threads / 32, 0,
+                        kGrouped ? min(32, io.threads) : 32, kGrouped};
     pdl_trigger();
     pdl_wait();
-    if (io.row >= a.in.m) return;
+    if (io.row >= a.in.m) return;  // (a whole warp)
     io.begin();
     const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0u;
     do {
@@ -422,13 +438,14 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) residual_norm_grad_kernel(con
     constexpr int C = Io::C;
     Io io(a.in, rows, full, &abort_flag, waits);
     constexpr bool kGrouped = KIND == kSmall || KIND == kSmallAny;
-    Reduction reduction{buffer + (kGrouped ? threadIdx.y * (io.threads / 32) * 4 : 0), io.tid, io.threads / 32, 0, kGrouped};
+    Reduction reduction{buffer + (kGrouped ? threadIdx.y * (io.threads / 32) * 4 : 0), io.tid, io.threads / 32, 0,
+                        kGrouped ? min(32, io.threads) : 32, kGrouped};
     const bool pre = a.pre.kind != EMTK_NORM_NONE, post = a.post.kind != EMTK_NORM_NONE;
     const bool pre_mean = a.pre.kind == EMTK_NORM_LAYER, post_mean = a.post.kind == EMTK_NORM_LAYER;
     const int n = a.in.n;
     pdl_trigger();
     pdl_wait();
-    if (io.row >= a.in.m) return;
+    if (io.row >= a.in.m) return;  // (a whole warp)
     io.begin();
     const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0u;
     do {
@@ -486,7 +503,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) residual_norm_grad_kernel(con
             stats.q_mean = pre_mean ? v[2] * a.inverse_n : 0.f;
             stats.qy = v[3] * a.inverse_n * stats.ry * stats.ry;
         }
-        if (a.stats && io.tid == 0) a.stats[io.row] = stats;
+        if (a.stats && io.tid == 0 && io.live) a.stats[io.row] = stats;
         const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0};
         float u[2] = {};  // the sums for the block's norm
 #pragma unroll
@@ -705,11 +722,13 @@ struct Shape {
 };
 Shape shape_of(int n, bool on_grid, bool bulk) {
     const int all = (n + kPiece - 1) / kPiece;
+    const bool whole = on_grid && n % kPiece == 0;
     if (all <= kGroupThreads) {
-        const int threads = (all + 31) / 32 * 32;
-        return {on_grid && n % kPiece == 0 ? kSmall : kSmallAny, threads, std::min(kMostGroups, 256 / threads)};
+        int threads = (all + 31) / 32 * 32;
+        while (threads <= 32 && threads > 4 && threads / 2 >= all) threads /= 2;
+        return {whole ? kSmall : kSmallAny, threads, threads < 32 ? 128 / threads : std::min(kMostGroups, 256 / threads)};
     }
-    return {!bulk && on_grid && n % kPiece == 0 ? kDirect : kBulk, ((all + 1) / 2 + 31) / 32 * 32, 1};
+    return {bulk ? kBulk : whole ? kDirect : kDirectAny, ((all + 1) / 2 + 31) / 32 * 32, 1};
 }
 
 // Blocks of an SM at once, as far as registers and shared memory go.
@@ -740,7 +759,9 @@ cudaError_t run(SeamArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) 
                             : h.threads <= 512 ? residual_norm_kernel<F16, kDirect, 512>
                                                : residual_norm_kernel<F16, kDirect, 1024>, h, 2, 64, a, nn, s);
         default:
-            return run_rows(h.threads <= 512 ? residual_norm_kernel<F16, kBulk, 512> : residual_norm_kernel<F16, kBulk, 1024>, h, 2, 64, a, nn, s);
+            return run_rows(h.threads <= 256   ? residual_norm_kernel<F16, kDirectAny, 256>
+                            : h.threads <= 512 ? residual_norm_kernel<F16, kDirectAny, 512>
+                                               : residual_norm_kernel<F16, kDirectAny, 1024>, h, 2, 64, a, nn, s);
     }
 }
 template <bool F16>
@@ -787,8 +808,6 @@ Slices slices_of(int m, int n, int gate_every, bool block, int sms) {
 template <bool F16>
 static cudaError_t init_kernels() {
     cudaError_t e = cudaSuccess;
-    for (void (*kernel)(const SeamArgs, const Waits) : {residual_norm_kernel<F16, kBulk, 512>, residual_norm_kernel<F16, kBulk, 1024>})
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024);
     for (void (*kernel)(const SeamGradArgs, const Waits) :
          {residual_norm_grad_kernel<F16, kBulk, 256, 3>, residual_norm_grad_kernel<F16, kBulk, 384, 2>,
           residual_norm_grad_kernel<F16, kBulk, 512, 1>, residual_norm_grad_kernel<F16, kBulk, 1024, 1>})
