@@ -34,7 +34,7 @@ struct NormArgs {
 };
 NormArgs norm_args(const emtk_norm &n) {
     const int f32 = n.param_type == EMTK_TYPE_F32;
-    return {n.kind, n.eps, {n.weight, f32}, {n.bias, f32}};
+    return {n.kind, n.eps, param_of(n.weight, f32), param_of(n.bias, f32)};
 }
 
 // The sums of K (1, 2 or 4) values over a group's threads, in every thread.  In a warp
@@ -145,18 +145,20 @@ struct Waits {  // of the kernels' bounded waits
 //   kSmall    several to a block (and to a warp, where they are short), a piece a thread, on the
 //             grid and of whole pieces
 //   kSmallAny the same, anywhere
-//   kBulk     a block goes from row to row, two pieces a thread, anywhere: a row of each matrix is
-//             copied to shared memory, a row or two ahead, in the aligned 16-byte pieces
-//             that it lies in, and shifted into place from there: many rows are on their
-//             way without a register.  Rows whose outer pieces would reach beyond the
-//             matrix are copied by elements.
+//   kBulk     a block goes from row to row, two pieces a thread: a row of each matrix is copied
+//             to shared memory, a row or two ahead, so that many rows are on their way
+//             without a register
+//   kBulkAny  the same, anywhere: in the aligned 16-byte pieces that it lies in, shifted into
+//             place from there.  Rows whose outer pieces would reach beyond the matrix
+//             are copied by elements.
 // A thread's pieces are tid and tid + threads; but for the last of a thread, they are whole.
-enum Kind : int { kDirect, kDirectAny, kSmall, kSmallAny, kBulk };
+enum Kind : int { kDirect, kDirectAny, kSmall, kSmallAny, kBulk, kBulkAny };
+constexpr bool is_bulk(Kind k) { return k == kBulk || k == kBulkAny; }
 
 template <bool F16, Kind KIND, int COUNT>  // COUNT: matrices
 struct RowIo {
     static constexpr int C = KIND == kSmall || KIND == kSmallAny ? 1 : 2;
-    static constexpr bool ODD = KIND != kDirect && KIND != kSmall;
+    static constexpr bool ODD = KIND == kDirectAny || KIND == kSmallAny || KIND == kBulkAny;
     const Inputs &a;
     int64_t row;
     int tid, threads;
@@ -178,7 +180,7 @@ struct RowIo {
         last = column(C - 1) + kPiece > a.n;
         live = row < a.m;
         if (C == 1 && threads < 32) row = min(row, (int64_t)a.m - 1);  // its warp's exchanges need all lanes
-        if (KIND == kBulk) {
+        if (is_bulk(KIND)) {
             if (tid == 0) {
                 for (int i = 0; i < kMostStages; ++i) mbar_init(smem_u32(full + i), 1);
                 *abort_flag = 0;
@@ -190,11 +192,11 @@ struct RowIo {
     __device__ __forceinline__ int column(int k) const { return (k * threads + tid) * kPiece; }
 
     // ---- kBulk: rows on their way
-    __device__ __forceinline__ int head(int i, int64_t r) const { return (int)(reinterpret_cast<uintptr_t>(a.in[i].row(r)) % 16); }
+    __device__ __forceinline__ int head(int i, int64_t r) const { return ODD ? (int)(reinterpret_cast<uintptr_t>(a.in[i].row(r)) % 16) : 0; }
     __device__ __forceinline__ int bytes(int i, int64_t r) const { return (head(i, r) + 2 * a.n + 15) / 16 * 16; }
     __device__ __forceinline__ uint8_t *place(int s, int i) const { return stages + (s * COUNT + i) * a.row_bytes; }
     __device__ __forceinline__ bool by_elements(int64_t r) const {
-        if (r >= kPiece && r < a.m - kPiece) return false;  // the 14 bytes around are of rows between
+        if (!ODD || (r >= kPiece && r < a.m - kPiece)) return false;  // the 14 bytes around are of rows between
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
             if (!a.in[i].p) continue;
@@ -216,12 +218,12 @@ struct RowIo {
                 bulk_load(smem_u32(place(s, i)), reinterpret_cast<const uint8_t *>(a.in[i].row(r)) - head(i, r), bytes(i, r), bar);
     }
     __device__ __forceinline__ void begin() const {
-        if (KIND == kBulk && tid == 0)
+        if (is_bulk(KIND) && tid == 0)
             for (int i = 0; i < a.stages; ++i) fetch(row + (int64_t)i * gridDim.x, i);
     }
     // The row's arrival; all threads.
     __device__ __forceinline__ void wait() {
-        if (KIND != kBulk) return;
+        if (!is_bulk(KIND)) return;
         if (by_elements(row)) {
             __syncthreads();
 #pragma unroll
@@ -239,17 +241,17 @@ struct RowIo {
     }
     // Every thread has taken its pieces, and met the others since: the stage may be filled again.
     __device__ __forceinline__ void release() {
-        if (KIND != kBulk) return;
+        if (!is_bulk(KIND)) return;
         if (tid == 0) fetch(row + (int64_t)a.stages * gridDim.x, stage);
         if (++stage == a.stages) stage = 0;
     }
     __device__ __forceinline__ bool next() {  // to the block's next row
-        if (KIND != kBulk) return false;
+        if (!is_bulk(KIND)) return false;
         row += gridDim.x;
         return row < a.m;
     }
     __device__ __forceinline__ void end() const {
-        if (KIND != kBulk || ok) return;
+        if (!is_bulk(KIND) || ok) return;
         const uint64_t t0 = global_timer_ns();  // copies in flight land within microseconds: leave them a millisecond
         while (global_timer_ns() - t0 < 1000000u) {
         }
@@ -263,6 +265,14 @@ struct RowIo {
             for (int i = 0; i < 4; ++i) w[k][i] = 0u;
         if (!a.in[which].p) return;
         if constexpr (KIND == kBulk) {
+            const uint4 *const p = reinterpret_cast<const uint4 *>(place(stage, which)) + tid;
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                if (k == C - 1 && last) continue;
+                const uint4 x = p[k * threads];
+                w[k][0] = x.x, w[k][1] = x.y, w[k][2] = x.z, w[k][3] = x.w;
+            }
+        } else if constexpr (KIND == kBulkAny) {
             const uint4 *const base = reinterpret_cast<const uint4 *>(place(stage, which));
             const int halves = head(which, row) / 2, most = (a.n - 1) / kPiece;
 #pragma unroll
@@ -310,8 +320,7 @@ struct RowIo {
     }
     // A vector's columns of piece k; 0 from n on.
     __device__ __forceinline__ Eight param(const Param &p, int k) const {
-        if (KIND == kDirect && k < C - 1) return param8<F16>(p, column(k), 1 << 30);
-        return param8<F16>(p, column(k), a.n);
+        return param8<F16>(p, column(k), a.n, k < C - 1 || !last);
     }
     __device__ __forceinline__ void store(const Rows16 &to, int k, const Eight &e) const {
         uint32_t w[4];
@@ -357,7 +366,7 @@ struct SeamArgs {
     NormArgs post, pre;
     Drop drop;
     float scale, inverse_n;
-    int gate_every;
+    int gate_every, gate_vec;  // gate_vec: its rows are on 16 bytes
 };
 
 template <bool F16, Kind KIND, int THREADS>
@@ -382,7 +391,7 @@ __global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_con
         uint32_t wb[C][4], wr[C][4];
         io.load(kInBlock, wb);
         io.load(kInResidual, wr);
-        if (KIND == kBulk) {
+        if (is_bulk(KIND)) {
             __syncthreads();
             io.release();
         }
@@ -390,7 +399,7 @@ __global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_con
 #pragma unroll
         for (int k = 0; k < C; ++k) v[k] = values8<F16>(wb[k]);
         if (a.post.kind != EMTK_NORM_NONE) normalise<F16>(a.post, v, io, a.inverse_n, reduction);
-        const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0};
+        const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0, a.gate_vec};
 #pragma unroll
         for (int k = 0; k < C; ++k) {
             if (a.drop.below) dropped(a.drop, offset, (uint32_t)io.row, (uint32_t)(k * io.threads + io.tid), v[k]);
@@ -424,7 +433,7 @@ struct SeamGradArgs {
     NormArgs post, pre;
     Drop drop;
     float scale, inverse_n;
-    int gate_every;
+    int gate_every, gate_vec;  // gate_vec: its rows are on 16 bytes
     RowStats *stats;  // null: no sums are wanted
 };
 
@@ -462,7 +471,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) residual_norm_grad_kernel(con
 #pragma unroll
         for (int k = 0; k < C; ++k) b[k] = values8<F16>(w[k]);
         io.load(kInDy, wt);
-        if (KIND == kBulk) {
+        if (is_bulk(KIND)) {
             __syncthreads();
             io.release();
         }
@@ -504,7 +513,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) residual_norm_grad_kernel(con
             stats.qy = v[3] * a.inverse_n * stats.ry * stats.ry;
         }
         if (a.stats && io.tid == 0 && io.live) a.stats[io.row] = stats;
-        const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0};
+        const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0, a.gate_vec};
         float u[2] = {};  // the sums for the block's norm
 #pragma unroll
         for (int k = 0; k < C; ++k) {
@@ -616,9 +625,10 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
     weight.fill(1.f);
     post_weight.fill(1.f);
     post_bias.fill(0.f);
-    if (in && g.pre.weight.p) weight = param8<F16>(g.pre.weight, c, n);
-    if (BLOCK && in && g.post.weight.p) post_weight = param8<F16>(g.post.weight, c, n);
-    if (BLOCK && in && g.post.bias.p) post_bias = param8<F16>(g.post.bias, c, n);
+    const bool full = c + kPiece <= n;
+    if (in && g.pre.weight.p) weight = param8<F16>(g.pre.weight, c, n, full);
+    if (BLOCK && in && g.post.weight.p) post_weight = param8<F16>(g.post.weight, c, n, full);
+    if (BLOCK && in && g.post.bias.p) post_bias = param8<F16>(g.post.bias, c, n, full);
     const uint64_t offset = BLOCK && g.drop.below ? drop_offset(g.drop) : 0u;
     // where whole gate rows are summed, one after another
     for (int64_t begin = r0; begin < r1;) {
@@ -660,7 +670,7 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
                     sum[kSumGate].v[i] = fma2(t.v[i], fma2(b.v[i], post_weight.v[i], post_bias.v[i]), sum[kSumGate].v[i]);
                 }
                 if (g.gate.p && in) {
-                    const Eight gate = param8<F16>({g.gate.row(row / g.gate_every), 0}, c, n);
+                    const Eight gate = param8<F16>({g.gate.row(row / g.gate_every), 0, g.gate_vec}, c, n, full);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) t.v[i] = t.v[i] * gate.v[i];
                 }
@@ -728,7 +738,7 @@ Shape shape_of(int n, bool on_grid, bool bulk) {
         while (threads <= 32 && threads > 4 && threads / 2 >= all) threads /= 2;
         return {whole ? kSmall : kSmallAny, threads, threads < 32 ? 128 / threads : std::min(kMostGroups, 256 / threads)};
     }
-    return {bulk ? kBulk : whole ? kDirect : kDirectAny, ((all + 1) / 2 + 31) / 32 * 32, 1};
+    return {bulk ? (whole ? kBulk : kBulkAny) : whole ? kDirect : kDirectAny, ((all + 1) / 2 + 31) / 32 * 32, 1};
 }
 
 // Blocks of an SM at once, as far as registers and shared memory go.
@@ -740,7 +750,7 @@ template <typename Args>
 cudaError_t run_rows(void (*kernel)(const Args, const Waits), const Shape &h, int inputs, int registers, Args &a, const emtk_nn *nn, cudaStream_t s) {
     int64_t blocks = ((int64_t)a.in.m + h.groups - 1) / h.groups;
     size_t shared = 0;
-    if (h.kind == kBulk) {
+    if (is_bulk(h.kind)) {
         const size_t row = (size_t)inputs * a.in.row_bytes;
         a.in.stages = 2 * row <= 222 * 1024 ? 2 : 1;
         shared = a.in.stages * row;
@@ -764,16 +774,20 @@ cudaError_t run(SeamArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) 
                                                : residual_norm_kernel<F16, kDirectAny, 1024>, h, 2, 64, a, nn, s);
     }
 }
+template <bool F16, Kind KIND>
+cudaError_t run_bulk(SeamGradArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) {
+    if (h.threads <= 256) return run_rows(residual_norm_grad_kernel<F16, KIND, 256, 3>, h, 4, 80, a, nn, s);
+    if (h.threads <= 384) return run_rows(residual_norm_grad_kernel<F16, KIND, 384, 2>, h, 4, 80, a, nn, s);
+    if (h.threads <= 512) return run_rows(residual_norm_grad_kernel<F16, KIND, 512, 1>, h, 4, 128, a, nn, s);
+    return run_rows(residual_norm_grad_kernel<F16, KIND, 1024, 1>, h, 4, 64, a, nn, s);
+}
 template <bool F16>
 cudaError_t run(SeamGradArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) {
     switch (h.kind) {
         case kSmall: return run_rows(residual_norm_grad_kernel<F16, kSmall, 256, 3>, h, 4, 80, a, nn, s);
         case kSmallAny: return run_rows(residual_norm_grad_kernel<F16, kSmallAny, 256, 3>, h, 4, 80, a, nn, s);
-        default:
-            if (h.threads <= 256) return run_rows(residual_norm_grad_kernel<F16, kBulk, 256, 3>, h, 4, 80, a, nn, s);
-            if (h.threads <= 384) return run_rows(residual_norm_grad_kernel<F16, kBulk, 384, 2>, h, 4, 80, a, nn, s);
-            if (h.threads <= 512) return run_rows(residual_norm_grad_kernel<F16, kBulk, 512, 1>, h, 4, 128, a, nn, s);
-            return run_rows(residual_norm_grad_kernel<F16, kBulk, 1024, 1>, h, 4, 64, a, nn, s);
+        case kBulk: return run_bulk<F16, kBulk>(a, h, nn, s);
+        default: return run_bulk<F16, kBulkAny>(a, h, nn, s);
     }
 }
 template <typename Args>
@@ -805,24 +819,26 @@ Slices slices_of(int m, int n, int gate_every, bool block, int sms) {
 
 }  // namespace
 
-template <bool F16>
+template <bool F16, Kind KIND>
 static cudaError_t init_kernels() {
     cudaError_t e = cudaSuccess;
     for (void (*kernel)(const SeamGradArgs, const Waits) :
-         {residual_norm_grad_kernel<F16, kBulk, 256, 3>, residual_norm_grad_kernel<F16, kBulk, 384, 2>,
-          residual_norm_grad_kernel<F16, kBulk, 512, 1>, residual_norm_grad_kernel<F16, kBulk, 1024, 1>})
+         {residual_norm_grad_kernel<F16, KIND, 256, 3>, residual_norm_grad_kernel<F16, KIND, 384, 2>,
+          residual_norm_grad_kernel<F16, KIND, 512, 1>, residual_norm_grad_kernel<F16, KIND, 1024, 1>})
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 222 * 1024);
     return e;
 }
 cudaError_t init_norm_kernels() {
-    const cudaError_t e = init_kernels<false>();
-    return e == cudaSuccess ? init_kernels<true>() : e;
+    for (const cudaError_t e : {init_kernels<false, kBulk>(), init_kernels<true, kBulk>(), init_kernels<false, kBulkAny>(), init_kernels<true, kBulkAny>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
 }
 
 cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, const emtk_nn *nn, cudaStream_t s) {
     SeamArgs a{};
     a.in = {{rows16_of(p.residual), rows16_of(p.block)}, p.m, p.n, bulk_row_bytes(p.n), 1};
     a.gate = rows16_of(p.gate);
+    a.gate_vec = on_grid(p.gate, 2);
     a.y = rows16_of(p.y);
     a.h = rows16_of(p.h);
     a.post = norm_args(p.post);
@@ -849,6 +865,7 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
     SeamGradArgs a{};
     a.in = {{rows16_of(p.y), rows16_of(p.dh), rows16_of(p.block), rows16_of(p.dy)}, p.m, p.n, bulk_row_bytes(p.n), 1};
     a.gate = rows16_of(p.gate);
+    a.gate_vec = on_grid(p.gate, 2);
     a.d_residual = rows16_of(p.d_residual);
     a.d_block = rows16_of(p.d_block);
     a.post = norm_args(p.post);

@@ -154,15 +154,16 @@ __device__ __forceinline__ void store_run(uint16_t *p, int n, const uint32_t (&w
 // ---- parameters of a row's columns: 16 bits or fp32, vectors at any alignment
 struct Param {
     const void *p;
-    int f32;
+    int f32, vec;  // vec: on 16 bytes
 };
-// Columns c .. of one that is there; those from n on are 0.
+inline Param param_of(const void *p, bool f32) { return {p, f32, reinterpret_cast<uintptr_t>(p) % 16 == 0}; }
+// Columns c .. of one that is there; those from n on are 0.  whole: none of them.
 template <bool F16>
-__device__ __forceinline__ Eight param8(const Param &a, int c, int n) {
+__device__ __forceinline__ Eight param8(const Param &a, int c, int n, bool whole) {
     Eight e;
     if (a.f32) {
         const float *const p = static_cast<const float *>(a.p) + c;
-        if (c + kPiece <= n && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+        if (a.vec && whole) {
             const float4 lo = __ldg(reinterpret_cast<const float4 *>(p)), hi = __ldg(reinterpret_cast<const float4 *>(p) + 1);
             e.v[0] = make_float2(lo.x, lo.y), e.v[1] = make_float2(lo.z, lo.w);
             e.v[2] = make_float2(hi.x, hi.y), e.v[3] = make_float2(hi.z, hi.w);
@@ -175,7 +176,7 @@ __device__ __forceinline__ Eight param8(const Param &a, int c, int n) {
     }
     const uint16_t *const p = static_cast<const uint16_t *>(a.p) + c;
     uint32_t w[4] = {};
-    if (c + kPiece <= n && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+    if (a.vec && whole) {
         const uint4 q = __ldg(reinterpret_cast<const uint4 *>(p));
         w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
     } else {
