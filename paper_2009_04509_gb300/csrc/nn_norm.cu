@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_con
 #pragma unroll
         for (int k = 0; k < C; ++k) v[k] = values8<F16>(wb[k]);
         if (a.post.kind != EMTK_NORM_NONE) normalise<F16>(a.post, v, io, a.inverse_n, reduction);
-        const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0, a.gate_vec};
+        const Param gate{a.gate.p ? a.gate.row((int)io.row / a.gate_every) : nullptr, 0, a.gate_vec};
 #pragma unroll
         for (int k = 0; k < C; ++k) {
             if (a.drop.below) dropped(a.drop, offset, (uint32_t)io.row, (uint32_t)(k * io.threads + io.tid), v[k]);
@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) residual_norm_grad_kernel(con
             stats.qy = v[3] * a.inverse_n * stats.ry * stats.ry;
         }
         if (a.stats && io.tid == 0 && io.live) a.stats[io.row] = stats;
-        const Param gate{a.gate.p ? a.gate.row(io.row / a.gate_every) : nullptr, 0, a.gate_vec};
+        const Param gate{a.gate.p ? a.gate.row((int)io.row / a.gate_every) : nullptr, 0, a.gate_vec};
         float u[2] = {};  // the sums for the block's norm
 #pragma unroll
         for (int k = 0; k < C; ++k) {
@@ -630,11 +630,22 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
     if (BLOCK && in && g.post.weight.p) post_weight = param8<F16>(g.post.weight, c, n, full);
     if (BLOCK && in && g.post.bias.p) post_bias = param8<F16>(g.post.bias, c, n, full);
     const uint64_t offset = BLOCK && g.drop.below ? drop_offset(g.drop) : 0u;
-    // where whole gate rows are summed, one after another
+    // a gate row's rows after another's, where their sums are apart; all at once where only the
+    // gate that they are multiplied with changes
+    const bool one_gate = a.gate_out || a.slices.parts > 1 || a.slices.groups_each == 1;
     for (int64_t begin = r0; begin < r1;) {
-        const int64_t group = begin / g.gate_every, end = a.gate_out ? min((group + 1) * g.gate_every, r1) : r1;
+        const int group = (int)begin / g.gate_every;
+        const int64_t end = a.gate_out ? min((int64_t)(group + 1) * g.gate_every, r1) : r1;
+        Eight gate;
+        gate.fill(1.f);
+        if (BLOCK && g.gate.p && in && one_gate) gate = param8<F16>({g.gate.row(group), 0, g.gate_vec}, c, n, full);
         Piece16<ANY> wy, wd, wb, wt;
+        float4 s;
+        float2 s2;
         auto fetch = [&](int64_t row) {
+            s = __ldg(reinterpret_cast<const float4 *>(g.stats + row));
+            if (BLOCK) s2 = __ldg(reinterpret_cast<const float2 *>(g.stats + row) + 2);
+            if (!in) return;
             if (pre) wy.load(g.in.in[kInY], row, c, m, n);
             if (pre) wd.load(g.in.in[kInDh], row, c, m, n);
             if (BLOCK) wb.load(g.in.in[kInOut], row, c, m, n);
@@ -645,14 +656,12 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
         wb.clear();
         wt.clear();
         int64_t row = begin + threadIdx.x / 32;
-        if (in && row < end) fetch(row);
+        if (row < end) fetch(row);
         for (; row < end; row += kSumRows) {
             Eight y = wy.template values<F16>(), d = wd.template values<F16>();
             Eight b = wb.template values<F16>(), t = wt.template values<F16>();
-            const float4 s = __ldg(reinterpret_cast<const float4 *>(g.stats + row));
-            const float2 s2 = __ldg(reinterpret_cast<const float2 *>(g.stats + row) + 2);
-            if (in && row + kSumRows < end) fetch(row + kSumRows);
             const float mean_y = s.x, ry = s.y, q_mean = s.z, qy = s.w, mean_b = s2.x, rb = s2.y;
+            if (row + kSumRows < end) fetch(row + kSumRows);
             if (pre) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -669,13 +678,10 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
                     b.v[i] = (b.v[i] - both(mean_b)) * both(rb);
                     sum[kSumGate].v[i] = fma2(t.v[i], fma2(b.v[i], post_weight.v[i], post_bias.v[i]), sum[kSumGate].v[i]);
                 }
-                if (g.gate.p && in) {
-                    const Eight gate = param8<F16>({g.gate.row(row / g.gate_every), 0, g.gate_vec}, c, n, full);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) t.v[i] = t.v[i] * gate.v[i];
-                }
+                if (g.gate.p && in && !one_gate) gate = param8<F16>({g.gate.row((int)row / g.gate_every), 0, g.gate_vec}, c, n, full);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    t.v[i] = t.v[i] * gate.v[i];
                     sum[kSumPostW].v[i] = fma2(t.v[i], b.v[i], sum[kSumPostW].v[i]);
                     sum[kSumPostB].v[i] = sum[kSumPostB].v[i] + t.v[i];
                 }
