@@ -196,12 +196,14 @@ struct RowIo {
     __device__ __forceinline__ int bytes(int i, int64_t r) const { return (head(i, r) + 2 * a.n + 15) / 16 * 16; }
     __device__ __forceinline__ uint8_t *place(int s, int i) const { return stages + (s * COUNT + i) * a.row_bytes; }
     __device__ __forceinline__ bool by_elements(int64_t r) const {
-        if (!ODD || (r >= kPiece && r < a.m - kPiece)) return false;  // the 14 bytes around are of rows between
+        if constexpr (ODD) {
+            if (r >= kPiece && r < a.m - kPiece) return false;  // the 14 bytes around are of rows between
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            if (!a.in[i].p) continue;
-            const int64_t first = r * a.in[i].row_bytes - head(i, r), end = (a.m - 1) * a.in[i].row_bytes + 2 * (int64_t)a.n;
-            if (first < 0 || first + bytes(i, r) > end) return true;
+            for (int i = 0; i < COUNT; ++i) {
+                if (!a.in[i].p) continue;
+                const int64_t first = r * a.in[i].row_bytes - head(i, r), end = (a.m - 1) * a.in[i].row_bytes + 2 * (int64_t)a.n;
+                if (first < 0 || first + bytes(i, r) > end) return true;
+            }
         }
         return false;
     }
@@ -584,37 +586,93 @@ struct SumArgs {
 constexpr int kSumBlocks = 3, kSumBlocksPre = 5;  // of an SM at once
 constexpr int kSumThreads = 128, kSumRows = kSumThreads / 32;
 
-// The sums of the block's rows of threads for a run of columns, in order, to `to`.
-__device__ __forceinline__ void flush_sum(Eight &e, float (*shared)[32 * kPiece], float *to, int c0, int n) {
+// How rows lie: on the 16-byte grid; off it, but all matrices' alike; anyhow.
+//   kAlike: the row 8 rows on lies as this one does, so a warp that takes every eighth row has
+//   its lanes' aligned 16 bytes at the same columns in each, c .. c + 7 with c = -shift of 8,
+//   and nothing is shifted into place: only the sums are, once, when they are joined.
+//   (8192 x 5461, as kAny: 290 us of such a call, 340 with fewer blocks at once.)
+enum Lie : int { kGrid, kAlike, kAny };
+constexpr int kAlikeColumns = 31 * kPiece;  // of a block: its 32 lanes' pieces hold them at any shift
+
+template <Lie LIE>
+struct SumPiece {
+    Piece16<LIE == kAny> w;
+    __device__ __forceinline__ void clear() { w.clear(); }
+    __device__ __forceinline__ void load(const Rows16 &a, int64_t row, int c, int m, int n) {
+        if constexpr (LIE == kAlike) {
+            // what lies around a row is of its neighbours, but for the first and last rows'
+            if ((c >= 0 || row >= kPiece) && (c + kPiece <= n || row < m - kPiece)) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(a.row(row) + c);
+                w.x[0] = x.x, w.x[1] = x.y, w.x[2] = x.z, w.x[3] = x.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w.x[i] = 0u;
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i)
+                    if (c + i >= 0 && c + i < n) w.x[i / 2] |= (uint32_t)a.row(row)[c + i] << (16 * (i % 2));
+            }
+        } else {
+            w.load(a, row, c, m, n);
+        }
+    }
+    template <bool F16>
+    __device__ __forceinline__ Eight values() const {
+        return w.template values<F16>();
+    }
+};
+template <bool F16, Lie LIE>
+__device__ __forceinline__ Eight sum_param(const Param &p, int c, int n) {
+    if constexpr (LIE == kAlike) {
+        float v[kPiece];
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+            v[i] = 0.f;
+            if (c + i < 0 || c + i >= n) continue;
+            v[i] = p.f32 ? __ldg(static_cast<const float *>(p.p) + c + i) : from16<F16>(__ldg(static_cast<const uint16_t *>(p.p) + c + i));
+        }
+        Eight e;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.v[i] = make_float2(v[2 * i], v[2 * i + 1]);
+        return e;
+    } else {
+        return param8<F16>(p, c, n, c + kPiece <= n);
+    }
+}
+
+// The sums of the block's warps for its columns c0 .. (`columns` of them, below n), in order, to
+// `to`; shift: columns before c0 that the warp's pieces begin at.
+__device__ __forceinline__ void flush_sum(Eight &e, float (*shared)[33 * kPiece], float *to, int c0, int columns, int shift, int n) {
     __syncthreads();
-    float *const mine = shared[threadIdx.x / 32] + threadIdx.x % 32;  // value i of a lane: 32 i on, so that lanes meet in no bank
+    float *const mine = shared[threadIdx.x / 32] + threadIdx.x % 32 * kPiece + kPiece - shift;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        mine[64 * i] = e.v[i].x;
-        mine[64 * i + 32] = e.v[i].y;
+        mine[2 * i] = e.v[i].x;
+        mine[2 * i + 1] = e.v[i].y;
     }
     __syncthreads();
 #pragma unroll
     for (int c = threadIdx.x; c < 32 * kPiece; c += kSumThreads) {
-        const int at = c % kPiece * 32 + c / kPiece;
         float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < kSumRows; ++r) sum += shared[r][at];
-        if (c0 + c < n) to[c0 + c] = sum;
+        for (int r = 0; r < kSumRows; ++r) sum += shared[r][kPiece + c];
+        if (c < columns && c0 + c < n) to[c0 + c] = sum;
     }
     e.fill(0.f);
 }
 
-// A block takes 256 columns and a slice's rows, a warp every fourth of them, a piece to a
-// lane.  BLOCK: sums over the block's output (all inputs are read); else of the norm after
-// it alone (y and dh).
-template <bool F16, bool ANY, bool BLOCK>
+// A block takes 256 columns and a slice's rows, a warp every fourth of them (kAlike: 248 columns, a
+// warp every eighth row, and two blocks share a slice), a piece to a lane.  BLOCK: sums
+// over the block's output (all inputs are read); else of the norm after it alone (y and dh).
+template <bool F16, Lie LIE, bool BLOCK>
 __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPre) residual_norm_sum_kernel(const __grid_constant__ SumArgs a) {
-    __shared__ float shared[kSumRows][32 * kPiece];
+    __shared__ float shared[kSumRows][33 * kPiece];
     const SeamGradArgs &g = a.g;
     const int n = g.in.n, m = g.in.m, slice = blockIdx.y;
-    const int c0 = blockIdx.x * 32 * kPiece, c = c0 + threadIdx.x % 32 * kPiece;
-    const bool in = c < n, pre = g.pre.kind != EMTK_NORM_NONE;
+    constexpr int kColumns = LIE == kAlike ? kAlikeColumns : 32 * kPiece, kStep = LIE == kAlike ? 8 : kSumRows;
+    const int phase = threadIdx.x / 32 + (LIE == kAlike ? kSumRows * (int)blockIdx.z : 0);  // of the warp's rows
+    const int shift = LIE == kAlike ? (int)(reinterpret_cast<uintptr_t>(g.in.in[BLOCK ? kInOut : kInY].row(phase)) % 16) / 2 : 0;
+    const int c0 = blockIdx.x * kColumns, c = c0 + (int)(threadIdx.x % 32) * kPiece - shift;
+    const bool in = c < n && c < c0 + kColumns, pre = g.pre.kind != EMTK_NORM_NONE;
     pdl_trigger();
     pdl_wait();
     int64_t r0, r1;
@@ -625,10 +683,9 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
     weight.fill(1.f);
     post_weight.fill(1.f);
     post_bias.fill(0.f);
-    const bool full = c + kPiece <= n;
-    if (in && g.pre.weight.p) weight = param8<F16>(g.pre.weight, c, n, full);
-    if (BLOCK && in && g.post.weight.p) post_weight = param8<F16>(g.post.weight, c, n, full);
-    if (BLOCK && in && g.post.bias.p) post_bias = param8<F16>(g.post.bias, c, n, full);
+    if (in && g.pre.weight.p) weight = sum_param<F16, LIE>(g.pre.weight, c, n);
+    if (BLOCK && in && g.post.weight.p) post_weight = sum_param<F16, LIE>(g.post.weight, c, n);
+    if (BLOCK && in && g.post.bias.p) post_bias = sum_param<F16, LIE>(g.post.bias, c, n);
     const uint64_t offset = BLOCK && g.drop.below ? drop_offset(g.drop) : 0u;
     // a gate row's rows after another's, where their sums are apart; all at once where only the
     // gate that they are multiplied with changes
@@ -638,8 +695,8 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
         const int64_t end = a.gate_out ? min((int64_t)(group + 1) * g.gate_every, r1) : r1;
         Eight gate;
         gate.fill(1.f);
-        if (BLOCK && g.gate.p && in && one_gate) gate = param8<F16>({g.gate.row(group), 0, g.gate_vec}, c, n, full);
-        Piece16<ANY> wy, wd, wb, wt;
+        if (BLOCK && g.gate.p && in && one_gate) gate = sum_param<F16, LIE>({g.gate.row(group), 0, g.gate_vec}, c, n);
+        SumPiece<LIE> wy, wd, wb, wt;
         float4 s;
         float2 s2;
         auto fetch = [&](int64_t row) {
@@ -655,13 +712,13 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
         wd.clear();
         wb.clear();
         wt.clear();
-        int64_t row = begin + threadIdx.x / 32;
+        int64_t row = LIE == kAlike ? begin + ((phase - (int)begin) & 7) : begin + phase;
         if (row < end) fetch(row);
-        for (; row < end; row += kSumRows) {
+        for (; row < end; row += kStep) {
             Eight y = wy.template values<F16>(), d = wd.template values<F16>();
             Eight b = wb.template values<F16>(), t = wt.template values<F16>();
             const float mean_y = s.x, ry = s.y, q_mean = s.z, qy = s.w, mean_b = s2.x, rb = s2.y;
-            if (row + kSumRows < end) fetch(row + kSumRows);
+            if (row + kStep < end) fetch(row + kStep);
             if (pre) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -672,13 +729,23 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
                 }
             }
             if constexpr (BLOCK) {
-                if (g.drop.below) dropped(g.drop, offset, (uint32_t)row, (uint32_t)(c / kPiece), t);
+                if (g.drop.below) {
+                    uint32_t x[8], z[4];
+                    drop_numbers(g.drop, offset, (uint32_t)row, (uint32_t)(c >> 3), x);
+                    if (LIE == kAlike && shift) {  // the piece is of two pieces' columns
+                        drop_numbers(g.drop, offset, (uint32_t)row, (uint32_t)(c >> 3) + 1u, x + 4);
+                        shift_words(x, c & 7, z);
+                        dropped_by(g.drop, z, t);
+                    } else {
+                        dropped_by(g.drop, x, t);
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     b.v[i] = (b.v[i] - both(mean_b)) * both(rb);
                     sum[kSumGate].v[i] = fma2(t.v[i], fma2(b.v[i], post_weight.v[i], post_bias.v[i]), sum[kSumGate].v[i]);
                 }
-                if (g.gate.p && in && !one_gate) gate = param8<F16>({g.gate.row((int)row / g.gate_every), 0, g.gate_vec}, c, n, full);
+                if (g.gate.p && in && !one_gate) gate = sum_param<F16, LIE>({g.gate.row((int)row / g.gate_every), 0, g.gate_vec}, c, n);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     t.v[i] = t.v[i] * gate.v[i];
@@ -687,12 +754,12 @@ __global__ void __launch_bounds__(kSumThreads, BLOCK ? kSumBlocks : kSumBlocksPr
                 }
             }
         }
-        if (BLOCK && a.gate_out) flush_sum(sum[BLOCK ? kSumGate : 0], shared, a.gate_out + group * a.gate_ld, c0, n);
+        if (BLOCK && a.gate_out) flush_sum(sum[BLOCK ? kSumGate : 0], shared, a.gate_out + group * a.gate_ld, c0, kColumns, shift, n);
         begin = end;
     }
 #pragma unroll
     for (int i = 0; i < (BLOCK ? kSums : 2); ++i)
-        if (a.partial[i]) flush_sum(sum[i], shared, a.partial[i] + (int64_t)slice * n, c0, n);
+        if (a.partial[i]) flush_sum(sum[i], shared, a.partial[i] + ((int64_t)slice * gridDim.z + blockIdx.z) * n, c0, kColumns, shift, n);
 }
 
 // Adds slices' sums: a block takes 32 columns of one result, each of its warps every
@@ -801,10 +868,15 @@ cudaError_t run(Args &a, int type, const Shape &h, const emtk_nn *nn, cudaStream
     return type == EMTK_TYPE_F16 ? run<true>(a, h, nn, s) : run<false>(a, h, nn, s);
 }
 
+// Blocks across.
+int64_t sum_columns(int n, Lie lie) {
+    const int64_t each = lie == kAlike ? kAlikeColumns : 32 * kPiece;
+    return (n + each - 1) / each;
+}
 // How the columns' kernel cuts the rows: as many blocks as run at once (a second round of
 // few blocks costs as much as the first), of 16 rows at least.
-Slices slices_of(int m, int n, int gate_every, bool block, int sms) {
-    const int64_t columns = ((int64_t)n + 32 * kPiece - 1) / (32 * kPiece);
+Slices slices_of(int m, int n, int gate_every, bool block, Lie lie, int sms) {
+    const int64_t columns = sum_columns(n, lie) * (lie == kAlike ? 2 : 1);
     const int64_t want = std::max<int64_t>(1, std::min<int64_t>((block ? kSumBlocks : kSumBlocksPre) * (int64_t)sms / columns, ((int64_t)m + 15) / 16));
     const int64_t groups = std::max<int64_t>(1, ((int64_t)m + gate_every - 1) / gate_every);
     Slices l;
@@ -862,9 +934,43 @@ static int norm_sums(const emtk_residual_norm_grad_args &p) {
     return (p.dw_pre ? 1 : 0) + (p.db_pre ? 1 : 0) + (p.dw_post ? 1 : 0) + (p.db_post ? 1 : 0) + (p.d_gate.d ? 1 : 0);
 }
 static bool block_sums(const emtk_residual_norm_grad_args &p) { return p.dw_post || p.db_post || p.d_gate.d; }
+template <bool F16, bool BLOCK>
+static void (*sum_kernel(Lie lie))(const SumArgs) {
+    return lie == kGrid    ? residual_norm_sum_kernel<F16, kGrid, BLOCK>
+           : lie == kAlike ? residual_norm_sum_kernel<F16, kAlike, BLOCK>
+                           : residual_norm_sum_kernel<F16, kAny, BLOCK>;
+}
+// The columns' kernel of a call and its slices.
+struct SumPlan {
+    Lie lie;
+    Slices slices;
+    int64_t partials;  // of each slice's sums
+};
+static SumPlan sum_plan(const emtk_residual_norm_grad_args &p, int sms) {
+    const emtk_matrix *const in[] = {&p.y, &p.dh, &p.dy, &p.block};
+    bool grid = true, alike = true;
+    const emtk_matrix *one = nullptr;
+    for (int i = 0; i < (block_sums(p) ? 4 : 2); ++i) {
+        if (!in[i]->d) continue;
+        grid = grid && on_grid(*in[i], p.m);
+        if (one) alike = alike && (reinterpret_cast<uintptr_t>(one->d) - reinterpret_cast<uintptr_t>(in[i]->d)) % 16 == 0 && (one->ld - in[i]->ld) % 8 == 0;
+        one = in[i];
+    }
+    SumPlan plan;
+    plan.lie = grid ? kGrid : alike ? kAlike : kAny;
+    plan.slices = slices_of(p.m, p.n, p.gate_every, block_sums(p), plan.lie, sms);
+    if (plan.lie == kAlike && p.d_gate.d && plan.slices.parts == 1) {  // a gate row's sum is one block's
+        plan.lie = kAny;
+        plan.slices = slices_of(p.m, p.n, p.gate_every, block_sums(p), plan.lie, sms);
+    }
+    plan.partials = plan.lie == kAlike ? 2 : 1;
+    return plan;
+}
 size_t residual_norm_workspace(const emtk_residual_norm_grad_args &p, int sms) {
     const int sums = norm_sums(p);
-    return sums ? (size_t)p.m * sizeof(RowStats) + (size_t)sums * slices_of(p.m, p.n, p.gate_every, block_sums(p), sms).count * p.n * sizeof(float) : 0;
+    if (!sums) return 0;
+    const SumPlan plan = sum_plan(p, sms);
+    return (size_t)p.m * sizeof(RowStats) + (size_t)sums * plan.slices.count * plan.partials * p.n * sizeof(float);
 }
 
 cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s) {
@@ -882,12 +988,12 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
     a.gate_every = p.gate_every;
     const int sums = norm_sums(p);
     if (sums) a.stats = static_cast<RowStats *>(workspace);
-    const bool odd = !(on_grid(p.dy, p.m) && on_grid(p.dh, p.m) && on_grid(p.y, p.m) && on_grid(p.block, p.m));
-    const bool whole = !odd && on_grid(p.d_residual, p.m) && on_grid(p.d_block, p.m);
+    const bool whole = on_grid(p.dy, p.m) && on_grid(p.dh, p.m) && on_grid(p.y, p.m) && on_grid(p.block, p.m) && on_grid(p.d_residual, p.m) && on_grid(p.d_block, p.m);
     cudaError_t e = p.m > 0 ? run(a, p.type, shape_of(p.n, whole, true), nn, s) : cudaSuccess;
     if (e != cudaSuccess || !sums) return e;
 
-    const Slices slices = slices_of(p.m, p.n, p.gate_every, block_sums(p), nn->sm_count);
+    const SumPlan plan = sum_plan(p, nn->sm_count);
+    const Slices &slices = plan.slices;
     SumArgs t{};
     t.g = a;
     t.slices = slices;
@@ -902,7 +1008,7 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
             continue;
         }
         t.partial[i] = at;
-        at += (size_t)slices.count * p.n;
+        at += (size_t)slices.count * plan.partials * p.n;
         if (i == kSumGate) {
             j.gate_from = t.partial[i];
             j.gate_to = out[i];
@@ -912,18 +1018,13 @@ cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, voi
             j.to[j.results++] = out[i];
         }
     }
-    j.slices = slices.count;
-    j.parts = slices.parts;
+    j.slices = (int)(slices.count * plan.partials);
+    j.parts = (int)(slices.parts * plan.partials);
     j.n = p.n;
-    const bool block = block_sums(p), f16 = p.type == EMTK_TYPE_F16;
-    void (*kernel)(const SumArgs);
-    if (block)
-        kernel = odd ? (f16 ? residual_norm_sum_kernel<true, true, true> : residual_norm_sum_kernel<false, true, true>)
-                     : (f16 ? residual_norm_sum_kernel<true, false, true> : residual_norm_sum_kernel<false, false, true>);
-    else
-        kernel = odd ? (f16 ? residual_norm_sum_kernel<true, true, false> : residual_norm_sum_kernel<false, true, false>)
-                     : (f16 ? residual_norm_sum_kernel<true, false, false> : residual_norm_sum_kernel<false, false, false>);
-    e = launch_pdl(kernel, dim3((unsigned)((p.n + 32 * kPiece - 1) / (32 * kPiece)), (unsigned)slices.count), dim3(kSumThreads), 0, s, t);
+    const bool f16 = p.type == EMTK_TYPE_F16;
+    void (*const kernel)(const SumArgs) = block_sums(p) ? (f16 ? sum_kernel<true, true>(plan.lie) : sum_kernel<false, true>(plan.lie))
+                                                        : (f16 ? sum_kernel<true, false>(plan.lie) : sum_kernel<false, false>(plan.lie));
+    e = launch_pdl(kernel, dim3((unsigned)sum_columns(p.n, plan.lie), (unsigned)slices.count, (unsigned)plan.partials), dim3(kSumThreads), 0, s, t);
     const int gates = j.gate_to ? std::max(1, slices.count / slices.parts) : 0;
     if (e == cudaSuccess && j.results + gates > 0)
         e = launch_pdl(residual_norm_join_kernel, dim3((unsigned)((p.n + 31) / 32), (unsigned)(j.results + gates)),

@@ -208,9 +208,9 @@ inline Drop drop_of(const emtk_drop &d) {
 // The call's offset, as the device has it.
 __device__ __forceinline__ uint64_t drop_offset(const Drop &d) { return d.offset + (d.d_offset ? *d.d_offset : 0u); }
 
-// The piece's elements under dropout: row r, columns 8 g ..
-__device__ __forceinline__ void dropped(const Drop &d, uint64_t offset, uint32_t r, uint32_t g, Eight &e) {
-    uint32_t x[4] = {g, r, (uint32_t)offset, (uint32_t)(offset >> 32)};
+// The random numbers of row r, columns 8 g ..
+__device__ __forceinline__ void drop_numbers(const Drop &d, uint64_t offset, uint32_t r, uint32_t g, uint32_t *x) {
+    x[0] = g, x[1] = r, x[2] = (uint32_t)offset, x[3] = (uint32_t)(offset >> 32);
     uint32_t k0 = (uint32_t)d.seed, k1 = (uint32_t)(d.seed >> 32);
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
@@ -222,12 +222,21 @@ __device__ __forceinline__ void dropped(const Drop &d, uint64_t offset, uint32_t
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
+}
+// Eight elements under their numbers.
+__device__ __forceinline__ void dropped_by(const Drop &d, const uint32_t *x, Eight &e) {
     const uint32_t high = d.below << 16;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 v = e.v[i] * both(d.factor);
         e.v[i] = make_float2((x[i] << 16) >= high ? v.x : 0.f, x[i] >= high ? v.y : 0.f);
     }
+}
+// The piece's elements under dropout: row r, columns 8 g ..
+__device__ __forceinline__ void dropped(const Drop &d, uint64_t offset, uint32_t r, uint32_t g, Eight &e) {
+    uint32_t x[4];
+    drop_numbers(d, offset, r, g, x);
+    dropped_by(d, x, e);
 }
 
 }  // namespace

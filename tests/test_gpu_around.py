@@ -337,6 +337,33 @@ def test_residual_norm_backward(lib, nn, i, dtype):
         assert torch.equal(dy.t, first[0]) and dy.surroundings_untouched()
 
 
+@pytest.mark.parametrize("n,m", [(40, 61), (517, 100), (2311, 40), (1000, 9), (8, 33), (3, 50)])
+@pytest.mark.parametrize("gate_rows", [1, 3, 1000])
+def test_gradients_do_not_depend_on_where_matrices_lie(lib, nn, m, n, gate_rows):
+    """All on the 16-byte grid, all off it alike, each otherwise: sums over the same values in other orders."""
+    g = gen(n)
+    vals = [(randn(g, m, n) * s).to(torch.bfloat16) for s in (1.0, 1.0, 2.0, 1.0)]
+    w1, w2, c2 = randn(g, n), randn(g, n), randn(g, n)
+    gate = randn(g, -(-m // gate_rows), n).to(torch.bfloat16)
+    results = []
+    for pads in ((-n % 8,) * 4, (-n % 8 + 3,) * 4, (0, 1, 2, 5)):
+        dy, dh, y, b = (Buf(m, n, torch.bfloat16, p, 0 if p == pads[0] and len(set(pads)) == 1 else i, v).t
+                        for i, (p, v) in enumerate(zip(pads, vals)))
+        if len(set(pads)) == 1 and pads[0] % 8:
+            assert len({t.data_ptr() % 16 for t in (dy, dh, y, b)}) == 1
+        dr, db = torch.empty_like(vals[0]), torch.empty_like(vals[0])
+        f = [torch.empty(n, device="cuda") for _ in range(4)]
+        dg = torch.empty(gate.shape, device="cuda")
+        lib.emtk_residual_norm_backward(nn, dy, dh, y, b, dr, db, post=lib.Norm("layer", w1, c2), pre=lib.Norm("rms", w2), gate=gate, gate_every=gate_rows,
+                                        drop=lib.Drop(0.2, 5, 6), d_gate=dg, dw_pre=f[0], db_pre=f[1], dw_post=f[2], db_post=f[3])
+        results.append([dr, db, dg] + f)
+    for other in results[1:]:
+        assert torch.equal(other[0], results[0][0]) and torch.equal(other[1], results[0][1])
+        for a, z in zip(results[0][2:], other[2:]):
+            # m terms each, added in another order: their magnitudes are within the largest times m
+            assert (a - z).abs().max() <= (m / 8 + 16) * 2.0 ** -23 * m * 40
+
+
 def test_residual_norm_gradients_against_differences(lib, nn):
     """The backward call against differences of the definition that the forward call is held to."""
     m, n, eps = 3, 24, 1e-3
