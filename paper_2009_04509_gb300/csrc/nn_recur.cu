@@ -39,7 +39,7 @@ namespace {
 
 constexpr int kLanes = 16, kCols = 2 * kLanes;  // two columns a lane
 constexpr int kRuns = 8, kLen = 16, kTile = kRuns * kLen, kThreads = kLanes * kRuns;
-constexpr int kShort = 8;  // steps up to which a thread takes a whole sequence
+constexpr int kShort = 8;  // steps of a sequence, on average, up to which a thread takes all of it
 static_assert(kTile == EMTK_RECURRENCE_STEP, "states are kept once a tile");
 
 // Where what is kept of a sequence's tile lies: tiles of different sequences, in order and with gaps.
@@ -186,15 +186,28 @@ constexpr int kPlane = kTile * kLanes;  // words
 // The words of a thread's run: word i is its step i.
 __device__ __forceinline__ uint32_t *run_of(uint32_t *plane, int run, int lane) { return plane + run * kLen * kLanes + lane; }
 
-// Rows row .. row + kTile - 1 into `plane`, those from `end` on as `fill`, by all threads.
+// Rows row .. row + kTile - 1 into `plane`, those from `end` on as `fill`, by all threads; a
+// thread's loads together.
 __device__ __forceinline__ void fill_plane(uint32_t *plane, const Plane &a, int64_t row, int64_t end, int col, int valid, bool words,
                                            uint32_t fill) {
-    const int lane = threadIdx.x % kLanes;
-    int r = threadIdx.x / kLanes;
-    const uint8_t *p = place(a, row + r, col);
-#pragma unroll 8
-    for (int i = 0; i < kLen; ++i, r += kRuns, p += kRuns * a.row_bytes)
-        plane[r * kLanes + lane] = row + r < end ? load_pair(p, valid, words) : fill;
+    const int lane = threadIdx.x % kLanes, r0 = threadIdx.x / kLanes;
+    const uint8_t *p = place(a, row + r0, col);
+    const int left = (int)min((int64_t)kTile, end - row) - r0;  // rows from the thread's first on
+    uint32_t v[kLen];
+    if (words && valid == 2) {
+#pragma unroll
+        for (int i = 0; i < kLen; ++i, p += kRuns * a.row_bytes) v[i] = i * kRuns < left ? __ldg(reinterpret_cast<const uint32_t *>(p)) : fill;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLen; ++i, p += kRuns * a.row_bytes) {
+            const uint16_t *const h = reinterpret_cast<const uint16_t *>(p);
+            const uint32_t lo = i * kRuns < left && valid > 0 ? __ldg(h) : fill & 0xffffu;
+            const uint32_t hi = i * kRuns < left && valid > 1 ? __ldg(h + 1) : fill >> 16;
+            v[i] = lo | hi << 16;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kLen; ++i) plane[(r0 + i * kRuns) * kLanes + lane] = v[i];
 }
 __device__ __forceinline__ void empty_plane(const uint32_t *plane, const Plane &a, int64_t row, int64_t end, int col, int valid, bool words) {
     const int lane = threadIdx.x % kLanes;
@@ -227,6 +240,8 @@ __device__ __forceinline__ float4 local_run(const uint32_t *f, const uint32_t *x
     return make_float4(factor_of(product.x, rest.x), factor_of(product.y, rest.y), h.x, h.y);
 }
 
+// Of a run without steps: it keeps all and makes nothing.
+__device__ __forceinline__ float4 no_run() { return make_float4(-0.f, -0.f, 0.f, 0.f); }
 // The same from its end, for p.
 template <bool F16, int ACT>
 __device__ __forceinline__ float2 local_back(const float2 (&m)[kLen], const uint32_t *d, const uint32_t *o, bool gated) {
@@ -348,11 +363,12 @@ __global__ void __launch_bounds__(kThreads, 4) recur_kernel(const __grid_constan
             if (gated) fill_plane(stage + 2 * kPlane, a.o, row, u.r1, u.col, u.valid, words, 0u);
             __syncthreads();
         }
-        if (count < kLen) mask_run<3>(stage, u.run, u.lane, count, kFill);
+        const bool work = __any_sync(0xffffffffu, count > 0);  // of the warp's two runs
+        if (work && count < kLen) mask_run<3>(stage, u.run, u.lane, count, kFill);
         const uint32_t *const f = run_of(stage, u.run, u.lane), *const o = run_of(stage + 2 * kPlane, u.run, u.lane);
         uint32_t *const x = run_of(stage + kPlane, u.run, u.lane);
         float2 m[kLen], h;
-        runs[turn][u.run][u.lane] = local_run<F16>(f, x, m);
+        runs[turn][u.run][u.lane] = work ? local_run<F16>(f, x, m) : no_run();
         __syncthreads();
         if (TMA && i > 0) {  // the other stage's results have been read: its next tile
             if (threadIdx.x == 0) bulk_wait_read();
@@ -364,11 +380,13 @@ __global__ void __launch_bounds__(kThreads, 4) recur_kernel(const __grid_constan
             if (r == u.run) h = carry;
             carry = then(carry, runs[turn][r][u.lane]);
         }
+        if (work) {
 #pragma unroll
-        for (int j = 0; j < kLen; ++j) {
-            h = step(m[j], h, values_of<F16>(x[j * kLanes]));
-            const float2 y = gated ? h * act2<ACT>(values_of<F16>(o[j * kLanes])) : h;
-            x[j * kLanes] = pack16<F16>(y.x, y.y);
+            for (int j = 0; j < kLen; ++j) {
+                h = step(m[j], h, values_of<F16>(x[j * kLanes]));
+                const float2 y = gated ? h * act2<ACT>(values_of<F16>(o[j * kLanes])) : h;
+                x[j * kLanes] = pack16<F16>(y.x, y.y);
+            }
         }
         if (TMA) bulk_fence();
         __syncthreads();
@@ -382,6 +400,29 @@ __global__ void __launch_bounds__(kThreads, 4) recur_kernel(const __grid_constan
     }
     if (a.last && !a.starts && u.run == 0) store_state(a.last, u.seq, n, u.col, u.valid, carry);
     if (TMA) pipe_end(pipe);
+}
+
+// A step's gradients, from the states before and after it and the p that comes into it, which
+// becomes the one that leaves it.
+struct Slopes {
+    float2 df, dx;
+};
+template <bool F16, int ACT>
+__device__ __forceinline__ Slopes slopes(float2 m, float2 before, float2 after, uint32_t wf, uint32_t wx, uint32_t wo, uint32_t wd, bool gated,
+                                         float2 &p, float2 &d_o) {
+    const float2 dy = values_of<F16>(wd);
+    float2 g = p + dy;
+    if (gated) {
+        const float2 o = values_of<F16>(wo);
+        float2 act, slope;
+        act_slope<ACT>(o.x, act.x, slope.x);
+        act_slope<ACT>(o.y, act.y, slope.y);
+        g = fma2(dy, act, p);
+        d_o = dy * slope * after;
+    }
+    const float2 f = values_of<F16>(wf), slope_f = make_float2(slope_of(f.x, m.x), slope_of(f.y, m.y));
+    p = kept(m, g);
+    return {g * (before - values_of<F16>(wx)) * slope_f, -m * g};
 }
 
 // Backwards: the tiles of a sequence from its last, or (a.starts) a tile.
@@ -430,13 +471,14 @@ __global__ void __launch_bounds__(kThreads, 3) recur_grad_kernel(const __grid_co
             fill_plane(stage + 3 * kPlane, a.dy, row, u.r1, u.col, u.valid, words, 0u);
             __syncthreads();
         }
-        if (count < kLen) mask_run<4>(stage, u.run, u.lane, count, kFill);
+        const bool work = __any_sync(0xffffffffu, count > 0);
+        if (work && count < kLen) mask_run<4>(stage, u.run, u.lane, count, kFill);
         uint32_t *const f = run_of(stage, u.run, u.lane), *const x = run_of(stage + kPlane, u.run, u.lane),
                  *const o = run_of(stage + 2 * kPlane, u.run, u.lane);
         const uint32_t *const d = run_of(stage + 3 * kPlane, u.run, u.lane);
         float2 m[kLen], p;
-        runs[turn][u.run][u.lane] = local_run<F16>(f, x, m);
-        back[turn][u.run][u.lane] = local_back<F16, ACT>(m, d, o, gated);
+        runs[turn][u.run][u.lane] = work ? local_run<F16>(f, x, m) : no_run();
+        back[turn][u.run][u.lane] = work ? local_back<F16, ACT>(m, d, o, gated) : both(0.f);
         __syncthreads();
         if (TMA && i > 0) {
             if (threadIdx.x == 0) bulk_wait_read();
@@ -448,29 +490,21 @@ __global__ void __launch_bounds__(kThreads, 3) recur_grad_kernel(const __grid_co
             const float4 c = runs[turn][r][u.lane];
             carry = back[turn][r][u.lane] + times(make_float2(c.x, c.y), carry);
         }
-        for (int r = 0; r < u.run; ++r) h = then(h, runs[turn][r][u.lane]);
-        float2 before[kLen + 1];  // the state before each step, and after the last
-        before[0] = h;
+        if (work) {
+            for (int r = 0; r < u.run; ++r) h = then(h, runs[turn][r][u.lane]);
+            float2 before[kLen + 1];  // the state before each step, and after the last
+            before[0] = h;
 #pragma unroll
-        for (int j = 0; j < kLen; ++j) before[j + 1] = step(m[j], before[j], values_of<F16>(x[j * kLanes]));
+            for (int j = 0; j < kLen; ++j) before[j + 1] = step(m[j], before[j], values_of<F16>(x[j * kLanes]));
 #pragma unroll
-        for (int j = kLen - 1; j >= 0; --j) {
-            const float2 dy = values_of<F16>(d[j * kLanes]), xj = values_of<F16>(x[j * kLanes]);
-            float2 g = p + dy;
-            if (gated) {
-                const float2 oj = values_of<F16>(o[j * kLanes]);
-                float2 act, slope;
-                act_slope<ACT>(oj.x, act.x, slope.x);
-                act_slope<ACT>(oj.y, act.y, slope.y);
-                g = fma2(dy, act, p);
-                const float2 d_o = dy * slope * before[j + 1];
-                o[j * kLanes] = pack16<F16>(d_o.x, d_o.y);
+            for (int j = kLen - 1; j >= 0; --j) {
+                float2 d_o;
+                const Slopes g = slopes<F16, ACT>(m[j], before[j], before[j + 1], f[j * kLanes], x[j * kLanes], gated ? o[j * kLanes] : 0u,
+                                                  d[j * kLanes], gated, p, d_o);
+                f[j * kLanes] = pack16<F16>(g.df.x, g.df.y);
+                x[j * kLanes] = pack16<F16>(g.dx.x, g.dx.y);
+                if (gated) o[j * kLanes] = pack16<F16>(d_o.x, d_o.y);
             }
-            const float2 fj = values_of<F16>(f[j * kLanes]), slope_f = make_float2(slope_of(fj.x, m[j].x), slope_of(fj.y, m[j].y));
-            const float2 dx = -m[j] * g, df = g * (before[j] - xj) * slope_f;
-            f[j * kLanes] = pack16<F16>(df.x, df.y);
-            x[j * kLanes] = pack16<F16>(dx.x, dx.y);
-            p = kept(m[j], g);
         }
         if (TMA) bulk_fence();
         __syncthreads();
@@ -527,11 +561,12 @@ __global__ void __launch_bounds__(kThreads) tile_sum_kernel(const __grid_constan
         __syncthreads();
     }
     const int count = (int)max(min((int64_t)kLen, u.r1 - row - u.run * kLen), (int64_t)0);
-    if (count < kLen) mask_run<BACK ? 4 : 2>(planes, u.run, u.lane, count, kFill);
+    const bool work = __any_sync(0xffffffffu, count > 0);
+    if (work && count < kLen) mask_run<BACK ? 4 : 2>(planes, u.run, u.lane, count, kFill);
     float2 m[kLen];
     const uint32_t *const x = run_of(planes + kX * kPlane, u.run, u.lane);
-    float4 mine = local_run<F16>(run_of(planes, u.run, u.lane), x, m);
-    if (BACK) {
+    float4 mine = work ? local_run<F16>(run_of(planes, u.run, u.lane), x, m) : no_run();
+    if (BACK && work) {
         const float2 p = local_back<F16, ACT>(m, x, run_of(planes + 2 * kPlane, u.run, u.lane), gated);
         mine.z = p.x;
         mine.w = p.y;
@@ -606,7 +641,7 @@ __global__ void __launch_bounds__(32 * kScanWarps) tile_scan_kernel(const __grid
     if (end && in && warp == 0) end[(int64_t)seq * n + col] = carry;
 }
 
-// Sequences of up to kShort steps, all of one length: two columns of one to a thread.
+// Short sequences: two columns of one to a thread, step by step, kShort steps' loads together.
 template <bool F16, int ACT>
 __global__ void __launch_bounds__(256) recur_short_kernel(const __grid_constant__ RecurArgs a) {
     const int pairs = (a.at.n + 1) / 2, n = a.at.n;
@@ -617,19 +652,78 @@ __global__ void __launch_bounds__(256) recur_short_kernel(const __grid_constant_
     pdl_trigger();
     pdl_wait();
     if (s >= a.at.seqs) return;
-    const int64_t r0 = s * a.at.length;
+    int r0, r1;
+    a.at.rows_of((int)s, r0, r1);
     float2 h = a.state ? load_state(a.state, s, n, col, valid) : both(0.f);
-    if (a.states) store_state(a.states, r0 / kTile + s, n, col, valid, h);
+    for (int first = r0; first < r1; first += kShort) {
+        uint32_t f[kShort], x[kShort], o[kShort];
 #pragma unroll
-    for (int i = 0; i < kShort; ++i) {
-        if (i >= a.at.length) break;
-        const uint32_t f = load_pair(place(a.f, r0 + i, col), valid, words), x = load_pair(place(a.x, r0 + i, col), valid, words);
-        const uint32_t o = gated ? load_pair(place(a.o, r0 + i, col), valid, words) : 0u;
-        h = step(minus_rest<F16>(f), h, values_of<F16>(x));
-        const float2 y = gated ? h * act2<ACT>(values_of<F16>(o)) : h;
-        store_pair(place(a.y, r0 + i, col), valid, words, pack16<F16>(y.x, y.y));
+        for (int i = 0; i < kShort; ++i) {
+            if (first + i >= r1) break;
+            f[i] = load_pair(place(a.f, first + i, col), valid, words);
+            x[i] = load_pair(place(a.x, first + i, col), valid, words);
+            if (gated) o[i] = load_pair(place(a.o, first + i, col), valid, words);
+        }
+#pragma unroll
+        for (int i = 0; i < kShort; ++i) {
+            if (first + i >= r1) break;
+            if (a.states && (first + i - r0) % kTile == 0) store_state(a.states, place_of(r0, (first + i - r0) / kTile, (int)s), n, col, valid, h);
+            h = step(minus_rest<F16>(f[i]), h, values_of<F16>(x[i]));
+            const float2 y = gated ? h * act2<ACT>(values_of<F16>(o[i])) : h;
+            store_pair(place(a.y, first + i, col), valid, words, pack16<F16>(y.x, y.y));
+        }
     }
     if (a.last) store_state(a.last, s, n, col, valid, h);
+}
+
+// The same backwards, from the last steps on; the state before each lot of steps is had from the
+// one that was kept, the first step's where the sequence is short.
+template <bool F16, int ACT>
+__global__ void __launch_bounds__(256) recur_short_grad_kernel(const __grid_constant__ RecurGradArgs a) {
+    const int pairs = (a.at.n + 1) / 2, n = a.at.n;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t s = at / pairs;
+    const int col = (int)(at - s * pairs) * 2, valid = min(n - col, 2);
+    const bool words = a.words != 0, gated = a.o.p != nullptr;
+    pdl_trigger();
+    pdl_wait();
+    if (s >= a.at.seqs) return;
+    int r0, r1;
+    a.at.rows_of((int)s, r0, r1);
+    float2 p = a.d_last ? load_state(a.d_last, s, n, col, valid) : both(0.f);
+    for (int lot = (r1 - r0 - 1) / kShort; r1 > r0 && lot >= 0; --lot) {
+        const int first = r0 + lot * kShort, tile = lot * kShort / kTile;
+        uint32_t wf[kShort], wx[kShort], wo[kShort], wd[kShort];
+#pragma unroll
+        for (int i = 0; i < kShort; ++i) {
+            if (first + i >= r1) break;
+            wf[i] = load_pair(place(a.f, first + i, col), valid, words);
+            wx[i] = load_pair(place(a.x, first + i, col), valid, words);
+            wd[i] = load_pair(place(a.dy, first + i, col), valid, words);
+            if (gated) wo[i] = load_pair(place(a.o, first + i, col), valid, words);
+        }
+        float2 h = load_state(a.states, place_of(r0, tile, (int)s), n, col, valid);
+        for (int row = r0 + tile * kTile; row < first; ++row)
+            h = step(minus_rest<F16>(load_pair(place(a.f, row, col), valid, words)), h, values_of<F16>(load_pair(place(a.x, row, col), valid, words)));
+        float2 m[kShort], before[kShort + 1];
+        before[0] = h;
+#pragma unroll
+        for (int i = 0; i < kShort; ++i) {
+            if (first + i >= r1) break;
+            m[i] = minus_rest<F16>(wf[i]);
+            before[i + 1] = step(m[i], before[i], values_of<F16>(wx[i]));
+        }
+#pragma unroll
+        for (int i = kShort - 1; i >= 0; --i) {
+            if (first + i >= r1) continue;
+            float2 d_o;
+            const Slopes g = slopes<F16, ACT>(m[i], before[i], before[i + 1], wf[i], wx[i], wo[i], wd[i], gated, p, d_o);
+            if (a.df.p) store_pair(place(a.df, first + i, col), valid, words, pack16<F16>(g.df.x, g.df.y));
+            if (a.dx.p) store_pair(place(a.dx, first + i, col), valid, words, pack16<F16>(g.dx.x, g.dx.y));
+            if (a.d_o.p) store_pair(place(a.d_o, first + i, col), valid, words, pack16<F16>(d_o.x, d_o.y));
+        }
+    }
+    if (a.d_state) store_state(a.d_state, s, n, col, valid, p);
 }
 
 // ---------------------------------------------------------------- host
@@ -637,11 +731,18 @@ bool on_words(const emtk_matrix &m, int rows) {
     return !m.d || (reinterpret_cast<uintptr_t>(m.d) % 4 == 0 && (rows <= 1 || m.ld % 2 == 0));
 }
 
-// Whether blocks go along whole sequences: all of one length, and three units (32 columns
-// of one) to every two SMs.  20000 rows of 2048 columns, forward and backward: 256 units 107 and
-// 187 us, as independent tiles 103 and 212; 64 units 281 and 535, independent 95 and 202;
-// 1024 units (of 1250 rows) 59 and 134, independent as with 64.
-bool along(int seqs, int col_tiles, int sms) { return 2 * (int64_t)seqs * col_tiles >= 3 * sms; }
+// Whether blocks go along whole sequences: three units (32 columns of one) to every two
+// SMs, and all of one length, or not so long that one of them would keep the others
+// waiting.  20000 rows of 2048 columns, forward and backward: 256 units 107 and 187 us, as
+// independent tiles 103 and 212; 64 units 281 and 535, independent 95 and 202; 1024 units (of 1250 rows)
+// 59 and 134, independent as with 64.  16896 rows of 498 columns in 88 sequences of unlike lengths:
+// both passes 410 us as independent tiles, most of whose places are empty.
+bool along(bool uniform, int rows, int seqs, int col_tiles, int sms) {
+    return 2 * (int64_t)seqs * col_tiles >= 3 * sms && (uniform || rows / seqs <= 4 * kTile);
+}
+// Whether a thread takes a whole sequence: a tile would be nearly empty.  Backwards, a sequence
+// longer than kShort steps costs a thread its square, so unlike lengths have to be shorter.
+bool step_by_step(bool uniform, bool forward, int rows, int seqs) { return rows / seqs <= (uniform || forward ? kShort : kShort / 4); }
 int64_t places(int rows, int seqs) { return (int64_t)rows / kTile + seqs; }
 
 // Workspace of independent tiles: (q, H) and, where they are not kept anyway, the starts.
@@ -662,6 +763,12 @@ cudaError_t run_tiles(Kernel kernel, int planes, bool tma, const Args &a, const 
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(kThreads), shared_bytes(planes, tma, whole), s, a, maps);
 }
 
+template <typename Args>
+cudaError_t run_short(void (*kernel)(const Args), const Args &a, cudaStream_t s) {
+    const int64_t blocks = ((int64_t)a.at.seqs * ((a.at.n + 1) / 2) + 255) / 256;
+    return grid_ok(blocks) ? launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), 0, s, a) : cudaErrorInvalidValue;
+}
+
 // Each tile's start, by the first two kernels.
 template <bool F16, int ACT, bool BACK>
 cudaError_t run_starts(const RecurGradArgs &a, const Tiles *maps, void *workspace, const float *begin, float *starts, float *end,
@@ -679,12 +786,8 @@ cudaError_t run_starts(const RecurGradArgs &a, const Tiles *maps, void *workspac
 
 template <bool F16, int ACT>
 cudaError_t run(RecurArgs a, const Tiles *maps, void *workspace, int sms, cudaStream_t s) {
-    if (!a.at.offsets && a.at.length <= kShort) {
-        const int64_t blocks = ((int64_t)a.at.seqs * ((a.at.n + 1) / 2) + 255) / 256;
-        if (!grid_ok(blocks)) return cudaErrorInvalidValue;
-        return launch_pdl(recur_short_kernel<F16, ACT>, dim3((unsigned)blocks), dim3(256), 0, s, a);
-    }
-    if (a.at.offsets || !along(a.at.seqs, a.col_tiles, sms)) {
+    if (step_by_step(!a.at.offsets, true, a.at.rows, a.at.seqs)) return run_short(recur_short_kernel<F16, ACT>, a, s);
+    if (!along(!a.at.offsets, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
         RecurGradArgs g{};
         g.f = a.f;
         g.x = a.x;
@@ -701,7 +804,8 @@ cudaError_t run(RecurArgs a, const Tiles *maps, void *workspace, int sms, cudaSt
 }
 template <bool F16, int ACT>
 cudaError_t run(RecurGradArgs a, const Tiles *maps, void *workspace, int sms, cudaStream_t s) {
-    if (a.at.offsets || !along(a.at.seqs, a.col_tiles, sms)) {
+    if (step_by_step(!a.at.offsets, false, a.at.rows, a.at.seqs)) return run_short(recur_short_grad_kernel<F16, ACT>, a, s);
+    if (!along(!a.at.offsets, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
         float *const starts = sums_in(workspace, places(a.at.rows, a.at.seqs), a.at.n).made + places(a.at.rows, a.at.seqs) * a.at.n;
         const cudaError_t e = run_starts<F16, ACT, true>(a, maps, workspace, a.d_last, starts, a.d_state, s);
         if (e != cudaSuccess) return e;
@@ -759,8 +863,8 @@ cudaError_t init_recur_kernels() {
 }
 
 size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, bool forward, int sms) {
-    if (n == 0 || seqs == 0 || (uniform && forward && rows / seqs <= kShort)) return 0;
-    const bool whole = uniform && along(seqs, (n + kCols - 1) / kCols, sms);
+    if (n == 0 || seqs == 0 || step_by_step(uniform, forward, rows, seqs)) return 0;
+    const bool whole = along(uniform, rows, seqs, (n + kCols - 1) / kCols, sms);
     return whole ? 0 : 3 * sizeof(float) * places(rows, seqs) * n;
 }
 
@@ -779,7 +883,7 @@ cudaError_t launch_recurrence(const emtk_recurrence_args &p, void *workspace, co
     a.words = on_words(p.f, p.rows) && on_words(p.x, p.rows) && on_words(p.o, p.rows) && on_words(p.y, p.rows);
     Tiles maps;
     const emtk_matrix *const in[] = {&p.f, &p.x, &p.o}, *const out[] = {&p.y};
-    const bool tma = (p.offsets || a.at.length > kShort) && make_maps(nn, maps, in, out, p.rows, p.n);
+    const bool tma = !step_by_step(!p.offsets, true, p.rows, p.seqs) && make_maps(nn, maps, in, out, p.rows, p.n);
     return p.type == EMTK_TYPE_F16 ? run<true>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s)
                                    : run<false>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s);
 }
@@ -803,7 +907,7 @@ cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, void *wor
               on_words(p.df, p.rows) && on_words(p.dx, p.rows) && on_words(p.d_o, p.rows);
     Tiles maps;
     const emtk_matrix *const in[] = {&p.f, &p.x, &p.o, &p.dy}, *const out[] = {&p.df, &p.dx, &p.d_o};
-    const bool tma = make_maps(nn, maps, in, out, p.rows, p.n);
+    const bool tma = !step_by_step(!p.offsets, false, p.rows, p.seqs) && make_maps(nn, maps, in, out, p.rows, p.n);
     return p.type == EMTK_TYPE_F16 ? run<true>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s)
                                    : run<false>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s);
 }

@@ -620,6 +620,8 @@ def recur_case(i):
     r = random.Random(50 + i)
     lengths = r.choice([[1], [5], [8], [9], [127], [128], [129], [300], [700], [1025], [2600], [1] * 70, [3] * 40, [8] * 9, [64] * 5, [130] * 3, [300] * 20,
                         [5, 0, 131, 1, 260, 0], [0, 0], [2000, 3, 700], [1] * 5 + [0] * 3 + [1200]])
+    if i >= 48:  # short ones on average, one of them long; lots of steps that end inside one; runs without steps
+        lengths = [[1] * 300 + [1500], [2, 0, 7, 9, 8, 16, 17, 0, 1], [24] * 90, [100] * 60, [1, 40, 17, 16, 130] * 12][i - 48]
     uniform = len(set(lengths)) == 1 and lengths[0] > 0
     return dict(lengths=lengths, offsets=not uniform or r.random() < 0.4, lead=r.choice([0, 0, 3]), tail=r.choice([0, 0, 5]),
                 n=r.choice([1, 2, 7, 31, 32, 33, 64, 100]), act=r.choice(["none", "relu", "gelu", "silu", "sigmoid"]), gated=r.random() < 0.7,
@@ -627,7 +629,7 @@ def recur_case(i):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-@pytest.mark.parametrize("i", range(48))
+@pytest.mark.parametrize("i", range(53))
 def test_recurrence(lib, nn, i, dtype):
     """Both passes.  An error of b of a few E (and |f| E, of the exponential) moves the state by so much of max |x - h|;
     the roundings of a step stay for as long as the state does, at most min(T, 1 / b) steps.  A step passes g - b g on,
