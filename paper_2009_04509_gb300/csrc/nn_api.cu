@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <new>
 
 #include "emtk_internal.h"
@@ -162,6 +163,30 @@ emtk_matrix Staging::operator()(const emtk_matrix &m, int rows, int cols) {
     Copy16 &c = copies[n++];
     c = {m, {ws.take(2 * (size_t)rows * ld16(cols)), ld16(cols), nullptr, 0}, rows, cols};
     return c.to;
+}
+
+// The workspace of a recurrence's call, which begins with what its kernels leave each other;
+// inputs that are to be read from a copy there become that copy.
+template <typename Args>
+emtk_status recurrence_inputs(emtk_nn *nn, const Args &a, std::initializer_list<emtk_matrix *> inputs, bool forward, cudaStream_t s) {
+    const bool uniform = a.offsets == nullptr;
+    const size_t kept = recurrence_workspace(a.rows, a.n, a.seqs, uniform, forward, nn->sm_count);
+    CallSpace ws{nn};
+    Staging stage{ws};
+    for (int pass = 0; pass < 2; ++pass) {
+        stage.n = 0;
+        ws.take(kept);
+        for (emtk_matrix *m : inputs) {
+            if (!recurrence_copies(*m, a.rows, a.n, a.seqs, uniform, forward)) continue;
+            const emtk_matrix there = stage(*m, a.rows, a.n);
+            if (pass == 1) *m = there;
+        }
+        if (pass == 0) {
+            const emtk_status st = ws.ensure(s);
+            if (st != EMTK_OK) return st;
+        }
+    }
+    return status_of(launch_copy16((emtk_type)a.type, stage.copies, stage.n, nn->sm_count, s));
 }
 
 MmOperand rows_of(const emtk_matrix &m) { return {m.d, m.ld, false}; }
@@ -705,10 +730,10 @@ emtk_status emtk_recurrence(emtk_nn *nn, const emtk_recurrence_args *p, emtk_str
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk recurrence");
-    void *space = nullptr;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const emtk_status st = one_space(nn, recurrence_workspace(a.rows, a.n, a.seqs, a.offsets == nullptr, true, nn->sm_count), s, &space);
-    return st != EMTK_OK ? st : status_of(launch_recurrence(a, space, nn, s));
+    emtk_recurrence_args b = a;
+    const emtk_status st = recurrence_inputs(nn, a, {&b.f, &b.x, &b.o}, true, s);
+    return st != EMTK_OK ? st : status_of(launch_recurrence(b, nn->ws, nn, s));
 }
 
 emtk_status emtk_recurrence_backward(emtk_nn *nn, const emtk_recurrence_grad_args *p, emtk_stream stream) {
@@ -734,10 +759,10 @@ emtk_status emtk_recurrence_backward(emtk_nn *nn, const emtk_recurrence_grad_arg
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk recurrence backward");
-    void *space = nullptr;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const emtk_status st = one_space(nn, recurrence_workspace(a.rows, a.n, a.seqs, a.offsets == nullptr, false, nn->sm_count), s, &space);
-    return st != EMTK_OK ? st : status_of(launch_recurrence_grad(a, space, nn, s));
+    emtk_recurrence_grad_args b = a;
+    const emtk_status st = recurrence_inputs(nn, a, {&b.f, &b.x, &b.o, &b.dy}, false, s);
+    return st != EMTK_OK ? st : status_of(launch_recurrence_grad(b, nn->ws, nn, s));
 }
 
 }  // extern "C"

@@ -87,6 +87,7 @@ struct Waits {  // of the kernels' bounded waits
 constexpr int kMostIn = 4;  // matrices of a tile: f, x, o and dy, in this order
 struct Tiles {
     CUtensorMap in[kMostIn], out[3];  // out: y, or df, dx, d_o; of what is there
+    int store;                        // whole tiles of results leave by TMA
     Waits waits;
 };
 
@@ -276,9 +277,9 @@ struct Unit {
 };
 
 // Tiles on their way: two stages of planes, filled by TMA a tile ahead, one barrier each.
-// A stage's results take its inputs' places and leave by TMA too, where rows are whole
-// pieces of 16 bytes (at 31 columns a store wrote the 32nd, the caller's padding); it is
-// filled again once they are read, in the middle of the next tile.
+// A stage's results take its inputs' places and leave by TMA too, where they lie on its
+// grid and rows are whole pieces of 16 bytes (at 31 columns a store wrote the 32nd, the
+// caller's padding); it is filled again once they are read, in the middle of the next tile.
 struct Pipe {
     uint32_t *stages;  // [2][planes][kPlane]
     uint64_t *full;    // [2]
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 4) recur_kernel(const __grid_constan
         }
         if (TMA) bulk_fence();
         __syncthreads();
-        if (TMA && n % 8 == 0 && row + kTile <= u.r1) {
+        if (TMA && maps.store && row + kTile <= u.r1) {
             if (threadIdx.x == 0) bulk_store(&maps.out[0], smem_u32(stage + kPlane), u.col0, (int)row);
         } else {
             empty_plane(stage + kPlane, a.y, row, u.r1, u.col, u.valid, words);
@@ -509,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 3) recur_grad_kernel(const __grid_co
         if (TMA) bulk_fence();
         __syncthreads();
         const Plane *const out[3] = {&a.df, &a.dx, &a.d_o};
-        if (TMA && n % 8 == 0 && row + kTile <= u.r1) {
+        if (TMA && maps.store && row + kTile <= u.r1) {
             if (threadIdx.x == 0) {
 #pragma unroll
                 for (int k = 0; k < 3; ++k)
@@ -825,17 +826,17 @@ cudaError_t run(const Args &a, const Tiles *maps, void *workspace, int act, int 
     }
 }
 
-// Tensor maps of the matrices that are there; false if one lies off TMA's 16-byte grid.
+// Tensor maps of the matrices that are there; false if one that is read lies off TMA's grid.
 template <int IN, int OUT>
 bool make_maps(const emtk_nn *nn, Tiles &t, const emtk_matrix *const (&in)[IN], const emtk_matrix *const (&out)[OUT], int rows, int n) {
     t.waits = {nn->status, nn->timeout_ns};
     for (const emtk_matrix *m : in)
         if (m->d && !mm_operand_ok(m->d, m->ld, rows)) return false;
-    for (const emtk_matrix *m : out)
-        if (m->d && !mm_operand_ok(m->d, m->ld, rows)) return false;
+    t.store = n % 8 == 0;
+    for (const emtk_matrix *m : out) t.store = t.store && (!m->d || mm_operand_ok(m->d, m->ld, rows));
     for (int i = 0; i < IN; ++i)
         if (in[i]->d && !encode_rows(nn, &t.in[i], *in[i], rows, n, kCols, kTile)) return false;
-    for (int i = 0; i < OUT; ++i)
+    for (int i = 0; t.store && i < OUT; ++i)
         if (out[i]->d && !encode_rows(nn, &t.out[i], *out[i], rows, n, kCols, kTile)) return false;
     return rows > 0;
 }
@@ -860,6 +861,15 @@ cudaError_t init_kernels() {
 cudaError_t init_recur_kernels() {
     const cudaError_t e = init_kernels<false>();
     return e == cudaSuccess ? init_kernels<true>() : e;
+}
+
+// An input that only loads of two bytes reach is copied to rows that TMA reads, where there is much of
+// it. 800 x 1000 steps of 64 columns, an element off the grid, forward and backward: 294 and 603 us as
+// they lie, 195 and 377 copied; 88 x 192 of 498: 39 and 129, 45 and 91. Two elements off it stay where
+// they lie: 147 and 351, 189 and 345.
+bool recurrence_copies(const emtk_matrix &m, int rows, int n, int seqs, bool uniform, bool forward) {
+    const bool odd = (reinterpret_cast<uintptr_t>(m.d) | (uintptr_t)m.ld * 2) & 3;
+    return m.d && odd && (int64_t)rows * n >= (forward ? 10 : 4) << 20 && !step_by_step(uniform, forward, rows, seqs);
 }
 
 size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, bool forward, int sms) {

@@ -714,6 +714,31 @@ def test_recurrence_step_by_step_is_the_whole(lib, nn):
         near(whole, y.double(), "bf16", 2.0 ** -8 * y.double().abs() + 4 * 340 * E * top)
 
 
+@pytest.mark.parametrize("pad", [0, 1, 3])
+def test_recurrence_of_many_values(lib, nn, pad):
+    """Large enough that inputs off the 16-byte grid are copied first: the same bits as on it, and nothing beside the outputs."""
+    lengths = [5000, 0, 17, 4200, 1401]
+    at = np.cumsum([0] + lengths).tolist()
+    rows, n, seqs = at[-1], 1000, len(lengths)
+    g = gen(7)
+    vals = [(randn(g, rows, n) + (2.0 if i == 0 else 0.0)).to(torch.bfloat16) for i in range(4)]
+    assert rows * n >= 10 << 20
+    results = []
+    for p in (0, pad):
+        f, x, o, dy = (Buf(rows, n, torch.bfloat16, p, 0, v) for v in vals)
+        outs = [Buf(rows, n, torch.bfloat16, p, 0) for _ in range(4)]
+        for offsets in (torch.tensor(at, dtype=torch.int32, device="cuda"), None):
+            k = seqs if offsets is not None else 2
+            kept = lib.emtk_recurrence_states(rows, n, k)
+            shared = dict(o=o.t, act="gelu", seqs=k, offsets=offsets)
+            lib.emtk_recurrence(nn, f.t, x.t, outs[0].t, states=kept, **shared)
+            lib.emtk_recurrence_backward(nn, dy.t, f.t, x.t, kept, outs[1].t, outs[2].t, d_o=outs[3].t, **shared)
+            results.append([b.t.clone() for b in outs])
+            assert all(b.surroundings_untouched() for b in outs)
+    for i in range(2):
+        assert all(torch.equal(a, z) for a, z in zip(results[i], results[2 + i]))
+
+
 def test_far_gates(lib, nn):
     """Forget gates that keep all (f = 100, infinity), nothing (f = -100, -infinity), and one state among many: finite,
     exact at the ends; NaN stays in its column from its step on."""
