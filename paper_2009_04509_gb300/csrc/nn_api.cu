@@ -170,14 +170,14 @@ emtk_matrix Staging::operator()(const emtk_matrix &m, int rows, int cols) {
 template <typename Args>
 emtk_status recurrence_inputs(emtk_nn *nn, const Args &a, std::initializer_list<emtk_matrix *> inputs, bool forward, cudaStream_t s) {
     const bool uniform = a.offsets == nullptr;
-    const size_t kept = recurrence_workspace(a.rows, a.n, a.seqs, uniform, forward, nn->sm_count);
+    const size_t kept = recurrence_workspace(a.rows, a.n, a.seqs, uniform, nn->sm_count);
     CallSpace ws{nn};
     Staging stage{ws};
     for (int pass = 0; pass < 2; ++pass) {
         stage.n = 0;
         ws.take(kept);
         for (emtk_matrix *m : inputs) {
-            if (!recurrence_copies(*m, a.rows, a.n, a.seqs, uniform, forward)) continue;
+            if (!recurrence_copies(*m, a.rows, a.n, a.seqs, uniform, forward, nn->sm_count)) continue;
             const emtk_matrix there = stage(*m, a.rows, a.n);
             if (pass == 1) *m = there;
         }

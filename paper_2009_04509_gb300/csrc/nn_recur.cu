@@ -39,7 +39,8 @@ namespace {
 
 constexpr int kLanes = 16, kCols = 2 * kLanes;  // two columns a lane
 constexpr int kRuns = 8, kLen = 16, kTile = kRuns * kLen, kThreads = kLanes * kRuns;
-constexpr int kShort = 8;  // steps of a sequence, on average, up to which a thread takes all of it
+// A thread takes a whole sequence below kLong steps, in lots of kLot, where sequences are short on average.
+constexpr int kLot = 8, kLong = 64;
 static_assert(kTile == EMTK_RECURRENCE_STEP, "states are kept once a tile");
 
 // Where what is kept of a sequence's tile lies: tiles of different sequences, in order and with gaps.
@@ -54,6 +55,7 @@ Plane plane_of(const emtk_matrix &m) { return {static_cast<uint8_t *>(m.d), 2 * 
 struct Sequences {
     const int32_t *offsets;
     int rows, n, seqs, length;  // length: of each, without offsets
+    int long_only;              // blocks are to sequences of kLong steps and more alone
     __device__ __forceinline__ void rows_of(int s, int &r0, int &r1) const {
         if (offsets) {
             r0 = min(max(__ldg(offsets + s), 0), rows);
@@ -64,7 +66,8 @@ struct Sequences {
         }
     }
     // The sequence whose tiles' places include this one, if any's do: the last that begins
-    // at it or before.  All lanes of a warp look together.
+    // at it or before (or, of rows, the one that has this row).  All lanes of a warp look together.
+    template <bool ROW>
     __device__ __forceinline__ int at_place(int place) const {
         int low = 0, high = seqs;  // it is in low .. high - 1
         const int lane = threadIdx.x & 31;
@@ -72,7 +75,7 @@ struct Sequences {
             const int step = (high - low + 31) / 32, s = low + lane * step;
             int r0 = 0, r1;
             if (s < high) rows_of(s, r0, r1);
-            const uint32_t before = __ballot_sync(0xffffffffu, s < high && (lane == 0 || place_of(r0, 0, s) <= place));
+            const uint32_t before = __ballot_sync(0xffffffffu, s < high && (lane == 0 || (ROW ? r0 : place_of(r0, 0, s)) <= place));
             low += (31 - __clz(before)) * step;
             high = min(low + step, high);
         }
@@ -255,9 +258,11 @@ __device__ __forceinline__ float2 local_back(const float2 (&m)[kLen], const uint
     return p;
 }
 
-// Where a block works: a sequence's columns, all of its tiles or the one at a place.
+// Where a block works: a sequence's columns, all of its tiles or the one at a place.  Long
+// sequences among short ones are found by the first of the rows 0, kLong, 2 kLong .. that they have.
 struct Unit {
     int run, lane, seq, col0, col, valid;
+    bool any;  // false: a row that no long sequence is found by
     int r0, r1, tile, tiles;  // the sequence's rows; the tiles to do, from `tile` on (or from its end)
     __device__ __forceinline__ Unit(const Sequences &at, int col_tiles, bool one_tile)
         : run(threadIdx.x / kLanes), lane(threadIdx.x % kLanes) {
@@ -265,8 +270,9 @@ struct Unit {
         col0 = ((int)blockIdx.x - unit * col_tiles) * kCols;
         col = col0 + 2 * lane;
         valid = min(max(at.n - col, 0), 2);
-        seq = one_tile ? at.at_place(unit) : unit;
+        seq = one_tile ? at.at_place<false>(unit) : at.long_only ? at.at_place<true>(unit * kLong) : unit;
         at.rows_of(seq, r0, r1);
+        any = !at.long_only || (r1 - r0 >= kLong && (r0 + kLong - 1) / kLong == unit);
         tiles = (r1 - r0 + kTile - 1) / kTile;
         tile = 0;
         if (one_tile) {
@@ -338,6 +344,7 @@ __global__ void __launch_bounds__(kThreads, 4) recur_kernel(const __grid_constan
     pdl_trigger();
     pdl_wait();
     const Unit u(a.at, a.col_tiles, a.starts != nullptr);
+    if (!u.any) return;
     const bool has[kMostIn] = {true, true, gated, false};
     auto fetch = [&](int i, int s) {  // the i-th tile
         if (TMA && threadIdx.x == 0 && i < u.tiles) pipe.load(maps, has, s, u.col0, u.r0 + (u.tile + i) * kTile);
@@ -443,6 +450,7 @@ __global__ void __launch_bounds__(kThreads, 3) recur_grad_kernel(const __grid_co
     pdl_trigger();
     pdl_wait();
     const Unit u(a.at, a.col_tiles, a.starts != nullptr);
+    if (!u.any) return;
     const bool has[kMostIn] = {true, true, gated, true};
     auto fetch = [&](int i, int s) {
         if (TMA && threadIdx.x == 0 && i < u.tiles) pipe.load(maps, has, s, u.col0, u.r0 + (u.tile + u.tiles - 1 - i) * kTile);
@@ -642,7 +650,7 @@ __global__ void __launch_bounds__(32 * kScanWarps) tile_scan_kernel(const __grid
     if (end && in && warp == 0) end[(int64_t)seq * n + col] = carry;
 }
 
-// Short sequences: two columns of one to a thread, step by step, kShort steps' loads together.
+// Short sequences: two columns of one to a thread, step by step, kLot steps' loads together.
 template <bool F16, int ACT>
 __global__ void __launch_bounds__(256) recur_short_kernel(const __grid_constant__ RecurArgs a) {
     const int pairs = (a.at.n + 1) / 2, n = a.at.n;
@@ -655,20 +663,21 @@ __global__ void __launch_bounds__(256) recur_short_kernel(const __grid_constant_
     if (s >= a.at.seqs) return;
     int r0, r1;
     a.at.rows_of((int)s, r0, r1);
+    if (r1 - r0 >= kLong) return;
     float2 h = a.state ? load_state(a.state, s, n, col, valid) : both(0.f);
-    for (int first = r0; first < r1; first += kShort) {
-        uint32_t f[kShort], x[kShort], o[kShort];
+    if (a.states && r1 > r0) store_state(a.states, place_of(r0, 0, (int)s), n, col, valid, h);
+    for (int first = r0; first < r1; first += kLot) {
+        uint32_t f[kLot], x[kLot], o[kLot];
 #pragma unroll
-        for (int i = 0; i < kShort; ++i) {
+        for (int i = 0; i < kLot; ++i) {
             if (first + i >= r1) break;
             f[i] = load_pair(place(a.f, first + i, col), valid, words);
             x[i] = load_pair(place(a.x, first + i, col), valid, words);
             if (gated) o[i] = load_pair(place(a.o, first + i, col), valid, words);
         }
 #pragma unroll
-        for (int i = 0; i < kShort; ++i) {
+        for (int i = 0; i < kLot; ++i) {
             if (first + i >= r1) break;
-            if (a.states && (first + i - r0) % kTile == 0) store_state(a.states, place_of(r0, (first + i - r0) / kTile, (int)s), n, col, valid, h);
             h = step(minus_rest<F16>(f[i]), h, values_of<F16>(x[i]));
             const float2 y = gated ? h * act2<ACT>(values_of<F16>(o[i])) : h;
             store_pair(place(a.y, first + i, col), valid, words, pack16<F16>(y.x, y.y));
@@ -677,8 +686,7 @@ __global__ void __launch_bounds__(256) recur_short_kernel(const __grid_constant_
     if (a.last) store_state(a.last, s, n, col, valid, h);
 }
 
-// The same backwards, from the last steps on; the state before each lot of steps is had from the
-// one that was kept, the first step's where the sequence is short.
+// The same backwards: along the lots once for the state before each, then from the last to the first.
 template <bool F16, int ACT>
 __global__ void __launch_bounds__(256) recur_short_grad_kernel(const __grid_constant__ RecurGradArgs a) {
     const int pairs = (a.at.n + 1) / 2, n = a.at.n;
@@ -691,31 +699,45 @@ __global__ void __launch_bounds__(256) recur_short_grad_kernel(const __grid_cons
     if (s >= a.at.seqs) return;
     int r0, r1;
     a.at.rows_of((int)s, r0, r1);
+    if (r1 - r0 >= kLong) return;
     float2 p = a.d_last ? load_state(a.d_last, s, n, col, valid) : both(0.f);
-    for (int lot = (r1 - r0 - 1) / kShort; r1 > r0 && lot >= 0; --lot) {
-        const int first = r0 + lot * kShort, tile = lot * kShort / kTile;
-        uint32_t wf[kShort], wx[kShort], wo[kShort], wd[kShort];
+    float2 starts[kLong / kLot];
+    uint32_t wf[kLot], wx[kLot];
+    const int last = (r1 - r0 - 1) / kLot;  // the last lot
+    if (r1 > r0) starts[0] = load_state(a.states, place_of(r0, 0, (int)s), n, col, valid);
+    for (int lot = 0; lot < last; ++lot) {
+        const int first = r0 + lot * kLot;
 #pragma unroll
-        for (int i = 0; i < kShort; ++i) {
+        for (int i = 0; i < kLot; ++i) {
+            wf[i] = load_pair(place(a.f, first + i, col), valid, words);
+            wx[i] = load_pair(place(a.x, first + i, col), valid, words);
+        }
+        float2 h = starts[lot];
+#pragma unroll
+        for (int i = 0; i < kLot; ++i) h = step(minus_rest<F16>(wf[i]), h, values_of<F16>(wx[i]));
+        starts[lot + 1] = h;
+    }
+    for (int lot = last; r1 > r0 && lot >= 0; --lot) {
+        const int first = r0 + lot * kLot;
+        uint32_t wo[kLot], wd[kLot];
+#pragma unroll
+        for (int i = 0; i < kLot; ++i) {
             if (first + i >= r1) break;
             wf[i] = load_pair(place(a.f, first + i, col), valid, words);
             wx[i] = load_pair(place(a.x, first + i, col), valid, words);
             wd[i] = load_pair(place(a.dy, first + i, col), valid, words);
             if (gated) wo[i] = load_pair(place(a.o, first + i, col), valid, words);
         }
-        float2 h = load_state(a.states, place_of(r0, tile, (int)s), n, col, valid);
-        for (int row = r0 + tile * kTile; row < first; ++row)
-            h = step(minus_rest<F16>(load_pair(place(a.f, row, col), valid, words)), h, values_of<F16>(load_pair(place(a.x, row, col), valid, words)));
-        float2 m[kShort], before[kShort + 1];
-        before[0] = h;
+        float2 m[kLot], before[kLot + 1];
+        before[0] = starts[lot];
 #pragma unroll
-        for (int i = 0; i < kShort; ++i) {
+        for (int i = 0; i < kLot; ++i) {
             if (first + i >= r1) break;
             m[i] = minus_rest<F16>(wf[i]);
             before[i + 1] = step(m[i], before[i], values_of<F16>(wx[i]));
         }
 #pragma unroll
-        for (int i = kShort - 1; i >= 0; --i) {
+        for (int i = kLot - 1; i >= 0; --i) {
             if (first + i >= r1) continue;
             float2 d_o;
             const Slopes g = slopes<F16, ACT>(m[i], before[i], before[i + 1], wf[i], wx[i], wo[i], wd[i], gated, p, d_o);
@@ -741,9 +763,18 @@ bool on_words(const emtk_matrix &m, int rows) {
 bool along(bool uniform, int rows, int seqs, int col_tiles, int sms) {
     return 2 * (int64_t)seqs * col_tiles >= 3 * sms && (uniform || rows / seqs <= 4 * kTile);
 }
-// Whether a thread takes a whole sequence: a tile would be nearly empty.  Backwards, a sequence
-// longer than kShort steps costs a thread its square, so unlike lengths have to be shorter.
-bool step_by_step(bool uniform, bool forward, int rows, int seqs) { return rows / seqs <= (uniform || forward ? kShort : kShort / 4); }
+// Whether a thread takes a whole sequence, as a tile would be nearly empty: of unlike ones those below
+// kLong steps where that is so on average, the others are left to blocks that go along them.  Forward and
+// backward, 320 sequences of 1024 columns, of 0 - 8 steps 8.2 and 12.4 us, a tile to each 48 and 128; of
+// 0 - 120 steps 64 and 139, 66 and 163; one of 8192 steps and 800 single steps of 2048 columns 142 and 322,
+// 273 and 739.  Equal ones: 64 of 16 steps of 2048 columns 5.8 and 10.8 us, a tile to each 20.7 and 57;
+// where blocks are no more than the SMs hold at once, tiles are as fast (16 of 16 of 1024: 4.9 and 8.6, 4.2
+// and 12.7) and faster for more steps (16 of 32: 8.5 and 16.3, 4.0 and 12.6).
+bool step_by_step(bool uniform, int rows, int seqs, int n, int sms) {
+    const int length = rows / seqs;
+    const bool many = (int64_t)seqs * ((n + kCols - 1) / kCols) > 4 * sms;
+    return length <= kLot || (uniform ? length < kLong && many : length <= kLong);
+}
 int64_t places(int rows, int seqs) { return (int64_t)rows / kTile + seqs; }
 
 // Workspace of independent tiles: (q, H) and, where they are not kept anyway, the starts.
@@ -759,15 +790,23 @@ bool grid_ok(int64_t blocks) { return blocks <= INT32_MAX; }
 template <typename Kernel, typename Args>
 cudaError_t run_tiles(Kernel kernel, int planes, bool tma, const Args &a, const Tiles &maps, cudaStream_t s) {
     const bool whole = a.starts == nullptr;
-    const int64_t blocks = (whole ? a.at.seqs : places(a.at.rows, a.at.seqs)) * a.col_tiles;
+    const int64_t blocks =
+        (!whole ? places(a.at.rows, a.at.seqs) : a.at.long_only ? (a.at.rows + kLong - 1) / kLong : a.at.seqs) * (int64_t)a.col_tiles;
     if (!grid_ok(blocks)) return cudaErrorInvalidValue;
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(kThreads), shared_bytes(planes, tma, whole), s, a, maps);
 }
 
+// Whether no sequence is left to blocks, with short ones step by step.
+bool no_long(const int32_t *offsets, int rows) { return !offsets || rows < kLong; }
+// The short sequences; `a` is left with the long ones, `done` if there can be none.
 template <typename Args>
-cudaError_t run_short(void (*kernel)(const Args), const Args &a, cudaStream_t s) {
+cudaError_t run_short(void (*kernel)(const Args), Args &a, bool &done, cudaStream_t s) {
     const int64_t blocks = ((int64_t)a.at.seqs * ((a.at.n + 1) / 2) + 255) / 256;
-    return grid_ok(blocks) ? launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), 0, s, a) : cudaErrorInvalidValue;
+    if (!grid_ok(blocks)) return cudaErrorInvalidValue;
+    const cudaError_t e = launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), 0, s, a);
+    done = e != cudaSuccess || no_long(a.at.offsets, a.at.rows);
+    a.at.long_only = 1;
+    return e;
 }
 
 // Each tile's start, by the first two kernels.
@@ -787,8 +826,11 @@ cudaError_t run_starts(const RecurGradArgs &a, const Tiles *maps, void *workspac
 
 template <bool F16, int ACT>
 cudaError_t run(RecurArgs a, const Tiles *maps, void *workspace, int sms, cudaStream_t s) {
-    if (step_by_step(!a.at.offsets, true, a.at.rows, a.at.seqs)) return run_short(recur_short_kernel<F16, ACT>, a, s);
-    if (!along(!a.at.offsets, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
+    if (step_by_step(!a.at.offsets, a.at.rows, a.at.seqs, a.at.n, sms)) {
+        bool done;
+        const cudaError_t e = run_short(recur_short_kernel<F16, ACT>, a, done, s);
+        if (done) return e;
+    } else if (!along(!a.at.offsets, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
         RecurGradArgs g{};
         g.f = a.f;
         g.x = a.x;
@@ -805,8 +847,11 @@ cudaError_t run(RecurArgs a, const Tiles *maps, void *workspace, int sms, cudaSt
 }
 template <bool F16, int ACT>
 cudaError_t run(RecurGradArgs a, const Tiles *maps, void *workspace, int sms, cudaStream_t s) {
-    if (step_by_step(!a.at.offsets, false, a.at.rows, a.at.seqs)) return run_short(recur_short_grad_kernel<F16, ACT>, a, s);
-    if (!along(!a.at.offsets, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
+    if (step_by_step(!a.at.offsets, a.at.rows, a.at.seqs, a.at.n, sms)) {
+        bool done;
+        const cudaError_t e = run_short(recur_short_grad_kernel<F16, ACT>, a, done, s);
+        if (done) return e;
+    } else if (!along(!a.at.offsets, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
         float *const starts = sums_in(workspace, places(a.at.rows, a.at.seqs), a.at.n).made + places(a.at.rows, a.at.seqs) * a.at.n;
         const cudaError_t e = run_starts<F16, ACT, true>(a, maps, workspace, a.d_last, starts, a.d_state, s);
         if (e != cudaSuccess) return e;
@@ -867,13 +912,13 @@ cudaError_t init_recur_kernels() {
 // it. 800 x 1000 steps of 64 columns, an element off the grid, forward and backward: 294 and 603 us as
 // they lie, 195 and 377 copied; 88 x 192 of 498: 39 and 129, 45 and 91. Two elements off it stay where
 // they lie: 147 and 351, 189 and 345.
-bool recurrence_copies(const emtk_matrix &m, int rows, int n, int seqs, bool uniform, bool forward) {
+bool recurrence_copies(const emtk_matrix &m, int rows, int n, int seqs, bool uniform, bool forward, int sms) {
     const bool odd = (reinterpret_cast<uintptr_t>(m.d) | (uintptr_t)m.ld * 2) & 3;
-    return m.d && odd && (int64_t)rows * n >= (forward ? 10 : 4) << 20 && !step_by_step(uniform, forward, rows, seqs);
+    return seqs > 0 && m.d && odd && (int64_t)rows * n >= (forward ? 10 : 4) << 20 && !step_by_step(uniform, rows, seqs, n, sms);
 }
 
-size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, bool forward, int sms) {
-    if (n == 0 || seqs == 0 || step_by_step(uniform, forward, rows, seqs)) return 0;
+size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, int sms) {
+    if (n == 0 || seqs == 0 || step_by_step(uniform, rows, seqs, n, sms)) return 0;
     const bool whole = along(uniform, rows, seqs, (n + kCols - 1) / kCols, sms);
     return whole ? 0 : 3 * sizeof(float) * places(rows, seqs) * n;
 }
@@ -885,7 +930,7 @@ cudaError_t launch_recurrence(const emtk_recurrence_args &p, void *workspace, co
     a.x = plane_of(p.x);
     a.o = plane_of(p.o);
     a.y = plane_of(p.y);
-    a.at = {p.offsets, p.rows, p.n, p.seqs, p.offsets ? 0 : p.rows / p.seqs};
+    a.at = {p.offsets, p.rows, p.n, p.seqs, p.offsets ? 0 : p.rows / p.seqs, 0};
     a.state = p.state;
     a.last = p.last;
     a.states = p.states;
@@ -893,7 +938,7 @@ cudaError_t launch_recurrence(const emtk_recurrence_args &p, void *workspace, co
     a.words = on_words(p.f, p.rows) && on_words(p.x, p.rows) && on_words(p.o, p.rows) && on_words(p.y, p.rows);
     Tiles maps;
     const emtk_matrix *const in[] = {&p.f, &p.x, &p.o}, *const out[] = {&p.y};
-    const bool tma = !step_by_step(!p.offsets, true, p.rows, p.seqs) && make_maps(nn, maps, in, out, p.rows, p.n);
+    const bool tma = !(step_by_step(!p.offsets, p.rows, p.seqs, p.n, nn->sm_count) && no_long(p.offsets, p.rows)) && make_maps(nn, maps, in, out, p.rows, p.n);
     return p.type == EMTK_TYPE_F16 ? run<true>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s)
                                    : run<false>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s);
 }
@@ -908,7 +953,7 @@ cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, void *wor
     a.df = plane_of(p.df);
     a.dx = plane_of(p.dx);
     a.d_o = plane_of(p.d_o);
-    a.at = {p.offsets, p.rows, p.n, p.seqs, p.offsets ? 0 : p.rows / p.seqs};
+    a.at = {p.offsets, p.rows, p.n, p.seqs, p.offsets ? 0 : p.rows / p.seqs, 0};
     a.states = p.states;
     a.d_last = p.d_last;
     a.d_state = p.d_state;
@@ -917,7 +962,7 @@ cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, void *wor
               on_words(p.df, p.rows) && on_words(p.dx, p.rows) && on_words(p.d_o, p.rows);
     Tiles maps;
     const emtk_matrix *const in[] = {&p.f, &p.x, &p.o, &p.dy}, *const out[] = {&p.df, &p.dx, &p.d_o};
-    const bool tma = !step_by_step(!p.offsets, false, p.rows, p.seqs) && make_maps(nn, maps, in, out, p.rows, p.n);
+    const bool tma = !(step_by_step(!p.offsets, p.rows, p.seqs, p.n, nn->sm_count) && no_long(p.offsets, p.rows)) && make_maps(nn, maps, in, out, p.rows, p.n);
     return p.type == EMTK_TYPE_F16 ? run<true>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s)
                                    : run<false>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s);
 }

@@ -621,7 +621,8 @@ def recur_case(i):
     lengths = r.choice([[1], [5], [8], [9], [127], [128], [129], [300], [700], [1025], [2600], [1] * 70, [3] * 40, [8] * 9, [64] * 5, [130] * 3, [300] * 20,
                         [5, 0, 131, 1, 260, 0], [0, 0], [2000, 3, 700], [1] * 5 + [0] * 3 + [1200]])
     if i >= 48:  # short ones on average, one of them long; lots of steps that end inside one; runs without steps
-        lengths = [[1] * 300 + [1500], [2, 0, 7, 9, 8, 16, 17, 0, 1], [24] * 90, [100] * 60, [1, 40, 17, 16, 130] * 12][i - 48]
+        lengths = [[1] * 300 + [1500], [2, 0, 7, 9, 8, 16, 17, 0, 1], [24] * 90, [100] * 60, [1, 40, 17, 16, 130] * 12,
+                   [64, 63, 0, 1] * 9 + [129, 2, 0, 65, 63, 5], [16] * 650, [63] * 620, [1] * 64 + [64] + [0] * 5 + [700] + [9] * 70][i - 48]
     uniform = len(set(lengths)) == 1 and lengths[0] > 0
     return dict(lengths=lengths, offsets=not uniform or r.random() < 0.4, lead=r.choice([0, 0, 3]), tail=r.choice([0, 0, 5]),
                 n=r.choice([1, 2, 7, 31, 32, 33, 64, 100]), act=r.choice(["none", "relu", "gelu", "silu", "sigmoid"]), gated=r.random() < 0.7,
@@ -629,7 +630,7 @@ def recur_case(i):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-@pytest.mark.parametrize("i", range(53))
+@pytest.mark.parametrize("i", range(57))
 def test_recurrence(lib, nn, i, dtype):
     """Both passes.  An error of b of a few E (and |f| E, of the exponential) moves the state by so much of max |x - h|;
     the roundings of a step stay for as long as the state does, at most min(T, 1 / b) steps.  A step passes g - b g on,
@@ -776,9 +777,10 @@ def test_long_memories_settle_right(lib, nn):
     assert (last.double() - want).abs().max() <= 2e-5 * want  # 12 |f| E of the exponential, and a rounding for every tile
 
 
-def test_unsound_offsets_stay_inside(lib, nn):
+@pytest.mark.parametrize("rows", [150, 300])
+def test_unsound_offsets_stay_inside(lib, nn, rows):
     """Offsets that fall, or lie outside the rows, are taken as within them: nothing outside is touched."""
-    rows, n = 300, 40
+    n = 40
     f, x = (Buf(rows, n, torch.bfloat16, 0, 0, randn(gen(s), rows, n)) for s in (1, 2))
     for offs in ([0, 200, 100, 300], [-5, 50, 400, 1000], [300, 300, 0, 0], [2 ** 31 - 1, -2 ** 31, 7, 290]):
         y, states, last = Buf(rows, n, torch.bfloat16), Buf(rows // 128 + 3, n, torch.float32), Buf(3, n, torch.float32)
