@@ -168,7 +168,7 @@ emtk_matrix Staging::operator()(const emtk_matrix &m, int rows, int cols) {
 // The workspace of a recurrence's call, which begins with what its kernels leave each other;
 // inputs that are to be read from a copy there become that copy.
 template <typename Args>
-emtk_status recurrence_inputs(emtk_nn *nn, const Args &a, std::initializer_list<emtk_matrix *> inputs, bool forward, cudaStream_t s) {
+emtk_status recurrence_inputs(emtk_nn *nn, const Args &a, std::initializer_list<emtk_matrix *> inputs, cudaStream_t s) {
     const bool uniform = a.offsets == nullptr;
     const size_t kept = recurrence_workspace(a.rows, a.n, a.seqs, uniform, nn->sm_count);
     CallSpace ws{nn};
@@ -177,7 +177,7 @@ emtk_status recurrence_inputs(emtk_nn *nn, const Args &a, std::initializer_list<
         stage.n = 0;
         ws.take(kept);
         for (emtk_matrix *m : inputs) {
-            if (!recurrence_copies(*m, a.rows, a.n, a.seqs, uniform, forward, nn->sm_count)) continue;
+            if (!recurrence_copies(*m, a.rows, a.n, a.seqs, uniform, nn->sm_count)) continue;
             const emtk_matrix there = stage(*m, a.rows, a.n);
             if (pass == 1) *m = there;
         }
@@ -732,7 +732,7 @@ emtk_status emtk_recurrence(emtk_nn *nn, const emtk_recurrence_args *p, emtk_str
     Range range("emtk recurrence");
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     emtk_recurrence_args b = a;
-    const emtk_status st = recurrence_inputs(nn, a, {&b.f, &b.x, &b.o}, true, s);
+    const emtk_status st = recurrence_inputs(nn, a, {&b.f, &b.x, &b.o}, s);
     return st != EMTK_OK ? st : status_of(launch_recurrence(b, nn->ws, nn, s));
 }
 
@@ -761,7 +761,7 @@ emtk_status emtk_recurrence_backward(emtk_nn *nn, const emtk_recurrence_grad_arg
     Range range("emtk recurrence backward");
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     emtk_recurrence_grad_args b = a;
-    const emtk_status st = recurrence_inputs(nn, a, {&b.f, &b.x, &b.o, &b.dy}, false, s);
+    const emtk_status st = recurrence_inputs(nn, a, {&b.f, &b.x, &b.o, &b.dy}, s);
     return st != EMTK_OK ? st : status_of(launch_recurrence_grad(b, nn->ws, nn, s));
 }
 

@@ -759,8 +759,10 @@ bool on_words(const emtk_matrix &m, int rows) {
 // waiting.  20000 rows of 2048 columns, forward and backward: 256 units 107 and 187 us, as
 // independent tiles 103 and 212; 64 units 281 and 535, independent 95 and 202; 1024 units (of 1250 rows)
 // 59 and 134, independent as with 64.  16896 rows of 498 columns in 88 sequences of unlike lengths:
-// both passes 410 us as independent tiles, most of whose places are empty.
+// both passes 410 us as independent tiles, most of whose places are empty.  Sequences of four tiles
+// at most are done before three kernels would be.
 bool along(bool uniform, int rows, int seqs, int col_tiles, int sms) {
+    if ((uniform ? rows / seqs : rows) <= 4 * kTile) return true;
     return 2 * (int64_t)seqs * col_tiles >= 3 * sms && (uniform || rows / seqs <= 4 * kTile);
 }
 // Whether a thread takes a whole sequence, as a tile would be nearly empty: of unlike ones those below
@@ -908,13 +910,14 @@ cudaError_t init_recur_kernels() {
     return e == cudaSuccess ? init_kernels<true>() : e;
 }
 
-// An input that only loads of two bytes reach is copied to rows that TMA reads, where there is much of
-// it. 800 x 1000 steps of 64 columns, an element off the grid, forward and backward: 294 and 603 us as
-// they lie, 195 and 377 copied; 88 x 192 of 498: 39 and 129, 45 and 91. Two elements off it stay where
-// they lie: 147 and 351, 189 and 345.
-bool recurrence_copies(const emtk_matrix &m, int rows, int n, int seqs, bool uniform, bool forward, int sms) {
+// An input that only loads of two bytes reach is copied to rows that TMA reads, but for short
+// sequences.  An element off the grid, forward and backward, as they lie and copied: 800 x 1000 steps
+// of 64 columns 294 and 603 us, 195 and 377; 8 x 512 of 136 24 and 54, 13 and 33; 88 x 192 of 498 43 and
+// 129, 44 and 91; 400 x 200 of 32 14 and 22, 15 and 24.  Two elements off it they are read as they lie: the
+// first 147 and 351, 189 and 345.
+bool recurrence_copies(const emtk_matrix &m, int rows, int n, int seqs, bool uniform, int sms) {
     const bool odd = (reinterpret_cast<uintptr_t>(m.d) | (uintptr_t)m.ld * 2) & 3;
-    return seqs > 0 && m.d && odd && (int64_t)rows * n >= (forward ? 10 : 4) << 20 && !step_by_step(uniform, rows, seqs, n, sms);
+    return seqs > 0 && m.d && odd && !step_by_step(uniform, rows, seqs, n, sms);
 }
 
 size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, int sms) {
