@@ -12,7 +12,8 @@
 // pieces' maxima, any K that are at hand bound the K-th from below, and every one of the
 // row's K largest lies in a piece whose maximum is at or above that bound: only the strips
 // of threads that hold such pieces are read again, and what is at or above the bound, a
-// few dozen as a rule, is ranked by comparing all with all.  (Each warp keeping a sorted list
+// few dozen as a rule, is ranked by comparing all with all.  Of the shortest rows' they are found
+// one after another, as all rows' are where there is no room for the candidates.  (Each warp keeping a sorted list
 // in its lanes took up to five times the whole pass: an insertion is a dozen dependent
 // exchanges.)
 //
@@ -350,7 +351,7 @@ __device__ __forceinline__ float token_logit(const LogprobArgs &a, const uint8_t
 
 // Room for a warp's candidates: where fewer lanes than K have a piece, all elements are.
 constexpr int kWarpRoom = 32 * 8 + 16;
-// Short rows: 2^lanes_log2 lanes to a row (a warp where the largest are wanted).
+// Short rows: 2^lanes_log2 lanes to a row; fewer than a warp look for the largest one after another.
 template <int TYPE, bool TOP>
 __global__ void __launch_bounds__(kThreads) logprob_lanes_kernel(const __grid_constant__ LogprobArgs a) {
     __shared__ uint64_t keys[TOP ? kWarps : 1][kWarpRoom];
@@ -373,8 +374,21 @@ __global__ void __launch_bounds__(kThreads) logprob_lanes_kernel(const __grid_co
         o.w = __shfl_xor_sync(0xffffffffu, sums.w, d);
         sums.join(o, a.k);
     }
+    if (in && lane == 0) finish_row(a, row, sums, token, z);
+    if (TOP && a.lanes_log2 < 5) {  // the largest one after another
+        uint64_t limit = ~0ull;
+        for (int i = 0; i < a.top; ++i) {
+            uint64_t key = next_below(strip, limit);
+            for (int d = lanes >> 1; d > 0; d >>= 1) {
+                const uint64_t other = __shfl_xor_sync(0xffffffffu, key, d);
+                key = other > key ? other : key;
+            }
+            limit = key;
+            if (in && lane == 0) finish_top(a, row, sums, key, i);
+        }
+        return;
+    }
     if (!in) return;
-    if (lane == 0) finish_row(a, row, sums, token, z);
     if constexpr (TOP) {
         const int warp = threadIdx.x / 32;
         const Found found{keys[warp], counts + warp, kWarpRoom};
@@ -598,8 +612,11 @@ template <int TYPE, bool TOP>
 cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
     const int pieces = a.v / Elem<TYPE>::kPer;
     if (pieces <= 256) {  // up to 8 pieces a lane
-        a.lanes_log2 = TOP ? 5 : 0;
         while (a.lanes_log2 < 5 && (2 << a.lanes_log2) < pieces) ++a.lanes_log2;
+        // The largest one after another or with a warp to a row: 20000 rows of 8, top 5, 4.9 and 19.9 us; 32768 of 64, top 5,
+        // 14.8 and 32.5; 20000 of 33 (fp32), top 8, 20.6 and 22.6, top 16 37.8 and 27.8; 32768 of 200, top 2, 25.5 and 30.6, top 5
+        // 47.9 and 32.2.
+        if (TOP && a.top * a.v > 320) a.lanes_log2 = 5;
         const int64_t rows = kThreads >> a.lanes_log2;
         return launch_pdl(logprob_lanes_kernel<TYPE, TOP>, dim3((unsigned)((a.m + rows - 1) / rows)), dim3(kThreads), 0, s, a);
     }

@@ -444,7 +444,7 @@ def logprobs64(z, tokens, temperature):
 
 
 LOGITS = [(1, 1), (5, 2), (300, 3), (4, 7), (9, 8), (3, 9), (40, 31), (7, 33), (3, 256), (2, 257), (5, 1000), (3, 2047), (2, 2049), (3, 2064), (2, 4100),
-          (1, 9000), (2, 50001), (1, 131072), (200, 2500), (1, 40000)]
+          (1, 9000), (2, 50001), (1, 131072), (200, 2500), (1, 40000), (65, 64), (50, 150)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "f32"])
