@@ -475,7 +475,7 @@ def _mat8(on, t, rows: int, cols: int, dtype, what: str) -> tuple:
 def _vec(on, t, n: int, what: str, f32: bool = False) -> int:
     if t is None:
         return 0
-    if t.shape != (n,) or t.get_device() != on or not t.is_contiguous():
+    if t.shape != (n,) or t.get_device() != on or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{what}: expected a contiguous vector of {n} on CUDA device {on}, got {tuple(t.shape)} on {t.device}")
     if f32 and _type_of(t, what, True) != EMTK_TYPE_F32:
         raise ValueError(f"{what}: dtype {t.dtype}, expected float32")
