@@ -138,15 +138,6 @@ struct CallSpace {
     }
 };
 
-// The workspace of a call that needs one piece.
-emtk_status one_space(emtk_nn *nn, size_t bytes, cudaStream_t s, void **space) {
-    CallSpace ws{nn};
-    ws.take(bytes);
-    const emtk_status st = ws.ensure(s);
-    if (st == EMTK_OK) *space = ws.take(bytes);
-    return st;
-}
-
 // Operands of a call's products that cannot be read where they lie (a
 // checkpoint, or rows off the 16-byte grid): each gets a copy in the workspace.
 struct Staging {
@@ -660,9 +651,25 @@ emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residual_norm_gr
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk residual norm backward");
+    // The sums past the block's norm read dy after d_residual is written: where that takes its place, a
+    // copy, which lies alike, so that the sums are the same.
+    const bool copied = a.m > 0 && a.dy.d && a.dy.d == a.d_residual.d && (a.d_gate.d || a.dw_post || a.db_post);
+    emtk_matrix copy{nullptr, ld16(a.n) + a.dy.ld % 8, nullptr, 0};
+    CallSpace ws{nn};
     void *space = nullptr;
-    const emtk_status st = one_space(nn, residual_norm_workspace(a, nn->sm_count), s, &space);
-    return st != EMTK_OK ? st : status_of(launch_residual_norm_grad(a, space, nn, s));
+    for (int pass = 0; pass < 2; ++pass) {
+        space = ws.take(residual_norm_workspace(a, nn->sm_count));
+        if (copied) copy.d = ws.take(16 + 2 * (size_t)a.m * copy.ld);
+        const emtk_status st = pass == 0 ? ws.ensure(s) : EMTK_OK;
+        if (st != EMTK_OK) return st;
+    }
+    if (copied) {
+        copy.d = static_cast<uint8_t *>(copy.d) + reinterpret_cast<uintptr_t>(a.dy.d) % 16;
+        const cudaError_t e = launch_dropout((emtk_type)a.type, a.m, a.n, a.dy, copy, emtk_drop{}, nn->sm_count, s);  // of nothing
+        if (e != cudaSuccess) return status_of(e);
+        a.dy = copy;
+    }
+    return status_of(launch_residual_norm_grad(a, space, nn, s));
 }
 
 emtk_status emtk_logprobs(emtk_nn *nn, const emtk_logprobs_args *p, emtk_stream stream) {

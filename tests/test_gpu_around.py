@@ -337,6 +337,23 @@ def test_residual_norm_backward(lib, nn, i, dtype):
         assert torch.equal(dy.t, first[0]) and dy.surroundings_untouched()
 
 
+@pytest.mark.parametrize("pads", [(0,) * 4, (1,) * 4, (3, 1, 0, 2), (1, 0, 0, 0)])
+@pytest.mark.parametrize("n,m,every", [(40, 61, 7), (517, 100, 100), (2312, 33, 1), (8, 1, 1)])
+def test_sums_with_d_residual_in_dys_place(lib, nn, n, m, every, pads):
+    """The sums past the block's norm are of the dy that was given: every result has the bits that it has apart."""
+    g = gen(n + m)
+    y, dh, b, dy = (Buf(m, n, torch.bfloat16, p, p, randn(g, m, n)).t for p in pads)
+    gate, w = randn(g, -(-m // every), n).to(torch.bfloat16), randn(g, n)
+    shared = dict(pre=lib.Norm("rms", w), post=lib.Norm("layer", w, w), gate=gate, gate_every=every, scale=0.5, drop=lib.Drop(0.25, 3, 4))
+    results = []
+    for place in (torch.empty_like(dy), dy):
+        sums = {k: torch.empty(n, device="cuda") for k in ("dw_pre", "db_pre", "dw_post", "db_post")}
+        d_block, d_gate = torch.empty(m, n, dtype=torch.bfloat16, device="cuda"), torch.empty(gate.shape, device="cuda")
+        lib.emtk_residual_norm_backward(nn, dy, dh, y, b, place, d_block, d_gate=d_gate, **sums, **shared)
+        results.append([place.clone(), d_block, d_gate, *sums.values()])
+    assert all(torch.equal(x, z) for x, z in zip(*results))
+
+
 @pytest.mark.parametrize("n,m", [(40, 61), (517, 100), (2311, 40), (1000, 9), (8, 33), (3, 50)])
 @pytest.mark.parametrize("gate_rows", [1, 3, 1000])
 def test_gradients_do_not_depend_on_where_matrices_lie(lib, nn, m, n, gate_rows):
