@@ -5,7 +5,9 @@
 //   l_j = (z_j - M) / T - ln S;   entropy = ln S - W / S;
 // when the maximum rises by d (in units of T), S becomes S exp(-d) and W exp(-d) (W - d S).
 // Two runs' triples join the same way.  HBM bounds large calls (one read of the logits;
-// the gradient one read and one write), the call small ones.
+// the gradient one read and one write), the call small ones.  8192 x 65536 in bf16 179 us (6.0 TB/s,
+// 0.88 of a copy's rate), its gradient 323 (6.65 TB/s, 0.98); one row of 131072 with its 8 largest
+// 8.3 us on a cluster of 8 blocks.  Two elements to an instruction took the first from 199 to 180 us.
 //
 // The K largest come from a second look at a small part of the row.  On the way each thread
 // notes the largest of its pieces (16 bytes; the lowest column among equals).  Of the
@@ -15,10 +17,11 @@
 // few dozen as a rule, is ranked by comparing all with all.  Of the shortest rows' they are found
 // one after another, as all rows' are where there is no room for the candidates.  (Each warp keeping a sorted list
 // in its lanes took up to five times the whole pass: an insertion is a dozen dependent
-// exchanges.)
+// exchanges; 1 x 131072, top 8, 18.2 us, and 8192 x 65536 753, now 8.3 and 268.)
 //
 // A row goes to a few lanes, to a block of threads, or, where rows are few and long, to a
-// cluster of blocks that join through shared memory.  Rows start anywhere: their aligned
+// cluster of blocks that join through shared memory (1 x 131072: 12.6 us by one block, 4.6 by eight;
+// 300 x 131072: 29.9 by one, 19.6 by two, 23.9 by eight).  Rows start anywhere: their aligned
 // 16-byte pieces are loaded whole, the up to 14 elements around them singly.
 #include <algorithm>
 
@@ -290,6 +293,20 @@ __device__ __forceinline__ void offer_strip(const Strip<TYPE> &s, int t, int lan
     for (int at = s.first - s.t + t + lane * s.threads; at < s.end; at += lanes * s.threads) offer_unit(s, at + 1, bound, found);
     if (s.ends && t == s.threads - 1 && lane == 0 && s.split.tail > 0) offer_unit(s, s.units() - 1, bound, found);
 }
+// The strip's largest unit below `limit`.
+template <int TYPE>
+__device__ __forceinline__ uint64_t next_unit(const Strip<TYPE> &s, uint64_t limit) {
+    uint64_t best = 0u;
+    auto look = [&](int unit) {
+        float z[Elem<TYPE>::kPer];
+        const uint64_t key = s.values(unit, z) ? key_of(order_of(largest(z)), unit) : 0u;
+        if (key < limit && key > best) best = key;
+    };
+    if (s.ends && s.t == 0) look(0);
+    for (int at = s.first; at < s.end; at += s.threads) look(at + 1);
+    if (s.ends && s.t == s.threads - 1) look(s.units() - 1);
+    return best;
+}
 // Where there was no room for all: the strip's largest element below `limit`.
 template <int TYPE>
 __device__ __forceinline__ uint64_t next_below(const Strip<TYPE> &s, uint64_t limit) {
@@ -351,6 +368,7 @@ __device__ __forceinline__ float token_logit(const LogprobArgs &a, const uint8_t
 
 // Room for a warp's candidates: where fewer lanes than K have a piece, all elements are.
 constexpr int kWarpRoom = 32 * 8 + 16;
+constexpr int kTopOfMaxima = 20;  // 32768 x 1000: the 32 largest 186 us from 32 maxima (no room), 88 from 64
 // Short rows: 2^lanes_log2 lanes to a row; fewer than a warp look for the largest one after another.
 template <int TYPE, bool TOP>
 __global__ void __launch_bounds__(kThreads) logprob_lanes_kernel(const __grid_constant__ LogprobArgs a) {
@@ -395,7 +413,15 @@ __global__ void __launch_bounds__(kThreads) logprob_lanes_kernel(const __grid_co
         if (lane == 0) counts[warp] = 0;
         keys[warp][lane] = best.key();
         __syncwarp();
-        const uint64_t bound = ranked(best.key(), rank_of(best.key(), keys[warp], 32), a.top - 1);
+        uint64_t bound;
+        if (a.top <= kTopOfMaxima) {
+            bound = ranked(best.key(), rank_of(best.key(), keys[warp], 32), a.top - 1);
+        } else {  // from the low end of 32 maxima much would be above it: of two pieces of each lane
+            const uint64_t second = next_unit(strip, best.key());
+            keys[warp][32 + lane] = second;
+            __syncwarp();
+            bound = max(ranked(best.key(), rank_of(best.key(), keys[warp], 64), a.top - 1), ranked(second, rank_of(second, keys[warp], 64), a.top - 1));
+        }
         __syncwarp();
         if (best.key() && best.key() >= bound) offer_strip(strip, lane, 0, 1, bound, found);
         __syncwarp();
@@ -454,13 +480,14 @@ __global__ void __launch_bounds__(kThreads) logprob_block_kernel(const __grid_co
     }
     if (lane == 0) warps[warp] = sums;
     if constexpr (TOP) {
-        // K pieces at or above it: an eighth of them of every warp, or all of one
+        // K pieces at or above it: as many of every warp whose lanes all have one, or all of one
         keys[threadIdx.x] = best.key();
         if (threadIdx.x == 0) count = 0;
         __syncwarp();
         const int mine = rank_of(best.key(), keys + 32 * warp, 32);
-        const uint64_t few = ranked(best.key(), mine, (a.top + kWarps - 1) / kWarps - 1), many = ranked(best.key(), mine, a.top - 1);
-        if (lane == 0) bounds[warp][0] = few, bounds[warp][1] = many;
+        const int full = max(1, min(kWarps, (strip.end - strip.first + (int)threadIdx.x) / 32));
+        const uint64_t few = ranked(best.key(), mine, (a.top + full - 1) / full - 1), many = ranked(best.key(), mine, a.top - 1);
+        if (lane == 0) bounds[warp][0] = warp < full ? few : ~0ull, bounds[warp][1] = many;
     }
     __syncwarp();
     if (cluster > 1) cluster_wait();
@@ -611,7 +638,12 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const __grid_con
 template <int TYPE, bool TOP>
 cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
     const int pieces = a.v / Elem<TYPE>::kPer;
-    if (pieces <= 256) {  // up to 8 pieces a lane
+    // A few lanes to a row where rows are many: a warp waits for no other.  Lanes and a block to a row, the sums alone:
+    // 32768 x 1000 21.8 and 112 us, 8192 x 32768 99 and 105, 2000 x 8192 12.8 and 12.3, 64 x 2048 3.5 and 2.8.  With the 8
+    // largest: 8192 x 8192 59 and 90, 8192 x 16384 116 and 114, 600 x 4096 10.2 and 9.3; the 32 largest: 8192 x 8192 94 and
+    // 109, 8192 x 16384 186 and 143.
+    const int most = !TOP ? 4096 : a.top <= kTopOfMaxima ? 2048 : 1024;
+    if (pieces <= 64 || (pieces <= most && (TOP ? 4 : 2) * (int64_t)pieces <= a.m)) {
         while (a.lanes_log2 < 5 && (2 << a.lanes_log2) < pieces) ++a.lanes_log2;
         // The largest one after another or with a warp to a row: 20000 rows of 8, top 5, 4.9 and 19.9 us; 32768 of 64, top 5,
         // 14.8 and 32.5; 20000 of 33 (fp32), top 8, 20.6 and 22.6, top 16 37.8 and 27.8; 32768 of 200, top 2, 25.5 and 30.6, top 5

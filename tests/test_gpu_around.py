@@ -461,7 +461,7 @@ def logprobs64(z, tokens, temperature):
 
 
 LOGITS = [(1, 1), (5, 2), (300, 3), (4, 7), (9, 8), (3, 9), (40, 31), (7, 33), (3, 256), (2, 257), (5, 1000), (3, 2047), (2, 2049), (3, 2064), (2, 4100),
-          (1, 9000), (2, 50001), (1, 131072), (200, 2500), (1, 40000), (65, 64), (50, 150)]
+          (1, 9000), (2, 50001), (1, 131072), (200, 2500), (1, 40000), (65, 64), (50, 150), (300, 600), (600, 1100), (1200, 2600)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "f32"])
@@ -567,7 +567,7 @@ def test_logprobs_of_odd_rows(lib, nn, v, dtype):
 
 def test_equal_logits_come_in_order(lib, nn):
     """Few values, many of them equal: the lowest index first, whatever the row's length and start."""
-    for m, v, shift in ((3, 40, 1), (2, 700, 0), (2, 5003, 3), (1, 100001, 0)):
+    for m, v, shift in ((3, 40, 1), (2, 700, 0), (2, 5003, 3), (1, 100001, 0), (400, 700, 3), (2100, 4001, 1)):
         z = Buf(m, v, torch.bfloat16, 1, shift, torch.randint(-3, 4, (m, v), generator=gen(v), device="cuda").float())
         tl, ti = torch.empty(m, 32, device="cuda"), torch.empty(m, 32, dtype=torch.int32, device="cuda")
         lib.emtk_logprobs(nn, z.t, top_logprob=tl, top_index=ti)
