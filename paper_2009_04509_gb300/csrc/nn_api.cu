@@ -161,7 +161,10 @@ emtk_matrix Staging::operator()(const emtk_matrix &m, int rows, int cols) {
 template <typename Args>
 emtk_status recurrence_inputs(emtk_nn *nn, const Args &a, std::initializer_list<emtk_matrix *> inputs, cudaStream_t s) {
     const bool uniform = a.offsets == nullptr;
-    const size_t kept = recurrence_workspace(a.rows, a.n, a.seqs, uniform, nn->sm_count);
+    bool tma = true;  // what is not copied lies on its grid
+    for (const emtk_matrix *m : inputs)
+        tma = tma && (!m->d || mm_operand_ok(m->d, m->ld, a.rows) || recurrence_copies(*m, a.rows, a.n, a.seqs, uniform, nn->sm_count));
+    const size_t kept = recurrence_workspace(a.rows, a.n, a.seqs, uniform, tma, nn->sm_count);
     CallSpace ws{nn};
     Staging stage{ws};
     for (int pass = 0; pass < 2; ++pass) {

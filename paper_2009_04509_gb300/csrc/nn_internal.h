@@ -179,7 +179,7 @@ cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, int sms, cuda
 cudaError_t init_recur_kernels();  // once per device
 // Whether a recurrence reads its input m from a copy.
 bool recurrence_copies(const emtk_matrix &m, int rows, int n, int seqs, bool uniform, int sms);
-size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, int sms);  // uniform: without offsets
+size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, bool tma, int sms);  // uniform: without offsets
 cudaError_t launch_recurrence(const emtk_recurrence_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s);  // nn_recur.cu
 cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s);
 

@@ -763,9 +763,12 @@ bool on_words(const emtk_matrix &m, int rows) {
 // 59 and 134, independent as with 64.  16896 rows of 498 columns in 88 sequences of unlike lengths:
 // both passes 410 us as independent tiles, most of whose places are empty.  Sequences of four tiles
 // at most are done before three kernels would be.
-bool along(bool uniform, int rows, int seqs, int col_tiles, int sms) {
+// Off TMA's grid a block has no tile ahead: three units to every SM (4 x 5000 steps of 2048 columns in rows
+// of 2050: along 206 and 379 us, independent 160 and 368; 10 x 2000: 165 and 317, 9 x 2222 independent 170 and 383).
+bool along(bool uniform, bool tma, int rows, int seqs, int col_tiles, int sms) {
     if ((uniform ? rows / seqs : rows) <= 4 * kTile) return true;
-    return 2 * (int64_t)seqs * col_tiles >= 3 * sms && (uniform || rows / seqs <= 4 * kTile);
+    const int64_t units = (int64_t)seqs * col_tiles;
+    return (tma ? 2 * units >= 3 * sms : units >= 3 * sms) && (uniform || rows / seqs <= 4 * kTile);
 }
 // Whether a thread takes a whole sequence, as a tile would be nearly empty: of unlike ones those below
 // kLong steps where that is so on average, the others are left to blocks that go along them.  Forward and
@@ -834,7 +837,7 @@ cudaError_t run(RecurArgs a, const Tiles *maps, void *workspace, int sms, cudaSt
         bool done;
         const cudaError_t e = run_short(recur_short_kernel<F16, ACT>, a, done, s);
         if (done) return e;
-    } else if (!along(!a.at.offsets, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
+    } else if (!along(!a.at.offsets, maps != nullptr, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
         RecurGradArgs g{};
         g.f = a.f;
         g.x = a.x;
@@ -855,7 +858,7 @@ cudaError_t run(RecurGradArgs a, const Tiles *maps, void *workspace, int sms, cu
         bool done;
         const cudaError_t e = run_short(recur_short_grad_kernel<F16, ACT>, a, done, s);
         if (done) return e;
-    } else if (!along(!a.at.offsets, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
+    } else if (!along(!a.at.offsets, maps != nullptr, a.at.rows, a.at.seqs, a.col_tiles, sms)) {
         float *const starts = sums_in(workspace, places(a.at.rows, a.at.seqs), a.at.n).made + places(a.at.rows, a.at.seqs) * a.at.n;
         const cudaError_t e = run_starts<F16, ACT, true>(a, maps, workspace, a.d_last, starts, a.d_state, s);
         if (e != cudaSuccess) return e;
@@ -875,19 +878,20 @@ cudaError_t run(const Args &a, const Tiles *maps, void *workspace, int act, int 
     }
 }
 
-// Tensor maps of the matrices that are there; false if one that is read lies off TMA's grid.
+// Tensor maps of the matrices that are there; `tma`: those that are read lie on TMA's grid.
 template <int IN, int OUT>
-bool make_maps(const emtk_nn *nn, Tiles &t, const emtk_matrix *const (&in)[IN], const emtk_matrix *const (&out)[OUT], int rows, int n) {
+cudaError_t make_maps(bool &tma, const emtk_nn *nn, Tiles &t, const emtk_matrix *const (&in)[IN], const emtk_matrix *const (&out)[OUT], int rows, int n) {
     t.waits = {nn->status, nn->timeout_ns};
-    for (const emtk_matrix *m : in)
-        if (m->d && !mm_operand_ok(m->d, m->ld, rows)) return false;
+    tma = true;
+    for (const emtk_matrix *m : in) tma = tma && (!m->d || mm_operand_ok(m->d, m->ld, rows));
+    if (!tma) return cudaSuccess;
     t.store = n % 8 == 0;
     for (const emtk_matrix *m : out) t.store = t.store && (!m->d || mm_operand_ok(m->d, m->ld, rows));
     for (int i = 0; i < IN; ++i)
-        if (in[i]->d && !encode_rows(nn, &t.in[i], *in[i], rows, n, kCols, kTile)) return false;
+        if (in[i]->d && !encode_rows(nn, &t.in[i], *in[i], rows, n, kCols, kTile)) return cudaErrorInvalidValue;
     for (int i = 0; t.store && i < OUT; ++i)
-        if (out[i]->d && !encode_rows(nn, &t.out[i], *out[i], rows, n, kCols, kTile)) return false;
-    return rows > 0;
+        if (out[i]->d && !encode_rows(nn, &t.out[i], *out[i], rows, n, kCols, kTile)) return cudaErrorInvalidValue;
+    return cudaSuccess;
 }
 
 template <bool F16, int ACT>
@@ -922,9 +926,9 @@ bool recurrence_copies(const emtk_matrix &m, int rows, int n, int seqs, bool uni
     return seqs > 0 && m.d && odd && !step_by_step(uniform, rows, seqs, n, sms);
 }
 
-size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, int sms) {
+size_t recurrence_workspace(int rows, int n, int seqs, bool uniform, bool tma, int sms) {
     if (n == 0 || seqs == 0 || step_by_step(uniform, rows, seqs, n, sms)) return 0;
-    const bool whole = along(uniform, rows, seqs, (n + kCols - 1) / kCols, sms);
+    const bool whole = along(uniform, tma, rows, seqs, (n + kCols - 1) / kCols, sms);
     return whole ? 0 : 3 * sizeof(float) * places(rows, seqs) * n;
 }
 
@@ -943,7 +947,11 @@ cudaError_t launch_recurrence(const emtk_recurrence_args &p, void *workspace, co
     a.words = on_words(p.f, p.rows) && on_words(p.x, p.rows) && on_words(p.o, p.rows) && on_words(p.y, p.rows);
     Tiles maps;
     const emtk_matrix *const in[] = {&p.f, &p.x, &p.o}, *const out[] = {&p.y};
-    const bool tma = !(step_by_step(!p.offsets, p.rows, p.seqs, p.n, nn->sm_count) && no_long(p.offsets, p.rows)) && make_maps(nn, maps, in, out, p.rows, p.n);
+    bool tma = false;
+    if (!(step_by_step(!p.offsets, p.rows, p.seqs, p.n, nn->sm_count) && no_long(p.offsets, p.rows))) {
+        const cudaError_t e = make_maps(tma, nn, maps, in, out, p.rows, p.n);
+        if (e != cudaSuccess) return e;
+    }
     return p.type == EMTK_TYPE_F16 ? run<true>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s)
                                    : run<false>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s);
 }
@@ -967,7 +975,11 @@ cudaError_t launch_recurrence_grad(const emtk_recurrence_grad_args &p, void *wor
               on_words(p.df, p.rows) && on_words(p.dx, p.rows) && on_words(p.d_o, p.rows);
     Tiles maps;
     const emtk_matrix *const in[] = {&p.f, &p.x, &p.o, &p.dy}, *const out[] = {&p.df, &p.dx, &p.d_o};
-    const bool tma = !(step_by_step(!p.offsets, p.rows, p.seqs, p.n, nn->sm_count) && no_long(p.offsets, p.rows)) && make_maps(nn, maps, in, out, p.rows, p.n);
+    bool tma = false;
+    if (!(step_by_step(!p.offsets, p.rows, p.seqs, p.n, nn->sm_count) && no_long(p.offsets, p.rows))) {
+        const cudaError_t e = make_maps(tma, nn, maps, in, out, p.rows, p.n);
+        if (e != cudaSuccess) return e;
+    }
     return p.type == EMTK_TYPE_F16 ? run<true>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s)
                                    : run<false>(a, tma ? &maps : nullptr, workspace, p.act, nn->sm_count, s);
 }
