@@ -17,7 +17,7 @@
 // of a row and its sums in shared memory took three times as long).  Sums of slices of
 // rows are joined in order, so results do not depend on timing.  16384 x 4096, both norms' and
 // the gate's sums: 159 us of rows (5.1 TB/s) and 126 of sums; 8192 x 5461, off the grid, where
-// shifting pieces into place bounds both: 189 and 180.
+// shifting pieces into place bounds both: 189 and 108 (8192 x 5464: 115 and 92).
 #include <algorithm>
 
 #include "emtk_internal.h"
