@@ -603,7 +603,7 @@ EMTK_API emtk_status emtk_residual_norm(emtk_nn *nn, const emtk_residual_norm_ar
  *   dw_pre, db_pre, dw_post, db_post [n], fp32: of the norms' weights and biases.
  * Every output may be absent.  y is needed for pre, block for d_block, d_gate,
  * dw_post and db_post; m = 0 makes the sums 0.  d_residual may be dy itself (same
- * address, same ld). */
+ * address, same ld); beside d_gate, dw_post or db_post dy is copied first then. */
 typedef struct {
     int32_t m, n, type, gate_every;
     float scale;
