@@ -1,9 +1,9 @@
 // Dropout with a mask that is never stored (nn_pieces.cuh has the generator).
 //
 // A lane takes pieces of 8 columns, neighbouring lanes neighbouring pieces of a row; HBM
-// bounds large ones (4 bytes a value), the call small ones: 16384 x 10240 in bf16 119 us, 5.6 TB/s, with
+// bounds large ones (4 bytes a value), the call small ones: 16384 x 10240 in bf16 118 us, 5.7 TB/s, with
 // the generator's 20 wide products to a piece beside it (the math pipes are what warps wait for most);
-// 235 x 333 3.1 us.  A worker's next run is found by adding: with two divisions a run 139 us.
+// 235 x 333 2.3 us.  A worker's next run is found by adding: with two divisions a run 139 us.
 #include <algorithm>
 
 #include "emtk_internal.h"
@@ -14,7 +14,7 @@ namespace emtk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFlight = 4;  // pieces of a thread whose loads are in flight together
+constexpr int kFlight = 2;  // pieces of a thread whose loads are in flight together (4: 65536 x 333 53 us; 2: 48)
 
 struct DropoutArgs {
     Rows16 x, y;
@@ -78,7 +78,7 @@ cudaError_t launch_dropout(emtk_type type, int m, int n, const emtk_matrix &x, c
     const int64_t cols = kPiece << a.lanes_log2;
     a.runs = (int)((n + cols - 1) / cols);
     const int64_t all = (int64_t)m * a.runs, per_block = kThreads >> a.lanes_log2;
-    const unsigned blocks = (unsigned)std::min<int64_t>((all + per_block - 1) / per_block, 8ll * sms);
+    const unsigned blocks = (unsigned)std::min<int64_t>((all + per_block - 1) / per_block, 16ll * sms);
     a.step_rows = blocks * per_block / a.runs;
     a.step_runs = (int)(blocks * per_block % a.runs);
     const bool any = !on_grid(x, m) || !on_grid(y, m), f16 = type == EMTK_TYPE_F16;
