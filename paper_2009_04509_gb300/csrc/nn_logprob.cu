@@ -35,7 +35,8 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostTop = 32, kMostCluster = 8;
-constexpr int kFlight = 4;  // pieces of a thread in flight
+// Pieces of a thread in flight: 512 x 131072 with 2, 4 and 8 51, 34 and 30 us, 8192 x 65536 174, 179 and 188, its gradient 332, 323 and 366.
+constexpr int kFlight = 4;
 
 constexpr float kFar = -1e4f;  // an exponent whose power is 0, in the place of -infinity where that would meet a 0
 
