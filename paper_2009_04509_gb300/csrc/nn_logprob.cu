@@ -41,6 +41,7 @@ constexpr int kFlight = 4;
 constexpr float kFar = -1e4f;  // an exponent whose power is 0, in the place of -infinity where that would meet a 0
 
 __device__ __forceinline__ float minus_infinity() { return __int_as_float(0xff800000); }
+__device__ __forceinline__ float not_a_number() { return __int_as_float(0x7fffffff); }
 
 // Elements of each type: TYPE is an emtk_type.
 template <int TYPE>
@@ -163,7 +164,7 @@ __device__ __forceinline__ uint32_t order_of(float z) {
     return z != z ? 1u : b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t order) {
-    return order == 1u ? __int_as_float(0x7fffffff) : __uint_as_float((order & 0x80000000u) ? order & 0x7fffffffu : ~order);
+    return order == 1u ? not_a_number() : __uint_as_float((order & 0x80000000u) ? order & 0x7fffffffu : ~order);
 }
 // The lowest place first among equals; 0: nothing.
 __device__ __forceinline__ uint64_t key_of(uint32_t order, int place) { return ((uint64_t)order << 32) | (uint32_t)~place; }
@@ -199,7 +200,8 @@ struct Strip {
     }
     __device__ __forceinline__ int column(int unit) const { return unit == 0 ? 0 : split.head + (unit - 1) * E::kPer; }
     __device__ __forceinline__ int units() const { return split.pieces + 2; }
-    // A unit's values, and how many there are.
+    // A unit's values, and how many there are; absent ones NaN, which largest() passes over: a unit of NaN alone is as low as
+    // its elements.
     __device__ __forceinline__ int values(int unit, float (&z)[E::kPer]) const {
         if (unit > 0 && unit <= split.pieces) {
             E::values(__ldg(reinterpret_cast<const uint4 *>(p + split.head) + unit - 1), z);
@@ -207,7 +209,7 @@ struct Strip {
         }
         const int n = unit == 0 ? split.head : split.tail;
 #pragma unroll
-        for (int i = 0; i < E::kPer; ++i) z[i] = i < n ? E::value(p[column(unit) + i]) : minus_infinity();
+        for (int i = 0; i < E::kPer; ++i) z[i] = i < n ? E::value(p[column(unit) + i]) : not_a_number();
         return n;
     }
 };
@@ -223,7 +225,7 @@ struct Best {
 };
 
 template <int N>
-__device__ __forceinline__ float largest(const float (&z)[N]) {
+__device__ __forceinline__ float largest(const float (&z)[N]) {  // NaN only if all are
     float top = z[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, z[i]);
@@ -241,10 +243,14 @@ __device__ __forceinline__ Sums take_strip(const Strip<TYPE> &s, float k, Best &
         if (TOP) best.offer(order_of(top), unit);
     };
     float z[E::kPer];
-    if (s.ends && s.t == 0 && s.split.head > 0) {
-        s.values(0, z);
-        take(z, largest(z), 0);
-    }
+    auto take_some = [&](int unit) {  // of the row's ends
+        const int n = s.values(unit, z);
+        const float top = largest(z);
+#pragma unroll
+        for (int i = 0; i < E::kPer; ++i) z[i] = i < n ? z[i] : minus_infinity();
+        take(z, top, unit);
+    };
+    if (s.ends && s.t == 0 && s.split.head > 0) take_some(0);
     const uint4 *const q = reinterpret_cast<const uint4 *>(s.p + s.split.head);
     for (int at = s.first; at < s.end; at += kFlight * s.threads) {
         uint4 w[kFlight];
@@ -258,10 +264,7 @@ __device__ __forceinline__ Sums take_strip(const Strip<TYPE> &s, float k, Best &
             take(z, E::largest(w[i]), at + i * s.threads + 1);
         }
     }
-    if (s.ends && s.t == s.threads - 1 && s.split.tail > 0) {
-        s.values(s.units() - 1, z);
-        take(z, largest(z), s.units() - 1);
-    }
+    if (s.ends && s.t == s.threads - 1 && s.split.tail > 0) take_some(s.units() - 1);
     return sums.all();
 }
 
@@ -353,7 +356,7 @@ __device__ __forceinline__ void finish_row(const LogprobArgs &a, int64_t row, co
     const bool empty = x.m == minus_infinity() && x.s == 0.f;
     const float log_s = logf(x.s);
     if (a.logprob)
-        a.logprob[row] = token < 0 ? 0.f : token >= a.v ? __int_as_float(0x7fffffff) : logprob_of(z, x, log_s, a.inverse_t);
+        a.logprob[row] = token < 0 ? 0.f : token >= a.v ? not_a_number() : logprob_of(z, x, log_s, a.inverse_t);
     if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - x.w * kLn2 / x.s;
     if (a.lse) a.lse[row] = empty ? minus_infinity() : fmaf(x.m, a.inverse_t, log_s);
 }

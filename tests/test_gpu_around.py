@@ -578,6 +578,33 @@ def test_equal_logits_come_in_order(lib, nn):
     assert ti[0].tolist() == list(range(59999, 59979, -1))
 
 
+@pytest.mark.parametrize("m,v", [(6, 9), (40, 20), (5, 150), (5, 300), (300, 600), (6, 1100), (5, 20000), (5, 50257)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "f32"])
+def test_the_largest_beside_nan(lib, nn, m, v, dtype):
+    """Rows of NaN, with fewer logits above it than are asked for, and with NaN alone where a row begins and ends: NaN counts
+    as the least logit, and every answer is one of the row's columns."""
+    g = gen(v)
+    for top in (1, 2, 5, 21, 32):
+        if top > v:
+            continue
+        for pad, shift in ((0, 0), (1, 0), (3, 5)):
+            rows = torch.full((5, v), math.nan, device="cuda")
+            few = torch.linspace(8, v - 9, top - 1).long().unique() if v > 64 else torch.arange(1, min(v - 1, top))
+            rows[1, few.cuda()] = randn(g, len(few))
+            rows[2, min(7, v // 3):max(v - 7, v - v // 3)] = -math.inf
+            rows[3, v // 2:v // 2 + top - 1] = randn(g, rows[3, v // 2:v // 2 + top - 1].shape[0])
+            rows[4, v // 2] = -math.inf
+            z = Buf(m, v, DT[dtype], pad, shift, rows[torch.arange(m, device="cuda") % 5])
+            tl, ti = torch.zeros(m, top, device="cuda"), torch.full((m, top), -7, dtype=torch.int32, device="cuda")
+            lib.emtk_logprobs(nn, z.t, top_logprob=tl, top_index=ti)
+            x = z.t.float().cpu().numpy()
+            nan = np.isnan(x)
+            want = np.stack([np.lexsort((np.arange(v), -np.where(nan[i], 0, x[i]), nan[i]))[:top] for i in range(min(m, 40))])
+            assert np.array_equal(ti[:40].cpu().numpy(), want), (top, pad, shift)
+            assert torch.equal(ti, ti[torch.arange(m, device="cuda") % 5]), (top, pad, shift)
+            assert torch.isnan(tl).all()
+
+
 def test_logprobs_of_empty_sizes(lib, nn):
     lib.emtk_logprobs(nn, torch.empty(0, 5, device="cuda"), entropy=torch.empty(0, device="cuda"))
     lp, ent, lse = (torch.empty(3, device="cuda") for _ in range(3))
