@@ -159,10 +159,10 @@ __device__ __forceinline__ float2 minus_rest(uint32_t w) {
 constexpr uint32_t kKeepAll16 = 0x7c007c00u, kKeepAll = 0x7f807f80u;  // f of a step that is not there: infinity
 __device__ __forceinline__ float2 step(float2 m, float2 h, float2 x) { return fma2(m, h - x, h); }  // a h + (1 - a) x
 __device__ __forceinline__ float2 kept(float2 m, float2 v) { return fma2(m, v, v); }                // a v
-// a (1 - a): a = exp(f) (1 - a), right to its last bits where it is small too; beyond 80 it is 1
+// a (1 - a): a = exp(f) (1 - a), right to its last bits where it is small too; beyond 80, where exp(f) may be infinity, it is 1
 __device__ __forceinline__ float slope_of(float f, float m) {
     const float b = -m;
-    return exp2_f((f > 80.f ? 80.f : f) * kLog2E) * b * b;
+    return (f > 80.f ? 1.f : exp2_f(f * kLog2E) * b) * b;
 }
 
 // ---- a run's factor, held as q (above); -0 is the complement 0

@@ -810,6 +810,28 @@ def test_far_gates(lib, nn):
     assert float(dstate[0, 0]) == T and float(dstate[0, 1]) == T and not dstate[0, 2:4].any()
 
 
+@pytest.mark.parametrize("T,seqs", [(6, 1), (300, 1), (300, 40), (20000, 1)])
+def test_slopes_of_gates_that_keep_nearly_all(lib, nn, T, seqs):
+    """f from 78 to 87: a (1 - a) = 1 - a to 33 digits, small but in bf16's range.  df = g (h - x) (1 - a) is off by (8 + 4 |f|) E of
+    the exponential and a rounding for every step that g comes through."""
+    n = 38
+    rows = T * seqs
+    f = (78 + 0.5 * (torch.arange(n, device="cuda") % 19)).to(torch.bfloat16).expand(rows, n).contiguous()
+    x = torch.full((rows, n), -2.0 ** 40, dtype=torch.bfloat16, device="cuda")
+    dy = torch.full((rows, n), 2.0 ** 60, dtype=torch.bfloat16, device="cuda")
+    state = torch.full((seqs, n), 2.0 ** 40, device="cuda")
+    y, df, dx = (torch.empty_like(x) for _ in range(3))
+    states = lib.emtk_recurrence_states(rows, n, seqs)
+    lib.emtk_recurrence(nn, f, x, y, seqs=seqs, state=state, states=states)
+    lib.emtk_recurrence_backward(nn, dy, f, x, states, df, dx, seqs=seqs)
+    g = 2.0 ** 60 * (T - torch.arange(T, device="cuda", dtype=torch.float64)).repeat(seqs)[:, None]
+    b = torch.sigmoid(-f.double())
+    off = (8 + 4 * 87 + T) * E
+    near(dx, g * b, "bf16", off * g * b, "dx")
+    want = g * 2.0 ** 41 * b * torch.sigmoid(f.double())
+    near(df, want, "bf16", off * want, "df")
+
+
 def test_long_memories_settle_right(lib, nn):
     """f = 12: a state that remembers 160,000 steps moves towards x by 6e-6 a step; what 1 - a loses in fp32 would show."""
     T, n = 20000, 32
