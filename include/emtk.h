@@ -616,8 +616,9 @@ typedef struct {
 EMTK_API emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residual_norm_grad_args *args,
                                                  emtk_stream stream);
 
-/* Log probabilities of logits [m][v] (BF16, F16 or F32) at a temperature > 0:
- * with l_j = z_j / temperature - ln sum_k exp(z_k / temperature) of a row,
+/* Log probabilities of logits [m][v] (BF16, F16 or F32) at a temperature > 0
+ * (at least 4.3e-39, so that log2(e) / temperature is finite in fp32): with
+ * l_j = z_j / temperature - ln sum_k exp(z_k / temperature) of a row,
  *   logprob [m] = l of the row's token; 0 where the token is negative (none is
  *                 given), NaN where it is v or more;
  *   entropy [m] = -sum_j exp(l_j) l_j;

@@ -80,6 +80,8 @@ struct Checks {
         need(n.param_type == type || n.param_type == EMTK_TYPE_F32);
         for (const void *p : {n.weight, n.bias}) vector(p, n.param_type == EMTK_TYPE_F32 ? 4 : 2);
     }
+    // > 0, and log2(e) / temperature, which the kernels scale logits by, finite.
+    void temperature(float t) { need(t > 0.f && t < INFINITY && 1.4426950408889634f * (1.f / t) < INFINITY); }
     void drop(const emtk_drop &d) {
         need(d.p >= 0.f && d.p < 1.f);
         vector(d.d_offset, 8);
@@ -680,8 +682,8 @@ emtk_status emtk_logprobs(emtk_nn *nn, const emtk_logprobs_args *p, emtk_stream 
     const emtk_logprobs_args &a = *p;
     Checks c;
     c.need(sizes_ok(a.m, a.v, 0) && (type16(a.type) || a.type == EMTK_TYPE_F32));
-    c.need(a.top >= 0 && a.top <= std::min(32, a.v) && a.temperature > 0.f && a.temperature < INFINITY &&
-           1.f / a.temperature < INFINITY);
+    c.need(a.top >= 0 && a.top <= std::min(32, a.v));
+    c.temperature(a.temperature);
     c.need((a.tokens == nullptr) == (a.logprob == nullptr));
     c.need((a.top > 0) == (a.top_logprob != nullptr) && (a.top > 0) == (a.top_index != nullptr));
     if (c.st != EMTK_OK) return c.st;
@@ -702,7 +704,7 @@ emtk_status emtk_logprobs_backward(emtk_nn *nn, const emtk_logprobs_grad_args *p
     const size_t elem = a.type == EMTK_TYPE_F32 ? 4 : 2;
     Checks c;
     c.need(sizes_ok(a.m, a.v, 0) && (type16(a.type) || a.type == EMTK_TYPE_F32));
-    c.need(a.temperature > 0.f && a.temperature < INFINITY && 1.f / a.temperature < INFINITY);
+    c.temperature(a.temperature);
     c.need(a.m == 0 || a.lse);
     c.need(!a.d_logprob || a.tokens);
     c.need(!a.d_entropy || a.entropy);

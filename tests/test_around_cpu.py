@@ -174,6 +174,13 @@ def test_refusals_without_device(lib, handle, entry):
     assert getattr(lib, name)(handle, None, None) == emtk.EMTK_ERR_ARG
 
 
+@pytest.mark.parametrize("t", [2.9e-39, 4e-39, 4.23e-39, 0.0, -1e-3, NAN, INF])
+def test_temperatures_too_small_to_scale_by_are_refused(lib, handle, t):
+    """log2(e) / T, which logits are scaled by, is beyond fp32 from 4.24e-39 down: 0 times it would be NaN."""
+    assert lib.emtk_logprobs(handle, logprobs(t=t), None) == emtk.EMTK_ERR_ARG
+    assert lib.emtk_logprobs_backward(handle, logprobs_grad(t=t), None) == emtk.EMTK_ERR_ARG
+
+
 def test_dropout_refusals_without_device(lib, handle):
     x, y = emtk._PACK_MATRIX.pack(*mat()), emtk._PACK_MATRIX.pack(*mat(A + 4096))
     drop = lambda p=0.5, t=0: emtk._PACK_DROP.pack(1, 2, t, p)  # noqa: E731

@@ -605,6 +605,16 @@ def test_the_largest_beside_nan(lib, nn, m, v, dtype):
             assert torch.isnan(tl).all()
 
 
+def test_the_smallest_temperature(lib, nn):
+    """All but the largest logits have probability 0, and nothing is NaN."""
+    t = 4.3e-39
+    z = torch.tensor([[0.0, -1.0, 0.0, -math.inf], [3.0, 2.0, 1.0, 3.0]], device="cuda")
+    tokens = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+    lp, ent = torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
+    lib.emtk_logprobs(nn, z, tokens, lp, ent, temperature=t)
+    assert (lp + math.log(2)).abs().max() <= 8 * E and (ent - math.log(2)).abs().max() <= 8 * E
+
+
 def test_logprobs_of_empty_sizes(lib, nn):
     lib.emtk_logprobs(nn, torch.empty(0, 5, device="cuda"), entropy=torch.empty(0, device="cuda"))
     lp, ent, lse = (torch.empty(3, device="cuda") for _ in range(3))
