@@ -706,7 +706,7 @@ cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, int sms, cuda
     a.m = p.m;
     a.v = p.v;
     a.inverse_t = 1.f / p.temperature;
-    const int64_t pieces = std::max(1, p.v * elem / 16);
+    const int64_t pieces = std::max<int64_t>(1, (int64_t)p.v * elem / 16);
     // Up to 8 pieces a thread, as long as threads are left for the SMs: 32768 x 1000 with 1, 4 and 8 pieces a thread 53, 28 and
     // 26 us, 4000 x 1000 with 1, 2 and 8 5.4, 4.5 and 6.2, 64 x 1000 1.8, 2.0 and 4.0.
     int each = 1;

@@ -615,6 +615,24 @@ def test_the_smallest_temperature(lib, nn):
     assert (lp + math.log(2)).abs().max() <= 8 * E and (ent - math.log(2)).abs().max() <= 8 * E
 
 
+@pytest.mark.parametrize("dtype,v", [("f32", 1 << 29), ("f32", (1 << 29) + 3), ("bf16", 1 << 30)])
+def test_rows_of_two_gigabytes(lib, nn, dtype, v):
+    """One row whose bytes pass 31 bits: its pieces go to all threads, and every element is written."""
+    z = torch.zeros(1, v, dtype=DT[dtype], device="cuda")
+    z[0, v - 1] = 3.0
+    dz = torch.full_like(z, math.nan)
+    lse, tl, ti = torch.empty(1, device="cuda"), torch.empty(1, 1, device="cuda"), torch.empty(1, 1, dtype=torch.int32, device="cuda")
+    lib.emtk_logprobs(nn, z, lse=lse, top_logprob=tl, top_index=ti)
+    total = v - 1 + math.exp(3.0)
+    assert ti.item() == v - 1 and abs(lse.item() - math.log(total)) <= 64 * E * math.log(total)
+    lib.emtk_logprobs_backward(nn, z, lse, dz, tokens=ti.view(-1), d_logprob=torch.ones(1, device="cuda"))
+    assert not torch.isnan(dz).any()
+    want = torch.full((3000,), -1 / total, dtype=torch.float64, device="cuda")
+    for part in (slice(0, 3000), slice(v // 2, v // 2 + 3000), slice(v - 3001, v - 1)):
+        near(dz[0, part], want, dtype, 64 * 21 * E / total)
+    near(dz[0, v - 1:], 1 - torch.full((1,), math.exp(3.0) / total, dtype=torch.float64, device="cuda"), dtype, 4 * E)
+
+
 def test_logprobs_of_empty_sizes(lib, nn):
     lib.emtk_logprobs(nn, torch.empty(0, 5, device="cuda"), entropy=torch.empty(0, device="cuda"))
     lp, ent, lse = (torch.empty(3, device="cuda") for _ in range(3))
