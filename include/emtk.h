@@ -622,7 +622,9 @@ EMTK_API emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residua
  *   logprob [m] = l of the row's token; 0 where the token is negative (none is
  *                 given), NaN where it is v or more;
  *   entropy [m] = -sum_j exp(l_j) l_j;
- *   lse [m]     = ln sum_k exp(z_k / temperature), for the backward call;
+ *   lse [m]     = ln sum_k exp(z_k / temperature), for the backward call
+ *                 (beyond fp32's range infinite: a row far from 0 at a small
+ *                 temperature);
  *   top_logprob, top_index [m][top]: the `top` largest, 0 <= top <= 32 and
  *                 top <= v, descending, the lowest index first among equals.
  * All fp32, contiguous, each or NULL (tokens and logprob go together, top's two
@@ -644,9 +646,11 @@ EMTK_API emtk_status emtk_logprobs(emtk_nn *nn, const emtk_logprobs_args *args, 
 /* The gradient of logits from d_logprob [m] and d_entropy [m] (each or NULL),
  * with the lse, and for d_entropy the entropy, that emtk_logprobs wrote:
  *   d_logits_j = (d_logprob (1[j is the token] - p_j) - d_entropy p_j (l_j + entropy)) / temperature
- * with p = exp(l); 0 where p_j = 0 and j is no token.  A token outside 0 .. v - 1
- * gets no d_logprob.  d_logits, of the logits' type, may be the logits themselves
- * (same address, same ld). */
+ * with p = exp(l); 0 where p_j = 0 and j is no token, and in a row of -infinity
+ * alone.  Up to 32 lse is taken as it is, off by a rounding, which is 2^-20 of p
+ * at most; in rows beyond, the logits' maximum and sum are taken again, a second
+ * read.  A token outside 0 .. v - 1 gets no d_logprob.  d_logits, of the logits'
+ * type, may be the logits themselves (same address, same ld). */
 typedef struct {
     int32_t m, v, type, reserved0;
     float temperature;

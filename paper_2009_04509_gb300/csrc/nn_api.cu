@@ -255,9 +255,11 @@ emtk_status emtk_nn_create(int device, int64_t workspace_bytes, int64_t wait_tim
     if (e == cudaSuccess) e = init_mm_kernels();
     if (e == cudaSuccess) e = init_norm_kernels();
     if (e == cudaSuccess) e = init_recur_kernels();
-    if (e == cudaSuccess) e = dev_alloc(&status, sizeof(int) + sizeof(SlopeRange));
+    const size_t head = align_up(sizeof(int) + sizeof(SlopeRange));
+    if (e == cudaSuccess) e = dev_alloc(&status, head + sizeof(float2) * kCutRows * nn->sm_count);
     nn->status = static_cast<int *>(status);
     nn->range = reinterpret_cast<SlopeRange *>(nn->status + 1);
+    nn->far_sums = reinterpret_cast<float2 *>(static_cast<uint8_t *>(status) + head);
     if (e == cudaSuccess) e = cudaMemset(nn->status, 0, sizeof(int) + sizeof(SlopeRange));
     if (e == cudaSuccess && workspace_bytes > 0) {
         e = dev_alloc(&nn->ws, (size_t)workspace_bytes);
@@ -719,7 +721,7 @@ emtk_status emtk_logprobs_backward(emtk_nn *nn, const emtk_logprobs_grad_args *p
     DeviceGuard g(nn->device);
     if (!g.ok) return EMTK_ERR_CUDA;
     Range range("emtk logprobs backward");
-    return status_of(launch_logprobs_grad(a, nn->sm_count, reinterpret_cast<cudaStream_t>(stream)));
+    return status_of(launch_logprobs_grad(a, nn, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 emtk_status emtk_recurrence(emtk_nn *nn, const emtk_recurrence_args *p, emtk_stream stream) {

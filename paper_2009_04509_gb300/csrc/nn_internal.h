@@ -25,6 +25,7 @@ struct emtk_nn {
     int debug_stall = 0;
     int *status = nullptr;   // device status word, as a context's
     emtk::SlopeRange *range = nullptr;  // beside it: of the running backward call's slopes
+    float2 *far_sums = nullptr;         // and [sm_count * kCutRows]: rows' sums that a gradient of logits takes again
     void *ws = nullptr;      // workspace of the running call
     size_t ws_bytes = 0;
     bool captured = false;   // a graph holds the workspace's address
@@ -37,6 +38,7 @@ struct emtk_nn {
 
 namespace emtk {
 
+constexpr int kCutRows = 4;   // for each SM, of a gradient of logits whose rows go to several blocks
 constexpr int kQ8Block = 32;  // columns that share a checkpoint scale
 constexpr int kMaxNormWidth = 16384;  // of residual norms: a row is held in a block's registers
 
@@ -175,7 +177,7 @@ cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, const emtk_nn
 size_t residual_norm_workspace(const emtk_residual_norm_grad_args &p, int sms);
 cudaError_t launch_residual_norm_grad(const emtk_residual_norm_grad_args &p, void *workspace, const emtk_nn *nn, cudaStream_t s);
 cudaError_t launch_logprobs(const emtk_logprobs_args &p, int sms, cudaStream_t s);  // nn_logprob.cu
-cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, int sms, cudaStream_t s);
+cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, const emtk_nn *nn, cudaStream_t s);
 cudaError_t init_recur_kernels();  // once per device
 // Whether a recurrence reads its input m from a copy.
 bool recurrence_copies(const emtk_matrix &m, int rows, int n, int seqs, bool uniform, int sms);

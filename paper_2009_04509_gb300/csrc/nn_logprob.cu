@@ -6,7 +6,7 @@
 // when the maximum rises by d (in units of T), S becomes S exp(-d) and W exp(-d) (W - d S).
 // Two runs' triples join the same way.  HBM bounds large calls (one read of the logits;
 // the gradient one read and one write), the call small ones.  8192 x 65536 in bf16 179 us (6.0 TB/s,
-// 0.88 of a copy's rate), its gradient 323 (6.65 TB/s, 0.98); one row of 131072 with its 8 largest
+// 0.88 of a copy's rate), its gradient 312 (6.9 TB/s, 1.01); one row of 131072 with its 8 largest
 // 8.3 us on a cluster of 8 blocks.  Two elements to an instruction took the first from 199 to 180 us.
 //
 // The K largest come from a second look at a small part of the row.  On the way each thread
@@ -170,6 +170,15 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 __device__ __forceinline__ uint64_t key_of(uint32_t order, int place) { return ((uint64_t)order << 32) | (uint32_t)~place; }
 __device__ __forceinline__ int place_of(uint64_t key) { return (int)~(uint32_t)key; }
 
+// lse is max / T + ln S rounded to fp32: off by up to half a step, and p = exp(z / T - lse) by so much of itself, 2^-20 up to
+// 32, where ordinary rows end.  Beyond, up to a row of the type's least values, whose lse holds nothing of ln S any more, the
+// gradient takes the row's maximum and S again: 8192 x 65536 in bf16 312 us of ordinary rows, 534 of such.  A row that is cut
+// among blocks and overwritten has its sums taken first, by the forward kernel, whose blocks leave ordinary rows at
+// once (1 x 131072 in place 2.7 us, 2.0 apart).  With its own code for such rows an ordinary element has no instruction more:
+// one for all took 345.
+constexpr float kFarLse = 32.f;
+__device__ __forceinline__ bool is_far(float lse) { return fabsf(lse) > kFarLse; }
+
 struct LogprobArgs {
     const uint8_t *z;
     int64_t row_bytes;
@@ -179,6 +188,8 @@ struct LogprobArgs {
     int m, v, top;
     float k, inverse_t;  // log2(e) / T, 1 / T
     int lanes_log2;      // of a row, in lanes_kernel
+    const float *far;    // the gradient's: rows whose lse is far alone, and of them
+    float2 *sums;        // the maximum and S
 };
 
 // A thread's strip of a row, thread t of `threads` at part `part` of `parts` of it: every
@@ -232,7 +243,8 @@ __device__ __forceinline__ float largest(const float (&z)[N]) {  // NaN only if 
     return top;
 }
 
-template <int TYPE, bool TOP>
+// WRITTEN: the kernel may write where the logits are, so they do not take the read-only path.
+template <int TYPE, bool TOP, bool WRITTEN = false, int FLIGHT = kFlight>
 __device__ __forceinline__ Sums take_strip(const Strip<TYPE> &s, float k, Best &best) {
     using E = Elem<TYPE>;
     Sums2 sums;
@@ -252,13 +264,13 @@ __device__ __forceinline__ Sums take_strip(const Strip<TYPE> &s, float k, Best &
     };
     if (s.ends && s.t == 0 && s.split.head > 0) take_some(0);
     const uint4 *const q = reinterpret_cast<const uint4 *>(s.p + s.split.head);
-    for (int at = s.first; at < s.end; at += kFlight * s.threads) {
-        uint4 w[kFlight];
+    for (int at = s.first; at < s.end; at += FLIGHT * s.threads) {
+        uint4 w[FLIGHT];
 #pragma unroll
-        for (int i = 0; i < kFlight; ++i)
-            if (at + i * s.threads < s.end) w[i] = __ldg(q + at + i * s.threads);
+        for (int i = 0; i < FLIGHT; ++i)
+            if (at + i * s.threads < s.end) w[i] = WRITTEN ? q[at + i * s.threads] : __ldg(q + at + i * s.threads);
 #pragma unroll
-        for (int i = 0; i < kFlight; ++i) {
+        for (int i = 0; i < FLIGHT; ++i) {
             if (at + i * s.threads >= s.end) continue;
             E::values(w[i], z);
             take(z, E::largest(w[i]), at + i * s.threads + 1);
@@ -359,6 +371,7 @@ __device__ __forceinline__ void finish_row(const LogprobArgs &a, int64_t row, co
         a.logprob[row] = token < 0 ? 0.f : token >= a.v ? not_a_number() : logprob_of(z, x, log_s, a.inverse_t);
     if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - x.w * kLn2 / x.s;
     if (a.lse) a.lse[row] = empty ? minus_infinity() : fmaf(x.m, a.inverse_t, log_s);
+    if (a.sums) a.sums[row] = make_float2(x.m, x.s);
 }
 __device__ __forceinline__ void finish_top(const LogprobArgs &a, int64_t row, const Sums &x, uint64_t key, int rank) {
     a.top_logprob[row * a.top + rank] = logprob_of(value_of((uint32_t)(key >> 32)), x, logf(x.s), a.inverse_t);
@@ -470,6 +483,10 @@ __global__ void __launch_bounds__(kThreads) logprob_block_kernel(const __grid_co
     if (cluster > 1) cluster_arrive();  // it has started
     pdl_trigger();
     pdl_wait();
+    if (a.far && !is_far(a.far[row])) {  // all of the row's blocks leave
+        if (cluster > 1) cluster_wait();
+        return;
+    }
     const int token = a.tokens ? a.tokens[row] : -1;
     const float z = threadIdx.x == 0 ? token_logit<TYPE>(a, p, token) : 0.f;
     const Strip<TYPE> strip(p, a.v, threadIdx.x, kThreads, rank, cluster);
@@ -575,49 +592,68 @@ struct LogprobGradArgs {
     const int32_t *tokens;
     const float *lse, *entropy, *d_logprob, *d_entropy;
     int m, v;
-    float inverse_t;
-    int lanes_log2;  // threads of a row
+    float k, inverse_t;  // log2(e) / T, 1 / T
+    int lanes_log2;      // threads of a row, in a block
+    const float2 *sums;  // far rows' maximum and S; null: the row's threads take them
 };
+
+// A row's maximum and S by its `lanes` threads (a power of two, to kThreads), of which this is t; in each of them.
+template <int TYPE>
+__device__ __forceinline__ float2 sums_again(const uint8_t *row, int v, float k, int t, int lanes) {
+    __shared__ Sums warps[kWarps];
+    const Strip<TYPE> strip(row, v, t, lanes, 0, 1);
+    Best none;
+    Sums sums = take_strip<TYPE, false, true, 1>(strip, k, none);
+    const int lane = threadIdx.x & 31, width = min(lanes, 32);
+    const uint32_t mask = (0xffffffffu >> (32 - width)) << (lane & ~(width - 1));
+    for (int d = width >> 1; d > 0; d >>= 1) {
+        Sums o;
+        o.m = __shfl_xor_sync(mask, sums.m, d);
+        o.s = __shfl_xor_sync(mask, sums.s, d);
+        o.w = 0.f;
+        sums.join(o, k);
+    }
+    if (lanes > 32) {
+        if (lane == 0) warps[threadIdx.x / 32] = sums;
+        switch ((int)threadIdx.x / lanes) {  // (by number: with one that is computed a block would hold all 16)
+            case 0: asm volatile("bar.sync 1, %0;" ::"r"(lanes) : "memory"); break;
+            case 1: asm volatile("bar.sync 2, %0;" ::"r"(lanes) : "memory"); break;
+            case 2: asm volatile("bar.sync 3, %0;" ::"r"(lanes) : "memory"); break;
+            default: asm volatile("bar.sync 4, %0;" ::"r"(lanes) : "memory");
+        }
+        const int first = (int)threadIdx.x / lanes * (lanes / 32);
+        sums = warps[first];
+        for (int w = 1; w < lanes / 32; ++w) sums.join(warps[first + w], k);
+    }
+    return make_float2(sums.m, sums.s);
+}
 
 // What a row's elements share.
 struct RowGrad {
-    float lse, inverse_t, dl, dh, dh_h;  // d_logprob, d_entropy, d_entropy * entropy
+    float base, lse, inverse_t, dl, dh, dh_h;  // d_logprob, d_entropy, d_entropy * entropy; FAR: the maximum, and ln S as lse
     int token;
+    bool empty;  // FAR, and of -infinity alone: nothing to change
+    template <bool FAR>
     __device__ __forceinline__ float of(float z, int column) const {
-        const float l = fmaf(z, inverse_t, -lse), p = exp2_f(l * kLog2E);
+        if (FAR && empty) return 0.f;
+        const float l = fmaf(FAR ? z - base : z, inverse_t, -lse), p = exp2_f(l * kLog2E);
         float g = p == 0.f ? 0.f : -p * (dl + fmaf(dh, l, dh_h));
         if (column == token) g += dl;
         return g * inverse_t;
     }
 };
 
-template <int TYPE>
-__global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const __grid_constant__ LogprobGradArgs a) {
+// A row's gradient by `threads` threads, of which this is t.
+template <int TYPE, bool FAR>
+__device__ __forceinline__ void write_row(const RowGrad &g, const typename Elem<TYPE>::T *z, typename Elem<TYPE>::T *dz, int v, int t, int threads) {
     using E = Elem<TYPE>;
-    using T = typename E::T;
-    const int lanes = 1 << a.lanes_log2, threads = lanes * gridDim.y;
-    const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> a.lanes_log2;
-    const int t = blockIdx.y * lanes + (threadIdx.x & (lanes - 1));
-    pdl_trigger();
-    pdl_wait();
-    if (row >= a.m) return;
-    const T *const z = reinterpret_cast<const T *>(a.z + row * a.row_bytes);
-    T *const dz = reinterpret_cast<T *>(a.dz + row * a.d_row_bytes);
-    RowGrad g;
-    g.lse = a.lse[row];
-    g.inverse_t = a.inverse_t;
-    g.token = a.tokens ? a.tokens[row] : -1;
-    g.dl = a.d_logprob && g.token >= 0 && g.token < a.v ? a.d_logprob[row] : 0.f;
-    g.dh = a.d_entropy ? a.d_entropy[row] : 0.f;
-    g.dh_h = a.d_entropy ? g.dh * a.entropy[row] : 0.f;
-    const bool empty = g.lse == minus_infinity();  // nothing to change
     // pieces where both rows lie alike on 16 bytes, else elements
     const bool alike = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
-    Split s = split_row<TYPE>(z, a.v);
-    if (!alike) s = {a.v, 0, 0};
+    Split s = split_row<TYPE>(z, v);
+    if (!alike) s = {v, 0, 0};
     for (int e = t; e < s.head + s.tail; e += threads) {
         const int column = e < s.head ? e : s.pieces * E::kPer + e;
-        dz[column] = E::stored(empty ? 0.f : g.of(E::value(z[column]), column));
+        dz[column] = E::stored(g.of<FAR>(E::value(z[column]), column));
     }
     const uint4 *const q = reinterpret_cast<const uint4 *>(z + s.head);
     uint4 *const to = reinterpret_cast<uint4 *>(dz + s.head);
@@ -632,13 +668,48 @@ __global__ void __launch_bounds__(kThreads) logprob_grad_kernel(const __grid_con
             float v[E::kPer];
             E::values(w[i], v);
 #pragma unroll
-            for (int j = 0; j < E::kPer; ++j)
-                v[j] = empty ? 0.f : g.of(v[j], s.head + (at + i * threads) * E::kPer + j);
+            for (int j = 0; j < E::kPer; ++j) v[j] = g.of<FAR>(v[j], s.head + (at + i * threads) * E::kPer + j);
             to[at + i * threads] = E::stored(v);
         }
     }
 }
 
+template <int TYPE>
+__global__ void __launch_bounds__(kThreads, 5) logprob_grad_kernel(const __grid_constant__ LogprobGradArgs a) {
+    using T = typename Elem<TYPE>::T;
+    const int lanes = 1 << a.lanes_log2, threads = lanes * gridDim.y;
+    const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> a.lanes_log2;
+    const int lane = threadIdx.x & (lanes - 1), t = blockIdx.y * lanes + lane;
+    pdl_trigger();
+    pdl_wait();
+    if (row >= a.m) return;
+    const T *const z = reinterpret_cast<const T *>(a.z + row * a.row_bytes);
+    T *const dz = reinterpret_cast<T *>(a.dz + row * a.d_row_bytes);
+    RowGrad g;
+    g.lse = a.lse[row];
+    g.inverse_t = a.inverse_t;
+    g.token = a.tokens ? a.tokens[row] : -1;
+    g.dl = a.d_logprob && g.token >= 0 && g.token < a.v ? a.d_logprob[row] : 0.f;
+    g.dh = a.d_entropy ? a.d_entropy[row] : 0.f;
+    g.dh_h = a.d_entropy ? g.dh * a.entropy[row] : 0.f;
+    if (!is_far(g.lse)) return write_row<TYPE, false>(g, z, dz, a.v, t, threads);
+    const float2 x = a.sums ? a.sums[row] : sums_again<TYPE>(reinterpret_cast<const uint8_t *>(z), a.v, a.k, lane, lanes);
+    g.base = x.x;
+    g.lse = logf(x.y);
+    g.empty = x.x == minus_infinity() && x.y == 0.f;
+    write_row<TYPE, true>(g, z, dz, a.v, t, threads);
+}
+
+template <int TYPE, bool TOP>
+cudaError_t run_blocks(const LogprobArgs &a, int sms, cudaStream_t s) {
+    const int pieces = a.v / Elem<TYPE>::kPer;
+    // blocks for every SM, each with a round of pieces at least
+    int cluster = 1;
+    while (cluster < kMostCluster && (int64_t)a.m * cluster < 2 * sms && pieces >= 2 * cluster * kThreads * kFlight) cluster *= 2;
+    if (cluster == 1)
+        return launch_pdl(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)a.m), dim3(kThreads), 0, s, a, cluster);
+    return launch_cluster(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)(a.m * cluster)), dim3(kThreads), 0, cluster, s, a, cluster);
+}
 template <int TYPE, bool TOP>
 cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
     const int pieces = a.v / Elem<TYPE>::kPer;
@@ -656,12 +727,7 @@ cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
         const int64_t rows = kThreads >> a.lanes_log2;
         return launch_pdl(logprob_lanes_kernel<TYPE, TOP>, dim3((unsigned)((a.m + rows - 1) / rows)), dim3(kThreads), 0, s, a);
     }
-    // blocks for every SM, each with a round of pieces at least
-    int cluster = 1;
-    while (cluster < kMostCluster && (int64_t)a.m * cluster < 2 * sms && pieces >= 2 * cluster * kThreads * kFlight) cluster *= 2;
-    if (cluster == 1)
-        return launch_pdl(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)a.m), dim3(kThreads), 0, s, a, cluster);
-    return launch_cluster(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)(a.m * cluster)), dim3(kThreads), 0, cluster, s, a, cluster);
+    return run_blocks<TYPE, TOP>(a, sms, s);
 }
 template <int TYPE>
 cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
@@ -690,7 +756,7 @@ cudaError_t launch_logprobs(const emtk_logprobs_args &p, int sms, cudaStream_t s
     return p.type == EMTK_TYPE_F16 ? run<EMTK_TYPE_F16>(a, sms, s) : run<EMTK_TYPE_BF16>(a, sms, s);
 }
 
-cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, int sms, cudaStream_t s) {
+cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, const emtk_nn *nn, cudaStream_t s) {
     if (p.m == 0 || p.v == 0) return cudaSuccess;
     LogprobGradArgs a{};
     const int elem = p.type == EMTK_TYPE_F32 ? 4 : 2;
@@ -706,6 +772,8 @@ cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, int sms, cuda
     a.m = p.m;
     a.v = p.v;
     a.inverse_t = 1.f / p.temperature;
+    a.k = kLog2E * a.inverse_t;
+    const int sms = nn->sm_count;
     const int64_t pieces = std::max<int64_t>(1, (int64_t)p.v * elem / 16);
     // Up to 8 pieces a thread, as long as threads are left for the SMs: 32768 x 1000 with 1, 4 and 8 pieces a thread 53, 28 and
     // 26 us, 4000 x 1000 with 1, 2 and 8 5.4, 4.5 and 6.2, 64 x 1000 1.8, 2.0 and 4.0.
@@ -715,10 +783,25 @@ cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, int sms, cuda
     const int64_t rows = kThreads >> a.lanes_log2;
     // long rows are cut where there are too few for every SM
     const int64_t blocks = (p.m + rows - 1) / rows, rounds = (pieces + kThreads * kFlight - 1) / (kThreads * kFlight);
-    const unsigned cut = (unsigned)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, 65535), 8ll * sms / blocks));
+    const unsigned cut = (unsigned)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rounds, 65535), 2ll * kCutRows * sms / blocks));
     void (*kernel)(const LogprobGradArgs) = p.type == EMTK_TYPE_F32   ? logprob_grad_kernel<EMTK_TYPE_F32>
                                             : p.type == EMTK_TYPE_F16 ? logprob_grad_kernel<EMTK_TYPE_F16>
                                                                       : logprob_grad_kernel<EMTK_TYPE_BF16>;
+    if (cut > 1 && a.dz == a.z) {  // a block would write while another of the row still reads: far rows' sums first
+        LogprobArgs f{};
+        f.z = a.z;
+        f.row_bytes = a.row_bytes;
+        f.m = p.m;
+        f.v = p.v;
+        f.k = a.k;
+        f.inverse_t = a.inverse_t;
+        f.far = p.lse;
+        a.sums = f.sums = nn->far_sums;
+        const cudaError_t e = p.type == EMTK_TYPE_F32   ? run_blocks<EMTK_TYPE_F32, false>(f, sms, s)
+                              : p.type == EMTK_TYPE_F16 ? run_blocks<EMTK_TYPE_F16, false>(f, sms, s)
+                                                        : run_blocks<EMTK_TYPE_BF16, false>(f, sms, s);
+        if (e != cudaSuccess) return e;
+    }
     return launch_pdl(kernel, dim3((unsigned)blocks, cut), dim3(kThreads), 0, s, a);
 }
 

@@ -633,6 +633,52 @@ def test_rows_of_two_gigabytes(lib, nn, dtype, v):
     near(dz[0, v - 1:], 1 - torch.full((1,), math.exp(3.0) / total, dtype=torch.float64, device="cuda"), dtype, 4 * E)
 
 
+@pytest.mark.parametrize("temperature", [1.0, 0.8, 0.01])
+@pytest.mark.parametrize("m,v", [(7, 5), (40, 33), (70, 500), (300, 600), (9, 2500), (7, 40000), (700, 4100), (3000, 1100)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "f32"])
+def test_gradient_of_logits_far_from_zero(lib, nn, m, v, temperature, dtype):
+    """Rows far from 0, of the type's least and largest values, and small temperatures: p is held as well as it is by the
+    row's own maximum and sum.  With T as fp32 has it, l' = (z - max) / T and l = l' - ln S: l' is off by 1.5 E |l'| <= 1.5 E |l|,
+    ln S by the v / 256 + 24 roundings of a sum of exponentials, 3 E for exp and 8 E where lse is used as it is
+    (up to 32), so p by (v / 256 + 48 + 4 |l|) E of itself; p = 0 beyond |l| = 104.  The entropy that is handed on is off by
+    such parts of its terms p and p l."""
+    t = float(np.float32(temperature))
+    g = gen(v)
+    low, high = torch.finfo(DT[dtype]).min, torch.finfo(DT[dtype]).max
+    rows = randn(g, 7, v)
+    rows[0] = low
+    rows[1] = low
+    rows[1, v // 2] = -math.inf
+    rows[2] += {"bf16": 100.0, "fp16": 1000.0, "f32": 1e5}[dtype]
+    rows[3] -= {"bf16": 100.0, "fp16": 1000.0, "f32": 1e5}[dtype]
+    rows[4] = high
+    rows[5] *= 4
+    rows[6, v - 1] = 40.0
+    z = Buf(m, v, DT[dtype], 1, 1, rows[torch.arange(m, device="cuda") % 7])
+    tokens = torch.randint(-1, v, (m,), generator=g, device="cuda").to(torch.int32)
+    dl, dh = randn(g, m), randn(g, m)
+    ent, lse = torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+    lib.emtk_logprobs(nn, z.t, entropy=ent, lse=lse, temperature=t)
+    l = torch.log_softmax(z.t.double() / t, 1)
+    p = l.exp()
+    l0 = torch.where(p > 0, l, 0.0).clamp_min(-1e4)
+    entropy = -(p * l0).sum(1, keepdim=True)
+    given = tokens >= 0
+    chosen = torch.zeros_like(l).scatter_(1, tokens.long().clamp(0)[:, None], given.double()[:, None])
+    a, e = (dl.double() * given)[:, None], dh.double()[:, None]
+    want = (a * (chosen - p) - e * p * (l0 + entropy)) / t
+    off = (v / 256 + 48 + 4 * l0.abs().clamp_max(104)) * E
+    off_h = (v / 256 + 48 + 4 * 104) * E * (1 + (p * l0.square()).sum(1, keepdim=True))
+    size = a.abs() * (chosen + p) + e.abs() * p * (l0.abs() + entropy + 1)
+    slack = (a.abs() * p * off + e.abs() * p * ((l0.abs() + entropy + 1) * off + off_h) + 4 * E * size) / t + 1e-33
+    dz = Buf(m, v, DT[dtype], 1, 1)
+    lib.emtk_logprobs_backward(nn, z.t, lse, dz.t, tokens=tokens, d_logprob=dl, entropy=ent, d_entropy=dh, temperature=t)
+    near(dz.t, want, dtype, slack, "d_logits")
+    assert dz.surroundings_untouched()
+    lib.emtk_logprobs_backward(nn, z.t, lse, z.t, tokens=tokens, d_logprob=dl, entropy=ent, d_entropy=dh, temperature=t)
+    assert torch.equal(z.t, dz.t) and z.surroundings_untouched()
+
+
 def test_logprobs_of_empty_sizes(lib, nn):
     lib.emtk_logprobs(nn, torch.empty(0, 5, device="cuda"), entropy=torch.empty(0, device="cuda"))
     lp, ent, lse = (torch.empty(3, device="cuda") for _ in range(3))
