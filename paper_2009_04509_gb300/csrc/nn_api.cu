@@ -672,7 +672,7 @@ emtk_status emtk_residual_norm_backward(emtk_nn *nn, const emtk_residual_norm_gr
     }
     if (copied) {
         copy.d = static_cast<uint8_t *>(copy.d) + reinterpret_cast<uintptr_t>(a.dy.d) % 16;
-        const cudaError_t e = launch_dropout((emtk_type)a.type, a.m, a.n, a.dy, copy, emtk_drop{}, nn->sm_count, s);  // of nothing
+        const cudaError_t e = launch_dropout((emtk_type)a.type, a.m, a.n, a.dy, copy, emtk_drop{}, nn->sm_count, s);  // of nothing: a copy to any rows
         if (e != cudaSuccess) return status_of(e);
         a.dy = copy;
     }

@@ -161,7 +161,8 @@ cudaError_t launch_gated_slope(emtk_type type, int act, int m, int f, const emtk
 cudaError_t launch_pack8(emtk_type type, int m, int k, const emtk_matrix &x, const emtk_matrix &q, int sms,
                          cudaStream_t s);
 // to = the values of from (a checkpoint, or a 16-bit matrix as it is), for up
-// to kMaxCopies matrices in one launch.
+// to kMaxCopies matrices in one launch.  A 16-bit matrix goes to rows on 16 bytes alone
+// (else cudaErrorInvalidValue); dropout of nothing copies one to any rows.
 constexpr int kMaxCopies = 4;
 struct Copy16 {
     emtk_matrix from, to;

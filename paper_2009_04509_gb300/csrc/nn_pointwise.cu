@@ -851,6 +851,7 @@ cudaError_t launch_copy16(emtk_type type, const Copy16 *copies, int n, int sms, 
         if (c.rows == 0 || c.cols == 0) continue;
         const Source from = source_of(c.from);
         const bool odd = !wide_matrix(c.to.d, 2 * c.to.ld, 16);  // a caller's values: the workspace's rows never are
+        if (odd && !from.scale) return cudaErrorInvalidValue;    // unpack_odd reads the scales
         const bool wide = from.scale && !odd && wide_source(from, c.cols);
         plans[jobs] = walk_plan(c.rows, (int64_t)c.cols + (odd ? kVec - 1 : 0), kVec, kThreads, false);
         blocks = std::max(blocks, plans[jobs].blocks(sms));

@@ -194,6 +194,41 @@ def test_dropout_refusals_without_device(lib, handle):
     assert call(None, 4, 16, 0, x, y, drop(), None) == emtk.EMTK_ERR_ARG
 
 
+COPY_DRIVER = r"""
+#include <cstdio>
+#include "nn_internal.h"
+int main() {
+    using namespace emtk;
+    static uint16_t room[256] __attribute__((aligned(16)));
+    for (int shift = 0; shift < 8; ++shift)
+        for (int ld : {16, 17}) {
+            const Copy16 copy = {{room, 16, nullptr, 0}, {room + 128 + shift, ld, nullptr, 0}, 4, 16};
+            if (shift == 0 && ld == 16) continue;  // a copy that there is
+            const cudaError_t e = launch_copy16(EMTK_TYPE_BF16, &copy, 1, 1, nullptr);
+            if (e != cudaErrorInvalidValue) return printf("%d elements off the grid, rows %d apart: %d\n", shift, ld, (int)e), 1;
+        }
+    return 0;
+}
+"""
+
+
+def test_copies_of_16_bits_to_rows_off_the_grid_are_refused(lib, tmp_path):
+    """Only a checkpoint is unpacked to rows off the 16-byte grid: that kernel reads the scales, which a 16-bit matrix has not.
+    The library's own launcher, in a program without a GPU's memory: it is to refuse before it launches."""
+    from paper_2009_04509_gb300 import build
+    cuda, obj = os.environ.get("CUDA_HOME", "/usr/local/cuda"), os.path.join(build.BUILD, "nn_pointwise.o")
+    if shutil.which("g++") is None or not os.path.exists(os.path.join(cuda, "include", "cuda.h")):
+        pytest.skip("no g++ or CUDA headers")
+    if not os.path.exists(obj):
+        build.build(force=True)
+    src, exe = tmp_path / "copy.cpp", tmp_path / "copy"
+    src.write_text(COPY_DRIVER)
+    subprocess.run(["g++", "-std=c++17", "-w", "-I", build.CSRC, "-I", os.path.join(cuda, "include"), str(src), obj, "-L", os.path.join(cuda, "lib64"),
+                    "-lcudart_static", "-ldl", "-lrt", "-lpthread", "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout
+
+
 def test_binding_refuses_tensors_of_another_device(monkeypatch):
     """A tensor of another GPU than the handle's is refused before the library sees its address, each argument alone.
     Stand-ins for the tensors and the library: no GPU is needed."""
