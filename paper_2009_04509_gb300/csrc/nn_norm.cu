@@ -148,7 +148,7 @@ struct Waits {  // of the kernels' bounded waits
 //   kSmall    several to a block (and to a warp, where they are short), a piece a thread, on the
 //             grid and of whole pieces
 //   kSmallAny the same, anywhere
-//   kBulk     a block goes from row to row, two pieces a thread: a row of each matrix is copied
+//   kBulk     (the gradients) a block goes from row to row, two pieces a thread: a row of each matrix is copied
 //             to shared memory, a row or two ahead, so that many rows are on their way
 //             without a register
 //   kBulkAny  the same, anywhere: in the aligned 16-byte pieces that it lies in, shifted into
@@ -167,7 +167,7 @@ struct RowIo {
     int tid, threads;
     bool last;  // the last piece is this thread's, or beyond the row
     bool live;  // false: a row that is not there, in a warp of rows that are
-    // kBulk
+    // kBulk; unset elsewhere
     uint8_t *stages;
     uint64_t *full;
     Guard guard;
@@ -175,14 +175,19 @@ struct RowIo {
     int stage = 0;
     bool ok = true;
 
-    __device__ __forceinline__ RowIo(const Inputs &inputs, uint8_t *shared, uint64_t *bars, uint32_t *abort_flag, const Waits &w)
-        : a(inputs), stages(shared), full(bars), guard{abort_flag, w.status, w.timeout_ns} {
+    __device__ __forceinline__ explicit RowIo(const Inputs &inputs) : a(inputs) {
         tid = threadIdx.x;
         threads = blockDim.x;
         row = KIND == kSmall || KIND == kSmallAny ? (int64_t)blockIdx.x * blockDim.y + threadIdx.y : (int64_t)blockIdx.x;
         last = column(C - 1) + kPiece > a.n;
         live = row < a.m;
         if (C == 1 && threads < 32) row = min(row, (int64_t)a.m - 1);  // its warp's exchanges need all lanes
+    }
+    // What kBulk has besides.
+    __device__ __forceinline__ RowIo(const Inputs &inputs, uint8_t *shared, uint64_t *bars, uint32_t *abort_flag, const Waits &w) : RowIo(inputs) {
+        stages = shared;
+        full = bars;
+        guard = {abort_flag, w.status, w.timeout_ns};
         if (is_bulk(KIND)) {
             if (tid == 0) {
                 for (int i = 0; i < kMostStages; ++i) mbar_init(smem_u32(full + i), 1);
@@ -375,52 +380,40 @@ struct SeamArgs {
 };
 
 template <bool F16, Kind KIND, int THREADS>
-__global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_constant__ SeamArgs a, const Waits waits) {
-    extern __shared__ __align__(128) uint8_t rows[];
+__global__ void __launch_bounds__(THREADS) residual_norm_kernel(const __grid_constant__ SeamArgs a) {
     __shared__ float buffer[2 * 4 * kMaxWarps];
-    __shared__ uint64_t full[kMostStages];
-    __shared__ uint32_t abort_flag;
     using Io = RowIo<F16, KIND, 2>;
     constexpr int C = Io::C;
-    Io io(a.in, rows, full, &abort_flag, waits);
+    const Io io(a.in);
     constexpr bool kGrouped = KIND == kSmall || KIND == kSmallAny;
     Reduction reduction{buffer + (kGrouped ? threadIdx.y * (io.threads / 32) * 4 : 0), io.tid, io.threads / 32, 0,
                         kGrouped ? min(32, io.threads) : 32, kGrouped};
     pdl_trigger();
     pdl_wait();
     if (io.row >= a.in.m) return;  // (a whole warp)
-    io.begin();
     const uint64_t offset = a.drop.below ? drop_offset(a.drop) : 0u;
-    do {
-        io.wait();
-        uint32_t wb[C][4], wr[C][4];
-        io.load(kInBlock, wb);
-        io.load(kInResidual, wr);
-        if (is_bulk(KIND)) {
-            __syncthreads();
-            io.release();
-        }
-        Eight v[C];
+    uint32_t wb[C][4], wr[C][4];
+    io.load(kInBlock, wb);
+    io.load(kInResidual, wr);
+    Eight v[C];
 #pragma unroll
-        for (int k = 0; k < C; ++k) v[k] = values8<F16>(wb[k]);
-        if (a.post.kind != EMTK_NORM_NONE) normalise<F16>(a.post, v, io, a.inverse_n, reduction);
-        const Param gate{a.gate.p ? a.gate.row((int)io.row / a.gate_every) : nullptr, 0, a.gate_vec};
+    for (int k = 0; k < C; ++k) v[k] = values8<F16>(wb[k]);
+    if (a.post.kind != EMTK_NORM_NONE) normalise<F16>(a.post, v, io, a.inverse_n, reduction);
+    const Param gate{a.gate.p ? a.gate.row((int)io.row / a.gate_every) : nullptr, 0, a.gate_vec};
 #pragma unroll
-        for (int k = 0; k < C; ++k) {
-            if (a.drop.below) dropped(a.drop, offset, (uint32_t)io.row, (uint32_t)(k * io.threads + io.tid), v[k]);
-            if (a.gate.p) v[k] = v[k] * io.param(gate, k);
-            const Eight r = values8<F16>(wr[k]);
+    for (int k = 0; k < C; ++k) {
+        if (a.drop.below) dropped(a.drop, offset, (uint32_t)io.row, (uint32_t)(k * io.threads + io.tid), v[k]);
+        if (a.gate.p) v[k] = v[k] * io.param(gate, k);
+        const Eight r = values8<F16>(wr[k]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[k].v[i] = fma2(r.v[i], both(a.scale), v[k].v[i]);
-            if (a.y.p) io.store(a.y, k, v[k]);
-        }
-        if (a.pre.kind != EMTK_NORM_NONE) {
-            normalise<F16>(a.pre, v, io, a.inverse_n, reduction);
+        for (int i = 0; i < 4; ++i) v[k].v[i] = fma2(r.v[i], both(a.scale), v[k].v[i]);
+        if (a.y.p) io.store(a.y, k, v[k]);
+    }
+    if (a.pre.kind != EMTK_NORM_NONE) {
+        normalise<F16>(a.pre, v, io, a.inverse_n, reduction);
 #pragma unroll
-            for (int k = 0; k < C; ++k) io.store(a.h, k, v[k]);
-        }
-    } while (io.next());
-    io.end();
+        for (int k = 0; k < C; ++k) io.store(a.h, k, v[k]);
+    }
 }
 
 // ---------------------------------------------------------------- gradients
@@ -822,17 +815,22 @@ Shape shape_of(int n, bool on_grid, bool bulk) {
     return {bulk ? (whole ? kBulk : kBulkAny) : whole ? kDirect : kDirectAny, ((all + 1) / 2 + 31) / 32 * 32, 1};
 }
 
-// Blocks of an SM at once, as far as registers and shared memory go.
+// The gradients' blocks of an SM at once, as far as registers and shared memory go.
 int blocks_of(const Shape &h, size_t shared, int registers) {
     return (int)std::max<size_t>(1, std::min<size_t>((size_t)65536 / (registers * h.threads), (size_t)222 * 1024 / (shared + 2560)));
 }
 
-template <typename Args>
-cudaError_t run_rows(void (*kernel)(const Args, const Waits), const Shape &h, int inputs, int registers, Args &a, const emtk_nn *nn, cudaStream_t s) {
+// The forward pass: a group of threads for each row.
+cudaError_t run_rows(void (*kernel)(const SeamArgs), const Shape &h, const SeamArgs &a, cudaStream_t s) {
+    const int64_t blocks = ((int64_t)a.in.m + h.groups - 1) / h.groups;
+    return launch_pdl(kernel, dim3((unsigned)blocks), dim3((unsigned)h.threads, (unsigned)h.groups), 0, s, a);
+}
+// The gradients.
+cudaError_t run_rows(void (*kernel)(const SeamGradArgs, const Waits), const Shape &h, int registers, SeamGradArgs &a, const emtk_nn *nn, cudaStream_t s) {
     int64_t blocks = ((int64_t)a.in.m + h.groups - 1) / h.groups;
     size_t shared = 0;
     if (is_bulk(h.kind)) {
-        const size_t row = (size_t)inputs * a.in.row_bytes;
+        const size_t row = (size_t)4 * a.in.row_bytes;
         a.in.stages = 2 * row <= 222 * 1024 ? 2 : 1;
         shared = a.in.stages * row;
         blocks = std::min<int64_t>(blocks, (int64_t)nn->sm_count * blocks_of(h, shared, registers));
@@ -841,32 +839,32 @@ cudaError_t run_rows(void (*kernel)(const Args, const Waits), const Shape &h, in
 }
 
 template <bool F16>
-cudaError_t run(SeamArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) {
+cudaError_t run(SeamArgs &a, const Shape &h, const emtk_nn *, cudaStream_t s) {
     switch (h.kind) {
-        case kSmall: return run_rows(residual_norm_kernel<F16, kSmall, 256>, h, 2, 64, a, nn, s);
-        case kSmallAny: return run_rows(residual_norm_kernel<F16, kSmallAny, 256>, h, 2, 64, a, nn, s);
+        case kSmall: return run_rows(residual_norm_kernel<F16, kSmall, 256>, h, a, s);
+        case kSmallAny: return run_rows(residual_norm_kernel<F16, kSmallAny, 256>, h, a, s);
         case kDirect:
             return run_rows(h.threads <= 256   ? residual_norm_kernel<F16, kDirect, 256>
                             : h.threads <= 512 ? residual_norm_kernel<F16, kDirect, 512>
-                                               : residual_norm_kernel<F16, kDirect, 1024>, h, 2, 64, a, nn, s);
+                                               : residual_norm_kernel<F16, kDirect, 1024>, h, a, s);
         default:
             return run_rows(h.threads <= 256   ? residual_norm_kernel<F16, kDirectAny, 256>
                             : h.threads <= 512 ? residual_norm_kernel<F16, kDirectAny, 512>
-                                               : residual_norm_kernel<F16, kDirectAny, 1024>, h, 2, 64, a, nn, s);
+                                               : residual_norm_kernel<F16, kDirectAny, 1024>, h, a, s);
     }
 }
 template <bool F16, Kind KIND>
 cudaError_t run_bulk(SeamGradArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) {
-    if (h.threads <= 256) return run_rows(residual_norm_grad_kernel<F16, KIND, 256, 3>, h, 4, 80, a, nn, s);
-    if (h.threads <= 384) return run_rows(residual_norm_grad_kernel<F16, KIND, 384, 2>, h, 4, 80, a, nn, s);
-    if (h.threads <= 512) return run_rows(residual_norm_grad_kernel<F16, KIND, 512, 1>, h, 4, 128, a, nn, s);
-    return run_rows(residual_norm_grad_kernel<F16, KIND, 1024, 1>, h, 4, 64, a, nn, s);
+    if (h.threads <= 256) return run_rows(residual_norm_grad_kernel<F16, KIND, 256, 3>, h, 80, a, nn, s);
+    if (h.threads <= 384) return run_rows(residual_norm_grad_kernel<F16, KIND, 384, 2>, h, 80, a, nn, s);
+    if (h.threads <= 512) return run_rows(residual_norm_grad_kernel<F16, KIND, 512, 1>, h, 128, a, nn, s);
+    return run_rows(residual_norm_grad_kernel<F16, KIND, 1024, 1>, h, 64, a, nn, s);
 }
 template <bool F16>
 cudaError_t run(SeamGradArgs &a, const Shape &h, const emtk_nn *nn, cudaStream_t s) {
     switch (h.kind) {
-        case kSmall: return run_rows(residual_norm_grad_kernel<F16, kSmall, 256, 3>, h, 4, 80, a, nn, s);
-        case kSmallAny: return run_rows(residual_norm_grad_kernel<F16, kSmallAny, 256, 3>, h, 4, 80, a, nn, s);
+        case kSmall: return run_rows(residual_norm_grad_kernel<F16, kSmall, 256, 3>, h, 80, a, nn, s);
+        case kSmallAny: return run_rows(residual_norm_grad_kernel<F16, kSmallAny, 256, 3>, h, 80, a, nn, s);
         case kBulk: return run_bulk<F16, kBulk>(a, h, nn, s);
         default: return run_bulk<F16, kBulkAny>(a, h, nn, s);
     }
@@ -922,7 +920,7 @@ cudaError_t init_norm_kernels() {
 
 cudaError_t launch_residual_norm(const emtk_residual_norm_args &p, const emtk_nn *nn, cudaStream_t s) {
     SeamArgs a{};
-    a.in = {{rows16_of(p.residual), rows16_of(p.block)}, p.m, p.n, bulk_row_bytes(p.n), 1};
+    a.in = {{rows16_of(p.residual), rows16_of(p.block)}, p.m, p.n, 0, 0};
     a.gate = rows16_of(p.gate);
     a.gate_vec = on_grid(p.gate, 2);
     a.y = rows16_of(p.y);

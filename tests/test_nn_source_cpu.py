@@ -40,6 +40,15 @@ def test_every_device_function_of_the_layers_is_called():
     assert [n for n in sorted(names) if len(re.findall(rf"\b{n}\b", text)) < 2] == []
 
 
+def test_no_copies_ahead_where_none_are_made():
+    """The forward norms' rows are loaded straight from memory: their kernel has no barriers, no shared rows, no bounded waits and
+    no loop over rows, and none of its kinds is that of the copies."""
+    src = _sources()["nn_norm.cu"]
+    kernel = src[src.index("residual_norm_kernel(const __grid_constant__"):src.index("// ---------------------------------------------------------------- gradients")]
+    assert re.findall(r"[Ww]aits|abort_flag|is_bulk|io\.(?:begin|wait|release|next|end)\b|extern __shared__", kernel) == []
+    assert re.findall(r"residual_norm_kernel<F16, (kBulk\w*)", src) == []
+
+
 def test_every_field_of_a_kernels_parameters_is_read():
     """A field of a structure that is passed to a kernel by value is read somewhere, not only set."""
     src = _sources()
