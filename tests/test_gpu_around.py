@@ -137,6 +137,22 @@ def test_dropout(lib, nn, i, size, dtype):
         assert torch.equal(before == 0, x.t.double() == 0) or p > 0
 
 
+@pytest.mark.parametrize("pad,shift", [(0, 0), (1, 3)])
+@pytest.mark.parametrize("m,n", [(30000, 333), (7001, 2048)])
+def test_dropout_of_many_pieces(lib, nn, m, n, pad, shift):
+    """More pieces than threads: every thread goes round its loop, on the grid and off it, apart and in place."""
+    x, y = Buf(m, n, torch.bfloat16, pad, shift, randn(gen(m), m, n)), Buf(m, n, torch.bfloat16, pad, shift)
+    x.t[x.t == 0] = 1.0
+    drop = lib.Drop(0.3, 5, 1 << 35)
+    lib.emtk_dropout(nn, x.t, y.t, drop)
+    d = factors(m, n, 0.3, 5, 1 << 35)
+    want = x.t.double() * d
+    near(y.t, want, "bf16", want.abs() * 2 * E)
+    assert torch.equal(y.t == 0, d == 0) and y.surroundings_untouched()
+    lib.emtk_dropout(nn, x.t, x.t, drop)
+    assert torch.equal(x.t, y.t) and x.surroundings_untouched()
+
+
 def test_dropped_values_are_zero_whatever_they_were(lib, nn):
     m, n = 40, 300
     x = torch.full((m, n), float("nan"), dtype=torch.float16, device="cuda")
@@ -335,6 +351,16 @@ def test_residual_norm_backward(lib, nn, i, dtype):
         lib.emtk_residual_norm_backward(nn, dy.t, opt(dh), y.t if c["pre"] else None, None, dy.t, None,
                                         **{k2: v2 for k2, v2 in shared.items() if k2 in ("pre", "scale")})
         assert torch.equal(dy.t, first[0]) and dy.surroundings_untouched()
+
+
+@pytest.mark.parametrize("post,pre,gate,every", [("layer", "rms", "vector", 1), ("rms", "layer", "rows", 7), (None, "layer", None, 1)])
+@pytest.mark.parametrize("m,n,pad,shift", [(2500, 2056, 0, 0), (2500, 2059, 1, 3), (400, 8200, 8, 0), (400, 8197, 0, 1), (333, 16384, 0, 0), (333, 16381, 0, 5)])
+def test_residual_norm_backward_of_many_rows(lib, nn, monkeypatch, m, n, pad, shift, post, pre, gate, every):
+    """More rows than blocks: a block goes from row to row through its stages, with two rows ahead or one."""
+    c = dict(norm_config(0), size=(m, n), pad=pad, shift=shift, out_pad=pad, out_shift=shift, post=post, pre=pre, gate=gate, every=every, p=0.2 if gate else 0.0,
+             scale=0.5, params="f32", weights=(1, 1), residual=True, dy=True, eps=1e-3)
+    monkeypatch.setitem(globals(), "norm_config", lambda i: c)
+    test_residual_norm_backward(lib, nn, 3, "bf16")
 
 
 @pytest.mark.parametrize("pads", [(0,) * 4, (1,) * 4, (3, 1, 0, 2), (1, 0, 0, 0)])
