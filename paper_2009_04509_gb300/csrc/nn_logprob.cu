@@ -173,8 +173,8 @@ __device__ __forceinline__ int place_of(uint64_t key) { return (int)~(uint32_t)k
 // lse is max / T + ln S rounded to fp32: off by up to half a step, and p = exp(z / T - lse) by so much of itself, 2^-20 up to
 // 32, where ordinary rows end.  Beyond, up to a row of the type's least values, whose lse holds nothing of ln S any more, the
 // gradient takes the row's maximum and S again: 8192 x 65536 in bf16 312 us of ordinary rows, 534 of such.  A row that is cut
-// among blocks and overwritten has its sums taken first, by the forward kernel, whose blocks leave ordinary rows at
-// once (1 x 131072 in place 2.7 us, 2.0 apart).  With its own code for such rows an ordinary element has no instruction more:
+// among blocks and overwritten has its sums taken first, by the forward kernel, a block to a row and so in the same order,
+// which leaves ordinary rows at once (1 x 131072 in place 2.7 us, 2.0 apart).  With its own code for such rows an ordinary element has no instruction more:
 // one for all took 345.
 constexpr float kFarLse = 32.f;
 __device__ __forceinline__ bool is_far(float lse) { return fabsf(lse) > kFarLse; }
@@ -483,10 +483,7 @@ __global__ void __launch_bounds__(kThreads) logprob_block_kernel(const __grid_co
     if (cluster > 1) cluster_arrive();  // it has started
     pdl_trigger();
     pdl_wait();
-    if (a.far && !is_far(a.far[row])) {  // all of the row's blocks leave
-        if (cluster > 1) cluster_wait();
-        return;
-    }
+    if (a.far && !is_far(a.far[row])) return;  // (without a cluster)
     const int token = a.tokens ? a.tokens[row] : -1;
     const float z = threadIdx.x == 0 ? token_logit<TYPE>(a, p, token) : 0.f;
     const Strip<TYPE> strip(p, a.v, threadIdx.x, kThreads, rank, cluster);
@@ -701,16 +698,6 @@ __global__ void __launch_bounds__(kThreads, 5) logprob_grad_kernel(const __grid_
 }
 
 template <int TYPE, bool TOP>
-cudaError_t run_blocks(const LogprobArgs &a, int sms, cudaStream_t s) {
-    const int pieces = a.v / Elem<TYPE>::kPer;
-    // blocks for every SM, each with a round of pieces at least
-    int cluster = 1;
-    while (cluster < kMostCluster && (int64_t)a.m * cluster < 2 * sms && pieces >= 2 * cluster * kThreads * kFlight) cluster *= 2;
-    if (cluster == 1)
-        return launch_pdl(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)a.m), dim3(kThreads), 0, s, a, cluster);
-    return launch_cluster(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)(a.m * cluster)), dim3(kThreads), 0, cluster, s, a, cluster);
-}
-template <int TYPE, bool TOP>
 cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
     const int pieces = a.v / Elem<TYPE>::kPer;
     // A few lanes to a row where rows are many: a warp waits for no other.  Lanes and a block to a row, the sums alone:
@@ -727,7 +714,12 @@ cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
         const int64_t rows = kThreads >> a.lanes_log2;
         return launch_pdl(logprob_lanes_kernel<TYPE, TOP>, dim3((unsigned)((a.m + rows - 1) / rows)), dim3(kThreads), 0, s, a);
     }
-    return run_blocks<TYPE, TOP>(a, sms, s);
+    // blocks for every SM, each with a round of pieces at least
+    int cluster = 1;
+    while (cluster < kMostCluster && (int64_t)a.m * cluster < 2 * sms && pieces >= 2 * cluster * kThreads * kFlight) cluster *= 2;
+    if (cluster == 1)
+        return launch_pdl(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)a.m), dim3(kThreads), 0, s, a, cluster);
+    return launch_cluster(logprob_block_kernel<TYPE, TOP>, dim3((unsigned)(a.m * cluster)), dim3(kThreads), 0, cluster, s, a, cluster);
 }
 template <int TYPE>
 cudaError_t run(LogprobArgs &a, int sms, cudaStream_t s) {
@@ -787,7 +779,7 @@ cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, const emtk_nn
     void (*kernel)(const LogprobGradArgs) = p.type == EMTK_TYPE_F32   ? logprob_grad_kernel<EMTK_TYPE_F32>
                                             : p.type == EMTK_TYPE_F16 ? logprob_grad_kernel<EMTK_TYPE_F16>
                                                                       : logprob_grad_kernel<EMTK_TYPE_BF16>;
-    if (cut > 1 && a.dz == a.z) {  // a block would write while another of the row still reads: far rows' sums first
+    if (cut > 1 && a.dz == a.z) {  // a block would write while another of the row still reads
         LogprobArgs f{};
         f.z = a.z;
         f.row_bytes = a.row_bytes;
@@ -797,9 +789,10 @@ cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, const emtk_nn
         f.inverse_t = a.inverse_t;
         f.far = p.lse;
         a.sums = f.sums = nn->far_sums;
-        const cudaError_t e = p.type == EMTK_TYPE_F32   ? run_blocks<EMTK_TYPE_F32, false>(f, sms, s)
-                              : p.type == EMTK_TYPE_F16 ? run_blocks<EMTK_TYPE_F16, false>(f, sms, s)
-                                                        : run_blocks<EMTK_TYPE_BF16, false>(f, sms, s);
+        void (*sums)(const LogprobArgs, int) = p.type == EMTK_TYPE_F32   ? logprob_block_kernel<EMTK_TYPE_F32, false>
+                                               : p.type == EMTK_TYPE_F16 ? logprob_block_kernel<EMTK_TYPE_F16, false>
+                                                                         : logprob_block_kernel<EMTK_TYPE_BF16, false>;
+        const cudaError_t e = launch_pdl(sums, dim3((unsigned)p.m), dim3(kThreads), 0, s, f, 1);
         if (e != cudaSuccess) return e;
     }
     return launch_pdl(kernel, dim3((unsigned)blocks, cut), dim3(kThreads), 0, s, a);

@@ -705,6 +705,23 @@ def test_gradient_of_logits_far_from_zero(lib, nn, m, v, temperature, dtype):
     assert torch.equal(z.t, dz.t) and z.surroundings_untouched()
 
 
+@pytest.mark.parametrize("m,v", [(1, 300007), (41, 102213), (600, 20000), (300, 2500)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradient_in_place_has_the_same_bits(lib, nn, m, v, dtype):
+    """Rows far from 0 among ordinary ones, cut among blocks or not: the same bits in the logits' place as apart."""
+    g = gen(m)
+    z = (randn(g, m, v) * 2 - 500.0 * (torch.arange(m, device="cuda") % 3 != 1)[:, None]).to(DT[dtype])
+    ent, lse, dl = torch.empty(m, device="cuda"), torch.empty(m, device="cuda"), randn(g, m)
+    tokens = torch.randint(0, v, (m,), generator=g, device="cuda").to(torch.int32)
+    lib.emtk_logprobs(nn, z, entropy=ent, lse=lse, temperature=0.7)
+    assert bool((lse[::3] < -32).all()) and bool((lse[1::3].abs() < 32).all())
+    dz = torch.empty_like(z)
+    args = dict(tokens=tokens, d_logprob=dl, entropy=ent, d_entropy=dl, temperature=0.7)
+    lib.emtk_logprobs_backward(nn, z, lse, dz, **args)
+    lib.emtk_logprobs_backward(nn, z, lse, z, **args)
+    assert torch.equal(z, dz)
+
+
 def test_logprobs_of_empty_sizes(lib, nn):
     lib.emtk_logprobs(nn, torch.empty(0, 5, device="cuda"), entropy=torch.empty(0, device="cuda"))
     lp, ent, lse = (torch.empty(3, device="cuda") for _ in range(3))
