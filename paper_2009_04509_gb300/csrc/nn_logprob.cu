@@ -358,9 +358,9 @@ __device__ __forceinline__ uint64_t ranked(uint64_t key, int rank, int which) {
     return has ? __shfl_sync(0xffffffffu, key, __ffs(has) - 1) : 0u;
 }
 
-// l of a logit, from the row's sums.
+// l of a logit, from the row's sums.  By halves: the type's least value less a large one may be beyond fp32 where l is not.
 __device__ __forceinline__ float logprob_of(float z, const Sums &x, float log_s, float inverse_t) {
-    return x.m == minus_infinity() && x.s == 0.f ? minus_infinity() : (z - x.m) * inverse_t - log_s;
+    return x.m == minus_infinity() && x.s == 0.f ? minus_infinity() : fmaf((0.5f * z - 0.5f * x.m) * inverse_t, 2.f, -log_s);
 }
 
 // A row's results; `z` is its token's logit.

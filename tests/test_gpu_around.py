@@ -722,6 +722,23 @@ def test_gradient_in_place_has_the_same_bits(lib, nn, m, v, dtype):
     assert torch.equal(z, dz)
 
 
+@pytest.mark.parametrize("v", [5, 700, 3000, 40000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logprobs_across_the_types_range(lib, nn, v, dtype):
+    """The type's least value beside its largest at a temperature that brings their distance into fp32: l is finite."""
+    top, t = torch.finfo(DT[dtype]).max, 20.0
+    z = torch.full((2, v), -top, dtype=DT[dtype], device="cuda")
+    z[:, 3] = top
+    z[1, 4] = top / 2
+    tokens = torch.tensor([1, 4], dtype=torch.int32, device="cuda")
+    lp, tl, ti = torch.empty(2, device="cuda"), torch.empty(2, 3, device="cuda"), torch.empty(2, 3, dtype=torch.int32, device="cuda")
+    lib.emtk_logprobs(nn, z, tokens, lp, top_logprob=tl, top_index=ti, temperature=t)
+    want = torch.log_softmax(z.double() / t, 1)
+    near(lp, want.gather(1, tokens.long()[:, None])[:, 0], "f32", 8 * E * float(top) / 10)
+    assert ti.tolist() == [[3, 0, 1], [3, 4, 0]]
+    near(tl, want.gather(1, ti.long()), "f32", 8 * E * want.gather(1, ti.long()).abs())
+
+
 def test_logprobs_of_empty_sizes(lib, nn):
     lib.emtk_logprobs(nn, torch.empty(0, 5, device="cuda"), entropy=torch.empty(0, device="cuda"))
     lp, ent, lse = (torch.empty(3, device="cuda") for _ in range(3))
