@@ -5,7 +5,7 @@
 //   l_j = (z_j - M) / T - ln S;   entropy = ln S - W / S;
 // when the maximum rises by d (in units of T), S becomes S exp(-d) and W exp(-d) (W - d S).
 // Two runs' triples join the same way.  HBM bounds large calls (one read of the logits;
-// the gradient one read and one write), the call small ones.  8192 x 65536 in bf16 179 us (6.0 TB/s,
+// the gradient one read and one write, two reads of rows far from 0), the call small ones.  8192 x 65536 in bf16 179 us (6.0 TB/s,
 // 0.88 of a copy's rate), its gradient 312 (6.9 TB/s, 1.01); one row of 131072 with its 8 largest
 // 8.3 us on a cluster of 8 blocks.  Two elements to an instruction took the first from 199 to 180 us.
 //
@@ -35,7 +35,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMostTop = 32, kMostCluster = 8;
-// Pieces of a thread in flight: 512 x 131072 with 2, 4 and 8 51, 34 and 30 us, 8192 x 65536 174, 179 and 188, its gradient 332, 323 and 366.
+// Pieces of a thread in flight: 512 x 131072 with 2, 4 and 8 42, 34 and 31 us, 8192 x 65536 192, 180 and 190, its gradient 324, 312 and 421.
 constexpr int kFlight = 4;
 
 constexpr float kFar = -1e4f;  // an exponent whose power is 0, in the place of -infinity where that would meet a 0
@@ -767,8 +767,8 @@ cudaError_t launch_logprobs_grad(const emtk_logprobs_grad_args &p, const emtk_nn
     a.k = kLog2E * a.inverse_t;
     const int sms = nn->sm_count;
     const int64_t pieces = std::max<int64_t>(1, (int64_t)p.v * elem / 16);
-    // Up to 8 pieces a thread, as long as threads are left for the SMs: 32768 x 1000 with 1, 4 and 8 pieces a thread 53, 28 and
-    // 26 us, 4000 x 1000 with 1, 2 and 8 5.4, 4.5 and 6.2, 64 x 1000 1.8, 2.0 and 4.0.
+    // Up to 8 pieces a thread, as long as threads are left for the SMs: 32768 x 1000 with 1, 4 and 8 pieces a thread 49, 25 and
+    // 23 us, 4000 x 1000 with 1, 2 and 8 5.3, 4.0 and 4.6, 64 x 1000 1.6, 1.8 and 2.8.
     int each = 1;
     while (each < 8 && p.m * pieces >= 2 * each * 1024ll * sms) each *= 2;
     while (a.lanes_log2 < 8 && ((int64_t)each << a.lanes_log2) < pieces) ++a.lanes_log2;

@@ -27,7 +27,7 @@
 // before it, which the forward pass kept.
 //
 // HBM bounds it: 8 bytes a value forward, 14 backward (16 bits, with o).  800 sequences of 1000
-// steps of 64 columns in bf16: 71 us forward (5.7 TB/s), 154 backward (4.7 TB/s; 159 registers leave 12
+// steps of 64 columns in bf16: 71 us forward (5.7 TB/s), 154 backward (4.7 TB/s; 142 registers leave 12
 // warps an SM, which wait for their own arithmetic); 20011 steps of 2048 in 4 sequences, as independent tiles, 104 and 195.
 #include <algorithm>
 
