@@ -1043,6 +1043,36 @@ def test_calls_in_a_graph_with_new_random_numbers(lib):
     lib.emtk_nn_destroy(nn)
 
 
+def test_gradients_of_logits_in_graphs(lib):
+    """Captured as a handle's first call, in the logits' place and apart, and replayed in turn over ordinary and far rows: as eager."""
+    nn, eager = lib.emtk_nn_create(), lib.emtk_nn_create()
+    m, v = 20, 30000
+    z, dz = torch.zeros(m, v, device="cuda"), torch.empty(m, v, device="cuda")
+    lse, dl, tokens = torch.zeros(m, device="cuda"), torch.ones(m, device="cuda"), torch.arange(m, dtype=torch.int32, device="cuda")
+    lib.emtk_logprobs_backward(eager, z, lse, dz, tokens=tokens, d_logprob=dl)  # kernels are loaded before a capture
+    lib.emtk_logprobs_backward(eager, z, lse, z, tokens=tokens, d_logprob=dl)
+    torch.cuda.synchronize()
+    graphs = []
+    for to in (dz, z):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            lib.emtk_logprobs_backward(nn, z, lse, to, tokens=tokens, d_logprob=dl)
+    for i, about in enumerate((0.0, 300.0, -1e6, 3e38)):
+        values = randn(gen(i), m, v) + about * (torch.arange(m, device="cuda") % 2)[:, None]
+        z.copy_(values)
+        lib.emtk_logprobs(eager, z, lse=lse)
+        want = torch.empty_like(z)
+        lib.emtk_logprobs_backward(eager, z, lse, want, tokens=tokens, d_logprob=dl)
+        for graph, out in zip(graphs, (dz, z)):
+            graph.replay()
+            assert torch.equal(out, want), (about, out is z)
+    torch.cuda.synchronize()
+    del graphs, graph
+    for h in (nn, eager):
+        assert lib.emtk_nn_check(h) == lib.EMTK_OK
+        lib.emtk_nn_destroy(h)
+
+
 def test_on_another_stream(lib):
     """Calls on a side stream, after work there that they must wait for."""
     nn = lib.emtk_nn_create()
